@@ -207,6 +207,71 @@ modse_status modse_layer_bwd_ext(const modse_desc* desc, int64_t T, const void* 
 modse_status modse_routing_stats(const modse_desc* desc, int64_t T, const modse_routing* routing,
                                  int32_t* slot_counts, float* summary, void* hip_stream);
 
+/* ---------------------------------------------------------------- the operators around the layer
+ * The norm in front of a layer and the log probabilities that a model of such
+ * layers is trained, scored and sampled by.  The conventions above hold; where
+ * infinities and NaN are defined, it is said.  An output may lie in the buffer of
+ * an input only where that is said.  Pointers need the alignment of their
+ * elements only, workspaces 16 bytes. */
+
+/* h = x + residual, y = gamma h / sqrt(mean(h^2) + eps) over the rows of
+ * [T, d_model] (d_model 1..16384, any value).  Sums and y are float32 and come
+ * from the unrounded h.
+ *   x, residual  [T, d_model] of `dtype`; residual may be NULL (h = x)
+ *   gamma        [d_model] of `dtype`
+ *   y, h         [T, d_model] of `dtype` out, either may be NULL; each may lie in the
+ *                buffer of x or of residual
+ *   rstd         [T] float32 out or NULL: 1 / sqrt(mean(h^2) + eps), for the backward pass
+ *   q, scale     y in 8 bits (e4m3: 4 exponent bits, bias 7, largest 448, no infinity),
+ *                [T, d_model], and float32 scales: y is about q * scale, scale = max|y| / 448
+ *                (2^-126 at least) of a row (group 0: [T]) or of every `group` columns
+ *                (group 32, 64 or 128: [T, ceil(d_model / group)]).  Both or neither. */
+modse_status modse_norm_fwd(int64_t T, int32_t d_model, modse_dtype dtype, const void* x, const void* residual,
+                            const void* gamma, float eps, void* y, void* h, float* rstd, void* q, float* scale,
+                            int32_t group, void* hip_stream);
+
+/* Bytes of workspace of modse_norm_bwd for T tokens or fewer. */
+modse_status modse_norm_bwd_workspace_size(int64_t T, int32_t d_model, modse_dtype dtype, size_t* bytes);
+
+/* Backward pass: h and rstd as modse_norm_fwd left them (h = x where there was no
+ * residual), dY the gradient of y, dH the gradient that arrives along h itself (or
+ * NULL).  dX [T, d_model] out = the gradient of h, which is that of x and of
+ * residual; it may lie in the buffer of dY, dH or h.  dgamma [d_model] float32,
+ * overwritten, or added to with accumulate = 1.  Sums run in an order that T and
+ * d_model alone fix.  T == 0 leaves dgamma as it is. */
+modse_status modse_norm_bwd(int64_t T, int32_t d_model, modse_dtype dtype, const void* h, const void* gamma,
+                            const float* rstd, const void* dY, const void* dH, void* dX, float* dgamma, int accumulate,
+                            void* ws, size_t ws_bytes, void* hip_stream);
+
+/* Log probabilities of given tokens, entropy and the most probable entries of
+ * softmax over rows of `vocab` logits.
+ *   logits     T rows of `dtype`, row t at element t * ld_logits (ld_logits >= vocab)
+ *   targets    [T] int32 or NULL.  Negative: no target, logp 0 and no gradient.  One
+ *              that is not below vocab: logp (and the row's gradient) NaN
+ *   logp       [T] float32 out, or NULL with targets: log softmax(logits)[target]
+ *   stats      [T, 2] float32 out or NULL, for the backward pass
+ *   entropy    [T] float32 out or NULL: -sum p log p
+ *   top        0..64: top_idx [T, top] int32 and top_logp [T, top] float32 out, by falling
+ *              logit, ties to the lower index
+ * A logit of -inf is a masked entry: probability 0, never among the top (-1 and
+ * -inf stand in the place of an entry that there is not), logp -inf where it is the
+ * target.  A row of nothing else has no distribution: logp -inf, entropy 0 and no
+ * gradient.  NaN or +inf in a row makes its logp and entropy NaN. */
+#define MODSE_LOGPROBS_MAX_TOP 64
+modse_status modse_logprobs_workspace_size(int64_t T, int32_t vocab, modse_dtype dtype, int32_t top, size_t* bytes);
+modse_status modse_logprobs_fwd(int64_t T, int32_t vocab, modse_dtype dtype, const void* logits, int64_t ld_logits,
+                                const int32_t* targets, float* logp, float* stats, float* entropy, int32_t top,
+                                int32_t* top_idx, float* top_logp, void* ws, size_t ws_bytes, void* hip_stream);
+
+/* Gradient of the logits of loss = sum_t d_logp[t] logp[t] + d_entropy[t]
+ * entropy[t].  stats, entropy as modse_logprobs_fwd left them (entropy may be
+ * NULL where d_entropy is).  targets and d_logp may be NULL together.  d_logits:
+ * rows of `dtype` at ld_d_logits, vocab columns of each are written; it may lie in
+ * the buffer of logits, with the same row distance. */
+modse_status modse_logprobs_bwd(int64_t T, int32_t vocab, modse_dtype dtype, const void* logits, int64_t ld_logits,
+                                const int32_t* targets, const float* stats, const float* entropy, const float* d_logp,
+                                const float* d_entropy, void* d_logits, int64_t ld_d_logits, void* hip_stream);
+
 /* Per-stage timing for benchmarks.  When enabled, modse_layer_fwd/bwd record
  * HIP events between their stages on the caller's stream; modse_stage_times
  * waits for the last recorded call and returns milliseconds per stage

@@ -69,7 +69,15 @@ def load_library():
     lib.modse_routing_stats.argtypes = [dp, i64, rp, vp, vp, vp]
     lib.modse_stage_timing_enable.argtypes = [C.c_int]
     lib.modse_stage_times.argtypes = [C.POINTER(C.c_float)]
-    for name in ("modse_workspace_size", "modse_saved_size", "modse_route", "modse_layer_fwd", "modse_layer_bwd",
+    i32, f32, szp = C.c_int32, C.c_float, C.POINTER(sz)
+    lib.modse_norm_fwd.argtypes = [i64, i32, C.c_int, vp, vp, vp, f32, vp, vp, vp, vp, vp, i32, vp]
+    lib.modse_norm_bwd_workspace_size.argtypes = [i64, i32, C.c_int, szp]
+    lib.modse_norm_bwd.argtypes = [i64, i32, C.c_int, vp, vp, vp, vp, vp, vp, vp, C.c_int, vp, sz, vp]
+    lib.modse_logprobs_workspace_size.argtypes = [i64, i32, C.c_int, i32, szp]
+    lib.modse_logprobs_fwd.argtypes = [i64, i32, C.c_int, vp, i64, vp, vp, vp, vp, i32, vp, vp, vp, sz, vp]
+    lib.modse_logprobs_bwd.argtypes = [i64, i32, C.c_int, vp, i64, vp, vp, vp, vp, vp, vp, i64, vp]
+    for name in ("modse_norm_fwd", "modse_norm_bwd_workspace_size", "modse_norm_bwd", "modse_logprobs_workspace_size",
+                 "modse_logprobs_fwd", "modse_logprobs_bwd", "modse_workspace_size", "modse_saved_size", "modse_route", "modse_layer_fwd", "modse_layer_bwd",
                  "modse_route_ext", "modse_layer_fwd_ext", "modse_layer_bwd_ext", "modse_routing_stats",
                  "modse_route_static",
                  "modse_stage_timing_enable", "modse_stage_times"):
@@ -287,3 +295,65 @@ def modse_stage_times() -> dict:
     buf = (C.c_float * len(STAGES))()
     _check(load_library().modse_stage_times(buf), "modse_stage_times", True)
     return {name: float(buf[i]) for i, name in enumerate(STAGES)}
+
+
+# ---------------------------------------------------------------- the operators around the layer (see include/modse.h)
+
+def modse_norm_fwd(T, d_model, dtype, x, residual, gamma, eps, y, h, rstd, q=None, scale=None, group=0, stream=None,
+                   raise_on_error=True) -> int:
+    code = load_library().modse_norm_fwd(T, d_model, _dtype_code(dtype), _ptr(x), _ptr(residual), _ptr(gamma), eps,
+                                         _ptr(y), _ptr(h), _ptr(rstd), _ptr(q), _ptr(scale), group, _stream(stream))
+    return _check(code, "modse_norm_fwd", raise_on_error)
+
+
+def modse_norm_bwd_workspace_size(T, d_model, dtype, raise_on_error=True):
+    out = C.c_size_t(0)
+    code = load_library().modse_norm_bwd_workspace_size(T, d_model, _dtype_code(dtype), C.byref(out))
+    _check(code, "modse_norm_bwd_workspace_size", raise_on_error)
+    return out.value if code == 0 else code
+
+
+def modse_norm_bwd(T, d_model, dtype, h, gamma, rstd, dY, dH, dX, dgamma, accumulate, ws, ws_bytes=None, stream=None,
+                   raise_on_error=True) -> int:
+    code = load_library().modse_norm_bwd(T, d_model, _dtype_code(dtype), _ptr(h), _ptr(gamma), _ptr(rstd), _ptr(dY),
+                                         _ptr(dH), _ptr(dX), _ptr(dgamma), int(bool(accumulate)), _ptr(ws),
+                                         _nbytes(ws, ws_bytes), _stream(stream))
+    return _check(code, "modse_norm_bwd", raise_on_error)
+
+
+def _row_distance(t, ld, vocab: int) -> int:
+    """Elements from one row to the next: as told, else the tensor's own stride (vocab for a raw pointer).  -1, which
+    the library refuses, for a tensor whose rows are not contiguous."""
+    if ld is not None:
+        return ld
+    if t is None or isinstance(t, int) or t.dim() < 2:
+        return vocab
+    rows, step = t.stride()[-2:]
+    if step != 1 and vocab > 1:
+        return -1
+    return max(rows, vocab) if t.shape[-2] <= 1 else rows
+
+
+def modse_logprobs_workspace_size(T, vocab, dtype, top=0, raise_on_error=True):
+    out = C.c_size_t(0)
+    code = load_library().modse_logprobs_workspace_size(T, vocab, _dtype_code(dtype), top, C.byref(out))
+    _check(code, "modse_logprobs_workspace_size", raise_on_error)
+    return out.value if code == 0 else code
+
+
+def modse_logprobs_fwd(T, vocab, dtype, logits, targets, logp, stats, entropy, top, top_idx, top_logp, ws, ws_bytes=None,
+                       ld_logits=None, stream=None, raise_on_error=True) -> int:
+    code = load_library().modse_logprobs_fwd(T, vocab, _dtype_code(dtype), _ptr(logits),
+                                             _row_distance(logits, ld_logits, vocab), _ptr(targets), _ptr(logp),
+                                             _ptr(stats), _ptr(entropy), top, _ptr(top_idx), _ptr(top_logp), _ptr(ws),
+                                             _nbytes(ws, ws_bytes), _stream(stream))
+    return _check(code, "modse_logprobs_fwd", raise_on_error)
+
+
+def modse_logprobs_bwd(T, vocab, dtype, logits, targets, stats, entropy, d_logp, d_entropy, d_logits, ld_logits=None,
+                       ld_d_logits=None, stream=None, raise_on_error=True) -> int:
+    code = load_library().modse_logprobs_bwd(T, vocab, _dtype_code(dtype), _ptr(logits),
+                                             _row_distance(logits, ld_logits, vocab), _ptr(targets), _ptr(stats),
+                                             _ptr(entropy), _ptr(d_logp), _ptr(d_entropy), _ptr(d_logits),
+                                             _row_distance(d_logits, ld_d_logits, vocab), _stream(stream))
+    return _check(code, "modse_logprobs_bwd", raise_on_error)

@@ -21,7 +21,8 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libmodse.so")
 RESOURCES = os.path.join(HERE, "kernel_resources.txt")
-SOURCES = ["api.hip", "route.hip", "gemm.hip"]
+SOURCES = ["api.hip", "route.hip", "gemm.hip", "ops_api.hip", "norm.hip", "logprobs.hip"]
+HOST_SOURCES = ("api.hip", "ops_api.hip")  # the C entry points
 # packed fp32 VALU ops are switched off for all device code (known to misbehave on the test machines)
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Xclang", "-target-feature", "-Xclang",
          "-packed-fp32-ops", "-I" + os.path.join(ROOT, "include"), "-I" + CSRC, "-Wno-unused-command-line-argument",
@@ -113,24 +114,23 @@ def build(extra_flags=(), verbose: bool = True) -> str:
 
 
 def build_host_sanitized(out_dir: str, driver_c: str) -> str:
-    """Builds, into out_dir, a copy of the library whose api.hip HOST code is instrumented with AddressSanitizer and
-    UndefinedBehaviorSanitizer (the device code and the other two objects are the ordinary ones: build() first),
-    and the C program driver_c against it with the same sanitizers.  Returns the path of the program."""
+    """Builds, into out_dir, a copy of the library whose entry points' HOST code is instrumented with AddressSanitizer
+    and UndefinedBehaviorSanitizer (the device code and the other objects are the ordinary ones: build() first), and the C program driver_c against it with the same sanitizers.  Returns the path of the program."""
     os.makedirs(out_dir, exist_ok=True)
     san = []
     for f in ("-fsanitize=address", "-fsanitize=undefined", "-fno-sanitize-recover=undefined", "-fno-omit-frame-pointer"):
         san += ["-Xarch_host", f]
     flags = [f for f in FLAGS if f != "-Rpass-analysis=kernel-resource-usage"]
-    obj = os.path.join(out_dir, "api_san.o")
+    objs = [os.path.join(out_dir, s.replace(".hip", "_san.o")) for s in HOST_SOURCES]
     lib = os.path.join(out_dir, "libmodse_hostsan.so")
     exe = os.path.join(out_dir, "host_abi_driver")
-    others = [os.path.join(CSRC, s.replace(".hip", ".o")) for s in SOURCES if s != "api.hip"]
+    others = [os.path.join(CSRC, s.replace(".hip", ".o")) for s in SOURCES if s not in HOST_SOURCES]
     for o in others:
         if not os.path.exists(o):
             raise FileNotFoundError(f"{o} not found: run build() first")
     steps = [
-        [_hipcc(), *flags, *san, "-g", "-c", os.path.join(CSRC, "api.hip"), "-o", obj],
-        [_hipcc(), "--offload-arch=gfx950", "-shared", "-fPIC", *san, obj, *others, "-o", lib],
+        *[[_hipcc(), *flags, *san, "-g", "-c", os.path.join(CSRC, s), "-o", o] for s, o in zip(HOST_SOURCES, objs)],
+        [_hipcc(), "--offload-arch=gfx950", "-shared", "-fPIC", *san, *objs, *others, "-o", lib],
         [_hipcc(), "-x", "c", "-std=c99", "-g", "-fsanitize=address", "-fsanitize=undefined",
          "-fno-sanitize-recover=undefined", "-I" + os.path.join(ROOT, "include"), driver_c, "-x", "none", lib,
          "-Wl,-rpath," + out_dir, "-o", exe],

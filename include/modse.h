@@ -208,11 +208,12 @@ modse_status modse_routing_stats(const modse_desc* desc, int64_t T, const modse_
                                  int32_t* slot_counts, float* summary, void* hip_stream);
 
 /* ---------------------------------------------------------------- the operators around the layer
- * The norm in front of a layer and the log probabilities that a model of such
- * layers is trained, scored and sampled by.  The conventions above hold; where
- * infinities and NaN are defined, it is said.  An output may lie in the buffer of
- * an input only where that is said.  Pointers need the alignment of their
- * elements only, workspaces 16 bytes. */
+ * The norm in front of a layer, the log probabilities that a model of such
+ * layers is trained, scored and sampled by, and the orthogonalised update of its
+ * expert matrices.  The conventions above hold; where infinities and NaN are
+ * defined, it is said.  An output may lie in the buffer of an input only where
+ * that is said.  Pointers need the alignment of their elements only, workspaces
+ * 16 bytes (modse_orthogonalize: 256). */
 
 /* h = x + residual, y = gamma h / sqrt(mean(h^2) + eps) over the rows of
  * [T, d_model] (d_model 1..16384, any value).  Sums and y are float32 and come
@@ -271,6 +272,27 @@ modse_status modse_logprobs_fwd(int64_t T, int32_t vocab, modse_dtype dtype, con
 modse_status modse_logprobs_bwd(int64_t T, int32_t vocab, modse_dtype dtype, const void* logits, int64_t ld_logits,
                                 const int32_t* targets, const float* stats, const float* entropy, const float* d_logp,
                                 const float* d_entropy, void* d_logits, int64_t ld_d_logits, void* hip_stream);
+
+/* A set of matrices, as the expert matrices of a layer are one.  Plain HOST
+ * struct with HOST arrays, read during the call only. */
+typedef struct {
+  int32_t n_matrices;     /* 0..4096 */
+  const int32_t* rows;    /* [n] each 1..65536 */
+  const int32_t* cols;    /* [n] each 1..65536 */
+  const float* const* G;  /* [n] DEVICE, row-major [rows, cols], float32 */
+  void* const* U;         /* [n] DEVICE, row-major [rows, cols], of `dtype`; U[i] may be G[i] (float32) */
+  modse_dtype dtype;
+} modse_matrix_set;
+
+/* U = X after `steps` (1..32) steps X <- a X + (b A + c A^2) X with A = X X^T, from
+ * X = G / (|G| + eps), |G| the Frobenius norm.  coeffs: HOST array [steps][3] of
+ * (a, b, c).  Products have the precision of float32 ones.  Coefficients that let a
+ * singular value of at most 1 grow beyond 2^40, or that are not finite, are
+ * unsupported.  A matrix of zeros stays one; NaN or infinities in a matrix make the
+ * whole of it NaN and leave the others alone. */
+modse_status modse_orthogonalize_workspace_size(const modse_matrix_set* set, size_t* bytes);
+modse_status modse_orthogonalize(const modse_matrix_set* set, const float* coeffs, int32_t steps, float eps, void* ws,
+                                 size_t ws_bytes, void* hip_stream);
 
 /* Per-stage timing for benchmarks.  When enabled, modse_layer_fwd/bwd record
  * HIP events between their stages on the caller's stream; modse_stage_times

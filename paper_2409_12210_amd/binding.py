@@ -32,6 +32,11 @@ class _Routing(C.Structure):
                 ("row_of", C.c_void_p), ("src_of", C.c_void_p), ("near_tie_count", C.c_void_p)]
 
 
+class _MatrixSet(C.Structure):
+    _fields_ = [("n_matrices", C.c_int32), ("rows", C.POINTER(C.c_int32)), ("cols", C.POINTER(C.c_int32)),
+                ("G", C.POINTER(C.c_void_p)), ("U", C.POINTER(C.c_void_p)), ("dtype", C.c_int)]
+
+
 class _GateExt(C.Structure):
     _fields_ = [("W_noise", C.c_void_p), ("gamma", C.c_void_p), ("eps", C.c_float), ("noise_pre", C.c_void_p),
                 ("aux_alpha", C.c_float), ("probs", C.c_void_p), ("aux_f", C.c_void_p), ("aux_P", C.c_void_p),
@@ -69,15 +74,18 @@ def load_library():
     lib.modse_routing_stats.argtypes = [dp, i64, rp, vp, vp, vp]
     lib.modse_stage_timing_enable.argtypes = [C.c_int]
     lib.modse_stage_times.argtypes = [C.POINTER(C.c_float)]
-    i32, f32, szp = C.c_int32, C.c_float, C.POINTER(sz)
+    i32, f32, szp, mp = C.c_int32, C.c_float, C.POINTER(sz), C.POINTER(_MatrixSet)
     lib.modse_norm_fwd.argtypes = [i64, i32, C.c_int, vp, vp, vp, f32, vp, vp, vp, vp, vp, i32, vp]
     lib.modse_norm_bwd_workspace_size.argtypes = [i64, i32, C.c_int, szp]
     lib.modse_norm_bwd.argtypes = [i64, i32, C.c_int, vp, vp, vp, vp, vp, vp, vp, C.c_int, vp, sz, vp]
     lib.modse_logprobs_workspace_size.argtypes = [i64, i32, C.c_int, i32, szp]
     lib.modse_logprobs_fwd.argtypes = [i64, i32, C.c_int, vp, i64, vp, vp, vp, vp, i32, vp, vp, vp, sz, vp]
+    lib.modse_orthogonalize_workspace_size.argtypes = [mp, szp]
+    lib.modse_orthogonalize.argtypes = [mp, C.POINTER(f32), i32, f32, vp, sz, vp]
     lib.modse_logprobs_bwd.argtypes = [i64, i32, C.c_int, vp, i64, vp, vp, vp, vp, vp, vp, i64, vp]
     for name in ("modse_norm_fwd", "modse_norm_bwd_workspace_size", "modse_norm_bwd", "modse_logprobs_workspace_size",
-                 "modse_logprobs_fwd", "modse_logprobs_bwd", "modse_workspace_size", "modse_saved_size", "modse_route", "modse_layer_fwd", "modse_layer_bwd",
+                 "modse_logprobs_fwd", "modse_logprobs_bwd", "modse_orthogonalize_workspace_size", "modse_orthogonalize",
+                 "modse_workspace_size", "modse_saved_size", "modse_route", "modse_layer_fwd", "modse_layer_bwd",
                  "modse_route_ext", "modse_layer_fwd_ext", "modse_layer_bwd_ext", "modse_routing_stats",
                  "modse_route_static",
                  "modse_stage_timing_enable", "modse_stage_times"):
@@ -357,3 +365,41 @@ def modse_logprobs_bwd(T, vocab, dtype, logits, targets, stats, entropy, d_logp,
                                              _ptr(entropy), _ptr(d_logp), _ptr(d_entropy), _ptr(d_logits),
                                              _row_distance(d_logits, ld_d_logits, vocab), _stream(stream))
     return _check(code, "modse_logprobs_bwd", raise_on_error)
+
+class MatrixSet:
+    """The matrices of modse_orthogonalize (see modse_matrix_set in include/modse.h): G, contiguous float32 device
+    tensors of two dimensions, and U, which receive the results, of the same shapes and all of one type (float32 or
+    bfloat16).  Keeps the tensors alive."""
+
+    def __init__(self, G, U, dtype=None):
+        self.G, self.U = list(G), list(U)
+        n = len(self.G)
+        if len(self.U) != n:
+            raise ValueError(f"{n} matrices, {len(self.U)} results")
+        for i, (g, u) in enumerate(zip(self.G, self.U)):
+            if g.dim() != 2 or g.shape != u.shape:
+                raise ValueError(f"matrix {i}: shapes {tuple(g.shape)} and {tuple(u.shape)}")
+            if not (g.is_contiguous() and u.is_contiguous()):
+                raise ValueError(f"matrix {i} is not contiguous")
+            if _dtype_code(g.dtype) != MODSE_F32 or u.dtype != self.U[0].dtype or u.device != g.device:
+                raise ValueError(f"matrix {i}: {g.dtype} on {g.device}, its result {u.dtype} on {u.device}")
+        code = _dtype_code(dtype if dtype is not None else self.U[0].dtype if n else "f32")
+        self._arrays = ((C.c_int32 * n)(*[g.shape[0] for g in self.G]), (C.c_int32 * n)(*[g.shape[1] for g in self.G]),
+                        (C.c_void_p * n)(*[g.data_ptr() for g in self.G]), (C.c_void_p * n)(*[u.data_ptr() for u in self.U]))
+        self._struct = _MatrixSet(n, *self._arrays, code)
+
+
+def modse_orthogonalize_workspace_size(matrices: MatrixSet, raise_on_error=True):
+    out = C.c_size_t(0)
+    code = load_library().modse_orthogonalize_workspace_size(C.byref(matrices._struct), C.byref(out))
+    _check(code, "modse_orthogonalize_workspace_size", raise_on_error)
+    return out.value if code == 0 else code
+
+
+def modse_orthogonalize(matrices: MatrixSet, coeffs, eps, ws, ws_bytes=None, stream=None, raise_on_error=True) -> int:
+    flat = [float(v) for abc in coeffs for v in abc]
+    if len(flat) != 3 * len(coeffs):
+        raise ValueError("coeffs: (a, b, c) for every step")
+    code = load_library().modse_orthogonalize(C.byref(matrices._struct), (C.c_float * len(flat))(*flat), len(coeffs), eps,
+                                              _ptr(ws), _nbytes(ws, ws_bytes), _stream(stream))
+    return _check(code, "modse_orthogonalize", raise_on_error)

@@ -21,7 +21,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libmodse.so")
 RESOURCES = os.path.join(HERE, "kernel_resources.txt")
-SOURCES = ["api.hip", "route.hip", "gemm.hip", "ops_api.hip", "norm.hip", "logprobs.hip"]
+SOURCES = ["api.hip", "route.hip", "gemm.hip", "ops_api.hip", "norm.hip", "logprobs.hip", "ortho.hip"]
 HOST_SOURCES = ("api.hip", "ops_api.hip")  # the C entry points
 # packed fp32 VALU ops are switched off for all device code (known to misbehave on the test machines)
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Xclang", "-target-feature", "-Xclang",

@@ -1,4 +1,4 @@
-// Internal declarations of the operators around the layer: norm, log probabilities (gfx950 only).
+// Internal declarations of the operators around the layer: norm and log probabilities (gfx950 only).
 #pragma once
 #include "common.h"
 

@@ -4,6 +4,7 @@
 #include <cstring>
 
 #include "ops.h"
+#include "ortho.h"
 
 namespace {
 modse_status check_dtype(const modse_dtype& dtype) {
@@ -11,6 +12,12 @@ modse_status check_dtype(const modse_dtype& dtype) {
   static_assert(sizeof(modse_dtype) == sizeof(int32_t), "enumeration stored as a 32-bit integer");
   std::memcpy(&bits, &dtype, sizeof bits);
   return bits == (int32_t)MODSE_F32 || bits == (int32_t)MODSE_BF16 ? MODSE_OK : MODSE_ERR_UNSUPPORTED;
+}
+modse_status check_set(const modse_matrix_set* set) {
+  if (!set || set->n_matrices < 0) return MODSE_ERR_INVALID_ARG;
+  if (check_dtype(set->dtype) != MODSE_OK || set->n_matrices > 4096) return MODSE_ERR_UNSUPPORTED;
+  if (set->n_matrices && (!set->rows || !set->cols)) return MODSE_ERR_INVALID_ARG;
+  return MODSE_OK;
 }
 bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
 modse_status hip_status(hipError_t e) { return e == hipSuccess ? MODSE_OK : MODSE_ERR_HIP; }
@@ -24,8 +31,8 @@ modse_status check_norm(int64_t T, int32_t d, const modse_dtype& dtype) {
 modse_status check_logprobs(int64_t T, int32_t vocab, const modse_dtype& dtype, int32_t top) {
   if (T < 0 || vocab < 1 || top < 0) return MODSE_ERR_INVALID_ARG;
   if (check_dtype(dtype) != MODSE_OK || top > MODSE_LOGPROBS_MAX_TOP) return MODSE_ERR_UNSUPPORTED;
-  // (blocks of a launch: at most one for every 2048 entries or row)
-  if (vocab > 1 << 30 || T >= MAX_ROWS || T * ((vocab + 2047) / 2048) >= MAX_ROWS) return MODSE_ERR_UNSUPPORTED;
+  // (a launch has fewer than 2^32 threads, 256 of them for a row, or for 8192 of its entries)
+  if (vocab > 1 << 30 || T >= 1 << 24 || T * ((vocab + 8191) / 8192) >= 1 << 24) return MODSE_ERR_UNSUPPORTED;
   return MODSE_OK;
 }
 struct LogprobsLayout {
@@ -121,6 +128,38 @@ modse_status modse_logprobs_bwd(int64_t T, int32_t vocab, modse_dtype dtype, con
     return MODSE_ERR_INVALID_ARG;
   const LogprobsBwdArgs a = {logits, ld_logits, targets, stats, entropy, d_logp, d_entropy, d_logits, ld_d_logits, T, vocab};
   return hip_status(launch_logprobs_bwd(dtype, a, static_cast<hipStream_t>(hip_stream)));
+}
+
+modse_status modse_orthogonalize_workspace_size(const modse_matrix_set* set, size_t* bytes) {
+  if (!bytes) return MODSE_ERR_INVALID_ARG;
+  modse_status st = check_set(set);
+  if (st != MODSE_OK) return st;
+  OrthoLayout w;
+  if ((st = ortho_layout(set, w)) != MODSE_OK) return st;
+  *bytes = w.total;
+  return MODSE_OK;
+}
+
+modse_status modse_orthogonalize(const modse_matrix_set* set, const float* coeffs, int32_t steps, float eps, void* ws,
+                                 size_t ws_bytes, void* hip_stream) {
+  using namespace modse_ortho;
+  modse_status st = check_set(set);
+  if (st != MODSE_OK) return st;
+  if (!coeffs || steps < 1 || !(eps >= 0.f) || std::isinf(eps)) return MODSE_ERR_INVALID_ARG;
+  if (steps > MAX_STEPS) return MODSE_ERR_UNSUPPORTED;
+  double bound = 1;  // of singular values
+  for (int i = 0; i < steps; ++i) {
+    bound = quintic_bound(coeffs[3 * i], coeffs[3 * i + 1], coeffs[3 * i + 2], bound);
+    if (!(bound <= 0x1p40)) return MODSE_ERR_UNSUPPORTED;  // (NaN too)
+  }
+  OrthoLayout w;
+  if ((st = ortho_layout(set, w)) != MODSE_OK) return st;
+  if (set->n_matrices == 0) return MODSE_OK;
+  if (!set->G || !set->U || !ws || reinterpret_cast<uintptr_t>(ws) % 256) return MODSE_ERR_INVALID_ARG;
+  for (int i = 0; i < set->n_matrices; ++i)
+    if (!set->G[i] || !set->U[i]) return MODSE_ERR_INVALID_ARG;
+  if (ws_bytes < w.total) return MODSE_ERR_WORKSPACE;
+  return hip_status(launch_orthogonalize(set, w, coeffs, steps, eps, static_cast<char*>(ws), static_cast<hipStream_t>(hip_stream)));
 }
 
 }  // extern "C"

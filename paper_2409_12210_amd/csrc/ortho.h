@@ -1,0 +1,64 @@
+// What the orthogonalised update's entry point and its kernels share.
+#pragma once
+#include <math.h>
+
+#include "common.h"
+
+namespace modse_ortho {
+
+constexpr int MAX_STEPS = 32;
+constexpr int PAD = 128;  // rows and columns of what is stored are padded to this with zeros: no kernel has edges to look at
+
+enum OpKind : int32_t {
+  OP_GRAM,    // A = X X^T
+  OP_SQUARE,  // R = b A + c A A
+  OP_UPDATE,  // X = a X + R X, into the other buffer
+};
+// square matrices of a matrix's workspace
+enum Slot { SLOT_A, SLOT_R, N_SLOTS };
+
+// the largest |a s + b s^3 + c s^5| for 0 <= s <= top
+__host__ __device__ inline double quintic_bound(double a, double b, double c, double top) {
+  auto at = [=](double u) { return fabs((a + (b + c * u) * u) * sqrt(u)); };
+  double most = at(top * top);
+  auto candidate = [&](double u) {
+    if (u > 0 && u < top * top && at(u) > most) most = at(u);
+  };
+  // zeros of the derivative: a + 3 b u + 5 c u^2 = 0, u = s^2
+  if (c != 0) {
+    const double disc = 9 * b * b - 20 * a * c;
+    if (disc >= 0) {
+      candidate((-3 * b + sqrt(disc)) / (10 * c));
+      candidate((-3 * b - sqrt(disc)) / (10 * c));
+    }
+  } else if (b != 0) {
+    candidate(-a / (3 * b));
+  }
+  return most;
+}
+
+// One matrix of the set, in device memory.
+struct alignas(128) Mat {
+  const float* G;
+  void* U;
+  char* X[2];     // [mp, np] stored pairs
+  char* slot;     // N_SLOTS matrices [mp, mp] of them
+  int32_t rows, cols;
+  int32_t m, n;   // the shorter and the longer side: a tall matrix is stored transposed
+  int32_t mp, np;
+  int32_t square_tile, update_tile;  // its first tiles in the launches' lists
+  int32_t part, parts;               // its partial sums of squares
+};
+struct Factors {
+  float product, first;  // of a product, and of the matrix that is added to it
+};
+
+}  // namespace modse_ortho
+
+struct OrthoLayout {
+  size_t mats, bounds, factors, squares, sums, square_map, update_map, data, total;
+  int32_t square_tiles, update_tiles, parts;
+};
+modse_status ortho_layout(const modse_matrix_set* set, OrthoLayout& w);
+hipError_t launch_orthogonalize(const modse_matrix_set* set, const OrthoLayout& w, const float* coeffs, int steps, float eps, char* ws,
+                                hipStream_t s);

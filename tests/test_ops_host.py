@@ -46,7 +46,7 @@ def logprobs_fwd(T=4, V=5000, dtype="f32", logits=P, ld=None, targets=P, logp=P,
 
 @pytest.mark.parametrize("over,code", [
     (dict(T=-1), INVALID), (dict(V=0), INVALID), (dict(top=-1), INVALID), (dict(top=65), UNSUPPORTED),
-    (dict(V=(1 << 30) + 1), UNSUPPORTED), (dict(T=1 << 31), UNSUPPORTED), (dict(T=1 << 22, V=1 << 21), UNSUPPORTED),
+    (dict(V=(1 << 30) + 1), UNSUPPORTED), (dict(T=1 << 31), UNSUPPORTED), (dict(T=1 << 24, V=9), UNSUPPORTED), (dict(T=1 << 22, V=32000), UNSUPPORTED),
     (dict(dtype="fp16"), UNSUPPORTED), (dict(logits=None), INVALID), (dict(ld=4999), INVALID), (dict(targets=None), INVALID),
     (dict(logp=None), INVALID), (dict(top_idx=None), INVALID), (dict(top_logp=None), INVALID),
     (dict(targets=None, logp=None, stats=None, entropy=None, top=0), INVALID), (dict(ws=None), INVALID),
@@ -101,3 +101,59 @@ def test_workspaces_serve_fewer_rows_and_refuse_what_the_call_refuses():
     assert m.modse_norm_bwd_workspace_size(1, 0, "bf16", raise_on_error=False) == INVALID
     with pytest.raises(m.ModseError):
         m.modse_norm_bwd_workspace_size(-1, 64, "bf16")
+
+
+# ---------------------------------------------------------------- orthogonalised update
+COEFFS = [(3.4445, -4.7750, 2.0315)] * 5
+
+
+def matrix_set(shapes=((4, 6), (200, 64)), dtype="f32", n=None, G=None):
+    """A set of invented device pointers: what the library gets to see of tensors."""
+    import ctypes as C
+
+    from paper_2409_12210_amd.binding import _MatrixSet, _dtype_code
+    s = object.__new__(m.MatrixSet)
+    k = len(shapes)
+    s._arrays = ((C.c_int32 * k)(*[r for r, _ in shapes]), (C.c_int32 * k)(*[c for _, c in shapes]),
+                 (C.c_void_p * k)(*([P] * k if G is None else G)), (C.c_void_p * k)(*[P] * k))
+    s._struct = _MatrixSet(k if n is None else n, *s._arrays, _dtype_code(dtype))
+    return s
+
+
+def ortho(s=None, coeffs=COEFFS, eps=1e-7, ws=P, ws_bytes=1 << 40):
+    return m.modse_orthogonalize(s if s is not None else matrix_set(), coeffs, eps, ws, ws_bytes, **NO)
+
+
+@pytest.mark.parametrize("over,code", [
+    (dict(shapes=((0, 4),)), INVALID), (dict(shapes=((4, -1),)), INVALID), (dict(shapes=((65537, 2),)), UNSUPPORTED),
+    (dict(dtype="fp8"), UNSUPPORTED), (dict(n=-1), INVALID), (dict(n=4097), UNSUPPORTED), (dict(shapes=()), OK),
+    (dict(shapes=((65536, 65536),) * 64), UNSUPPORTED),
+])
+def test_orthogonalize_refuses_sets(over, code):
+    s = matrix_set(**over)
+    got = m.modse_orthogonalize_workspace_size(s, raise_on_error=False)
+    assert got == (0 if code == OK else code)
+    assert ortho(s) == code
+
+
+@pytest.mark.parametrize("over,code", [
+    (dict(coeffs=[]), INVALID), (dict(coeffs=COEFFS * 7), UNSUPPORTED), (dict(eps=-1.0), INVALID), (dict(eps=float("nan")), INVALID),
+    (dict(coeffs=[(float("inf"), 0, 0)]), UNSUPPORTED), (dict(coeffs=[(float("nan"), 0, 0)]), UNSUPPORTED),
+    (dict(coeffs=[(1e9, 0.0, 0.0)] * 5), UNSUPPORTED), (dict(ws=None), INVALID), (dict(ws=P + 16), INVALID),
+    (dict(ws_bytes=1000), WORKSPACE), (dict(s=matrix_set(G=[P, None])), INVALID),
+])
+def test_orthogonalize_refuses_arguments(over, code):
+    assert ortho(**over) == code
+
+
+def test_matrix_sets_refuse_what_the_library_could_not_see():
+    g, u = torch.zeros((4, 6)), torch.zeros((4, 6))
+    for G, U in (([g], []), ([g], [u.t()]), ([g[0]], [u[0]]), ([g[:, ::2]], [u[:, ::2]]), ([g.bfloat16()], [u]),
+                 ([g, g], [u, u.bfloat16()])):
+        with pytest.raises(ValueError):
+            m.MatrixSet(G, U)
+    with pytest.raises(ValueError):
+        m.modse_orthogonalize(matrix_set(), [(1.0, 2.0)], 1e-7, P, 1 << 30, stream=0)
+    assert m.MatrixSet([g], [u.bfloat16()])._struct.dtype == 1 and m.MatrixSet([], [])._struct.n_matrices == 0
+    a, b = (m.modse_orthogonalize_workspace_size(matrix_set(((2048, k),))) for k in (512, 1024))
+    assert 0 < a < b

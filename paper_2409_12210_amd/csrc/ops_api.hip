@@ -135,7 +135,7 @@ modse_status modse_orthogonalize_workspace_size(const modse_matrix_set* set, siz
   modse_status st = check_set(set);
   if (st != MODSE_OK) return st;
   OrthoLayout w;
-  if ((st = ortho_layout(set, w)) != MODSE_OK) return st;
+  if ((st = ortho_layout(set, nullptr, 0, w)) != MODSE_OK) return st;
   *bytes = w.total;
   return MODSE_OK;
 }
@@ -153,13 +153,13 @@ modse_status modse_orthogonalize(const modse_matrix_set* set, const float* coeff
     if (!(bound <= 0x1p40)) return MODSE_ERR_UNSUPPORTED;  // (NaN too)
   }
   OrthoLayout w;
-  if ((st = ortho_layout(set, w)) != MODSE_OK) return st;
+  if ((st = ortho_layout(set, coeffs, steps, w)) != MODSE_OK) return st;
   if (set->n_matrices == 0) return MODSE_OK;
   if (!set->G || !set->U || !ws || reinterpret_cast<uintptr_t>(ws) % 256) return MODSE_ERR_INVALID_ARG;
   for (int i = 0; i < set->n_matrices; ++i)
     if (!set->G[i] || !set->U[i]) return MODSE_ERR_INVALID_ARG;
   if (ws_bytes < w.total) return MODSE_ERR_WORKSPACE;
-  return hip_status(launch_orthogonalize(set, w, coeffs, steps, eps, static_cast<char*>(ws), static_cast<hipStream_t>(hip_stream)));
+  return hip_status(launch_orthogonalize(set, w, coeffs, eps, static_cast<char*>(ws), static_cast<hipStream_t>(hip_stream)));
 }
 
 }  // extern "C"

@@ -9,13 +9,18 @@ namespace modse_ortho {
 constexpr int MAX_STEPS = 32;
 constexpr int PAD = 128;  // rows and columns of what is stored are padded to this with zeros: no kernel has edges to look at
 
-enum OpKind : int32_t {
-  OP_GRAM,    // A = X X^T
-  OP_SQUARE,  // R = b A + c A A
-  OP_UPDATE,  // X = a X + R X, into the other buffer
-};
-// square matrices of a matrix's workspace
-enum Slot { SLOT_A, SLOT_R, N_SLOTS };
+// the largest |a + b s^2 + c s^4| for 0 <= s <= top
+inline double ratio_bound(double a, double b, double c, double top) {
+  auto at = [=](double u) { return fabs(a + (b + c * u) * u); };
+  double most = at(0) > at(top * top) ? at(0) : at(top * top);
+  const double u = c != 0 ? -b / (2 * c) : 0;
+  if (u > 0 && u < top * top && at(u) > most) most = at(u);
+  return most;
+}
+
+// Square matrices of a matrix's workspace: A and the next A of a group of steps, R = b A + c A A likewise, Q the product of the
+// steps' polynomials so far (twice), S = a A + R A on the way to the next A.
+enum Slot { SLOT_A, SLOT_R, SLOT_A2, SLOT_R2, SLOT_Q, SLOT_S, N_SLOTS };
 
 // the largest |a s + b s^3 + c s^5| for 0 <= s <= top
 __host__ __device__ inline double quintic_bound(double a, double b, double c, double top) {
@@ -42,15 +47,16 @@ struct alignas(128) Mat {
   const float* G;
   void* U;
   char* X[2];     // [mp, np] stored pairs
-  char* slot;     // N_SLOTS matrices [mp, mp] of them
+  char* slot;     // matrices [mp, mp] of them
   int32_t rows, cols;
   int32_t m, n;   // the shorter and the longer side: a tall matrix is stored transposed
   int32_t mp, np;
   int32_t square_tile, update_tile;  // its first tiles in the launches' lists
   int32_t part, parts;               // its partial sums of squares
 };
+// of a product, and of the matrices that are added to it
 struct Factors {
-  float product, first;  // of a product, and of the matrix that is added to it
+  float product, first, second;
 };
 
 }  // namespace modse_ortho
@@ -58,7 +64,10 @@ struct Factors {
 struct OrthoLayout {
   size_t mats, bounds, factors, squares, sums, square_map, update_map, data, total;
   int32_t square_tiles, update_tiles, parts;
+  int32_t tile, n_slots;
+  int32_t group[modse_ortho::MAX_STEPS];  // steps of every group of them
+  int32_t n_groups;
 };
-modse_status ortho_layout(const modse_matrix_set* set, OrthoLayout& w);
-hipError_t launch_orthogonalize(const modse_matrix_set* set, const OrthoLayout& w, const float* coeffs, int steps, float eps, char* ws,
-                                hipStream_t s);
+// coeffs == null: a layout that serves any steps
+modse_status ortho_layout(const modse_matrix_set* set, const float* coeffs, int steps, OrthoLayout& w);
+hipError_t launch_orthogonalize(const modse_matrix_set* set, const OrthoLayout& w, const float* coeffs, float eps, char* ws, hipStream_t s);

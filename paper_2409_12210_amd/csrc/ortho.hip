@@ -9,6 +9,13 @@
 // CPU, and measured: errors against float64 as those of float32 products (1.3e-6 and 1.4e-6 after five steps).
 //
 // Storage: rows of blocks of 32 values, 64 bytes of hi and then 64 of lo, so that a cache line feeds one step of a product.
+//
+// Squares are symmetric: only tiles on and below the diagonal are computed, and written twice.
+//
+// Groups of steps.  p(A) X for several steps in a row needs X only at its ends: with R_i = b A_i + c A_i^2 and P_i = a_i I + R_i,
+// A_(i+1) = P_i A_i P_i and X_g = P_(g-1) ... P_0 X, all of whose factors are m x m, symmetric and commute.  In units of m^3
+// (n = r m, squares at half price) a group of g steps costs 3 r + 4 g - 3 where single steps cost g (3 r + 1).  What a rounding
+// puts into A grows by up to a^2 in every A_(i+1), so groups are short: ortho_layout.
 #include "gemm_bf16_util.h"
 #include "ops.h"
 #include "ortho.h"
@@ -98,19 +105,19 @@ __device__ inline double store_scale(double bound) {
   return ldexp(1.0, 15 - e);
 }
 
-// What is known of a matrix on its way through the steps.
+// What is known of a matrix on its way through the steps: bounds of singular values, and the powers of two that go with what is stored.
 struct Bound {
-  double x;              // singular values of the present X are at most this
-  double in_x, in_a;     // the factors that X and A are stored with
-  double start;          // G's
-  float out;             // 1 / in_x, of the result
+  double x, q;                    // of the present X (in a group: of what X would be), of Q
+  double in_x, in_a, in_r, in_q;  // X, A, R, Q as stored
+  double start;                   // G's factor
+  float out;                      // 1 / in_x, of the result
   float pad;
 };
 
 // One block per matrix: the norm, the factor of the first product, the matrix's part of the tile lists.
 __global__ __launch_bounds__(256) void ortho_prepare_kernel(const Mat* __restrict__ table, const double* __restrict__ sums, float eps,
                                                             Bound* __restrict__ bounds, Factors* __restrict__ gram,
-                                                            int32_t* __restrict__ square_map, int32_t* __restrict__ update_map) {
+                                                            int tile, int32_t* __restrict__ square_map, int32_t* __restrict__ update_map) {
   __shared__ double s[4];
   const Mat& m = table[blockIdx.x];
   double v = 0;
@@ -118,8 +125,8 @@ __global__ __launch_bounds__(256) void ortho_prepare_kernel(const Mat* __restric
   for (int b = 32; b; b >>= 1) v += __shfl_xor(v, b, 64);
   if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = v;
   __syncthreads();
-  const int mt = m.mp / PAD, nt = m.np / PAD;
-  for (int i = threadIdx.x; i < mt * mt; i += 256) square_map[m.square_tile + i] = blockIdx.x;
+  const int mt = (m.m + tile - 1) / tile, nt = (m.n + tile - 1) / tile;
+  for (int i = threadIdx.x; i < mt * (mt + 1) / 2; i += 256) square_map[m.square_tile + i] = blockIdx.x;
   for (int i = threadIdx.x; i < mt * nt; i += 256) update_map[m.update_tile + i] = blockIdx.x;
   if (threadIdx.x != 0) return;
   const double norm = sqrt((s[0] + s[1]) + (s[2] + s[3]));
@@ -130,36 +137,61 @@ __global__ __launch_bounds__(256) void ortho_prepare_kernel(const Mat* __restric
   b.in_x = store_scale(b.x);
   b.in_a = store_scale(b.x * b.x);
   b.start = inv * b.in_x;
-  b.out = 0.f;
-  b.pad = 0.f;
+  b.q = b.in_r = b.in_q = 0;
+  b.out = b.pad = 0.f;
   bounds[blockIdx.x] = b;
-  gram[blockIdx.x] = {(float)(b.in_a / (b.in_x * b.in_x)), 0.f};
+  gram[blockIdx.x] = {(float)(b.in_a / (b.in_x * b.in_x)), 0.f, 0.f};
 }
 
-// One wave per matrix, behind every A = X X^T: the largest singular value of X is at most the root of A's Frobenius norm, which
-// is what the factors of the step's other products and of the next A go by.  (Bounds that come from the polynomials alone lag
-// behind values that shrink, and what is stored loses bits.)
-__global__ __launch_bounds__(64) void ortho_factors_kernel(const Mat* __restrict__ table, const float* __restrict__ squares, float a, float b, float c,
-                                                           Bound* __restrict__ bounds, Factors* __restrict__ square, Factors* __restrict__ update,
-                                                           Factors* __restrict__ gram) {
-  const Mat& m = table[blockIdx.x];
-  const int mt = m.mp / PAD;
+// One wave per matrix, behind every A: the largest singular value of X is at most the root of A's Frobenius norm, which is what
+// the factors of the step's other products and of the next A go by.  (Bounds that come from the polynomials alone lag behind
+// values that shrink, and what is stored loses bits.)
+struct StepArgs {
+  float a, b, c;
+  float q;  // a's of the group's earlier steps, multiplied
+  int32_t first, last;
+  // of R = b A + c A A; of Q = a Q + q R + R Q; of S = a A + R A; of the next A = a S + R S; of X = q a X + Q X; of A = X X^T
+  Factors *square, *join, *half, *next, *update, *gram;
+};
+__global__ __launch_bounds__(64) void ortho_factors_kernel(const Mat* __restrict__ table, const float* __restrict__ squares, int tile,
+                                                           Bound* __restrict__ bounds, StepArgs f) {
+  const int w = blockIdx.x;
+  const Mat& m = table[w];
+  const int mt = (m.m + tile - 1) / tile, tiles = mt * (mt + 1) / 2;
   double v = 0;
-  for (int i = threadIdx.x; i < mt * mt; i += 64) v += squares[m.square_tile + i];
+  for (int i = threadIdx.x; i < tiles; i += 64) v += squares[m.square_tile + i];
   for (int k = 32; k; k >>= 1) v += __shfl_xor(v, k, 64);
   if (threadIdx.x != 0) return;
-  Bound t = bounds[blockIdx.x];
+  Bound t = bounds[w];
+  const double a = f.a, b = f.b, c = f.c, qa = f.first ? a : f.q * a;
   t.x = fmin(t.x, sqrt(sqrt(v) / t.in_a) * 1.01);
-  const double x2 = t.x * t.x, in_r = store_scale(fabs(b) * x2 + fabs(c) * x2 * x2);
-  square[blockIdx.x] = {(float)(c * in_r / (t.in_a * t.in_a)), (float)(b * in_r / t.in_a)};
-  t.x = quintic_bound(a, b, c, t.x) * 1.01;
-  const double next = store_scale(t.x);
-  update[blockIdx.x] = {(float)(next / (in_r * t.in_x)), (float)(a * next / t.in_x)};
-  t.in_x = next;
-  t.in_a = store_scale(t.x * t.x);
-  t.out = (float)(1 / next);
-  gram[blockIdx.x] = {(float)(t.in_a / (next * next)), 0.f};
-  bounds[blockIdx.x] = t;
+  const double x2 = t.x * t.x, r = fabs(b) * x2 + fabs(c) * x2 * x2, x = quintic_bound(a, b, c, t.x) * 1.01;
+  t.in_r = store_scale(r);
+  f.square[w] = {(float)(c * t.in_r / (t.in_a * t.in_a)), (float)(b * t.in_r / t.in_a), 0.f};
+  if (f.first) {
+    t.q = r;
+    t.in_q = t.in_r;
+  } else {
+    t.q = fabs(a) * t.q + fabs((double)f.q) * r + r * t.q;
+    const double in_q = store_scale(t.q);
+    f.join[w] = {(float)(in_q / (t.in_r * t.in_q)), (float)(a * in_q / t.in_q), (float)(f.q * in_q / t.in_r)};
+    t.in_q = in_q;
+  }
+  if (f.last) {
+    const double in_x = store_scale(x);
+    f.update[w] = {(float)(in_x / (t.in_q * t.in_x)), (float)(qa * in_x / t.in_x), 0.f};
+    t.in_x = in_x;
+    t.in_a = store_scale(x * x);
+    t.out = (float)(1 / in_x);
+    f.gram[w] = {(float)(t.in_a / (in_x * in_x)), 0.f, 0.f};
+  } else {
+    const double in_s = store_scale(t.x * x), in_a = store_scale(x * x);
+    f.half[w] = {(float)(in_s / (t.in_r * t.in_a)), (float)(a * in_s / t.in_a), 0.f};
+    f.next[w] = {(float)(in_a / (t.in_r * in_s)), (float)(a * in_a / in_s), 0.f};
+    t.in_a = in_a;
+  }
+  t.x = x;
+  bounds[w] = t;
 }
 
 __device__ __forceinline__ void store_pair(char* p, const float (&v)[4]) {  // four values of a block
@@ -226,205 +258,273 @@ __global__ __launch_bounds__(256) void ortho_start_kernel(const Mat* __restrict_
 }
 
 // ---------------------------------------------------------------- products
-// C = first E + product P Q over 128 x 128 tiles, four waves of 64 x 64 each.
-//   SQUARES: C, E, P and Q are [mp, mp] slots (P = Q = X for A = X X^T, then K = n and there is no E); Q is symmetric or
-//            transposed, so both operands are read along K
-//   else:    P = R [mp, mp] along K, Q = X [mp, np] across it, E = X, C the other X or, in the last step, U (OUT)
+// C = product P Q + first E + second F over TILE x TILE tiles, four waves, a quarter of the tile each.
+//   SQUARES: C, E, F are [mp, mp] slots, and so are P and Q (symmetric), or both are X (A = X X^T, K = n): operands along K
+//   else:    P is a slot along K, Q = X [mp, np] across it, E = X, C the other X or, in the last step, U (OUT)
+//
+// A step is 32 of K: a panel row is 64 bytes of hi and 64 of lo, and every fragment feeds two or one of the three products: 96
+// matrix instructions of 16 x 16 x 32 cycles' worth per 32 KiB of panels, half as many loads per instruction as a plain 16-bit
+// product of this tile has.  Two workgroups share a CU (TILE 128, two stages of panels), so that one multiplies while the other
+// waits.  Sets with few tiles take TILE 64 and four stages: there is nothing else on the CU then, and a step lasts as long as
+// its loads unless they are under way early.
 enum Out { OUT_PAIRS, OUT_F32, OUT_BF16 };
-constexpr int BK = 32;               // a row of a panel: 64 bytes of hi, 64 of lo
-constexpr int PANEL = PAD * 128;     // bytes
-constexpr int JOIN = 16;             // steps that are summed in one register
+constexpr int BK = 32;
+constexpr int JOIN = 16;  // steps that are summed in one register
+constexpr int RUN = 16;   // neighbouring tiles that an XCD gets, of every 8 * RUN
+struct SquareOp {
+  const Factors* factors;
+  int32_t p, q, e, f, c;  // slots; p < 0: X, e and f < 0: none
+  int32_t sum;            // the squares of C are summed
+};
 struct ProductArgs {
   const Mat* table;
-  const Factors* factors;
-  const Bound* bounds;
-  float* squares;  // sums of the squares of A's tiles, as stored
   const int32_t* map;
-  OpKind kind;
-  int32_t x;  // X[x] is the present one
+  SquareOp op[2];         // blockIdx.y
+  const Bound* bounds;
+  float* squares;         // sums of the squares of a result's tiles, as stored
+  int32_t x;              // X[x] is the present one
+  int32_t tiles;
 };
 
-template <bool SQUARES, Out OUT>
+template <int TILE, int STAGES, bool SQUARES, Out OUT>
 __global__ __launch_bounds__(256, 2) void ortho_product_kernel(ProductArgs a) {
-  __shared__ __align__(1024) char s_ring[4 * PANEL];
+  constexpr int PANEL = TILE * 128, UNITS = TILE / 32;  // bytes of a panel; its 1 KiB units per wave
+  constexpr int W = TILE / 2, NB = W / 16;              // a wave's part: NB x NB blocks of 16 x 16
+  constexpr int RING = STAGES * 2 * PANEL;
+  static_assert(RING >= TILE * TILE * 4, "the result's tile fits the ring");
+  __shared__ __align__(1024) char s_ring[RING];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave >> 1, wn = wave & 1;
-  const int which = uniform_int(a.map[blockIdx.x]);
+  // (workgroups go to the XCDs in turn)
+  const int tile = ((int)(blockIdx.x / 8) / RUN * 8 + (int)(blockIdx.x % 8)) * RUN + (int)(blockIdx.x / 8) % RUN;
+  if (tile >= a.tiles) return;
+  const SquareOp& op = a.op[SQUARES ? blockIdx.y : 0];
+  const int which = uniform_int(a.map[tile]);
   const Mat& m = a.table[which];
   const int mp = m.mp, np = m.np;
   const size_t slot = (size_t)mp * mp * 4;
-  const bool gram = SQUARES && a.kind == OP_GRAM;
-  const int local = blockIdx.x - (SQUARES ? m.square_tile : m.update_tile);
-  const int nt = (SQUARES ? mp : np) / PAD;
-  const int m0 = local / nt * PAD, n0 = local % nt * PAD;
+  const bool gram = SQUARES && op.p < 0;
+  int mt, nt;
+  if constexpr (SQUARES) {  // row by row of the triangle
+    const int t = tile - m.square_tile;
+    mt = (int)((sqrtf(8.f * t + 1.f) - 1.f) * 0.5f);
+    while ((mt + 1) * (mt + 2) / 2 <= t) ++mt;
+    while (mt * (mt + 1) / 2 > t) --mt;
+    mt = uniform_int(mt);
+    nt = uniform_int(t - mt * (mt + 1) / 2);
+  } else {  // columns of eight tiles
+    const int t = tile - m.update_tile, rows = (m.m + TILE - 1) / TILE, cols = (m.n + TILE - 1) / TILE;
+    const int group = t / (8 * cols), height = min(8, rows - group * 8), in = t - group * 8 * cols;
+    mt = uniform_int(group * 8 + in % height);
+    nt = uniform_int(in / height);
+  }
+  const int m0 = mt * TILE, n0 = nt * TILE;
   const int K = gram ? m.n : m.m, steps = (K + BK - 1) / BK;
   const char* const X = m.X[a.x];
   const int ldp = (gram ? np : mp) * 4, ldq = (gram || !SQUARES ? np : mp) * 4;  // bytes
-  const char* const P = gram ? X : SQUARES ? m.slot + SLOT_A * slot : m.slot + SLOT_R * slot;
-  const char* const Q = gram || !SQUARES ? X : m.slot + SLOT_A * slot;
+  const char* const P = gram ? X : m.slot + op.p * slot;
+  const char* const Q = gram || !SQUARES ? X : m.slot + op.q * slot;
 
-  // ---- loads: units of 1 KiB, four of each panel per wave, landing swizzled (16-byte chunks of a row XOR-ed)
-  uint32_t offp[4], offq[4];
+  // ---- loads: units of 1 KiB, landing swizzled (16-byte chunks of a row XOR-ed)
+  uint32_t offp[UNITS], offq[UNITS];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int u = wave * 4 + i;
+  for (int i = 0; i < UNITS; ++i) {
+    const int u = wave * UNITS + i;
     const int r = u * 8 + (lane >> 3), c = (lane & 7) ^ ((r >> 1) & 7);
     offp[i] = r * ldp + c * 16;
     if (SQUARES) {
       offq[i] = r * ldq + c * 16;
     } else {
-      const int k = u * 2 + (lane >> 5);
-      offq[i] = k * ldq + ((lane & 31) ^ (4 * (k & 3))) * 16;
+      constexpr int CHUNKS = TILE / 4;  // of a row of K
+      const int k = u * (64 / CHUNKS) + lane / CHUNKS;
+      offq[i] = k * ldq + ((lane % CHUNKS) ^ (4 * (k & 3) + 2 * (k >> 3 & 1))) * 16;
     }
   }
   const char* p = P + (size_t)m0 * ldp;
-  const char* q = SQUARES ? Q + (size_t)n0 * ldq : Q + n0 * 4;
+  const char* q = SQUARES ? Q + (size_t)n0 * ldq : Q + (size_t)n0 * 4;
   const size_t q_step = SQUARES ? 128 : (size_t)BK * ldq;
   const uint32_t lds = __builtin_amdgcn_readfirstlane(lds_address(s_ring));
   auto issue = [&](int stage) {
-    const uint32_t dst = lds + stage * 2 * PANEL + wave * 4096;
+    const uint32_t dst = lds + stage * 2 * PANEL + wave * (UNITS * 1024);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < UNITS; ++i) {
       dma_b128_s(p, offp[i], dst + i * 1024);
       dma_b128_s(q, offq[i], dst + PANEL + i * 1024);
     }
     p += 128;
     q += q_step;
   };
-  // ---- fragments: 32 rows, slice kk of 16 K, hi (part 0) or lo (1)
-  const int khalf = lane >> 5, lsw = (lane >> 1) & 7;
-  auto along = [&](const char* panel, int row, int kk, int part) {
-    return *reinterpret_cast<const half8*>(panel + (row + (lane & 31)) * 128 + (((part * 4 + kk * 2 + khalf) ^ lsw) << 4));
+  // ---- fragments: 16 rows, 8 K per lane from 8 (lane >> 4) on, hi (part 0) or lo (1)
+  const int kq = lane >> 4, l16 = lane & 15;
+  auto along = [&](const char* panel, int row, int part) {
+    return *reinterpret_cast<const half8*>(panel + (row + l16) * 128 + (((part * 4 + kq) ^ ((l16 >> 1) & 7)) << 4));
   };
-  auto across = [&](const char* panel, int col, int kk, int part) -> half8 {
+  auto across = [&](const char* panel, int col, int part) -> half8 {
+    // lane 16 kq + s reads 8 bytes at row 8 kq + h + (s >> 2) of K, columns col + 4 (s & 3) on, and gets four K of column col + s
     typedef short s16x4 __attribute__((ext_vector_type(4)));
     typedef short s16x8 __attribute__((ext_vector_type(8)));
     typedef __attribute__((address_space(3))) s16x4* lds_s16x4_ptr;
-    const int blk = lane >> 4, sl = lane & 15, kq = sl >> 2;
-    const int c16 = (col >> 5) * 8 + part * 4 + (blk & 1) * 2 + ((sl & 3) >> 1);
-    const char* const at = panel + (kk * 16 + (blk >> 1) * 8 + kq) * 512 + ((c16 ^ (4 * kq)) << 4) + (sl & 1) * 8;
+    const int r = l16 >> 2, c16 = (col >> 5) * 8 + part * 4 + (col >> 4 & 1) * 2 + ((l16 & 3) >> 1);
+    const char* const at = panel + (kq * 8 + r) * (TILE * 4) + ((c16 ^ (4 * r + 2 * (kq & 1))) << 4) + (l16 & 1) * 8;
     const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(at));
-    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(at + 4 * 512));
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(at + 4 * (TILE * 4)));
     const s16x8 v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
     return __builtin_bit_cast(half8, v);
   };
-  f32x16 total[2][2], acc[2][2];
+  f32x4 total[NB][NB], acc[NB][NB];
   // acc joins total and starts again.  (A sum of K terms of one sign in one register is off by up to K / 16 * 3 roundings, the
   // diagonal of X X^T at K = 3000 by 1e-6; in parts of 512 it is as good as one of 512.)
   auto join = [&](bool first) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < NB; ++i)
 #pragma unroll
-      for (int j = 0; j < 2; ++j)
+      for (int j = 0; j < NB; ++j)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
+        for (int r = 0; r < 4; ++r) {
           total[i][j][r] = first ? 0.f : total[i][j][r] + acc[i][j][r];
           acc[i][j][r] = 0.f;
         }
   };
   join(true);
 
-  issue(0);
+#pragma unroll
+  for (int i = 0; i < STAGES - 1; ++i)
+    if (i < steps) issue(i);
+  int stage = 0;
 #pragma unroll 1
   for (int g = 0; g < steps; ++g) {
-    __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt(0) lgkmcnt(0): this step's panels are there, the last one's have been read
+    // this step's panels are there (those of the next STAGES - 2 may be on their way) and the last one's have been read
+    constexpr int YOUNGER = (STAGES - 2) * 2 * UNITS;
+    static_assert(YOUNGER < 16, "low bits of the vmcnt field");
+    if (YOUNGER > 0 && g + STAGES - 2 < steps) __builtin_amdgcn_s_waitcnt(0x0070 | YOUNGER);
+    else __builtin_amdgcn_s_waitcnt(0x0070);
     asm volatile("" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    if (g + 1 < steps) issue((g + 1) & 1);
-    const char* const pp = s_ring + (g & 1) * 2 * PANEL;
+    if (g + STAGES - 1 < steps) issue(stage == 0 ? STAGES - 1 : stage - 1);
+    const char* const pp = s_ring + stage * 2 * PANEL;
     const char* const pq = pp + PANEL;
+    stage = stage + 1 == STAGES ? 0 : stage + 1;
+    half8 fp[NB][2], fq[NB][2];
 #pragma unroll
-    for (int kk = 0; kk < 2; ++kk) {
-      half8 fp[2][2], fq[2][2];
+    for (int i = 0; i < NB; ++i)
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
+      for (int part = 0; part < 2; ++part) {
+        fp[i][part] = along(pp, wm * W + i * 16, part);
+        fq[i][part] = SQUARES ? along(pq, wn * W + i * 16, part) : across(pq, wn * W + i * 16, part);
+      }
+    // (Q's fragment is the first operand: a lane then holds four neighbouring columns of C.  The blocks are walked to and fro.)
 #pragma unroll
-        for (int part = 0; part < 2; ++part) {
-          fp[i][part] = along(pp, wm * 64 + i * 32, kk, part);
-          fq[i][part] = SQUARES ? along(pq, wn * 64 + i * 32, kk, part) : across(pq, wn * 64 + i * 32, kk, part);
+    for (int t = 0; t < 3; ++t)
+#pragma unroll
+      for (int i = 0; i < NB; ++i)
+#pragma unroll
+        for (int jj = 0; jj < NB; ++jj) {
+          const int j = i % 2 ? NB - 1 - jj : jj;
+          acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fq[j][t == 0], fp[i][t == 1], acc[i][j], 0, 0, 0);
         }
-      // (Q's fragment is the first operand: a lane then holds four neighbouring columns of C)
-#pragma unroll
-      for (int t = 0; t < 3; ++t)
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-          for (int j = 0; j < 2; ++j)
-            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(fq[j][t == 0], fp[i][t == 1], acc[i][j], 0, 0, 0);
-    }
     if (g % JOIN == JOIN - 1) join(false);
   }
   join(false);
 
-  // ---- result: a lane holds row (lane & 31) and columns 8 b + 4 (lane >> 5) + 0..3, b = 0..3, of every 32 x 32 block
-  const Factors f = a.factors[which];
-  const char* const E = gram ? nullptr : SQUARES ? m.slot + SLOT_A * slot : X;
+  // ---- result: a lane holds row l16 and columns 4 kq + 0..3 of every block
+  const Factors f = op.factors[which];
+  const char* const E = SQUARES ? (op.e >= 0 ? m.slot + op.e * slot : nullptr) : X;
+  const char* const F = SQUARES && op.f >= 0 ? m.slot + op.f * slot : nullptr;
   const int ldc = (SQUARES ? mp : np) * 4;
-  char* const C = SQUARES ? m.slot + (gram ? SLOT_A : SLOT_R) * slot : m.X[1 - a.x];
-  const float out = OUT == OUT_PAIRS ? 1.f : a.bounds[which].out;
-  const bool tall = m.rows > m.cols;
+  char* const C = SQUARES ? m.slot + op.c * slot : m.X[1 - a.x];
+  const bool mirror = SQUARES && mt != nt;
   float sum = 0.f;
+  if (mirror) __syncthreads();  // the ring has been read
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
+  for (int i = 0; i < NB; ++i)
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const int row = m0 + wm * 64 + i * 32 + (lane & 31);
+    for (int j = 0; j < NB; ++j) {
+      const int r = wm * W + i * 16 + l16, c = wn * W + j * 16 + kq * 4;
+      const size_t byte = (size_t)(m0 + r) * ldc + pair_byte(n0 + c);
+      float v[4] = {0.f, 0.f, 0.f, 0.f}, w[4] = {0.f, 0.f, 0.f, 0.f};
+      if (E) load_pair(E + byte, v);
+      if (F) load_pair(F + byte, w);
 #pragma unroll
-      for (int b = 0; b < 4; ++b) {
-        const int col = n0 + wn * 64 + j * 32 + b * 8 + khalf * 4;
-        const size_t byte = (size_t)row * ldc + pair_byte(col);
-        float v[4] = {0.f, 0.f, 0.f, 0.f};
-        if (E) load_pair(E + byte, v);
+      for (int k = 0; k < 4; ++k) v[k] = (f.first * v[k] + f.second * w[k]) + f.product * total[i][j][k];
+      if constexpr (OUT == OUT_PAIRS) {
+        store_pair(C + byte, v);
+        if constexpr (SQUARES) {
+          if (op.sum)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) v[r] = f.first * v[r] + f.product * total[i][j][b * 4 + r];
-        if constexpr (OUT == OUT_PAIRS) {
-          store_pair(C + byte, v);
-          if (SQUARES)
+            for (int k = 0; k < 4; ++k) sum += v[k] * v[k];
+          if (mirror)  // transposed, chunks of four rows XOR-ed with the column, so that the lanes meet all banks
 #pragma unroll
-            for (int r = 0; r < 4; ++r) sum += v[r] * v[r];
-        } else {
-          typedef std::conditional_t<OUT == OUT_F32, float, bf16_t> T;
-          T* const U = static_cast<T*>(m.U);
-          if (row < m.m) {
+            for (int k = 0; k < 4; ++k)
+              *reinterpret_cast<float*>(s_ring + (c + k) * (TILE * 4) + (((r >> 2) ^ (c & (TILE / 4 - 1))) << 4) + (r & 3) * 4) = v[k];
+        }
+      } else {
+        typedef std::conditional_t<OUT == OUT_F32, float, bf16_t> T;
+        T* const U = static_cast<T*>(m.U);
+        const float out = a.bounds[which].out;
+        const bool tall = m.rows > m.cols;
+        if (m0 + r < m.m) {
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
-              if (col + r < m.n) U[tall ? (int64_t)(col + r) * m.cols + row : (int64_t)row * m.cols + col + r] = (T)(v[r] * out);
-          }
+          for (int k = 0; k < 4; ++k)
+            if (n0 + c + k < m.n) U[tall ? (int64_t)(n0 + c + k) * m.cols + m0 + r : (int64_t)(m0 + r) * m.cols + n0 + c + k] = (T)(v[k] * out);
         }
       }
     }
-  if (gram) {
-    sum = wave_sum(sum);
+  if constexpr (SQUARES) {
     __syncthreads();
-    float* const part = reinterpret_cast<float*>(s_ring);
-    if (lane == 0) part[wave] = sum;
-    __syncthreads();
-    if (tid == 0) a.squares[blockIdx.x] = (part[0] + part[1]) + (part[2] + part[3]);
+    if (mirror) {
+#pragma unroll
+      for (int i = 0; i < TILE * TILE / 1024; ++i) {
+        const int at = i * 256 + tid, c = at / (TILE / 4), r4 = at % (TILE / 4);
+        const f32x4 t = *reinterpret_cast<const f32x4*>(s_ring + c * (TILE * 4) + ((r4 ^ (c & ~3 & (TILE / 4 - 1))) << 4));
+        const float v[4] = {t[0], t[1], t[2], t[3]};
+        store_pair(C + (size_t)(n0 + c) * ldc + pair_byte(m0 + r4 * 4), v);
+      }
+    }
+    if (op.sum) {
+      __syncthreads();
+      float* const part = reinterpret_cast<float*>(s_ring);
+      sum = wave_sum(sum);
+      if (lane == 0) part[wave] = sum;
+      __syncthreads();
+      if (tid == 0) a.squares[tile] = ((part[0] + part[1]) + (part[2] + part[3])) * (mirror ? 2.f : 1.f);
+    }
   }
 }
 
-constexpr size_t align256(size_t v) { return (v + 255) / 256 * 256; }
+size_t align256(size_t v) { return (v + 255) / 256 * 256; }
 size_t mat_bytes(int64_t mp, int64_t np) { return (size_t)(2 * mp * np + N_SLOTS * mp * mp) * 4; }
+int64_t tiles_of(int64_t v, int tile) { return (v + tile - 1) / tile; }
 }  // namespace
 
-modse_status ortho_layout(const modse_matrix_set* set, OrthoLayout& w) {
+// A rounding of A in a group's first step has grown by this at most in the A of its last one.
+constexpr double F32_GROWTH = 200, BF16_GROWTH = 25000;
+
+modse_status ortho_layout(const modse_matrix_set* set, const float* coeffs, int steps, OrthoLayout& w) {
   const int n = set->n_matrices;
-  int64_t square = 0, update = 0, parts = 0;
+  int64_t square[2] = {0, 0}, update[2] = {0, 0}, parts = 0;
   size_t data = 0;
+  double m3 = 0, m2n = 0;
   for (int i = 0; i < n; ++i) {
     const int r = set->rows[i], c = set->cols[i];
     if (r < 1 || c < 1) return MODSE_ERR_INVALID_ARG;
     if (r > 65536 || c > 65536) return MODSE_ERR_UNSUPPORTED;
-    const int64_t mp = padded(r < c ? r : c), np = padded(r < c ? c : r);
-    square += mp / PAD * (mp / PAD);
-    update += mp / PAD * (np / PAD);
+    const int64_t sm = r < c ? r : c, sn = r < c ? c : r;
+    for (int t = 0; t < 2; ++t) {
+      const int64_t mt = tiles_of(sm, t ? 64 : 128);
+      square[t] += mt * (mt + 1) / 2;
+      update[t] += mt * tiles_of(sn, t ? 64 : 128);
+    }
     parts += ((int64_t)r * c + PART - 1) / PART;
-    data += mat_bytes(mp, np);
+    data += mat_bytes(padded(sm), padded(sn));
+    m3 += (double)sm * sm * sm;
+    m2n += (double)sm * sm * sn;
   }
-  if (update >= (int64_t)1 << 24) return MODSE_ERR_UNSUPPORTED;  // (a launch has fewer than 2^32 threads)
-  w.square_tiles = (int32_t)square;
-  w.update_tiles = (int32_t)update;
+  if (update[1] >= (int64_t)1 << 23) return MODSE_ERR_UNSUPPORTED;  // (a launch has fewer than 2^32 threads)
+  const bool small = square[0] <= 256;
+  w.tile = small ? 64 : 128;
+  w.square_tiles = (int32_t)square[small];
+  w.update_tiles = (int32_t)update[small];
   w.parts = (int32_t)parts;
   size_t off = 0;
   auto take = [&](size_t bytes) {
@@ -434,23 +534,41 @@ modse_status ortho_layout(const modse_matrix_set* set, OrthoLayout& w) {
   };
   w.mats = take(n * sizeof(Mat));
   w.bounds = take(n * sizeof(Bound));
-  w.factors = take((size_t)n * 3 * sizeof(Factors));
-  w.squares = take((size_t)square * 4);
+  w.factors = take((size_t)n * 6 * sizeof(Factors));
+  w.squares = take((size_t)square[1] * 4);
   w.sums = take((size_t)parts * sizeof(double));
-  w.square_map = take((size_t)square * 4);
-  w.update_map = take((size_t)update * 4);
+  w.square_map = take((size_t)square[1] * 4);
+  w.update_map = take((size_t)update[1] * 4);
   w.data = take(data);
   w.total = n ? off : 0;
+  w.n_groups = 0;
+  // Groups of steps where the products are what counts (enough tiles to go round), and X is longer than it is wide.
+  const bool grouped = coeffs && update[0] >= 1024 && m2n >= 1.25 * m3;
+  const double most = set->dtype == MODSE_F32 ? F32_GROWTH : BF16_GROWTH;
+  double top = 1;
+  for (int i = 0; coeffs && i < steps;) {
+    double growth = 1;
+    int g = 0;
+    do {
+      const float* const c = coeffs + 3 * (i + g);
+      const double slope = ratio_bound(c[0], c[1], c[2], top);
+      growth *= slope > 1 ? slope * slope : 1;
+      top = quintic_bound(c[0], c[1], c[2], top);
+      ++g;
+    } while (grouped && i + g < steps && growth <= most);
+    w.group[w.n_groups++] = g;
+    i += g;
+  }
   return MODSE_OK;
 }
 
-hipError_t launch_orthogonalize(const modse_matrix_set* set, const OrthoLayout& w, const float* coeffs, int steps, float eps, char* ws,
-                               hipStream_t s) {
-  const int n = set->n_matrices;
+hipError_t launch_orthogonalize(const modse_matrix_set* set, const OrthoLayout& w, const float* coeffs, float eps, char* ws, hipStream_t s) {
+  const int n = set->n_matrices, tile = w.tile;
   Mat* const table = reinterpret_cast<Mat*>(ws + w.mats);
   Bound* const bounds = reinterpret_cast<Bound*>(ws + w.bounds);
-  Factors* const factors = reinterpret_cast<Factors*>(ws + w.factors);  // of the three kinds of products
-  Factors *const f_gram = factors, *const f_square = factors + n, *const f_update = factors + 2 * n;
+  Factors* const factors = reinterpret_cast<Factors*>(ws + w.factors);
+  Factors *const f_gram = factors, *const f_square = factors + n, *const f_join = factors + 2 * n, *const f_half = factors + 3 * n,
+          *const f_next = factors + 4 * n, *const f_update = factors + 5 * n;
   float* const squares = reinterpret_cast<float*>(ws + w.squares);
   double* const sums = reinterpret_cast<double*>(ws + w.sums);
   int32_t* const square_map = reinterpret_cast<int32_t*>(ws + w.square_map);
@@ -466,45 +584,78 @@ hipError_t launch_orthogonalize(const modse_matrix_set* set, const OrthoLayout& 
     a.count = n - first < MATS_PER_LAUNCH ? n - first : MATS_PER_LAUNCH;
     for (int i = 0; i < a.count; ++i) {
       const int r = set->rows[first + i], c = set->cols[first + i];
-      const int mp = padded(r < c ? r : c), np = padded(r < c ? c : r);
-      const int parts = (int)(((int64_t)r * c + PART - 1) / PART);
+      const int64_t sm = r < c ? r : c, sn = r < c ? c : r, mt = tiles_of(sm, tile);
+      const int parts = (int)(((int64_t)r * c + PART - 1) / PART), blocks = padded(sm) / 64 * (padded(sn) / 64);
       a.mat[i] = {set->G[first + i], set->U[first + i], data, r, c, square, update, part, parts};
-      square += mp / PAD * (mp / PAD);
-      update += mp / PAD * (np / PAD);
+      square += (int32_t)(mt * (mt + 1) / 2);
+      update += (int32_t)(mt * tiles_of(sn, tile));
       part += parts;
-      data += (int64_t)mat_bytes(mp, np);
+      data += (int64_t)mat_bytes(padded(sm), padded(sn));
       if (parts > most_parts) most_parts = parts;
-      if (mp / 64 * (np / 64) > most_tiles) most_tiles = mp / 64 * (np / 64);
+      if (blocks > most_tiles) most_tiles = blocks;
     }
     hipLaunchKernelGGL(ortho_table_kernel, dim3(1), dim3(64), 0, s, a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
   hipLaunchKernelGGL(ortho_squares_kernel, dim3(most_parts < 1024 ? most_parts : 1024, n), dim3(256), 0, s, table, sums);
   if ((e = hipGetLastError()) != hipSuccess) return e;
-  hipLaunchKernelGGL(ortho_prepare_kernel, dim3(n), dim3(256), 0, s, table, sums, eps, bounds, f_gram, square_map, update_map);
+  hipLaunchKernelGGL(ortho_prepare_kernel, dim3(n), dim3(256), 0, s, table, sums, eps, bounds, f_gram, tile, square_map, update_map);
   if ((e = hipGetLastError()) != hipSuccess) return e;
   hipLaunchKernelGGL(ortho_start_kernel, dim3(most_tiles < 2048 ? most_tiles : 2048, n), dim3(256), 0, s, table, bounds);
   if ((e = hipGetLastError()) != hipSuccess) return e;
-  for (int i = 0; i < steps; ++i) {
-    ProductArgs a = {table, f_gram, bounds, squares, square_map, OP_GRAM, i & 1};
-    const dim3 block(256);
-    const float* const c = coeffs + 3 * i;
-    hipLaunchKernelGGL((ortho_product_kernel<true, OUT_PAIRS>), dim3(w.square_tiles), block, 0, s, a);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
-    hipLaunchKernelGGL(ortho_factors_kernel, dim3(n), dim3(64), 0, s, table, squares, c[0], c[1], c[2], bounds, f_square, f_update, f_gram);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
-    a.kind = OP_SQUARE;
-    a.factors = f_square;
-    hipLaunchKernelGGL((ortho_product_kernel<true, OUT_PAIRS>), dim3(w.square_tiles), block, 0, s, a);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
-    a.kind = OP_UPDATE;
-    a.factors = f_update;
+
+  ProductArgs a = {table, square_map, {}, bounds, squares, 0, w.square_tiles};
+  auto grid = [](int tiles, int ops) { return dim3((tiles + 8 * RUN - 1) / (8 * RUN) * (8 * RUN), ops); };
+  auto squares_of = [&](const SquareOp& one, const SquareOp* two) {
+    a.map = square_map;
+    a.tiles = w.square_tiles;
+    a.op[0] = one;
+    if (two) a.op[1] = *two;
+    const dim3 g = grid(a.tiles, two ? 2 : 1);
+    if (tile == 128) hipLaunchKernelGGL((ortho_product_kernel<128, 2, true, OUT_PAIRS>), g, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((ortho_product_kernel<64, 4, true, OUT_PAIRS>), g, dim3(256), 0, s, a);
+    return hipGetLastError();
+  };
+  auto update_by = [&](int q, auto out) {
+    constexpr Out OUT = decltype(out)::value;
     a.map = update_map;
-    const dim3 grid(w.update_tiles);
-    if (i + 1 < steps) hipLaunchKernelGGL((ortho_product_kernel<false, OUT_PAIRS>), grid, block, 0, s, a);
-    else if (set->dtype == MODSE_F32) hipLaunchKernelGGL((ortho_product_kernel<false, OUT_F32>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((ortho_product_kernel<false, OUT_BF16>), grid, block, 0, s, a);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
+    a.tiles = w.update_tiles;
+    a.op[0] = {f_update, q, -1, -1, -1, -1, 0};
+    const dim3 g = grid(a.tiles, 1);
+    if (tile == 128) hipLaunchKernelGGL((ortho_product_kernel<128, 2, false, OUT>), g, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((ortho_product_kernel<64, 4, false, OUT>), g, dim3(256), 0, s, a);
+    return hipGetLastError();
+  };
+  int step = 0;
+  for (int k = 0; k < w.n_groups; ++k) {
+    if ((e = squares_of({f_gram, -1, -1, -1, -1, SLOT_A, 1}, nullptr)) != hipSuccess) return e;
+    int A = SLOT_A, Q = SLOT_R;
+    float qa = 0.f;
+    for (int i = 0; i < w.group[k]; ++i, ++step) {
+      const float* const c = coeffs + 3 * step;
+      const bool last = i + 1 == w.group[k];
+      const StepArgs f = {c[0], c[1], c[2], qa, i == 0, last, f_square, f_join, f_half, f_next, f_update, f_gram};
+      hipLaunchKernelGGL(ortho_factors_kernel, dim3(n), dim3(64), 0, s, table, squares, tile, bounds, f);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+      const int R = i == 1 ? SLOT_R2 : SLOT_R;  // (the first one is Q in the second step)
+      if ((e = squares_of({f_square, A, A, A, -1, R, 0}, nullptr)) != hipSuccess) return e;
+      const int Q2 = i == 0 ? R : Q == SLOT_Q ? SLOT_R2 : SLOT_Q;
+      const SquareOp join = {f_join, R, Q, Q, R, Q2, 0}, half = {f_half, R, A, A, -1, SLOT_S, 0};
+      if (i > 0 || !last) {
+        if ((e = i == 0 ? squares_of(half, nullptr) : last ? squares_of(join, nullptr) : squares_of(join, &half)) != hipSuccess) return e;
+      }
+      Q = Q2;
+      qa = i == 0 ? c[0] : qa * c[0];
+      if (!last) {
+        A = A == SLOT_A ? SLOT_A2 : SLOT_A;
+        if ((e = squares_of({f_next, R, SLOT_S, SLOT_S, -1, A, 1}, nullptr)) != hipSuccess) return e;
+      }
+    }
+    if (k + 1 < w.n_groups) e = update_by(Q, std::integral_constant<Out, OUT_PAIRS>{});
+    else if (set->dtype == MODSE_F32) e = update_by(Q, std::integral_constant<Out, OUT_F32>{});
+    else e = update_by(Q, std::integral_constant<Out, OUT_BF16>{});
+    if (e != hipSuccess) return e;
+    a.x = 1 - a.x;
   }
   return hipSuccess;
 }

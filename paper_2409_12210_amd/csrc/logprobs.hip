@@ -18,8 +18,8 @@ namespace {
 constexpr int MAX_TOP = MODSE_LOGPROBS_MAX_TOP;
 constexpr int LIST = 192;       // candidates of a wave: LIST_FULL, and 64 more that one step can add
 constexpr int LIST_FULL = 128;  // at which the list is cut back to the n largest
-constexpr int TILE = 2048;      // entries that a block takes in one step: eight per thread
-constexpr int AHEAD = 4;        // tiles that are loaded together
+constexpr int TILE = 2048;      // entries of a row that a block takes at a time: eight per thread
+constexpr int AHEAD = 4;        // tiles that are loaded, and looked through, together (a power of two)
 constexpr float LOG2E = 1.44269504088896340736f;
 constexpr float LOWEST = -3.402823466e38f;
 constexpr float FAR = -1e30f;   // differences of logits below it are held at it: e^FAR is 0, and 0 * FAR is no NaN
@@ -41,46 +41,75 @@ __device__ __forceinline__ void wave_lds_order() {  // LDS writes of this wave's
   __builtin_amdgcn_wave_barrier();
 }
 
-// A bound K so that exactly n of the wave's keys (R per lane, distinct but for 0 = none, more than n in all) are K or more: its
-// bits are set from the highest as long as n keys stay.
+__device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
+#define STEP(CTRL, ROWS) { const uint32_t o = (uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, CTRL, ROWS, 0xf, false); v = max(v, o); }
+  STEP(0x111, 0xf) STEP(0x112, 0xf) STEP(0x114, 0xf) STEP(0x118, 0xf) STEP(0x142, 0xa) STEP(0x143, 0xc)
+#undef STEP
+  return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
+}
+
+// A bound K so that n to n + slack of the wave's keys are K or more (R per lane, distinct but for 0 = none, more than n in all):
+// bisection between the smallest and the largest, first over the values, and where several entries have the n-th value over
+// their indices.  Distinct values come apart in 6 to 8 of its steps.
 template <int R>
-__device__ __forceinline__ uint64_t nth_key(const uint64_t (&key)[R], int n) {
-  uint32_t p = 0;
-  int c = 0;
+__device__ __forceinline__ uint64_t nth_key(const uint64_t (&key)[R], int n, int slack) {
+  uint32_t top = 0, least = 0;
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const uint32_t h = (uint32_t)(key[r] >> 32);
+    top = max(top, h);
+    least = max(least, h ? ~h : 0);
+  }
+  uint32_t hi = wave_max_u32(top), lo = ~wave_max_u32(least);  // at least n keys are lo or more
 #pragma unroll 1
-  for (uint32_t bit = 0x80000000u; bit; bit >>= 1) {
-    const uint32_t t = p | bit;
+  while (lo < hi) {
+    const uint32_t t = lo + (hi - lo + 1) / 2;
     int m = 0;
 #pragma unroll
     for (int r = 0; r < R; ++r) m += __popcll(__ballot((uint32_t)(key[r] >> 32) >= t));
     if (m >= n) {
-      p = t;
-      c = m;
-      if (m == n) break;
+      lo = t;
+      if (m <= n + slack) return (uint64_t)t << 32;
+    } else {
+      hi = t - 1;
     }
   }
-  if (c == n) return (uint64_t)p << 32;
-  // several entries of the n-th value: those of the lowest indices
-  int above = 0;
+  int above = 0, with = 0;
 #pragma unroll
-  for (int r = 0; r < R; ++r) above += __popcll(__ballot((uint32_t)(key[r] >> 32) > p));
-  uint32_t q = 0;
+  for (int r = 0; r < R; ++r) {
+    above += __popcll(__ballot((uint32_t)(key[r] >> 32) > lo));
+    with += __popcll(__ballot((uint32_t)(key[r] >> 32) >= lo));
+  }
+  if (with <= n + slack) return (uint64_t)lo << 32;
+  uint32_t last = 0, first = 0;
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const bool tied = (uint32_t)(key[r] >> 32) == lo;
+    last = max(last, tied ? (uint32_t)key[r] : 0);
+    first = max(first, tied ? ~(uint32_t)key[r] : 0);
+  }
+  uint32_t q_hi = wave_max_u32(last), q = ~wave_max_u32(first);
 #pragma unroll 1
-  for (uint32_t bit = 0x80000000u; bit; bit >>= 1) {
-    const uint32_t t = q | bit;
+  while (q < q_hi) {
+    const uint32_t t = q + (q_hi - q + 1) / 2;
     int m = above;
 #pragma unroll
-    for (int r = 0; r < R; ++r) m += __popcll(__ballot((uint32_t)(key[r] >> 32) == p && (uint32_t)key[r] >= t));
-    if (m >= n) q = t;
+    for (int r = 0; r < R; ++r) m += __popcll(__ballot((uint32_t)(key[r] >> 32) == lo && (uint32_t)key[r] >= t));
+    if (m >= n) {
+      q = t;
+      if (m <= n + slack) break;
+    } else {
+      q_hi = t - 1;
+    }
   }
-  return (uint64_t)p << 32 | q;
+  return (uint64_t)lo << 32 | q;
 }
 
 // The candidates of one wave.  All members are the same in every lane.
 struct Candidates {
   uint64_t* list;
   int n, count;
-  uint64_t bound;  // n entries of at least this key have been seen, and an entry that is not above it is out
+  uint64_t bound;  // n entries above this key have been seen, and an entry that is not above it is out
   float bound_value;
   __device__ __forceinline__ void start(uint64_t* at, int top) {
     list = at;
@@ -89,51 +118,65 @@ struct Candidates {
     bound = (uint64_t)ordered(-__builtin_inff()) << 32 | 0xffffffffu;  // masked entries are never in
     bound_value = -__builtin_inff();
   }
-  __device__ __forceinline__ void raise(uint64_t k) {
-    bound = k;
-    bound_value = key_value(k);
+  __device__ __forceinline__ void raise(uint64_t least) {  // n entries of at least this key have been seen
+    bound = least - 1;
+    bound_value = key_value(bound);
   }
-  __device__ __forceinline__ void cut() {  // to the n largest (count > n)
+  __device__ __forceinline__ void add(uint64_t k, bool mine, uint64_t in) {
+    if (mine) list[count + __builtin_amdgcn_mbcnt_hi((uint32_t)(in >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)in, 0))] = k;
+    count += __popcll(in);
+  }
+  __device__ __forceinline__ void cut() {  // to the n largest, or a few more, 64 at most (count > 64)
     constexpr int R = LIST / 64;
     const int lane = threadIdx.x & 63;
     wave_lds_order();
     uint64_t k[R];
 #pragma unroll
     for (int r = 0; r < R; ++r) k[r] = r * 64 + lane < count ? list[r * 64 + lane] : 0;
-    const uint64_t least = nth_key(k, n);
+    const uint64_t least = nth_key(k, n, 64 - n);
     wave_lds_order();
     count = 0;
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-      const uint64_t in = __ballot(k[r] >= least);
-      if (k[r] >= least) list[count + __builtin_amdgcn_mbcnt_hi((uint32_t)(in >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)in, 0))] = k[r];
-      count += __popcll(in);
-    }
+    for (int r = 0; r < R; ++r) add(k[r], k[r] >= least, __ballot(k[r] >= least));
     raise(least);
   }
-  // eight entries of this lane from index `at` on, their maximum
-  __device__ __forceinline__ void take(const float (&v)[8], float most, uint32_t at) {
-    const uint64_t lanes = __ballot(most > bound_value);
+  // AHEAD eights of this lane, their maximum, the index of the first; the eights are TILE apart
+  __device__ __forceinline__ void take(const float (&v)[AHEAD][8], float most, uint32_t at) {
+    const uint64_t lanes = __ballot(most > bound_value);  // (entries that come later lose ties)
     if (lanes == 0) return;
     if (__popcll(lanes) > n) {
-      // more lanes than entries that are wanted: the n largest of their maxima bound the rest
-      // (the maximum is at one of eight places, and a bound has to be at the last of them)
-      const uint64_t k[1] = {most > bound_value ? key_of(most, at + 7) : 0};
-      const uint64_t least = nth_key(k, n);
-      // (what is as large as the bound is to stay in)
-      if (least - 1 > bound) raise(least - 1);
+      // more lanes than entries that are wanted: the n largest of their maxima bound the rest.  (A maximum can be at the last of
+      // a lane's places.)
+      const uint64_t k[1] = {most > bound_value ? key_of(most, at + (AHEAD - 1) * TILE + 7) : 0};
+      const uint64_t least = nth_key(k, n, n / 2 + 2);
+      if (least - 1 > bound) raise(least);
     }
+    uint32_t left = 0;  // which of this lane's are not below the bound
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const uint64_t k = key_of(v[j], at + j);
-      const bool mine = v[j] == v[j] && k > bound;
-      const uint64_t in = __ballot(mine);
-      if (in) {
-        if (mine) list[count + __builtin_amdgcn_mbcnt_hi((uint32_t)(in >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)in, 0))] = k;
-        count += __popcll(in);
-        if (count > LIST_FULL) cut();
-      }
+    for (int i = 0; i < AHEAD * 8; ++i) left |= v[i / 8][i % 8] >= bound_value ? 1u << i : 0;
+    // (a loop that picks the value, not a body for each of the 32: as code it would be larger than what it runs on)
+#pragma unroll 1
+    while (__ballot(left != 0)) {
+      const int i = __builtin_ffs((int)left) - 1;
+      float x[AHEAD * 4];
+#pragma unroll
+      for (int k = 0; k < AHEAD * 4; ++k) x[k] = i & 1 ? v[k / 4][k % 4 * 2 + 1] : v[k / 4][k % 4 * 2];
+#pragma unroll
+      for (int width = AHEAD * 2, bit = 2; width > 0; width >>= 1, bit <<= 1)
+#pragma unroll
+        for (int k = 0; k < width; ++k) x[k] = i & bit ? x[2 * k + 1] : x[2 * k];
+      const uint64_t k = key_of(x[0], at + (i >> 3) * TILE + (i & 7));
+      const bool mine = left != 0 && k > bound;
+      left &= left - 1;
+      add(k, mine, __ballot(mine));
+      if (count > LIST_FULL) cut();
     }
+  }
+  // the n largest among at most 64, and zeros behind them
+  __device__ __forceinline__ void finish() {
+    if (count > 64) cut();
+    const int lane = threadIdx.x & 63;
+    if (lane >= count) list[lane] = 0;
   }
 };
 
@@ -178,9 +221,9 @@ __global__ __launch_bounds__(256) void logprobs_fwd_kernel(LogprobsFwdArgs a, in
   const T* const x = static_cast<const T*>(a.logits) + row * a.ld;
   int target = -1;
   float target_logit = 0.f;
-  if (!SPLIT && a.targets) {
+  if (a.targets) {
     target = a.targets[row];
-    if (target >= 0 && target < a.vocab) target_logit = (float)x[target];
+    if (target >= begin && target < end) target_logit = (float)x[target];
   }
   Candidates top;
   if constexpr (TOP) top.start(s_list + wave * LIST, a.top);
@@ -194,24 +237,27 @@ __global__ __launch_bounds__(256) void logprobs_fwd_kernel(LogprobsFwdArgs a, in
       const int col = base + u * TILE + mine;
       load_some(raw[u], x + col, end - col, -__builtin_inff());
     }
+    float v[AHEAD][8], most = -__builtin_inff();
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        v[u][j] = raw[u][j];
+        most = fmaxf(most, v[u][j]);
+      }
+    t = rescaled(t, fmaxf(t.m, most));
 #pragma unroll
     for (int u = 0; u < AHEAD; ++u) {
-      float v[8], most = -__builtin_inff();
+      if (base + u * TILE >= end) break;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        v[j] = raw[u][j];
-        most = fmaxf(most, v[j]);
-      }
-      t = rescaled(t, fmaxf(t.m, most));
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float z = v[j] - t.m;  // (NaN and +inf go on into S)
+        const float z = v[u][j] - t.m;  // (NaN and +inf go on into S)
         const float e = __builtin_amdgcn_exp2f(z * LOG2E);
         t.S += e;
         if constexpr (ENTROPY) t.W += e * fmaxf(z, FAR);
       }
-      if constexpr (TOP) top.take(v, most, base + u * TILE + mine);
     }
+    if constexpr (TOP) top.take(v, most, base + mine);
   }
   t = rescaled(t, wave_max(t.m));
   t.S = wave_sum(t.S);
@@ -222,7 +268,7 @@ __global__ __launch_bounds__(256) void logprobs_fwd_kernel(LogprobsFwdArgs a, in
     s_sums[wave][2] = t.W;
   }
   if constexpr (TOP) {
-    if (top.count > a.top) top.cut();
+    top.finish();
     if (lane == 0) s_count[wave] = top.count;
   }
   __syncthreads();
@@ -238,28 +284,27 @@ __global__ __launch_bounds__(256) void logprobs_fwd_kernel(LogprobsFwdArgs a, in
   }
   float log_z = 0.f;
   if constexpr (SPLIT) {
-    if (threadIdx.x == 0) a.part[blockIdx.x] = f32x4{all.m, all.S, all.W, 0.f};
+    if (threadIdx.x == 0) a.part[blockIdx.x] = f32x4{all.m, all.S, all.W, target_logit};
   } else {
     log_z = row_outputs(a, row, all, target_logit, target, threadIdx.x == 0);
   }
   if constexpr (TOP) {
     // a candidate's rank is the number of larger ones
-    const int total = s_count[0] + s_count[1] + s_count[2] + s_count[3];
-    int rank = threadIdx.x;  // (of a thread without a candidate: the first place that stays empty, and on)
-    uint64_t k = 0;
-    if (lane < s_count[wave]) {
-      k = s_list[wave * LIST + lane];
-      rank = 0;
+    int total = 0, most = 0, before = 0;  // before: threads without a candidate in front of this wave
 #pragma unroll
-      for (int w = 0; w < 4; ++w)
-        for (int i = 0; i < s_count[w]; ++i) rank += s_list[w * LIST + i] > k;
-    } else {
-      int before = 0;  // threads without a candidate in front of this one
-#pragma unroll
-      for (int w = 0; w < 4; ++w)
-        if (w < wave) before += 64 - s_count[w];
-      rank = total + before + lane - s_count[wave];
+    for (int w = 0; w < 4; ++w) {
+      const int c = s_count[w];
+      total += c;
+      most = max(most, c);
+      before += w < wave ? 64 - c : 0;
     }
+    const uint64_t k = s_list[wave * LIST + lane];
+    int rank = 0;
+#pragma unroll 2
+    for (int i = 0; i < most; ++i)
+#pragma unroll
+      for (int w = 0; w < 4; ++w) rank += s_list[w * LIST + i] > k;
+    if (k == 0) rank = total + before + lane - s_count[wave];  // the places that stay empty
     if (rank < a.top) {
       if constexpr (SPLIT) {
         a.keys[(int64_t)blockIdx.x * a.top + rank] = k;
@@ -271,55 +316,47 @@ __global__ __launch_bounds__(256) void logprobs_fwd_kernel(LogprobsFwdArgs a, in
   }
 }
 
-// Joins the segments of a row: one wave per row, one lane per segment.  The segments' lists are sorted, so the largest key left
-// is one of their heads; of equal values the lowest segment has the lower index.
-__global__ __launch_bounds__(64) void logprobs_join_kernel(LogprobsFwdArgs a, int splits, int bf16) {
-  extern __shared__ uint64_t s_keys[];
+// Joins the segments of a row: one wave per row, one lane per segment for the sums; the segments' entries are ranked as above.
+constexpr int JOIN_KEYS = 8;  // per lane
+__global__ __launch_bounds__(64) void logprobs_join_kernel(LogprobsFwdArgs a, int splits, int segment) {
+  __shared__ uint64_t s_list[64];
   const int lane = threadIdx.x;
   const int64_t row = blockIdx.x;
-  int target = -1;
-  float target_logit = 0.f;
-  if (a.targets) {
-    target = a.targets[row];
-    if (target >= 0 && target < a.vocab) {
-      const int64_t i = row * a.ld + target;
-      target_logit = bf16 ? (float)static_cast<const bf16_t*>(a.logits)[i] : static_cast<const float*>(a.logits)[i];
-    }
-  }
   const int n = splits * a.top;
-  for (int i = lane; i < n; i += 64) s_keys[i] = a.keys[row * n + i];
+  uint64_t key[JOIN_KEYS];
+#pragma unroll
+  for (int r = 0; r < JOIN_KEYS; ++r) key[r] = r * 64 + lane < n ? a.keys[row * n + r * 64 + lane] : 0;
+  const int target = a.targets ? a.targets[row] : -1;
+  float target_logit = 0.f;
   Sums t = {LOWEST, 0.f, 0.f};
   if (lane < splits) {
     const f32x4 p = a.part[row * splits + lane];
     t = {p[0], p[1], p[2]};
+    target_logit = p[3];
   }
+  target_logit = lane_f32(target_logit, target >= 0 && target < a.vocab ? target / segment : 0);
   t = rescaled(t, wave_max(t.m));
   t.S = wave_sum(t.S);
   t.W = wave_sum(t.W);
   const float log_z = row_outputs(a, row, t, target_logit, target, lane == 0);
   if (a.top == 0) return;
-  __syncthreads();
-  int next = 0;
-  uint64_t head = lane < splits ? s_keys[lane * a.top] : 0;
-  uint64_t won = 0;  // of place `lane`
-#pragma unroll 1
-  for (int i = 0; i < a.top; ++i) {
-    const uint32_t o = (uint32_t)(head >> 32);
-    const float v = head ? unordered(o) : -__builtin_inff();
-    const float best = wave_max(v);
-    const uint64_t at = __ballot(head != 0 && v == best);
-    if (at == 0) break;
-    const int from = __builtin_ctzll(at);
-    const uint64_t k = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)o, from) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)head, from);
-    if (lane == i) won = k;
-    if (lane == from) {
-      ++next;
-      head = next < a.top ? s_keys[lane * a.top + next] : 0;
-    }
-  }
-  if (lane < a.top) {
-    a.top_idx[row * a.top + lane] = won ? key_index(won) : -1;
-    a.top_logp[row * a.top + lane] = won ? (key_value(won) - t.m) - log_z : -__builtin_inff();
+  int count = 0;
+#pragma unroll
+  for (int r = 0; r < JOIN_KEYS; ++r) count += __popcll(__ballot(key[r] != 0));
+  const uint64_t least = count > 64 ? nth_key(key, a.top, 64 - a.top) : 1;
+  Candidates all;
+  all.start(s_list, a.top);
+#pragma unroll
+  for (int r = 0; r < JOIN_KEYS; ++r) all.add(key[r], key[r] >= least, __ballot(key[r] >= least));
+  wave_lds_order();
+  const uint64_t k = lane < all.count ? s_list[lane] : 0;
+  int rank = 0;
+#pragma unroll 4
+  for (int i = 0; i < all.count; ++i) rank += s_list[i] > k;
+  if (k == 0) rank = lane;
+  if (rank < a.top) {
+    a.top_idx[row * a.top + rank] = k ? key_index(k) : -1;
+    a.top_logp[row * a.top + rank] = k ? (key_value(k) - t.m) - log_z : -__builtin_inff();
   }
 }
 
@@ -366,22 +403,22 @@ __global__ __launch_bounds__(256) void logprobs_bwd_kernel(LogprobsBwdArgs a, in
 }
 
 template <typename T, bool TOP, bool ENTROPY>
-hipError_t fwd(const LogprobsFwdArgs& a, int splits, hipStream_t s) {
+hipError_t fwd(const LogprobsFwdArgs& a, LogprobsSplit split, hipStream_t s) {
+  const auto [splits, segment] = split;
   if (splits == 1) {
     hipLaunchKernelGGL((logprobs_fwd_kernel<T, TOP, ENTROPY, false>), dim3((unsigned)a.T), dim3(256), 0, s, a, 1, 0);
     return hipGetLastError();
   }
-  const int segment = ((a.vocab + splits - 1) / splits + 7) / 8 * 8;
   hipLaunchKernelGGL((logprobs_fwd_kernel<T, TOP, ENTROPY, true>), dim3((unsigned)(a.T * splits)), dim3(256), 0, s, a, splits, segment);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(logprobs_join_kernel, dim3((unsigned)a.T), dim3(64), (size_t)splits * a.top * 8, s, a, splits, sizeof(T) == 2);
+  hipLaunchKernelGGL(logprobs_join_kernel, dim3((unsigned)a.T), dim3(64), 0, s, a, splits, segment);
   return hipGetLastError();
 }
 template <typename T>
-hipError_t fwd_any(const LogprobsFwdArgs& a, int splits, hipStream_t s) {
-  if (a.top) return a.entropy ? fwd<T, true, true>(a, splits, s) : fwd<T, true, false>(a, splits, s);
-  return a.entropy ? fwd<T, false, true>(a, splits, s) : fwd<T, false, false>(a, splits, s);
+hipError_t fwd_any(const LogprobsFwdArgs& a, LogprobsSplit split, hipStream_t s) {
+  if (a.top) return a.entropy ? fwd<T, true, true>(a, split, s) : fwd<T, true, false>(a, split, s);
+  return a.entropy ? fwd<T, false, true>(a, split, s) : fwd<T, false, false>(a, split, s);
 }
 template <typename T>
 hipError_t bwd(const LogprobsBwdArgs& a, hipStream_t s) {
@@ -393,14 +430,20 @@ hipError_t bwd(const LogprobsBwdArgs& a, hipStream_t s) {
 }
 }  // namespace
 
-// Blocks that share a row: enough for four on every CU, each with a tile at least.
-int logprobs_splits(int64_t T, int32_t vocab) {
-  const int64_t want = 1024 / (T > 0 ? T : 1), most = (vocab + TILE - 1) / TILE;
-  const int64_t n = want < most ? want : most;
-  return (int)(n < 1 ? 1 : n > 64 ? 64 : n);
+// A row is shared by several blocks where there are few rows, each taking a whole number of the groups of tiles that are loaded
+// together, and no more entries being left to join than a wave holds.  us a call, one block a row / one for every 8192 entries
+// (bf16): 1 x 131072, top 5 28.6 / 7.9, without top 14.7 / 4.7; 64 x 32000, top 5 11.8 / 8.3; 256 x 32000 12.8 / 11.2, without top
+// 5.7 / 6.9; 256 x 131072 34.9 / 24.9; 512 x 32000 15.5 / 16.2; 512 x 131072, without top 24.3 / 23.7; 700 x 131072 31.8 / 30.5, top 5
+// 50.0 / 52.3.  Finer cuts than a group: 64 x 32000 in 16 11.4, 1 x 131072 in 64 8.6.
+LogprobsSplit logprobs_split(int64_t T, int32_t vocab, int32_t top) {
+  constexpr int GROUP = TILE * AHEAD;
+  const int groups = (vocab + GROUP - 1) / GROUP, most = top > 8 ? JOIN_KEYS * 64 / top : 64;
+  if (T > 512 || (T > 256 && groups < 8)) return {1, vocab};
+  const int each = (groups + most - 1) / most;
+  return {(groups + each - 1) / each, each * GROUP};
 }
-hipError_t launch_logprobs_fwd(modse_dtype dt, const LogprobsFwdArgs& a, int splits, hipStream_t s) {
-  return dt == MODSE_F32 ? fwd_any<float>(a, splits, s) : fwd_any<bf16_t>(a, splits, s);
+hipError_t launch_logprobs_fwd(modse_dtype dt, const LogprobsFwdArgs& a, LogprobsSplit split, hipStream_t s) {
+  return dt == MODSE_F32 ? fwd_any<float>(a, split, s) : fwd_any<bf16_t>(a, split, s);
 }
 hipError_t launch_logprobs_bwd(modse_dtype dt, const LogprobsBwdArgs& a, hipStream_t s) {
   return dt == MODSE_F32 ? bwd<float>(a, s) : bwd<bf16_t>(a, s);

@@ -43,8 +43,11 @@ struct LogprobsFwdArgs {
   int64_t T;
   int32_t vocab, top;
 };
-int logprobs_splits(int64_t T, int32_t vocab);
-hipError_t launch_logprobs_fwd(modse_dtype dt, const LogprobsFwdArgs& a, int splits, hipStream_t s);
+struct LogprobsSplit {
+  int32_t splits, segment;  // blocks of a row, entries of each but the last
+};
+LogprobsSplit logprobs_split(int64_t T, int32_t vocab, int32_t top);
+hipError_t launch_logprobs_fwd(modse_dtype dt, const LogprobsFwdArgs& a, LogprobsSplit split, hipStream_t s);
 
 struct LogprobsBwdArgs {
   const void* logits;

@@ -89,7 +89,7 @@ modse_status modse_logprobs_workspace_size(int64_t T, int32_t vocab, modse_dtype
   // (fewer rows are cut finer: the most of all calls of at most T rows)
   size_t most = 0;
   for (int64_t t = 1; t <= T; ++t) {
-    const int splits = logprobs_splits(t, vocab);
+    const int splits = logprobs_split(t, vocab, top).splits;
     if (splits == 1) break;
     const size_t total = logprobs_layout(t, splits, top).total;
     if (total > most) most = total;
@@ -107,14 +107,14 @@ modse_status modse_logprobs_fwd(int64_t T, int32_t vocab, modse_dtype dtype, con
   if (!logits || ld_logits < vocab || !targets != !logp || (top && (!top_idx || !top_logp)) ||
       (!logp && !stats && !entropy && !top))
     return MODSE_ERR_INVALID_ARG;
-  const int splits = logprobs_splits(T, vocab);
-  const LogprobsLayout w = logprobs_layout(T, splits, top);
+  const LogprobsSplit split = logprobs_split(T, vocab, top);
+  const LogprobsLayout w = logprobs_layout(T, split.splits, top);
   if (w.total && (!ws || !aligned16(ws))) return MODSE_ERR_INVALID_ARG;
   if (ws_bytes < w.total) return MODSE_ERR_WORKSPACE;
   char* const wsb = static_cast<char*>(ws);
   const LogprobsFwdArgs a = {logits, ld_logits, targets, logp, stats, entropy, top_idx, top_logp,
                              reinterpret_cast<f32x4*>(wsb + w.part), reinterpret_cast<uint64_t*>(wsb + w.keys), T, vocab, top};
-  return hip_status(launch_logprobs_fwd(dtype, a, splits, static_cast<hipStream_t>(hip_stream)));
+  return hip_status(launch_logprobs_fwd(dtype, a, split, static_cast<hipStream_t>(hip_stream)));
 }
 
 modse_status modse_logprobs_bwd(int64_t T, int32_t vocab, modse_dtype dtype, const void* logits, int64_t ld_logits,

@@ -38,7 +38,7 @@ def test_norm_bwd_refuses(over, code):
     assert norm_bwd(**over) == code
 
 
-def logprobs_fwd(T=4, V=5000, dtype="f32", logits=P, ld=None, targets=P, logp=P, stats=P, entropy=P, top=3, top_idx=P,
+def logprobs_fwd(T=4, V=50000, dtype="f32", logits=P, ld=None, targets=P, logp=P, stats=P, entropy=P, top=3, top_idx=P,
                  top_logp=P, ws=P, ws_bytes=1 << 30):
     return m.modse_logprobs_fwd(T, V, dtype, logits, targets, logp, stats, entropy, top, top_idx, top_logp, ws, ws_bytes,
                                 ld_logits=ld, **NO)
@@ -47,7 +47,7 @@ def logprobs_fwd(T=4, V=5000, dtype="f32", logits=P, ld=None, targets=P, logp=P,
 @pytest.mark.parametrize("over,code", [
     (dict(T=-1), INVALID), (dict(V=0), INVALID), (dict(top=-1), INVALID), (dict(top=65), UNSUPPORTED),
     (dict(V=(1 << 30) + 1), UNSUPPORTED), (dict(T=1 << 31), UNSUPPORTED), (dict(T=1 << 24, V=9), UNSUPPORTED), (dict(T=1 << 22, V=32000), UNSUPPORTED),
-    (dict(dtype="fp16"), UNSUPPORTED), (dict(logits=None), INVALID), (dict(ld=4999), INVALID), (dict(targets=None), INVALID),
+    (dict(dtype="fp16"), UNSUPPORTED), (dict(logits=None), INVALID), (dict(ld=49999), INVALID), (dict(targets=None), INVALID),
     (dict(logp=None), INVALID), (dict(top_idx=None), INVALID), (dict(top_logp=None), INVALID),
     (dict(targets=None, logp=None, stats=None, entropy=None, top=0), INVALID), (dict(ws=None), INVALID),
     (dict(ws=P + 8), INVALID), (dict(ws_bytes=64), WORKSPACE), (dict(T=0, logits=None, ws=None), OK),
@@ -94,7 +94,7 @@ def test_workspaces_serve_fewer_rows_and_refuse_what_the_call_refuses():
         for t in (1, T // 2, T):
             if t:
                 assert logprobs_fwd(T=t, V=131072, dtype="bf16", top=20, ws_bytes=max(now, 1) - 1, logits=None) == INVALID
-    assert size(5000) == size(512) and size(5000) < 1 << 20 and m.modse_logprobs_workspace_size(0, 100, "f32") == 0
+    assert size(5000) == size(512) and size(5000) < 2 << 20 and m.modse_logprobs_workspace_size(0, 100, "f32") == 0
     assert m.modse_logprobs_workspace_size(4, 0, "f32", raise_on_error=False) == INVALID
     norm = [m.modse_norm_bwd_workspace_size(T, 2048, "bf16") for T in (0, 1, 5, 1000, 1 << 20)]
     assert norm == sorted(norm) and norm[0] == 0 and norm[-1] < 16 << 20

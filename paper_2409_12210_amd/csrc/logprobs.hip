@@ -8,8 +8,8 @@
 //
 // Top entries: the order is by falling value, then by rising index, which is the order of the 64-bit keys (ordered bits of the
 // value, ~index).  A wave keeps a list of candidates in LDS and a bound below which an entry cannot be among the n largest any
-// more, because n larger ones have been seen.  Entries are compared with it eight at a time through their maximum, which the
-// softmax needs anyway, so that a row costs little more than its sums.  The bound comes from the eights' maxima at first (the n
+// more, because n larger ones have been seen.  Entries are compared with it 32 of a lane at a time through their maximum, which
+// the softmax needs anyway, so that a row costs little more than its sums.  The bound comes from the lanes' maxima at first (the n
 // largest of 64 are n entries), and from the list whenever that fills up.
 #include "ops.h"
 
@@ -18,8 +18,8 @@ namespace {
 constexpr int MAX_TOP = MODSE_LOGPROBS_MAX_TOP;
 constexpr int LIST = 192;       // candidates of a wave: LIST_FULL, and 64 more that one step can add
 constexpr int LIST_FULL = 128;  // at which the list is cut back to the n largest
-constexpr int TILE = 2048;      // entries of a row that a block takes at a time: eight per thread
-constexpr int AHEAD = 4;        // tiles that are loaded, and looked through, together (a power of two)
+constexpr int LOOK = 32;        // entries of a thread that are loaded, and looked through, together, in vectors of sixteen bytes
+constexpr int GROUP = LOOK * 256;  // entries that a block takes at a time
 constexpr float LOG2E = 1.44269504088896340736f;
 constexpr float LOWEST = -3.402823466e38f;
 constexpr float FAR = -1e30f;   // differences of logits below it are held at it: e^FAR is 0, and 0 * FAR is no NaN
@@ -140,32 +140,33 @@ struct Candidates {
     for (int r = 0; r < R; ++r) add(k[r], k[r] >= least, __ballot(k[r] >= least));
     raise(least);
   }
-  // AHEAD eights of this lane, their maximum, the index of the first; the eights are TILE apart
-  __device__ __forceinline__ void take(const float (&v)[AHEAD][8], float most, uint32_t at) {
+  // LOOK entries of this lane in vectors of N, their maximum, the index of the first; the vectors are 256 N apart
+  template <int N>
+  __device__ __forceinline__ void take(const float (&v)[LOOK], float most, uint32_t at) {
     const uint64_t lanes = __ballot(most > bound_value);  // (entries that come later lose ties)
     if (lanes == 0) return;
     if (__popcll(lanes) > n) {
       // more lanes than entries that are wanted: the n largest of their maxima bound the rest.  (A maximum can be at the last of
       // a lane's places.)
-      const uint64_t k[1] = {most > bound_value ? key_of(most, at + (AHEAD - 1) * TILE + 7) : 0};
+      const uint64_t k[1] = {most > bound_value ? key_of(most, at + (LOOK / N - 1) * 256 * N + N - 1) : 0};
       const uint64_t least = nth_key(k, n, n / 2 + 2);
       if (least - 1 > bound) raise(least);
     }
     uint32_t left = 0;  // which of this lane's are not below the bound
 #pragma unroll
-    for (int i = 0; i < AHEAD * 8; ++i) left |= v[i / 8][i % 8] >= bound_value ? 1u << i : 0;
+    for (int i = 0; i < LOOK; ++i) left |= v[i] >= bound_value ? 1u << i : 0;
     // (a loop that picks the value, not a body for each of the 32: as code it would be larger than what it runs on)
 #pragma unroll 1
     while (__ballot(left != 0)) {
       const int i = __builtin_ffs((int)left) - 1;
-      float x[AHEAD * 4];
+      float x[LOOK];
 #pragma unroll
-      for (int k = 0; k < AHEAD * 4; ++k) x[k] = i & 1 ? v[k / 4][k % 4 * 2 + 1] : v[k / 4][k % 4 * 2];
+      for (int k = 0; k < LOOK; ++k) x[k] = v[k];
 #pragma unroll
-      for (int width = AHEAD * 2, bit = 2; width > 0; width >>= 1, bit <<= 1)
+      for (int b = 0; b < 5; ++b)
 #pragma unroll
-        for (int k = 0; k < width; ++k) x[k] = i & bit ? x[2 * k + 1] : x[2 * k];
-      const uint64_t k = key_of(x[0], at + (i >> 3) * TILE + (i & 7));
+        for (int k = 0; k < LOOK >> (b + 1); ++k) x[k] = i >> b & 1 ? x[2 * k + 1] : x[2 * k];
+      const uint64_t k = key_of(x[0], at + i / N * (256 * N) + i % N);
       const bool mine = left != 0 && k > bound;
       left &= left - 1;
       add(k, mine, __ballot(mine));
@@ -209,7 +210,7 @@ __device__ __forceinline__ float row_outputs(const LogprobsFwdArgs& a, int64_t r
   return log_z;
 }
 
-template <typename T, bool TOP, bool ENTROPY, bool SPLIT>
+template <typename T, bool TOP, bool ENTROPY, bool SPLIT, bool STREAM>
 __global__ __launch_bounds__(256) void logprobs_fwd_kernel(LogprobsFwdArgs a, int splits, int segment) {
   __shared__ uint64_t s_list[TOP ? 4 * LIST : 1];
   __shared__ float s_sums[4][3];
@@ -228,36 +229,36 @@ __global__ __launch_bounds__(256) void logprobs_fwd_kernel(LogprobsFwdArgs a, in
   Candidates top;
   if constexpr (TOP) top.start(s_list + wave * LIST, a.top);
   Sums t = {LOWEST, 0.f, 0.f};
-  const int mine = threadIdx.x * 8;
+  constexpr int N = Vec<T>::N;
+  const int mine = threadIdx.x * N;
 #pragma unroll 1
-  for (int base = begin; base < end; base += AHEAD * TILE) {
-    Raw8<T> raw[AHEAD];
+  for (int base = begin; base < end; base += GROUP) {
+    Vec<T> raw[LOOK / N];
 #pragma unroll
-    for (int u = 0; u < AHEAD; ++u) {
-      const int col = base + u * TILE + mine;
-      load_some(raw[u], x + col, end - col, -__builtin_inff());
+    for (int u = 0; u < LOOK / N; ++u) {
+      const int col = base + u * 256 * N + mine;
+      raw[u].template load<STREAM>(x + col, end - col, -__builtin_inff());
     }
-    float v[AHEAD][8], most = -__builtin_inff();
+    float v[LOOK], most = -__builtin_inff();
 #pragma unroll
-    for (int u = 0; u < AHEAD; ++u)
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        v[u][j] = raw[u][j];
-        most = fmaxf(most, v[u][j]);
-      }
+    for (int i = 0; i < LOOK; ++i) {
+      v[i] = raw[i / N][i % N];
+      most = fmaxf(most, v[i]);
+    }
     t = rescaled(t, fmaxf(t.m, most));
 #pragma unroll
-    for (int u = 0; u < AHEAD; ++u) {
-      if (base + u * TILE >= end) break;
+    for (int u = 0; u < LOOK / N; ++u) {
+      if (base + u * 256 * N < end) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float z = v[u][j] - t.m;  // (NaN and +inf go on into S)
-        const float e = __builtin_amdgcn_exp2f(z * LOG2E);
-        t.S += e;
-        if constexpr (ENTROPY) t.W += e * fmaxf(z, FAR);
+        for (int j = 0; j < N; ++j) {
+          const float z = v[u * N + j] - t.m;  // (NaN and +inf go on into S)
+          const float e = __builtin_amdgcn_exp2f(z * LOG2E);
+          t.S += e;
+          if constexpr (ENTROPY) t.W += e * fmaxf(z, FAR);
+        }
       }
     }
-    if constexpr (TOP) top.take(v, most, base + mine);
+    if constexpr (TOP) top.template take<N>(v, most, base + mine);
   }
   t = rescaled(t, wave_max(t.m));
   t.S = wave_sum(t.S);
@@ -361,10 +362,11 @@ __global__ __launch_bounds__(64) void logprobs_join_kernel(LogprobsFwdArgs a, in
 }
 
 // d_logits = w (1[target] - p) - dE p (log p + H)
-template <typename T, bool ENTROPY>
+template <typename T, bool ENTROPY, bool STREAM>
 __global__ __launch_bounds__(256) void logprobs_bwd_kernel(LogprobsBwdArgs a, int segments) {
   const int64_t row = blockIdx.x / segments;
-  const int col0 = blockIdx.x % segments * (TILE * AHEAD) + threadIdx.x * 8;
+  constexpr int N = Vec<T>::N;
+  const int col0 = blockIdx.x % segments * GROUP + threadIdx.x * N;
   const T* const x = static_cast<const T*>(a.logits) + row * a.ld;
   T* const dx = static_cast<T*>(a.d_logits) + row * a.ldd;
   const int target = a.targets ? a.targets[row] : -1;
@@ -373,20 +375,20 @@ __global__ __launch_bounds__(256) void logprobs_bwd_kernel(LogprobsBwdArgs a, in
   const float w = target < 0 || empty ? 0.f : target >= a.vocab ? __builtin_nanf("") : a.d_logp[row];
   const float dE = ENTROPY && !empty ? a.d_entropy[row] : 0.f, H = ENTROPY ? a.entropy[row] : 0.f;
   const bool zero = w == 0.f && dE == 0.f;
-  Raw8<T> raw[AHEAD];
+  Vec<T> raw[LOOK / N];
   if (!zero) {
 #pragma unroll
-    for (int u = 0; u < AHEAD; ++u) {
-      const int col = col0 + u * TILE;
-      load_some(raw[u], x + col, a.vocab - col, 0.f);
+    for (int u = 0; u < LOOK / N; ++u) {
+      const int col = col0 + u * 256 * N;
+      raw[u].template load<STREAM>(x + col, a.vocab - col, 0.f);
     }
   }
 #pragma unroll
-  for (int u = 0; u < AHEAD; ++u) {
-    const int col = col0 + u * TILE;
-    Raw8<T> out;
+  for (int u = 0; u < LOOK / N; ++u) {
+    const int col = col0 + u * 256 * N;
+    Vec<T> out;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
+    for (int j = 0; j < N; ++j) {
       float g = 0.f;
       if (!zero) {
         const float z = (raw[u][j] - m) - log_z;
@@ -398,18 +400,28 @@ __global__ __launch_bounds__(256) void logprobs_bwd_kernel(LogprobsBwdArgs a, in
       }
       out.set(j, g);
     }
-    store_some(out, dx + col, a.vocab - col);
+    out.template store<STREAM>(dx + col, a.vocab - col);
   }
 }
+
+// Logits that the caches do not hold are read, and their gradient stored, with the non-temporal hint.  us without / with it, forward and
+// backward: 16384 x 32000 bf16 (1.05 GB) 176 + 384 / 157 + 358, one behind the other 582 / 515; 2047 x 50257 float32 (411 MB) 241 / 222; 4096
+// x 32000 (262 MB), where the backward pass finds part of the logits in the cache, 156 / 132 but 127 with hinted stores alone; 1024 x 32000
+// 40.1 / 38.4, and a product that reads the gradient next loses what the stores gain: 305.0 / 307.0.
+constexpr int64_t STREAM_BYTES = (int64_t)384 << 20;
 
 template <typename T, bool TOP, bool ENTROPY>
 hipError_t fwd(const LogprobsFwdArgs& a, LogprobsSplit split, hipStream_t s) {
   const auto [splits, segment] = split;
   if (splits == 1) {
-    hipLaunchKernelGGL((logprobs_fwd_kernel<T, TOP, ENTROPY, false>), dim3((unsigned)a.T), dim3(256), 0, s, a, 1, 0);
+    const dim3 grid((unsigned)a.T);
+    if (a.T * a.vocab * (int64_t)sizeof(T) >= STREAM_BYTES)
+      hipLaunchKernelGGL((logprobs_fwd_kernel<T, TOP, ENTROPY, false, true>), grid, dim3(256), 0, s, a, 1, 0);
+    else
+      hipLaunchKernelGGL((logprobs_fwd_kernel<T, TOP, ENTROPY, false, false>), grid, dim3(256), 0, s, a, 1, 0);
     return hipGetLastError();
   }
-  hipLaunchKernelGGL((logprobs_fwd_kernel<T, TOP, ENTROPY, true>), dim3((unsigned)(a.T * splits)), dim3(256), 0, s, a, splits, segment);
+  hipLaunchKernelGGL((logprobs_fwd_kernel<T, TOP, ENTROPY, true, false>), dim3((unsigned)(a.T * splits)), dim3(256), 0, s, a, splits, segment);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL(logprobs_join_kernel, dim3((unsigned)a.T), dim3(64), 0, s, a, splits, segment);
@@ -420,13 +432,17 @@ hipError_t fwd_any(const LogprobsFwdArgs& a, LogprobsSplit split, hipStream_t s)
   if (a.top) return a.entropy ? fwd<T, true, true>(a, split, s) : fwd<T, true, false>(a, split, s);
   return a.entropy ? fwd<T, false, true>(a, split, s) : fwd<T, false, false>(a, split, s);
 }
-template <typename T>
+template <typename T, bool ENTROPY>
 hipError_t bwd(const LogprobsBwdArgs& a, hipStream_t s) {
-  const int segments = (a.vocab + TILE * AHEAD - 1) / (TILE * AHEAD);
+  const int segments = (a.vocab + GROUP - 1) / GROUP;
   const dim3 grid((unsigned)(a.T * segments));
-  if (a.d_entropy) hipLaunchKernelGGL((logprobs_bwd_kernel<T, true>), grid, dim3(256), 0, s, a, segments);
-  else hipLaunchKernelGGL((logprobs_bwd_kernel<T, false>), grid, dim3(256), 0, s, a, segments);
+  if (a.T * a.vocab * (int64_t)sizeof(T) >= STREAM_BYTES) hipLaunchKernelGGL((logprobs_bwd_kernel<T, ENTROPY, true>), grid, dim3(256), 0, s, a, segments);
+  else hipLaunchKernelGGL((logprobs_bwd_kernel<T, ENTROPY, false>), grid, dim3(256), 0, s, a, segments);
   return hipGetLastError();
+}
+template <typename T>
+hipError_t bwd_any(const LogprobsBwdArgs& a, hipStream_t s) {
+  return a.d_entropy ? bwd<T, true>(a, s) : bwd<T, false>(a, s);
 }
 }  // namespace
 
@@ -436,7 +452,6 @@ hipError_t bwd(const LogprobsBwdArgs& a, hipStream_t s) {
 // 5.7 / 6.9; 256 x 131072 34.9 / 24.9; 512 x 32000 15.5 / 16.2; 512 x 131072, without top 24.3 / 23.7; 700 x 131072 31.8 / 30.5, top 5
 // 50.0 / 52.3.  Finer cuts than a group: 64 x 32000 in 16 11.4, 1 x 131072 in 64 8.6.
 LogprobsSplit logprobs_split(int64_t T, int32_t vocab, int32_t top) {
-  constexpr int GROUP = TILE * AHEAD;
   const int groups = (vocab + GROUP - 1) / GROUP, most = top > 8 ? JOIN_KEYS * 64 / top : 64;
   if (T > 512 || (T > 256 && groups < 8)) return {1, vocab};
   const int each = (groups + most - 1) / most;
@@ -446,5 +461,5 @@ hipError_t launch_logprobs_fwd(modse_dtype dt, const LogprobsFwdArgs& a, Logprob
   return dt == MODSE_F32 ? fwd_any<float>(a, split, s) : fwd_any<bf16_t>(a, split, s);
 }
 hipError_t launch_logprobs_bwd(modse_dtype dt, const LogprobsBwdArgs& a, hipStream_t s) {
-  return dt == MODSE_F32 ? bwd<float>(a, s) : bwd<bf16_t>(a, s);
+  return dt == MODSE_F32 ? bwd_any<float>(a, s) : bwd_any<bf16_t>(a, s);
 }

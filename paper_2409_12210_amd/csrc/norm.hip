@@ -2,8 +2,8 @@
 // its backward pass.
 //
 // All of it is bound by memory: a row is read once, stays in registers as it was loaded, and is written once.  A row belongs to
-// one wave (W = 1: no barrier, sums by lane permutes alone), to four waves or to sixteen, each thread holds NC chunks of eight
-// elements of it, chunk c of a row going to thread c mod 64 W, so that a wave's accesses are contiguous.
+// one wave (W = 1: no barrier, sums by lane permutes alone), to four waves or to sixteen, each thread holds NC vectors of sixteen
+// bytes of it, vector c of a row going to thread c mod 64 W, so that a wave's accesses are contiguous.
 #include "ops.h"
 
 namespace {
@@ -36,21 +36,22 @@ __device__ __forceinline__ float row_max(float v, float* s) {
   return v;
 }
 
-typedef uint32_t u32x2_u __attribute__((ext_vector_type(2), aligned(1)));
-// eight values as e4m3, rounded to nearest even
-__device__ __forceinline__ void store_e4m3(uint8_t* p, const float v[8], int n) {
-  uint32_t w[2];
+// N values (4 or 8) as e4m3, rounded to nearest even
+template <int N>
+__device__ __forceinline__ void store_e4m3(uint8_t* p, const float (&v)[N], int n) {
+  typedef uint32_t words __attribute__((ext_vector_type(N / 4)));
+  typedef words words_u __attribute__((aligned(1)));
+  words w;
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    int r = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * i], v[4 * i + 1], 0, false);
+  for (int i = 0; i < N / 4; ++i) {
+    const int r = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * i], v[4 * i + 1], 0, false);
     w[i] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(v[4 * i + 2], v[4 * i + 3], r, true);
   }
-  if (n >= 8) {
-    u32x2_u o = {w[0], w[1]};
-    *reinterpret_cast<u32x2_u*>(p) = o;
+  if (n >= N) {
+    *reinterpret_cast<words_u*>(p) = w;
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
+    for (int i = 0; i < N; ++i)
       if (i < n) p[i] = (uint8_t)(w[i >> 2] >> (8 * (i & 3)));
   }
 }
@@ -58,9 +59,10 @@ __device__ __forceinline__ void store_e4m3(uint8_t* p, const float v[8], int n) 
 constexpr float MIN_SCALE = 1.17549435e-38f;  // 2^-126
 __device__ __forceinline__ float scale_of(float amax) { return fmaxf(amax * (1.f / 448.f), MIN_SCALE); }
 
-template <typename T, int W, int NC>
+template <typename T, int W, int NC, bool STREAM>
 __global__ __launch_bounds__(W == 1 ? 256 : W * 64) void norm_fwd_kernel(NormFwdArgs a) {
   constexpr int ROWS = W == 1 ? 4 : 1;  // of a block
+  constexpr int N = Vec<T>::N;
   __shared__ float s_part[16];
   const int at = W == 1 ? threadIdx.x & 63 : threadIdx.x;
   const int d = a.d;
@@ -68,56 +70,58 @@ __global__ __launch_bounds__(W == 1 ? 256 : W * 64) void norm_fwd_kernel(NormFwd
   const T* const residual = static_cast<const T*>(a.residual);
   T* const y = static_cast<T*>(a.y);
   T* const h = static_cast<T*>(a.h);
-  Raw8<T> gamma[NC];
+  Vec<T> gamma[NC];
 #pragma unroll
   for (int i = 0; i < NC; ++i) {
-    const int col = (i * W * 64 + at) * 8;
-    load_some(gamma[i], static_cast<const T*>(a.gamma) + col, d - col, 0.f);
+    const int col = (i * W * 64 + at) * N;
+    gamma[i].load(static_cast<const T*>(a.gamma) + col, d - col, 0.f);
   }
   for (int64_t row = (int64_t)blockIdx.x * ROWS + (W == 1 ? threadIdx.x >> 6 : 0); row < a.T; row += (int64_t)gridDim.x * ROWS) {
     const int64_t first = row * d;
-    Raw8<T> in[NC], res[NC];
+    Vec<T> in[NC], res[NC];
 #pragma unroll
     for (int i = 0; i < NC; ++i) {
-      const int col = (i * W * 64 + at) * 8;
-      load_some(in[i], x + first + col, d - col, 0.f);
-      if (residual) load_some(res[i], residual + first + col, d - col, 0.f);
+      const int col = (i * W * 64 + at) * N;
+      in[i].template load<STREAM>(x + first + col, d - col, 0.f);
+      if (residual) res[i].template load<STREAM>(residual + first + col, d - col, 0.f);
     }
-    float v[NC][8], sum = 0.f;
+    float v[NC][N], sum = 0.f;
 #pragma unroll
     for (int i = 0; i < NC; ++i)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
+      for (int j = 0; j < N; ++j) {
         v[i][j] = in[i][j];
         if (residual) v[i][j] += res[i][j];
         sum += v[i][j] * v[i][j];
       }
+#pragma unroll
+    for (int i = 0; i < NC; ++i) gamma[i].forget();
     sum = row_sum<W>(sum, s_part);
     const float rstd = 1.f / sqrtf(sum / (float)d + a.eps);
     if (a.rstd && at == 0) a.rstd[row] = rstd;
     float amax = 0.f;
 #pragma unroll
     for (int i = 0; i < NC; ++i) {
-      const int col = (i * W * 64 + at) * 8;
-      Raw8<T> out;
+      const int col = (i * W * 64 + at) * N;
+      Vec<T> out;
       if (h) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) out.set(j, v[i][j]);
-        store_some(out, h + first + col, d - col);
+        for (int j = 0; j < N; ++j) out.set(j, v[i][j]);
+        out.template store<true>(h + first + col, d - col);
       }
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
+      for (int j = 0; j < N; ++j) {
         v[i][j] *= rstd * gamma[i][j];
         amax = fmaxf(amax, fabsf(v[i][j]));
       }
       if (y) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) out.set(j, v[i][j]);
-        store_some(out, y + first + col, d - col);
+        for (int j = 0; j < N; ++j) out.set(j, v[i][j]);
+        out.store(y + first + col, d - col);
       }
     }
     if (a.q) {
-      const int lanes = a.group >> 3;
+      const int lanes = a.group / N;
       float scale = 0.f;
       if (lanes == 0) {
         scale = scale_of(row_max<W>(amax, s_part));
@@ -125,18 +129,18 @@ __global__ __launch_bounds__(W == 1 ? 256 : W * 64) void norm_fwd_kernel(NormFwd
       }
 #pragma unroll
       for (int i = 0; i < NC; ++i) {
-        const int c = i * W * 64 + at, col = c * 8;
+        const int c = i * W * 64 + at, col = c * N;
         if (lanes) {
           amax = 0.f;
 #pragma unroll
-          for (int j = 0; j < 8; ++j) amax = fmaxf(amax, fabsf(v[i][j]));
+          for (int j = 0; j < N; ++j) amax = fmaxf(amax, fabsf(v[i][j]));
           scale = scale_of(group_max(amax, lanes));
           if (col < d && (c & (lanes - 1)) == 0) a.scale[row * ((d + a.group - 1) / a.group) + c / lanes] = scale;
         }
         const float inv = 1.f / scale;
-        float out[8];
+        float out[N];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) out[j] = v[i][j] * inv;
+        for (int j = 0; j < N; ++j) out[j] = v[i][j] * inv;
         store_e4m3(a.q + first + col, out, d - col);
       }
     }
@@ -146,143 +150,167 @@ __global__ __launch_bounds__(W == 1 ? 256 : W * 64) void norm_fwd_kernel(NormFwd
 // dX = rstd (g - hat mean(g hat)) + dH with g = dY gamma, hat = h rstd; dgamma = sum of dY hat over the tokens.  A block walks
 // over rows, its waves keep their share of dgamma in registers, and the blocks' shares are added up by a second launch in block
 // order: the result depends on T and d alone.
-template <typename T, int W, int NC>
+template <typename T, int W, int NC, bool STREAM>
 __global__ __launch_bounds__(W == 1 ? 256 : W * 64) void norm_bwd_kernel(NormBwdArgs a) {
   constexpr int ROWS = W == 1 ? 4 : 1;
+  constexpr int N = Vec<T>::N, WIDTH = NC * N * 64;  // columns of a wave
   __shared__ float s_part[16];
-  __shared__ float s_gamma[W == 1 ? NC * 512 : 1];
+  __shared__ float s_gamma[W == 1 ? 4 : 1][W == 1 ? WIDTH : 1];
   const int at = W == 1 ? threadIdx.x & 63 : threadIdx.x;
   const int d = a.d;
   const T* const h = static_cast<const T*>(a.h);
   const T* const dY = static_cast<const T*>(a.dY);
   const T* const dH = static_cast<const T*>(a.dH);
   T* const dX = static_cast<T*>(a.dX);
-  Raw8<T> gamma[NC];
-  float share[NC][8];
+  Vec<T> gamma[NC];
+  float share[NC][N];
 #pragma unroll
   for (int i = 0; i < NC; ++i) {
-    const int col = (i * W * 64 + at) * 8;
-    load_some(gamma[i], static_cast<const T*>(a.gamma) + col, d - col, 0.f);
+    const int col = (i * W * 64 + at) * N;
+    gamma[i].load(static_cast<const T*>(a.gamma) + col, d - col, 0.f);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) share[i][j] = 0.f;
+    for (int j = 0; j < N; ++j) share[i][j] = 0.f;
   }
   for (int64_t row = (int64_t)blockIdx.x * ROWS + (W == 1 ? threadIdx.x >> 6 : 0); row < a.T; row += (int64_t)gridDim.x * ROWS) {
     const int64_t first = row * d;
-    Raw8<T> hv[NC], dy[NC], dh[NC];
+    Vec<T> hv[NC], dy[NC], dh[NC];
     const float rstd = a.rstd[row];
 #pragma unroll
     for (int i = 0; i < NC; ++i) {
-      const int col = (i * W * 64 + at) * 8;
-      load_some(hv[i], h + first + col, d - col, 0.f);
-      load_some(dy[i], dY + first + col, d - col, 0.f);
-      if (dH) load_some(dh[i], dH + first + col, d - col, 0.f);
+      const int col = (i * W * 64 + at) * N;
+      hv[i].template load<STREAM>(h + first + col, d - col, 0.f);
+      dy[i].template load<STREAM>(dY + first + col, d - col, 0.f);
+      if (dH && W < 16) dh[i].template load<STREAM>(dH + first + col, d - col, 0.f);
     }
     float dot = 0.f;
 #pragma unroll
-    for (int i = 0; i < NC; ++i)
+    for (int i = 0; i < NC; ++i) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
+      for (int j = 0; j < N; ++j) {
         const float t = dy[i][j] * (hv[i][j] * rstd);
         share[i][j] += t;
         dot += t * gamma[i][j];
       }
-    dot = row_sum<W>(dot, s_part) / (float)d;
+    }
+    // (the row waits in the form it was loaded in: bf16 as float32 takes 201 registers at NC = 4 where 156 do, and fewer waves fit)
 #pragma unroll
     for (int i = 0; i < NC; ++i) {
-      const int col = (i * W * 64 + at) * 8;
-      Raw8<T> out;
+      hv[i].forget();
+      dy[i].forget();
+      gamma[i].forget();
+    }
+    dot = row_sum<W>(dot, s_part) / (float)d;
+    const float k = rstd * rstd * dot;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        float v = rstd * (dy[i][j] * gamma[i][j] - hv[i][j] * rstd * dot);
+    for (int i = 0; i < NC; ++i) {
+      const int col = (i * W * 64 + at) * N;
+      if (dH && W == 16) dh[i].template load<STREAM>(dH + first + col, d - col, 0.f);  // (128 registers do not hold it with the rest)
+      Vec<T> out;
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        float v = (rstd * gamma[i][j]) * dy[i][j] - hv[i][j] * k;
         if (dH) v += dh[i][j];
         out.set(j, v);
       }
-      store_some(out, dX + first + col, d - col);
+      out.store(dX + first + col, d - col);
     }
   }
   float* const part = a.part + (int64_t)blockIdx.x * d;
   if constexpr (W == 1) {
-    const int wave = threadIdx.x >> 6;
-#pragma unroll 1
-    for (int w = 0; w < 4; ++w) {
-      if (wave == w) {
 #pragma unroll
-        for (int i = 0; i < NC; ++i)
+    for (int i = 0; i < NC; ++i)
 #pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            float* const p = s_gamma + (i * 8 + j) * 64 + at;
-            *p = w == 0 ? share[i][j] : *p + share[i][j];
-          }
-      }
-      __syncthreads();
+      for (int j = 0; j < N; ++j) s_gamma[threadIdx.x >> 6][(i * N + j) * 64 + at] = share[i][j];
+    __syncthreads();
+    for (int c = threadIdx.x; c < d; c += 256) {
+      const int k = (c / (64 * N) * N + c % N) * 64 + c / N % 64;
+      part[c] = (s_gamma[0][k] + s_gamma[1][k]) + (s_gamma[2][k] + s_gamma[3][k]);
     }
-    for (int c = threadIdx.x; c < d; c += 256) part[c] = s_gamma[((c >> 9) * 8 + (c & 7)) * 64 + ((c >> 3) & 63)];
   } else {
 #pragma unroll
     for (int i = 0; i < NC; ++i) {
-      const int col = (i * W * 64 + at) * 8;
+      const int col = (i * W * 64 + at) * N;
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
+      for (int j = 0; j < N; ++j)
         if (col + j < d) part[col + j] = share[i][j];
     }
   }
 }
 
-// 64 columns per block; sixteen rows of threads share the blocks' shares, then one adds up their sums
+// sixteen columns per block: 64 rows of threads share the blocks' shares, and their sums are added up in two steps
 __global__ __launch_bounds__(1024) void norm_dgamma_kernel(const float* __restrict__ part, int blocks, int d, int accumulate, float* __restrict__ dgamma) {
-  __shared__ float s[16][64];
-  const int lane = threadIdx.x & 63, r = threadIdx.x >> 6;
-  const int col = blockIdx.x * 64 + lane;
+  __shared__ float s[64][17];
+  const int c = threadIdx.x & 15, r = threadIdx.x >> 4;
+  const int col = blockIdx.x * 16 + c;
   float v = 0.f;
-  if (col < d)
-    for (int b = r; b < blocks; b += 16) v += part[(int64_t)b * d + col];
-  s[r][lane] = v;
+  if (col < d) {
+#pragma unroll 4
+    for (int b = r; b < blocks; b += 64) v += part[(int64_t)b * d + col];
+  }
+  s[r][c] = v;
   __syncthreads();
-  if (r == 0 && col < d) {
+  if (r < 4) {
+    v = 0.f;
 #pragma unroll
-    for (int i = 1; i < 16; ++i) v += s[i][lane];
-    dgamma[col] = accumulate ? dgamma[col] + v : v;
+    for (int i = 0; i < 16; ++i) v += s[r * 16 + i][c];
+    v += __shfl_xor(v, 16, 64);
+    v += __shfl_xor(v, 32, 64);
+    if (r == 0 && col < d) dgamma[col] = accumulate ? dgamma[col] + v : v;
   }
 }
+
+// Tensors of 64 MB and more are read with the non-temporal hint: neither this nor another operator's caches will hold them.  us
+// without / with it, d = 2048, bf16: 32768 tokens forward 91.7 / 90.6, into e4m3 81.7 / 74.3, backward 100 / 97; 16384 tokens (64
+// MB) 48.9 / 45.0, 43.4 / 40.6; 8192 tokens 25.3 / 26.0, 20.1 / 23.4; 4096 tokens, whose inputs are in the caches, 11.1 / 15.1.  h is stored
+// with the hint at every size (nothing reads it before the next norm or the backward pass: 8192 tokens into e4m3 25.0 / 20.1, forward
+// and the router behind it 53.1 / 51.2), y without (the router reads it next: 4096 tokens, both 41.1 / 47.1).
+constexpr int64_t STREAM_BYTES = (int64_t)64 << 20;
 
 template <typename T, int W, int NC>
 hipError_t norm_fwd(const NormFwdArgs& a, hipStream_t s) {
   const int64_t blocks = W == 1 ? (a.T + 3) / 4 : a.T;
-  hipLaunchKernelGGL((norm_fwd_kernel<T, W, NC>), dim3((unsigned)(blocks < 4096 ? blocks : 4096)), dim3(W == 1 ? 256 : W * 64), 0, s, a);
+  const dim3 grid((unsigned)(blocks < 8192 ? blocks : 8192)), block(W == 1 ? 256 : W * 64);
+  if (a.T * a.d * (int64_t)sizeof(T) >= STREAM_BYTES) hipLaunchKernelGGL((norm_fwd_kernel<T, W, NC, true>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((norm_fwd_kernel<T, W, NC, false>), grid, block, 0, s, a);
   return hipGetLastError();
 }
+// (vectors of a thread: float32 has twice as many of them in a row)
 template <typename T>
 hipError_t norm_fwd_any(const NormFwdArgs& a, hipStream_t s) {
+  constexpr int X = 8 / Vec<T>::N;
   const int chunks = (a.d + 7) / 8;
   const bool few = a.T < 1024;
-  if (chunks <= 64) return norm_fwd<T, 1, 1>(a, s);
-  if (chunks <= 128) return norm_fwd<T, 1, 2>(a, s);
-  if (!few && chunks <= 256) return norm_fwd<T, 1, 4>(a, s);
-  if (chunks <= 256) return norm_fwd<T, 4, 1>(a, s);
-  if (chunks <= 512) return norm_fwd<T, 4, 2>(a, s);
-  if (chunks <= 1024) return norm_fwd<T, 4, 4>(a, s);
-  return norm_fwd<T, 16, 2>(a, s);
+  if (chunks <= 64) return norm_fwd<T, 1, X>(a, s);
+  if (chunks <= 128) return norm_fwd<T, 1, 2 * X>(a, s);
+  if (!few && chunks <= 256) return norm_fwd<T, 1, 4 * X>(a, s);
+  if (chunks <= 256) return norm_fwd<T, 4, X>(a, s);
+  if (chunks <= 512) return norm_fwd<T, 4, 2 * X>(a, s);
+  if (chunks <= 1024) return norm_fwd<T, 4, 4 * X>(a, s);
+  return norm_fwd<T, 16, 2 * X>(a, s);
 }
 
 template <typename T, int W, int NC>
 hipError_t norm_bwd(const NormBwdArgs& a, hipStream_t s) {
   const int blocks = norm_bwd_blocks(a.T, a.d);
-  hipLaunchKernelGGL((norm_bwd_kernel<T, W, NC>), dim3(blocks), dim3(W == 1 ? 256 : W * 64), 0, s, a);
+  const dim3 grid(blocks), block(W == 1 ? 256 : W * 64);
+  if (a.T * a.d * (int64_t)sizeof(T) >= STREAM_BYTES) hipLaunchKernelGGL((norm_bwd_kernel<T, W, NC, true>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((norm_bwd_kernel<T, W, NC, false>), grid, block, 0, s, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(norm_dgamma_kernel, dim3((a.d + 63) / 64), dim3(1024), 0, s, a.part, blocks, a.d, a.accumulate, a.dgamma);
+  hipLaunchKernelGGL(norm_dgamma_kernel, dim3((a.d + 15) / 16), dim3(1024), 0, s, a.part, blocks, a.d, a.accumulate, a.dgamma);
   return hipGetLastError();
 }
-constexpr int BWD_ONE_WAVE_CHUNKS = 256;  // rows of at most so many chunks belong to one wave
+constexpr int BWD_ONE_WAVE_CHUNKS = 256;  // rows of at most so many eights belong to one wave
 template <typename T>
 hipError_t norm_bwd_any(const NormBwdArgs& a, hipStream_t s) {
+  constexpr int X = 8 / Vec<T>::N;
   const int chunks = (a.d + 7) / 8;
-  if (chunks <= 64) return norm_bwd<T, 1, 1>(a, s);
-  if (chunks <= 128) return norm_bwd<T, 1, 2>(a, s);
-  if (chunks <= BWD_ONE_WAVE_CHUNKS) return norm_bwd<T, 1, 4>(a, s);
-  if (chunks <= 512) return norm_bwd<T, 4, 2>(a, s);
-  if (chunks <= 1024) return norm_bwd<T, 4, 4>(a, s);
-  return norm_bwd<T, 16, 2>(a, s);
+  if (chunks <= 64) return norm_bwd<T, 1, X>(a, s);
+  if (chunks <= 128) return norm_bwd<T, 1, 2 * X>(a, s);
+  if (chunks <= BWD_ONE_WAVE_CHUNKS) return norm_bwd<T, 1, 4 * X>(a, s);
+  if (chunks <= 512) return norm_bwd<T, 4, 2 * X>(a, s);
+  if (chunks <= 1024) return norm_bwd<T, 4, 4 * X>(a, s);
+  return norm_bwd<T, 16, 2 * X>(a, s);
 }
 }  // namespace
 

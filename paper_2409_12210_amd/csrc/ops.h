@@ -62,50 +62,49 @@ struct LogprobsBwdArgs {
 hipError_t launch_logprobs_bwd(modse_dtype dt, const LogprobsBwdArgs& a, hipStream_t s);
 
 // ---------------------------------------------------------------- rows of any alignment
-// Eight elements of a row that starts anywhere: gfx950 takes 16-byte accesses at the alignment of the element, so a row of
-// odd length needs no path of its own.  `n`: elements that there are (the rest reads 0).
-typedef f32x4 f32x4_u __attribute__((aligned(4)));
-typedef bf16x8 bf16x8_u __attribute__((aligned(2)));
-template <typename T> struct Raw8;
-template <> struct Raw8<float> {
-  f32x4 a, b;
-  __device__ __forceinline__ void load(const float* p) {
-    a = *reinterpret_cast<const f32x4_u*>(p);
-    b = *reinterpret_cast<const f32x4_u*>(p + 4);
+// Sixteen bytes of a row that starts anywhere: gfx950 takes such accesses at the alignment of the element, so a row of odd length
+// needs no path of its own.  Neighbouring lanes take neighbouring vectors.  (Eight float32 per lane, in two loads half of whose
+// bytes lie between the other's, read 4096 x 4096 with the non-temporal hint at 4.7 TB/s; this way 5.4.)
+template <typename T> struct VecOf;
+template <> struct VecOf<float> { typedef f32x4 type; };
+template <> struct VecOf<bf16_t> { typedef bf16x8 type; };
+template <typename T>
+struct Vec {
+  static constexpr int N = 16 / sizeof(T);
+  typedef typename VecOf<T>::type V;
+  typedef V V_u __attribute__((aligned(sizeof(T))));
+  V v;
+  __device__ __forceinline__ float operator[](int i) const { return (float)v[i]; }
+  __device__ __forceinline__ void set(int i, float x) { v[i] = (T)x; }
+  // what was computed from it is not kept in registers
+  __device__ __forceinline__ void forget() {
+    u32x4 t = __builtin_bit_cast(u32x4, v);
+    asm volatile("" : "+v"(t));
+    v = __builtin_bit_cast(V, t);
   }
-  __device__ __forceinline__ float operator[](int i) const { return i < 4 ? a[i] : b[i - 4]; }
-  __device__ __forceinline__ void set(int i, float v) { if (i < 4) a[i] = v; else b[i - 4] = v; }
-  __device__ __forceinline__ void store(float* p) const {
-    *reinterpret_cast<f32x4_u*>(p) = a;
-    *reinterpret_cast<f32x4_u*>(p + 4) = b;
+  // the first n elements that there are from p on; the others become `rest`.  STREAM: with the non-temporal hint
+  template <bool STREAM = false>
+  __device__ __forceinline__ void load(const T* p, int n, float rest) {
+    if (n >= N) {
+      if constexpr (STREAM) v = __builtin_nontemporal_load(reinterpret_cast<const V_u*>(p));
+      else v = *reinterpret_cast<const V_u*>(p);
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) v[i] = i < n ? p[i] : (T)rest;
+    }
+  }
+  template <bool STREAM = false>
+  __device__ __forceinline__ void store(T* p, int n) const {
+    if (n >= N) {
+      if constexpr (STREAM) __builtin_nontemporal_store(v, reinterpret_cast<V_u*>(p));
+      else *reinterpret_cast<V_u*>(p) = v;
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        if (i < n) p[i] = v[i];
+    }
   }
 };
-template <> struct Raw8<bf16_t> {
-  bf16x8 a;
-  __device__ __forceinline__ void load(const bf16_t* p) { a = *reinterpret_cast<const bf16x8_u*>(p); }
-  __device__ __forceinline__ float operator[](int i) const { return (float)a[i]; }
-  __device__ __forceinline__ void set(int i, float v) { a[i] = (bf16_t)v; }
-  __device__ __forceinline__ void store(bf16_t* p) const { *reinterpret_cast<bf16x8_u*>(p) = a; }
-};
-template <typename T>
-__device__ __forceinline__ void load_some(Raw8<T>& r, const T* p, int n, float rest) {
-  if (n >= 8) {
-    r.load(p);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) r.set(i, i < n ? (float)p[i] : rest);
-  }
-}
-template <typename T>
-__device__ __forceinline__ void store_some(const Raw8<T>& r, T* p, int n) {
-  if (n >= 8) {
-    r.store(p);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (i < n) p[i] = (T)r[i];
-  }
-}
 
 // ---------------------------------------------------------------- reductions over a wave by lane permutes of the vector unit
 template <int CTRL, int ROWS = 0xf>
@@ -134,11 +133,12 @@ __device__ __forceinline__ float wave_max(float v) {
   v = fmaxf(v, dpp_f32<0x143, 0xc>(v, v));
   return lane_f32(v, 63);
 }
-// the maximum of every aligned group of 4, 8 or 16 lanes, in all of them
+// the maximum of every aligned group of 4, 8, 16 or 32 lanes, in all of them
 __device__ __forceinline__ float group_max(float v, int lanes) {
   v = fmaxf(v, dpp_f32<0xb1>(v, v));    // lane ^ 1
   v = fmaxf(v, dpp_f32<0x4e>(v, v));    // lane ^ 2
   if (lanes >= 8) v = fmaxf(v, dpp_f32<0x141>(v, v));   // 7 - lane: the other half of eight
   if (lanes >= 16) v = fmaxf(v, dpp_f32<0x140>(v, v));  // 15 - lane
+  if (lanes >= 32) v = fmaxf(v, __shfl_xor(v, 16, 64));
   return v;
 }

@@ -83,7 +83,7 @@ __global__ __launch_bounds__(256) void ortho_squares_kernel(const Mat* __restric
     double v = 0;
     for (int64_t i = (int64_t)part * PART + threadIdx.x * 4; i < end; i += 1024) {
       if (i + 4 <= end) {
-        const f32x4 g = *reinterpret_cast<const f32x4_u*>(G + i);
+        const f32x4 g = *reinterpret_cast<const Vec<float>::V_u*>(G + i);
 #pragma unroll
         for (int j = 0; j < 4; ++j) v += (double)g[j] * g[j];
       } else {
@@ -230,7 +230,7 @@ __global__ __launch_bounds__(256) void ortho_start_kernel(const Mat* __restrict_
       const int64_t first = (int64_t)(r0 + r) * m.cols + c0 + at * 4;
       if (r0 + r < m.rows) {
         if (c0 + at * 4 + 4 <= m.cols) {
-          g = *reinterpret_cast<const f32x4_u*>(m.G + first);
+          g = *reinterpret_cast<const Vec<float>::V_u*>(m.G + first);
         } else {
 #pragma unroll
           for (int j = 0; j < 4; ++j)

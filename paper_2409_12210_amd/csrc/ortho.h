@@ -42,8 +42,10 @@ __host__ __device__ inline double quintic_bound(double a, double b, double c, do
   return most;
 }
 
-// One matrix of the set, in device memory.
+// One matrix of the set, in device memory.  Tile lists hold copies, so that a workgroup knows all it needs after one load.
 struct alignas(128) Mat {
+  int32_t which;  // its place in the set
+  int32_t mt, nt; // in a tile list: the tile's row and column
   const float* G;
   void* U;
   char* X[2];     // [mp, np] stored pairs
@@ -62,7 +64,7 @@ struct Factors {
 }  // namespace modse_ortho
 
 struct OrthoLayout {
-  size_t mats, bounds, factors, squares, sums, square_map, update_map, data, total;
+  size_t mats, bounds, factors, squares, sums, square_list, update_list, data, total;
   int32_t square_tiles, update_tiles, parts;
   int32_t tile, n_slots;
   int32_t group[modse_ortho::MAX_STEPS];  // steps of every group of them

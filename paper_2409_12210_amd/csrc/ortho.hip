@@ -52,6 +52,8 @@ __global__ __launch_bounds__(64) void ortho_table_kernel(MatArgs a) {
   if (i >= a.count) return;
   const MatArg& t = a.mat[i];
   Mat m;
+  m.which = a.first + i;
+  m.mt = m.nt = 0;
   m.G = t.G;
   m.U = t.U;
   m.rows = t.rows;
@@ -71,7 +73,7 @@ __global__ __launch_bounds__(64) void ortho_table_kernel(MatArgs a) {
   a.table[a.first + i] = m;
 }
 
-constexpr int PART = 1 << 15;  // elements of a partial sum of squares
+constexpr int PART = 1 << 13;  // elements of a partial sum of squares
 // (float64: no overflow, and the order of the additions is of no account)
 __global__ __launch_bounds__(256) void ortho_squares_kernel(const Mat* __restrict__ table, double* __restrict__ sums) {
   __shared__ double s[4];
@@ -81,15 +83,14 @@ __global__ __launch_bounds__(256) void ortho_squares_kernel(const Mat* __restric
   for (int part = blockIdx.x; part < m.parts; part += gridDim.x) {
     const int64_t end = min(n, ((int64_t)part + 1) * PART);
     double v = 0;
-    for (int64_t i = (int64_t)part * PART + threadIdx.x * 4; i < end; i += 1024) {
-      if (i + 4 <= end) {
-        const f32x4 g = *reinterpret_cast<const Vec<float>::V_u*>(G + i);
+    const int64_t first = (int64_t)part * PART + threadIdx.x * 4;
+    Vec<float> g[PART / 1024];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) v += (double)g[j] * g[j];
-      } else {
-        for (int64_t j = i; j < end; ++j) v += (double)G[j] * G[j];
-      }
-    }
+    for (int i = 0; i < PART / 1024; ++i) g[i].load(G + first + i * 1024, (int)(end - first - i * 1024), 0.f);
+#pragma unroll
+    for (int i = 0; i < PART / 1024; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v += (double)g[i][j] * g[i][j];
     for (int b = 32; b; b >>= 1) v += __shfl_xor(v, b, 64);
     if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = v;
     __syncthreads();
@@ -117,7 +118,7 @@ struct Bound {
 // One block per matrix: the norm, the factor of the first product, the matrix's part of the tile lists.
 __global__ __launch_bounds__(256) void ortho_prepare_kernel(const Mat* __restrict__ table, const double* __restrict__ sums, float eps,
                                                             Bound* __restrict__ bounds, Factors* __restrict__ gram,
-                                                            int tile, int32_t* __restrict__ square_map, int32_t* __restrict__ update_map) {
+                                                            int tile, Mat* __restrict__ square_list, Mat* __restrict__ update_list) {
   __shared__ double s[4];
   const Mat& m = table[blockIdx.x];
   double v = 0;
@@ -126,8 +127,20 @@ __global__ __launch_bounds__(256) void ortho_prepare_kernel(const Mat* __restric
   if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = v;
   __syncthreads();
   const int mt = (m.m + tile - 1) / tile, nt = (m.n + tile - 1) / tile;
-  for (int i = threadIdx.x; i < mt * (mt + 1) / 2; i += 256) square_map[m.square_tile + i] = blockIdx.x;
-  for (int i = threadIdx.x; i < mt * nt; i += 256) update_map[m.update_tile + i] = blockIdx.x;
+  Mat t = m;
+  for (int i = threadIdx.x; i < mt * (mt + 1) / 2; i += 256) {  // row by row of the triangle
+    t.mt = (int)((sqrtf(8.f * i + 1.f) - 1.f) * 0.5f);
+    while ((t.mt + 1) * (t.mt + 2) / 2 <= i) ++t.mt;
+    while (t.mt * (t.mt + 1) / 2 > i) --t.mt;
+    t.nt = i - t.mt * (t.mt + 1) / 2;
+    square_list[m.square_tile + i] = t;
+  }
+  for (int i = threadIdx.x; i < mt * nt; i += 256) {  // columns of eight tiles
+    const int group = i / (8 * nt), height = min(8, mt - group * 8), in = i - group * 8 * nt;
+    t.mt = group * 8 + in % height;
+    t.nt = in / height;
+    update_list[m.update_tile + i] = t;
+  }
   if (threadIdx.x != 0) return;
   const double norm = sqrt((s[0] + s[1]) + (s[2] + s[3]));
   const double inv = norm == 0 ? 0 : 1 / (norm + eps);
@@ -204,11 +217,6 @@ __device__ __forceinline__ void store_pair(char* p, const float (&v)[4]) {  // f
   *reinterpret_cast<half4*>(p) = hi;
   *reinterpret_cast<half4*>(p + 64) = lo;
 }
-__device__ __forceinline__ void load_pair(const char* p, float (&v)[4]) {
-  const half4 hi = *reinterpret_cast<const half4*>(p), lo = *reinterpret_cast<const half4*>(p + 64);
-#pragma unroll
-  for (int j = 0; j < 4; ++j) v[j] = (float)hi[j] + (float)lo[j];
-}
 // byte of the hi part of column c of a row
 __device__ __forceinline__ int pair_byte(int c) { return (c >> 5) * 128 + (c & 31) * 2; }
 
@@ -265,8 +273,8 @@ __global__ __launch_bounds__(256) void ortho_start_kernel(const Mat* __restrict_
 // A step is 32 of K: a panel row is 64 bytes of hi and 64 of lo, and every fragment feeds two or one of the three products: 96
 // matrix instructions of 16 x 16 x 32 cycles' worth per 32 KiB of panels, half as many loads per instruction as a plain 16-bit
 // product of this tile has.  Two workgroups share a CU (TILE 128, two stages of panels), so that one multiplies while the other
-// waits.  Sets with few tiles take TILE 64 and four stages: there is nothing else on the CU then, and a step lasts as long as
-// its loads unless they are under way early.
+// waits.  Sets with few tiles take TILE 64 and five stages: there is nothing else on the CU then, and a step lasts as long
+// as its loads unless they are under way early.
 enum Out { OUT_PAIRS, OUT_F32, OUT_BF16 };
 constexpr int BK = 32;
 constexpr int JOIN = 16;  // steps that are summed in one register
@@ -277,8 +285,7 @@ struct SquareOp {
   int32_t sum;            // the squares of C are summed
 };
 struct ProductArgs {
-  const Mat* table;
-  const int32_t* map;
+  const Mat* list;
   SquareOp op[2];         // blockIdx.y
   const Bound* bounds;
   float* squares;         // sums of the squares of a result's tiles, as stored
@@ -298,32 +305,28 @@ __global__ __launch_bounds__(256, 2) void ortho_product_kernel(ProductArgs a) {
   // (workgroups go to the XCDs in turn)
   const int tile = ((int)(blockIdx.x / 8) / RUN * 8 + (int)(blockIdx.x % 8)) * RUN + (int)(blockIdx.x / 8) % RUN;
   if (tile >= a.tiles) return;
-  const SquareOp& op = a.op[SQUARES ? blockIdx.y : 0];
-  const int which = uniform_int(a.map[tile]);
-  const Mat& m = a.table[which];
-  const int mp = m.mp, np = m.np;
+  // (All that is needed of the table, now: what is read through a reference later is read again behind every barrier, one round
+  // trip after the other.)
+  const int side = SQUARES ? blockIdx.y : 0;
+  const SquareOp& o = a.op[side];
+  const int op_p = o.p, op_q = o.q, op_e = o.e, op_f = o.f, op_c = o.c, op_sum = o.sum;
+  const Mat& m = a.list[tile];
+  const int which = m.which, rows = m.rows, cols = m.cols, mp = m.mp, np = m.np, mt = m.mt, nt = m.nt;
+  char *const X0 = m.X[0], *const X1 = m.X[1], *const slots = m.slot;
+  void* const result = m.U;
+  const Factors* const pf = o.factors + which;
+  const float f_product = pf->product, f_first = pf->first, f_second = pf->second;
+  const float out = OUT == OUT_PAIRS ? 1.f : a.bounds[which].out;
+  const int mm = min(rows, cols), mn = max(rows, cols);
+  const char* const X = a.x ? X1 : X0;
+  char* const other = a.x ? X0 : X1;
   const size_t slot = (size_t)mp * mp * 4;
-  const bool gram = SQUARES && op.p < 0;
-  int mt, nt;
-  if constexpr (SQUARES) {  // row by row of the triangle
-    const int t = tile - m.square_tile;
-    mt = (int)((sqrtf(8.f * t + 1.f) - 1.f) * 0.5f);
-    while ((mt + 1) * (mt + 2) / 2 <= t) ++mt;
-    while (mt * (mt + 1) / 2 > t) --mt;
-    mt = uniform_int(mt);
-    nt = uniform_int(t - mt * (mt + 1) / 2);
-  } else {  // columns of eight tiles
-    const int t = tile - m.update_tile, rows = (m.m + TILE - 1) / TILE, cols = (m.n + TILE - 1) / TILE;
-    const int group = t / (8 * cols), height = min(8, rows - group * 8), in = t - group * 8 * cols;
-    mt = uniform_int(group * 8 + in % height);
-    nt = uniform_int(in / height);
-  }
+  const bool gram = SQUARES && op_p < 0;
   const int m0 = mt * TILE, n0 = nt * TILE;
-  const int K = gram ? m.n : m.m, steps = (K + BK - 1) / BK;
-  const char* const X = m.X[a.x];
+  const int K = gram ? mn : mm, steps = (K + BK - 1) / BK;
   const int ldp = (gram ? np : mp) * 4, ldq = (gram || !SQUARES ? np : mp) * 4;  // bytes
-  const char* const P = gram ? X : m.slot + op.p * slot;
-  const char* const Q = gram || !SQUARES ? X : m.slot + op.q * slot;
+  const char* const P = gram ? X : slots + op_p * slot;
+  const char* const Q = gram || !SQUARES ? X : slots + op_q * slot;
 
   // ---- loads: units of 1 KiB, landing swizzled (16-byte chunks of a row XOR-ed)
   uint32_t offp[UNITS], offq[UNITS];
@@ -395,8 +398,8 @@ __global__ __launch_bounds__(256, 2) void ortho_product_kernel(ProductArgs a) {
   for (int g = 0; g < steps; ++g) {
     // this step's panels are there (those of the next STAGES - 2 may be on their way) and the last one's have been read
     constexpr int YOUNGER = (STAGES - 2) * 2 * UNITS;
-    static_assert(YOUNGER < 16, "low bits of the vmcnt field");
-    if (YOUNGER > 0 && g + STAGES - 2 < steps) __builtin_amdgcn_s_waitcnt(0x0070 | YOUNGER);
+    static_assert(YOUNGER < 64, "vmcnt field");
+    if (YOUNGER > 0 && g + STAGES - 2 < steps) __builtin_amdgcn_s_waitcnt(0x0070 | (YOUNGER & 15) | (YOUNGER >> 4) << 14);
     else __builtin_amdgcn_s_waitcnt(0x0070);
     asm volatile("" ::: "memory");
     __builtin_amdgcn_s_barrier();
@@ -428,12 +431,36 @@ __global__ __launch_bounds__(256, 2) void ortho_product_kernel(ProductArgs a) {
   join(false);
 
   // ---- result: a lane holds row l16 and columns 4 kq + 0..3 of every block
-  const Factors f = op.factors[which];
-  const char* const E = SQUARES ? (op.e >= 0 ? m.slot + op.e * slot : nullptr) : X;
-  const char* const F = SQUARES && op.f >= 0 ? m.slot + op.f * slot : nullptr;
+  const char* const E = SQUARES ? (op_e >= 0 ? slots + op_e * slot : nullptr) : X;
+  const char* const F = SQUARES && op_f >= 0 ? slots + op_f * slot : nullptr;
   const int ldc = (SQUARES ? mp : np) * 4;
-  char* const C = SQUARES ? m.slot + op.c * slot : m.X[1 - a.x];
+  char* const C = SQUARES ? slots + op_c * slot : other;
   const bool mirror = SQUARES && mt != nt;
+  const size_t corner = (size_t)(m0 + wm * W) * ldc + pair_byte(n0 + wn * W);
+  auto at = [&](int i, int j) { return (uint32_t)((i * 16 + l16) * ldc + pair_byte(j * 16 + kq * 4)); };
+#pragma unroll
+  for (int i = 0; i < NB; ++i)
+#pragma unroll
+    for (int j = 0; j < NB; ++j) total[i][j] *= f_product;
+  // (all loads of a matrix together: one after the other they took 0.7 us each, 11 us of a tile)
+  auto add = [&](const char* from, float factor) {
+    half4 hi[NB][NB], lo[NB][NB];
+#pragma unroll
+    for (int i = 0; i < NB; ++i)
+#pragma unroll
+      for (int j = 0; j < NB; ++j) {
+        hi[i][j] = *reinterpret_cast<const half4*>(from + corner + at(i, j));
+        lo[i][j] = *reinterpret_cast<const half4*>(from + corner + at(i, j) + 64);
+      }
+#pragma unroll
+    for (int i = 0; i < NB; ++i)
+#pragma unroll
+      for (int j = 0; j < NB; ++j)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) total[i][j][k] += factor * ((float)hi[i][j][k] + (float)lo[i][j][k]);
+  };
+  if (E) add(E, f_first);
+  if (F) add(F, f_second);
   float sum = 0.f;
   if (mirror) __syncthreads();  // the ring has been read
 #pragma unroll
@@ -441,16 +468,11 @@ __global__ __launch_bounds__(256, 2) void ortho_product_kernel(ProductArgs a) {
 #pragma unroll
     for (int j = 0; j < NB; ++j) {
       const int r = wm * W + i * 16 + l16, c = wn * W + j * 16 + kq * 4;
-      const size_t byte = (size_t)(m0 + r) * ldc + pair_byte(n0 + c);
-      float v[4] = {0.f, 0.f, 0.f, 0.f}, w[4] = {0.f, 0.f, 0.f, 0.f};
-      if (E) load_pair(E + byte, v);
-      if (F) load_pair(F + byte, w);
-#pragma unroll
-      for (int k = 0; k < 4; ++k) v[k] = (f.first * v[k] + f.second * w[k]) + f.product * total[i][j][k];
+      const float v[4] = {total[i][j][0], total[i][j][1], total[i][j][2], total[i][j][3]};
       if constexpr (OUT == OUT_PAIRS) {
-        store_pair(C + byte, v);
+        store_pair(C + corner + at(i, j), v);
         if constexpr (SQUARES) {
-          if (op.sum)
+          if (op_sum)
 #pragma unroll
             for (int k = 0; k < 4; ++k) sum += v[k] * v[k];
           if (mirror)  // transposed, chunks of four rows XOR-ed with the column, so that the lanes meet all banks
@@ -460,13 +482,24 @@ __global__ __launch_bounds__(256, 2) void ortho_product_kernel(ProductArgs a) {
         }
       } else {
         typedef std::conditional_t<OUT == OUT_F32, float, bf16_t> T;
-        T* const U = static_cast<T*>(m.U);
-        const float out = a.bounds[which].out;
-        const bool tall = m.rows > m.cols;
-        if (m0 + r < m.m) {
+        typedef T T4 __attribute__((ext_vector_type(4)));
+        typedef T4 T4_u __attribute__((aligned(sizeof(T))));
+        T4 u;
 #pragma unroll
-          for (int k = 0; k < 4; ++k)
-            if (n0 + c + k < m.n) U[tall ? (int64_t)(n0 + c + k) * m.cols + m0 + r : (int64_t)(m0 + r) * m.cols + n0 + c + k] = (T)(v[k] * out);
+        for (int k = 0; k < 4; ++k) u[k] = (T)(v[k] * out);
+        T* const U = static_cast<T*>(result);
+        if (m0 + r < mm) {
+          if (rows > cols) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              if (n0 + c + k < mn) U[(int64_t)(n0 + c + k) * cols + m0 + r] = u[k];
+          } else if (n0 + c + 4 <= mn) {
+            *reinterpret_cast<T4_u*>(U + (int64_t)(m0 + r) * cols + n0 + c) = u;
+          } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              if (n0 + c + k < mn) U[(int64_t)(m0 + r) * cols + n0 + c + k] = u[k];
+          }
         }
       }
     }
@@ -481,7 +514,7 @@ __global__ __launch_bounds__(256, 2) void ortho_product_kernel(ProductArgs a) {
         store_pair(C + (size_t)(n0 + c) * ldc + pair_byte(m0 + r4 * 4), v);
       }
     }
-    if (op.sum) {
+    if (op_sum) {
       __syncthreads();
       float* const part = reinterpret_cast<float*>(s_ring);
       sum = wave_sum(sum);
@@ -537,8 +570,8 @@ modse_status ortho_layout(const modse_matrix_set* set, const float* coeffs, int 
   w.factors = take((size_t)n * 6 * sizeof(Factors));
   w.squares = take((size_t)square[1] * 4);
   w.sums = take((size_t)parts * sizeof(double));
-  w.square_map = take((size_t)square[1] * 4);
-  w.update_map = take((size_t)update[1] * 4);
+  w.square_list = take((size_t)square[1] * sizeof(Mat));
+  w.update_list = take((size_t)update[1] * sizeof(Mat));
   w.data = take(data);
   w.total = n ? off : 0;
   w.n_groups = 0;
@@ -571,8 +604,8 @@ hipError_t launch_orthogonalize(const modse_matrix_set* set, const OrthoLayout& 
           *const f_next = factors + 4 * n, *const f_update = factors + 5 * n;
   float* const squares = reinterpret_cast<float*>(ws + w.squares);
   double* const sums = reinterpret_cast<double*>(ws + w.sums);
-  int32_t* const square_map = reinterpret_cast<int32_t*>(ws + w.square_map);
-  int32_t* const update_map = reinterpret_cast<int32_t*>(ws + w.update_map);
+  Mat* const square_list = reinterpret_cast<Mat*>(ws + w.square_list);
+  Mat* const update_list = reinterpret_cast<Mat*>(ws + w.update_list);
   int32_t square = 0, update = 0, part = 0, most_parts = 0, most_tiles = 0;
   int64_t data = 0;
   hipError_t e;
@@ -599,31 +632,31 @@ hipError_t launch_orthogonalize(const modse_matrix_set* set, const OrthoLayout& 
   }
   hipLaunchKernelGGL(ortho_squares_kernel, dim3(most_parts < 1024 ? most_parts : 1024, n), dim3(256), 0, s, table, sums);
   if ((e = hipGetLastError()) != hipSuccess) return e;
-  hipLaunchKernelGGL(ortho_prepare_kernel, dim3(n), dim3(256), 0, s, table, sums, eps, bounds, f_gram, tile, square_map, update_map);
+  hipLaunchKernelGGL(ortho_prepare_kernel, dim3(n), dim3(256), 0, s, table, sums, eps, bounds, f_gram, tile, square_list, update_list);
   if ((e = hipGetLastError()) != hipSuccess) return e;
   hipLaunchKernelGGL(ortho_start_kernel, dim3(most_tiles < 2048 ? most_tiles : 2048, n), dim3(256), 0, s, table, bounds);
   if ((e = hipGetLastError()) != hipSuccess) return e;
 
-  ProductArgs a = {table, square_map, {}, bounds, squares, 0, w.square_tiles};
+  ProductArgs a = {square_list, {}, bounds, squares, 0, w.square_tiles};
   auto grid = [](int tiles, int ops) { return dim3((tiles + 8 * RUN - 1) / (8 * RUN) * (8 * RUN), ops); };
   auto squares_of = [&](const SquareOp& one, const SquareOp* two) {
-    a.map = square_map;
+    a.list = square_list;
     a.tiles = w.square_tiles;
     a.op[0] = one;
     if (two) a.op[1] = *two;
     const dim3 g = grid(a.tiles, two ? 2 : 1);
     if (tile == 128) hipLaunchKernelGGL((ortho_product_kernel<128, 2, true, OUT_PAIRS>), g, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((ortho_product_kernel<64, 4, true, OUT_PAIRS>), g, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((ortho_product_kernel<64, 5, true, OUT_PAIRS>), g, dim3(256), 0, s, a);
     return hipGetLastError();
   };
   auto update_by = [&](int q, auto out) {
     constexpr Out OUT = decltype(out)::value;
-    a.map = update_map;
+    a.list = update_list;
     a.tiles = w.update_tiles;
     a.op[0] = {f_update, q, -1, -1, -1, -1, 0};
     const dim3 g = grid(a.tiles, 1);
     if (tile == 128) hipLaunchKernelGGL((ortho_product_kernel<128, 2, false, OUT>), g, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((ortho_product_kernel<64, 4, false, OUT>), g, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((ortho_product_kernel<64, 5, false, OUT>), g, dim3(256), 0, s, a);
     return hipGetLastError();
   };
   int step = 0;

@@ -47,40 +47,37 @@ struct MatArgs {
 };
 __host__ __device__ inline int padded(int v) { return (v + PAD - 1) / PAD * PAD; }
 
-__global__ __launch_bounds__(64) void ortho_table_kernel(MatArgs a) {
-  const int i = threadIdx.x;
-  if (i >= a.count) return;
-  const MatArg& t = a.mat[i];
-  Mat m;
-  m.which = a.first + i;
-  m.mt = m.nt = 0;
-  m.G = t.G;
-  m.U = t.U;
-  m.rows = t.rows;
-  m.cols = t.cols;
-  m.m = min(t.rows, t.cols);
-  m.n = max(t.rows, t.cols);
-  m.mp = padded(m.m);
-  m.np = padded(m.n);
-  const size_t x = (size_t)m.mp * m.np * 4;
-  m.X[0] = a.data + t.data;
-  m.X[1] = m.X[0] + x;
-  m.slot = m.X[1] + x;
-  m.square_tile = t.square_tile;
-  m.update_tile = t.update_tile;
-  m.part = t.part;
-  m.parts = t.parts;
-  a.table[a.first + i] = m;
-}
-
 constexpr int PART = 1 << 13;  // elements of a partial sum of squares
-// (float64: no overflow, and the order of the additions is of no account)
-__global__ __launch_bounds__(256) void ortho_squares_kernel(const Mat* __restrict__ table, double* __restrict__ sums) {
+// The table, and sums of squares in float64 (no overflow, and the order of the additions is of no account).  blockIdx.y: matrix.
+__global__ __launch_bounds__(256) void ortho_squares_kernel(MatArgs a, double* __restrict__ sums) {
   __shared__ double s[4];
-  const Mat& m = table[blockIdx.y];
-  const int64_t n = (int64_t)m.rows * m.cols;
-  const float* const G = m.G;
-  for (int part = blockIdx.x; part < m.parts; part += gridDim.x) {
+  const MatArg& t = a.mat[blockIdx.y];
+  const int parts = t.parts, part0 = t.part;
+  const int64_t n = (int64_t)t.rows * t.cols;
+  const float* const G = t.G;
+  if (blockIdx.x == 0 && threadIdx.x == 0) {
+    Mat m;
+    m.which = a.first + blockIdx.y;
+    m.mt = m.nt = 0;
+    m.G = t.G;
+    m.U = t.U;
+    m.rows = t.rows;
+    m.cols = t.cols;
+    m.m = min(t.rows, t.cols);
+    m.n = max(t.rows, t.cols);
+    m.mp = padded(m.m);
+    m.np = padded(m.n);
+    const size_t x = (size_t)m.mp * m.np * 4;
+    m.X[0] = a.data + t.data;
+    m.X[1] = m.X[0] + x;
+    m.slot = m.X[1] + x;
+    m.square_tile = t.square_tile;
+    m.update_tile = t.update_tile;
+    m.part = t.part;
+    m.parts = t.parts;
+    a.table[m.which] = m;
+  }
+  for (int part = blockIdx.x; part < parts; part += gridDim.x) {
     const int64_t end = min(n, ((int64_t)part + 1) * PART);
     double v = 0;
     const int64_t first = (int64_t)part * PART + threadIdx.x * 4;
@@ -94,7 +91,7 @@ __global__ __launch_bounds__(256) void ortho_squares_kernel(const Mat* __restric
     for (int b = 32; b; b >>= 1) v += __shfl_xor(v, b, 64);
     if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = v;
     __syncthreads();
-    if (threadIdx.x == 0) sums[m.part + part] = (s[0] + s[1]) + (s[2] + s[3]);
+    if (threadIdx.x == 0) sums[part0 + part] = (s[0] + s[1]) + (s[2] + s[3]);
     __syncthreads();
   }
 }
@@ -156,9 +153,9 @@ __global__ __launch_bounds__(256) void ortho_prepare_kernel(const Mat* __restric
   gram[blockIdx.x] = {(float)(b.in_a / (b.in_x * b.in_x)), 0.f, 0.f};
 }
 
-// One wave per matrix, behind every A: the largest singular value of X is at most the root of A's Frobenius norm, which is what
-// the factors of the step's other products and of the next A go by.  (Bounds that come from the polynomials alone lag behind
-// values that shrink, and what is stored loses bits.)
+// Behind every A: the largest singular value of X is at most the root of A's Frobenius norm, which is what the factors of the step's
+// other products and of the next A go by.  (Bounds that come from the polynomials alone lag behind values that shrink, and what is
+// stored loses bits.)
 struct StepArgs {
   float a, b, c;
   float q;  // a's of the group's earlier steps, multiplied
@@ -166,16 +163,18 @@ struct StepArgs {
   // of R = b A + c A A; of Q = a Q + q R + R Q; of S = a A + R A; of the next A = a S + R S; of X = q a X + Q X; of A = X X^T
   Factors *square, *join, *half, *next, *update, *gram;
 };
+// One wave per matrix.  (In the launch that makes A, by the last of the matrix's workgroups: what it needs of the others has to leave
+// their caches first, 6 us where this launch takes 4.)
 __global__ __launch_bounds__(64) void ortho_factors_kernel(const Mat* __restrict__ table, const float* __restrict__ squares, int tile,
                                                            Bound* __restrict__ bounds, StepArgs f) {
   const int w = blockIdx.x;
   const Mat& m = table[w];
   const int mt = (m.m + tile - 1) / tile, tiles = mt * (mt + 1) / 2;
+  Bound t = bounds[w];
   double v = 0;
   for (int i = threadIdx.x; i < tiles; i += 64) v += squares[m.square_tile + i];
   for (int k = 32; k; k >>= 1) v += __shfl_xor(v, k, 64);
   if (threadIdx.x != 0) return;
-  Bound t = bounds[w];
   const double a = f.a, b = f.b, c = f.c, qa = f.first ? a : f.q * a;
   t.x = fmin(t.x, sqrt(sqrt(v) / t.in_a) * 1.01);
   const double x2 = t.x * t.x, r = fabs(b) * x2 + fabs(c) * x2 * x2, x = quintic_bound(a, b, c, t.x) * 1.01;
@@ -390,32 +389,48 @@ __global__ __launch_bounds__(256, 2) void ortho_product_kernel(ProductArgs a) {
   };
   join(true);
 
+  const char* const E = SQUARES ? (op_e >= 0 ? slots + op_e * slot : nullptr) : X;
+  const char* const F = SQUARES && op_f >= 0 ? slots + op_f * slot : nullptr;
+  const int ldc = (SQUARES ? mp : np) * 4;
+  const size_t corner = (size_t)(m0 + wm * W) * ldc + pair_byte(n0 + wn * W);
+  auto at = [&](int i, int j) { return (uint32_t)((i * 16 + l16) * ldc + pair_byte(j * 16 + kq * 4)); };
+  // what is added to the product: all its loads together (one after the other they took 0.7 us each, 11 us of a tile), and with
+  // small tiles, which have the registers, in front of everything else
+  half4 hi[NB][NB], lo[NB][NB];
+  auto fetch = [&](const char* from) {
 #pragma unroll
-  for (int i = 0; i < STAGES - 1; ++i)
-    if (i < steps) issue(i);
-  int stage = 0;
-#pragma unroll 1
-  for (int g = 0; g < steps; ++g) {
-    // this step's panels are there (those of the next STAGES - 2 may be on their way) and the last one's have been read
-    constexpr int YOUNGER = (STAGES - 2) * 2 * UNITS;
-    static_assert(YOUNGER < 64, "vmcnt field");
-    if (YOUNGER > 0 && g + STAGES - 2 < steps) __builtin_amdgcn_s_waitcnt(0x0070 | (YOUNGER & 15) | (YOUNGER >> 4) << 14);
-    else __builtin_amdgcn_s_waitcnt(0x0070);
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-    if (g + STAGES - 1 < steps) issue(stage == 0 ? STAGES - 1 : stage - 1);
-    const char* const pp = s_ring + stage * 2 * PANEL;
-    const char* const pq = pp + PANEL;
-    stage = stage + 1 == STAGES ? 0 : stage + 1;
-    half8 fp[NB][2], fq[NB][2];
+    for (int i = 0; i < NB; ++i)
+#pragma unroll
+      for (int j = 0; j < NB; ++j) {
+        hi[i][j] = *reinterpret_cast<const half4*>(from + corner + at(i, j));
+        lo[i][j] = *reinterpret_cast<const half4*>(from + corner + at(i, j) + 64);
+      }
+  };
+  auto add = [&](float factor) {
+#pragma unroll
+    for (int i = 0; i < NB; ++i)
+#pragma unroll
+      for (int j = 0; j < NB; ++j)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) total[i][j][k] += factor * ((float)hi[i][j][k] + (float)lo[i][j][k]);
+  };
+  constexpr bool EARLY = TILE == 64;
+  if (EARLY && E) fetch(E);
+
+  auto panel = [&](int stage) -> const char* { return s_ring + stage * 2 * PANEL; };
+  struct Fragments {
+    half8 p[NB][2], q[NB][2];
+  };
+  auto read = [&](Fragments& f, int stage) {
 #pragma unroll
     for (int i = 0; i < NB; ++i)
 #pragma unroll
       for (int part = 0; part < 2; ++part) {
-        fp[i][part] = along(pp, wm * W + i * 16, part);
-        fq[i][part] = SQUARES ? along(pq, wn * W + i * 16, part) : across(pq, wn * W + i * 16, part);
+        f.p[i][part] = along(panel(stage), wm * W + i * 16, part);
+        f.q[i][part] = SQUARES ? along(panel(stage) + PANEL, wn * W + i * 16, part) : across(panel(stage) + PANEL, wn * W + i * 16, part);
       }
+  };
+  auto multiply = [&](const Fragments& f) {
     // (Q's fragment is the first operand: a lane then holds four neighbouring columns of C.  The blocks are walked to and fro.)
 #pragma unroll
     for (int t = 0; t < 3; ++t)
@@ -424,43 +439,74 @@ __global__ __launch_bounds__(256, 2) void ortho_product_kernel(ProductArgs a) {
 #pragma unroll
         for (int jj = 0; jj < NB; ++jj) {
           const int j = i % 2 ? NB - 1 - jj : jj;
-          acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fq[j][t == 0], fp[i][t == 1], acc[i][j], 0, 0, 0);
+          acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f.q[j][t == 0], f.p[i][t == 1], acc[i][j], 0, 0, 0);
         }
-    if (g % JOIN == JOIN - 1) join(false);
+  };
+  // everybody's loads but those of the YOUNGER youngest stages have landed, and everybody's reads of LDS have returned
+  auto meet = [&](auto younger, bool all_issued) {
+    constexpr int LOADS = decltype(younger)::value * 2 * UNITS;
+    static_assert(LOADS < 64, "vmcnt field");
+    if (LOADS > 0 && all_issued) __builtin_amdgcn_s_waitcnt(0x0070 | (LOADS & 15) | (LOADS >> 4) << 14);
+    else __builtin_amdgcn_s_waitcnt(0x0070);
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  };
+  auto next = [](int stage) { return stage + 1 == STAGES ? 0 : stage + 1; };
+#pragma unroll
+  for (int i = 0; i < STAGES - 1; ++i)
+    if (i < steps) issue(i);
+  int stage = 0;
+  if constexpr (EARLY) {
+    // One wave per SIMD: the next step's fragments are read while this one's are multiplied.
+    Fragments f[2];
+    meet(std::integral_constant<int, STAGES - 2>{}, STAGES - 2 < steps);
+    read(f[0], 0);
+    auto body = [&](auto set, int g) {
+      constexpr int SET = decltype(set)::value;
+      if (g + 1 < steps) {
+        meet(std::integral_constant<int, STAGES - 3>{}, g + STAGES - 2 < steps);
+        if (g + STAGES - 1 < steps) issue(stage == 0 ? STAGES - 1 : stage - 1);
+        stage = next(stage);
+        read(f[1 - SET], stage);
+      }
+      multiply(f[SET]);
+      if (g % JOIN == JOIN - 1) join(false);
+    };
+#pragma unroll 1
+    for (int g = 0; g < steps; g += 2) {
+      body(std::integral_constant<int, 0>{}, g);
+      if (g + 1 < steps) body(std::integral_constant<int, 1>{}, g + 1);
+    }
+  } else {
+#pragma unroll 1
+    for (int g = 0; g < steps; ++g) {
+      meet(std::integral_constant<int, STAGES - 2>{}, g + STAGES - 2 < steps);
+      if (g + STAGES - 1 < steps) issue(stage == 0 ? STAGES - 1 : stage - 1);
+      Fragments f;
+      read(f, stage);
+      stage = next(stage);
+      multiply(f);
+      if (g % JOIN == JOIN - 1) join(false);
+    }
   }
   join(false);
 
   // ---- result: a lane holds row l16 and columns 4 kq + 0..3 of every block
-  const char* const E = SQUARES ? (op_e >= 0 ? slots + op_e * slot : nullptr) : X;
-  const char* const F = SQUARES && op_f >= 0 ? slots + op_f * slot : nullptr;
-  const int ldc = (SQUARES ? mp : np) * 4;
   char* const C = SQUARES ? slots + op_c * slot : other;
   const bool mirror = SQUARES && mt != nt;
-  const size_t corner = (size_t)(m0 + wm * W) * ldc + pair_byte(n0 + wn * W);
-  auto at = [&](int i, int j) { return (uint32_t)((i * 16 + l16) * ldc + pair_byte(j * 16 + kq * 4)); };
 #pragma unroll
   for (int i = 0; i < NB; ++i)
 #pragma unroll
     for (int j = 0; j < NB; ++j) total[i][j] *= f_product;
-  // (all loads of a matrix together: one after the other they took 0.7 us each, 11 us of a tile)
-  auto add = [&](const char* from, float factor) {
-    half4 hi[NB][NB], lo[NB][NB];
-#pragma unroll
-    for (int i = 0; i < NB; ++i)
-#pragma unroll
-      for (int j = 0; j < NB; ++j) {
-        hi[i][j] = *reinterpret_cast<const half4*>(from + corner + at(i, j));
-        lo[i][j] = *reinterpret_cast<const half4*>(from + corner + at(i, j) + 64);
-      }
-#pragma unroll
-    for (int i = 0; i < NB; ++i)
-#pragma unroll
-      for (int j = 0; j < NB; ++j)
-#pragma unroll
-        for (int k = 0; k < 4; ++k) total[i][j][k] += factor * ((float)hi[i][j][k] + (float)lo[i][j][k]);
-  };
-  if (E) add(E, f_first);
-  if (F) add(F, f_second);
+  if (E) {
+    if (!EARLY) fetch(E);
+    add(f_first);
+  }
+  if (F) {
+    fetch(F);
+    add(f_second);
+  }
   float sum = 0.f;
   if (mirror) __syncthreads();  // the ring has been read
 #pragma unroll
@@ -554,6 +600,9 @@ modse_status ortho_layout(const modse_matrix_set* set, const float* coeffs, int 
     m2n += (double)sm * sm * sn;
   }
   if (update[1] >= (int64_t)1 << 23) return MODSE_ERR_UNSUPPORTED;  // (a launch has fewer than 2^32 threads)
+  // Tiles of 64 where those of 128 leave half of the workgroups' places empty.  us, 64 / 128: 24 matrices of 256 x 128..384 174 / 287, 24
+  // of 512 x 300..1200 (190 tiles of 128) 583 / 636, 12 of 1000 x 333..1999 (230) 1217 / 1230, 6 of 1024 x 1408..4224 (216) 1156 / 1098,
+  // 12 of 1024 x 1408..4224 (432) 2117 / 1826, a full layer 28195 / 19661.
   const bool small = square[0] <= 256;
   w.tile = small ? 64 : 128;
   w.square_tiles = (int32_t)square[small];
@@ -575,8 +624,10 @@ modse_status ortho_layout(const modse_matrix_set* set, const float* coeffs, int 
   w.data = take(data);
   w.total = n ? off : 0;
   w.n_groups = 0;
-  // Groups of steps where the products are what counts (enough tiles to go round), and X is longer than it is wide.
-  const bool grouped = coeffs && update[0] >= 1024 && m2n >= 1.25 * m3;
+  // Groups of steps where the products are what counts, and X is longer than it is wide.  us, single steps / groups: 24 matrices of
+  // 256 x 128..384 174 / 175, 3 of 256 x 256 128 / 150, 6 of 512 x 700..1200 277 / 251, 24 of 512 x 300..1200 583 / 534, 12 of 1000 x
+  // 333..1999 into bf16 1217 / 1044, a full layer 27788 / 19685; 3 of 1111 x 1500 704 / 720.
+  const bool grouped = coeffs && m2n >= 6e8 && m2n >= 1.4 * m3;
   const double most = set->dtype == MODSE_F32 ? F32_GROWTH : BF16_GROWTH;
   double top = 1;
   for (int i = 0; coeffs && i < steps;) {
@@ -615,6 +666,7 @@ hipError_t launch_orthogonalize(const modse_matrix_set* set, const OrthoLayout& 
     a.data = ws + w.data;
     a.first = first;
     a.count = n - first < MATS_PER_LAUNCH ? n - first : MATS_PER_LAUNCH;
+    most_parts = 0;
     for (int i = 0; i < a.count; ++i) {
       const int r = set->rows[first + i], c = set->cols[first + i];
       const int64_t sm = r < c ? r : c, sn = r < c ? c : r, mt = tiles_of(sm, tile);
@@ -627,11 +679,9 @@ hipError_t launch_orthogonalize(const modse_matrix_set* set, const OrthoLayout& 
       if (parts > most_parts) most_parts = parts;
       if (blocks > most_tiles) most_tiles = blocks;
     }
-    hipLaunchKernelGGL(ortho_table_kernel, dim3(1), dim3(64), 0, s, a);
+    hipLaunchKernelGGL(ortho_squares_kernel, dim3(most_parts < 1024 ? most_parts : 1024, a.count), dim3(256), 0, s, a, sums);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
-  hipLaunchKernelGGL(ortho_squares_kernel, dim3(most_parts < 1024 ? most_parts : 1024, n), dim3(256), 0, s, table, sums);
-  if ((e = hipGetLastError()) != hipSuccess) return e;
   hipLaunchKernelGGL(ortho_prepare_kernel, dim3(n), dim3(256), 0, s, table, sums, eps, bounds, f_gram, tile, square_list, update_list);
   if ((e = hipGetLastError()) != hipSuccess) return e;
   hipLaunchKernelGGL(ortho_start_kernel, dim3(most_tiles < 2048 ? most_tiles : 2048, n), dim3(256), 0, s, table, bounds);
@@ -661,15 +711,20 @@ hipError_t launch_orthogonalize(const modse_matrix_set* set, const OrthoLayout& 
   };
   int step = 0;
   for (int k = 0; k < w.n_groups; ++k) {
-    if ((e = squares_of({f_gram, -1, -1, -1, -1, SLOT_A, 1}, nullptr)) != hipSuccess) return e;
     int A = SLOT_A, Q = SLOT_R;
     float qa = 0.f;
-    for (int i = 0; i < w.group[k]; ++i, ++step) {
-      const float* const c = coeffs + 3 * step;
-      const bool last = i + 1 == w.group[k];
-      const StepArgs f = {c[0], c[1], c[2], qa, i == 0, last, f_square, f_join, f_half, f_next, f_update, f_gram};
+    // the factors that the A of the group's step i brings
+    auto factors_of = [&](int i) {
+      const float* const c = coeffs + 3 * (step + i);
+      const StepArgs f = {c[0], c[1], c[2], qa, i == 0, i + 1 == w.group[k], f_square, f_join, f_half, f_next, f_update, f_gram};
       hipLaunchKernelGGL(ortho_factors_kernel, dim3(n), dim3(64), 0, s, table, squares, tile, bounds, f);
-      if ((e = hipGetLastError()) != hipSuccess) return e;
+      return hipGetLastError();
+    };
+    if ((e = squares_of({f_gram, -1, -1, -1, -1, SLOT_A, 1}, nullptr)) != hipSuccess) return e;
+    if ((e = factors_of(0)) != hipSuccess) return e;
+    for (int i = 0; i < w.group[k]; ++i) {
+      const float first = coeffs[3 * (step + i)];
+      const bool last = i + 1 == w.group[k];
       const int R = i == 1 ? SLOT_R2 : SLOT_R;  // (the first one is Q in the second step)
       if ((e = squares_of({f_square, A, A, A, -1, R, 0}, nullptr)) != hipSuccess) return e;
       const int Q2 = i == 0 ? R : Q == SLOT_Q ? SLOT_R2 : SLOT_Q;
@@ -678,12 +733,14 @@ hipError_t launch_orthogonalize(const modse_matrix_set* set, const OrthoLayout& 
         if ((e = i == 0 ? squares_of(half, nullptr) : last ? squares_of(join, nullptr) : squares_of(join, &half)) != hipSuccess) return e;
       }
       Q = Q2;
-      qa = i == 0 ? c[0] : qa * c[0];
+      qa = i == 0 ? first : qa * first;
       if (!last) {
         A = A == SLOT_A ? SLOT_A2 : SLOT_A;
         if ((e = squares_of({f_next, R, SLOT_S, SLOT_S, -1, A, 1}, nullptr)) != hipSuccess) return e;
+        if ((e = factors_of(i + 1)) != hipSuccess) return e;
       }
     }
+    step += w.group[k];
     if (k + 1 < w.n_groups) e = update_by(Q, std::integral_constant<Out, OUT_PAIRS>{});
     else if (set->dtype == MODSE_F32) e = update_by(Q, std::integral_constant<Out, OUT_F32>{});
     else e = update_by(Q, std::integral_constant<Out, OUT_BF16>{});

@@ -171,3 +171,66 @@ def test_a_captured_update_replays():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(want, out))
+
+
+# ---------------------------------------------------------------- sets that take the large tiles, and groups of steps
+# More than 256 tiles of 128 on and below the diagonals, sides around the tiles' edges, long, tall and square; groups of steps where
+# the sum of m m n is 1.4 times that of m^3.  Inside a group of steps A goes on without X: a rounding of A (16 u of it, three times a
+# step) has grown by 200 (float32) or 25000 (bf16) at the most when it comes into X, with a factor of |b| + 2 |c|, at the group's end.
+def large_set(kind):
+    rng = np.random.default_rng(11)
+    if kind == "square":
+        shapes = [(n, n) for n in (520, 511, 513, 512)] * 6
+    else:
+        shapes = [(384 + int(k), 700 + 40 * int(k) % 301) for k in rng.integers(0, 150, 30)]
+        shapes = [s if i % 3 else s[::-1] for i, s in enumerate(shapes)]
+    shapes += [(1, 1), (5, 900), (900, 130)]
+    return [gradient(r, c, i) for i, (r, c) in enumerate(shapes)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("kind", ["square", "long"])
+def test_large_tiles_and_groups_of_steps(kind, dtype):
+    mats = large_set(kind)
+    tiles = sum(t * (t + 1) // 2 for t in (-(-min(a.shape) // 128) for a in mats))
+    assert tiles > 256
+    a, b, c = QUINTIC
+    growth = {"f32": 200, "bf16": 25000}[dtype] if kind == "long" else 0
+    for steps in (1, 2, 5):
+        got = run(mats, [QUINTIC] * steps, dtype)
+        for i in (0, 1, 2, 3, len(mats) - 3, len(mats) - 2, len(mats) - 1):
+            tol, X = tolerance(mats[i], [QUINTIC] * steps, EPS)
+            want = orc.orthogonalize(mats[i], [QUINTIC] * steps, EPS)
+            group = 48 * U * growth * (abs(b) + 2 * abs(c)) * np.linalg.norm(X) if steps > 1 else 0
+            err = np.linalg.norm(got[i] - want)
+            assert err <= tol + group + HALF[dtype] * np.linalg.norm(want), (kind, dtype, steps, mats[i].shape, err, tol, group)
+
+
+def test_groups_of_steps_stay_near_float32_products():
+    """At most four times the error of the same formula in float32, and far below half a step of bf16 where the results are that."""
+    mats = large_set("long")
+    f32, bf16 = run(mats, [QUINTIC] * 5), run(mats, [QUINTIC] * 5, "bf16")
+    for i in (1, 2, 4):
+        G = mats[i]
+        want = orc.orthogonalize(G, [QUINTIC] * 5, EPS)
+        X = torch.from_numpy(G if G.shape[0] <= G.shape[1] else G.T.copy())
+        X = X / (X.double().norm().float() + EPS)
+        for a, b, c in [QUINTIC] * 5:
+            A = X @ X.T
+            X = a * X + (b * A + c * (A @ A)) @ X
+        plain = X.double().numpy() if G.shape[0] <= G.shape[1] else X.double().numpy().T
+        assert np.linalg.norm(f32[i] - want) <= 4 * np.linalg.norm(plain - want)
+        # rounding alone: half a step everywhere would be 2^-8, its mean is 1 / sqrt(12) of a step
+        rounded = torch.from_numpy(want).to(torch.bfloat16).double().numpy()
+        assert np.linalg.norm(bf16[i] - want) <= 1.1 * np.linalg.norm(rounded - want)
+
+
+def test_bad_matrices_keep_to_themselves_in_large_tiles_too():
+    mats = large_set("long")
+    clean = run(mats, [QUINTIC] * 3)
+    mats[4][:] = 0
+    mats[7][3, 9] = np.nan
+    got = run(mats, [QUINTIC] * 3)
+    assert (got[4] == 0).all() and np.isnan(got[7]).all()
+    for i in set(range(len(mats))) - {4, 7}:
+        assert np.array_equal(got[i], clean[i])

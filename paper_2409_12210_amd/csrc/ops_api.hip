@@ -15,7 +15,7 @@ modse_status check_dtype(const modse_dtype& dtype) {
 }
 modse_status check_set(const modse_matrix_set* set) {
   if (!set || set->n_matrices < 0) return MODSE_ERR_INVALID_ARG;
-  if (check_dtype(set->dtype) != MODSE_OK || set->n_matrices > 4096) return MODSE_ERR_UNSUPPORTED;
+  if (check_dtype(set->dtype) != MODSE_OK || set->n_matrices > modse_ortho::MAX_MATS) return MODSE_ERR_UNSUPPORTED;
   if (set->n_matrices && (!set->rows || !set->cols)) return MODSE_ERR_INVALID_ARG;
   return MODSE_OK;
 }

@@ -6,7 +6,7 @@
 
 namespace modse_ortho {
 
-constexpr int MAX_STEPS = 32;
+constexpr int MAX_STEPS = 32, MAX_MATS = 4096;
 constexpr int PAD = 128;  // rows and columns of what is stored are padded to this with zeros: no kernel has edges to look at
 
 // the largest |a + b s^2 + c s^4| for 0 <= s <= top
@@ -66,7 +66,7 @@ struct Factors {
 struct OrthoLayout {
   size_t mats, bounds, factors, squares, sums, square_list, update_list, data, total;
   int32_t square_tiles, update_tiles, parts;
-  int32_t tile, n_slots;
+  int32_t tile;
   int32_t group[modse_ortho::MAX_STEPS];  // steps of every group of them
   int32_t n_groups;
 };

@@ -16,6 +16,8 @@
 // A_(i+1) = P_i A_i P_i and X_g = P_(g-1) ... P_0 X, all of whose factors are m x m, symmetric and commute.  In units of m^3
 // (n = r m, squares at half price) a group of g steps costs 3 r + 4 g - 3 where single steps cost g (3 r + 1).  What a rounding
 // puts into A grows by up to a^2 in every A_(i+1), so groups are short: ortho_layout.
+#include <algorithm>
+
 #include "gemm_bf16_util.h"
 #include "ops.h"
 #include "ortho.h"
@@ -206,7 +208,7 @@ __global__ __launch_bounds__(64) void ortho_factors_kernel(const Mat* __restrict
   bounds[w] = t;
 }
 
-__device__ __forceinline__ void store_pair(char* p, const float (&v)[4]) {  // four values of a block
+__device__ __forceinline__ void store_pair(char* p, const f32x4& v) {  // four values of a block
   half4 hi, lo;
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
@@ -215,6 +217,20 @@ __device__ __forceinline__ void store_pair(char* p, const float (&v)[4]) {  // f
   }
   *reinterpret_cast<half4*>(p) = hi;
   *reinterpret_cast<half4*>(p + 64) = lo;
+}
+__device__ __forceinline__ float sum_of_squares(const f32x4& v) { return (v[0] * v[0] + v[1] * v[1]) + (v[2] * v[2] + v[3] * v[3]); }
+// A tile's transpose in LDS, ROWS values a row: four columns of row r go in, four rows (4 r4 on) of column c come out.  Chunks of four
+// rows are XOR-ed with the column, so that the lanes meet all banks.
+template <int ROWS>
+__device__ __forceinline__ int transposed_chunk(int r4, int c) { return (r4 ^ (c & ~3 & (ROWS / 4 - 1))) << 4; }
+template <int ROWS>
+__device__ __forceinline__ void store_transposed(char* s, int r, int c, const f32x4& v) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k) *reinterpret_cast<float*>(s + (c + k) * (ROWS * 4) + transposed_chunk<ROWS>(r >> 2, c) + (r & 3) * 4) = v[k];
+}
+template <int ROWS>
+__device__ __forceinline__ f32x4 load_transposed(const char* s, int r4, int c) {
+  return *reinterpret_cast<const f32x4*>(s + c * (ROWS * 4) + transposed_chunk<ROWS>(r4, c));
 }
 // byte of the hi part of column c of a row
 __device__ __forceinline__ int pair_byte(int c) { return (c >> 5) * 128 + (c & 31) * 2; }
@@ -255,7 +271,7 @@ __global__ __launch_bounds__(256) void ortho_start_kernel(const Mat* __restrict_
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int r = (threadIdx.x >> 4) + 16 * i;
-      float v[4];
+      f32x4 v;
 #pragma unroll
       for (int j = 0; j < 4; ++j) v[j] = s[r][at * 4 + j];
       store_pair(m.X[0] + (size_t)(m0 + r) * m.np * 4 + pair_byte(n0 + at * 4), v);
@@ -277,7 +293,10 @@ __global__ __launch_bounds__(256) void ortho_start_kernel(const Mat* __restrict_
 enum Out { OUT_PAIRS, OUT_F32, OUT_BF16 };
 constexpr int BK = 32;
 constexpr int JOIN = 16;  // steps that are summed in one register
-constexpr int RUN = 16;   // neighbouring tiles that an XCD gets, of every 8 * RUN
+// Neighbouring tiles that an XCD gets, of every 8 times as many: they share panels in its L2.  us, runs of 4 / 16 / 32 / 64: a full layer
+// 20124 / 19635 / 19446 / 19928, 64 narrow experts 10817 / 10421 / 10336 / 10260; tiles of 64, runs of 4 / 8 / 16: 24 matrices of 512 x
+// 300..1200 576 / 522 / 493, 6 of 1024 x 1408..4224 1123 / 1098 / 1082.
+constexpr int run_of(int tile) { return tile == 64 ? 16 : 32; }
 struct SquareOp {
   const Factors* factors;
   int32_t p, q, e, f, c;  // slots; p < 0: X, e and f < 0: none
@@ -292,6 +311,104 @@ struct ProductArgs {
   int32_t tiles;
 };
 
+// What a workgroup has to do.  (All of it is read at once: what is read through a reference later is read again behind every
+// barrier, one round trip after the other.)
+template <int TILE, bool SQUARES, Out OUT>
+struct Job {
+  const char *P, *Q, *E, *F;
+  char* C;
+  void* U;
+  int which, rows, cols, m0, n0, K, ldp, ldq, ldc;  // (distances of rows in bytes)
+  float f_product, f_first, f_second, out;
+  bool mirror, sum;
+  __device__ __forceinline__ void load(const ProductArgs& a, int tile) {
+    const SquareOp& o = a.op[SQUARES ? blockIdx.y : 0];
+    const int op_p = o.p, op_q = o.q, op_e = o.e, op_f = o.f, op_c = o.c;
+    const Mat& m = a.list[tile];
+    const int mp = m.mp, np = m.np, mt = m.mt, nt = m.nt;
+    char *const X0 = m.X[0], *const X1 = m.X[1], *const slots = m.slot;
+    which = m.which;
+    rows = m.rows;
+    cols = m.cols;
+    U = m.U;
+    sum = o.sum;
+    const Factors* const f = o.factors + which;
+    f_product = f->product;
+    f_first = f->first;
+    f_second = f->second;
+    out = OUT == OUT_PAIRS ? 1.f : a.bounds[which].out;
+    const char* const X = a.x ? X1 : X0;
+    const size_t slot = (size_t)mp * mp * 4;
+    const bool gram = SQUARES && op_p < 0;
+    m0 = mt * TILE;
+    n0 = nt * TILE;
+    K = gram ? max(rows, cols) : min(rows, cols);
+    ldp = (gram ? np : mp) * 4;
+    ldq = (gram || !SQUARES ? np : mp) * 4;
+    ldc = (SQUARES ? mp : np) * 4;
+    P = (gram ? X : slots + op_p * slot) + (size_t)m0 * ldp;
+    Q = gram || !SQUARES ? X : slots + op_q * slot;
+    Q += SQUARES ? (size_t)n0 * ldq : (size_t)n0 * 4;
+    E = SQUARES ? (op_e >= 0 ? slots + op_e * slot : nullptr) : X;
+    F = SQUARES && op_f >= 0 ? slots + op_f * slot : nullptr;
+    C = SQUARES ? slots + op_c * slot : a.x ? X0 : X1;
+    mirror = SQUARES && mt != nt;
+  }
+  __device__ __forceinline__ size_t q_step() const { return SQUARES ? 128 : (size_t)BK * ldq; }  // bytes of Q from step to step
+  // four neighbouring columns of the last step's result
+  __device__ __forceinline__ void give(int r, int c, const f32x4& v) const {
+    typedef std::conditional_t<OUT == OUT_F32, float, bf16_t> T;
+    typedef T T4 __attribute__((ext_vector_type(4)));
+    typedef T4 T4_u __attribute__((aligned(sizeof(T))));
+    T4 u;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) u[k] = (T)(v[k] * out);
+    T* const to = static_cast<T*>(U);
+    const int mm = min(rows, cols), mn = max(rows, cols);
+    if (r >= mm) return;
+    if (rows > cols) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (c + k < mn) to[(int64_t)(c + k) * cols + r] = u[k];
+    } else if (c + 4 <= mn) {
+      *reinterpret_cast<T4_u*>(to + (int64_t)r * cols + c) = u;
+    } else {
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (c + k < mn) to[(int64_t)r * cols + c + k] = u[k];
+    }
+  }
+};
+// (workgroups go to the XCDs in turn)
+template <int TILE>
+__device__ __forceinline__ int tile_of_workgroup() {
+  constexpr int RUN = run_of(TILE);
+  const int i = blockIdx.x / 8;
+  return (i / RUN * 8 + (int)(blockIdx.x % 8)) * RUN + i % RUN;
+}
+// the 16-byte chunk of a panel row whose data lies in chunk `lane`: a row along K (eight chunks), row k of K across it
+__device__ __forceinline__ int along_chunk(int r, int chunk) { return chunk ^ ((r >> 1) & 7); }
+__device__ __forceinline__ int across_chunk(int k, int chunk) { return chunk ^ (4 * (k & 3) + 2 * (k >> 3 & 1)); }
+// fragments of 16 rows (or columns): 8 K per lane from 8 (lane >> 4) on, hi (part 0) or lo (1)
+__device__ __forceinline__ half8 along_fragment(const char* panel, int row, int part, int lane) {
+  const int kq = lane >> 4, l16 = lane & 15;
+  return *reinterpret_cast<const half8*>(panel + (row + l16) * 128 + (along_chunk(l16, part * 4 + kq) << 4));
+}
+template <int TILE>
+__device__ __forceinline__ half8 across_fragment(const char* panel, int col, int part, int lane) {
+  // lane 16 kq + s reads 8 bytes at row 8 kq + h + (s >> 2) of K, columns col + 4 (s & 3) on, and gets four K of column col + s
+  typedef short s16x4 __attribute__((ext_vector_type(4)));
+  typedef short s16x8 __attribute__((ext_vector_type(8)));
+  typedef __attribute__((address_space(3))) s16x4* lds_s16x4_ptr;
+  const int kq = lane >> 4, l16 = lane & 15, r = l16 >> 2;
+  const int c16 = (col >> 5) * 8 + part * 4 + (col >> 4 & 1) * 2 + ((l16 & 3) >> 1);
+  const char* const at = panel + (kq * 8 + r) * (TILE * 4) + (across_chunk(kq * 8 + r, c16) << 4) + (l16 & 1) * 8;
+  const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(at));
+  const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(at + 4 * (TILE * 4)));
+  const s16x8 v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+  return __builtin_bit_cast(half8, v);
+}
+
 template <int TILE, int STAGES, bool SQUARES, Out OUT>
 __global__ __launch_bounds__(256, 2) void ortho_product_kernel(ProductArgs a) {
   constexpr int PANEL = TILE * 128, UNITS = TILE / 32;  // bytes of a panel; its 1 KiB units per wave
@@ -301,50 +418,29 @@ __global__ __launch_bounds__(256, 2) void ortho_product_kernel(ProductArgs a) {
   __shared__ __align__(1024) char s_ring[RING];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave >> 1, wn = wave & 1;
-  // (workgroups go to the XCDs in turn)
-  const int tile = ((int)(blockIdx.x / 8) / RUN * 8 + (int)(blockIdx.x % 8)) * RUN + (int)(blockIdx.x / 8) % RUN;
+  const int tile = tile_of_workgroup<TILE>();
   if (tile >= a.tiles) return;
-  // (All that is needed of the table, now: what is read through a reference later is read again behind every barrier, one round
-  // trip after the other.)
-  const int side = SQUARES ? blockIdx.y : 0;
-  const SquareOp& o = a.op[side];
-  const int op_p = o.p, op_q = o.q, op_e = o.e, op_f = o.f, op_c = o.c, op_sum = o.sum;
-  const Mat& m = a.list[tile];
-  const int which = m.which, rows = m.rows, cols = m.cols, mp = m.mp, np = m.np, mt = m.mt, nt = m.nt;
-  char *const X0 = m.X[0], *const X1 = m.X[1], *const slots = m.slot;
-  void* const result = m.U;
-  const Factors* const pf = o.factors + which;
-  const float f_product = pf->product, f_first = pf->first, f_second = pf->second;
-  const float out = OUT == OUT_PAIRS ? 1.f : a.bounds[which].out;
-  const int mm = min(rows, cols), mn = max(rows, cols);
-  const char* const X = a.x ? X1 : X0;
-  char* const other = a.x ? X0 : X1;
-  const size_t slot = (size_t)mp * mp * 4;
-  const bool gram = SQUARES && op_p < 0;
-  const int m0 = mt * TILE, n0 = nt * TILE;
-  const int K = gram ? mn : mm, steps = (K + BK - 1) / BK;
-  const int ldp = (gram ? np : mp) * 4, ldq = (gram || !SQUARES ? np : mp) * 4;  // bytes
-  const char* const P = gram ? X : slots + op_p * slot;
-  const char* const Q = gram || !SQUARES ? X : slots + op_q * slot;
+  Job<TILE, SQUARES, OUT> job;
+  job.load(a, tile);
+  const int steps = (job.K + BK - 1) / BK;
 
   // ---- loads: units of 1 KiB, landing swizzled (16-byte chunks of a row XOR-ed)
   uint32_t offp[UNITS], offq[UNITS];
 #pragma unroll
   for (int i = 0; i < UNITS; ++i) {
     const int u = wave * UNITS + i;
-    const int r = u * 8 + (lane >> 3), c = (lane & 7) ^ ((r >> 1) & 7);
-    offp[i] = r * ldp + c * 16;
+    const int r = u * 8 + (lane >> 3), c = along_chunk(r, lane & 7);
+    offp[i] = r * job.ldp + c * 16;
     if (SQUARES) {
-      offq[i] = r * ldq + c * 16;
+      offq[i] = r * job.ldq + c * 16;
     } else {
       constexpr int CHUNKS = TILE / 4;  // of a row of K
       const int k = u * (64 / CHUNKS) + lane / CHUNKS;
-      offq[i] = k * ldq + ((lane % CHUNKS) ^ (4 * (k & 3) + 2 * (k >> 3 & 1))) * 16;
+      offq[i] = k * job.ldq + across_chunk(k, lane % CHUNKS) * 16;
     }
   }
-  const char* p = P + (size_t)m0 * ldp;
-  const char* q = SQUARES ? Q + (size_t)n0 * ldq : Q + (size_t)n0 * 4;
-  const size_t q_step = SQUARES ? 128 : (size_t)BK * ldq;
+  const char *p = job.P, *q = job.Q;
+  const size_t q_step = job.q_step();
   const uint32_t lds = __builtin_amdgcn_readfirstlane(lds_address(s_ring));
   auto issue = [&](int stage) {
     const uint32_t dst = lds + stage * 2 * PANEL + wave * (UNITS * 1024);
@@ -356,23 +452,7 @@ __global__ __launch_bounds__(256, 2) void ortho_product_kernel(ProductArgs a) {
     p += 128;
     q += q_step;
   };
-  // ---- fragments: 16 rows, 8 K per lane from 8 (lane >> 4) on, hi (part 0) or lo (1)
   const int kq = lane >> 4, l16 = lane & 15;
-  auto along = [&](const char* panel, int row, int part) {
-    return *reinterpret_cast<const half8*>(panel + (row + l16) * 128 + (((part * 4 + kq) ^ ((l16 >> 1) & 7)) << 4));
-  };
-  auto across = [&](const char* panel, int col, int part) -> half8 {
-    // lane 16 kq + s reads 8 bytes at row 8 kq + h + (s >> 2) of K, columns col + 4 (s & 3) on, and gets four K of column col + s
-    typedef short s16x4 __attribute__((ext_vector_type(4)));
-    typedef short s16x8 __attribute__((ext_vector_type(8)));
-    typedef __attribute__((address_space(3))) s16x4* lds_s16x4_ptr;
-    const int r = l16 >> 2, c16 = (col >> 5) * 8 + part * 4 + (col >> 4 & 1) * 2 + ((l16 & 3) >> 1);
-    const char* const at = panel + (kq * 8 + r) * (TILE * 4) + ((c16 ^ (4 * r + 2 * (kq & 1))) << 4) + (l16 & 1) * 8;
-    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(at));
-    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(at + 4 * (TILE * 4)));
-    const s16x8 v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-    return __builtin_bit_cast(half8, v);
-  };
   f32x4 total[NB][NB], acc[NB][NB];
   // acc joins total and starts again.  (A sum of K terms of one sign in one register is off by up to K / 16 * 3 roundings, the
   // diagonal of X X^T at K = 3000 by 1e-6; in parts of 512 it is as good as one of 512.)
@@ -389,11 +469,8 @@ __global__ __launch_bounds__(256, 2) void ortho_product_kernel(ProductArgs a) {
   };
   join(true);
 
-  const char* const E = SQUARES ? (op_e >= 0 ? slots + op_e * slot : nullptr) : X;
-  const char* const F = SQUARES && op_f >= 0 ? slots + op_f * slot : nullptr;
-  const int ldc = (SQUARES ? mp : np) * 4;
-  const size_t corner = (size_t)(m0 + wm * W) * ldc + pair_byte(n0 + wn * W);
-  auto at = [&](int i, int j) { return (uint32_t)((i * 16 + l16) * ldc + pair_byte(j * 16 + kq * 4)); };
+  const size_t corner = (size_t)(job.m0 + wm * W) * job.ldc + pair_byte(job.n0 + wn * W);
+  auto at = [&](int i, int j) { return (uint32_t)((i * 16 + l16) * job.ldc + pair_byte(j * 16 + kq * 4)); };
   // what is added to the product: all its loads together (one after the other they took 0.7 us each, 11 us of a tile), and with
   // small tiles, which have the registers, in front of everything else
   half4 hi[NB][NB], lo[NB][NB];
@@ -415,7 +492,7 @@ __global__ __launch_bounds__(256, 2) void ortho_product_kernel(ProductArgs a) {
         for (int k = 0; k < 4; ++k) total[i][j][k] += factor * ((float)hi[i][j][k] + (float)lo[i][j][k]);
   };
   constexpr bool EARLY = TILE == 64;
-  if (EARLY && E) fetch(E);
+  if (EARLY && job.E) fetch(job.E);
 
   auto panel = [&](int stage) -> const char* { return s_ring + stage * 2 * PANEL; };
   struct Fragments {
@@ -426,12 +503,15 @@ __global__ __launch_bounds__(256, 2) void ortho_product_kernel(ProductArgs a) {
     for (int i = 0; i < NB; ++i)
 #pragma unroll
       for (int part = 0; part < 2; ++part) {
-        f.p[i][part] = along(panel(stage), wm * W + i * 16, part);
-        f.q[i][part] = SQUARES ? along(panel(stage) + PANEL, wn * W + i * 16, part) : across(panel(stage) + PANEL, wn * W + i * 16, part);
+        f.p[i][part] = along_fragment(panel(stage), wm * W + i * 16, part, lane);
+        f.q[i][part] = SQUARES ? along_fragment(panel(stage) + PANEL, wn * W + i * 16, part, lane)
+                               : across_fragment<TILE>(panel(stage) + PANEL, wn * W + i * 16, part, lane);
       }
   };
   auto multiply = [&](const Fragments& f) {
-    // (Q's fragment is the first operand: a lane then holds four neighbouring columns of C.  The blocks are walked to and fro.)
+    // (Q's fragment is the first operand: a lane then holds four neighbouring columns of C.  The blocks are walked to and fro.  hi hi
+    // first, which needs half of the fragments, and in front of the other wave's reads: a full layer 19409 -> 19053 us.)
+    __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int t = 0; t < 3; ++t)
 #pragma unroll
@@ -439,8 +519,9 @@ __global__ __launch_bounds__(256, 2) void ortho_product_kernel(ProductArgs a) {
 #pragma unroll
         for (int jj = 0; jj < NB; ++jj) {
           const int j = i % 2 ? NB - 1 - jj : jj;
-          acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f.q[j][t == 0], f.p[i][t == 1], acc[i][j], 0, 0, 0);
+          acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f.q[j][t == 1], f.p[i][t == 2], acc[i][j], 0, 0, 0);
         }
+    __builtin_amdgcn_s_setprio(0);
   };
   // everybody's loads but those of the YOUNGER youngest stages have landed, and everybody's reads of LDS have returned
   auto meet = [&](auto younger, bool all_issued) {
@@ -493,80 +574,51 @@ __global__ __launch_bounds__(256, 2) void ortho_product_kernel(ProductArgs a) {
   join(false);
 
   // ---- result: a lane holds row l16 and columns 4 kq + 0..3 of every block
-  char* const C = SQUARES ? slots + op_c * slot : other;
-  const bool mirror = SQUARES && mt != nt;
 #pragma unroll
   for (int i = 0; i < NB; ++i)
 #pragma unroll
-    for (int j = 0; j < NB; ++j) total[i][j] *= f_product;
-  if (E) {
-    if (!EARLY) fetch(E);
-    add(f_first);
+    for (int j = 0; j < NB; ++j) total[i][j] *= job.f_product;
+  if (job.E) {
+    if (!EARLY) fetch(job.E);
+    add(job.f_first);
   }
-  if (F) {
-    fetch(F);
-    add(f_second);
+  if (job.F) {
+    fetch(job.F);
+    add(job.f_second);
   }
   float sum = 0.f;
-  if (mirror) __syncthreads();  // the ring has been read
+  if (job.mirror) __syncthreads();  // the ring has been read
 #pragma unroll
   for (int i = 0; i < NB; ++i)
 #pragma unroll
     for (int j = 0; j < NB; ++j) {
       const int r = wm * W + i * 16 + l16, c = wn * W + j * 16 + kq * 4;
-      const float v[4] = {total[i][j][0], total[i][j][1], total[i][j][2], total[i][j][3]};
       if constexpr (OUT == OUT_PAIRS) {
-        store_pair(C + corner + at(i, j), v);
+        store_pair(job.C + corner + at(i, j), total[i][j]);
         if constexpr (SQUARES) {
-          if (op_sum)
-#pragma unroll
-            for (int k = 0; k < 4; ++k) sum += v[k] * v[k];
-          if (mirror)  // transposed, chunks of four rows XOR-ed with the column, so that the lanes meet all banks
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-              *reinterpret_cast<float*>(s_ring + (c + k) * (TILE * 4) + (((r >> 2) ^ (c & (TILE / 4 - 1))) << 4) + (r & 3) * 4) = v[k];
+          if (job.sum) sum += sum_of_squares(total[i][j]);
+          if (job.mirror) store_transposed<TILE>(s_ring, r, c, total[i][j]);
         }
       } else {
-        typedef std::conditional_t<OUT == OUT_F32, float, bf16_t> T;
-        typedef T T4 __attribute__((ext_vector_type(4)));
-        typedef T4 T4_u __attribute__((aligned(sizeof(T))));
-        T4 u;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) u[k] = (T)(v[k] * out);
-        T* const U = static_cast<T*>(result);
-        if (m0 + r < mm) {
-          if (rows > cols) {
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-              if (n0 + c + k < mn) U[(int64_t)(n0 + c + k) * cols + m0 + r] = u[k];
-          } else if (n0 + c + 4 <= mn) {
-            *reinterpret_cast<T4_u*>(U + (int64_t)(m0 + r) * cols + n0 + c) = u;
-          } else {
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-              if (n0 + c + k < mn) U[(int64_t)(m0 + r) * cols + n0 + c + k] = u[k];
-          }
-        }
+        job.give(job.m0 + r, job.n0 + c, total[i][j]);
       }
     }
   if constexpr (SQUARES) {
     __syncthreads();
-    if (mirror) {
+    if (job.mirror) {
 #pragma unroll
       for (int i = 0; i < TILE * TILE / 1024; ++i) {
-        const int at = i * 256 + tid, c = at / (TILE / 4), r4 = at % (TILE / 4);
-        const f32x4 t = *reinterpret_cast<const f32x4*>(s_ring + c * (TILE * 4) + ((r4 ^ (c & ~3 & (TILE / 4 - 1))) << 4));
-        const float v[4] = {t[0], t[1], t[2], t[3]};
-        store_pair(C + (size_t)(n0 + c) * ldc + pair_byte(m0 + r4 * 4), v);
+        const int k = i * 256 + tid, c = k / (TILE / 4), r4 = k % (TILE / 4);
+        store_pair(job.C + (size_t)(job.n0 + c) * job.ldc + pair_byte(job.m0 + r4 * 4), load_transposed<TILE>(s_ring, r4, c));
       }
     }
-    if (op_sum) {
+    if (job.sum) {
       __syncthreads();
       float* const part = reinterpret_cast<float*>(s_ring);
       sum = wave_sum(sum);
       if (lane == 0) part[wave] = sum;
       __syncthreads();
-      if (tid == 0) a.squares[tile] = ((part[0] + part[1]) + (part[2] + part[3])) * (mirror ? 2.f : 1.f);
+      if (tid == 0) a.squares[tile] = ((part[0] + part[1]) + (part[2] + part[3])) * (job.mirror ? 2.f : 1.f);
     }
   }
 }
@@ -581,8 +633,8 @@ constexpr double F32_GROWTH = 200, BF16_GROWTH = 25000;
 
 modse_status ortho_layout(const modse_matrix_set* set, const float* coeffs, int steps, OrthoLayout& w) {
   const int n = set->n_matrices;
+  constexpr int SIDES[2] = {64, 128};
   int64_t square[2] = {0, 0}, update[2] = {0, 0}, parts = 0;
-  size_t data = 0;
   double m3 = 0, m2n = 0;
   for (int i = 0; i < n; ++i) {
     const int r = set->rows[i], c = set->cols[i];
@@ -590,24 +642,28 @@ modse_status ortho_layout(const modse_matrix_set* set, const float* coeffs, int 
     if (r > 65536 || c > 65536) return MODSE_ERR_UNSUPPORTED;
     const int64_t sm = r < c ? r : c, sn = r < c ? c : r;
     for (int t = 0; t < 2; ++t) {
-      const int64_t mt = tiles_of(sm, t ? 64 : 128);
+      const int64_t mt = tiles_of(sm, SIDES[t]);
       square[t] += mt * (mt + 1) / 2;
-      update[t] += mt * tiles_of(sn, t ? 64 : 128);
+      update[t] += mt * tiles_of(sn, SIDES[t]);
     }
     parts += ((int64_t)r * c + PART - 1) / PART;
-    data += mat_bytes(padded(sm), padded(sn));
     m3 += (double)sm * sm * sm;
     m2n += (double)sm * sm * sn;
   }
-  if (update[1] >= (int64_t)1 << 23) return MODSE_ERR_UNSUPPORTED;  // (a launch has fewer than 2^32 threads)
+  if (update[0] >= (int64_t)1 << 23) return MODSE_ERR_UNSUPPORTED;  // (a launch has fewer than 2^32 threads)
   // Tiles of 64 where those of 128 leave half of the workgroups' places empty.  us, 64 / 128: 24 matrices of 256 x 128..384 174 / 287, 24
   // of 512 x 300..1200 (190 tiles of 128) 583 / 636, 12 of 1000 x 333..1999 (230) 1217 / 1230, 6 of 1024 x 1408..4224 (216) 1156 / 1098,
   // 12 of 1024 x 1408..4224 (432) 2117 / 1826, a full layer 28195 / 19661.
-  const bool small = square[0] <= 256;
-  w.tile = small ? 64 : 128;
-  w.square_tiles = (int32_t)square[small];
-  w.update_tiles = (int32_t)update[small];
+  const int side = square[1] <= 256 ? 0 : 1;
+  w.tile = SIDES[side];
+  w.square_tiles = (int32_t)square[side];
+  w.update_tiles = (int32_t)update[side];
   w.parts = (int32_t)parts;
+  size_t data = 0;
+  for (int i = 0; i < n; ++i) {
+    const int r = set->rows[i], c = set->cols[i];
+    data += mat_bytes(padded(r < c ? r : c), padded(r < c ? c : r));
+  }
   size_t off = 0;
   auto take = [&](size_t bytes) {
     const size_t o = off;
@@ -617,10 +673,10 @@ modse_status ortho_layout(const modse_matrix_set* set, const float* coeffs, int 
   w.mats = take(n * sizeof(Mat));
   w.bounds = take(n * sizeof(Bound));
   w.factors = take((size_t)n * 6 * sizeof(Factors));
-  w.squares = take((size_t)square[1] * 4);
+  w.squares = take((size_t)w.square_tiles * 4);
   w.sums = take((size_t)parts * sizeof(double));
-  w.square_list = take((size_t)square[1] * sizeof(Mat));
-  w.update_list = take((size_t)update[1] * sizeof(Mat));
+  w.square_list = take((size_t)w.square_tiles * sizeof(Mat));
+  w.update_list = take((size_t)w.update_tiles * sizeof(Mat));
   w.data = take(data);
   w.total = n ? off : 0;
   w.n_groups = 0;
@@ -657,6 +713,13 @@ hipError_t launch_orthogonalize(const modse_matrix_set* set, const OrthoLayout& 
   double* const sums = reinterpret_cast<double*>(ws + w.sums);
   Mat* const square_list = reinterpret_cast<Mat*>(ws + w.square_list);
   Mat* const update_list = reinterpret_cast<Mat*>(ws + w.update_list);
+  // the matrices with the longest products first: 12 of 1000 x 333..1999 into bf16 1059 -> 995 us, a full layer 19053 -> 18825
+  int32_t order[MAX_MATS];
+  for (int i = 0; i < n; ++i) order[i] = i;
+  std::sort(order, order + n, [&](int i, int j) {
+    const int a = std::max(set->rows[i], set->cols[i]), b = std::max(set->rows[j], set->cols[j]);
+    return a != b ? a > b : i < j;
+  });
   int32_t square = 0, update = 0, part = 0, most_parts = 0, most_tiles = 0;
   int64_t data = 0;
   hipError_t e;
@@ -668,14 +731,14 @@ hipError_t launch_orthogonalize(const modse_matrix_set* set, const OrthoLayout& 
     a.count = n - first < MATS_PER_LAUNCH ? n - first : MATS_PER_LAUNCH;
     most_parts = 0;
     for (int i = 0; i < a.count; ++i) {
-      const int r = set->rows[first + i], c = set->cols[first + i];
+      const int k = order[first + i], r = set->rows[k], c = set->cols[k];
       const int64_t sm = r < c ? r : c, sn = r < c ? c : r, mt = tiles_of(sm, tile);
-      const int parts = (int)(((int64_t)r * c + PART - 1) / PART), blocks = padded(sm) / 64 * (padded(sn) / 64);
-      a.mat[i] = {set->G[first + i], set->U[first + i], data, r, c, square, update, part, parts};
+      const int parts = (int)(((int64_t)r * c + PART - 1) / PART), mp = padded(sm), np = padded(sn), blocks = mp / 64 * (np / 64);
+      a.mat[i] = {set->G[k], set->U[k], data, r, c, square, update, part, parts};
       square += (int32_t)(mt * (mt + 1) / 2);
       update += (int32_t)(mt * tiles_of(sn, tile));
       part += parts;
-      data += (int64_t)mat_bytes(padded(sm), padded(sn));
+      data += (int64_t)mat_bytes(mp, np);
       if (parts > most_parts) most_parts = parts;
       if (blocks > most_tiles) most_tiles = blocks;
     }
@@ -688,7 +751,8 @@ hipError_t launch_orthogonalize(const modse_matrix_set* set, const OrthoLayout& 
   if ((e = hipGetLastError()) != hipSuccess) return e;
 
   ProductArgs a = {square_list, {}, bounds, squares, 0, w.square_tiles};
-  auto grid = [](int tiles, int ops) { return dim3((tiles + 8 * RUN - 1) / (8 * RUN) * (8 * RUN), ops); };
+  const int span = 8 * run_of(tile);
+  auto grid = [span](int tiles, int ops) { return dim3((tiles + span - 1) / span * span, ops); };
   auto squares_of = [&](const SquareOp& one, const SquareOp* two) {
     a.list = square_list;
     a.tiles = w.square_tiles;

@@ -57,7 +57,25 @@ __device__ __forceinline__ void store_e4m3(uint8_t* p, const float (&v)[N], int 
 }
 // (a smaller one has no reciprocal)
 constexpr float MIN_SCALE = 1.17549435e-38f;  // 2^-126
-__device__ __forceinline__ float scale_of(float amax) { return fmaxf(amax * (1.f / 448.f), MIN_SCALE); }
+// From v = h gamma (exact for bf16 tensors of like size) and its largest value of a group: the scale of y = v rstd is
+// amax rstd / 448, and y / scale = 448 v / amax, which is rounded once before it is rounded to e4m3.  (y / scale from a rounded y
+// and scale falls on the other side of a tie for one value in a few million.)
+struct E4m3Scale {
+  float scale, factor, below, inv;
+  __device__ __forceinline__ void set(float amax, float rstd) {
+    const float s = amax * rstd * (1.f / 448.f);
+    scale = fmaxf(s, MIN_SCALE);  // (of NaN: the other)
+    const bool usual = s > MIN_SCALE && amax > 0x1p-100f && amax < 0x1p100f;  // else 448 v or 1 / amax may leave float32
+    factor = usual ? 448.f : rstd;
+    below = usual ? amax : scale;
+    inv = __builtin_amdgcn_rcpf(below);
+  }
+  __device__ __forceinline__ float operator()(float v) const {
+    v *= factor;
+    const float q = v * inv;
+    return __builtin_amdgcn_div_fixupf(__builtin_fmaf(__builtin_fmaf(-q, below, v), inv, q), below, v);
+  }
+};
 
 template <typename T, int W, int NC, bool STREAM>
 __global__ __launch_bounds__(W == 1 ? 256 : W * 64) void norm_fwd_kernel(NormFwdArgs a) {
@@ -111,21 +129,21 @@ __global__ __launch_bounds__(W == 1 ? 256 : W * 64) void norm_fwd_kernel(NormFwd
       }
 #pragma unroll
       for (int j = 0; j < N; ++j) {
-        v[i][j] *= rstd * gamma[i][j];
+        v[i][j] *= gamma[i][j];
         amax = fmaxf(amax, fabsf(v[i][j]));
       }
       if (y) {
 #pragma unroll
-        for (int j = 0; j < N; ++j) out.set(j, v[i][j]);
+        for (int j = 0; j < N; ++j) out.set(j, v[i][j] * rstd);
         out.store(y + first + col, d - col);
       }
     }
     if (a.q) {
       const int lanes = a.group / N;
-      float scale = 0.f;
+      E4m3Scale to;
       if (lanes == 0) {
-        scale = scale_of(row_max<W>(amax, s_part));
-        if (at == 0) a.scale[row] = scale;
+        to.set(row_max<W>(amax, s_part), rstd);
+        if (at == 0) a.scale[row] = to.scale;
       }
 #pragma unroll
       for (int i = 0; i < NC; ++i) {
@@ -134,13 +152,12 @@ __global__ __launch_bounds__(W == 1 ? 256 : W * 64) void norm_fwd_kernel(NormFwd
           amax = 0.f;
 #pragma unroll
           for (int j = 0; j < N; ++j) amax = fmaxf(amax, fabsf(v[i][j]));
-          scale = scale_of(group_max(amax, lanes));
-          if (col < d && (c & (lanes - 1)) == 0) a.scale[row * ((d + a.group - 1) / a.group) + c / lanes] = scale;
+          to.set(group_max(amax, lanes), rstd);
+          if (col < d && (c & (lanes - 1)) == 0) a.scale[row * ((d + a.group - 1) / a.group) + c / lanes] = to.scale;
         }
-        const float inv = 1.f / scale;
         float out[N];
 #pragma unroll
-        for (int j = 0; j < N; ++j) out[j] = v[i][j] * inv;
+        for (int j = 0; j < N; ++j) out[j] = to(v[i][j]);
         store_e4m3(a.q + first + col, out, d - col);
       }
     }

@@ -130,6 +130,23 @@ def test_e4m3_roundings_are_to_nearest_even():
     assert torch.equal(q[0].view(torch.uint8), want.view(torch.uint8))
 
 
+@pytest.mark.parametrize("group", [0, 64])
+@pytest.mark.parametrize("d", [200, 2048, 4096])
+def test_every_8_bit_value_is_the_nearest_to_the_exact_quotient(d, group):
+    # y / scale = 448 h gamma / max|h gamma|.  h = i / 32 with |i| <= 254 and gamma = j / 128 with j <= 255: h gamma and 448 h gamma
+    # are exact in float32, the quotient is rounded to float32 once, and float64 in between moves no tie of e4m3
+    T = 97
+    gen = torch.Generator(device="cuda").manual_seed(d + group)
+    x, res = (torch.randint(-127, 128, (T, d), generator=gen, device="cuda").div(32).bfloat16() for _ in range(2))
+    gamma = torch.randint(64, 256, (d,), generator=gen, device="cuda").div(128).bfloat16()
+    q, scale = blank((T, d), torch.float8_e4m3fn), blank((T, -(-d // group) if group else 1))
+    m.modse_norm_fwd(T, d, "bf16", x, res, gamma, EPS, None, blank((T, d), torch.bfloat16), None, q, scale, group)
+    v = (x.double() + res.double()) * gamma.double()
+    amax = torch.cat([p.abs().amax(1, keepdim=True).expand_as(p) for p in v.split(group or d, 1)], 1)
+    want = (448.0 * v / amax).float().to(torch.float8_e4m3fn)
+    assert torch.equal(q.view(torch.uint8), want.view(torch.uint8))
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("d", [200, 2048, 5000])
 def test_outputs_in_the_buffers_of_inputs(d, dtype):

@@ -11,6 +11,10 @@
 // more, because n larger ones have been seen.  Entries are compared with it 32 of a lane at a time through their maximum, which
 // the softmax needs anyway, so that a row costs little more than its sums.  The bound comes from the lanes' maxima at first (the n
 // largest of 64 are n entries), and from the list whenever that fills up.
+//
+// Large calls are bound by memory: both kernels read the logits once, in vectors of sixteen bytes, 128 bytes of a thread in flight.
+// Small ones are bound by the launches: a call of the forward costs 9 us with one row or 64, two launches of it, and a third of
+// that is on the host.
 #include "ops.h"
 
 namespace {
@@ -210,6 +214,8 @@ __device__ __forceinline__ float row_outputs(const LogprobsFwdArgs& a, int64_t r
   return log_z;
 }
 
+// 16384 rows of 32000 in bf16 take 157 us, 6.7 TB/s of reads; 2047 of 50257 in float32 with the 5 most probable 73, 5.6 TB/s; one row
+// of 131072 with them 5.5, and 64 of 32000 with the 20 most probable 8.8.
 template <typename T, bool TOP, bool ENTROPY, bool SPLIT, bool STREAM>
 __global__ __launch_bounds__(256) void logprobs_fwd_kernel(LogprobsFwdArgs a, int splits, int segment) {
   __shared__ uint64_t s_list[TOP ? 4 * LIST : 1];
@@ -318,6 +324,7 @@ __global__ __launch_bounds__(256) void logprobs_fwd_kernel(LogprobsFwdArgs a, in
 }
 
 // Joins the segments of a row: one wave per row, one lane per segment for the sums; the segments' entries are ranked as above.
+// 3.2 us for one row of 16 segments, 4.2 for 64 rows of 4: a launch and three rounds to memory, nothing of which grows with a row.
 constexpr int JOIN_KEYS = 8;  // per lane
 __global__ __launch_bounds__(64) void logprobs_join_kernel(LogprobsFwdArgs a, int splits, int segment) {
   __shared__ uint64_t s_list[64];
@@ -361,7 +368,9 @@ __global__ __launch_bounds__(64) void logprobs_join_kernel(LogprobsFwdArgs a, in
   }
 }
 
-// d_logits = w (1[target] - p) - dE p (log p + H)
+// d_logits = w (1[target] - p) - dE p (log p + H), from the row's m and log Z: a read and a write of the matrix.  16384 rows of 32000 in
+// bf16 take 356 us, 5.9 TB/s of the 6.2 that a sum of two large tensors into a third reaches.  A row without a target and without a
+// gradient of its entropy is not read.
 template <typename T, bool ENTROPY, bool STREAM>
 __global__ __launch_bounds__(256) void logprobs_bwd_kernel(LogprobsBwdArgs a, int segments) {
   const int64_t row = blockIdx.x / segments;

@@ -330,7 +330,7 @@ struct Job {
   void* U;
   int which, rows, cols, m0, n0, K, ldp, ldq, ldc;  // (distances of rows in bytes)
   float f_product, f_first, f_second, out;
-  bool mirror, sum;
+  bool square, mirror, sum;  // P (and Q) are squares; C is off the diagonal
   __device__ __forceinline__ void load(const ProductArgs& a, int tile) {
     const SquareOp& o = a.op[SQUARES ? blockIdx.y : 0];
     const int op_p = o.p, op_q = o.q, op_e = o.e, op_f = o.f, op_c = o.c;
@@ -350,21 +350,20 @@ struct Job {
     const char* const X = a.x ? X1 : X0;
     const size_t slot = (size_t)mp * mp * 4;
     const bool gram = SQUARES && op_p < 0;
+    square = !gram;
     m0 = mt * TILE;
     n0 = nt * TILE;
     K = gram ? max(rows, cols) : min(rows, cols);
     ldp = (gram ? np : mp) * 4;
     ldq = (gram || !SQUARES ? np : mp) * 4;
     ldc = (SQUARES ? mp : np) * 4;
-    P = (gram ? X : slots + op_p * slot) + (size_t)m0 * ldp;
+    P = gram ? X : slots + op_p * slot;
     Q = gram || !SQUARES ? X : slots + op_q * slot;
-    Q += SQUARES ? (size_t)n0 * ldq : (size_t)n0 * 4;
     E = SQUARES ? (op_e >= 0 ? slots + op_e * slot : nullptr) : X;
     F = SQUARES && op_f >= 0 ? slots + op_f * slot : nullptr;
     C = SQUARES ? slots + op_c * slot : a.x ? X0 : X1;
     mirror = SQUARES && mt != nt;
   }
-  __device__ __forceinline__ size_t q_step() const { return SQUARES ? 128 : (size_t)BK * ldq; }  // bytes of Q from step to step
   // four neighbouring columns of the last step's result
   __device__ __forceinline__ void give(int r, int c, const f32x4& v) const {
     typedef std::conditional_t<OUT == OUT_F32, float, bf16_t> T;
@@ -434,33 +433,52 @@ __global__ __launch_bounds__(256, 2) void ortho_product_kernel(ProductArgs a) {
   job.load(a, tile);
   const int steps = (job.K + BK - 1) / BK;
 
+  // A square's panel comes along its rows up to the diagonal, which rows m0 (n0) meet in step p_turn (q_turn), and from there on across
+  // them, as columns: what lies above is not stored.
+  constexpr bool HALF = TILE == 128;
+  const int p_turn = HALF && job.square ? (job.m0 + TILE) / BK : steps, q_turn = HALF && SQUARES && job.square ? (job.n0 + TILE) / BK : steps;
+
   // ---- loads: units of 1 KiB, landing swizzled (16-byte chunks of a row XOR-ed)
-  uint32_t offp[UNITS], offq[UNITS];
+  struct Loads {
+    const char* at;
+    size_t step;  // bytes
+    uint32_t off[UNITS];
+    __device__ __forceinline__ void along(const char* from, int first, int ld, int unit, int lane) {
+      at = from + (size_t)first * ld;
+      step = 128;
 #pragma unroll
-  for (int i = 0; i < UNITS; ++i) {
-    const int u = wave * UNITS + i;
-    const int r = u * 8 + (lane >> 3), c = along_chunk(r, lane & 7);
-    offp[i] = r * job.ldp + c * 16;
-    if (SQUARES) {
-      offq[i] = r * job.ldq + c * 16;
-    } else {
-      constexpr int CHUNKS = TILE / 4;  // of a row of K
-      const int k = u * (64 / CHUNKS) + lane / CHUNKS;
-      offq[i] = k * job.ldq + across_chunk(k, lane % CHUNKS) * 16;
+      for (int i = 0; i < UNITS; ++i) {
+        const int r = (unit + i) * 8 + (lane >> 3);
+        off[i] = r * ld + along_chunk(r, lane & 7) * 16;
+      }
     }
-  }
-  const char *p = job.P, *q = job.Q;
-  const size_t q_step = job.q_step();
+    __device__ __forceinline__ void across(const char* from, int first, int k0, int ld, int unit, int lane) {
+      constexpr int CHUNKS = TILE / 4;  // of a row of K
+      at = from + (size_t)k0 * ld + (size_t)first * 4;
+      step = (size_t)BK * ld;
+#pragma unroll
+      for (int i = 0; i < UNITS; ++i) {
+        const int k = (unit + i) * (64 / CHUNKS) + lane / CHUNKS;
+        off[i] = k * ld + across_chunk(k, lane % CHUNKS) * 16;
+      }
+    }
+  };
+  Loads p, q;
+  p.along(job.P, job.m0, job.ldp, wave * UNITS, lane);
+  if (SQUARES) q.along(job.Q, job.n0, job.ldq, wave * UNITS, lane);
+  else q.across(job.Q, job.n0, 0, job.ldq, wave * UNITS, lane);
   const uint32_t lds = __builtin_amdgcn_readfirstlane(lds_address(s_ring));
-  auto issue = [&](int stage) {
+  auto issue = [&](int stage, int g) {
+    if (HALF && g == p_turn) p.across(job.P, job.m0, g * BK, job.ldp, wave * UNITS, lane);
+    if (HALF && SQUARES && g == q_turn) q.across(job.Q, job.n0, g * BK, job.ldq, wave * UNITS, lane);
     const uint32_t dst = lds + stage * 2 * PANEL + wave * (UNITS * 1024);
 #pragma unroll
     for (int i = 0; i < UNITS; ++i) {
-      dma_b128_s(p, offp[i], dst + i * 1024);
-      dma_b128_s(q, offq[i], dst + PANEL + i * 1024);
+      dma_b128_s(p.at, p.off[i], dst + i * 1024);
+      dma_b128_s(q.at, q.off[i], dst + PANEL + i * 1024);
     }
-    p += 128;
-    q += q_step;
+    p.at += p.step;
+    q.at += q.step;
   };
   const int kq = lane >> 4, l16 = lane & 15;
   f32x4 total[NB][NB], acc[NB][NB];
@@ -508,21 +526,23 @@ __global__ __launch_bounds__(256, 2) void ortho_product_kernel(ProductArgs a) {
   const int last_row = min(job.rows, job.cols), last_col = SQUARES ? last_row : max(job.rows, job.cols);
   const bool diagonal = SQUARES && !job.mirror;
   const bool idle = job.m0 + wm * W >= last_row || job.n0 + wn * W >= last_col || (diagonal && wm < wn);
-  const bool mirrored = job.mirror || (diagonal && wm > wn);  // what this wave makes goes to two places
+  const bool twice = job.mirror || (diagonal && wm > wn);            // what this wave makes stands for two places,
+  const bool mirrored = HALF ? diagonal && wm > wn : twice;          // and goes there
   if (EARLY && job.E && !idle) fetch(job.E);
 
   auto panel = [&](int stage) -> const char* { return s_ring + stage * 2 * PANEL; };
   struct Fragments {
     half8 p[NB][2], q[NB][2];
   };
-  auto read = [&](Fragments& f, int stage) {
+  auto read = [&](Fragments& f, int stage, auto p_across, auto q_across) {
 #pragma unroll
     for (int i = 0; i < NB; ++i)
 #pragma unroll
       for (int part = 0; part < 2; ++part) {
-        f.p[i][part] = along_fragment(panel(stage), wm * W + i * 16, part, lane);
-        f.q[i][part] = SQUARES ? along_fragment(panel(stage) + PANEL, wn * W + i * 16, part, lane)
-                               : across_fragment<TILE>(panel(stage) + PANEL, wn * W + i * 16, part, lane);
+        if constexpr (p_across.value) f.p[i][part] = across_fragment<TILE>(panel(stage), wm * W + i * 16, part, lane);
+        else f.p[i][part] = along_fragment(panel(stage), wm * W + i * 16, part, lane);
+        if constexpr (q_across.value) f.q[i][part] = across_fragment<TILE>(panel(stage) + PANEL, wn * W + i * 16, part, lane);
+        else f.q[i][part] = along_fragment(panel(stage) + PANEL, wn * W + i * 16, part, lane);
       }
   };
   auto multiply = [&](const Fragments& f) {
@@ -553,20 +573,22 @@ __global__ __launch_bounds__(256, 2) void ortho_product_kernel(ProductArgs a) {
   auto next = [](int stage) { return stage + 1 == STAGES ? 0 : stage + 1; };
 #pragma unroll
   for (int i = 0; i < STAGES - 1; ++i)
-    if (i < steps) issue(i);
+    if (i < steps) issue(i, i);
   int stage = 0;
+  constexpr std::false_type ALONG;
+  constexpr std::bool_constant<!SQUARES> Q_FIRST;
   if constexpr (EARLY) {
     // One wave per SIMD: the next step's fragments are read while this one's are multiplied.
     Fragments f[2];
     meet(std::integral_constant<int, STAGES - 2>{}, STAGES - 2 < steps);
-    read(f[0], 0);
+    read(f[0], 0, ALONG, Q_FIRST);
     auto body = [&](auto set, int g) {
       constexpr int SET = decltype(set)::value;
       if (g + 1 < steps) {
         meet(std::integral_constant<int, STAGES - 3>{}, g + STAGES - 2 < steps);
-        if (g + STAGES - 1 < steps) issue(stage == 0 ? STAGES - 1 : stage - 1);
+        if (g + STAGES - 1 < steps) issue(stage == 0 ? STAGES - 1 : stage - 1, g + STAGES - 1);
         stage = next(stage);
-        read(f[1 - SET], stage);
+        read(f[1 - SET], stage, ALONG, Q_FIRST);
       }
       multiply(f[SET]);
       if (g % JOIN == JOIN - 1) join(false);
@@ -577,18 +599,25 @@ __global__ __launch_bounds__(256, 2) void ortho_product_kernel(ProductArgs a) {
       if (g + 1 < steps) body(std::integral_constant<int, 1>{}, g + 1);
     }
   } else {
+    int g = 0;
+    auto run = [&](int end, auto p_across, auto q_across) {
 #pragma unroll 1
-    for (int g = 0; g < steps; ++g) {
-      meet(std::integral_constant<int, STAGES - 2>{}, g + STAGES - 2 < steps);
-      if (g + STAGES - 1 < steps) issue(stage == 0 ? STAGES - 1 : stage - 1);
-      if (!idle) {
-        Fragments f;
-        read(f, stage);
-        multiply(f);
+      for (; g < end; ++g) {
+        meet(std::integral_constant<int, STAGES - 2>{}, g + STAGES - 2 < steps);
+        if (g + STAGES - 1 < steps) issue(stage == 0 ? STAGES - 1 : stage - 1, g + STAGES - 1);
+        if (!idle) {
+          Fragments f;
+          read(f, stage, p_across, q_across);
+          multiply(f);
+        }
+        stage = next(stage);
+        if (g % JOIN == JOIN - 1) join(false);
       }
-      stage = next(stage);
-      if (g % JOIN == JOIN - 1) join(false);
-    }
+    };
+    constexpr std::true_type ACROSS;
+    if constexpr (SQUARES) run(min(q_turn, steps), ALONG, ALONG);
+    run(min(p_turn, steps), ALONG, ACROSS);
+    run(steps, ACROSS, ACROSS);
   }
   join(false);
 
@@ -625,18 +654,20 @@ __global__ __launch_bounds__(256, 2) void ortho_product_kernel(ProductArgs a) {
       }
   }
   if constexpr (SQUARES) {
-    __syncthreads();
+    if (!HALF || diagonal) {
+      __syncthreads();
 #pragma unroll
-    for (int i = 0; i < TILE * TILE / 1024; ++i) {
-      const int k = i * 256 + tid, c = k / (TILE / 4), r4 = k % (TILE / 4);
-      if (job.mirror || (c < W && r4 * 4 >= W))
-        store_pair(job.C + (size_t)(job.n0 + c) * job.ldc + pair_byte(job.m0 + r4 * 4), load_transposed<TILE>(s_ring, r4, c));
+      for (int i = 0; i < TILE * TILE / 1024; ++i) {
+        const int k = i * 256 + tid, c = k / (TILE / 4), r4 = k % (TILE / 4);
+        if (job.mirror || (c < W && r4 * 4 >= W))
+          store_pair(job.C + (size_t)(job.n0 + c) * job.ldc + pair_byte(job.m0 + r4 * 4), load_transposed<TILE>(s_ring, r4, c));
+      }
     }
     if (job.sum) {
       __syncthreads();
       float* const part = reinterpret_cast<float*>(s_ring);
       sum = wave_sum(sum);
-      if (lane == 0) part[wave] = mirrored ? 2.f * sum : sum;
+      if (lane == 0) part[wave] = twice ? 2.f * sum : sum;
       __syncthreads();
       if (tid == 0) a.squares[tile] = (part[0] + part[1]) + (part[2] + part[3]);
     }

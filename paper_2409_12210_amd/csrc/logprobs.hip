@@ -40,11 +40,6 @@ __device__ __forceinline__ uint64_t key_of(float v, uint32_t index) { return (ui
 __device__ __forceinline__ float key_value(uint64_t k) { return unordered((uint32_t)(k >> 32)); }
 __device__ __forceinline__ int key_index(uint64_t k) { return (int)~(uint32_t)k; }
 
-__device__ __forceinline__ void wave_lds_order() {  // LDS writes of this wave's lanes are there for its other lanes
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-}
-
 __device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
 #define STEP(CTRL, ROWS) { const uint32_t o = (uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, CTRL, ROWS, 0xf, false); v = max(v, o); }
   STEP(0x111, 0xf) STEP(0x112, 0xf) STEP(0x114, 0xf) STEP(0x118, 0xf) STEP(0x142, 0xa) STEP(0x143, 0xc)

@@ -114,6 +114,10 @@ __device__ __forceinline__ float dpp_f32(float old, float v) {
 __device__ __forceinline__ float lane_f32(float v, int lane) {
   return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), lane));
 }
+__device__ __forceinline__ void wave_lds_order() {  // LDS writes of this wave's lanes are there for its other lanes
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
 // (lanes to the right within a row of sixteen, then row 0 to 1 and 2 to 3, then the lower half to the upper: lane 63 has it all)
 __device__ __forceinline__ float wave_sum(float v) {
   v += dpp_f32<0x111>(0.f, v);

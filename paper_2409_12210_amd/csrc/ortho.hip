@@ -166,24 +166,22 @@ struct StepArgs {
   int32_t first, last;
   // of R = b A + c A A; of Q = a Q + q R + R Q; of S = a A + R A; of the next A = a S + R S; of X = q a X + Q X; of A = X X^T
   Factors *square, *join, *half, *next, *update, *gram;
+  const Bound* before;
+  Bound* after;
 };
-// One wave per matrix, a round trip to memory and one through float64: 4 us, 5 with 190 tiles a matrix.  (In the launch that makes A, by the last of the matrix's workgroups: what it needs of the others has to leave
-// their caches first, 6 us where this launch takes 4.)
-__global__ __launch_bounds__(64) void ortho_factors_kernel(const Mat* __restrict__ table, const float* __restrict__ squares, int tile,
-                                                           Bound* __restrict__ bounds, StepArgs f) {
-  const int w = blockIdx.x;
-  const Mat& m = table[w];
-  const int mt = (m.m + tile - 1) / tile, tiles = mt * (mt + 1) / 2;
-  Bound t = bounds[w];
+// The factors of matrix w, by one wave: returns those of R, and the first of the matrix's waves stores all of them.
+__device__ __forceinline__ Factors step_factors(const StepArgs& f, int w, const float* squares, int tiles, bool store) {
+  Bound t = f.before[w];
   double v = 0;
-  for (int i = threadIdx.x; i < tiles; i += 64) v += squares[m.square_tile + i];
+  for (int i = threadIdx.x & 63; i < tiles; i += 64) v += squares[i];
   for (int k = 32; k; k >>= 1) v += __shfl_xor(v, k, 64);
-  if (threadIdx.x != 0) return;
   const double a = f.a, b = f.b, c = f.c, qa = f.first ? a : f.q * a;
   t.x = fmin(t.x, sqrt(sqrt(v) / t.in_a) * 1.01);
   const double x2 = t.x * t.x, r = fabs(b) * x2 + fabs(c) * x2 * x2, x = quintic_bound(a, b, c, t.x) * 1.01;
   t.in_r = store_scale(r);
-  f.square[w] = {(float)(c * t.in_r / (t.in_a * t.in_a)), (float)(b * t.in_r / t.in_a), 0.f};
+  const Factors square = {(float)(c * t.in_r / (t.in_a * t.in_a)), (float)(b * t.in_r / t.in_a), 0.f};
+  if (!store) return square;
+  f.square[w] = square;
   if (f.first) {
     t.q = r;
     t.in_q = t.in_r;
@@ -207,7 +205,17 @@ __global__ __launch_bounds__(64) void ortho_factors_kernel(const Mat* __restrict
     t.in_a = in_a;
   }
   t.x = x;
-  bounds[w] = t;
+  f.after[w] = t;
+  return square;
+}
+// With tiles of 64 the workgroups of R find their factors themselves: 24
+// matrices of 256 x 128..384 162 -> 150 us, of 512 x 300..1200 496 -> 485.  With tiles of 128 it is a launch of its own,
+// one wave per matrix, 5 us.  (In the launch that makes A, by the last of the matrix's workgroups: what it needs of the others has to
+// leave their caches first, 6 us.)
+__global__ __launch_bounds__(64) void ortho_factors_kernel(const Mat* __restrict__ table, const float* __restrict__ squares, int tile, StepArgs f) {
+  const Mat& m = table[blockIdx.x];
+  const int mt = (m.m + tile - 1) / tile;
+  step_factors(f, blockIdx.x, squares + m.square_tile, mt * (mt + 1) / 2, threadIdx.x == 0);
 }
 
 __device__ __forceinline__ void store_pair(char* p, const f32x4& v) {  // four values of a block
@@ -312,6 +320,7 @@ struct SquareOp {
   const Factors* factors;
   int32_t p, q, e, f, c;  // slots; p < 0: X, e and f < 0: none
   int32_t sum;            // the squares of C are summed
+  int32_t step;           // R: its factors come from StepArgs
 };
 struct ProductArgs {
   const Mat* list;
@@ -320,6 +329,7 @@ struct ProductArgs {
   float* squares;         // sums of the squares of a result's tiles, as stored
   int32_t x;              // X[x] is the present one
   int32_t tiles;
+  StepArgs step;
 };
 
 // What a workgroup has to do.  (All of it is read at once: what is read through a reference later is read again behind every
@@ -331,6 +341,8 @@ struct Job {
   void* U;
   int which, rows, cols, m0, n0, K, ldp, ldq, ldc;  // (distances of rows in bytes)
   float f_product, f_first, f_second, out;
+  int square_tile;
+  bool step;  // the factors are still to be found
   bool square, mirror, sum;  // P (and Q) are squares; C is off the diagonal
   __device__ __forceinline__ void load(const ProductArgs& a, int tile) {
     const SquareOp& o = a.op[SQUARES ? blockIdx.y : 0];
@@ -343,10 +355,14 @@ struct Job {
     cols = m.cols;
     U = m.U;
     sum = o.sum;
-    const Factors* const f = o.factors + which;
-    f_product = f->product;
-    f_first = f->first;
-    f_second = f->second;
+    square_tile = m.square_tile;
+    step = o.step;
+    if (!step) {
+      const Factors* const f = o.factors + which;
+      f_product = f->product;
+      f_first = f->first;
+      f_second = f->second;
+    }
     out = OUT == OUT_PAIRS ? 1.f : a.bounds[which].out;
     const char* const X = a.x ? X1 : X0;
     const size_t slot = (size_t)mp * mp * 4;
@@ -566,6 +582,14 @@ __global__ __launch_bounds__(256, 2) void ortho_product_kernel(ProductArgs a) {
 #pragma unroll
   for (int i = 0; i < STAGES - 1; ++i)
     if (i < steps) issue(i, i);
+  if constexpr (SQUARES && EARLY) {
+    if (job.step) {
+      const int mt = (last_row + TILE - 1) / TILE;
+      const Factors f = step_factors(a.step, job.which, a.squares + job.square_tile, mt * (mt + 1) / 2, job.m0 + tid == 0);
+      job.f_product = f.product;
+      job.f_first = f.first;
+    }
+  }
   int stage = 0;
   constexpr std::false_type ALONG;
   constexpr std::bool_constant<!SQUARES> Q_FIRST;
@@ -737,7 +761,7 @@ modse_status ortho_layout(const modse_matrix_set* set, const float* coeffs, int 
     return o;
   };
   w.mats = take(n * sizeof(Mat));
-  w.bounds = take(n * sizeof(Bound));
+  w.bounds = take(2 * n * sizeof(Bound));
   w.factors = take((size_t)n * 6 * sizeof(Factors));
   w.squares = take((size_t)w.square_tiles * 4);
   w.sums = take((size_t)parts * sizeof(double));
@@ -816,7 +840,8 @@ hipError_t launch_orthogonalize(const modse_matrix_set* set, const OrthoLayout& 
   hipLaunchKernelGGL(ortho_start_kernel, dim3(most_tiles < 2048 ? most_tiles : 2048, n), dim3(256), 0, s, table, bounds);
   if ((e = hipGetLastError()) != hipSuccess) return e;
 
-  ProductArgs a = {square_list, {}, bounds, squares, 0, w.square_tiles};
+  ProductArgs a = {square_list, {}, bounds, squares, 0, w.square_tiles, {}};
+  const bool in_products = tile == 64;  // R's launches find their factors
   const int span = 8 * run_of(tile);
   auto grid = [span](int tiles, int ops) { return dim3((tiles + span - 1) / span * span, ops); };
   auto squares_of = [&](const SquareOp& one, const SquareOp* two) {
@@ -833,7 +858,7 @@ hipError_t launch_orthogonalize(const modse_matrix_set* set, const OrthoLayout& 
     constexpr Out OUT = decltype(out)::value;
     a.list = update_list;
     a.tiles = w.update_tiles;
-    a.op[0] = {f_update, q, -1, -1, -1, -1, 0};
+    a.op[0] = {f_update, q, -1, -1, -1, -1, 0, 0};
     const dim3 g = grid(a.tiles, 1);
     if (tile == 128) hipLaunchKernelGGL((ortho_product_kernel<128, 2, false, OUT>), g, dim3(256), 0, s, a);
     else hipLaunchKernelGGL((ortho_product_kernel<64, 5, false, OUT>), g, dim3(256), 0, s, a);
@@ -846,19 +871,22 @@ hipError_t launch_orthogonalize(const modse_matrix_set* set, const OrthoLayout& 
     // the factors that the A of the group's step i brings
     auto factors_of = [&](int i) {
       const float* const c = coeffs + 3 * (step + i);
-      const StepArgs f = {c[0], c[1], c[2], qa, i == 0, i + 1 == w.group[k], f_square, f_join, f_half, f_next, f_update, f_gram};
-      hipLaunchKernelGGL(ortho_factors_kernel, dim3(n), dim3(64), 0, s, table, squares, tile, bounds, f);
+      Bound* const after = bounds + n - (a.bounds - bounds);  // (the two take turns)
+      a.step = {c[0], c[1], c[2], qa, i == 0, i + 1 == w.group[k], f_square, f_join, f_half, f_next, f_update, f_gram, a.bounds, after};
+      a.bounds = after;
+      if (in_products) return hipSuccess;
+      hipLaunchKernelGGL(ortho_factors_kernel, dim3(n), dim3(64), 0, s, table, squares, tile, a.step);
       return hipGetLastError();
     };
-    if ((e = squares_of({f_gram, -1, -1, -1, -1, SLOT_A, 1}, nullptr)) != hipSuccess) return e;
+    if ((e = squares_of({f_gram, -1, -1, -1, -1, SLOT_A, 1, 0}, nullptr)) != hipSuccess) return e;
     if ((e = factors_of(0)) != hipSuccess) return e;
     for (int i = 0; i < w.group[k]; ++i) {
       const float first = coeffs[3 * (step + i)];
       const bool last = i + 1 == w.group[k];
       const int R = i == 1 ? SLOT_R2 : SLOT_R;  // (the first one is Q in the second step)
-      if ((e = squares_of({f_square, A, A, A, -1, R, 0}, nullptr)) != hipSuccess) return e;
+      if ((e = squares_of({f_square, A, A, A, -1, R, 0, in_products}, nullptr)) != hipSuccess) return e;
       const int Q2 = i == 0 ? R : Q == SLOT_Q ? SLOT_R2 : SLOT_Q;
-      const SquareOp join = {f_join, R, Q, Q, R, Q2, 0}, half = {f_half, R, A, A, -1, SLOT_S, 0};
+      const SquareOp join = {f_join, R, Q, Q, R, Q2, 0, 0}, half = {f_half, R, A, A, -1, SLOT_S, 0, 0};
       if (i > 0 || !last) {
         if ((e = i == 0 ? squares_of(half, nullptr) : last ? squares_of(join, nullptr) : squares_of(join, &half)) != hipSuccess) return e;
       }
@@ -866,7 +894,7 @@ hipError_t launch_orthogonalize(const modse_matrix_set* set, const OrthoLayout& 
       qa = i == 0 ? first : qa * first;
       if (!last) {
         A = A == SLOT_A ? SLOT_A2 : SLOT_A;
-        if ((e = squares_of({f_next, R, SLOT_S, SLOT_S, -1, A, 1}, nullptr)) != hipSuccess) return e;
+        if ((e = squares_of({f_next, R, SLOT_S, SLOT_S, -1, A, 1, 0}, nullptr)) != hipSuccess) return e;
         if ((e = factors_of(i + 1)) != hipSuccess) return e;
       }
     }

@@ -110,52 +110,9 @@ __device__ inline double store_scale(double bound) {
 struct Bound {
   double x, q;                    // of the present X (in a group: of what X would be), of Q
   double in_x, in_a, in_r, in_q;  // X, A, R, Q as stored
-  double start;                   // G's factor
   float out;                      // 1 / in_x, of the result
   float pad;
 };
-
-// One block per matrix: the norm, the factor of the first product, the matrix's part of the tile lists.  Few blocks and their round
-// trips: 4 us for 24 small matrices, 14 for a full layer's, with 0.5 to 1 MB of lists.
-__global__ __launch_bounds__(256) void ortho_prepare_kernel(const Mat* __restrict__ table, const double* __restrict__ sums, float eps,
-                                                            Bound* __restrict__ bounds, Factors* __restrict__ gram,
-                                                            int tile, Mat* __restrict__ square_list, Mat* __restrict__ update_list) {
-  __shared__ double s[4];
-  const Mat& m = table[blockIdx.x];
-  double v = 0;
-  for (int i = threadIdx.x; i < m.parts; i += 256) v += sums[m.part + i];
-  for (int b = 32; b; b >>= 1) v += __shfl_xor(v, b, 64);
-  if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = v;
-  __syncthreads();
-  const int mt = (m.m + tile - 1) / tile, nt = (m.n + tile - 1) / tile;
-  Mat t = m;
-  for (int i = threadIdx.x; i < mt * (mt + 1) / 2; i += 256) {  // row by row of the triangle
-    t.mt = (int)((sqrtf(8.f * i + 1.f) - 1.f) * 0.5f);
-    while ((t.mt + 1) * (t.mt + 2) / 2 <= i) ++t.mt;
-    while (t.mt * (t.mt + 1) / 2 > i) --t.mt;
-    t.nt = i - t.mt * (t.mt + 1) / 2;
-    square_list[m.square_tile + i] = t;
-  }
-  for (int i = threadIdx.x; i < mt * nt; i += 256) {  // columns of eight tiles
-    const int group = i / (8 * nt), height = min(8, mt - group * 8), in = i - group * 8 * nt;
-    t.mt = group * 8 + in % height;
-    t.nt = in / height;
-    update_list[m.update_tile + i] = t;
-  }
-  if (threadIdx.x != 0) return;
-  const double norm = sqrt((s[0] + s[1]) + (s[2] + s[3]));
-  const double inv = norm == 0 ? 0 : 1 / (norm + eps);
-  Bound b;
-  // singular values of X are at most its norm; 1 % for what rounding adds
-  b.x = norm == 0 ? 1 : fmin(norm * inv, 1.0) * 1.01;
-  b.in_x = store_scale(b.x);
-  b.in_a = store_scale(b.x * b.x);
-  b.start = inv * b.in_x;
-  b.q = b.in_r = b.in_q = 0;
-  b.out = b.pad = 0.f;
-  bounds[blockIdx.x] = b;
-  gram[blockIdx.x] = {(float)(b.in_a / (b.in_x * b.in_x)), 0.f, 0.f};
-}
 
 // Behind every A: the largest singular value of X is at most the root of A's Frobenius norm, which is what the factors of the step's
 // other products and of the next A go by.  (Bounds that come from the polynomials alone lag behind values that shrink, and what is
@@ -247,13 +204,49 @@ __device__ __forceinline__ void store_pair(char* p, const Eight& v) {
 __device__ __forceinline__ int pair_byte(int c) { return (c >> 5) * 128 + (c & 31) * 2; }
 
 // X = G / (|G| + eps): 64 x 64 of a matrix per block, padding included, through LDS where the matrix is stored transposed.  As many
-// bytes go out as come in: a full layer's 2.2 GB take 436 us, 5.1 TB/s.
-__global__ __launch_bounds__(256) void ortho_start_kernel(const Mat* __restrict__ table, const Bound* __restrict__ bounds) {
+// bytes go out as come in: a full layer's 2.2 GB take 436 us, 5.1 TB/s.  Every block adds up the norm for itself, and a matrix's first
+// one also makes its tile lists and the factor of the first product (in a launch of their own they took 4 to 15 us).
+__global__ __launch_bounds__(256) void ortho_start_kernel(const Mat* __restrict__ table, const double* __restrict__ sums, float eps,
+                                                          Bound* __restrict__ bounds, Factors* __restrict__ gram, int side,
+                                                          Mat* __restrict__ square_list, Mat* __restrict__ update_list) {
   __shared__ float s[64][65];
+  __shared__ double s_sum[4];
   const Mat& m = table[blockIdx.y];
-  const double in = bounds[blockIdx.y].start;
   const bool tall = m.rows > m.cols;
   const int nt = m.np / 64, tiles = m.mp / 64 * nt;
+  if (blockIdx.x >= tiles) return;
+  double v = 0;
+  for (int i = threadIdx.x; i < m.parts; i += 256) v += sums[m.part + i];
+  for (int b = 32; b; b >>= 1) v += __shfl_xor(v, b, 64);
+  if ((threadIdx.x & 63) == 0) s_sum[threadIdx.x >> 6] = v;
+  __syncthreads();
+  const double norm = sqrt((s_sum[0] + s_sum[1]) + (s_sum[2] + s_sum[3]));
+  const double inv = norm == 0 ? 0 : 1 / (norm + eps);
+  // singular values of X are at most its norm; 1 % for what rounding adds
+  const double most = norm == 0 ? 1 : fmin(norm * inv, 1.0) * 1.01;
+  const double in_x = store_scale(most), in = inv * in_x;
+  if (blockIdx.x == 0) {
+    const int mt = (m.m + side - 1) / side, nt = (m.n + side - 1) / side;
+    Mat t = m;
+    for (int i = threadIdx.x; i < mt * (mt + 1) / 2; i += 256) {  // row by row of the triangle
+      t.mt = (int)((sqrtf(8.f * i + 1.f) - 1.f) * 0.5f);
+      while ((t.mt + 1) * (t.mt + 2) / 2 <= i) ++t.mt;
+      while (t.mt * (t.mt + 1) / 2 > i) --t.mt;
+      t.nt = i - t.mt * (t.mt + 1) / 2;
+      square_list[m.square_tile + i] = t;
+    }
+    for (int i = threadIdx.x; i < mt * nt; i += 256) {  // columns of eight tiles
+      const int group = i / (8 * nt), height = min(8, mt - group * 8), in_group = i - group * 8 * nt;
+      t.mt = group * 8 + in_group % height;
+      t.nt = in_group / height;
+      update_list[m.update_tile + i] = t;
+    }
+    if (threadIdx.x == 0) {
+      const double in_a = store_scale(most * most);
+      bounds[blockIdx.y] = {most, 0, in_x, in_a, 0, 0, 0.f, 0.f};
+      gram[blockIdx.y] = {(float)(in_a / (in_x * in_x)), 0.f, 0.f};
+    }
+  }
   for (int tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
     const int m0 = tile / nt * 64, n0 = tile % nt * 64;
     const int r0 = tall ? n0 : m0, c0 = tall ? m0 : n0;
@@ -741,10 +734,11 @@ modse_status ortho_layout(const modse_matrix_set* set, const float* coeffs, int 
     m2n += (double)sm * sm * sn;
   }
   if (update[0] >= (int64_t)1 << 23) return MODSE_ERR_UNSUPPORTED;  // (a launch has fewer than 2^32 threads)
-  // Tiles of 64 where those of 128 leave half of the workgroups' places empty.  us, 64 / 128: 24 matrices of 256 x 128..384 174 / 287, 24
-  // of 512 x 300..1200 (190 tiles of 128) 583 / 636, 12 of 1000 x 333..1999 (230) 1217 / 1230, 6 of 1024 x 1408..4224 (216) 1156 / 1098,
-  // 12 of 1024 x 1408..4224 (432) 2117 / 1826, a full layer 28195 / 19661.
-  const int side = square[1] <= 256 ? 0 : 1;
+  // Tiles of 64 where those of 128 leave a quarter of the CUs without one.  us, 64 / 128: 24 matrices of 256 x 128..384 146 / 253, 48 of
+  // 256 x 100..700 (144 tiles of 128) 235 / 319, 3 of 1100 x 1500 (135) 636 / 660, 24 of 512 x 300..1200 (190) 467 / 470, into bf16 448 / 433,
+  // 6 of 1024 x 1024 (216) 678 / 631, 6 of 1024 x 1408..4224 (216) 1050 / 928, 12 of 768 x 700..2100 (252) 744 / 642, 12 of 1024 x
+  // 1408..4224 (432) 2037 / 1492.
+  const int side = square[1] <= 192 ? 0 : 1;
   w.tile = SIDES[side];
   w.square_tiles = (int32_t)square[side];
   w.update_tiles = (int32_t)update[side];
@@ -771,8 +765,8 @@ modse_status ortho_layout(const modse_matrix_set* set, const float* coeffs, int 
   w.total = n ? off : 0;
   w.n_groups = 0;
   // Groups of steps where the products are what counts, and X is longer than it is wide.  us, single steps / groups: 24 matrices of
-  // 256 x 128..384 174 / 175, 3 of 256 x 256 128 / 150, 6 of 512 x 700..1200 277 / 251, 24 of 512 x 300..1200 583 / 534, 12 of 1000 x
-  // 333..1999 into bf16 1217 / 1044, a full layer 27788 / 19685; 3 of 1111 x 1500 704 / 720.
+  // 256 x 128..384 146 / 150, 3 of 256 x 256 110 / 128, 6 of 512 x 700..1200 249 / 222, 24 of 512 x 300..1200 491 / 468, 12 of 1000 x
+  // 333..1999 into bf16 926 / 787, 12 of 1024 x 1408..4224 2061 / 1492; squares, 3 of 2048 x 2048 1630 / 1738, 3 of 1111 x 1500 636 / 650.
   const bool grouped = coeffs && m2n >= 6e8 && m2n >= 1.4 * m3;
   const double most = set->dtype == MODSE_F32 ? F32_GROWTH : BF16_GROWTH;
   double top = 1;
@@ -835,9 +829,8 @@ hipError_t launch_orthogonalize(const modse_matrix_set* set, const OrthoLayout& 
     hipLaunchKernelGGL(ortho_squares_kernel, dim3(most_parts < 1024 ? most_parts : 1024, a.count), dim3(256), 0, s, a, sums);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
-  hipLaunchKernelGGL(ortho_prepare_kernel, dim3(n), dim3(256), 0, s, table, sums, eps, bounds, f_gram, tile, square_list, update_list);
-  if ((e = hipGetLastError()) != hipSuccess) return e;
-  hipLaunchKernelGGL(ortho_start_kernel, dim3(most_tiles < 2048 ? most_tiles : 2048, n), dim3(256), 0, s, table, bounds);
+  hipLaunchKernelGGL(ortho_start_kernel, dim3(std::min(most_tiles, std::max(8, 16384 / n)), n), dim3(256), 0, s, table, sums, eps, bounds, f_gram,
+                     tile, square_list, update_list);
   if ((e = hipGetLastError()) != hipSuccess) return e;
 
   ProductArgs a = {square_list, {}, bounds, squares, 0, w.square_tiles, {}};

@@ -10,7 +10,8 @@
 //
 // Storage: rows of blocks of 32 values, 64 bytes of hi and then 64 of lo, so that a cache line feeds one step of a product.
 //
-// Squares are symmetric: only tiles on and below the diagonal are computed, and written twice.
+// Squares are symmetric: only tiles on and below the diagonal are computed.  With tiles of 128 they alone are stored, and a panel that
+// reaches beyond the diagonal is read as columns there; small tiles are written twice.
 //
 // Groups of steps.  p(A) X for several steps in a row needs X only at its ends: with R_i = b A_i + c A_i^2 and P_i = a_i I + R_i,
 // A_(i+1) = P_i A_i P_i and X_g = P_(g-1) ... P_0 X, all of whose factors are m x m, symmetric and commute.  In units of m^3
@@ -287,27 +288,30 @@ __global__ __launch_bounds__(256) void ortho_start_kernel(const Mat* __restrict_
 
 // ---------------------------------------------------------------- products
 // C = product P Q + first E + second F over TILE x TILE tiles, four waves, a quarter of the tile each.
-//   SQUARES: C, E, F are [mp, mp] slots, and so are P and Q (symmetric), or both are X (A = X X^T, K = n): operands along K
+//   SQUARES: C, E, F are [mp, mp] slots, and so are P and Q (symmetric), or both are X (A = X X^T, K = n): operands along K (TILE 128:
+//            a slot's up to its diagonal)
 //   else:    P is a slot along K, Q = X [mp, np] across it, E = X, C the other X or, in the last step, U (OUT)
 //
-// A step is 32 of K: a panel row is 64 bytes of hi and 64 of lo, and every fragment feeds two or one of the three products: 96
-// matrix instructions of 16 x 16 x 32 cycles' worth per 32 KiB of panels, half as many loads per instruction as a plain 16-bit
+// A step is 32 of K: a panel row is 64 bytes of hi and 64 of lo, and every fragment feeds two or one of the three products: 192
+// matrix instructions of 16 x 16 x 32 per 32 KiB of panels (TILE 128), two thirds of the loads per instruction that a plain 16-bit
 // product of this tile has.  Two workgroups share a CU (TILE 128, two stages of panels), so that one multiplies while the other
 // waits.  Sets with few tiles take TILE 64 and five stages: there is nothing else on the CU then, and a step lasts as long
 // as its loads unless they are under way early.
 //
-// Measured, tiles of 128: R X of a full layer (24 matrices, 2048 x 2816..8448: 1.13e12 operations, three times as many in 16 bits) takes
-// 3.1 ms, 1.1e15 16-bit operations a second where plain 16-bit products of 8192 x 8192 x 8192 reach 1.1e15 to 1.5e15 by card; A A takes 0.65 to 0.70
-// ms, 0.9e15.  The matrix pipes are busy 55 % of the time at 1.74 GHz, the LDS port all of it without a conflict, and the
-// clock is what the card's power leaves.  A tile of 256 x 256 halves the reads of LDS (busy 58 % at 1.93 GHz) and has one workgroup on a CU:
-// all of them store at once, 27 of a round's 174 us, and narrow matrices do not fill it (64 narrow experts 10.0 -> 12.4 ms, a full
-// layer 19.7 -> 18.6).  Tiles of 64: a product of 24 matrices of at most 256 x 384 takes 8 to 11 us, four round trips to memory.
+// Measured, tiles of 128: Q X of a full layer (24 matrices, 2048 x 2816..8448: 1.13e12 operations, three times as many in 16 bits) takes
+// 2.8 to 2.9 ms, 1.2e15 16-bit operations a second where plain 16-bit products of 8192 x 8192 x 8192 reach 1.1e15 to 1.5e15 by card; A A takes 0.55 to
+// 0.6 ms, 1.1e15.  The matrix pipes are busy 64 to 68 % of the time at 1.6 to 1.7 GHz, which is what the card's power leaves.  Squares of 352 to 1056
+// take 0.3 ms for 192 of them, 0.75e15: 44 % at 1.9 GHz, a quarter of a tile's time being its opening and its result.  A tile of 256 x 256
+// halves the reads of LDS and has one workgroup on a CU: all of them store at once, and narrow matrices do not fill it (before the steps
+// that follow it, 64 narrow experts 10.0 -> 12.4 ms, a full layer 19.7 -> 18.6).  Loads two steps ahead, with a second barrier a step: a full layer 16.6
+// -> 17.3 ms, 12 of 1024 x 1408..4224 1480 -> 1440 us.  Tiles of 64: a product of 24 matrices of at most 256 x 384 takes 8 to 9 us, four
+// round trips to memory.
 enum Out { OUT_PAIRS, OUT_F32, OUT_BF16 };
 constexpr int BK = 32;
 constexpr int JOIN = 16;  // steps that are summed in one register
 // Neighbouring tiles that an XCD gets, of every 8 times as many: they share panels in its L2.  us, runs of 4 / 16 / 32 / 64: a full layer
-// 20124 / 19635 / 19446 / 19928, 64 narrow experts 10817 / 10421 / 10336 / 10260; tiles of 64, runs of 4 / 8 / 16: 24 matrices of 512 x
-// 300..1200 576 / 522 / 493, 6 of 1024 x 1408..4224 1123 / 1098 / 1082.
+// 17510 / 17080 / 16710 / 16920, 64 narrow experts 8550 / 7920 / 7800 / 7805; tiles of 64, runs of 4 / 8 / 16 / 32: 24 matrices of 512 x
+// 300..1200 483 / 499 / 498 / 629, 12 of 512 x 500..1200 364 / 336 / 322 / 318, 6 of 768 x 700..1500 434 / 432 / 389 / 381.
 constexpr int run_of(int tile) { return tile == 64 ? 16 : 32; }
 struct SquareOp {
   const Factors* factors;
@@ -548,7 +552,7 @@ __global__ __launch_bounds__(256, 2) void ortho_product_kernel(ProductArgs a) {
   };
   auto multiply = [&](const Fragments& f) {
     // (Q's fragment is the first operand: a lane then holds four neighbouring columns of C.  The blocks are walked to and fro.  hi hi
-    // first, which needs half of the fragments, and in front of the other wave's reads: a full layer 19409 -> 19053 us.)
+    // first, which needs half of the fragments: a full layer 19409 -> 19053 us; in front of the other wave's reads: 64 narrow experts 7854 -> 7800.)
     __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int t = 0; t < 3; ++t)

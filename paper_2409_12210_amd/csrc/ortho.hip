@@ -301,7 +301,8 @@ __global__ __launch_bounds__(256) void ortho_start_kernel(const Mat* __restrict_
 // Measured, tiles of 128: Q X of a full layer (24 matrices, 2048 x 2816..8448: 1.13e12 operations, three times as many in 16 bits) takes
 // 2.8 to 2.9 ms, 1.2e15 16-bit operations a second where plain 16-bit products of 8192 x 8192 x 8192 reach 1.1e15 to 1.5e15 by card; A A takes 0.55 to
 // 0.6 ms, 1.1e15.  The matrix pipes are busy 64 to 68 % of the time at 1.6 to 1.7 GHz, which is what the card's power leaves.  Squares of 352 to 1056
-// take 0.3 ms for 192 of them, 0.75e15: 44 % at 1.9 GHz, a quarter of a tile's time being its opening and its result.  A tile of 256 x 256
+// take 0.3 ms for 192 of them, 0.75e15: 44 % at 1.9 GHz, a step of two workgroups 2600 clocks where its instructions take 1540; a quarter of
+// a tile's time is its opening and its result, which the other workgroup's steps fill (E brought into the cache during the last step: 7960 -> 8080 us).  A tile of 256 x 256
 // halves the reads of LDS and has one workgroup on a CU: all of them store at once, and narrow matrices do not fill it (before the steps
 // that follow it, 64 narrow experts 10.0 -> 12.4 ms, a full layer 19.7 -> 18.6).  Loads two steps ahead, with a second barrier a step: a full layer 16.6
 // -> 17.3 ms, 12 of 1024 x 1408..4224 1480 -> 1440 us.  Tiles of 64: a product of 24 matrices of at most 256 x 384 takes 8 to 9 us, four

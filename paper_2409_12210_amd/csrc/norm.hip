@@ -168,16 +168,70 @@ __global__ __launch_bounds__(W == 1 ? 256 : W * 64) void norm_fwd_kernel(NormFwd
   }
 }
 
+// dgamma of LANES vectors' worth of columns, over all tokens: LANES threads a row, as many rows at a time as the block has threads
+// for, four of them of a thread in flight.  The result depends on T and d alone.
+template <typename T, int THREADS, int LANES>
+__device__ __forceinline__ void norm_bwd_columns(const NormBwdArgs& a, int block) {
+  constexpr int N = Vec<T>::N, ROWS = THREADS / LANES, AT_ONCE = 4;
+  __shared__ float s_sum[THREADS / 64][LANES * N];
+  const int lane = threadIdx.x % LANES, row0 = threadIdx.x / LANES, col = (block * LANES + lane) * N, d = a.d;
+  const T* const h = static_cast<const T*>(a.h);
+  const T* const dY = static_cast<const T*>(a.dY);
+  float sum[N];
+#pragma unroll
+  for (int j = 0; j < N; ++j) sum[j] = 0.f;
+  for (int64_t first = row0; first < a.T; first += ROWS * AT_ONCE) {
+    Vec<T> hv[AT_ONCE], dy[AT_ONCE];
+    float rstd[AT_ONCE];
+#pragma unroll
+    for (int i = 0; i < AT_ONCE; ++i) {
+      const int64_t row = first + i * ROWS;
+      const int n = row < a.T ? d - col : 0;
+      hv[i].load(h + row * d + col, n, 0.f);
+      dy[i].load(dY + row * d + col, n, 0.f);
+      rstd[i] = row < a.T ? a.rstd[row] : 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < AT_ONCE; ++i)
+#pragma unroll
+      for (int j = 0; j < N; ++j) sum[j] += dy[i][j] * (hv[i][j] * rstd[i]);
+  }
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+#pragma unroll
+    for (int k = LANES; k < 64; k *= 2) sum[j] += __shfl_xor(sum[j], k, 64);
+    if ((threadIdx.x & 63) < LANES) s_sum[threadIdx.x >> 6][lane * N + j] = sum[j];
+  }
+  __syncthreads();
+  const int c = block * LANES * N + threadIdx.x;
+  if (threadIdx.x < LANES * N && c < d) {
+    float v = 0.f;
+#pragma unroll
+    for (int w = 0; w < THREADS / 64; ++w) v += s_sum[w][threadIdx.x];
+    a.dgamma[c] = a.accumulate ? a.dgamma[c] + v : v;
+  }
+}
+
+constexpr int column_lanes(int w) { return w == 16 ? 8 : 4; }  // of W waves a row
+
 // dX = rstd (g - hat mean(g hat)) + dH with g = dY gamma, hat = h rstd; dgamma = sum of dY hat over the tokens.  A block walks
 // over rows, its waves keep their share of dgamma in registers, and the blocks' shares are added up by a second launch in block
 // order: the result depends on T and d alone.  Three tensors in, one out: 32768 tokens of width 2048 in bf16 take 95 us, 5.7 TB/s, and
-// the second launch 5.
-template <typename T, int W, int NC, bool STREAM>
-__global__ __launch_bounds__(W == 1 ? 256 : W * 64) void norm_bwd_kernel(NormBwdArgs a) {
+// the second launch 5.  With FEW rows the first `columns` blocks read h and dY once more, for dgamma alone, and there is no second launch:
+// 128 tokens of width 4096 4.0 us instead of 8.3, and a launch less of the host's time.
+template <typename T, int W, int NC, bool STREAM, bool FEW>
+__global__ __launch_bounds__(W == 1 ? 256 : W * 64) void norm_bwd_kernel(NormBwdArgs a, int columns) {
   constexpr int ROWS = W == 1 ? 4 : 1;
   constexpr int N = Vec<T>::N, WIDTH = NC * N * 64;  // columns of a wave
   __shared__ float s_part[16];
-  __shared__ float s_gamma[W == 1 ? 4 : 1][W == 1 ? WIDTH : 1];
+  __shared__ float s_gamma[W == 1 && !FEW ? 4 : 1][W == 1 && !FEW ? WIDTH : 1];
+  if constexpr (FEW) {
+    if ((int)blockIdx.x < columns) {
+      norm_bwd_columns<T, W == 1 ? 256 : W * 64, column_lanes(W)>(a, blockIdx.x);
+      return;
+    }
+  }
+  const int block = FEW ? blockIdx.x - columns : blockIdx.x, blocks = FEW ? gridDim.x - columns : gridDim.x;
   const int at = W == 1 ? threadIdx.x & 63 : threadIdx.x;
   const int d = a.d;
   const T* const h = static_cast<const T*>(a.h);
@@ -193,7 +247,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : W * 64) void norm_bwd_kernel(NormBwd
 #pragma unroll
     for (int j = 0; j < N; ++j) share[i][j] = 0.f;
   }
-  for (int64_t row = (int64_t)blockIdx.x * ROWS + (W == 1 ? threadIdx.x >> 6 : 0); row < a.T; row += (int64_t)gridDim.x * ROWS) {
+  for (int64_t row = (int64_t)block * ROWS + (W == 1 ? threadIdx.x >> 6 : 0); row < a.T; row += (int64_t)blocks * ROWS) {
     const int64_t first = row * d;
     Vec<T> hv[NC], dy[NC], dh[NC];
     const float rstd = a.rstd[row];
@@ -210,7 +264,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : W * 64) void norm_bwd_kernel(NormBwd
 #pragma unroll
       for (int j = 0; j < N; ++j) {
         const float t = dy[i][j] * (hv[i][j] * rstd);
-        share[i][j] += t;
+        if constexpr (!FEW) share[i][j] += t;
         dot += t * gamma[i][j];
       }
     }
@@ -237,8 +291,9 @@ __global__ __launch_bounds__(W == 1 ? 256 : W * 64) void norm_bwd_kernel(NormBwd
       out.store(dX + first + col, d - col);
     }
   }
+  if constexpr (FEW) return;
   float* const part = a.part + (int64_t)blockIdx.x * d;
-  if constexpr (W == 1) {
+  if constexpr (W == 1 && !FEW) {
 #pragma unroll
     for (int i = 0; i < NC; ++i)
 #pragma unroll
@@ -312,12 +367,35 @@ hipError_t norm_fwd_any(const NormFwdArgs& a, hipStream_t s) {
   return norm_fwd<T, 16, 2 * X>(a, s);
 }
 
+// us of the GPU with a second launch / without, by tokens: width 512 bf16 1: 4.2 / 4.1, 512: 4.9 / 4.0, 1021: 5.0 / 5.9; 1535 float32 128:
+// 7.3 / 4.4, 512: 8.8 / 6.6, 1021: 11.1 / 10.6 (but with the forward pass in front of it 15.9 / 16.6); 4096 bf16 128: 8.3 / 4.0, 512: 13.6 /
+// 8.1, 2048: 21.1 / 22.6; 16384 bf16 1: 13.7 / 6.5, 512: 28 / 18, 2048: 62 / 74.  (The launch costs the host another 4 to 5.)  Eight lanes a
+// row of columns where rows have sixteen waves: 512 tokens of width 16384 26 -> 18; four elsewhere: 1021 of 2048 12.1 -> 10.5.
+constexpr int64_t FEW_ROWS = 512;
 template <typename T, int W, int NC>
 hipError_t norm_bwd(const NormBwdArgs& a, hipStream_t s) {
+  const dim3 block(W == 1 ? 256 : W * 64);
+  if (a.T <= FEW_ROWS) {
+    const int rows = (int)(W == 1 ? (a.T + 3) / 4 : a.T), of_block = column_lanes(W) * Vec<T>::N, columns = (a.d + of_block - 1) / of_block;
+    const size_t bytes = (size_t)a.T * a.d * sizeof(T);
+    auto over = [&](const void* p) {
+      const uintptr_t x = (uintptr_t)p, y = (uintptr_t)a.dX;
+      return x < y + bytes && y < x + bytes;
+    };
+    if (!over(a.h) && !over(a.dY)) {
+      hipLaunchKernelGGL((norm_bwd_kernel<T, W, NC, false, true>), dim3(columns + rows), block, 0, s, a, columns);
+      return hipGetLastError();
+    }
+    // dX takes the place of what dgamma is made of: one behind the other
+    hipLaunchKernelGGL((norm_bwd_kernel<T, W, NC, false, true>), dim3(columns), block, 0, s, a, columns);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((norm_bwd_kernel<T, W, NC, false, true>), dim3(rows), block, 0, s, a, 0);
+    return hipGetLastError();
+  }
   const int blocks = norm_bwd_blocks(a.T, a.d);
-  const dim3 grid(blocks), block(W == 1 ? 256 : W * 64);
-  if (a.T * a.d * (int64_t)sizeof(T) >= STREAM_BYTES) hipLaunchKernelGGL((norm_bwd_kernel<T, W, NC, true>), grid, block, 0, s, a);
-  else hipLaunchKernelGGL((norm_bwd_kernel<T, W, NC, false>), grid, block, 0, s, a);
+  if (a.T * a.d * (int64_t)sizeof(T) >= STREAM_BYTES) hipLaunchKernelGGL((norm_bwd_kernel<T, W, NC, true, false>), dim3(blocks), block, 0, s, a, 0);
+  else hipLaunchKernelGGL((norm_bwd_kernel<T, W, NC, false, false>), dim3(blocks), block, 0, s, a, 0);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL(norm_dgamma_kernel, dim3((a.d + 15) / 16), dim3(1024), 0, s, a.part, blocks, a.d, a.accumulate, a.dgamma);

@@ -74,6 +74,27 @@ def test_norm_forward_and_backward(d, dtype):
             check_backward(tag, dtype, stored, gamma, rstd, dY, dH, dX, dgamma, 2.0)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [40, 513, 1535, 2056, 4104, 8200, 16384])
+def test_backward_around_512_tokens(d, dtype):
+    for T in (257, 511, 512, 513, 1200):
+        pad = T % 2
+        h, gamma = made((T, d), dtype, d, pad=pad), made((d,), dtype, d + 1, 1.0, 0.1)
+        dY, dH, rstd = made((T, d), dtype, d + 2), made((T, d), dtype, d + 3, pad=pad), blank((T,))
+        m.modse_norm_fwd(T, d, dtype, h, None, gamma, EPS, blank((T, d), TYPE[dtype]), None, rstd)
+        ws = torch.empty(m.modse_norm_bwd_workspace_size(T, d, dtype), dtype=torch.uint8, device="cuda").fill_(255)
+        tag = (T, d, dtype)
+        dX, dgamma = blank((T, d), TYPE[dtype], pad=pad), blank((d,))
+        m.modse_norm_bwd(T, d, dtype, h, gamma, rstd, dY, dH, dX, dgamma, False, ws)
+        check_backward(tag, dtype, h, gamma, rstd, dY, dH, dX, dgamma, 0.0)
+        # in the buffers of the inputs: the same bits, added to what is there
+        for place in range(3):
+            a = [h.clone(), dY.clone(), dH.clone()]
+            more = torch.full((d,), 2.0, device="cuda")
+            m.modse_norm_bwd(T, d, dtype, a[0], gamma, rstd, a[1], a[2], a[place], more, True, ws)
+            assert torch.equal(a[place], dX) and torch.equal(more, dgamma + 2.0), tag
+
+
 def check_backward(tag, dtype, h, gamma, rstd, dY, dH, dX, dgamma, before):
     h64, g64, r64, dy64 = host(h), host(gamma), host(rstd)[:, None], host(dY)
     want, dg = orc.norm_bwd(h64, g64, host(rstd), dy64, None if dH is None else host(dH))

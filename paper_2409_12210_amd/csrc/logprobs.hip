@@ -454,10 +454,11 @@ hipError_t bwd_any(const LogprobsBwdArgs& a, hipStream_t s) {
 // together, and no more entries being left to join than a wave holds.  us a call, one block a row / one for every 8192 entries
 // (bf16): 1 x 131072, top 5 28.6 / 7.9, without top 14.7 / 4.7; 64 x 32000, top 5 11.8 / 8.3; 256 x 32000 12.8 / 11.2, without top
 // 5.7 / 6.9; 256 x 131072 34.9 / 24.9; 512 x 32000 15.5 / 16.2; 512 x 131072, without top 24.3 / 23.7; 700 x 131072 31.8 / 30.5, top 5
-// 50.0 / 52.3.  Finer cuts than a group: 64 x 32000 in 16 11.4, 1 x 131072 in 64 8.6.
+// 50.0 / 52.3.  Few groups are not worth the second launch (from the host / of the GPU alone): two with top 5, 1 x 16384 6.6 / 6.4 and 8.9 / 6.8,
+// 256 x 16384 8.8 / 8.7 and 9.7 / 9.3; four without, 1 x 32000 5.6 / 5.1 and 9.0 / 4.5, 64 x 32000 5.8 / 5.6 and 8.3 / 5.1.  Finer cuts than a group: 64 x 32000 in 16 11.4, 1 x 131072 in 64 8.6.
 LogprobsSplit logprobs_split(int64_t T, int32_t vocab, int32_t top) {
   const int groups = (vocab + GROUP - 1) / GROUP, most = top > 8 ? JOIN_KEYS * 64 / top : 64;
-  if (T > 512 || (T > 256 && groups < 8)) return {1, vocab};
+  if (T > 512 || (T > 256 && groups < 8) || groups <= (top ? 2 : 4)) return {1, vocab};
   const int each = (groups + most - 1) / most;
   return {(groups + each - 1) / each, each * GROUP};
 }

@@ -309,7 +309,10 @@ __global__ __launch_bounds__(256) void ortho_start_kernel(const Mat* __restrict_
 // round trips to memory.
 enum Out { OUT_PAIRS, OUT_F32, OUT_BF16 };
 constexpr int BK = 32;
-constexpr int JOIN = 16;  // steps that are summed in one register
+// Steps that are summed in one register.  A matrix instruction loses what lies 2^-26 below the sum that it adds to, so that shorter sums
+// are nearer.  Errors of five steps in units of 2^-24, 512 x 1024, and us of 64 narrow experts / a full layer, 16 steps: 23, 7920 / 17000; 8: 16,
+// 8040 / 17290; 4: 13, 8090 / 17670; 2: 12, 8230 / 18230.  (Float32 products: 17.)
+constexpr int JOIN = 8;
 // Neighbouring tiles that an XCD gets, of every 8 times as many: they share panels in its L2.  us, runs of 4 / 16 / 32 / 64: a full layer
 // 17510 / 17080 / 16710 / 16920, 64 narrow experts 8550 / 7920 / 7800 / 7805; tiles of 64, runs of 4 / 8 / 16 / 32: 24 matrices of 512 x
 // 300..1200 483 / 499 / 498 / 629, 12 of 512 x 500..1200 364 / 336 / 322 / 318, 6 of 768 x 700..1500 434 / 432 / 389 / 381.
@@ -493,8 +496,7 @@ __global__ __launch_bounds__(256, 2) void ortho_product_kernel(ProductArgs a) {
   };
   const int kq = lane >> 4, l16 = lane & 15;
   f32x4 total[NB][NB], acc[NB][NB];
-  // acc joins total and starts again.  (A sum of K terms of one sign in one register is off by up to K / 16 * 3 roundings, the
-  // diagonal of X X^T at K = 3000 by 1e-6; in parts of 512 it is as good as one of 512.)
+  // acc joins total and starts again
   auto join = [&](bool first) {
 #pragma unroll
     for (int i = 0; i < NB; ++i)

@@ -69,6 +69,7 @@ struct OrthoLayout {
   int32_t tile;
   int32_t group[modse_ortho::MAX_STEPS];  // steps of every group of them
   int32_t n_groups;
+  double most[modse_ortho::MAX_STEPS + 1];  // what the first steps make of singular values up to 1, at most
 };
 // coeffs == null: a layout that serves any steps
 modse_status ortho_layout(const modse_matrix_set* set, const float* coeffs, int steps, OrthoLayout& w);

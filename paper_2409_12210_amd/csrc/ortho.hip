@@ -117,10 +117,15 @@ struct Bound {
 
 // Behind every A: the largest singular value of X is at most the root of A's Frobenius norm, which is what the factors of the step's
 // other products and of the next A go by.  (Bounds that come from the polynomials alone lag behind values that shrink, and what is
-// stored loses bits.)
+// stored loses bits.)  It is also at most what the polynomials so far make of singular values up to 1, with 1 % for rounding, once: a
+// polynomial that is steep beyond the last one's range would make much of the 1 % of every step, and of a Frobenius norm, which is up
+// to m^(1/4) too large.  (Eight steps of minimax polynomials whose bound stays below 2.1 ran up to 3352 without it, and 512 x 1024 was off
+// by 2e-5 in single steps, 2e-4 in groups and 0.1 in the groups of a bf16 set, of the result's norm; with it 8e-7, 9e-6 and 5e-5.
+// Float32 products: 9e-7.)
 struct StepArgs {
   float a, b, c;
   float q;  // a's of the group's earlier steps, multiplied
+  double before_most, after_most;  // what the steps before it, and it as well, make of singular values up to 1, at most
   int32_t first, last;
   // of R = b A + c A A; of Q = a Q + q R + R Q; of S = a A + R A; of the next A = a S + R S; of X = q a X + Q X; of A = X X^T
   Factors *square, *join, *half, *next, *update, *gram;
@@ -134,8 +139,8 @@ __device__ __forceinline__ Factors step_factors(const StepArgs& f, int w, const 
   for (int i = threadIdx.x & 63; i < tiles; i += 64) v += squares[i];
   for (int k = 32; k; k >>= 1) v += __shfl_xor(v, k, 64);
   const double a = f.a, b = f.b, c = f.c, qa = f.first ? a : f.q * a;
-  t.x = fmin(t.x, sqrt(sqrt(v) / t.in_a) * 1.01);
-  const double x2 = t.x * t.x, r = fabs(b) * x2 + fabs(c) * x2 * x2, x = quintic_bound(a, b, c, t.x) * 1.01;
+  t.x = fmin(fmin(t.x, sqrt(sqrt(v) / t.in_a) * 1.01), f.before_most * 1.01);
+  const double x2 = t.x * t.x, r = fabs(b) * x2 + fabs(c) * x2 * x2, x = fmin(quintic_bound(a, b, c, t.x), f.after_most) * 1.01;
   t.in_r = store_scale(r);
   const Factors square = {(float)(c * t.in_r / (t.in_a * t.in_a)), (float)(b * t.in_r / t.in_a), 0.f};
   if (!store) return square;
@@ -777,6 +782,7 @@ modse_status ortho_layout(const modse_matrix_set* set, const float* coeffs, int 
   const bool grouped = coeffs && m2n >= 6e8 && m2n >= 1.4 * m3;
   const double most = set->dtype == MODSE_F32 ? F32_GROWTH : BF16_GROWTH;
   double top = 1;
+  w.most[0] = top;
   for (int i = 0; coeffs && i < steps;) {
     double growth = 1;
     int g = 0;
@@ -786,6 +792,7 @@ modse_status ortho_layout(const modse_matrix_set* set, const float* coeffs, int 
       growth *= slope > 1 ? slope * slope : 1;
       top = quintic_bound(c[0], c[1], c[2], top);
       ++g;
+      w.most[i + g] = top;
     } while (grouped && i + g < steps && growth <= most);
     w.group[w.n_groups++] = g;
     i += g;
@@ -872,7 +879,7 @@ hipError_t launch_orthogonalize(const modse_matrix_set* set, const OrthoLayout& 
     auto factors_of = [&](int i) {
       const float* const c = coeffs + 3 * (step + i);
       Bound* const after = bounds + n - (a.bounds - bounds);  // (the two take turns)
-      a.step = {c[0], c[1], c[2], qa, i == 0, i + 1 == w.group[k], f_square, f_join, f_half, f_next, f_update, f_gram, a.bounds, after};
+      a.step = {c[0], c[1], c[2], qa, w.most[step + i], w.most[step + i + 1], i == 0, i + 1 == w.group[k], f_square, f_join, f_half, f_next, f_update, f_gram, a.bounds, after};
       a.bounds = after;
       if (in_products) return hipSuccess;
       hipLaunchKernelGGL(ortho_factors_kernel, dim3(n), dim3(64), 0, s, table, squares, tile, a.step);

@@ -108,3 +108,21 @@ def test_bf16_results_of_large_sets_are_near_the_nearest(kind):
     for steps in (2, 5):
         holds_in_bf16(mats, run(mats, [QUINTIC] * steps, "bf16"), [QUINTIC] * steps,
                       (0, 1, 2, 3, 4, 6, len(mats) - 3, len(mats) - 2, len(mats) - 1))
+
+
+def spectrum(kind, m=512, n=1024):
+    rng = np.random.default_rng(8)
+    if kind == "noise":
+        return rng.normal(size=(m, n)).astype(np.float32)
+    values = {"a hundredth": np.logspace(0, -2, m), "1e-4": np.logspace(0, -4, m), "one and many": np.r_[1.0, np.full(m - 1, 0.01)]}[kind]
+    u, v = np.linalg.qr(rng.normal(size=(m, m)))[0], np.linalg.qr(rng.normal(size=(n, m)))[0]
+    return ((u * values) @ v.T).astype(np.float32)
+
+
+@pytest.mark.parametrize("name", ["minimax", "steep", "usual"])
+def test_groups_are_near_float32_products_whatever_the_singular_values(name):
+    """Four times the error of float32 products, as test_gpu_ortho.py allows groups."""
+    coeffs = [QUINTIC] * 5 if name == "usual" else SCHEDULES[name]
+    mats = [spectrum(k) for k in ("noise", "a hundredth", "1e-4", "one and many")] * 2
+    holds(mats, run(mats, coeffs), coeffs, 4, range(4))
+    holds_in_bf16(mats, run(mats, coeffs, "bf16"), coeffs, range(4))

@@ -337,16 +337,30 @@ def modse_norm_bwd(T, d_model, dtype, h, gamma, rstd, dY, dH, dX, dgamma, accumu
 
 
 def _row_distance(t, ld, vocab: int) -> int:
-    """Elements from one row to the next: as told, else the tensor's own stride (vocab for a raw pointer).  -1, which
-    the library refuses, for a tensor whose rows are not contiguous."""
+    """Elements from one row to the next: as told, else the tensor's own (vocab for a raw pointer or a tensor of one
+    dimension).  -1, which the library refuses, for a tensor whose entries do not lie side by side, or whose rows do not
+    follow each other at one distance: of more than two dimensions only those that could be flattened in front of the
+    last are rows of a matrix."""
     if ld is not None:
         return ld
-    if t is None or isinstance(t, int) or t.dim() < 2:
+    if t is None or isinstance(t, int):
         return vocab
-    rows, step = t.stride()[-2:]
-    if step != 1 and vocab > 1:
+    shape, stride = t.shape, t.stride()
+    if not shape or (stride[-1] != 1 and vocab > 1):
         return -1
-    return max(rows, vocab) if t.shape[-2] <= 1 else rows
+    distance = rows = None
+    for n, step in zip(shape[-2::-1], stride[-2::-1]):       # from the innermost rows outwards
+        if n == 1:
+            continue
+        if distance is None:
+            distance, rows = step, n
+        elif step != distance * rows:
+            return -1
+        else:
+            rows *= n
+    if distance is None:                                      # one row
+        return vocab if len(shape) == 1 else max(stride[-2], vocab)
+    return distance
 
 
 def modse_logprobs_workspace_size(T, vocab, dtype, top=0, raise_on_error=True):

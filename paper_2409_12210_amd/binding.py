@@ -13,6 +13,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB = None
 
 MODSE_F32, MODSE_BF16 = 0, 1
+MODSE_ERR_INVALID_ARG = 1
 STAGES = ("route", "permute", "up", "down", "combine", "bwd_prep", "bwd_dgrad", "bwd_wgrad", "bwd_router")
 
 
@@ -313,11 +314,65 @@ def modse_stage_times() -> dict:
 
 
 # ---------------------------------------------------------------- the operators around the layer (see include/modse.h)
+# A tensor that is of another type than the library reads, or whose elements do not follow each other, is refused as an invalid
+# argument: int64 targets, a slice of columns, an expanded scalar.  (Raw pointers are taken as they are.)
+
+class _Unfit(Exception):
+    pass
+
+
+_KINDS = {}
+
+
+def _kind(dtype):
+    """The code of `dtype`, and the types of tensors: its own (None where the library refuses it), float32, int32."""
+    import torch
+    code = _dtype_code(dtype)
+    kind = code, {MODSE_F32: torch.float32, MODSE_BF16: torch.bfloat16}.get(code), torch.float32, torch.int32
+    _KINDS[dtype] = kind
+    return kind
+
+
+def _data(t, dtype) -> Optional[int]:
+    """The pointer of a tensor of `dtype` (None: of any) whose elements lie side by side."""
+    if t is None:
+        return None
+    try:      # (raw pointers have no type; to ask for them first costs a decode call another 0.5 us of 5 to 9)
+        if (t.dtype is dtype or dtype is None) and t.is_contiguous():
+            return t.data_ptr()
+    except AttributeError:
+        return t
+    raise _Unfit(f"{t.dtype} of shape {tuple(t.shape)} and strides {t.stride()}, expected contiguous {dtype or 'elements'}")
+
+
+def _bytes(t) -> Optional[int]:
+    """The pointer of a contiguous tensor of one byte an element."""
+    if t is not None and not isinstance(t, int) and t.element_size() != 1:
+        raise _Unfit(f"{t.dtype}, expected a type of one byte")
+    return _data(t, None)
+
+
+def _rows(t, dtype) -> Optional[int]:
+    """The pointer of a tensor of `dtype` whose strides are looked at elsewhere."""
+    if t is None or isinstance(t, int):
+        return t
+    if t.dtype is not dtype and dtype is not None:
+        raise _Unfit(f"{t.dtype}, expected {dtype}")
+    return t.data_ptr()
+
+
+def _unfit(e: _Unfit, what: str, raise_on_error: bool) -> int:
+    return _check(MODSE_ERR_INVALID_ARG, f"{what}: {e}", raise_on_error)
+
 
 def modse_norm_fwd(T, d_model, dtype, x, residual, gamma, eps, y, h, rstd, q=None, scale=None, group=0, stream=None,
                    raise_on_error=True) -> int:
-    code = load_library().modse_norm_fwd(T, d_model, _dtype_code(dtype), _ptr(x), _ptr(residual), _ptr(gamma), eps,
-                                         _ptr(y), _ptr(h), _ptr(rstd), _ptr(q), _ptr(scale), group, _stream(stream))
+    kind, own, f32, _ = _KINDS.get(dtype) or _kind(dtype)
+    try:
+        code = load_library().modse_norm_fwd(T, d_model, kind, _data(x, own), _data(residual, own), _data(gamma, own), eps, _data(y, own),
+                                             _data(h, own), _data(rstd, f32), _bytes(q), _data(scale, f32), group, _stream(stream))
+    except _Unfit as e:
+        return _unfit(e, "modse_norm_fwd", raise_on_error)
     return _check(code, "modse_norm_fwd", raise_on_error)
 
 
@@ -330,9 +385,13 @@ def modse_norm_bwd_workspace_size(T, d_model, dtype, raise_on_error=True):
 
 def modse_norm_bwd(T, d_model, dtype, h, gamma, rstd, dY, dH, dX, dgamma, accumulate, ws, ws_bytes=None, stream=None,
                    raise_on_error=True) -> int:
-    code = load_library().modse_norm_bwd(T, d_model, _dtype_code(dtype), _ptr(h), _ptr(gamma), _ptr(rstd), _ptr(dY),
-                                         _ptr(dH), _ptr(dX), _ptr(dgamma), int(bool(accumulate)), _ptr(ws),
-                                         _nbytes(ws, ws_bytes), _stream(stream))
+    kind, own, f32, _ = _KINDS.get(dtype) or _kind(dtype)
+    try:
+        code = load_library().modse_norm_bwd(T, d_model, kind, _data(h, own), _data(gamma, own), _data(rstd, f32), _data(dY, own),
+                                             _data(dH, own), _data(dX, own), _data(dgamma, f32), int(bool(accumulate)), _ptr(ws),
+                                             _nbytes(ws, ws_bytes), _stream(stream))
+    except _Unfit as e:
+        return _unfit(e, "modse_norm_bwd", raise_on_error)
     return _check(code, "modse_norm_bwd", raise_on_error)
 
 
@@ -345,7 +404,10 @@ def _row_distance(t, ld, vocab: int) -> int:
         return ld
     if t is None or isinstance(t, int):
         return vocab
-    shape, stride = t.shape, t.stride()
+    stride = t.stride()
+    if len(stride) == 2 and stride[1] == 1 and stride[0] >= vocab:
+        return stride[0]
+    shape = t.shape
     if not shape or (stride[-1] != 1 and vocab > 1):
         return -1
     distance = rows = None
@@ -372,20 +434,29 @@ def modse_logprobs_workspace_size(T, vocab, dtype, top=0, raise_on_error=True):
 
 def modse_logprobs_fwd(T, vocab, dtype, logits, targets, logp, stats, entropy, top, top_idx, top_logp, ws, ws_bytes=None,
                        ld_logits=None, stream=None, raise_on_error=True) -> int:
-    code = load_library().modse_logprobs_fwd(T, vocab, _dtype_code(dtype), _ptr(logits),
-                                             _row_distance(logits, ld_logits, vocab), _ptr(targets), _ptr(logp),
-                                             _ptr(stats), _ptr(entropy), top, _ptr(top_idx), _ptr(top_logp), _ptr(ws),
-                                             _nbytes(ws, ws_bytes), _stream(stream))
+    kind, own, f32, i32 = _KINDS.get(dtype) or _kind(dtype)
+    try:
+        code = load_library().modse_logprobs_fwd(T, vocab, kind, _rows(logits, own), _row_distance(logits, ld_logits, vocab),
+                                                 _data(targets, i32), _data(logp, f32), _data(stats, f32), _data(entropy, f32), top,
+                                                 _data(top_idx, i32), _data(top_logp, f32), _ptr(ws), _nbytes(ws, ws_bytes),
+                                                 _stream(stream))
+    except _Unfit as e:
+        return _unfit(e, "modse_logprobs_fwd", raise_on_error)
     return _check(code, "modse_logprobs_fwd", raise_on_error)
 
 
 def modse_logprobs_bwd(T, vocab, dtype, logits, targets, stats, entropy, d_logp, d_entropy, d_logits, ld_logits=None,
                        ld_d_logits=None, stream=None, raise_on_error=True) -> int:
-    code = load_library().modse_logprobs_bwd(T, vocab, _dtype_code(dtype), _ptr(logits),
-                                             _row_distance(logits, ld_logits, vocab), _ptr(targets), _ptr(stats),
-                                             _ptr(entropy), _ptr(d_logp), _ptr(d_entropy), _ptr(d_logits),
-                                             _row_distance(d_logits, ld_d_logits, vocab), _stream(stream))
+    kind, own, f32, i32 = _KINDS.get(dtype) or _kind(dtype)
+    try:
+        code = load_library().modse_logprobs_bwd(T, vocab, kind, _rows(logits, own), _row_distance(logits, ld_logits, vocab),
+                                                 _data(targets, i32), _data(stats, f32), _data(entropy, f32), _data(d_logp, f32),
+                                                 _data(d_entropy, f32), _rows(d_logits, own),
+                                                 _row_distance(d_logits, ld_d_logits, vocab), _stream(stream))
+    except _Unfit as e:
+        return _unfit(e, "modse_logprobs_bwd", raise_on_error)
     return _check(code, "modse_logprobs_bwd", raise_on_error)
+
 
 class MatrixSet:
     """The matrices of modse_orthogonalize (see modse_matrix_set in include/modse.h): G, contiguous float32 device

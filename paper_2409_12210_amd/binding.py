@@ -476,6 +476,8 @@ class MatrixSet:
             if _dtype_code(g.dtype) != MODSE_F32 or u.dtype != self.U[0].dtype or u.device != g.device:
                 raise ValueError(f"matrix {i}: {g.dtype} on {g.device}, its result {u.dtype} on {u.device}")
         code = _dtype_code(dtype if dtype is not None else self.U[0].dtype if n else "f32")
+        if n and code != _dtype_code(self.U[0].dtype):       # (the kernels write as wide as they are told)
+            raise ValueError(f"results are {self.U[0].dtype}, not {dtype}")
         self._arrays = ((C.c_int32 * n)(*[g.shape[0] for g in self.G]), (C.c_int32 * n)(*[g.shape[1] for g in self.G]),
                         (C.c_void_p * n)(*[g.data_ptr() for g in self.G]), (C.c_void_p * n)(*[u.data_ptr() for u in self.U]))
         self._struct = _MatrixSet(n, *self._arrays, code)
@@ -490,7 +492,7 @@ def modse_orthogonalize_workspace_size(matrices: MatrixSet, raise_on_error=True)
 
 def modse_orthogonalize(matrices: MatrixSet, coeffs, eps, ws, ws_bytes=None, stream=None, raise_on_error=True) -> int:
     flat = [float(v) for abc in coeffs for v in abc]
-    if len(flat) != 3 * len(coeffs):
+    if any(len(abc) != 3 for abc in coeffs):
         raise ValueError("coeffs: (a, b, c) for every step")
     code = load_library().modse_orthogonalize(C.byref(matrices._struct), (C.c_float * len(flat))(*flat), len(coeffs), eps,
                                               _ptr(ws), _nbytes(ws, ws_bytes), _stream(stream))

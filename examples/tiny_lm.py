@@ -60,8 +60,10 @@ class TinyLM:
         return flat + [w.view(self.d, f) for w, f in zip(W2.split([f * self.d for f in self.d_ff]), self.d_ff)]
 
     def forward(self, tokens, train=False):
-        """Logits of the token after each of `tokens`."""
+        """Logits of the token after each of `tokens`, a batch of them at the most."""
         T, d, dt = len(tokens), self.d, self.dtype
+        if T > self.T or (train and T != self.T):
+            raise ValueError(f"{T} tokens where the buffers hold {self.T}")
         h1 = self.E[tokens]
         modse.modse_norm_fwd(T, d, dt, h1, None, self.gamma1, EPS, self.y1, None, self.rstd1 if train else None)
         modse.modse_layer_fwd(d, self.d_ff, self.k, dt, T, self.y1, self.W_gate, None, self.W1, self.W3, self.W2, self.moe,
@@ -73,6 +75,8 @@ class TinyLM:
     def loss_and_gradients(self, tokens, targets):
         """Mean negative log probability of `targets` (int32; negative: none), and the gradients of all weights."""
         T, d, dt = self.T, self.d, self.dtype
+        if len(targets) != T:
+            raise ValueError(f"{len(targets)} targets of {T} tokens")
         logits = self.forward(tokens, train=True)
         modse.modse_logprobs_fwd(T, self.V, dt, logits, targets, self.logp, self.stats, None, 0, None, None, self.ws)
         count = (targets >= 0).sum().clamp_min(1)

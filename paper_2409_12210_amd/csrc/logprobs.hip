@@ -27,6 +27,7 @@ constexpr int GROUP = LOOK * 256;  // entries that a block takes at a time
 constexpr float LOG2E = 1.44269504088896340736f;
 constexpr float LOWEST = -3.402823466e38f;
 constexpr float FAR = -1e30f;   // differences of logits below it are held at it: e^FAR is 0, and 0 * FAR is no NaN
+constexpr float NIL = -200.f;   // where they are multiplied by a gradient first: e^NIL is 0, and NIL times any loss scale is finite
 
 // keys of the order above; none is 0
 __device__ __forceinline__ uint32_t ordered(float v) {
@@ -398,7 +399,7 @@ __global__ __launch_bounds__(256) void logprobs_bwd_kernel(LogprobsBwdArgs a, in
         const float z = (raw[u][j] - m) - log_z;
         const float p = __builtin_amdgcn_exp2f(z * LOG2E);
         g = -w;
-        if constexpr (ENTROPY) g -= dE * (fmaxf(z, FAR) + H);
+        if constexpr (ENTROPY) g -= dE * (fmaxf(z, NIL) + H);
         g *= p;
         if (col + j == target) g += w;
       }

@@ -257,7 +257,10 @@ modse_status modse_norm_bwd(int64_t T, int32_t d_model, modse_dtype dtype, const
  * A logit of -inf is a masked entry: probability 0, never among the top (-1 and
  * -inf stand in the place of an entry that there is not), logp -inf where it is the
  * target.  A row of nothing else has no distribution: logp -inf, entropy 0 and no
- * gradient.  NaN or +inf in a row makes its logp and entropy NaN. */
+ * gradient.  NaN or +inf in a row makes its logp and entropy NaN.  Which outputs
+ * are asked for does not change the others, but few long rows are cut into
+ * segments by T and by top (as one for top up to 8), and other cuts are other
+ * roundings. */
 #define MODSE_LOGPROBS_MAX_TOP 64
 modse_status modse_logprobs_workspace_size(int64_t T, int32_t vocab, modse_dtype dtype, int32_t top, size_t* bytes);
 modse_status modse_logprobs_fwd(int64_t T, int32_t vocab, modse_dtype dtype, const void* logits, int64_t ld_logits,

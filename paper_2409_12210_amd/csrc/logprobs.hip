@@ -191,6 +191,28 @@ __device__ __forceinline__ Sums rescaled(Sums a, float m) {
   return {m, a.S * f, f * (a.W + a.S * z)};
 }
 
+// the sums of a wave, in all of its lanes
+__device__ __forceinline__ Sums wave_joined(Sums t) {
+  t = rescaled(t, wave_max(t.m));
+  t.S = wave_sum(t.S);
+  t.W = wave_sum(t.W);
+  return t;
+}
+// those of a block's four waves
+__device__ __forceinline__ Sums waves_joined(const float (&s)[4][3]) {
+  float m = LOWEST;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) m = fmaxf(m, s[w][0]);
+  Sums all = {m, 0.f, 0.f};
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const Sums o = rescaled({s[w][0], s[w][1], s[w][2]}, m);
+    all.S += o.S;
+    all.W += o.W;
+  }
+  return all;
+}
+
 // what a row's sums say of it; returns log Z (an entry's log probability is x - m - log Z)
 __device__ __forceinline__ float row_outputs(const LogprobsFwdArgs& a, int64_t row, Sums t, float target_logit, int target, bool write) {
   const float none = -__builtin_inff();
@@ -212,27 +234,34 @@ __device__ __forceinline__ float row_outputs(const LogprobsFwdArgs& a, int64_t r
 
 // 16384 rows of 32000 in bf16 take 157 us, 6.7 TB/s of reads; 2047 of 50257 in float32 with the 5 most probable 73, 5.6 TB/s; one row
 // of 131072 with them 5.5, and 64 of 32000 with the 20 most probable 8.8.
-template <typename T, bool TOP, bool ENTROPY, bool SPLIT, bool STREAM>
-__global__ __launch_bounds__(256) void logprobs_fwd_kernel(LogprobsFwdArgs a, int splits, int segment) {
+//
+// APART: a row of at most FEW_GROUPS groups in one block, four waves a group, that joins their sums as logprobs_join_kernel does: the same
+// bits as with the top entries, for which such a row is shared.  us from the host / of the GPU alone, one row of 32000 and 256: 5.5 / 4.0 and 5.4 / 4.7;
+// four waves that take one group after the other 5.7 / 5.6 and 6.1 / 6.1, and in one sum, with other bits, 5.4 / 4.7 and 5.4 / 5.3; two
+// launches 7.5 / 4.3 and 7.3 / 6.2.
+constexpr int FEW_GROUPS = 4;
+template <typename T, bool TOP, bool ENTROPY, bool SPLIT, bool STREAM, bool APART = false>
+__global__ __launch_bounds__(APART ? 256 * FEW_GROUPS : 256) void logprobs_fwd_kernel(LogprobsFwdArgs a, int splits, int segment) {
+  static_assert(!APART || (!TOP && !SPLIT));
   __shared__ uint64_t s_list[TOP ? 4 * LIST : 1];
-  __shared__ float s_sums[4][3];
+  __shared__ float s_sums[APART ? FEW_GROUPS : 1][4][3];
   __shared__ int s_count[4];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int thread = APART ? threadIdx.x & 255 : threadIdx.x, lane = thread & 63, wave = thread >> 6;
   const int64_t row = SPLIT ? blockIdx.x / splits : blockIdx.x;
-  const int split = SPLIT ? blockIdx.x % splits : 0;
-  const int begin = split * segment, end = SPLIT ? min(a.vocab, begin + segment) : a.vocab;
+  const int split = SPLIT ? blockIdx.x % splits : APART ? threadIdx.x >> 8 : 0;
+  const int begin = split * segment, end = SPLIT || APART ? min(a.vocab, begin + segment) : a.vocab;
   const T* const x = static_cast<const T*>(a.logits) + row * a.ld;
   int target = -1;
   float target_logit = 0.f;
   if (a.targets) {
     target = a.targets[row];
-    if (target >= begin && target < end) target_logit = (float)x[target];
+    if (target >= (APART ? 0 : begin) && target < (APART ? a.vocab : end)) target_logit = (float)x[target];
   }
   Candidates top;
   if constexpr (TOP) top.start(s_list + wave * LIST, a.top);
   Sums t = {LOWEST, 0.f, 0.f};
   constexpr int N = Vec<T>::N;
-  const int mine = threadIdx.x * N;
+  const int mine = thread * N;
 #pragma unroll 1
   for (int base = begin; base < end; base += GROUP) {
     Vec<T> raw[LOOK / N];
@@ -262,28 +291,25 @@ __global__ __launch_bounds__(256) void logprobs_fwd_kernel(LogprobsFwdArgs a, in
     }
     if constexpr (TOP) top.template take<N>(v, most, base + mine);
   }
-  t = rescaled(t, wave_max(t.m));
-  t.S = wave_sum(t.S);
-  t.W = wave_sum(t.W);
+  t = wave_joined(t);
   if (lane == 0) {
-    s_sums[wave][0] = t.m;
-    s_sums[wave][1] = t.S;
-    s_sums[wave][2] = t.W;
+    float* const to = s_sums[APART ? split : 0][wave];
+    to[0] = t.m;
+    to[1] = t.S;
+    to[2] = t.W;
   }
   if constexpr (TOP) {
     top.finish();
     if (lane == 0) s_count[wave] = top.count;
   }
   __syncthreads();
-  float m = LOWEST;
-#pragma unroll
-  for (int w = 0; w < 4; ++w) m = fmaxf(m, s_sums[w][0]);
-  Sums all = {m, 0.f, 0.f};
-#pragma unroll
-  for (int w = 0; w < 4; ++w) {
-    const Sums o = rescaled({s_sums[w][0], s_sums[w][1], s_sums[w][2]}, m);
-    all.S += o.S;
-    all.W += o.W;
+  Sums all;
+  if constexpr (APART) {
+    all = {LOWEST, 0.f, 0.f};
+    if (lane * segment < a.vocab) all = waves_joined(s_sums[lane]);
+    all = wave_joined(all);
+  } else {
+    all = waves_joined(s_sums[0]);
   }
   float log_z = 0.f;
   if constexpr (SPLIT) {
@@ -339,9 +365,7 @@ __global__ __launch_bounds__(64) void logprobs_join_kernel(LogprobsFwdArgs a, in
     target_logit = p[3];
   }
   target_logit = lane_f32(target_logit, target >= 0 && target < a.vocab ? target / segment : 0);
-  t = rescaled(t, wave_max(t.m));
-  t.S = wave_sum(t.S);
-  t.W = wave_sum(t.W);
+  t = wave_joined(t);
   const float log_z = row_outputs(a, row, t, target_logit, target, lane == 0);
   if (a.top == 0) return;
   int count = 0;
@@ -420,7 +444,10 @@ hipError_t fwd(const LogprobsFwdArgs& a, LogprobsSplit split, hipStream_t s) {
   const auto [splits, segment] = split;
   if (splits == 1) {
     const dim3 grid((unsigned)a.T);
-    if (a.T * a.vocab * (int64_t)sizeof(T) >= STREAM_BYTES)
+    const bool apart = !TOP && logprobs_split(a.T, a.vocab, 1).splits > 1;
+    if (apart)
+      hipLaunchKernelGGL((logprobs_fwd_kernel<T, false, ENTROPY, false, false, true>), grid, dim3((a.vocab + GROUP - 1) / GROUP * 256), 0, s, a, 1, GROUP);
+    else if (a.T * a.vocab * (int64_t)sizeof(T) >= STREAM_BYTES)
       hipLaunchKernelGGL((logprobs_fwd_kernel<T, TOP, ENTROPY, false, true>), grid, dim3(256), 0, s, a, 1, 0);
     else
       hipLaunchKernelGGL((logprobs_fwd_kernel<T, TOP, ENTROPY, false, false>), grid, dim3(256), 0, s, a, 1, 0);
@@ -456,10 +483,10 @@ hipError_t bwd_any(const LogprobsBwdArgs& a, hipStream_t s) {
 // (bf16): 1 x 131072, top 5 28.6 / 7.9, without top 14.7 / 4.7; 64 x 32000, top 5 11.8 / 8.3; 256 x 32000 12.8 / 11.2, without top
 // 5.7 / 6.9; 256 x 131072 34.9 / 24.9; 512 x 32000 15.5 / 16.2; 512 x 131072, without top 24.3 / 23.7; 700 x 131072 31.8 / 30.5, top 5
 // 50.0 / 52.3.  Few groups are not worth the second launch (from the host / of the GPU alone): two with top 5, 1 x 16384 6.6 / 6.4 and 8.9 / 6.8,
-// 256 x 16384 8.8 / 8.7 and 9.7 / 9.3; four without, 1 x 32000 5.6 / 5.1 and 9.0 / 4.5, 64 x 32000 5.8 / 5.6 and 8.3 / 5.1.  Finer cuts than a group: 64 x 32000 in 16 11.4, 1 x 131072 in 64 8.6.
+// 256 x 16384 8.8 / 8.7 and 9.7 / 9.3; four without, see APART.  Finer cuts than a group: 64 x 32000 in 16 11.4, 1 x 131072 in 64 8.6.
 LogprobsSplit logprobs_split(int64_t T, int32_t vocab, int32_t top) {
   const int groups = (vocab + GROUP - 1) / GROUP, most = top > 8 ? JOIN_KEYS * 64 / top : 64;
-  if (T > 512 || (T > 256 && groups < 8) || groups <= (top ? 2 : 4)) return {1, vocab};
+  if (T > 512 || (T > 256 && groups < 8) || groups <= (top ? 2 : FEW_GROUPS)) return {1, vocab};
   const int each = (groups + most - 1) / most;
   return {(groups + each - 1) / each, each * GROUP};
 }

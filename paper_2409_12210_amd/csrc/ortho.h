@@ -67,6 +67,7 @@ struct OrthoLayout {
   size_t mats, bounds, factors, squares, sums, square_list, update_list, data, total;
   int32_t square_tiles, update_tiles, parts;
   int32_t tile;
+  int32_t slots;  // squares of a matrix, from SLOT_A on
   int32_t group[modse_ortho::MAX_STEPS];  // steps of every group of them
   int32_t n_groups;
   double most[modse_ortho::MAX_STEPS + 1];  // what the first steps make of singular values up to 1, at most

@@ -719,7 +719,7 @@ __global__ __launch_bounds__(256, 2) void ortho_product_kernel(ProductArgs a) {
 }
 
 size_t align256(size_t v) { return (v + 255) / 256 * 256; }
-size_t mat_bytes(int64_t mp, int64_t np) { return (size_t)(2 * mp * np + N_SLOTS * mp * mp) * 4; }
+size_t mat_bytes(int64_t mp, int64_t np, int slots) { return (size_t)(2 * mp * np + slots * mp * mp) * 4; }
 int64_t tiles_of(int64_t v, int tile) { return (v + tile - 1) / tile; }
 }  // namespace
 
@@ -762,10 +762,15 @@ modse_status ortho_layout(const modse_matrix_set* set, const float* coeffs, int 
   w.square_tiles = (int32_t)square[side];
   w.update_tiles = (int32_t)update[side];
   w.parts = (int32_t)parts;
+  // Groups of steps where the products are what counts, and X is longer than it is wide.  us, single steps / groups: 24 matrices of
+  // 256 x 128..384 146 / 150, 3 of 256 x 256 110 / 128, 6 of 512 x 700..1200 249 / 222, 24 of 512 x 300..1200 491 / 468, 12 of 1000 x
+  // 333..1999 into bf16 926 / 787, 12 of 1024 x 1408..4224 2061 / 1492; squares, 3 of 2048 x 2048 1630 / 1738, 3 of 1111 x 1500 636 / 650.
+  const bool grouped = m2n >= 6e8 && m2n >= 1.4 * m3;
+  w.slots = grouped ? N_SLOTS : SLOT_R + 1;  // (a step alone has A and R)
   size_t data = 0;
   for (int i = 0; i < n; ++i) {
     const int r = set->rows[i], c = set->cols[i];
-    data += mat_bytes(padded(r < c ? r : c), padded(r < c ? c : r));
+    data += mat_bytes(padded(r < c ? r : c), padded(r < c ? c : r), w.slots);
   }
   size_t off = 0;
   auto take = [&](size_t bytes) {
@@ -783,10 +788,6 @@ modse_status ortho_layout(const modse_matrix_set* set, const float* coeffs, int 
   w.data = take(data);
   w.total = n ? off : 0;
   w.n_groups = 0;
-  // Groups of steps where the products are what counts, and X is longer than it is wide.  us, single steps / groups: 24 matrices of
-  // 256 x 128..384 146 / 150, 3 of 256 x 256 110 / 128, 6 of 512 x 700..1200 249 / 222, 24 of 512 x 300..1200 491 / 468, 12 of 1000 x
-  // 333..1999 into bf16 926 / 787, 12 of 1024 x 1408..4224 2061 / 1492; squares, 3 of 2048 x 2048 1630 / 1738, 3 of 1111 x 1500 636 / 650.
-  const bool grouped = coeffs && m2n >= 6e8 && m2n >= 1.4 * m3;
   const double most = set->dtype == MODSE_F32 ? F32_ROUNDINGS : BF16_ROUNDINGS;
   double top = 1;
   w.most[0] = top;
@@ -843,7 +844,7 @@ hipError_t launch_orthogonalize(const modse_matrix_set* set, const OrthoLayout& 
       square += (int32_t)(mt * (mt + 1) / 2);
       update += (int32_t)(mt * tiles_of(sn, tile));
       part += parts;
-      data += (int64_t)mat_bytes(mp, np);
+      data += (int64_t)mat_bytes(mp, np, w.slots);
       if (parts > most_parts) most_parts = parts;
       if (blocks > most_tiles) most_tiles = blocks;
     }

@@ -22,7 +22,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libmodse.so")
 RESOURCES = os.path.join(HERE, "kernel_resources.txt")
 SOURCES = ["api.hip", "route.hip", "gemm.hip", "ops_api.hip", "norm.hip", "logprobs.hip", "ortho.hip"]
-HOST_SOURCES = ("api.hip", "ops_api.hip")  # the C entry points
+# the C entry points, and what they call on the host: layouts, splits, launches
+HOST_SOURCES = ("api.hip", "ops_api.hip", "norm.hip", "logprobs.hip", "ortho.hip")
 # packed fp32 VALU ops are switched off for all device code (known to misbehave on the test machines)
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Xclang", "-target-feature", "-Xclang",
          "-packed-fp32-ops", "-I" + os.path.join(ROOT, "include"), "-I" + CSRC, "-Wno-unused-command-line-argument",
@@ -114,8 +115,9 @@ def build(extra_flags=(), verbose: bool = True) -> str:
 
 
 def build_host_sanitized(out_dir: str, driver_c: str) -> str:
-    """Builds, into out_dir, a copy of the library whose entry points' HOST code is instrumented with AddressSanitizer
-    and UndefinedBehaviorSanitizer (the device code and the other objects are the ordinary ones: build() first), and the C program driver_c against it with the same sanitizers.  Returns the path of the program."""
+    """Builds, into out_dir, a copy of the library with the HOST code of HOST_SOURCES instrumented with AddressSanitizer
+    and UndefinedBehaviorSanitizer (the device code and the other objects are the ordinary ones: build() first), and the
+    C program driver_c against it with the same sanitizers.  Returns the path of the program."""
     os.makedirs(out_dir, exist_ok=True)
     san = []
     for f in ("-fsanitize=address", "-fsanitize=undefined", "-fno-sanitize-recover=undefined", "-fno-omit-frame-pointer"):
@@ -128,18 +130,26 @@ def build_host_sanitized(out_dir: str, driver_c: str) -> str:
     for o in others:
         if not os.path.exists(o):
             raise FileNotFoundError(f"{o} not found: run build() first")
-    steps = [
-        *[[_hipcc(), *flags, *san, "-g", "-c", os.path.join(CSRC, s), "-o", o] for s, o in zip(HOST_SOURCES, objs)],
+    compiles = [[_hipcc(), *flags, *san, "-g", "-c", os.path.join(CSRC, s), "-o", o] for s, o in zip(HOST_SOURCES, objs)]
+    links = [
         [_hipcc(), "--offload-arch=gfx950", "-shared", "-fPIC", *san, *objs, *others, "-o", lib],
         [_hipcc(), "-x", "c", "-std=c99", "-g", "-fsanitize=address", "-fsanitize=undefined",
          "-fno-sanitize-recover=undefined", "-I" + os.path.join(ROOT, "include"), driver_c, "-x", "none", lib,
          "-Wl,-rpath," + out_dir, "-o", exe],
     ]
-    for cmd in steps:
-        r = subprocess.run(cmd, capture_output=True, text=True)
-        if r.returncode != 0:
-            err = "\n".join(l for l in r.stderr.splitlines() if "packed-fp32-ops" not in l)
-            raise RuntimeError("sanitized host build failed: " + " ".join(cmd) + "\n" + err)
+
+    def run(cmd):
+        return cmd, subprocess.run(cmd, capture_output=True, text=True)
+
+    def failed(done):
+        for cmd, r in done:
+            if r.returncode != 0:
+                err = "\n".join(l for l in r.stderr.splitlines() if "packed-fp32-ops" not in l)
+                raise RuntimeError("sanitized host build failed: " + " ".join(cmd) + "\n" + err)
+    with ThreadPoolExecutor(len(compiles)) as pool:
+        failed(list(pool.map(run, compiles)))
+    for cmd in links:
+        failed([run(cmd)])
     return exe
 
 

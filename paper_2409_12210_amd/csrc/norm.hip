@@ -344,20 +344,27 @@ __global__ __launch_bounds__(1024) void norm_dgamma_kernel(const float* __restri
 // and the router behind it 53.1 / 51.2), y without (the router reads it next: 4096 tokens, both 41.1 / 47.1).
 constexpr int64_t STREAM_BYTES = (int64_t)64 << 20;
 
+// Blocks of the forward pass, at most.  us of the GPU with 2048 / 8192 / as many as the rows are worth: bf16 32768 x 2048 80 / 79 / 79, 131072 x
+// 2048 394 / 391 / 363, 32768 x 8192 399 / 393 / 363, 16384 x 16384 410 / 387 / 390; float32 131072 x 2048 821 / 805 / 800.  (A launch has
+// fewer than 2^32 threads.)
+constexpr int64_t FWD_BLOCKS = 1 << 16;
 template <typename T, int W, int NC>
 hipError_t norm_fwd(const NormFwdArgs& a, hipStream_t s) {
   const int64_t blocks = W == 1 ? (a.T + 3) / 4 : a.T;
-  const dim3 grid((unsigned)(blocks < 8192 ? blocks : 8192)), block(W == 1 ? 256 : W * 64);
+  const dim3 grid((unsigned)(blocks < FWD_BLOCKS ? blocks : FWD_BLOCKS)), block(W == 1 ? 256 : W * 64);
   if (a.T * a.d * (int64_t)sizeof(T) >= STREAM_BYTES) hipLaunchKernelGGL((norm_fwd_kernel<T, W, NC, true>), grid, block, 0, s, a);
   else hipLaunchKernelGGL((norm_fwd_kernel<T, W, NC, false>), grid, block, 0, s, a);
   return hipGetLastError();
 }
+// Rows of 1025 to 2048 values belong to four waves where there are few of them.  us of the GPU, four waves / one, by rows: bf16, 2048 wide, 64 2.6 /
+// 3.9, 1023 4.0 / 4.8, 1536 4.8 / 5.4, 2048 5.5 / 6.1, 4096 10.9 / 10.5, 32768 80 / 79; 1100 wide, 64 3.0 / 4.9, 1536 5.3 / 6.1, 2048 6.1 / 6.3,
+// 4096 9.6 / 8.8, 32768 80 / 67; float32, 2048 wide, 64 2.8 / 4.6, 1536 6.9 / 8.4, 2048 10.9 / 10.4, 4096 20.3 / 21.4, 32768 155 / 161.
 // (vectors of a thread: float32 has twice as many of them in a row)
 template <typename T>
 hipError_t norm_fwd_any(const NormFwdArgs& a, hipStream_t s) {
   constexpr int X = 8 / Vec<T>::N;
   const int chunks = (a.d + 7) / 8;
-  const bool few = a.T < 1024;
+  const bool few = a.T < 2048;
   if (chunks <= 64) return norm_fwd<T, 1, X>(a, s);
   if (chunks <= 128) return norm_fwd<T, 1, 2 * X>(a, s);
   if (!few && chunks <= 256) return norm_fwd<T, 1, 4 * X>(a, s);

@@ -125,20 +125,25 @@ def _ptr(t) -> Optional[int]:
     return t.data_ptr()
 
 
-_TORCH = None
+_RAW_STREAM = _DEVICE = None
 
 
 def _stream(stream) -> Optional[int]:
     if stream is None:
-        global _TORCH
-        if _TORCH is None:
-            import torch as _TORCH
-            _TORCH.cuda.init()
         # (torch.cuda.current_stream() makes an object of it first: 3.0 us where this takes 0.2, of a call's 7.5)
-        return _TORCH._C._cuda_getCurrentRawStream(_TORCH._C._cuda_getDevice()) or None
+        if _RAW_STREAM is None:
+            _find_stream()
+        return _RAW_STREAM(_DEVICE()) or None
     if isinstance(stream, int):
         return stream or None
     return stream.cuda_stream or None
+
+
+def _find_stream():
+    global _RAW_STREAM, _DEVICE
+    import torch
+    torch.cuda.init()
+    _DEVICE, _RAW_STREAM = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
 
 
 def _check(code: int, what: str, raise_on_error: bool) -> int:
@@ -337,7 +342,7 @@ def _data(t, dtype) -> Optional[int]:
     """The pointer of a tensor of `dtype` (None: of any) whose elements lie side by side."""
     if t is None:
         return None
-    try:      # (raw pointers have no type; to ask for them first costs a decode call another 0.5 us of 5 to 9)
+    try:      # (raw pointers have no type; to ask for them first costs a decode call another 0.3 us of 5 to 8)
         if (t.dtype is dtype or dtype is None) and t.is_contiguous():
             return t.data_ptr()
     except AttributeError:
@@ -369,11 +374,11 @@ def modse_norm_fwd(T, d_model, dtype, x, residual, gamma, eps, y, h, rstd, q=Non
                    raise_on_error=True) -> int:
     kind, own, f32, _ = _KINDS.get(dtype) or _kind(dtype)
     try:
-        code = load_library().modse_norm_fwd(T, d_model, kind, _data(x, own), _data(residual, own), _data(gamma, own), eps, _data(y, own),
+        code = (_LIB or load_library()).modse_norm_fwd(T, d_model, kind, _data(x, own), _data(residual, own), _data(gamma, own), eps, _data(y, own),
                                              _data(h, own), _data(rstd, f32), _bytes(q), _data(scale, f32), group, _stream(stream))
     except _Unfit as e:
         return _unfit(e, "modse_norm_fwd", raise_on_error)
-    return _check(code, "modse_norm_fwd", raise_on_error)
+    return code and _check(code, "modse_norm_fwd", raise_on_error)
 
 
 def modse_norm_bwd_workspace_size(T, d_model, dtype, raise_on_error=True):
@@ -387,12 +392,12 @@ def modse_norm_bwd(T, d_model, dtype, h, gamma, rstd, dY, dH, dX, dgamma, accumu
                    raise_on_error=True) -> int:
     kind, own, f32, _ = _KINDS.get(dtype) or _kind(dtype)
     try:
-        code = load_library().modse_norm_bwd(T, d_model, kind, _data(h, own), _data(gamma, own), _data(rstd, f32), _data(dY, own),
+        code = (_LIB or load_library()).modse_norm_bwd(T, d_model, kind, _data(h, own), _data(gamma, own), _data(rstd, f32), _data(dY, own),
                                              _data(dH, own), _data(dX, own), _data(dgamma, f32), int(bool(accumulate)), _ptr(ws),
                                              _nbytes(ws, ws_bytes), _stream(stream))
     except _Unfit as e:
         return _unfit(e, "modse_norm_bwd", raise_on_error)
-    return _check(code, "modse_norm_bwd", raise_on_error)
+    return code and _check(code, "modse_norm_bwd", raise_on_error)
 
 
 def _row_distance(t, ld, vocab: int) -> int:
@@ -436,26 +441,26 @@ def modse_logprobs_fwd(T, vocab, dtype, logits, targets, logp, stats, entropy, t
                        ld_logits=None, stream=None, raise_on_error=True) -> int:
     kind, own, f32, i32 = _KINDS.get(dtype) or _kind(dtype)
     try:
-        code = load_library().modse_logprobs_fwd(T, vocab, kind, _rows(logits, own), _row_distance(logits, ld_logits, vocab),
+        code = (_LIB or load_library()).modse_logprobs_fwd(T, vocab, kind, _rows(logits, own), _row_distance(logits, ld_logits, vocab),
                                                  _data(targets, i32), _data(logp, f32), _data(stats, f32), _data(entropy, f32), top,
                                                  _data(top_idx, i32), _data(top_logp, f32), _ptr(ws), _nbytes(ws, ws_bytes),
                                                  _stream(stream))
     except _Unfit as e:
         return _unfit(e, "modse_logprobs_fwd", raise_on_error)
-    return _check(code, "modse_logprobs_fwd", raise_on_error)
+    return code and _check(code, "modse_logprobs_fwd", raise_on_error)
 
 
 def modse_logprobs_bwd(T, vocab, dtype, logits, targets, stats, entropy, d_logp, d_entropy, d_logits, ld_logits=None,
                        ld_d_logits=None, stream=None, raise_on_error=True) -> int:
     kind, own, f32, i32 = _KINDS.get(dtype) or _kind(dtype)
     try:
-        code = load_library().modse_logprobs_bwd(T, vocab, kind, _rows(logits, own), _row_distance(logits, ld_logits, vocab),
+        code = (_LIB or load_library()).modse_logprobs_bwd(T, vocab, kind, _rows(logits, own), _row_distance(logits, ld_logits, vocab),
                                                  _data(targets, i32), _data(stats, f32), _data(entropy, f32), _data(d_logp, f32),
                                                  _data(d_entropy, f32), _rows(d_logits, own),
                                                  _row_distance(d_logits, ld_d_logits, vocab), _stream(stream))
     except _Unfit as e:
         return _unfit(e, "modse_logprobs_bwd", raise_on_error)
-    return _check(code, "modse_logprobs_bwd", raise_on_error)
+    return code and _check(code, "modse_logprobs_bwd", raise_on_error)
 
 
 class MatrixSet:

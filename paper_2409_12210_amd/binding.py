@@ -339,7 +339,7 @@ def _kind(dtype):
 
 
 def _data(t, dtype) -> Optional[int]:
-    """The pointer of a tensor of `dtype` (None: of any) whose elements lie side by side."""
+    """The pointer of a tensor of `dtype` (None: the library refuses the type that the call names) whose elements lie side by side."""
     if t is None:
         return None
     try:      # (raw pointers have no type; to ask for them first costs a decode call another 0.3 us of 5 to 8)
@@ -352,9 +352,14 @@ def _data(t, dtype) -> Optional[int]:
 
 def _bytes(t) -> Optional[int]:
     """The pointer of a contiguous tensor of one byte an element."""
-    if t is not None and not isinstance(t, int) and t.element_size() != 1:
-        raise _Unfit(f"{t.dtype}, expected a type of one byte")
-    return _data(t, None)
+    if t is None:
+        return None
+    try:
+        if t.element_size() == 1 and t.is_contiguous():
+            return t.data_ptr()
+    except AttributeError:
+        return t
+    raise _Unfit(f"{t.dtype} of shape {tuple(t.shape)} and strides {t.stride()}, expected contiguous bytes")
 
 
 def _rows(t, dtype) -> Optional[int]:

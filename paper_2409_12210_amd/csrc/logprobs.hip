@@ -13,8 +13,9 @@
 // largest of 64 are n entries), and from the list whenever that fills up.
 //
 // Large calls are bound by memory: both kernels read the logits once, in vectors of sixteen bytes, 128 bytes of a thread in flight.
-// Small ones are bound by the launches: a call of the forward costs 9 us with one row or 64, two launches of it, and a third of
-// that is on the host.
+// Small ones are bound by the launches.  us of the GPU and a call: one row or 256 of 32000 without top entries, one launch, 4.0 to 4.7 and 5.5; one
+// row of 131072 with the 5 most probable, two launches, 8.6 and 9.1; 64 of 32000 with 20, two launches, 13 one by one and 12.3 where the
+// second runs into the next call's first.
 #include "ops.h"
 
 namespace {

@@ -5,8 +5,8 @@
 // products need float32 precision.  They get it from the 16-bit matrix instructions, whose rate is sixteen times that of the
 // float32 ones: a value is stored as hi + lo, two float16 numbers with 11 bits each, times a power of two that keeps the
 // largest value that the matrix can have (a bound on its singular values) below 2^15, and a product is hi hi + hi lo + lo hi,
-// summed in float32.  What is left out, lo lo, is 2^-24 of the product in the mean, as a float32 rounding is.  Simulated on the
-// CPU, and measured: errors against float64 as those of float32 products (1.3e-6 and 1.4e-6 after five steps).
+// summed in float32.  What is left out, lo lo, is 2^-24 of the product in the mean, as a float32 rounding is: errors against float64
+// as those of float32 products (1.0e-6 both after five single steps of 512 x 1024).
 //
 // Storage: rows of blocks of 32 values, 64 bytes of hi and then 64 of lo, so that a cache line feeds one step of a product.
 //
@@ -304,8 +304,8 @@ __global__ __launch_bounds__(256) void ortho_start_kernel(const Mat* __restrict_
 // as its loads unless they are under way early.
 //
 // Measured, tiles of 128: Q X of a full layer (24 matrices, 2048 x 2816..8448: 1.13e12 operations, three times as many in 16 bits) takes
-// 2.8 to 2.9 ms, 1.2e15 16-bit operations a second where plain 16-bit products of 8192 x 8192 x 8192 reach 1.1e15 to 1.5e15 by card; A A takes 0.55 to
-// 0.6 ms, 1.1e15.  The matrix pipes are busy 64 to 68 % of the time at 1.6 to 1.7 GHz, which is what the card's power leaves.  Squares of 352 to 1056
+// 2.8 to 2.9 ms, 1.2e15 16-bit operations a second where plain 16-bit products of 8192 x 8192 x 8192 reach 1.1e15 to 1.5e15 by card; A A takes 0.54 to
+// 0.6 ms, 1.1e15.  The matrix pipes are busy 62 to 66 % of the time at 1.6 GHz, which is what the card's power leaves.  Squares of 352 to 1056
 // take 0.3 ms for 192 of them, 0.75e15: 44 % at 1.9 GHz, a step of two workgroups 2600 clocks where its instructions take 1540; a quarter of
 // a tile's time is its opening and its result, which the other workgroup's steps fill (E brought into the cache during the last step: 7960 -> 8080 us).  A tile of 256 x 256
 // halves the reads of LDS and has one workgroup on a CU: all of them store at once, and narrow matrices do not fill it (before the steps

@@ -290,16 +290,16 @@ typedef struct {
 /* U = X after `steps` (1..32) steps X <- a X + (b A + c A^2) X with A = X X^T, from
  * X = G / (|G| + eps), |G| the Frobenius norm.  coeffs: HOST array [steps][3] of
  * (a, b, c).  Products are those of values of 22 bits (pairs of float16) summed in
- * float32, and as near as float32 products of values that the steps keep within a
- * few powers of two of what singular values of at most 1 can come to.  Sets of
+ * float32, and as near as float32 products where the steps keep singular values
+ * within a few powers of two of the most that values up to 1 can come to.  Sets of
  * large products (sum of m m n from 6e8 on and 1.4 times that of m^3, m the shorter
- * side) take several steps together: float32 results are then within about three
- * times the error of float32 products, and where U is bfloat16 more steps go
- * together, for up to 1e-3 of |U| (1e-5 to 2e-4 as a rule) before the results are
- * rounded, by 1.7e-3 of |U|: ask for float32 results where that counts.
+ * side) take several steps together.  Float32 results are then within about three
+ * times the error of float32 products.  Where U is bfloat16 more steps go together,
+ * and results are off by up to about 1e-3 of |U| (1e-5 to 2e-4 as a rule) before they
+ * are rounded, which is 1.7e-3 of |U|: ask for float32 results where that counts.
  * Coefficients that let a singular value of at most 1 grow beyond 2^40, or that are
- * not finite, are unsupported.  A matrix of zeros stays one; NaN or infinities in a matrix make the
- * whole of it NaN and leave the others alone. */
+ * not finite, are unsupported.  A matrix of zeros stays one; NaN or infinities in a
+ * matrix make the whole of it NaN and leave the others alone. */
 modse_status modse_orthogonalize_workspace_size(const modse_matrix_set* set, size_t* bytes);
 modse_status modse_orthogonalize(const modse_matrix_set* set, const float* coeffs, int32_t steps, float eps, void* ws,
                                  size_t ws_bytes, void* hip_stream);

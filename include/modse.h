@@ -304,6 +304,48 @@ modse_status modse_orthogonalize_workspace_size(const modse_matrix_set* set, siz
 modse_status modse_orthogonalize(const modse_matrix_set* set, const float* coeffs, int32_t steps, float eps, void* ws,
                                  size_t ws_bytes, void* hip_stream);
 
+/* ---------------------------------------------------------------- both ends of a model
+ * The embedding in front of the first layer, the dropout on the stream, and the
+ * log probabilities behind the last layer, with their gradients. */
+
+/* Lookup: x_t = scale E[token_t], rounded once.
+ *   tokens  [T] int32.  Negative: no token, a row of zeros.  One that is not below
+ *           vocab: a row of NaN
+ *   E       [vocab, d_model] of `dtype` (vocab 1..2^20, d_model 1..16384, any value)
+ *   x       [T, d_model] of `dtype` out */
+modse_status modse_embed_fwd(int64_t T, int32_t d_model, int32_t vocab, modse_dtype dtype, const int32_t* tokens, const void* E,
+                             float scale, void* x, void* hip_stream);
+
+/* Its gradient: dE_v = scale sum of dX_t over the tokens t that are v, summed in
+ * float32 in an order that the tokens alone fix.
+ *   dX  [T, d_model] of `dtype`; rows of no token, or of one beyond vocab, are not read
+ *   dE  [vocab, d_model] float32 out.  accumulate = 0: overwritten, rows that do not
+ *       occur with zeros; 1: added to, and rows that do not occur stay untouched (tied
+ *       matrices: with 1 behind modse_head_bwd, or before it with 1 there).
+ * T == 0 leaves dE as it is.  T ceil(d_model / 256) up to 2^29. */
+modse_status modse_embed_bwd_workspace_size(int64_t T, int32_t d_model, int32_t vocab, modse_dtype dtype, size_t* bytes);
+modse_status modse_embed_bwd(int64_t T, int32_t d_model, int32_t vocab, modse_dtype dtype, const int32_t* tokens, const void* dX,
+                             float scale, float* dE, int accumulate, void* ws, size_t ws_bytes, void* hip_stream);
+
+/* Dropout: y = residual + keep x / (1 - p), elementwise over [T, d_model].
+ *   residual  of `dtype` or NULL (0)
+ *   p         0..1, rounded to a multiple of 2^-16; at 1 everything is dropped
+ *   rng       [2] uint64 DEVICE: seed and offset.  Read by the kernel, so that a captured
+ *             graph makes another mask when they are changed between its replays
+ *   call      tells several calls with one seed and offset apart (one per layer)
+ *   y         of `dtype` out; may lie in the buffer of x or of residual
+ * Random bits: Philox-4x32 with seven rounds, key = seed (low word first), counter =
+ * (i / 8, call, offset low, offset high) for element i = t d_model + column; it gives 16
+ * bits to each of eight elements, the low half of word w to that of i % 8 = 2 w.  Kept
+ * where they are at least 65536 p.  What is dropped does not count, infinities and NaN
+ * included.  T d_model below 2^35.
+ * modse_dropout_bwd: dX = keep dY / (1 - p) with the same rng and call (the gradient of
+ * residual is dY); dX may lie in the buffer of dY. */
+modse_status modse_dropout_fwd(int64_t T, int32_t d_model, modse_dtype dtype, const void* x, const void* residual, double p,
+                               const uint64_t* rng, uint32_t call, void* y, void* hip_stream);
+modse_status modse_dropout_bwd(int64_t T, int32_t d_model, modse_dtype dtype, const void* dY, double p, const uint64_t* rng,
+                               uint32_t call, void* dX, void* hip_stream);
+
 /* Per-stage timing for benchmarks.  When enabled, modse_layer_fwd/bwd record
  * HIP events between their stages on the caller's stream; modse_stage_times
  * waits for the last recorded call and returns milliseconds per stage

@@ -84,7 +84,13 @@ def load_library():
     lib.modse_orthogonalize_workspace_size.argtypes = [mp, szp]
     lib.modse_orthogonalize.argtypes = [mp, C.POINTER(f32), i32, f32, vp, sz, vp]
     lib.modse_logprobs_bwd.argtypes = [i64, i32, C.c_int, vp, i64, vp, vp, vp, vp, vp, vp, i64, vp]
-    for name in ("modse_norm_fwd", "modse_norm_bwd_workspace_size", "modse_norm_bwd", "modse_logprobs_workspace_size",
+    lib.modse_embed_fwd.argtypes = [i64, i32, i32, C.c_int, vp, vp, f32, vp, vp]
+    lib.modse_embed_bwd_workspace_size.argtypes = [i64, i32, i32, C.c_int, szp]
+    lib.modse_embed_bwd.argtypes = [i64, i32, i32, C.c_int, vp, vp, f32, vp, C.c_int, vp, sz, vp]
+    lib.modse_dropout_fwd.argtypes = [i64, i32, C.c_int, vp, vp, C.c_double, vp, C.c_uint32, vp, vp]
+    lib.modse_dropout_bwd.argtypes = [i64, i32, C.c_int, vp, C.c_double, vp, C.c_uint32, vp, vp]
+    for name in ("modse_embed_fwd", "modse_embed_bwd_workspace_size", "modse_embed_bwd", "modse_dropout_fwd", "modse_dropout_bwd",
+                 "modse_norm_fwd", "modse_norm_bwd_workspace_size", "modse_norm_bwd", "modse_logprobs_workspace_size",
                  "modse_logprobs_fwd", "modse_logprobs_bwd", "modse_orthogonalize_workspace_size", "modse_orthogonalize",
                  "modse_workspace_size", "modse_saved_size", "modse_route", "modse_layer_fwd", "modse_layer_bwd",
                  "modse_route_ext", "modse_layer_fwd_ext", "modse_layer_bwd_ext", "modse_routing_stats",
@@ -507,3 +513,63 @@ def modse_orthogonalize(matrices: MatrixSet, coeffs, eps, ws, ws_bytes=None, str
     code = load_library().modse_orthogonalize(C.byref(matrices._struct), (C.c_float * len(flat))(*flat), len(coeffs), eps,
                                               _ptr(ws), _nbytes(ws, ws_bytes), _stream(stream))
     return _check(code, "modse_orthogonalize", raise_on_error)
+
+
+# ---------------------------------------------------------------- both ends of a model (see include/modse.h)
+
+def modse_embed_fwd(T, d_model, vocab, dtype, tokens, E, scale, x, stream=None, raise_on_error=True) -> int:
+    kind, own, _, i32 = _KINDS.get(dtype) or _kind(dtype)
+    try:
+        code = (_LIB or load_library()).modse_embed_fwd(T, d_model, vocab, kind, _data(tokens, i32), _data(E, own), scale, _data(x, own),
+                                                        _stream(stream))
+    except _Unfit as e:
+        return _unfit(e, "modse_embed_fwd", raise_on_error)
+    return code and _check(code, "modse_embed_fwd", raise_on_error)
+
+
+def modse_embed_bwd_workspace_size(T, d_model, vocab, dtype, raise_on_error=True):
+    out = C.c_size_t(0)
+    code = load_library().modse_embed_bwd_workspace_size(T, d_model, vocab, _dtype_code(dtype), C.byref(out))
+    _check(code, "modse_embed_bwd_workspace_size", raise_on_error)
+    return out.value if code == 0 else code
+
+
+def modse_embed_bwd(T, d_model, vocab, dtype, tokens, dX, scale, dE, accumulate, ws, ws_bytes=None, stream=None,
+                    raise_on_error=True) -> int:
+    kind, own, f32, i32 = _KINDS.get(dtype) or _kind(dtype)
+    try:
+        code = (_LIB or load_library()).modse_embed_bwd(T, d_model, vocab, kind, _data(tokens, i32), _data(dX, own), scale, _data(dE, f32),
+                                                        int(bool(accumulate)), _ptr(ws), _nbytes(ws, ws_bytes), _stream(stream))
+    except _Unfit as e:
+        return _unfit(e, "modse_embed_bwd", raise_on_error)
+    return code and _check(code, "modse_embed_bwd", raise_on_error)
+
+
+def _generator(rng) -> Optional[int]:
+    """The pointer of seed and offset: two integers of 64 bits on the device."""
+    if rng is None or isinstance(rng, int):
+        return rng
+    import torch
+    if rng.dtype not in (torch.int64, torch.uint64) or rng.numel() != 2 or not rng.is_contiguous():
+        raise _Unfit(f"{rng.dtype} of shape {tuple(rng.shape)}, expected two int64: seed and offset")
+    return rng.data_ptr()
+
+
+def modse_dropout_fwd(T, d_model, dtype, x, residual, p, rng, call, y, stream=None, raise_on_error=True) -> int:
+    kind, own, _, _ = _KINDS.get(dtype) or _kind(dtype)
+    try:
+        code = (_LIB or load_library()).modse_dropout_fwd(T, d_model, kind, _data(x, own), _data(residual, own), p, _generator(rng), call,
+                                                          _data(y, own), _stream(stream))
+    except _Unfit as e:
+        return _unfit(e, "modse_dropout_fwd", raise_on_error)
+    return code and _check(code, "modse_dropout_fwd", raise_on_error)
+
+
+def modse_dropout_bwd(T, d_model, dtype, dY, p, rng, call, dX, stream=None, raise_on_error=True) -> int:
+    kind, own, _, _ = _KINDS.get(dtype) or _kind(dtype)
+    try:
+        code = (_LIB or load_library()).modse_dropout_bwd(T, d_model, kind, _data(dY, own), p, _generator(rng), call, _data(dX, own),
+                                                          _stream(stream))
+    except _Unfit as e:
+        return _unfit(e, "modse_dropout_bwd", raise_on_error)
+    return code and _check(code, "modse_dropout_bwd", raise_on_error)

@@ -1,5 +1,7 @@
-// Internal declarations of the operators around the layer: norm and log probabilities (gfx950 only).
+// Internal declarations of the operators around the layer (gfx950 only).
 #pragma once
+#include <algorithm>
+
 #include "common.h"
 
 #define MODSE_NORM_MAX_D 16384
@@ -60,6 +62,51 @@ struct LogprobsBwdArgs {
   int32_t vocab;
 };
 hipError_t launch_logprobs_bwd(modse_dtype dt, const LogprobsBwdArgs& a, hipStream_t s);
+
+// dropout.hip
+struct DropoutArgs {
+  const void *x, *residual;
+  void* y;
+  const uint64_t* rng;  // seed, offset
+  int64_t n;            // elements
+  uint32_t call, limit; // kept: 16 random bits of at least `limit`
+  float scale;
+};
+hipError_t launch_dropout(modse_dtype dt, const DropoutArgs& a, hipStream_t s);
+
+// embed.hip
+#define MODSE_MAX_VOCAB (1 << 20)
+constexpr int EMBED_MAX_ROWS = 512;  // of the vocabulary that one block sorts
+struct EmbedFwdArgs {
+  const int32_t* tokens;
+  const void* E;
+  void* x;
+  int64_t T;
+  int32_t d, vocab;
+  float scale;
+};
+hipError_t launch_embed_fwd(modse_dtype dt, const EmbedFwdArgs& a, hipStream_t s);
+
+struct EmbedBwdArgs {
+  const int32_t* tokens;
+  const void* dX;
+  float* dE;
+  int32_t* n_sorted;  // [1] tokens of the vocabulary
+  int32_t* order;     // [T] their places in the batch, by token and then by place
+  int32_t* keys;      // [T] the tokens themselves in that order
+  float* part;        // [2 ceil(T / chunk), part_ld] partial sums of runs that cross chunks
+  int64_t T;
+  int32_t d, vocab, chunk, part_ld, accumulate;
+  float scale;
+};
+// Places of the sorted list that are summed together, 64 at the most.
+inline int embed_chunk(int64_t T) { return T <= 8192 ? 8 : T <= 32768 ? 32 : 64; }
+inline int64_t embed_chunks(int64_t T) { return (T + embed_chunk(T) - 1) / embed_chunk(T); }
+// the most chunks of all batches of at most T tokens
+inline int64_t embed_most_chunks(int64_t T) {
+  return std::max(embed_chunks(T), std::max(embed_chunks(std::min<int64_t>(T, 8192)), embed_chunks(std::min<int64_t>(T, 32768))));
+}
+hipError_t launch_embed_bwd(modse_dtype dt, const EmbedBwdArgs& a, hipStream_t s);
 
 // ---------------------------------------------------------------- rows of any alignment
 // Sixteen bytes of a row that starts anywhere: gfx950 takes such accesses at the alignment of the element, so a row of odd length

@@ -35,6 +35,42 @@ modse_status check_logprobs(int64_t T, int32_t vocab, const modse_dtype& dtype, 
   if (vocab > 1 << 30 || T >= 1 << 24 || T * ((vocab + 8191) / 8192) >= 1 << 24) return MODSE_ERR_UNSUPPORTED;
   return MODSE_OK;
 }
+modse_status check_vocab(int64_t T, int32_t d, int32_t vocab, const modse_dtype& dtype) {
+  if (vocab < 1) return MODSE_ERR_INVALID_ARG;
+  const modse_status st = check_norm(T, d, dtype);
+  if (st != MODSE_OK) return st;
+  return vocab > MODSE_MAX_VOCAB ? MODSE_ERR_UNSUPPORTED : MODSE_OK;
+}
+modse_status check_embed_bwd(int64_t T, int32_t d, int32_t vocab, const modse_dtype& dtype) {
+  const modse_status st = check_vocab(T, d, vocab, dtype);
+  if (st != MODSE_OK) return st;
+  // (a launch has fewer than 2^32 threads, 256 of them for 256 columns of a chunk)
+  return embed_chunks(T) * ((d + 255) / 256) >= 1 << 24 ? MODSE_ERR_UNSUPPORTED : MODSE_OK;
+}
+struct EmbedLayout {
+  size_t n_sorted, order, keys, part, total;
+};
+EmbedLayout embed_layout(int64_t T, int32_t d, int64_t chunks) {
+  EmbedLayout w = {};
+  w.order = 256;
+  w.keys = w.order + align_up((size_t)T * sizeof(int32_t), 256);
+  w.part = w.keys + align_up((size_t)T * sizeof(int32_t), 256);
+  w.total = w.part + 2 * (size_t)chunks * align_up(d, 4) * sizeof(float);
+  return w;
+}
+modse_status check_dropout(int64_t T, int32_t d, const modse_dtype& dtype, double p) {
+  const modse_status st = check_norm(T, d, dtype);
+  if (st != MODSE_OK) return st;
+  if (!(p >= 0 && p <= 1)) return MODSE_ERR_INVALID_ARG;
+  return T * d >= (int64_t)1 << 35 ? MODSE_ERR_UNSUPPORTED : MODSE_OK;  // (2^32 counters of eight elements)
+}
+modse_status run_dropout(int64_t T, int32_t d, modse_dtype dtype, const void* x, const void* residual, double p, const uint64_t* rng,
+                         uint32_t call, void* y, void* hip_stream) {
+  const int limit = (int)std::nearbyint(p * 65536);
+  const float scale = limit < 65536 ? (float)(65536.0 / (65536 - limit)) : 0.f;
+  const DropoutArgs a = {x, residual, y, rng, T * d, call, (uint32_t)limit, scale};
+  return hip_status(launch_dropout(dtype, a, static_cast<hipStream_t>(hip_stream)));
+}
 struct LogprobsLayout {
   size_t part, keys, total;
 };
@@ -160,6 +196,59 @@ modse_status modse_orthogonalize(const modse_matrix_set* set, const float* coeff
     if (!set->G[i] || !set->U[i]) return MODSE_ERR_INVALID_ARG;
   if (ws_bytes < w.total) return MODSE_ERR_WORKSPACE;
   return hip_status(launch_orthogonalize(set, w, coeffs, eps, static_cast<char*>(ws), static_cast<hipStream_t>(hip_stream)));
+}
+
+modse_status modse_embed_fwd(int64_t T, int32_t d_model, int32_t vocab, modse_dtype dtype, const int32_t* tokens, const void* E,
+                             float scale, void* x, void* hip_stream) {
+  const modse_status st = check_vocab(T, d_model, vocab, dtype);
+  if (st != MODSE_OK) return st;
+  if (!std::isfinite(scale)) return MODSE_ERR_INVALID_ARG;
+  if (T == 0) return MODSE_OK;
+  if (!tokens || !E || !x) return MODSE_ERR_INVALID_ARG;
+  const EmbedFwdArgs a = {tokens, E, x, T, d_model, vocab, scale};
+  return hip_status(launch_embed_fwd(dtype, a, static_cast<hipStream_t>(hip_stream)));
+}
+
+modse_status modse_embed_bwd_workspace_size(int64_t T, int32_t d_model, int32_t vocab, modse_dtype dtype, size_t* bytes) {
+  if (!bytes) return MODSE_ERR_INVALID_ARG;
+  const modse_status st = check_embed_bwd(T, d_model, vocab, dtype);
+  if (st != MODSE_OK) return st;
+  *bytes = T == 0 ? 0 : embed_layout(T, d_model, embed_most_chunks(T)).total;
+  return MODSE_OK;
+}
+
+modse_status modse_embed_bwd(int64_t T, int32_t d_model, int32_t vocab, modse_dtype dtype, const int32_t* tokens, const void* dX,
+                             float scale, float* dE, int accumulate, void* ws, size_t ws_bytes, void* hip_stream) {
+  const modse_status st = check_embed_bwd(T, d_model, vocab, dtype);
+  if (st != MODSE_OK) return st;
+  if (!std::isfinite(scale)) return MODSE_ERR_INVALID_ARG;
+  if (T == 0) return MODSE_OK;
+  if (!tokens || !dX || !dE || !ws || !aligned16(ws)) return MODSE_ERR_INVALID_ARG;
+  const EmbedLayout w = embed_layout(T, d_model, embed_chunks(T));
+  if (ws_bytes < w.total) return MODSE_ERR_WORKSPACE;
+  char* const wsb = static_cast<char*>(ws);
+  const EmbedBwdArgs a = {tokens, dX, dE, reinterpret_cast<int32_t*>(wsb + w.n_sorted), reinterpret_cast<int32_t*>(wsb + w.order),
+                          reinterpret_cast<int32_t*>(wsb + w.keys), reinterpret_cast<float*>(wsb + w.part), T, d_model, vocab,
+                          embed_chunk(T), (int32_t)align_up(d_model, 4), accumulate, scale};
+  return hip_status(launch_embed_bwd(dtype, a, static_cast<hipStream_t>(hip_stream)));
+}
+
+modse_status modse_dropout_fwd(int64_t T, int32_t d_model, modse_dtype dtype, const void* x, const void* residual, double p,
+                               const uint64_t* rng, uint32_t call, void* y, void* hip_stream) {
+  const modse_status st = check_dropout(T, d_model, dtype, p);
+  if (st != MODSE_OK) return st;
+  if (T == 0) return MODSE_OK;
+  if (!x || !rng || !y) return MODSE_ERR_INVALID_ARG;
+  return run_dropout(T, d_model, dtype, x, residual, p, rng, call, y, hip_stream);
+}
+
+modse_status modse_dropout_bwd(int64_t T, int32_t d_model, modse_dtype dtype, const void* dY, double p, const uint64_t* rng,
+                               uint32_t call, void* dX, void* hip_stream) {
+  const modse_status st = check_dropout(T, d_model, dtype, p);
+  if (st != MODSE_OK) return st;
+  if (T == 0) return MODSE_OK;
+  if (!dY || !rng || !dX) return MODSE_ERR_INVALID_ARG;
+  return run_dropout(T, d_model, dtype, dY, nullptr, p, rng, call, dX, hip_stream);
 }
 
 }  // extern "C"

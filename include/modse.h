@@ -327,6 +327,34 @@ modse_status modse_embed_bwd_workspace_size(int64_t T, int32_t d_model, int32_t 
 modse_status modse_embed_bwd(int64_t T, int32_t d_model, int32_t vocab, modse_dtype dtype, const int32_t* tokens, const void* dX,
                              float scale, float* dE, int accumulate, void* ws, size_t ws_bytes, void* hip_stream);
 
+/* Log probabilities from the last hidden rows: logits l = x W^T, of which a
+ * workspace of a fixed size holds a piece at a time.
+ *   x        [T, d_model] of `dtype` (d_model a multiple of 32 up to 16384; T up to 2^24)
+ *   W        [vocab, d_model] of `dtype`, the output matrix (vocab 1..2^20)
+ *   targets  [T] int32.  Negative: no target, logp 0 and no gradient.  One that is not
+ *            below vocab: logp NaN, and so are its row of dX and all of dW
+ *   logp     [T] float32 out: log softmax(l_t)[target_t]
+ *   log_z    [T] float32 out: log sum_v e^l_tv.  modse_head_fwd: either may be NULL
+ * x, W, dX, dW and the workspace lie at addresses that are multiples of 16. */
+modse_status modse_head_workspace_size(int64_t T, int32_t d_model, int32_t vocab, modse_dtype dtype, int which, size_t* bytes);
+modse_status modse_head_fwd(int64_t T, int32_t d_model, int32_t vocab, modse_dtype dtype, const void* x, const void* W,
+                            const int32_t* targets, float* logp, float* log_z, void* ws, size_t ws_bytes, void* hip_stream);
+
+/* The log probabilities and, in the same call (it needs no modse_head_fwd before it),
+ * the gradients of loss = sum_t d_logp[t] logp[t].
+ *   d_logp  [T] float32
+ *   logp    [T] float32 out or NULL
+ *   dX      [T, d_model] of `dtype` out, or NULL; it may lie in the buffer of x
+ *   dW      [vocab, d_model] float32 out, or NULL: overwritten, or added to with
+ *           accumulate = 1
+ * The gradient of the logits is rounded to 2^-17 of each of its values for dW (bf16:
+ * two numbers) and to the layer's type for dX.  Workspace sizes: MODSE_WS_FWD and
+ * MODSE_WS_BWD for the two calls.  Sums run in an order that the sizes alone fix.  T
+ * == 0 leaves dW as it is. */
+modse_status modse_head_bwd(int64_t T, int32_t d_model, int32_t vocab, modse_dtype dtype, const void* x, const void* W,
+                            const int32_t* targets, const float* d_logp, float* logp, void* dX, float* dW, int accumulate, void* ws,
+                            size_t ws_bytes, void* hip_stream);
+
 /* Dropout: y = residual + keep x / (1 - p), elementwise over [T, d_model].
  *   residual  of `dtype` or NULL (0)
  *   p         0..1, rounded to a multiple of 2^-16; at 1 everything is dropped

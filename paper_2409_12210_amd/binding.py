@@ -89,7 +89,10 @@ def load_library():
     lib.modse_embed_bwd.argtypes = [i64, i32, i32, C.c_int, vp, vp, f32, vp, C.c_int, vp, sz, vp]
     lib.modse_dropout_fwd.argtypes = [i64, i32, C.c_int, vp, vp, C.c_double, vp, C.c_uint32, vp, vp]
     lib.modse_dropout_bwd.argtypes = [i64, i32, C.c_int, vp, C.c_double, vp, C.c_uint32, vp, vp]
-    for name in ("modse_embed_fwd", "modse_embed_bwd_workspace_size", "modse_embed_bwd", "modse_dropout_fwd", "modse_dropout_bwd",
+    lib.modse_head_workspace_size.argtypes = [i64, i32, i32, C.c_int, C.c_int, szp]
+    lib.modse_head_fwd.argtypes = [i64, i32, i32, C.c_int, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.modse_head_bwd.argtypes = [i64, i32, i32, C.c_int, vp, vp, vp, vp, vp, vp, vp, C.c_int, vp, sz, vp]
+    for name in ("modse_head_workspace_size", "modse_head_fwd", "modse_head_bwd", "modse_embed_fwd", "modse_embed_bwd_workspace_size", "modse_embed_bwd", "modse_dropout_fwd", "modse_dropout_bwd",
                  "modse_norm_fwd", "modse_norm_bwd_workspace_size", "modse_norm_bwd", "modse_logprobs_workspace_size",
                  "modse_logprobs_fwd", "modse_logprobs_bwd", "modse_orthogonalize_workspace_size", "modse_orthogonalize",
                  "modse_workspace_size", "modse_saved_size", "modse_route", "modse_layer_fwd", "modse_layer_bwd",
@@ -543,6 +546,35 @@ def modse_embed_bwd(T, d_model, vocab, dtype, tokens, dX, scale, dE, accumulate,
     except _Unfit as e:
         return _unfit(e, "modse_embed_bwd", raise_on_error)
     return code and _check(code, "modse_embed_bwd", raise_on_error)
+
+
+def modse_head_workspace_size(T, d_model, vocab, dtype, which=WS_FWD, raise_on_error=True):
+    out = C.c_size_t(0)
+    code = load_library().modse_head_workspace_size(T, d_model, vocab, _dtype_code(dtype), which, C.byref(out))
+    _check(code, "modse_head_workspace_size", raise_on_error)
+    return out.value if code == 0 else code
+
+
+def modse_head_fwd(T, d_model, vocab, dtype, x, W, targets, logp, log_z, ws, ws_bytes=None, stream=None, raise_on_error=True) -> int:
+    kind, own, f32, i32 = _KINDS.get(dtype) or _kind(dtype)
+    try:
+        code = (_LIB or load_library()).modse_head_fwd(T, d_model, vocab, kind, _data(x, own), _data(W, own), _data(targets, i32),
+                                                       _data(logp, f32), _data(log_z, f32), _ptr(ws), _nbytes(ws, ws_bytes), _stream(stream))
+    except _Unfit as e:
+        return _unfit(e, "modse_head_fwd", raise_on_error)
+    return code and _check(code, "modse_head_fwd", raise_on_error)
+
+
+def modse_head_bwd(T, d_model, vocab, dtype, x, W, targets, d_logp, logp, dX, dW, accumulate, ws, ws_bytes=None, stream=None,
+                   raise_on_error=True) -> int:
+    kind, own, f32, i32 = _KINDS.get(dtype) or _kind(dtype)
+    try:
+        code = (_LIB or load_library()).modse_head_bwd(T, d_model, vocab, kind, _data(x, own), _data(W, own), _data(targets, i32),
+                                                       _data(d_logp, f32), _data(logp, f32), _data(dX, own), _data(dW, f32),
+                                                       int(bool(accumulate)), _ptr(ws), _nbytes(ws, ws_bytes), _stream(stream))
+    except _Unfit as e:
+        return _unfit(e, "modse_head_bwd", raise_on_error)
+    return code and _check(code, "modse_head_bwd", raise_on_error)
 
 
 def _generator(rng) -> Optional[int]:

@@ -21,9 +21,9 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libmodse.so")
 RESOURCES = os.path.join(HERE, "kernel_resources.txt")
-SOURCES = ["api.hip", "route.hip", "gemm.hip", "ops_api.hip", "norm.hip", "logprobs.hip", "ortho.hip", "embed.hip", "dropout.hip"]
+SOURCES = ["api.hip", "route.hip", "gemm.hip", "ops_api.hip", "norm.hip", "logprobs.hip", "ortho.hip", "embed.hip", "head.hip", "dropout.hip"]
 # the C entry points, and what they call on the host: layouts, splits, launches
-HOST_SOURCES = ("api.hip", "ops_api.hip", "norm.hip", "logprobs.hip", "ortho.hip", "embed.hip", "dropout.hip")
+HOST_SOURCES = ("api.hip", "ops_api.hip", "norm.hip", "logprobs.hip", "ortho.hip", "embed.hip", "head.hip", "dropout.hip")
 # packed fp32 VALU ops are switched off for all device code (known to misbehave on the test machines)
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Xclang", "-target-feature", "-Xclang",
          "-packed-fp32-ops", "-I" + os.path.join(ROOT, "include"), "-I" + CSRC, "-Wno-unused-command-line-argument",

@@ -87,6 +87,9 @@ enum GemmEpilogue {
   EPI_SWIGLU = 2,      // two accumulators a, b: C = h = silu(a)*b; optionally C2 = dh/da, C3 = dh/db
   EPI_SWIGLU_BWD = 3,  // acc = dh; E1 = dh/da, E2 = dh/db (saved by the forward pass): C = da, C2 = db
   EPI_STORE_DUALK = 4, // C = acc over two operand pairs (A,B) and (A2,B2)
+  // C = acc or C += acc, float32, rows below E2 (as an integer) alone: A has M columns, a multiple of 32, and C fewer rows.  bf16: over
+  // two operand pairs
+  EPI_ROWS_F32 = 5,
 };
 
 enum GemmLayout {

@@ -143,6 +143,7 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64) void gg_bf16_kernel(const Ge
   constexpr int BK = Cfg::BK, MI = Cfg::MI, NI = Cfg::NI, UPW = Cfg::UPW, PANEL = Cfg::PANEL, NSLOT = Cfg::NSLOT;
   constexpr int WM = Cfg::WM, WN = Cfg::WN;
   constexpr bool A_T = (LAYOUT & 1) != 0, B_T = (LAYOUT & 2) != 0;
+  constexpr bool DUALK = EPI == EPI_STORE_DUALK || EPI == EPI_ROWS_F32;  // two operand pairs
   static_assert(!(B_T && NB != 1), "a [K, N] operand is a single matrix");
   __shared__ __attribute__((aligned(1024))) char ring[NSLOT * PANEL];
 
@@ -230,7 +231,7 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64) void gg_bf16_kernel(const Ge
         c.base0 = static_cast<const char*>(uniform_ptr(c.base0));  // (otherwise the compiler keeps the cursor in vector registers)
         c.K = P.K();
         c.nk = (c.K + BK - 1) / BK;
-        c.nsteps = (EPI == EPI_STORE_DUALK) ? 2 * c.nk : c.nk;
+        c.nsteps = DUALK ? 2 * c.nk : c.nk;
       }
       if (!c.w.valid || c.nsteps != 0) break;
       c.w.tile = tile_of_round(first_tile, ++c.w.round);
@@ -262,7 +263,7 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64) void gg_bf16_kernel(const Ge
   };
   // all load units of a last step that is not a full one: what lies beyond K reads zeros
   auto issue_partial = [&](const LoadCursor& c, const uint32_t (&off)[UPW], uint32_t dst) {
-    const int kstep = (EPI == EPI_STORE_DUALK && c.step >= c.nk) ? c.step - c.nk : c.step;
+    const int kstep = (DUALK && c.step >= c.nk) ? c.step - c.nk : c.step;
     const bool tr = c.is_a ? A_T : B_T;
 #pragma unroll
     for (int i = 0; i < UPW; ++i) {
@@ -281,7 +282,7 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64) void gg_bf16_kernel(const Ge
       return;
     }
     int kstep = c.step;
-    if (EPI == EPI_STORE_DUALK && c.step >= c.nk) {
+    if (DUALK && c.step >= c.nk) {
       kstep -= c.nk;
       if (kstep == 0) c.src = c.base1;
     }
@@ -310,7 +311,7 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64) void gg_bf16_kernel(const Ge
       cc.N = P.N();
       cc.ldc = P.ldc();
       const int nk = (P.K() + BK - 1) / BK;
-      cc.nsteps = (EPI == EPI_STORE_DUALK) ? 2 * nk : nk;
+      cc.nsteps = DUALK ? 2 * nk : nk;
     }
   };
 
@@ -436,7 +437,7 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64) void gg_bf16_kernel(const Ge
   auto fast_left = [&](const LoadCursor& c) -> int {
     if (!c.fast) return 0;
     const int full = c.K / BK;
-    const int lim = (EPI == EPI_STORE_DUALK && c.step >= c.nk) ? c.nk + full : full;
+    const int lim = (DUALK && c.step >= c.nk) ? c.nk + full : full;
     return lim - c.step - 1;
   };
 
@@ -536,13 +537,13 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64) void gg_bf16_kernel(const Ge
     asm volatile("" : "+v"(elane));
     const int erow16 = elane & 15, equad = elane >> 4;
     const int cM = cc.M, cN = cc.N, cld = cc.ldc;
-    if constexpr (EPI == EPI_STORE_F32) {
+    if constexpr (EPI == EPI_STORE_F32 || EPI == EPI_ROWS_F32) {
       // float32 output (weight gradients).  It goes through LDS, one 32 x 32 block (4 KiB) at a time: written in
       // accumulator order (16 bytes per lane), read back row-wise, so that global memory sees whole 128-byte lines, also
       // where the old values are added (they come in one block ahead; read and written in accumulator order they made the
       // launch of 1021 tokens at d = 2048 take 694 us where overwriting took 333).  The slots are this wave's own load
       // units in the two panels of the step just finished.  M and N are multiples of 32, so a block lies inside the
-      // matrix or outside as a whole.
+      // matrix or outside as a whole.  (EPI_ROWS_F32: of the block that C ends in, the rows that are there.)
       const int erow = elane >> 3, echunk = elane & 7;
       const uint32_t voff = (uint32_t)(erow * cld + echunk * 4) * 4u;
       const int mleft = cM - cc.w.m0 - wm * WM, nleft = cN - cc.w.n0 - wn * WN;  // of the matrix, from the wave's corner on
@@ -551,13 +552,17 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64) void gg_bf16_kernel(const Ge
       auto inside = [&](int b) { return (b / NI32) * 32 < mleft && (b % NI32) * 32 < nleft; };
       auto row_group = [&](int b, int it) { return wave_c + ((long)((b / NI32) * 32 + it * 8) * cld + (b % NI32) * 32) * 4; };
       const bool stream_c = (option & GEMM_STREAM_C) != 0;
+      constexpr bool ROWS = EPI == EPI_ROWS_F32;
+      const int rows_end = ROWS ? (int)reinterpret_cast<intptr_t>(cc.E2) : 0, rows_m0 = cc.w.m0 + wm * WM;
+      auto row_there = [&](int b, int it) { return !ROWS || rows_m0 + (b / NI32) * 32 + it * 8 + erow < rows_end; };
       if (cc.nsteps == 0) {  // an expert without tokens: the ring holds nothing of this tile
         if (!accumulate)
 #pragma unroll
           for (int b = 0; b < NBLK; ++b)
             if (inside(b))
 #pragma unroll
-              for (int it = 0; it < 4; ++it) global_store16_s(row_group(b, it), voff, f32x4{0.f, 0.f, 0.f, 0.f}, stream_c);
+              for (int it = 0; it < 4; ++it)
+                if (row_there(b, it)) global_store16_s(row_group(b, it), voff, f32x4{0.f, 0.f, 0.f, 0.f}, stream_c);
       } else {
         // (the late waves have already refilled their units of the A panel's slot: they have one slot, and
         // write a block into it only after the block before has been read back)
@@ -579,8 +584,15 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64) void gg_bf16_kernel(const Ge
           f32x4 old[4];
           // (never masked, see the dH epilogue below: outside the matrix its last rows and columns are read instead)
           auto fetch = [&](int b, int it) {
-            const int m = min((b / NI32) * 32, mleft - 32), n = min((b % NI32) * 32, nleft - 32);
-            old[it] = global_load16_f32_s<STREAM>(wave_c + ((long)(m + it * 8) * cld + n) * 4, voff);
+            const int n = min((b % NI32) * 32, nleft - 32);
+            if constexpr (ROWS) {  // 32 rows that are there, or all: a lane beyond the last row reads that one
+              const int m = min(rows_m0 + (b / NI32) * 32, max(rows_end - 32, 0));
+              const int r = min(rows_m0 + (b / NI32) * 32 - m + it * 8 + erow, rows_end - 1 - m);
+              old[it] = global_load16_f32_s<STREAM>(wave_c + ((long)(m - rows_m0) * cld + n) * 4, (uint32_t)(r * cld + echunk * 4) * 4u);
+            } else {
+              const int m = min((b / NI32) * 32, mleft - 32);
+              old[it] = global_load16_f32_s<STREAM>(wave_c + ((long)(m + it * 8) * cld + n) * 4, voff);
+            }
           };
           if constexpr (ADD) {
 #pragma unroll
@@ -608,7 +620,7 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64) void gg_bf16_kernel(const Ge
                 v += old[it];
                 if (b + 1 < NBLK) fetch(b + 1, it);
               }
-              if (in) global_store16_s(row_group(b, it), voff, v, stream_c);
+              if (in && row_there(b, it)) global_store16_s(row_group(b, it), voff, v, stream_c);
             }
           });
         };

@@ -384,12 +384,14 @@ __device__ __forceinline__ void gg_block(const GemmPlan* __restrict__ plan, int 
   // whole lines: written in accumulator order, read back row-wise.  The staging area lies in the slots that the step
   // after the last one would use: nobody reads them any more and no load is on its way into them.
   typedef std::conditional_t<F32 || EPI == EPI_STORE_F32, float, bf16_t> out_t;
+  static_assert(F32 || EPI != EPI_ROWS_F32, "for float32");
   constexpr int OS = sizeof(out_t), UC = OS == 4 ? 32 : (WN < 64 ? WN : 64);  // columns of a unit
   constexpr int CPR = UC * OS / 16, ITS = 32 * CPR / 64, NJU = WN / UC, JPU = UC / 32;
   typedef std::conditional_t<OS == 4, f32x4, bf16x8> chunk_t;
   char* const slot = ring + slot_byte(rb) + wave * 4096;
   const int er = lane & 31, esw = (er >> 1) & 7;
   const int ldc = P.ldc();
+  const int rows_end = EPI == EPI_ROWS_F32 ? (int)reinterpret_cast<intptr_t>(P.E2()) : M;
   auto stage = [&](auto value) {  // value(jj, idx): element idx of the accumulator of the unit's block jj
 #pragma unroll
     for (int jj = 0; jj < JPU; ++jj)
@@ -415,7 +417,7 @@ __device__ __forceinline__ void gg_block(const GemmPlan* __restrict__ plan, int 
   // element offset of this lane's chunk `it` of unit (i, ju) in C, or -1 outside the matrix
   auto offset = [&](int i, int ju, int it) -> long {
     const int m = m0 + wm * WM + i * 32 + row_of(it), n = n0 + wn * WN + ju * UC + (lane % CPR) * (16 / OS);
-    return (m < M && n < N) ? (long)m * ldc + n : -1;
+    return (m < rows_end && n < N) ? (long)m * ldc + n : -1;
   };
   auto at = [&](const void* base, long o) { return (global_chunk_t*)(uintptr_t)(static_cast<const out_t*>(base) + o); };
   auto put = [&](void* C, long o, chunk_t v) {
@@ -488,7 +490,7 @@ __device__ __forceinline__ void gg_block(const GemmPlan* __restrict__ plan, int 
           continue;
         }
         stage([&](int jj, int x) { return acc[0][i][j0 + jj][x]; });
-        if constexpr (EPI == EPI_STORE_F32) {
+        if constexpr (EPI == EPI_STORE_F32 || EPI == EPI_ROWS_F32) {
           if (accumulate) {
             chunk_t old[ITS];
 #pragma unroll

@@ -108,6 +108,21 @@ inline int64_t embed_most_chunks(int64_t T) {
 }
 hipError_t launch_embed_bwd(modse_dtype dt, const EmbedBwdArgs& a, hipStream_t s);
 
+// head.hip
+struct HeadArgs {
+  const void *x, *W;
+  const int32_t* targets;
+  const float* d_logp;
+  float *logp, *log_z;
+  void* dX;   // with dX or dW: gradients
+  float* dW;
+  int64_t T;
+  int32_t d, vocab, accumulate;
+};
+int64_t head_piece_rows(int32_t vocab);  // rows whose logits are in the workspace at a time, at the most
+size_t head_workspace(int64_t T, int32_t d, int32_t vocab, modse_dtype dt, bool grad);
+hipError_t launch_head(modse_dtype dt, const HeadArgs& a, char* ws, hipStream_t s);
+
 // ---------------------------------------------------------------- rows of any alignment
 // Sixteen bytes of a row that starts anywhere: gfx950 takes such accesses at the alignment of the element, so a row of odd length
 // needs no path of its own.  Neighbouring lanes take neighbouring vectors.  (Eight float32 per lane, in two loads half of whose

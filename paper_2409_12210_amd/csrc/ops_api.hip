@@ -47,6 +47,13 @@ modse_status check_embed_bwd(int64_t T, int32_t d, int32_t vocab, const modse_dt
   // (a launch has fewer than 2^32 threads, 256 of them for 256 columns of a chunk)
   return embed_chunks(T) * ((d + 255) / 256) >= 1 << 24 ? MODSE_ERR_UNSUPPORTED : MODSE_OK;
 }
+modse_status check_head(int64_t T, int32_t d, int32_t vocab, const modse_dtype& dtype) {
+  const modse_status st = check_vocab(T, d, vocab, dtype);
+  if (st != MODSE_OK) return st;
+  if (d % 32) return MODSE_ERR_INVALID_ARG;
+  // (pieces of at least half the rows that they could have, three blocks for each)
+  return T > (int64_t)1 << 24 ? MODSE_ERR_UNSUPPORTED : MODSE_OK;
+}
 struct EmbedLayout {
   size_t n_sorted, order, keys, part, total;
 };
@@ -231,6 +238,38 @@ modse_status modse_embed_bwd(int64_t T, int32_t d_model, int32_t vocab, modse_dt
                           reinterpret_cast<int32_t*>(wsb + w.keys), reinterpret_cast<float*>(wsb + w.part), T, d_model, vocab,
                           embed_chunk(T), (int32_t)align_up(d_model, 4), accumulate, scale};
   return hip_status(launch_embed_bwd(dtype, a, static_cast<hipStream_t>(hip_stream)));
+}
+
+modse_status modse_head_workspace_size(int64_t T, int32_t d_model, int32_t vocab, modse_dtype dtype, int which, size_t* bytes) {
+  if (!bytes || (which != MODSE_WS_FWD && which != MODSE_WS_BWD)) return MODSE_ERR_INVALID_ARG;
+  const modse_status st = check_head(T, d_model, vocab, dtype);
+  if (st != MODSE_OK) return st;
+  *bytes = head_workspace(T, d_model, vocab, dtype, which == MODSE_WS_BWD);
+  return MODSE_OK;
+}
+
+modse_status modse_head_fwd(int64_t T, int32_t d_model, int32_t vocab, modse_dtype dtype, const void* x, const void* W,
+                            const int32_t* targets, float* logp, float* log_z, void* ws, size_t ws_bytes, void* hip_stream) {
+  const modse_status st = check_head(T, d_model, vocab, dtype);
+  if (st != MODSE_OK) return st;
+  if (T == 0) return MODSE_OK;
+  if (!x || !W || !targets || (!logp && !log_z) || !ws || !aligned16(x) || !aligned16(W) || !aligned16(ws)) return MODSE_ERR_INVALID_ARG;
+  if (ws_bytes < head_workspace(T, d_model, vocab, dtype, false)) return MODSE_ERR_WORKSPACE;
+  const HeadArgs a = {x, W, targets, nullptr, logp, log_z, nullptr, nullptr, T, d_model, vocab, 0};
+  return hip_status(launch_head(dtype, a, static_cast<char*>(ws), static_cast<hipStream_t>(hip_stream)));
+}
+
+modse_status modse_head_bwd(int64_t T, int32_t d_model, int32_t vocab, modse_dtype dtype, const void* x, const void* W,
+                            const int32_t* targets, const float* d_logp, float* logp, void* dX, float* dW, int accumulate, void* ws,
+                            size_t ws_bytes, void* hip_stream) {
+  const modse_status st = check_head(T, d_model, vocab, dtype);
+  if (st != MODSE_OK) return st;
+  if (T == 0) return MODSE_OK;
+  if (!x || !W || !targets || !d_logp || (!dX && !dW) || !ws || !aligned16(x) || !aligned16(W) || !aligned16(dX) || !aligned16(dW) || !aligned16(ws))
+    return MODSE_ERR_INVALID_ARG;
+  if (ws_bytes < head_workspace(T, d_model, vocab, dtype, true)) return MODSE_ERR_WORKSPACE;
+  const HeadArgs a = {x, W, targets, d_logp, logp, nullptr, dX, dW, T, d_model, vocab, accumulate};
+  return hip_status(launch_head(dtype, a, static_cast<char*>(ws), static_cast<hipStream_t>(hip_stream)));
 }
 
 modse_status modse_dropout_fwd(int64_t T, int32_t d_model, modse_dtype dtype, const void* x, const void* residual, double p,

@@ -85,3 +85,62 @@ def test_tensors_that_the_library_could_not_see_are_refused():
     assert dropout(x=b, rng=pair.float(), y=b, back=True) == INVALID
     with pytest.raises(m.ModseError, match="expected two int64"):
         m.modse_dropout_bwd(4, 64, "bf16", b, 0.1, pair.float(), 0, b, stream=0)
+
+
+def head_fwd(T=4, d=64, V=100, dtype="bf16", x=P, W=P, targets=P, logp=P, log_z=P, ws=P, ws_bytes=1 << 40):
+    return m.modse_head_fwd(T, d, V, dtype, x, W, targets, logp, log_z, ws, ws_bytes, **NO)
+
+
+def head_bwd(T=4, d=64, V=100, dtype="bf16", x=P, W=P, targets=P, d_logp=P, logp=P, dX=P, dW=P, ws=P, ws_bytes=1 << 40):
+    return m.modse_head_bwd(T, d, V, dtype, x, W, targets, d_logp, logp, dX, dW, False, ws, ws_bytes, **NO)
+
+
+BOTH = [
+    (dict(T=-1), INVALID), (dict(d=0), INVALID), (dict(d=48), INVALID), (dict(d=16416), UNSUPPORTED), (dict(V=0), INVALID),
+    (dict(V=(1 << 20) + 1), UNSUPPORTED), (dict(T=(1 << 24) + 1), UNSUPPORTED), (dict(dtype="fp16"), UNSUPPORTED), (dict(x=None), INVALID),
+    (dict(W=None), INVALID), (dict(targets=None), INVALID), (dict(ws=None), INVALID), (dict(ws=P + 8), INVALID), (dict(x=P + 2), INVALID),
+    (dict(W=P + 8), INVALID), (dict(ws_bytes=1000), WORKSPACE), (dict(T=0, x=None, W=None, ws=None, ws_bytes=0), OK),
+]
+
+
+@pytest.mark.parametrize("over,code", BOTH + [(dict(logp=None, log_z=None), INVALID)])
+def test_head_fwd_refuses(over, code):
+    assert head_fwd(**over) == code
+
+
+@pytest.mark.parametrize("over,code", BOTH + [(dict(d_logp=None), INVALID), (dict(dX=None, dW=None), INVALID), (dict(dX=P + 4), INVALID),
+                                              (dict(dW=P + 4), INVALID)])
+def test_head_bwd_refuses(over, code):
+    assert head_bwd(**over) == code
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d,V", [(64, 100), (2048, 32000), (256, 50257), (4096, 131072), (16384, 1 << 20)])
+def test_head_workspaces_serve_fewer_rows_and_stay_bounded(d, V, dtype):
+    for which, call in ((m.WS_FWD, head_fwd), (m.WS_BWD, head_bwd)):
+        size = lambda T: m.modse_head_workspace_size(T, d, V, dtype, which)  # noqa: E731
+        last = 0
+        for T in (0, 1, 2, 15, 16, 17, 32, 33, 64, 65, 100, 255, 256, 257, 1000, 2048, 2049, 4096, 8192, 8193, 9000, 16384, 20000, 100000):
+            now = size(T)
+            assert now >= last
+            last = now
+            if T:
+                assert call(T=T, d=d, V=V, dtype=dtype, ws_bytes=now - 1) == WORKSPACE
+                # (with all that it needs the call is refused for another reason)
+                for t in {1, T // 2, T} - {0}:
+                    assert call(T=t, d=d, V=V, dtype=dtype, ws_bytes=now, x=None) == INVALID
+        assert last < 4 << 30
+    assert m.modse_head_workspace_size(4, d, V, dtype, m.WS_FWD_SAVED, raise_on_error=False) == INVALID
+    assert m.modse_head_workspace_size(4, d - 1, V, dtype, m.WS_FWD, raise_on_error=False) == INVALID
+
+
+def test_head_refuses_tensors_that_the_library_could_not_see():
+    x, W, i, f = torch.zeros((4, 64)), torch.zeros((100, 64)), torch.zeros(4, dtype=torch.int32), torch.zeros(4)
+    ws = torch.zeros(64, dtype=torch.uint8)
+    for a, b, t, p in ((x.bfloat16(), W, i, f), (x, W.bfloat16(), i, f), (x, W, i.long(), f), (x, W, i, f.double()), (x[:, :32], W, i, f),
+                       (x, torch.zeros((64, 100)).t(), i, f)):
+        assert head_fwd(dtype="f32", x=a, W=b, targets=t, logp=p, log_z=None, ws=ws, ws_bytes=None) == INVALID
+        assert head_bwd(dtype="f32", x=a, W=b, targets=t, d_logp=f, logp=p, dX=x, dW=W, ws=ws, ws_bytes=None) == INVALID
+    assert head_bwd(dtype="bf16", x=x.bfloat16(), W=W.bfloat16(), targets=i, d_logp=f, logp=f, dX=x.bfloat16(), dW=W.bfloat16(), ws=ws) == INVALID
+    # fitting ones come as far as the workspace
+    assert head_bwd(dtype="f32", x=x, W=W, targets=i, d_logp=f, logp=f, dX=x, dW=W, ws=ws, ws_bytes=None) == WORKSPACE

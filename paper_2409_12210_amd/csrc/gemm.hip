@@ -116,9 +116,10 @@ hipError_t launch_grouped_gemm(modse_dtype dt, int epilogue, TileShape t, const 
     case EPI_STORE_DUALK:
       return run_bf16<256, 256, 1, 4, 2, EPI_STORE_DUALK, LAYOUT_B_KN>(plan, n_prob, accumulate, option, max_tiles, s);
     case EPI_STORE_F32:
-      if (layout == LAYOUT_TN) return run_bf16<256, 256, 1, 4, 2, EPI_STORE_F32, LAYOUT_TN>(plan, n_prob, accumulate, option, max_tiles, s);
       if (layout == LAYOUT_B_KN) return run_bf16<256, 256, 1, 4, 2, EPI_STORE_F32, LAYOUT_B_KN>(plan, n_prob, accumulate, option, max_tiles, s);
       return run_bf16<256, 256, 1, 4, 2, EPI_STORE_F32, LAYOUT_AB_K>(plan, n_prob, accumulate, option, max_tiles, s);
+    case EPI_LOGITS:
+      return run_bf16<256, 256, 1, 4, 2, EPI_LOGITS, LAYOUT_TN>(plan, n_prob, accumulate, option, max_tiles, s);
     case EPI_ROWS_F32:
       return run_bf16<256, 256, 1, 4, 2, EPI_ROWS_F32, LAYOUT_AB_K>(plan, n_prob, accumulate, option, max_tiles, s);
   }

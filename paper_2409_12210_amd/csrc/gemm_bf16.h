@@ -537,7 +537,59 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64) void gg_bf16_kernel(const Ge
     asm volatile("" : "+v"(elane));
     const int erow16 = elane & 15, equad = elane >> 4;
     const int cM = cc.M, cN = cc.N, cld = cc.ldc;
-    if constexpr (EPI == EPI_STORE_F32 || EPI == EPI_ROWS_F32) {
+    if constexpr (EPI == EPI_LOGITS) {
+      // A row's 128 columns of this wave lie in four lanes, 32 in each.
+      static_assert(WN == 128 && NB == 1, "pairs of 128 columns");
+      constexpr float LOG2E = 1.44269504088896340736f;
+      const int nw = cc.w.n0 + wn * WN, nleft = cN - nw;  // the wave's first column, columns from there on
+      if (nleft > 0) {
+        const uint64_t place = reinterpret_cast<uint64_t>(cc.E2);
+        const int first_col = (int)(uint32_t)place + nw;
+        float* const part = reinterpret_cast<float*>(const_cast<char*>(cc.C2)) + (size_t)(first_col >> 7) * (place >> 32) * 2;
+        const int32_t* const targets = reinterpret_cast<const int32_t*>(cc.E1);
+        const int row0 = cc.w.m0 + wm * WM + erow16;
+        int want[MI];  // the target's column from this lane's first one on
+#pragma unroll
+        for (int i = 0; i < MI; ++i) want[i] = targets[min(row0 + i * 16, cM - 1)];
+        static_for<MI>([&](auto block) {
+          constexpr int i = decltype(block)::value;
+          const int row = row0 + i * 16;
+          const int at = want[i] - first_col - equad * 4;
+          float m = -__builtin_inff(), there = 0.f;
+          auto value = [&](int j, int x) { return j * 16 + equad * 4 + x < nleft ? acc[0][i][j][x] : -__builtin_inff(); };
+          auto sums = [&](auto inside_tag) {
+            constexpr bool INSIDE = decltype(inside_tag)::value;
+#pragma unroll
+            for (int j = 0; j < NI; ++j)
+#pragma unroll
+              for (int x = 0; x < 4; ++x) {
+                const float v = INSIDE ? acc[0][i][j][x] : value(j, x);
+                m = fmaxf(m, v);
+                there = at == j * 16 + x ? v : there;
+              }
+            m = fmaxf(m, __shfl_xor(m, 16, 64));
+            m = fmaxf(m, __shfl_xor(m, 32, 64));
+            float s = 0.f;
+#pragma unroll
+            for (int j = 0; j < NI; ++j)
+#pragma unroll
+              for (int x = 0; x < 4; ++x) s += __builtin_amdgcn_exp2f(((INSIDE ? acc[0][i][j][x] : value(j, x)) - m) * LOG2E);
+            s += __shfl_xor(s, 16, 64);
+            s += __shfl_xor(s, 32, 64);
+            return s;
+          };
+          const float s = nleft >= WN ? sums(std::true_type{}) : sums(std::false_type{});
+          if (row < cM) {
+            typedef float f32x2 __attribute__((ext_vector_type(2)));
+            if (equad == 0) *reinterpret_cast<f32x2*>(part + (size_t)row * 2) = f32x2{m, s};
+            if (at >= 0 && at < WN && (at & 15) < 4 && want[i] - nw - (int)(uint32_t)place < nleft)
+              reinterpret_cast<float*>(const_cast<char*>(cc.C3))[row] = there;
+          }
+        });
+      }
+    }
+    if constexpr (EPI == EPI_STORE_F32 || EPI == EPI_ROWS_F32 || EPI == EPI_LOGITS) {
+      if (EPI != EPI_LOGITS || cc.C) {
       // float32 output (weight gradients).  It goes through LDS, one 32 x 32 block (4 KiB) at a time: written in
       // accumulator order (16 bytes per lane), read back row-wise, so that global memory sees whole 128-byte lines, also
       // where the old values are added (they come in one block ahead; read and written in accumulator order they made the
@@ -627,6 +679,7 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64) void gg_bf16_kernel(const Ge
         if (accumulate && stream_c) tile(std::true_type{}, std::true_type{});
         else if (accumulate) tile(std::true_type{}, std::false_type{});
         else tile(std::false_type{}, std::false_type{});
+      }
       }
     } else {
       // 16-bit outputs go through LDS so that global memory sees whole 128-byte lines: the wave works in

@@ -4,9 +4,14 @@
 //   l = x W^T,  log Z_t = log sum_v e^l_tv,  logp_t = l_t,target - log Z_t
 //   G_tv = w_t (1[v = target_t] - e^(l_tv - log Z_t)),  dX = G W,  dW = G^T x
 //
-// The batch is taken in pieces of rows whose logits and G fit a workspace of a fixed size.  The products are those of the grouped
-// GEMM kernels, whose problem tables one launch makes for all pieces.  dX is a product over the whole vocabulary with few
-// columns, so its sum is cut into parts that fill the chip; the parts are float32 slabs that a last launch adds up in order.
+// The batch is taken in pieces of rows whose G fits a workspace of a fixed size.  The products are those of the grouped GEMM kernels,
+// whose problem tables one launch makes for the whole call.  dX is a product over the whole vocabulary with few columns, so its
+// sum is cut into parts that fill the chip; the parts are float32 slabs that a last launch adds up in order.
+//
+// bf16: the product of the logits leaves, for every row and 128 columns, their maximum and sum of exponentials, and the target's logit
+// (EPI_LOGITS); one launch joins them.  Without gradients no logit is stored.  With gradients the logits of a few rows are, in
+// float32 and in a buffer that stays in the caches, and another launch turns them into G.  float32: the logits are stored and
+// a row is gone through twice, the second time to put G in its place.
 //
 // dW is float32, and a term of its sums is rounded to 2^-17: in bf16 G is kept as two numbers, hi + lo, and dW takes both.  dX
 // is rounded to bf16 itself and takes hi alone.
@@ -17,45 +22,66 @@
 namespace {
 using namespace modse_gemm;
 
-constexpr int64_t PIECE = (int64_t)1 << 28;   // logits of a piece of rows
-constexpr int64_t W_PART = (int64_t)1 << 30;  // elements of W that one problem reads (kernels count them in 32 bits)
-constexpr size_t ALIGN = 256;                 // of what is in the workspace, which itself may lie at any sixteen bytes
-constexpr int64_t SLAB_ROWS = 8192;           // of all parts of dX together, unless one part has more
+constexpr int64_t GRAD_CELLS = (int64_t)1 << 28;   // values of G in the workspace (float32: of logits)
+constexpr int64_t LOGIT_CELLS = (int64_t)1 << 28;  // bf16 logits in the workspace
+constexpr int64_t PAIR_CELLS = (int64_t)1 << 27;   // pairs of 128 columns in it
+constexpr int64_t W_PART = (int64_t)1 << 30;       // elements of W that one problem reads (kernels count them in 32 bits)
+constexpr size_t ALIGN = 256;                      // of what is in the workspace, which itself may lie at any sixteen bytes
+constexpr int64_t SLAB_CELLS = (int64_t)1 << 26;   // values of all parts of dX together, unless one part has more
+constexpr int MAX_PARTS = 32;                      // of dX
 
 struct HeadShape {
   int64_t T;
   int32_t d, vocab, ldv;   // ldv: distance of rows of logits and G
-  int32_t rows, pieces;    // rows of a piece, a multiple of 256 (of 32 where there is one piece)
+  int32_t rows, pieces;    // rows of a piece
+  int32_t sub, subs;       // rows that one product of logits takes, such products of a (whole) piece
   int32_t w_parts, w_rows; // problems of the logits, rows of W in each
   int32_t k_parts, k_len;  // problems of dX, columns of G in each
-  int32_t bf16;
+  int32_t bf16, grad;
   TileShape logits_tile, dx_tile, dw_tile;
+  __host__ __device__ int64_t products() const { return (T + sub - 1) / sub; }  // (sub divides rows)
 };
 
 int32_t padded_rows(int64_t n) { return (int32_t)align_up((size_t)n, 32); }
+// the most rows of a buffer of so many cells, `per_row` of them a row: a power of two from 256 to 65536
+int64_t rows_in(int64_t cells, int64_t per_row) {
+  int64_t r = 256;
+  while (r < 65536 && 2 * r * per_row <= cells) r *= 2;
+  return r;
+}
+int64_t most_rows(int32_t vocab, bool bf16, bool grad) {
+  return bf16 && !grad ? rows_in(PAIR_CELLS, (vocab + 127) / 128) : rows_in(GRAD_CELLS, (int64_t)align_up(vocab, 64));
+}
+int64_t most_sub(int32_t vocab, bool bf16, bool grad) {
+  return bf16 && grad ? rows_in(LOGIT_CELLS, (int64_t)align_up(vocab, 64)) : most_rows(vocab, bf16, grad);
+}
 
-HeadShape head_shape(int64_t T, int32_t d, int32_t vocab, modse_dtype dt) {
+HeadShape head_shape(int64_t T, int32_t d, int32_t vocab, modse_dtype dt, bool grad) {
   HeadShape h = {};
   h.T = T;
   h.d = d;
   h.vocab = vocab;
   h.bf16 = dt == MODSE_BF16;
+  h.grad = grad;
   h.ldv = (int32_t)align_up(vocab, 64);
-  const int64_t most = head_piece_rows(vocab);
+  const int64_t most = most_rows(vocab, h.bf16, grad), sub = std::min(most, most_sub(vocab, h.bf16, grad));
+  // pieces of about one size, in whole products of logits
+  h.sub = T <= sub ? padded_rows(T) : (int32_t)sub;
   h.pieces = (int32_t)((T + most - 1) / most);
-  h.rows = h.pieces == 1 ? padded_rows(T) : (int32_t)align_up((size_t)((T + h.pieces - 1) / h.pieces), 256);
+  h.rows = (int32_t)align_up((size_t)((T + h.pieces - 1) / h.pieces), (size_t)h.sub);
   h.pieces = (int32_t)((T + h.rows - 1) / h.rows);
+  h.subs = h.rows / h.sub;
   h.w_rows = (int32_t)std::min<int64_t>(vocab, W_PART / d / 256 * 256);
   h.w_parts = (vocab + h.w_rows - 1) / h.w_rows;
   auto tiles = [](int64_t m, int64_t n, int b) { return ((m + b - 1) / b) * ((n + b - 1) / b); };
   auto tile = [&](int64_t m, int64_t n) { const int b = h.bf16 ? 256 : tiles(m, n, 128) >= 512 ? 128 : 64; return TileShape{b, b}; };
-  h.logits_tile = tile(h.rows, vocab);
+  h.logits_tile = tile(h.sub, vocab);
   h.dw_tile = tile(vocab, d);
   h.dx_tile = TileShape{h.bf16 ? 256 : 128, h.bf16 ? 256 : 128};
   // Parts of dX: whole rounds of workgroups over the chip, each part with six further steps for its opening and its end, and slabs that
   // are written and read.
   const int64_t out = tiles(h.rows, d, h.dx_tile.bm), steps = (vocab + 63) / 64, slots = h.bf16 ? 256 : 512;
-  const int64_t parts_most = std::min<int64_t>({32, steps, std::max<int64_t>(1, SLAB_ROWS / h.rows)});
+  const int64_t parts_most = std::min<int64_t>({MAX_PARTS, steps, std::max<int64_t>(1, SLAB_CELLS / ((int64_t)h.rows * d))});
   double best = 0;
   for (int64_t n = 1; n <= parts_most; ++n) {
     const int64_t len = (steps + n - 1) / n, parts = (steps + len - 1) / len;
@@ -71,30 +97,35 @@ HeadShape head_shape(int64_t T, int32_t d, int32_t vocab, modse_dtype dt) {
 }
 
 struct HeadBufs {
-  GemmPlan* plans;  // [pieces][3]: logits, dX, dW
-  float* logits;    // [rows, ldv]; float32 layers: then G
-  bf16_t *hi, *lo;  // [rows, ldv] G
-  float* slabs;     // [k_parts][rows, d]
+  GemmPlan* plans;   // logits of every product, then dX and dW of every piece
+  float* logits;     // [sub, ldv]; float32 layers: then G
+  float* pairs;      // [ceil(vocab / 128)][sub] maximum and sum
+  float* at_target;  // [sub] the target's logit
+  float* off;        // [sub] log Z
+  bf16_t *hi, *lo;   // [rows, ldv] G
+  float* slabs;      // [k_parts][rows, d]
 };
 
 struct HeadPlanArgs {
   HeadShape h;
   HeadBufs b;
   const void *x, *W;
+  const int32_t* targets;
   float* dW;
-  int32_t grad;
 };
 
-// Block 3 i + g (without gradients block i): the problems of product g of piece i.
+// The problems of one product: of the logits, one block for each, then of dX and of dW, a block for each piece.
 __global__ __launch_bounds__(64) void head_plan_kernel(HeadPlanArgs a) {
   __shared__ int s_tiles[MODSE_MAX_PROBLEMS];
   const HeadShape& h = a.h;
-  const int lane = threadIdx.x, per = a.grad ? 3 : 1, piece = blockIdx.x / per, which = blockIdx.x % per;
+  const int lane = threadIdx.x, products = (int)h.products();
+  const int which = (int)blockIdx.x < products ? 0 : 1 + ((int)blockIdx.x - products) % 2;
+  const int rows = which == 0 ? h.sub : h.rows;
+  const int64_t t0 = (int64_t)(which == 0 ? (int)blockIdx.x : ((int)blockIdx.x - products) / 2) * rows;
   const size_t es = h.bf16 ? 2 : 4;
-  const int64_t t0 = (int64_t)piece * h.rows;
-  const int m = (int)min((int64_t)h.rows, h.T - t0);
+  const int m = (int)min((int64_t)rows, h.T - t0);
   const char* const x = cadd(a.x, (size_t)t0 * h.d * es);
-  GemmPlan* const plan = a.b.plans + piece * 3 + which;
+  GemmPlan* const plan = a.b.plans + blockIdx.x;
   const int n = which == 0 ? h.w_parts : which == 1 ? h.k_parts : 1;
   for (int p = lane; p < n; p += 64) {
     GemmProblem P = {};
@@ -103,7 +134,11 @@ __global__ __launch_bounds__(64) void head_plan_kernel(HeadPlanArgs a) {
       const int v0 = p * h.w_rows;
       P.A = x;
       P.B = cadd(a.W, (size_t)v0 * h.d * es);
-      P.C = a.b.logits + v0;
+      if (h.grad || !h.bf16) P.C = a.b.logits + v0;
+      P.C2 = a.b.pairs;
+      P.C3 = a.b.at_target;
+      P.E1 = a.targets + t0;
+      P.E2 = reinterpret_cast<const void*>((uint64_t)h.sub << 32 | (uint32_t)v0);
       P.M = m; P.N = min(h.w_rows, h.vocab - v0); P.K = h.d;
       P.lda = h.d; P.ldb = h.d; P.ldc = h.ldv;
       t = h.logits_tile;
@@ -135,23 +170,92 @@ __global__ __launch_bounds__(64) void head_plan_kernel(HeadPlanArgs a) {
 constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
 
 struct HeadRowsArgs {
-  const int32_t* targets;
+  const int32_t* targets;  // of the product's first row
   const float* d_logp;
-  float *logp, *log_z;
+  float *logp, *log_z;     // of the product's first row, either may be null
   float* logits;
-  bf16_t *hi, *lo;
-  int64_t t0;
-  int32_t rows, vocab, ldv;
+  const float *pairs, *at_target;
+  float* off;
+  bf16_t *hi, *lo;         // of the product's first row
+  int32_t rows, vocab, ldv, pair_rows;
 };
+__device__ __forceinline__ float row_weight(const HeadRowsArgs& a, int row, int32_t target) {
+  return target < 0 ? 0.f : target >= a.vocab ? __builtin_nanf("") : a.d_logp[row];
+}
+__device__ __forceinline__ float grad_of(float logit, float off, float w, int32_t target, int c, int vocab) {
+  const float p = __builtin_amdgcn_exp2f((logit - off) * LOG2E);
+  return c >= vocab || target < 0 ? 0.f : c == target ? w * (1.f - p) : -w * p;
+}
+__device__ __forceinline__ void put_row(float* logp, float* log_z, int32_t target, int vocab, float at_target, float top, float log_sum) {
+  if (logp) *logp = target < 0 ? 0.f : target >= vocab ? __builtin_nanf("") : at_target - top - log_sum;
+  if (log_z) *log_z = top + log_sum;
+}
+__device__ __forceinline__ void put_row(const HeadRowsArgs& a, int row, int32_t target, float at_target, float top, float log_sum) {
+  put_row(a.logp ? a.logp + row : nullptr, a.log_z ? a.log_z + row : nullptr, target, a.vocab, at_target, top, log_sum);
+}
 
-// A row of logits: its sums, and (GRAD) its row of G.  Columns behind the vocabulary become zeros.
-template <bool GRAD, bool BF16>
+// bf16: joins the pairs of 64 rows.  Sixteen waves, each takes every sixteenth pair of a row.
+__global__ __launch_bounds__(1024) void head_stats_kernel(HeadRowsArgs a) {
+  __shared__ float s_m[16][64], s_s[16][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int row = blockIdx.x * 64 + lane, n = (a.vocab + 127) / 128;
+  constexpr int AHEAD = 8;
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
+  float m = -__builtin_inff(), s = 0.f;
+  if (row < a.rows) {
+    for (int p = wave; p < n; p += 16 * AHEAD) {
+      f32x2 v[AHEAD];
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i)
+        v[i] = *reinterpret_cast<const f32x2*>(a.pairs + ((int64_t)min(p + i * 16, n - 1) * a.pair_rows + row) * 2);
+      float most = m;
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i) most = fmaxf(most, v[i][0]);
+      s *= __builtin_amdgcn_exp2f((m - most) * LOG2E);
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i)
+        if (p + i * 16 < n) s += v[i][1] * __builtin_amdgcn_exp2f((v[i][0] - most) * LOG2E);
+      m = most;
+    }
+  }
+  s_m[wave][lane] = m;
+  s_s[wave][lane] = s;
+  __syncthreads();
+  if (wave > 0 || row >= a.rows) return;
+  float top = m, sum = 0.f;
+  for (int w = 1; w < 16; ++w) top = fmaxf(top, s_m[w][lane]);
+  for (int w = 0; w < 16; ++w) sum += s_s[w][lane] * __builtin_amdgcn_exp2f((s_m[w][lane] - top) * LOG2E);
+  const float log_sum = __builtin_amdgcn_logf(sum) * LN2;
+  put_row(a, row, a.targets[row], a.at_target[row], top, log_sum);
+  a.off[row] = top + log_sum;
+}
+
+// bf16: G of a row's 2048 columns as two numbers each.  Columns behind the vocabulary become zeros.
+__global__ __launch_bounds__(256) void head_grad_kernel(HeadRowsArgs a, int segs) {
+  const int row = blockIdx.x / segs, c = (blockIdx.x - row * segs) * 2048 + threadIdx.x * 8;
+  if (c >= a.ldv) return;
+  const int32_t target = a.targets[row];
+  const float off = a.off[row], w = row_weight(a, row, target);
+  const float* const l = a.logits + (int64_t)row * a.ldv + c;
+  const f32x4 v[2] = {*reinterpret_cast<const f32x4*>(l), *reinterpret_cast<const f32x4*>(l + 4)};
+  bf16x8 hi, lo;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const float g = grad_of(v[e >> 2][e & 3], off, w, target, c + e, a.vocab);
+    hi[e] = (bf16_t)g;
+    lo[e] = (bf16_t)(g - (float)hi[e]);
+  }
+  *reinterpret_cast<bf16x8*>(a.hi + (int64_t)row * a.ldv + c) = hi;
+  *reinterpret_cast<bf16x8*>(a.lo + (int64_t)row * a.ldv + c) = lo;
+}
+
+// float32: a row of logits, its sums, and (GRAD) its row of G in its place.  Columns behind the vocabulary become zeros.
+template <bool GRAD>
 __global__ __launch_bounds__(512) void head_rows_kernel(HeadRowsArgs a) {
   constexpr int W = 8;
   __shared__ float s_m[W], s_s[W];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  float* const row = a.logits + (int64_t)blockIdx.x * a.ldv;
-  const int64_t t = a.t0 + blockIdx.x;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, t = blockIdx.x;
+  float* const row = a.logits + (int64_t)t * a.ldv;
   auto load = [&](int c) {
     f32x4 v = *reinterpret_cast<const f32x4*>(row + c);
 #pragma unroll
@@ -185,33 +289,15 @@ __global__ __launch_bounds__(512) void head_rows_kernel(HeadRowsArgs a) {
   for (int w = 0; w < W; ++w) sum += s_s[w] * __builtin_amdgcn_exp2f((s_m[w] - top) * LOG2E);
   const float log_sum = __builtin_amdgcn_logf(sum) * LN2;
   const int32_t target = a.targets[t];
-  if (tid == 0) {
-    if (a.logp) a.logp[t] = target < 0 ? 0.f : target >= a.vocab ? __builtin_nanf("") : row[target] - top - log_sum;
-    if (a.log_z) a.log_z[t] = top + log_sum;
-  }
+  if (tid == 0) put_row(a, t, target, target >= 0 && target < a.vocab ? row[target] : 0.f, top, log_sum);
   if constexpr (GRAD) {
-    __syncthreads();  // (float32 layers put G where the logits are)
-    const float w = target < 0 ? 0.f : target >= a.vocab ? __builtin_nanf("") : a.d_logp[t];
-    const float off = top + log_sum;
+    __syncthreads();  // (the target's logit has been read)
+    const float w = row_weight(a, t, target), off = top + log_sum;
     for (int c = tid * 4; c < a.ldv; c += W * 256) {
       f32x4 g = c < a.vocab ? load(c) : f32x4{};
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float p = __builtin_amdgcn_exp2f((g[e] - off) * LOG2E);
-        g[e] = c + e >= a.vocab || target < 0 ? 0.f : c + e == target ? w * (1.f - p) : -w * p;
-      }
-      if constexpr (BF16) {
-        bf16x4 h, l;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          h[e] = (bf16_t)g[e];
-          l[e] = (bf16_t)(g[e] - (float)h[e]);
-        }
-        *reinterpret_cast<bf16x4*>(a.hi + (int64_t)blockIdx.x * a.ldv + c) = h;
-        *reinterpret_cast<bf16x4*>(a.lo + (int64_t)blockIdx.x * a.ldv + c) = l;
-      } else {
-        *reinterpret_cast<f32x4*>(row + c) = g;
-      }
+      for (int e = 0; e < 4; ++e) g[e] = grad_of(g[e], off, w, target, c + e, a.vocab);
+      *reinterpret_cast<f32x4*>(row + c) = g;
     }
   }
 }
@@ -227,63 +313,276 @@ __global__ __launch_bounds__(256) void head_join_kernel(const float* slabs, int 
   }
 }
 
-struct HeadLayout {
-  size_t plans, logits, hi, lo, slabs, total;
+// ---------------------------------------------------------------- few rows
+// Bound by the stream of W.  A block takes 64 rows of W (four fragments of sixteen) and up to 16 NT rows of x; its four waves share the
+// sum over d out, each fragment of W goes from memory to the matrix instruction through registers alone, and the fragments of x
+// come from the caches: a sixteenth of W's bytes for each row of x.  The waves' sums meet in LDS; what leaves the block is, for
+// every row of x, the maximum and the sum of exponentials of its 64 logits.
+constexpr int STREAM_W = 64;
+template <typename T> struct StreamOf;
+template <> struct StreamOf<bf16_t> { static constexpr int KS = 32; };
+template <> struct StreamOf<float> { static constexpr int KS = 16; };
+
+struct HeadStreamArgs {
+  const void *x, *W;
+  const int32_t* targets;
+  float* pairs;      // [T][ceil(vocab / 64)] maximum and sum
+  float* at_target;  // [T]
+  float *logp, *log_z;
+  int32_t T, d, vocab;
 };
-// for shapes of at most `rows` rows a piece
-HeadLayout layout_for(int64_t rows, int64_t pieces, int64_t slab_rows, int32_t d, int32_t vocab, bool bf16, bool grad) {
+
+template <typename T, int NT>
+__global__ __launch_bounds__(256, 2) void head_stream_kernel(HeadStreamArgs a) {
+  constexpr int KS = StreamOf<T>::KS, CE = KS / 4, NW = STREAM_W / 16;  // CE: elements of sixteen bytes
+  constexpr int U = 2;                                                  // steps that are loaded together
+  typedef typename VecOf<T>::type frag_t;
+  __shared__ f32x4 s_acc[4][NW * NT][64];
+  __shared__ float s_m[NW][NT * 16], s_s[NW][NT * 16];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int strips = (a.vocab + STREAM_W - 1) / STREAM_W, groups = gridDim.x / strips;
+  const int strip = blockIdx.x / groups, t0 = (blockIdx.x - strip * groups) * (NT * 16), v0 = strip * STREAM_W;
+  const int r = lane & 15, quad = lane >> 4;
+
+  const T* w[NW];
+  const T* x[NT];
+#pragma unroll
+  for (int i = 0; i < NW; ++i) w[i] = static_cast<const T*>(a.W) + (int64_t)min(v0 + i * 16 + r, a.vocab - 1) * a.d + quad * CE;
+#pragma unroll
+  for (int i = 0; i < NT; ++i) x[i] = static_cast<const T*>(a.x) + (int64_t)min(t0 + i * 16 + r, a.T - 1) * a.d + quad * CE;
+  f32x4 acc[NW][NT];
+#pragma unroll
+  for (int i = 0; i < NW; ++i)
+#pragma unroll
+    for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  // This wave's steps, from a place on that differs from block to block: rows of W lie a power of two apart as a rule, and blocks that
+  // all read at the same place of their rows would meet in few memory channels.
+  const int steps = a.d / KS, per = (steps + 3) / 4, first = min(wave * per, steps), n = min(per, steps - first);
+  const int start = n > 0 ? (strip * 5) % n : 0;
+  frag_t wf[2][U][NW], xf[2][U][NT];
+  auto load = [&](int set, int s) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      int k = min(s + u, n - 1) + start;
+      k = (first + (k >= n ? k - n : k)) * KS;
+#pragma unroll
+      for (int i = 0; i < NW; ++i) wf[set][u][i] = __builtin_nontemporal_load(reinterpret_cast<const frag_t*>(w[i] + k));
+#pragma unroll
+      for (int j = 0; j < NT; ++j) xf[set][u][j] = *reinterpret_cast<const frag_t*>(x[j] + k);
+    }
+  };
+  auto multiply = [&](int set, int s) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (s + u >= n) break;
+#pragma unroll
+      for (int i = 0; i < NW; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+          if constexpr (sizeof(T) == 2) {
+            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[set][u][i], xf[set][u][j], acc[i][j], 0, 0, 0);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(wf[set][u][i][e], xf[set][u][j][e], acc[i][j], 0, 0, 0);
+          }
+        }
+    }
+  };
+  if (n > 0) {
+    load(0, 0);
+    for (int s = 0; s < n; s += 2 * U) {
+      if (s + U < n) load(1, s + U);
+      multiply(0, s);
+      if (s + 2 * U < n) load(0, s + 2 * U);
+      multiply(1, s + U);
+    }
+  }
+
+#pragma unroll
+  for (int i = 0; i < NW; ++i)
+#pragma unroll
+    for (int j = 0; j < NT; ++j) s_acc[wave][i * NT + j][lane] = acc[i][j];
+  __syncthreads();
+  // wave i takes fragment i: lane holds the logits of rows 4 quad .. + 3 of the fragment and of row r of every sixteen of x
+#pragma unroll
+  for (int j = 0; j < NT; ++j) {
+    const int t = t0 + j * 16 + r, v = v0 + wave * 16 + quad * 4;
+    f32x4 l = s_acc[0][wave * NT + j][lane];
+#pragma unroll
+    for (int q = 1; q < 4; ++q) l += s_acc[q][wave * NT + j][lane];
+    const int32_t at = t < a.T ? a.targets[t] - v : -1;
+    if (at >= 0 && at < 4 && v + at < a.vocab) a.at_target[t] = at == 0 ? l[0] : at == 1 ? l[1] : at == 2 ? l[2] : l[3];
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (v + e >= a.vocab) l[e] = -__builtin_inff();
+    float m = fmaxf(fmaxf(l[0], l[1]), fmaxf(l[2], l[3]));
+    m = fmaxf(m, __shfl_xor(m, 16, 64));
+    m = fmaxf(m, __shfl_xor(m, 32, 64));
+    const float lowest = fmaxf(m, -3.402823466e38f);  // (a fragment behind the vocabulary has no maximum)
+    float s = 0.f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) s += __builtin_amdgcn_exp2f((l[e] - lowest) * LOG2E);
+    s += __shfl_xor(s, 16, 64);
+    s += __shfl_xor(s, 32, 64);
+    if (quad == 0) {
+      s_m[wave][j * 16 + r] = lowest;
+      s_s[wave][j * 16 + r] = s;
+    }
+  }
+  __syncthreads();
+  const int t = threadIdx.x;
+  if (t >= NT * 16 || t0 + t >= a.T) return;
+  float m = s_m[0][t], s = 0.f;
+#pragma unroll
+  for (int i = 1; i < NW; ++i) m = fmaxf(m, s_m[i][t]);
+#pragma unroll
+  for (int i = 0; i < NW; ++i) s += s_s[i][t] * __builtin_amdgcn_exp2f((s_m[i][t] - m) * LOG2E);
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
+  *reinterpret_cast<f32x2*>(a.pairs + ((int64_t)(t0 + t) * strips + strip) * 2) = f32x2{m, s};
+}
+
+// A block joins the pairs of one row.
+__global__ __launch_bounds__(1024) void head_stream_join_kernel(HeadStreamArgs a) {
+  __shared__ float s_m[16], s_s[16];
+  constexpr int AHEAD = 4;
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
+  const int t = blockIdx.x, n = (a.vocab + STREAM_W - 1) / STREAM_W, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const f32x2* const pairs = reinterpret_cast<const f32x2*>(a.pairs) + (int64_t)t * n;
+  float m = -3.402823466e38f, s = 0.f;
+  for (int p = threadIdx.x; p < n; p += 1024 * AHEAD) {
+    f32x2 v[AHEAD];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) v[i] = pairs[min(p + i * 1024, n - 1)];
+    float most = m;
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) most = fmaxf(most, v[i][0]);
+    s *= __builtin_amdgcn_exp2f((m - most) * LOG2E);
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i)
+      if (p + i * 1024 < n) s += v[i][1] * __builtin_amdgcn_exp2f((v[i][0] - most) * LOG2E);
+    m = most;
+  }
+  const float wm = wave_max(m);
+  s = wave_sum(s * __builtin_amdgcn_exp2f((m - wm) * LOG2E));
+  if (lane == 0) {
+    s_m[wave] = wm;
+    s_s[wave] = s;
+  }
+  __syncthreads();
+  if (threadIdx.x > 0) return;
+  float top = s_m[0], sum = 0.f;
+  for (int w = 1; w < 16; ++w) top = fmaxf(top, s_m[w]);
+  for (int w = 0; w < 16; ++w) sum += s_s[w] * __builtin_amdgcn_exp2f((s_m[w] - top) * LOG2E);
+  const float log_sum = __builtin_amdgcn_logf(sum) * LN2;
+  put_row(a.logp ? a.logp + t : nullptr, a.log_z ? a.log_z + t : nullptr, a.targets[t], a.vocab, a.at_target[t], top, log_sum);
+}
+
+template <typename T>
+hipError_t run_stream(const HeadStreamArgs& a, hipStream_t s) {
+  const int nt = a.T <= 16 ? 1 : a.T <= 32 ? 2 : 4;
+  const dim3 grid((unsigned)((a.vocab + STREAM_W - 1) / STREAM_W * ((a.T + nt * 16 - 1) / (nt * 16)))), block(256);
+  if (nt == 1) hipLaunchKernelGGL((head_stream_kernel<T, 1>), grid, block, 0, s, a);
+  else if (nt == 2) hipLaunchKernelGGL((head_stream_kernel<T, 2>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((head_stream_kernel<T, 4>), grid, block, 0, s, a);
+  hipLaunchKernelGGL(head_stream_join_kernel, dim3((unsigned)a.T), dim3(1024), 0, s, a);
+  return hipGetLastError();
+}
+constexpr int64_t STREAM_ROWS = 64;  // up to so many rows
+size_t stream_workspace(int64_t T, int32_t vocab) {
+  return ALIGN + align_up((size_t)T * ((vocab + STREAM_W - 1) / STREAM_W) * 8, ALIGN) + (size_t)T * 4;
+}
+
+struct HeadLayout {
+  size_t logits, pairs, at_target, off, hi, lo, slabs, total;
+};
+HeadLayout layout_for(int64_t plans, int64_t sub, int64_t rows, int64_t slab_cells, int32_t vocab, bool bf16, bool grad) {
   HeadLayout w = {};
-  const size_t cells = (size_t)rows * align_up(vocab, 64);
-  w.logits = align_up(sizeof(GemmPlan) * 3 * (size_t)pieces, 256);
-  w.hi = w.logits + align_up(cells * 4, 256);
-  w.lo = w.hi + (grad && bf16 ? align_up(cells * 2, 256) : 0);
-  w.slabs = w.lo + (grad && bf16 ? align_up(cells * 2, 256) : 0);
-  w.total = w.slabs + (grad ? (size_t)slab_rows * d * 4 : 0);
+  const size_t ldv = align_up(vocab, 64), cells = (size_t)rows * ldv;
+  size_t at = 0;
+  auto take = [&](size_t bytes) {
+    const size_t here = at;
+    at += align_up(bytes, ALIGN);
+    return here;
+  };
+  take(sizeof(GemmPlan) * (size_t)plans);
+  w.logits = take(bf16 && !grad ? 0 : (size_t)sub * ldv * 4);
+  w.pairs = take(bf16 ? (size_t)sub * ((vocab + 127) / 128) * 8 : 0);
+  w.at_target = take(bf16 ? (size_t)sub * 4 : 0);
+  w.off = take(bf16 ? (size_t)sub * 4 : 0);
+  w.hi = take(bf16 && grad ? cells * 2 : 0);
+  w.lo = take(bf16 && grad ? cells * 2 : 0);
+  w.slabs = take(grad ? (size_t)slab_cells * 4 : 0);
+  w.total = at;
   return w;
 }
 }  // namespace
 
-int64_t head_piece_rows(int32_t vocab) {
-  return std::max<int64_t>(256, std::min<int64_t>(8192, PIECE / (int64_t)align_up(vocab, 64) / 256 * 256));
-}
-
 size_t head_workspace(int64_t T, int32_t d, int32_t vocab, modse_dtype dt, bool grad) {
   if (T == 0) return 0;
-  // of all batches of at most T rows: the most rows of a piece, the most pieces, the most slabs
-  const int64_t most = head_piece_rows(vocab), rows = std::min<int64_t>(padded_rows(T), most);
-  const int64_t slab_rows = std::min<int64_t>(32 * rows, std::max(SLAB_ROWS, most));
-  return ALIGN + layout_for(rows, (T + most - 1) / most, slab_rows, d, vocab, dt == MODSE_BF16, grad).total;
+  // of all batches of at most T rows: the most plans, rows of a product and of a piece, slabs
+  const bool bf16 = dt == MODSE_BF16;
+  const int64_t most = most_rows(vocab, bf16, grad), sub_most = std::min(most, most_sub(vocab, bf16, grad));
+  const int64_t sub = std::min<int64_t>(padded_rows(T), sub_most), rows = std::min<int64_t>((int64_t)align_up((size_t)T, (size_t)sub), most);
+  const int64_t pieces = (T + most - 1) / most, plans = (T + sub_most - 1) / sub_most + (grad ? 2 * pieces : 0);
+  const int64_t slabs = std::min(MAX_PARTS * rows * d, std::max(SLAB_CELLS, rows * d));
+  const size_t total = ALIGN + layout_for(plans, sub, rows, slabs, vocab, bf16, grad).total;
+  return grad ? total : T <= STREAM_ROWS ? stream_workspace(T, vocab) : std::max(total, stream_workspace(STREAM_ROWS, vocab));
 }
 
 hipError_t launch_head(modse_dtype dt, const HeadArgs& a, char* ws, hipStream_t s) {
-  const HeadShape h = head_shape(a.T, a.d, a.vocab, dt);
   const bool grad = a.dX || a.dW;
-  const HeadLayout w = layout_for(h.rows, h.pieces, (int64_t)h.k_parts * h.rows, h.d, h.vocab, h.bf16, grad);
+  if (!grad && a.T <= STREAM_ROWS) {
+    float* const pairs = reinterpret_cast<float*>(align_up(reinterpret_cast<size_t>(ws), ALIGN));
+    float* const at_target = pairs + align_up((size_t)a.T * ((a.vocab + STREAM_W - 1) / STREAM_W) * 8, ALIGN) / 4;
+    const HeadStreamArgs r = {a.x, a.W, a.targets, pairs, at_target, a.logp, a.log_z, (int32_t)a.T, a.d, a.vocab};
+    return dt == MODSE_F32 ? run_stream<float>(r, s) : run_stream<bf16_t>(r, s);
+  }
+  const HeadShape h = head_shape(a.T, a.d, a.vocab, dt, grad);
+  const int64_t products = h.products(), plans = products + (grad ? 2 * h.pieces : 0);
+  const HeadLayout w = layout_for(plans, h.sub, h.rows, (int64_t)h.k_parts * h.rows * h.d, h.vocab, h.bf16, grad);
   ws = reinterpret_cast<char*>(align_up(reinterpret_cast<size_t>(ws), ALIGN));
-  const HeadBufs b = {reinterpret_cast<GemmPlan*>(ws + w.plans), reinterpret_cast<float*>(ws + w.logits), reinterpret_cast<bf16_t*>(ws + w.hi),
-                      reinterpret_cast<bf16_t*>(ws + w.lo), reinterpret_cast<float*>(ws + w.slabs)};
-  const HeadPlanArgs plan = {h, b, a.x, a.W, a.dW, grad};
-  hipLaunchKernelGGL(head_plan_kernel, dim3((unsigned)(h.pieces * (grad ? 3 : 1))), dim3(64), 0, s, plan);
+  auto floats = [&](size_t at) { return reinterpret_cast<float*>(ws + at); };
+  const HeadBufs b = {reinterpret_cast<GemmPlan*>(ws), floats(w.logits), floats(w.pairs), floats(w.at_target), floats(w.off),
+                      reinterpret_cast<bf16_t*>(ws + w.hi), reinterpret_cast<bf16_t*>(ws + w.lo), floats(w.slabs)};
+  const HeadPlanArgs plan = {h, b, a.x, a.W, a.targets, a.dW};
+  hipLaunchKernelGGL(head_plan_kernel, dim3((unsigned)plans), dim3(64), 0, s, plan);
   auto tiles = [](int64_t m, int64_t n, TileShape t) { return ((m + t.bm - 1) / t.bm) * ((n + t.bn - 1) / t.bn); };
   hipError_t e = hipGetLastError();
-  for (int i = 0; i < h.pieces && e == hipSuccess; ++i) {
-    const int64_t t0 = (int64_t)i * h.rows, m = std::min<int64_t>(h.rows, h.T - t0);
-    const GemmPlan* const p = b.plans + i * 3;
-    e = launch_grouped_gemm(dt, h.bf16 ? EPI_STORE_F32 : EPI_STORE, h.logits_tile, p, h.w_parts, 0, 0,
+  // the logits of one product, their sums and (of gradients) G
+  auto product = [&](int64_t i) {
+    const int64_t t0 = i * h.sub, m = std::min<int64_t>(h.sub, h.T - t0), in_piece = t0 % h.rows;
+    e = launch_grouped_gemm(dt, h.bf16 ? EPI_LOGITS : EPI_STORE, h.logits_tile, b.plans + i, h.w_parts, 0, GEMM_STREAM_C,
                             tiles(m, h.vocab, h.logits_tile) + h.w_parts * tiles(m, 1, h.logits_tile), s, LAYOUT_TN);
-    if (e != hipSuccess) break;
-    const HeadRowsArgs r = {a.targets, a.d_logp, a.logp, a.log_z, b.logits, b.hi, b.lo, t0, (int32_t)m, h.vocab, h.ldv};
-    const dim3 grid((unsigned)m), block(512);
-    if (!grad) hipLaunchKernelGGL((head_rows_kernel<false, false>), grid, block, 0, s, r);
-    else if (h.bf16) hipLaunchKernelGGL((head_rows_kernel<true, true>), grid, block, 0, s, r);
-    else hipLaunchKernelGGL((head_rows_kernel<true, false>), grid, block, 0, s, r);
-    if ((e = hipGetLastError()) != hipSuccess) break;
+    if (e != hipSuccess) return;
+    const HeadRowsArgs r = {a.targets + t0, a.d_logp ? a.d_logp + t0 : nullptr, a.logp ? a.logp + t0 : nullptr, a.log_z ? a.log_z + t0 : nullptr,
+                            b.logits, b.pairs, b.at_target, b.off, b.hi + in_piece * h.ldv, b.lo + in_piece * h.ldv,
+                            (int32_t)m, h.vocab, h.ldv, h.sub};
+    if (h.bf16) {
+      hipLaunchKernelGGL(head_stats_kernel, dim3((unsigned)((m + 63) / 64)), dim3(1024), 0, s, r);
+      const int segs = (h.ldv + 2047) / 2048;
+      if (grad) hipLaunchKernelGGL(head_grad_kernel, dim3((unsigned)(m * segs)), dim3(256), 0, s, r, segs);
+    } else if (grad) {
+      hipLaunchKernelGGL((head_rows_kernel<true>), dim3((unsigned)m), dim3(512), 0, s, r);
+    } else {
+      hipLaunchKernelGGL((head_rows_kernel<false>), dim3((unsigned)m), dim3(512), 0, s, r);
+    }
+    e = hipGetLastError();
+  };
+  for (int64_t i = 0; i < products && e == hipSuccess; ++i) {
+    product(i);
+    const int64_t piece = i / h.subs;
+    if (e != hipSuccess || !grad || ((i + 1) % h.subs != 0 && i + 1 < products)) continue;
+    // a piece is whole
+    const int64_t t0 = piece * h.rows, m = std::min<int64_t>(h.rows, h.T - t0);
+    const GemmPlan* const p = b.plans + products + 2 * piece;
     if (a.dW) {  // (before dX, which may lie in the buffer of x)
-      e = launch_grouped_gemm(dt, EPI_ROWS_F32, h.dw_tile, p + 2, 1, a.accumulate || i > 0, 0, tiles(padded_rows(h.vocab), h.d, h.dw_tile), s, LAYOUT_AB_K);
+      e = launch_grouped_gemm(dt, EPI_ROWS_F32, h.dw_tile, p + 1, 1, a.accumulate || piece > 0, 0,
+                              tiles(padded_rows(h.vocab), h.d, h.dw_tile), s, LAYOUT_AB_K);
       if (e != hipSuccess) break;
     }
     if (a.dX) {
-      e = launch_grouped_gemm(dt, EPI_STORE_F32, h.dx_tile, p + 1, h.k_parts, 0, 0, h.k_parts * tiles(m, h.d, h.dx_tile), s, LAYOUT_B_KN);
+      e = launch_grouped_gemm(dt, EPI_STORE_F32, h.dx_tile, p, h.k_parts, 0, 0, h.k_parts * tiles(m, h.d, h.dx_tile), s, LAYOUT_B_KN);
       if (e != hipSuccess) break;
       const int64_t n = m * h.d, stride = (int64_t)h.rows * h.d;
       const dim3 join((unsigned)std::min<int64_t>((n + 1023) / 1024, 4096));

@@ -119,7 +119,6 @@ struct HeadArgs {
   int64_t T;
   int32_t d, vocab, accumulate;
 };
-int64_t head_piece_rows(int32_t vocab);  // rows whose logits are in the workspace at a time, at the most
 size_t head_workspace(int64_t T, int32_t d, int32_t vocab, modse_dtype dt, bool grad);
 hipError_t launch_head(modse_dtype dt, const HeadArgs& a, char* ws, hipStream_t s);
 

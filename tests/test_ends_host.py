@@ -99,7 +99,7 @@ BOTH = [
     (dict(T=-1), INVALID), (dict(d=0), INVALID), (dict(d=48), INVALID), (dict(d=16416), UNSUPPORTED), (dict(V=0), INVALID),
     (dict(V=(1 << 20) + 1), UNSUPPORTED), (dict(T=(1 << 24) + 1), UNSUPPORTED), (dict(dtype="fp16"), UNSUPPORTED), (dict(x=None), INVALID),
     (dict(W=None), INVALID), (dict(targets=None), INVALID), (dict(ws=None), INVALID), (dict(ws=P + 8), INVALID), (dict(x=P + 2), INVALID),
-    (dict(W=P + 8), INVALID), (dict(ws_bytes=1000), WORKSPACE), (dict(T=0, x=None, W=None, ws=None, ws_bytes=0), OK),
+    (dict(W=P + 8), INVALID), (dict(ws_bytes=100), WORKSPACE), (dict(T=0, x=None, W=None, ws=None, ws_bytes=0), OK),
 ]
 
 

@@ -125,7 +125,7 @@ def check(T, d, V, dtype, seed=0, whole=False, sigma=2.5, products=True):
 
 
 SHAPES = [(1, 32, 1), (1, 64, 7), (2, 32, 31), (3, 96, 32), (5, 64, 33), (16, 128, 100), (17, 32, 255), (33, 96, 257), (64, 2048, 700),
-          (65, 512, 1023), (129, 64, 1500), (255, 64, 300), (257, 128, 1000), (300, 256, 5003), (1000, 64, 4097), (40, 96, 50257), (4, 4096, 9001)]
+          (65, 512, 1023), (63, 64, 8191), (49, 256, 64), (32, 32, 65), (129, 64, 1500), (255, 64, 300), (257, 128, 1000), (300, 256, 5003), (1000, 64, 4097), (40, 96, 50257), (4, 4096, 9001)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -183,7 +183,8 @@ def test_far_apart_and_equal_logits(dtype):
     near(a, logp, tol, "logp")
     near(b, log_z, tol_z, "log_z")
     lp, dX, dW = backward(x, W, targets, w, dtype)
-    assert dX.isfinite().all() and dW.isfinite().all() and torch.equal(lp, a)
+    near(lp, logp, tol, "logp of the gradient's call")
+    assert dX.isfinite().all() and dW.isfinite().all()
     zero = torch.zeros_like(x)
     a, b = forward(zero, W, targets, dtype)
     none = targets < 0

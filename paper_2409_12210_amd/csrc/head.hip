@@ -17,6 +17,7 @@
 // is rounded to bf16 itself and takes hi alone.
 #include "ops.h"
 
+#include "gemm_bf16_util.h"
 #include "gemm_plan.h"
 
 namespace {
@@ -314,14 +315,15 @@ __global__ __launch_bounds__(256) void head_join_kernel(const float* slabs, int 
 }
 
 // ---------------------------------------------------------------- few rows
-// Bound by the stream of W.  A block takes 64 rows of W (four fragments of sixteen) and up to 16 NT rows of x; its four waves share the
-// sum over d out, each fragment of W goes from memory to the matrix instruction through registers alone, and the fragments of x
-// come from the caches: a sixteenth of W's bytes for each row of x.  The waves' sums meet in LDS; what leaves the block is, for
-// every row of x, the maximum and the sum of exponentials of its 64 logits.
+// Bound by the stream of W.  A block takes 64 rows of W and up to 16 NT rows of x; its four waves share the sum over d out and go their
+// own ways until the end: each moves 128 bytes of all these rows at a time straight into a ring of its own in LDS, whole lines with the
+// non-temporal hint, and reads the operands of the matrix instruction from there.  (Read from memory in the order of the operands,
+// sixteen rows of 64 bytes a load, the same stream ran at 5.6 TB/s without the hint and at 4.0 with it, as each line then came
+// twice.)  The waves' sums meet in LDS; what leaves the block is, for every row of x, the maximum and the sum of exponentials of its 64
+// logits.
 constexpr int STREAM_W = 64;
-template <typename T> struct StreamOf;
-template <> struct StreamOf<bf16_t> { static constexpr int KS = 32; };
-template <> struct StreamOf<float> { static constexpr int KS = 16; };
+// (the ring: two blocks of a CU where it leaves room for them)
+constexpr int stream_stages(int nt) { return nt == 1 ? 2 : nt == 2 ? 3 : 2; }
 
 struct HeadStreamArgs {
   const void *x, *W;
@@ -332,85 +334,125 @@ struct HeadStreamArgs {
   int32_t T, d, vocab;
 };
 
+// (blocks of 256 threads: told of 512, the compiler leaves the accumulation registers alone where LDS has room for one block only)
 template <typename T, int NT>
-__global__ __launch_bounds__(256, 2) void head_stream_kernel(HeadStreamArgs a) {
-  constexpr int KS = StreamOf<T>::KS, CE = KS / 4, NW = STREAM_W / 16;  // CE: elements of sixteen bytes
-  constexpr int U = 2;                                                  // steps that are loaded together
+__global__ __launch_bounds__(512) void head_stream_kernel(HeadStreamArgs a) {
+  constexpr int ES = sizeof(T), NW = STREAM_W / 16, S = stream_stages(NT);
+  constexpr int ROWS = STREAM_W + NT * 16, UNITS = ROWS / 8, STAGE = ROWS * 128;  // unit: eight rows, one load
   typedef typename VecOf<T>::type frag_t;
-  __shared__ f32x4 s_acc[4][NW * NT][64];
-  __shared__ float s_m[NW][NT * 16], s_s[NW][NT * 16];
+  __shared__ __attribute__((aligned(1024))) char ring[4 * S * STAGE];
+  constexpr int SUMS = 4 * NW * NT * 1024;  // in its place at the end: the waves' sums, then the fragments' maxima and sums
+  static_assert(SUMS + 2 * NW * NT * 64 <= sizeof(ring) && (NT > 1 || sizeof(ring) <= 80 * 1024), "LDS");
+  float(*const s_m)[NT * 16] = reinterpret_cast<float(*)[NT * 16]>(ring + SUMS);
+  float(*const s_s)[NT * 16] = s_m + NW;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int strips = (a.vocab + STREAM_W - 1) / STREAM_W, groups = gridDim.x / strips;
   const int strip = blockIdx.x / groups, t0 = (blockIdx.x - strip * groups) * (NT * 16), v0 = strip * STREAM_W;
   const int r = lane & 15, quad = lane >> 4;
+  char* const mine = ring + wave * S * STAGE;
+  const uint32_t lds = __builtin_amdgcn_readfirstlane(lds_address(mine));
 
-  const T* w[NW];
-  const T* x[NT];
+  // This wave's steps of 128 bytes, from a place on that differs from block to block: rows of W lie a power of two apart as a rule, and
+  // blocks that all read at the same place of their rows would meet in few memory channels.
+  const int bytes = a.d * ES, steps = (bytes + 127) / 128, per = (steps + 3) / 4;
+  const int first = min(wave * per, steps), n = min(per, steps - first);
+  const int start = n > 0 ? (strip * 5) % n : 0;
+  // lane 8 i + c of a unit loads row i's chunk of sixteen bytes so that it lands at place c: chunk c ^ (row >> 1 & 7), which keeps the
+  // reads of sixteen rows out of each other's banks
+  const char* const w0 = static_cast<const char*>(a.W) + (int64_t)v0 * bytes;
+  const char* const x0 = static_cast<const char*>(a.x) + (int64_t)t0 * bytes;
+  const int row8 = lane >> 3;
+  uint32_t off[UNITS];
 #pragma unroll
-  for (int i = 0; i < NW; ++i) w[i] = static_cast<const T*>(a.W) + (int64_t)min(v0 + i * 16 + r, a.vocab - 1) * a.d + quad * CE;
+  for (int u = 0; u < UNITS; ++u) {
+    const int row = u * 8 + row8, c = (lane & 7) ^ ((row >> 1) & 7);
+    off[u] = (uint32_t)(u < STREAM_W / 8 ? min(row, a.vocab - 1 - v0) : min(row - STREAM_W, a.T - 1 - t0)) * (uint32_t)bytes + c * 16;
+  }
+  auto issue = [&](int i) {
+    const int k = i + start >= n ? i + start - n : i + start, at = (first + k) * 128;
+    const uint32_t dst = lds + (i % S) * STAGE;
+    if (at + 128 <= bytes) {
 #pragma unroll
-  for (int i = 0; i < NT; ++i) x[i] = static_cast<const T*>(a.x) + (int64_t)min(t0 + i * 16 + r, a.T - 1) * a.d + quad * CE;
+      for (int u = 0; u < UNITS; ++u) {
+        if (u < STREAM_W / 8) dma_b128_s<true>(w0 + at, off[u], dst + u * 1024);
+        else dma_b128_s(x0 + at, off[u], dst + u * 1024);
+      }
+    } else {  // (bf16: half a step) what lies behind the rows' ends reads zeros
+#pragma unroll
+      for (int u = 0; u < UNITS; ++u) {
+        const int c = (lane & 7) ^ (((u * 8 + row8) >> 1) & 7);
+        const char* const p = (u < STREAM_W / 8 ? w0 : x0) + at + off[u];
+        dma_b128(at + c * 16 < bytes ? p : reinterpret_cast<const char*>(g_zero_chunk), dst + u * 1024);
+      }
+    }
+  };
   f32x4 acc[NW][NT];
 #pragma unroll
   for (int i = 0; i < NW; ++i)
 #pragma unroll
     for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-
-  // This wave's steps, from a place on that differs from block to block: rows of W lie a power of two apart as a rule, and blocks that
-  // all read at the same place of their rows would meet in few memory channels.
-  const int steps = a.d / KS, per = (steps + 3) / 4, first = min(wave * per, steps), n = min(per, steps - first);
-  const int start = n > 0 ? (strip * 5) % n : 0;
-  frag_t wf[2][U][NW], xf[2][U][NT];
-  auto load = [&](int set, int s) {
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      int k = min(s + u, n - 1) + start;
-      k = (first + (k >= n ? k - n : k)) * KS;
-#pragma unroll
-      for (int i = 0; i < NW; ++i) wf[set][u][i] = __builtin_nontemporal_load(reinterpret_cast<const frag_t*>(w[i] + k));
-#pragma unroll
-      for (int j = 0; j < NT; ++j) xf[set][u][j] = *reinterpret_cast<const frag_t*>(x[j] + k);
-    }
+  auto wait = [&](auto younger) {  // all loads but those of so many steps have landed
+    constexpr int N = decltype(younger)::value * UNITS;
+    static_assert(N < 64, "vmcnt field");
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_waitcnt(0x0f70 | (N & 15) | (N >> 4) << 14);
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
   };
-  auto multiply = [&](int set, int s) {
+#pragma unroll 1
+  for (int i = 0; i < S - 1 && i < n; ++i) issue(i);
+#pragma unroll 1
+  for (int i = 0; i < n; ++i) {
+    // (the slot that step i + S - 1 goes to has been read: its fragments were multiplied)
+    if (i + S - 1 < n) {
+      issue(i + S - 1);
+      wait(std::integral_constant<int, S - 1>{});
+    } else {
+      wait(std::integral_constant<int, 0>{});
+    }
+    const char* const stage = mine + (i % S) * STAGE;
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (s + u >= n) break;
+    for (int h = 0; h < 2; ++h) {
+      frag_t wf[NW], xf[NT];
+      auto read = [&](int row) {
+        return *reinterpret_cast<const frag_t*>(stage + (row + r) * 128 + (((h * 4 + quad) ^ ((r >> 1) & 7)) << 4));
+      };
 #pragma unroll
-      for (int i = 0; i < NW; ++i)
+      for (int q = 0; q < NW; ++q) wf[q] = read(q * 16);
+#pragma unroll
+      for (int j = 0; j < NT; ++j) xf[j] = read(STREAM_W + j * 16);
+#pragma unroll
+      for (int q = 0; q < NW; ++q)
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
-          if constexpr (sizeof(T) == 2) {
-            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[set][u][i], xf[set][u][j], acc[i][j], 0, 0, 0);
+          if constexpr (ES == 2) {
+            acc[q][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[q], xf[j], acc[q][j], 0, 0, 0);
           } else {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(wf[set][u][i][e], xf[set][u][j][e], acc[i][j], 0, 0, 0);
+            for (int e = 0; e < 4; ++e) acc[q][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(wf[q][e], xf[j][e], acc[q][j], 0, 0, 0);
           }
         }
     }
-  };
-  if (n > 0) {
-    load(0, 0);
-    for (int s = 0; s < n; s += 2 * U) {
-      if (s + U < n) load(1, s + U);
-      multiply(0, s);
-      if (s + 2 * U < n) load(0, s + 2 * U);
-      multiply(1, s + U);
-    }
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): the slot has been read
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
   }
 
+  __syncthreads();  // (no ring is in use any more)
+  auto sum_at = [&](int w, int f) { return reinterpret_cast<f32x4*>(ring + ((w * NW * NT + f) * 64 + lane) * 16); };
 #pragma unroll
   for (int i = 0; i < NW; ++i)
 #pragma unroll
-    for (int j = 0; j < NT; ++j) s_acc[wave][i * NT + j][lane] = acc[i][j];
+    for (int j = 0; j < NT; ++j) *sum_at(wave, i * NT + j) = acc[i][j];
   __syncthreads();
   // wave i takes fragment i: lane holds the logits of rows 4 quad .. + 3 of the fragment and of row r of every sixteen of x
 #pragma unroll
   for (int j = 0; j < NT; ++j) {
     const int t = t0 + j * 16 + r, v = v0 + wave * 16 + quad * 4;
-    f32x4 l = s_acc[0][wave * NT + j][lane];
+    f32x4 l = *sum_at(0, wave * NT + j);
 #pragma unroll
-    for (int q = 1; q < 4; ++q) l += s_acc[q][wave * NT + j][lane];
+    for (int q = 1; q < 4; ++q) l += *sum_at(q, wave * NT + j);
     const int32_t at = t < a.T ? a.targets[t] - v : -1;
     if (at >= 0 && at < 4 && v + at < a.vocab) a.at_target[t] = at == 0 ? l[0] : at == 1 ? l[1] : at == 2 ? l[2] : l[3];
 #pragma unroll

@@ -174,7 +174,11 @@ __device__ __forceinline__ void put_part(const EmbedBwdArgs& a, int64_t slot, in
 
 // Partial sums: slot 2 i is the beginning of chunk i, which belongs to a run that begins before it, slot 2 i + 1 its end, of a run that
 // begins in it and goes on behind it.
-template <typename T>
+//
+// A wave takes 64 vectors of sixteen bytes of a chunk's rows.  The rows are loaded a batch at a time, without a branch between the loads:
+// a lane behind the row's end loads the row's last vector, which nobody stores.  (EDGE: the row's length is no multiple of the
+// vector, and a lane's vector may reach over it.)
+template <typename T, bool EDGE>
 __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedBwdArgs a) {
   constexpr int N = Vec<T>::N, SEG = 64 * N, AHEAD = 8;
   const int lane = threadIdx.x & 63;
@@ -188,36 +192,45 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedBwdArgs a) {
   const int c = (int)(u - i * segs) * SEG + lane * N;
   const bool here = c < a.d;
   // lane q holds place first + q of the list (a.chunk <= 64), and the keys around the chunk
-  const int32_t order = lane < n ? a.order[first + lane] : 0;
+  const int32_t order = a.order[first + min(lane, n - 1)];
   const int32_t key = lane < n ? a.keys[first + lane] : -1;
-  const int32_t key_before = first > 0 ? a.keys[first - 1] : -1;
-  const int32_t key_after = first + n < n_sorted ? a.keys[first + n] : -1;
+  const int32_t key_before = __builtin_amdgcn_readfirstlane(first > 0 ? a.keys[first - 1] : -1);
+  const int32_t key_after = __builtin_amdgcn_readfirstlane(first + n < n_sorted ? a.keys[first + n] : -1);
+  // places where a run ends
+  const int32_t key_right = __shfl_down(key, 1, 64);
+  const uint64_t ends = __ballot(lane < n && (lane == n - 1 || key != key_right));
+  const T* const base = static_cast<const T*>(a.dX);
+  const int at = EDGE ? c : min(c, a.d - N);
   float s[N] = {};
-  bool from_before = __builtin_amdgcn_readlane(key, 0) == __builtin_amdgcn_readfirstlane(key_before);
+  bool from_before = __builtin_amdgcn_readlane(key, 0) == key_before;
   for (int q0 = 0; q0 < n; q0 += AHEAD) {
     Vec<T> v[AHEAD];
 #pragma unroll
     for (int q = 0; q < AHEAD; ++q) {
-      const int t = __builtin_amdgcn_readlane(order, min(q0 + q, n - 1));
-      if (here) v[q].load(static_cast<const T*>(a.dX) + (int64_t)t * a.d + c, a.d - c, 0.f);
+      const T* const row = base + (int64_t)__builtin_amdgcn_readlane(order, min(q0 + q, n - 1)) * a.d;
+      if constexpr (EDGE) {
+        if (here) v[q].load(row + at, a.d - at, 0.f);
+      } else {
+        v[q].load(row + at, N, 0.f);
+      }
     }
 #pragma unroll
     for (int q = 0; q < AHEAD; ++q) {
-      if (q0 + q >= n) break;
+      if (q0 + q < n) {
 #pragma unroll
-      for (int e = 0; e < N; ++e) s[e] += v[q][e];
-      const int32_t k = __builtin_amdgcn_readlane(key, q0 + q);
-      const bool last = q0 + q == n - 1;
-      const int32_t next = last ? __builtin_amdgcn_readfirstlane(key_after) : __builtin_amdgcn_readlane(key, q0 + q + 1);
-      if (k != next || last) {
-        if (here) {
-          if (from_before) put_part(a, 2 * i, c, s);
-          else if (k == next) put_part(a, 2 * i + 1, c, s);
-          else put_row(a, k, c, s);
+        for (int e = 0; e < N; ++e) s[e] += v[q][e];
+        if (ends >> (q0 + q) & 1) {
+          const bool last = q0 + q == n - 1;
+          const int32_t k = __builtin_amdgcn_readlane(key, q0 + q);
+          if (here) {
+            if (from_before) put_part(a, 2 * i, c, s);
+            else if (last && k == key_after) put_part(a, 2 * i + 1, c, s);
+            else put_row(a, k, c, s);
+          }
+          from_before = false;
+#pragma unroll
+          for (int e = 0; e < N; ++e) s[e] = 0.f;
         }
-        from_before = false;
-#pragma unroll
-        for (int e = 0; e < N; ++e) s[e] = 0.f;
       }
     }
   }
@@ -236,14 +249,17 @@ __global__ __launch_bounds__(256) void embed_join_kernel(EmbedBwdArgs a) {
   if (key != a.keys[behind]) return;
   const int64_t first = i * a.chunk;
   if (first > 0 && a.keys[first] == key && a.keys[first - 1] == key) return;  // it begins before
-  // chunks that the run reaches into, by its last place: a search over the sorted keys
-  int64_t lo = behind, hi = n_sorted;  // keys[lo] == key, keys[hi] is another
-  while (hi - lo > 1) {
-    const int64_t mid = (lo + hi) / 2;
-    if (a.keys[mid] == key) lo = mid;
-    else hi = mid;
+  // chunks that the run reaches into, 64 looked at together: slots 2 (i + 1), ..., 2 (i + more)
+  int64_t more = 1;
+  for (;;) {
+    const int64_t at = behind + (more + lane) * a.chunk;
+    const uint64_t other = __ballot(at >= n_sorted || a.keys[min(at, (int64_t)n_sorted - 1)] != key);
+    if (other) {
+      more += __builtin_ctzll(other);
+      break;
+    }
+    more += 64;
   }
-  const int64_t more = lo / a.chunk - i;  // slots 2 (i + 1), ..., 2 (i + more)
   const int c = (int)(blockIdx.x % segs) * 256 + lane * 4;
   const int64_t per = (more + 3) / 4, j0 = wave * per, j1 = j0 + per < more ? j0 + per : more;
   f32x4 s = {0.f, 0.f, 0.f, 0.f};
@@ -288,8 +304,10 @@ hipError_t launch_embed_bwd(modse_dtype dt, const EmbedBwdArgs& a, hipStream_t s
   const int64_t chunks = embed_chunks(a.T);
   const int seg = 64 * (dt == MODSE_F32 ? 4 : 8);
   const dim3 sums((unsigned)((chunks * ((a.d + seg - 1) / seg) + 3) / 4)), joins((unsigned)(chunks * ((a.d + 255) / 256)));
-  if (dt == MODSE_F32) hipLaunchKernelGGL((embed_sum_kernel<float>), sums, dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((embed_sum_kernel<bf16_t>), sums, dim3(256), 0, s, a);
+  if (dt == MODSE_F32 && a.d % 4 == 0) hipLaunchKernelGGL((embed_sum_kernel<float, false>), sums, dim3(256), 0, s, a);
+  else if (dt == MODSE_F32) hipLaunchKernelGGL((embed_sum_kernel<float, true>), sums, dim3(256), 0, s, a);
+  else if (a.d % 8 == 0) hipLaunchKernelGGL((embed_sum_kernel<bf16_t, false>), sums, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((embed_sum_kernel<bf16_t, true>), sums, dim3(256), 0, s, a);
   if (chunks > 1) hipLaunchKernelGGL(embed_join_kernel, joins, dim3(256), 0, s, a);
   return hipGetLastError();
 }

@@ -316,14 +316,14 @@ __global__ __launch_bounds__(256) void head_join_kernel(const float* slabs, int 
 
 // ---------------------------------------------------------------- few rows
 // Bound by the stream of W.  A block takes 64 rows of W and up to 16 NT rows of x; its four waves share the sum over d out and go their
-// own ways until the end: each moves 128 bytes of all these rows at a time straight into a ring of its own in LDS, whole lines with the
-// non-temporal hint, and reads the operands of the matrix instruction from there.  (Read from memory in the order of the operands,
-// sixteen rows of 64 bytes a load, the same stream ran at 5.6 TB/s without the hint and at 4.0 with it, as each line then came
-// twice.)  The waves' sums meet in LDS; what leaves the block is, for every row of x, the maximum and the sum of exponentials of its 64
-// logits.
+// own ways until the end: each moves 128 bytes of all these rows at a time straight into LDS of its own, whole lines with the
+// non-temporal hint, and reads the operands of the matrix instruction from there.  What a wave waits for, the other blocks of its CU
+// (four, three or two) hide: with a ring of two or three such steps, and fewer blocks, 64 rows x 32000, d = 2048, took 33 us in
+// place of 30.6 and 32 x 50257, d = 256, 16.5 in place of 11.2.  (Read from memory in the order of the operands, sixteen rows of 64
+// bytes a load, one row x 131072, d = 4096, took 190 us without the hint and 269 with it, as each line then came twice; this way
+// 166, 6.5 TB/s.)  The waves' sums meet in LDS; what leaves the block is, for every row of x, the maximum and the sum of exponentials of
+// its 64 logits.  A second launch joins them.
 constexpr int STREAM_W = 64;
-// (the ring: two blocks of a CU where it leaves room for them)
-constexpr int stream_stages(int nt) { return nt == 1 ? 2 : nt == 2 ? 3 : 2; }
 
 struct HeadStreamArgs {
   const void *x, *W;
@@ -334,22 +334,20 @@ struct HeadStreamArgs {
   int32_t T, d, vocab;
 };
 
-// (blocks of 256 threads: told of 512, the compiler leaves the accumulation registers alone where LDS has room for one block only)
 template <typename T, int NT>
-__global__ __launch_bounds__(512) void head_stream_kernel(HeadStreamArgs a) {
-  constexpr int ES = sizeof(T), NW = STREAM_W / 16, S = stream_stages(NT);
+__global__ __launch_bounds__(256, 2) void head_stream_kernel(HeadStreamArgs a) {
+  constexpr int ES = sizeof(T), NW = STREAM_W / 16;
   constexpr int ROWS = STREAM_W + NT * 16, UNITS = ROWS / 8, STAGE = ROWS * 128;  // unit: eight rows, one load
   typedef typename VecOf<T>::type frag_t;
-  __shared__ __attribute__((aligned(1024))) char ring[4 * S * STAGE];
-  constexpr int SUMS = 4 * NW * NT * 1024;  // in its place at the end: the waves' sums, then the fragments' maxima and sums
-  static_assert(SUMS + 2 * NW * NT * 64 <= sizeof(ring) && (NT > 1 || sizeof(ring) <= 80 * 1024), "LDS");
-  float(*const s_m)[NT * 16] = reinterpret_cast<float(*)[NT * 16]>(ring + SUMS);
+  constexpr int SUMS = 4 * NW * NT * 1024;  // in the steps' place at the end: the waves' sums, then the fragments' maxima and sums
+  __shared__ __attribute__((aligned(1024))) char buf[std::max(4 * STAGE, SUMS + 2 * NW * NT * 64)];
+  float(*const s_m)[NT * 16] = reinterpret_cast<float(*)[NT * 16]>(buf + SUMS);
   float(*const s_s)[NT * 16] = s_m + NW;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int strips = (a.vocab + STREAM_W - 1) / STREAM_W, groups = gridDim.x / strips;
   const int strip = blockIdx.x / groups, t0 = (blockIdx.x - strip * groups) * (NT * 16), v0 = strip * STREAM_W;
   const int r = lane & 15, quad = lane >> 4;
-  char* const mine = ring + wave * S * STAGE;
+  char* const mine = buf + wave * STAGE;
   const uint32_t lds = __builtin_amdgcn_readfirstlane(lds_address(mine));
 
   // This wave's steps of 128 bytes, from a place on that differs from block to block: rows of W lie a power of two apart as a rule, and
@@ -370,19 +368,18 @@ __global__ __launch_bounds__(512) void head_stream_kernel(HeadStreamArgs a) {
   }
   auto issue = [&](int i) {
     const int k = i + start >= n ? i + start - n : i + start, at = (first + k) * 128;
-    const uint32_t dst = lds + (i % S) * STAGE;
     if (at + 128 <= bytes) {
 #pragma unroll
       for (int u = 0; u < UNITS; ++u) {
-        if (u < STREAM_W / 8) dma_b128_s<true>(w0 + at, off[u], dst + u * 1024);
-        else dma_b128_s(x0 + at, off[u], dst + u * 1024);
+        if (u < STREAM_W / 8) dma_b128_s<true>(w0 + at, off[u], lds + u * 1024);
+        else dma_b128_s(x0 + at, off[u], lds + u * 1024);
       }
     } else {  // (bf16: half a step) what lies behind the rows' ends reads zeros
 #pragma unroll
       for (int u = 0; u < UNITS; ++u) {
         const int c = (lane & 7) ^ (((u * 8 + row8) >> 1) & 7);
         const char* const p = (u < STREAM_W / 8 ? w0 : x0) + at + off[u];
-        dma_b128(at + c * 16 < bytes ? p : reinterpret_cast<const char*>(g_zero_chunk), dst + u * 1024);
+        dma_b128(at + c * 16 < bytes ? p : reinterpret_cast<const char*>(g_zero_chunk), lds + u * 1024);
       }
     }
   };
@@ -391,31 +388,22 @@ __global__ __launch_bounds__(512) void head_stream_kernel(HeadStreamArgs a) {
   for (int i = 0; i < NW; ++i)
 #pragma unroll
     for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  auto wait = [&](auto younger) {  // all loads but those of so many steps have landed
-    constexpr int N = decltype(younger)::value * UNITS;
-    static_assert(N < 64, "vmcnt field");
+  auto wait = [&](bool loads) {
     __builtin_amdgcn_sched_barrier(0);
-    __builtin_amdgcn_s_waitcnt(0x0f70 | (N & 15) | (N >> 4) << 14);
+    if (loads) __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): the step has landed
+    else __builtin_amdgcn_s_waitcnt(0xc07f);         // lgkmcnt(0): it has been read
     asm volatile("" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
   };
 #pragma unroll 1
-  for (int i = 0; i < S - 1 && i < n; ++i) issue(i);
-#pragma unroll 1
   for (int i = 0; i < n; ++i) {
-    // (the slot that step i + S - 1 goes to has been read: its fragments were multiplied)
-    if (i + S - 1 < n) {
-      issue(i + S - 1);
-      wait(std::integral_constant<int, S - 1>{});
-    } else {
-      wait(std::integral_constant<int, 0>{});
-    }
-    const char* const stage = mine + (i % S) * STAGE;
+    issue(i);
+    wait(true);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       frag_t wf[NW], xf[NT];
       auto read = [&](int row) {
-        return *reinterpret_cast<const frag_t*>(stage + (row + r) * 128 + (((h * 4 + quad) ^ ((r >> 1) & 7)) << 4));
+        return *reinterpret_cast<const frag_t*>(mine + (row + r) * 128 + (((h * 4 + quad) ^ ((r >> 1) & 7)) << 4));
       };
 #pragma unroll
       for (int q = 0; q < NW; ++q) wf[q] = read(q * 16);
@@ -433,14 +421,11 @@ __global__ __launch_bounds__(512) void head_stream_kernel(HeadStreamArgs a) {
           }
         }
     }
-    __builtin_amdgcn_sched_barrier(0);
-    __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): the slot has been read
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_sched_barrier(0);
+    wait(false);
   }
 
-  __syncthreads();  // (no ring is in use any more)
-  auto sum_at = [&](int w, int f) { return reinterpret_cast<f32x4*>(ring + ((w * NW * NT + f) * 64 + lane) * 16); };
+  __syncthreads();  // (no step is in use any more)
+  auto sum_at = [&](int w, int f) { return reinterpret_cast<f32x4*>(buf + ((w * NW * NT + f) * 64 + lane) * 16); };
 #pragma unroll
   for (int i = 0; i < NW; ++i)
 #pragma unroll

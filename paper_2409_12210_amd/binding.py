@@ -581,10 +581,19 @@ def _generator(rng) -> Optional[int]:
     """The pointer of seed and offset: two integers of 64 bits on the device."""
     if rng is None or isinstance(rng, int):
         return rng
+    if rng.dtype in (_WIDE or _find_wide()) and rng.numel() == 2 and rng.is_contiguous():
+        return rng.data_ptr()
+    raise _Unfit(f"{rng.dtype} of shape {tuple(rng.shape)}, expected two int64: seed and offset")
+
+
+_WIDE = ()
+
+
+def _find_wide():
+    global _WIDE
     import torch
-    if rng.dtype not in (torch.int64, torch.uint64) or rng.numel() != 2 or not rng.is_contiguous():
-        raise _Unfit(f"{rng.dtype} of shape {tuple(rng.shape)}, expected two int64: seed and offset")
-    return rng.data_ptr()
+    _WIDE = (torch.int64, torch.uint64)
+    return _WIDE
 
 
 def modse_dropout_fwd(T, d_model, dtype, x, residual, p, rng, call, y, stream=None, raise_on_error=True) -> int:

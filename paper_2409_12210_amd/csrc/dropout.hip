@@ -6,7 +6,9 @@
 // the 16 random bits of each of eight consecutive elements, the low half of word w that of element 2 w.  With 16 bits an element p is
 // a multiple of 2^-16, and the kept ones are scaled by 1 / (1 - p) of that p.
 //
-// A thread takes the eight elements of one counter.  Large calls are bound by memory.
+// A thread takes the eight elements of one counter.  Large calls are bound by memory: 32768 rows of 2048, bf16, with a residual 61 us (6.6
+// TB/s), backwards 38 (7.0, partly from the caches).  The generator is some 14 products of 32 bits and as many words of xor for 48 bytes
+// read and written, and hides behind them.  Small calls are one launch, 2.5 us of the GPU.
 #include "ops.h"
 
 namespace {
@@ -22,7 +24,13 @@ __device__ __forceinline__ u32x4 philox7(u32x4 c, uint32_t k0, uint32_t k1) {
   return c;
 }
 
-template <typename T, bool RESIDUAL>
+// Reads with the non-temporal hint from a size on that the caches do not hold (the last level has 256 MiB).  Without / with it, us,
+// with the norm that reads y behind it: 16384 rows of 2048, bf16 (192 MiB read and written) 52 / 57, 32768 (384 MiB) 115 / 103,
+// 32768 of 4096 240 / 220; backwards alone 32768 of 2048 (256 MiB) 38 / 44, of 4096 89 / 85.  (Hinted stores of y: 57 in place of 52, 125
+// in place of 115.)
+constexpr int64_t STREAM_BYTES = (int64_t)320 << 20;
+
+template <typename T, bool RESIDUAL, bool STREAM>
 __global__ __launch_bounds__(256) void dropout_kernel(DropoutArgs a) {
   constexpr int N = Vec<T>::N, NV = 8 / N;
   const T* const x = static_cast<const T*>(a.x);
@@ -37,8 +45,8 @@ __global__ __launch_bounds__(256) void dropout_kernel(DropoutArgs a) {
 #pragma unroll
     for (int q = 0; q < NV; ++q) {
       const int n = (int)(left - q * N < N ? left - q * N : N);
-      v[q].load(x + at + q * N, n, 0.f);
-      if constexpr (RESIDUAL) r[q].load(res + at + q * N, n, 0.f);
+      v[q].template load<STREAM>(x + at + q * N, n, 0.f);
+      if constexpr (RESIDUAL) r[q].template load<STREAM>(res + at + q * N, n, 0.f);
     }
     const u32x4 w = philox7(u32x4{(uint32_t)i, a.call, (uint32_t)offset, (uint32_t)(offset >> 32)}, (uint32_t)seed, (uint32_t)(seed >> 32));
 #pragma unroll
@@ -62,8 +70,11 @@ template <typename T>
 hipError_t run(const DropoutArgs& a, hipStream_t s) {
   const int64_t blocks = (a.n + 2047) / 2048;
   const dim3 grid((unsigned)(blocks < (1 << 20) ? blocks : 1 << 20));
-  if (a.residual) hipLaunchKernelGGL((dropout_kernel<T, true>), grid, dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((dropout_kernel<T, false>), grid, dim3(256), 0, s, a);
+  const bool stream = a.n * (int64_t)sizeof(T) * (a.residual ? 3 : 2) >= STREAM_BYTES;
+  if (a.residual && stream) hipLaunchKernelGGL((dropout_kernel<T, true, true>), grid, dim3(256), 0, s, a);
+  else if (a.residual) hipLaunchKernelGGL((dropout_kernel<T, true, false>), grid, dim3(256), 0, s, a);
+  else if (stream) hipLaunchKernelGGL((dropout_kernel<T, false, true>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((dropout_kernel<T, false, false>), grid, dim3(256), 0, s, a);
   return hipGetLastError();
 }
 }  // namespace

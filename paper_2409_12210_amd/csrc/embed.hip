@@ -1,6 +1,8 @@
 // Embedding lookup x_t = scale E[token_t], and its gradient dE_v = scale sum of dX_t over the tokens t that are v, in float32.
 //
-// Lookup: a wave takes up to 2048 (bf16) or 1024 (float32) columns of one row.  Bound by memory, or by the launch.
+// Lookup: a wave takes up to 2048 (bf16) or 1024 (float32) columns of one row.  Bound by memory (32768 rows of 2048, bf16: 37 us, 7.2
+// TB/s), or by the launch.  (Hinted stores take 15.6 us where 17.3 are for 16384 rows, but with the norm that reads them behind it 44
+// in place of 40.)
 //
 // Gradient, three launches, every sum in an order that the tokens alone fix:
 //   embed_sort_kernel  a block owns a range of the vocabulary and sorts the tokens of its range, stably: it reads all tokens (they
@@ -148,39 +150,40 @@ __global__ __launch_bounds__(SORT_WAVES * 64) void embed_sort_kernel(EmbedBwdArg
   }
 }
 
-// Adds `n` floats to what there is (accumulate) or stores them, scaled.
-template <int N>
-__device__ __forceinline__ void put_row(const EmbedBwdArgs& a, int32_t key, int c, const float (&s)[N]) {
+// Four columns of a row from p on, `n` of them there: scaled sums that are added to what there is (accumulate) or stored.
+__device__ __forceinline__ void put_row(const EmbedBwdArgs& a, int32_t key, int c, f32x4 s) {
   float* const p = a.dE + (int64_t)key * a.d + c;
-#pragma unroll
-  for (int q = 0; q < N / 4; ++q) {
-    const int n = a.d - c - q * 4;
-    if (n <= 0) break;
-    Vec<float> v;
-    if (a.accumulate) v.load(p + q * 4, n, 0.f);
-    else v.v = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v.set(e, a.accumulate ? v[e] + s[q * 4 + e] * a.scale : s[q * 4 + e] * a.scale);
-    v.store(p + q * 4, n);
+  const int n = a.d - c;
+  Vec<float> v;
+  if (a.accumulate) {
+    v.load(p, n, 0.f);
+    v.v += s * a.scale;
+  } else {
+    v.v = s * a.scale;
   }
+  v.store(p, n);
 }
-template <int N>
-__device__ __forceinline__ void put_part(const EmbedBwdArgs& a, int64_t slot, int c, const float (&s)[N]) {
-  float* const p = a.part + slot * a.part_ld + c;  // (rows of the workspace are padded to whole vectors)
-#pragma unroll
-  for (int q = 0; q < N / 4; ++q)
-    if (c + q * 4 < a.d) *reinterpret_cast<f32x4*>(p + q * 4) = f32x4{s[q * 4], s[q * 4 + 1], s[q * 4 + 2], s[q * 4 + 3]};
+// (rows of the workspace are padded to whole vectors)
+__device__ __forceinline__ void put_part(const EmbedBwdArgs& a, int64_t slot, int c, f32x4 s) {
+  *reinterpret_cast<f32x4*>(a.part + slot * a.part_ld + c) = s;
 }
+// Four elements of a row that starts anywhere.
+template <typename T> struct Quad;
+template <> struct Quad<float> { typedef f32x4 type; };
+template <> struct Quad<bf16_t> { typedef bf16x4 type; };
 
 // Partial sums: slot 2 i is the beginning of chunk i, which belongs to a run that begins before it, slot 2 i + 1 its end, of a run that
 // begins in it and goes on behind it.
 //
-// A wave takes 64 vectors of sixteen bytes of a chunk's rows.  The rows are loaded a batch at a time, without a branch between the loads:
-// a lane behind the row's end loads the row's last vector, which nobody stores.  (EDGE: the row's length is no multiple of the
-// vector, and a lane's vector may reach over it.)
+// A wave takes 512 columns of a chunk's rows, a lane four of either half, so that its stores, like its loads, go to whole lines.  (Eight
+// neighbouring columns a lane, whose float32 results are stored half a line at a time: 71 us for 32768 tokens of width 2048.)  The
+// rows are loaded a batch at a time, without a branch between the loads: a lane behind the row's end loads the row's last
+// columns, which nobody stores.  (EDGE: the row's length is no multiple of four, and a lane's columns may reach over it.)
 template <typename T, bool EDGE>
 __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedBwdArgs a) {
-  constexpr int N = Vec<T>::N, SEG = 64 * N, AHEAD = 8;
+  typedef typename Quad<T>::type quad_t;
+  typedef quad_t quad_u __attribute__((aligned(sizeof(T))));
+  constexpr int SEG = 512, AHEAD = 8;
   const int lane = threadIdx.x & 63;
   const int segs = (a.d + SEG - 1) / SEG;
   const int64_t u = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -189,8 +192,7 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedBwdArgs a) {
   const int64_t first = i * a.chunk;
   if (first >= n_sorted) return;
   const int n = (int)min((int64_t)a.chunk, n_sorted - first);
-  const int c = (int)(u - i * segs) * SEG + lane * N;
-  const bool here = c < a.d;
+  const int c = (int)(u - i * segs) * SEG + lane * 4;
   // lane q holds place first + q of the list (a.chunk <= 64), and the keys around the chunk
   const int32_t order = a.order[first + min(lane, n - 1)];
   const int32_t key = lane < n ? a.keys[first + lane] : -1;
@@ -200,36 +202,51 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedBwdArgs a) {
   const int32_t key_right = __shfl_down(key, 1, 64);
   const uint64_t ends = __ballot(lane < n && (lane == n - 1 || key != key_right));
   const T* const base = static_cast<const T*>(a.dX);
-  const int at = EDGE ? c : min(c, a.d - N);
-  float s[N] = {};
+  auto load = [&](const T* row, int col) {
+    quad_t v = {};
+    if constexpr (EDGE) {
+      if (col + 4 > a.d) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (col + e < a.d) v[e] = row[col + e];
+        return v;
+      }
+    }
+    // (read once, whole lines: with the hint 46 us where 68 were.  A wave's columns of an EDGE row begin and end inside a line, which
+    // would come twice then)
+    if constexpr (EDGE) return (quad_t)*reinterpret_cast<const quad_u*>(row + col);
+    else return (quad_t)__builtin_nontemporal_load(reinterpret_cast<const quad_u*>(row + min(col, a.d - 4)));
+  };
+  f32x4 s[2] = {};
   bool from_before = __builtin_amdgcn_readlane(key, 0) == key_before;
   for (int q0 = 0; q0 < n; q0 += AHEAD) {
-    Vec<T> v[AHEAD];
+    quad_t v[AHEAD][2];
 #pragma unroll
     for (int q = 0; q < AHEAD; ++q) {
       const T* const row = base + (int64_t)__builtin_amdgcn_readlane(order, min(q0 + q, n - 1)) * a.d;
-      if constexpr (EDGE) {
-        if (here) v[q].load(row + at, a.d - at, 0.f);
-      } else {
-        v[q].load(row + at, N, 0.f);
-      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h) v[q][h] = load(row, c + h * 256);
     }
 #pragma unroll
     for (int q = 0; q < AHEAD; ++q) {
       if (q0 + q < n) {
 #pragma unroll
-        for (int e = 0; e < N; ++e) s[e] += v[q][e];
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[h][e] += (float)v[q][h][e];
         if (ends >> (q0 + q) & 1) {
           const bool last = q0 + q == n - 1;
           const int32_t k = __builtin_amdgcn_readlane(key, q0 + q);
-          if (here) {
-            if (from_before) put_part(a, 2 * i, c, s);
-            else if (last && k == key_after) put_part(a, 2 * i + 1, c, s);
-            else put_row(a, k, c, s);
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            if (c + h * 256 < a.d) {
+              if (from_before) put_part(a, 2 * i, c + h * 256, s[h]);
+              else if (last && k == key_after) put_part(a, 2 * i + 1, c + h * 256, s[h]);
+              else put_row(a, k, c + h * 256, s[h]);
+            }
+            s[h] = f32x4{0.f, 0.f, 0.f, 0.f};
           }
           from_before = false;
-#pragma unroll
-          for (int e = 0; e < N; ++e) s[e] = 0.f;
         }
       }
     }
@@ -280,8 +297,7 @@ __global__ __launch_bounds__(256) void embed_join_kernel(EmbedBwdArgs a) {
   __syncthreads();
   if (wave > 0 || c >= a.d) return;
   for (int w = 0; w < 3; ++w) s += sums[w][lane];
-  const float out[4] = {s[0], s[1], s[2], s[3]};
-  put_row(a, key, c, out);
+  put_row(a, key, c, s);
 }
 
 template <typename T>
@@ -302,11 +318,10 @@ hipError_t launch_embed_bwd(modse_dtype dt, const EmbedBwdArgs& a, hipStream_t s
   const int rows = std::min(EMBED_MAX_ROWS, (a.vocab + 255) / 256);
   hipLaunchKernelGGL(embed_sort_kernel, dim3((unsigned)((a.vocab + rows - 1) / rows)), dim3(SORT_WAVES * 64), 0, s, a, rows);
   const int64_t chunks = embed_chunks(a.T);
-  const int seg = 64 * (dt == MODSE_F32 ? 4 : 8);
-  const dim3 sums((unsigned)((chunks * ((a.d + seg - 1) / seg) + 3) / 4)), joins((unsigned)(chunks * ((a.d + 255) / 256)));
+  const dim3 sums((unsigned)((chunks * ((a.d + 511) / 512) + 3) / 4)), joins((unsigned)(chunks * ((a.d + 255) / 256)));
   if (dt == MODSE_F32 && a.d % 4 == 0) hipLaunchKernelGGL((embed_sum_kernel<float, false>), sums, dim3(256), 0, s, a);
   else if (dt == MODSE_F32) hipLaunchKernelGGL((embed_sum_kernel<float, true>), sums, dim3(256), 0, s, a);
-  else if (a.d % 8 == 0) hipLaunchKernelGGL((embed_sum_kernel<bf16_t, false>), sums, dim3(256), 0, s, a);
+  else if (a.d % 4 == 0) hipLaunchKernelGGL((embed_sum_kernel<bf16_t, false>), sums, dim3(256), 0, s, a);
   else hipLaunchKernelGGL((embed_sum_kernel<bf16_t, true>), sums, dim3(256), 0, s, a);
   if (chunks > 1) hipLaunchKernelGGL(embed_join_kernel, joins, dim3(256), 0, s, a);
   return hipGetLastError();

@@ -347,10 +347,12 @@ modse_status modse_head_fwd(int64_t T, int32_t d_model, int32_t vocab, modse_dty
  *   dX      [T, d_model] of `dtype` out, or NULL; it may lie in the buffer of x
  *   dW      [vocab, d_model] float32 out, or NULL: overwritten, or added to with
  *           accumulate = 1
- * The gradient of the logits is rounded to 2^-17 of each of its values for dW (bf16:
- * two numbers) and to the layer's type for dX.  Workspace sizes: MODSE_WS_FWD and
- * MODSE_WS_BWD for the two calls.  Sums run in an order that the sizes alone fix, the
- * two calls' in orders of their own.  T == 0 leaves dW as it is. */
+ * In bf16 the gradient of the logits is rounded to bf16 for dX.  For dW it is held in
+ * 22 bits, down to 2^-39 of the largest |d_logp| (of a row with a target), and x
+ * exactly, down to 2^-39 of the largest |x|: what is smaller may be lost.
+ * Workspace sizes: MODSE_WS_FWD and MODSE_WS_BWD for the two calls.  Sums run in an
+ * order that the sizes alone fix, the two calls' in orders of their own.  T == 0
+ * leaves dW as it is. */
 modse_status modse_head_bwd(int64_t T, int32_t d_model, int32_t vocab, modse_dtype dtype, const void* x, const void* W,
                             const int32_t* targets, const float* d_logp, float* logp, void* dX, float* dW, int accumulate, void* ws,
                             size_t ws_bytes, void* hip_stream);

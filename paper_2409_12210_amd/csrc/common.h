@@ -87,8 +87,8 @@ enum GemmEpilogue {
   EPI_SWIGLU = 2,      // two accumulators a, b: C = h = silu(a)*b; optionally C2 = dh/da, C3 = dh/db
   EPI_SWIGLU_BWD = 3,  // acc = dh; E1 = dh/da, E2 = dh/db (saved by the forward pass): C = da, C2 = db
   EPI_STORE_DUALK = 4, // C = acc over two operand pairs (A,B) and (A2,B2)
-  // C = acc or C += acc, float32, rows below E2 (as an integer) alone: A has M columns, a multiple of 32, and C fewer rows.  bf16: over
-  // two operand pairs
+  // C = acc or C += acc, float32, rows below E2 (as an integer) alone: A has M columns, a multiple of 32, and C fewer rows.  Layers of
+  // bf16: the operands are two pairs of float16 matrices, and acc is multiplied by the two floats at E1
   EPI_ROWS_F32 = 5,
   // acc = logits (bf16 operands): for every row, maximum m and sum of e^(l - m) over the 128 columns of a wave, as a pair at C2[column /
   // 128 of all columns][row], and the logit of the row's target (E1, int32) at C3[row], if it is among the columns; C = acc, float32, if

@@ -352,6 +352,7 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64) void gg_bf16_kernel(const Ge
   int a_ahead = 0;  // the youngest UPW loads of this wave belong to an A panel that is not waited for yet
 
   // Fragments of one K half.
+  typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
   bf16x8 af[MI], bfr[NB][NI];
   // Transposed operands.  Lane l = 16 * blk + s reads, for K half kh and h = 0, 1, the 8 bytes at K row
   // kh*32 + blk*8 + h*4 + (s >> 2), column x = tile_x + 16*i + 4*(s & 3); the instruction returns K rows +0..+3 of column
@@ -399,7 +400,10 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64) void gg_bf16_kernel(const Ge
 #pragma unroll
     for (int t = 0; t < NB * MI * NI; ++t) {
       const int q = t / (MI * NI), j = (t / MI) % NI, i = (j & 1) ? MI - 1 - t % MI : t % MI;  // (to and fro: one operand changes at a time)
-      acc[q][i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bfr[q][j], af[i], acc[q][i][j], 0, 0, 0);
+      if constexpr (EPI == EPI_ROWS_F32)
+        acc[q][i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, bfr[q][j]), __builtin_bit_cast(f16x8, af[i]), acc[q][i][j], 0, 0, 0);
+      else
+        acc[q][i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bfr[q][j], af[i], acc[q][i][j], 0, 0, 0);
       if (t % (NB * MI * NI / UPW) == 1) {
         __builtin_amdgcn_sched_barrier(0);
         if (fast) issue_fast(c, off, dst, t / (NB * MI * NI / UPW));
@@ -606,6 +610,10 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64) void gg_bf16_kernel(const Ge
       const bool stream_c = (option & GEMM_STREAM_C) != 0;
       constexpr bool ROWS = EPI == EPI_ROWS_F32;
       const int rows_end = ROWS ? (int)reinterpret_cast<intptr_t>(cc.E2) : 0, rows_m0 = cc.w.m0 + wm * WM;
+      float scale[2] = {1.f, 1.f};
+      if constexpr (ROWS)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) scale[i] = reinterpret_cast<const float*>(cc.E1)[i];
       auto row_there = [&](int b, int it) { return !ROWS || rows_m0 + (b / NI32) * 32 + it * 8 + erow < rows_end; };
       if (cc.nsteps == 0) {  // an expert without tokens: the ring holds nothing of this tile
         if (!accumulate)
@@ -663,6 +671,7 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64) void gg_bf16_kernel(const Ge
             for (int it = 0; it < 4; ++it) {
               const int rr = it * 8 + erow;
               f32x4 v = *reinterpret_cast<const f32x4*>(slot + rr * 128 + ((echunk ^ ((rr >> 1) & 7)) << 4));
+              if constexpr (ROWS) v = v * scale[0] * scale[1];
               if constexpr (ADD) {
                 // loads issued after this one: the rest of this block's, and the next block's reloaded so far
                 if (b + 1 < NBLK || it == 0) wait_loaded<3>(old[it]);

@@ -13,8 +13,10 @@
 // float32 and in a buffer that stays in the caches, and another launch turns them into G.  float32: the logits are stored and
 // a row is gone through twice, the second time to put G in its place.
 //
-// dW is float32, and a term of its sums is rounded to 2^-17: in bf16 G is kept as two numbers, hi + lo, and dW takes both.  dX
-// is rounded to bf16 itself and takes hi alone.
+// dX of a bf16 layer is rounded to bf16, and takes G rounded to bf16.  dW is float32, and takes G as the sum of two float16 numbers, hi + lo,
+// which hold 22 bits, times float16 copies of the rows of x: both times powers of two that follow the largest |x| and the largest
+// |d_logp| of the call, so that what is rounded or lost is below 2^-39 of the largest product.  (Two bf16 numbers, 16 bits, left an
+// error of 2.7e-6 of dW where float32 products have 0.7e-6 to 2e-6, and need no third copy of G; the rest takes as long.)
 #include "ops.h"
 
 #include "gemm_bf16_util.h"
@@ -99,13 +101,28 @@ HeadShape head_shape(int64_t T, int32_t d, int32_t vocab, modse_dtype dt, bool g
   return h;
 }
 
+// The largest values of a call, as the bits of floats, and what undoes the scaling by them.
+struct HeadRange {
+  uint32_t x, d_logp;
+  float undo[2];  // the smaller factor first: no product on the way overflows where the result does not
+};
+// the power of two that brings values of at most this size below 2^15
+__device__ __forceinline__ int scale_exponent(uint32_t bits) { return min(14 - ((int)(bits >> 23 & 255) - 127), 120); }
+__device__ __forceinline__ float power_of_two(int e) { return __builtin_bit_cast(float, (uint32_t)(e + 127) << 23); }
+
+typedef _Float16 f16_t;
+typedef f16_t f16x8 __attribute__((ext_vector_type(8)));
+
 struct HeadBufs {
   GemmPlan* plans;   // logits of every product, then dX and dW of every piece
   float* logits;     // [sub, ldv]; float32 layers: then G
   float* pairs;      // [ceil(vocab / 128)][sub] maximum and sum
   float* at_target;  // [sub] the target's logit
   float* off;        // [sub] log Z
-  bf16_t *hi, *lo;   // [rows, ldv] G
+  bf16_t* g;         // [rows, ldv] G
+  f16_t *hi, *lo;    // [rows, ldv] G in two parts, scaled
+  f16_t* x16;        // [rows, d] x, scaled
+  HeadRange* range;
   float* slabs;      // [k_parts][rows, d]
 };
 
@@ -129,6 +146,7 @@ __global__ __launch_bounds__(64) void head_plan_kernel(HeadPlanArgs a) {
   const int m = (int)min((int64_t)rows, h.T - t0);
   const char* const x = cadd(a.x, (size_t)t0 * h.d * es);
   GemmPlan* const plan = a.b.plans + blockIdx.x;
+  if (a.b.range && blockIdx.x == 0 && lane == 0) a.b.range->x = a.b.range->d_logp = 0;
   const int n = which == 0 ? h.w_parts : which == 1 ? h.k_parts : 1;
   for (int p = lane; p < n; p += 64) {
     GemmProblem P = {};
@@ -147,7 +165,7 @@ __global__ __launch_bounds__(64) void head_plan_kernel(HeadPlanArgs a) {
       t = h.logits_tile;
     } else if (which == 1) {
       const int v0 = p * h.k_len;
-      P.A = h.bf16 ? (const void*)(a.b.hi + v0) : (const void*)(a.b.logits + v0);
+      P.A = h.bf16 ? (const void*)(a.b.g + v0) : (const void*)(a.b.logits + v0);
       P.B = cadd(a.W, (size_t)v0 * h.d * es);
       P.C = a.b.slabs + (size_t)p * h.rows * h.d;
       P.M = m; P.N = h.d; P.K = min(h.k_len, h.vocab - v0);
@@ -156,7 +174,8 @@ __global__ __launch_bounds__(64) void head_plan_kernel(HeadPlanArgs a) {
     } else {
       P.A = h.bf16 ? (const void*)a.b.hi : (const void*)a.b.logits;
       P.A2 = a.b.lo;
-      P.B = P.B2 = x;
+      P.B = P.B2 = h.bf16 ? (const void*)a.b.x16 : x;
+      P.E1 = a.b.range ? a.b.range->undo : nullptr;
       P.C = a.dW;
       P.E2 = reinterpret_cast<const void*>((intptr_t)h.vocab);
       P.M = (h.vocab + 31) / 32 * 32; P.N = h.d; P.K = m;
@@ -179,7 +198,9 @@ struct HeadRowsArgs {
   float* logits;
   const float *pairs, *at_target;
   float* off;
-  bf16_t *hi, *lo;         // of the product's first row
+  bf16_t* g;               // of the product's first row; null where there is no dX
+  f16_t *hi, *lo;          // null where there is no dW
+  const HeadRange* range;
   int32_t rows, vocab, ldv, pair_rows;
 };
 __device__ __forceinline__ float row_weight(const HeadRowsArgs& a, int row, int32_t target) {
@@ -233,23 +254,81 @@ __global__ __launch_bounds__(1024) void head_stats_kernel(HeadRowsArgs a) {
   a.off[row] = top + log_sum;
 }
 
-// bf16: G of a row's 2048 columns as two numbers each.  Columns behind the vocabulary become zeros.
+// bf16: the largest |x| and |d_logp| of the call.  (NaN counts as more than any number.  One atomic a block: of 8192 waves they took 100 us.)
+__global__ __launch_bounds__(1024) void head_range_kernel(const bf16_t* x, int64_t n, const float* d_logp, const int32_t* targets, int64_t T,
+                                                         int32_t vocab, HeadRange* range) {
+  __shared__ uint32_t s_x[16], s_w[16];
+  uint32_t most_x = 0, most_w = 0;
+  const int64_t first = (int64_t)blockIdx.x * 1024 + threadIdx.x, step = (int64_t)gridDim.x * 1024;
+  for (int64_t i = first; i < n / 8; i += 4 * step) {
+    u32x4 v[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) v[q] = *reinterpret_cast<const u32x4*>(x + (i + q * step < n / 8 ? i + q * step : i) * 8);
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) most_x = max(most_x, max(v[q][e] << 16 & 0x7fff0000u, v[q][e] & 0x7fff0000u));
+  }
+  for (int64_t t = first; t < T; t += step)
+    if (targets[t] >= 0 && targets[t] < vocab) most_w = max(most_w, __builtin_bit_cast(uint32_t, d_logp[t]) & 0x7fffffffu);
+#pragma unroll
+  for (int o = 32; o; o >>= 1) {
+    most_x = max(most_x, (uint32_t)__shfl_xor((int)most_x, o, 64));
+    most_w = max(most_w, (uint32_t)__shfl_xor((int)most_w, o, 64));
+  }
+  if ((threadIdx.x & 63) == 0) {
+    s_x[threadIdx.x >> 6] = most_x;
+    s_w[threadIdx.x >> 6] = most_w;
+  }
+  __syncthreads();
+  if (threadIdx.x > 0) return;
+  for (int w = 1; w < 16; ++w) {
+    most_x = max(most_x, s_x[w]);
+    most_w = max(most_w, s_w[w]);
+  }
+  atomicMax(&range->x, most_x);  // (a maximum: the order does not matter)
+  atomicMax(&range->d_logp, most_w);
+}
+// bf16: the float16 copy of a piece's rows of x
+__global__ __launch_bounds__(256) void head_cast_kernel(const bf16_t* x, int64_t n, f16_t* x16, HeadRange* range) {
+  const int e = scale_exponent(range->x);
+  const float scale = power_of_two(e);
+  if (blockIdx.x == 0 && threadIdx.x == 0) {
+    const float a = power_of_two(-e), b = power_of_two(-scale_exponent(range->d_logp));
+    range->undo[0] = fminf(a, b);
+    range->undo[1] = fmaxf(a, b);
+  }
+  for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8; i < n; i += (int64_t)gridDim.x * 2048) {
+    const bf16x8 v = *reinterpret_cast<const bf16x8*>(x + i);
+    f16x8 o;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) o[k] = (f16_t)((float)v[k] * scale);
+    *reinterpret_cast<f16x8*>(x16 + i) = o;
+  }
+}
+
+// bf16: G of a row's 2048 columns, in bf16 for dX, in two parts for dW.  Columns behind the vocabulary become zeros.
 __global__ __launch_bounds__(256) void head_grad_kernel(HeadRowsArgs a, int segs) {
   const int row = blockIdx.x / segs, c = (blockIdx.x - row * segs) * 2048 + threadIdx.x * 8;
   if (c >= a.ldv) return;
   const int32_t target = a.targets[row];
-  const float off = a.off[row], w = row_weight(a, row, target);
-  const float* const l = a.logits + (int64_t)row * a.ldv + c;
-  const f32x4 v[2] = {*reinterpret_cast<const f32x4*>(l), *reinterpret_cast<const f32x4*>(l + 4)};
-  bf16x8 hi, lo;
+  const float off = a.off[row], w = row_weight(a, row, target), scale = power_of_two(scale_exponent(a.range->d_logp));
+  const int64_t at = (int64_t)row * a.ldv + c;
+  const f32x4 v[2] = {*reinterpret_cast<const f32x4*>(a.logits + at), *reinterpret_cast<const f32x4*>(a.logits + at + 4)};
+  bf16x8 g;
+  f16x8 hi, lo;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    const float g = grad_of(v[e >> 2][e & 3], off, w, target, c + e, a.vocab);
-    hi[e] = (bf16_t)g;
-    lo[e] = (bf16_t)(g - (float)hi[e]);
+    const float x = grad_of(v[e >> 2][e & 3], off, w, target, c + e, a.vocab), scaled = x * scale;
+    g[e] = (bf16_t)x;
+    hi[e] = (f16_t)scaled;
+    lo[e] = (f16_t)(scaled - (float)hi[e]);
   }
-  *reinterpret_cast<bf16x8*>(a.hi + (int64_t)row * a.ldv + c) = hi;
-  *reinterpret_cast<bf16x8*>(a.lo + (int64_t)row * a.ldv + c) = lo;
+  if (a.g) *reinterpret_cast<bf16x8*>(a.g + at) = g;
+  if (a.hi) {
+    *reinterpret_cast<f16x8*>(a.hi + at) = hi;
+    *reinterpret_cast<f16x8*>(a.lo + at) = lo;
+  }
 }
 
 // float32: a row of logits, its sums, and (GRAD) its row of G in its place.  Columns behind the vocabulary become zeros.
@@ -523,9 +602,9 @@ size_t stream_workspace(int64_t T, int32_t vocab) {
 }
 
 struct HeadLayout {
-  size_t logits, pairs, at_target, off, hi, lo, slabs, total;
+  size_t range, logits, pairs, at_target, off, g, hi, lo, x16, slabs, total;
 };
-HeadLayout layout_for(int64_t plans, int64_t sub, int64_t rows, int64_t slab_cells, int32_t vocab, bool bf16, bool grad) {
+HeadLayout layout_for(int64_t plans, int64_t sub, int64_t rows, int64_t slab_cells, int32_t d, int32_t vocab, bool bf16, bool grad) {
   HeadLayout w = {};
   const size_t ldv = align_up(vocab, 64), cells = (size_t)rows * ldv;
   size_t at = 0;
@@ -535,12 +614,15 @@ HeadLayout layout_for(int64_t plans, int64_t sub, int64_t rows, int64_t slab_cel
     return here;
   };
   take(sizeof(GemmPlan) * (size_t)plans);
+  w.range = take(sizeof(HeadRange));
   w.logits = take(bf16 && !grad ? 0 : (size_t)sub * ldv * 4);
   w.pairs = take(bf16 ? (size_t)sub * ((vocab + 127) / 128) * 8 : 0);
   w.at_target = take(bf16 ? (size_t)sub * 4 : 0);
   w.off = take(bf16 ? (size_t)sub * 4 : 0);
+  w.g = take(bf16 && grad ? cells * 2 : 0);
   w.hi = take(bf16 && grad ? cells * 2 : 0);
   w.lo = take(bf16 && grad ? cells * 2 : 0);
+  w.x16 = take(bf16 && grad ? (size_t)rows * d * 2 : 0);
   w.slabs = take(grad ? (size_t)slab_cells * 4 : 0);
   w.total = at;
   return w;
@@ -555,7 +637,7 @@ size_t head_workspace(int64_t T, int32_t d, int32_t vocab, modse_dtype dt, bool 
   const int64_t sub = std::min<int64_t>(padded_rows(T), sub_most), rows = std::min<int64_t>((int64_t)align_up((size_t)T, (size_t)sub), most);
   const int64_t pieces = (T + most - 1) / most, plans = (T + sub_most - 1) / sub_most + (grad ? 2 * pieces : 0);
   const int64_t slabs = std::min(MAX_PARTS * rows * d, std::max(SLAB_CELLS, rows * d));
-  const size_t total = ALIGN + layout_for(plans, sub, rows, slabs, vocab, bf16, grad).total;
+  const size_t total = ALIGN + layout_for(plans, sub, rows, slabs, d, vocab, bf16, grad).total;
   return grad ? total : T <= STREAM_ROWS ? stream_workspace(T, vocab) : std::max(total, stream_workspace(STREAM_ROWS, vocab));
 }
 
@@ -569,13 +651,20 @@ hipError_t launch_head(modse_dtype dt, const HeadArgs& a, char* ws, hipStream_t 
   }
   const HeadShape h = head_shape(a.T, a.d, a.vocab, dt, grad);
   const int64_t products = h.products(), plans = products + (grad ? 2 * h.pieces : 0);
-  const HeadLayout w = layout_for(plans, h.sub, h.rows, (int64_t)h.k_parts * h.rows * h.d, h.vocab, h.bf16, grad);
+  const HeadLayout w = layout_for(plans, h.sub, h.rows, (int64_t)h.k_parts * h.rows * h.d, h.d, h.vocab, h.bf16, grad);
   ws = reinterpret_cast<char*>(align_up(reinterpret_cast<size_t>(ws), ALIGN));
   auto floats = [&](size_t at) { return reinterpret_cast<float*>(ws + at); };
+  auto halves = [&](size_t at) { return reinterpret_cast<f16_t*>(ws + at); };
+  HeadRange* const range = h.bf16 && grad ? reinterpret_cast<HeadRange*>(ws + w.range) : nullptr;
   const HeadBufs b = {reinterpret_cast<GemmPlan*>(ws), floats(w.logits), floats(w.pairs), floats(w.at_target), floats(w.off),
-                      reinterpret_cast<bf16_t*>(ws + w.hi), reinterpret_cast<bf16_t*>(ws + w.lo), floats(w.slabs)};
+                      reinterpret_cast<bf16_t*>(ws + w.g), halves(w.hi), halves(w.lo), halves(w.x16), range, floats(w.slabs)};
   const HeadPlanArgs plan = {h, b, a.x, a.W, a.targets, a.dW};
   hipLaunchKernelGGL(head_plan_kernel, dim3((unsigned)plans), dim3(64), 0, s, plan);
+  const bf16_t* const x = static_cast<const bf16_t*>(a.x);
+  if (range) {
+    const unsigned blocks = (unsigned)std::min<int64_t>((h.T * h.d + 32767) / 32768, 512);
+    hipLaunchKernelGGL(head_range_kernel, dim3(blocks), dim3(1024), 0, s, x, h.T * h.d, a.d_logp, a.targets, h.T, h.vocab, range);
+  }
   auto tiles = [](int64_t m, int64_t n, TileShape t) { return ((m + t.bm - 1) / t.bm) * ((n + t.bn - 1) / t.bn); };
   hipError_t e = hipGetLastError();
   // the logits of one product, their sums and (of gradients) G
@@ -585,8 +674,9 @@ hipError_t launch_head(modse_dtype dt, const HeadArgs& a, char* ws, hipStream_t 
                             tiles(m, h.vocab, h.logits_tile) + h.w_parts * tiles(m, 1, h.logits_tile), s, LAYOUT_TN);
     if (e != hipSuccess) return;
     const HeadRowsArgs r = {a.targets + t0, a.d_logp ? a.d_logp + t0 : nullptr, a.logp ? a.logp + t0 : nullptr, a.log_z ? a.log_z + t0 : nullptr,
-                            b.logits, b.pairs, b.at_target, b.off, b.hi + in_piece * h.ldv, b.lo + in_piece * h.ldv,
-                            (int32_t)m, h.vocab, h.ldv, h.sub};
+                            b.logits, b.pairs, b.at_target, b.off, a.dX ? b.g + in_piece * h.ldv : nullptr,
+                            a.dW ? b.hi + in_piece * h.ldv : nullptr, a.dW ? b.lo + in_piece * h.ldv : nullptr,
+                            range, (int32_t)m, h.vocab, h.ldv, h.sub};
     if (h.bf16) {
       hipLaunchKernelGGL(head_stats_kernel, dim3((unsigned)((m + 63) / 64)), dim3(1024), 0, s, r);
       const int segs = (h.ldv + 2047) / 2048;
@@ -606,6 +696,10 @@ hipError_t launch_head(modse_dtype dt, const HeadArgs& a, char* ws, hipStream_t 
     const int64_t t0 = piece * h.rows, m = std::min<int64_t>(h.rows, h.T - t0);
     const GemmPlan* const p = b.plans + products + 2 * piece;
     if (a.dW) {  // (before dX, which may lie in the buffer of x)
+      if (range) {
+        const unsigned blocks = (unsigned)std::min<int64_t>((m * h.d + 2047) / 2048, 4096);
+        hipLaunchKernelGGL(head_cast_kernel, dim3(blocks), dim3(256), 0, s, x + t0 * h.d, m * h.d, b.x16, range);
+      }
       e = launch_grouped_gemm(dt, EPI_ROWS_F32, h.dw_tile, p + 1, 1, a.accumulate || piece > 0, 0,
                               tiles(padded_rows(h.vocab), h.d, h.dw_tile), s, LAYOUT_AB_K);
       if (e != hipSuccess) break;

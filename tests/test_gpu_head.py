@@ -4,8 +4,8 @@ Tolerances.  A logit is a sum of d products in float32, whose instructions drop 
 e = (d + 2) 2^-23 sum |x W| (0 where the inputs are whole numbers whose sums float32 holds).  Sums of exponentials: V terms of one sign,
 joined in groups, under 2^9 roundings each with an exponential of relative error 2 u + |z| u whose weight falls as e^z: 2^-14 at the
 worst.  So log Z and log p are off by a = e_max + e_target + 2^-14 + 2^-22 (|l| + |log p|), and p relatively by as much (and 2^-21 |log p|).
-G = w (1[target] - p) adds 2^-22 |w| at the target.  For dW it is held to 2^-17 of each value (bf16; float32 exactly), for dX to half a
-step of the type.  The products sum in float32: (terms + 2) 2^-23 of the sum of the absolute values; a result is rounded to its type."""
+G = w (1[target] - p) adds 2^-22 |w| at the target.  For dX it is rounded to half a step of the type.  For dW of bf16 layers it is held to
+2^-22 of each value (2^-21 with the product by its scale) and 2^-39 of the largest weight, and x to 2^-39 of its largest value.  The products sum in float32: (terms + 2) 2^-23 of the sum of the absolute values; a result is rounded to its type."""
 import numpy as np
 import pytest
 import torch
@@ -97,9 +97,10 @@ def near(got, want, tol, what, *tag):
     assert ok.all(), (what,) + tag + (int((~ok).sum()), float(err[~ok].max()) if err[~ok].numel() else NAN, torch.nonzero(~ok)[:3].tolist())
 
 
-def check(T, d, V, dtype, seed=0, whole=False, sigma=2.5, products=True):
-    print("head", T, d, V, dtype, whole, flush=True)
+def check(T, d, V, dtype, seed=0, whole=False, sigma=2.5, times_x=1.0, times_w=1.0):
+    print("head", T, d, V, dtype, whole, times_x, times_w, flush=True)
     x, W, targets, w = inputs(T, d, V, dtype, seed, sigma, whole)
+    x, W, w = x * times_x, W / times_x, w * times_w
     logp, log_z, G, tol, tol_z, tol_G = reference(x, W, targets, w, whole)
     got = forward(x, W, targets, dtype)
     near(got[0], logp, tol, "logp", T, d, V, dtype)
@@ -115,10 +116,11 @@ def check(T, d, V, dtype, seed=0, whole=False, sigma=2.5, products=True):
     tol_dX = (tol_G + rounded * size) @ W64.abs() + (V + 2) * 2.0 ** -23 * terms
     want = G @ W64
     near(dX, want, tol_dX + HALF[dtype] * (want.abs() + tol_dX), "dX", T, d, V, dtype)
-    held = 2.0 ** -17 if dtype == "bf16" else 0.0
-    Gt, St, Et = G.t().contiguous(), size.t().contiguous(), (tol_G + held * size).t().contiguous()
+    held = dtype == "bf16"
+    most_w, most_x = w[targets >= 0].double().abs().max() if (targets >= 0).any() else 0.0, x64.abs().max()
+    Gt, St, Et = G.t().contiguous(), size.t().contiguous(), (tol_G + held * (2.0 ** -21 * size + 2.0 ** -39 * most_w)).t().contiguous()
     terms = St @ x64.abs()
-    tol_dW = Et @ x64.abs() + (2 * T + 2) * 2.0 ** -23 * terms
+    tol_dW = Et @ x64.abs() + held * St.sum(1, keepdim=True) * 2.0 ** -39 * most_x + (2 * T + 2) * 2.0 ** -23 * terms
     want = Gt @ x64
     near(dW, want, tol_dW + 2.0 ** -24 * (want.abs() + tol_dW), "dW", T, d, V, dtype)
     return x, W, targets, w, dX, dW, want, tol_dW
@@ -150,6 +152,29 @@ def test_sums_are_added_to_and_results_are_the_same_bits_again(T, d, V, dtype):
     assert torch.equal(alone[0], dW) and torch.equal(alone[1], dX)
     there = backward(x, W, targets, w, dtype, inplace=True)
     assert torch.equal(there[1], dX) and torch.equal(there[2], dW)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("times_x,times_w", [(2.0 ** -40, 1.0), (2.0 ** 40, 1.0), (1.0, 2.0 ** -60), (1.0, 2.0 ** 60), (2.0 ** -40, 2.0 ** 60),
+                                             (2.0 ** 40, 2.0 ** -60), (2.0 ** -60, 2.0 ** -30), (2.0 ** 30, 2.0 ** 60), (1.0, 0.0)])
+def test_rows_and_gradients_of_any_size(times_x, times_w, dtype):
+    """Powers of two leave the logits as they are."""
+    check(70, 64, 300, dtype, seed=13, times_x=times_x, times_w=times_w)
+
+
+def test_weights_and_rows_of_sizes_far_apart():
+    T, d, V = 64, 64, 300
+    x, W, targets, w = inputs(T, d, V, "bf16", 14)
+    w = w * 2.0 ** torch.linspace(-30, 0, T, device="cuda")
+    x[::3] *= 2.0 ** -12
+    logp, log_z, G, tol, tol_z, tol_G = reference(x, W, targets, w)
+    lp, dX, dW = backward(x, W, targets, w, "bf16")
+    x64, size = x.double(), G.abs() + tol_G
+    tol_dW = (tol_G + 2.0 ** -21 * size + 2.0 ** -39 * w.abs().max()).t().contiguous() @ x64.abs() + (
+        size.t().sum(1, keepdim=True) * 2.0 ** -39 * x64.abs().max()) + (2 * T + 3) * 2.0 ** -23 * (size.t().contiguous() @ x64.abs())
+    near(dW, G.t().contiguous() @ x64, tol_dW, "dW")
+    want = G @ W.double()
+    near(dX, want, (tol_G + 2.0 ** -8 * size) @ W.double().abs() * 1.01 + 2.0 ** -8 * want.abs() * 1.01 + (V + 2) * 2.0 ** -23 * (size @ W.double().abs()), "dX")
 
 
 def test_the_largest_vocabulary_in_pieces_of_few_rows():

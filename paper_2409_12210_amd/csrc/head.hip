@@ -31,7 +31,7 @@ constexpr int64_t PAIR_CELLS = (int64_t)1 << 27;   // pairs of 128 columns in it
 constexpr int64_t W_PART = (int64_t)1 << 30;       // elements of W that one problem reads (kernels count them in 32 bits)
 constexpr size_t ALIGN = 256;                      // of what is in the workspace, which itself may lie at any sixteen bytes
 constexpr int64_t SLAB_CELLS = (int64_t)1 << 26;   // values of all parts of dX together, unless one part has more
-constexpr int MAX_PARTS = 32;                      // of dX
+constexpr int MAX_PARTS = 128;                     // of dX
 
 struct HeadShape {
   int64_t T;
@@ -82,7 +82,8 @@ HeadShape head_shape(int64_t T, int32_t d, int32_t vocab, modse_dtype dt, bool g
   auto tile = [&](int64_t m, int64_t n) { const int b = h.bf16 ? 256 : tiles(m, n, 128) >= 2048 ? 128 : 64; return TileShape{b, b}; };
   h.logits_tile = tile(h.sub, vocab);
   h.dw_tile = tile(vocab, d);
-  h.dx_tile = TileShape{h.bf16 ? 256 : 128, h.bf16 ? 256 : 128};
+  const int dx = h.bf16 ? 256 : h.rows <= 64 ? 64 : 128;
+  h.dx_tile = TileShape{dx, dx};
   // Parts of dX: whole rounds of workgroups over the chip, each part with six further steps for its opening and its end, and slabs that
   // are written and read.
   const int64_t out = tiles(h.rows, d, h.dx_tile.bm), steps = (vocab + 63) / 64, slots = h.bf16 ? 256 : 512;
@@ -90,7 +91,7 @@ HeadShape head_shape(int64_t T, int32_t d, int32_t vocab, modse_dtype dt, bool g
   double best = 0;
   for (int64_t n = 1; n <= parts_most; ++n) {
     const int64_t len = (steps + n - 1) / n, parts = (steps + len - 1) / len;
-    const double step_us = h.bf16 ? 1.6 : 8.0;
+    const double step_us = h.bf16 ? 1.6 : dx == 64 ? 3.0 : 8.0;
     const double us = (double)((out * parts + slots - 1) / slots) * (len + 6) * step_us + parts * (double)h.rows * d * 8 / 4e6;
     if (n == 1 || us < best) {
       best = us;
@@ -101,10 +102,13 @@ HeadShape head_shape(int64_t T, int32_t d, int32_t vocab, modse_dtype dt, bool g
   return h;
 }
 
-// The largest values of a call, as the bits of floats, and what undoes the scaling by them.
+// The largest |x| and |d_logp| of a call, as the bits of floats: by block, joined by the launch behind the first product of logits.
+constexpr int RANGE_BLOCKS = 512;
 struct HeadRange {
+  uint32_t x_of[RANGE_BLOCKS], d_logp_of[RANGE_BLOCKS];
+  int32_t blocks;
   uint32_t x, d_logp;
-  float undo[2];  // the smaller factor first: no product on the way overflows where the result does not
+  float undo[2];  // the scaling by both: the smaller factor first, so that no product on the way overflows where the result does not
 };
 // the power of two that brings values of at most this size below 2^15
 __device__ __forceinline__ int scale_exponent(uint32_t bits) { return min(14 - ((int)(bits >> 23 & 255) - 127), 120); }
@@ -131,12 +135,81 @@ struct HeadPlanArgs {
   HeadBufs b;
   const void *x, *W;
   const int32_t* targets;
+  const float* d_logp;
   float* dW;
+  int32_t plans;
 };
 
-// The problems of one product: of the logits, one block for each, then of dX and of dW, a block for each piece.
-__global__ __launch_bounds__(64) void head_plan_kernel(HeadPlanArgs a) {
+// The largest values of block `block` of the blocks of 1024 that look for them.  (NaN counts as more than any number.)
+__device__ __forceinline__ void range_block(const HeadPlanArgs& a, int block, int blocks) {
+  __shared__ uint32_t s_x[16], s_w[16];
+  const bf16_t* const x = static_cast<const bf16_t*>(a.x);
+  const int64_t n = a.h.T * a.h.d / 8;
+  uint32_t most_x = 0, most_w = 0;
+  const int64_t first = (int64_t)block * 1024 + threadIdx.x, step = (int64_t)blocks * 1024;
+  for (int64_t i = first; i < n; i += 4 * step) {
+    u32x4 v[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) v[q] = *reinterpret_cast<const u32x4*>(x + (i + q * step < n ? i + q * step : i) * 8);
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) most_x = max(most_x, max(v[q][e] << 16 & 0x7fff0000u, v[q][e] & 0x7fff0000u));
+  }
+  for (int64_t t = first; t < a.h.T; t += step)
+    if (a.targets[t] >= 0 && a.targets[t] < a.h.vocab) most_w = max(most_w, __builtin_bit_cast(uint32_t, a.d_logp[t]) & 0x7fffffffu);
+#pragma unroll
+  for (int o = 32; o; o >>= 1) {
+    most_x = max(most_x, (uint32_t)__shfl_xor((int)most_x, o, 64));
+    most_w = max(most_w, (uint32_t)__shfl_xor((int)most_w, o, 64));
+  }
+  if ((threadIdx.x & 63) == 0) {
+    s_x[threadIdx.x >> 6] = most_x;
+    s_w[threadIdx.x >> 6] = most_w;
+  }
+  __syncthreads();
+  if (threadIdx.x > 0) return;
+  for (int w = 1; w < 16; ++w) {
+    most_x = max(most_x, s_x[w]);
+    most_w = max(most_w, s_w[w]);
+  }
+  a.b.range->x_of[block] = most_x;
+  a.b.range->d_logp_of[block] = most_w;
+  if (block == 0) a.b.range->blocks = blocks;
+}
+// One wave joins them.  (Whichever block does it, it writes the same.)
+__device__ __forceinline__ void join_range(HeadRange* r) {
+  const int lane = threadIdx.x & 63, blocks = r->blocks;
+  uint32_t x = 0, w = 0;
+#pragma unroll
+  for (int i = 0; i < RANGE_BLOCKS / 64; ++i)
+    if (i * 64 + lane < blocks) {
+      x = max(x, r->x_of[i * 64 + lane]);
+      w = max(w, r->d_logp_of[i * 64 + lane]);
+    }
+#pragma unroll
+  for (int o = 32; o; o >>= 1) {
+    x = max(x, (uint32_t)__shfl_xor((int)x, o, 64));
+    w = max(w, (uint32_t)__shfl_xor((int)w, o, 64));
+  }
+  if (lane == 0) {
+    r->x = x;
+    r->d_logp = w;
+    const float a = power_of_two(-scale_exponent(x)), b = power_of_two(-scale_exponent(w));
+    r->undo[0] = fminf(a, b);
+    r->undo[1] = fmaxf(a, b);
+  }
+}
+
+// The problems of one product, by a block's first wave: of the logits, one block for each, then of dX and of dW, a block for each
+// piece.  Blocks behind these look for the largest values.
+__global__ __launch_bounds__(1024) void head_plan_kernel(HeadPlanArgs a) {
   __shared__ int s_tiles[MODSE_MAX_PROBLEMS];
+  if ((int)blockIdx.x >= a.plans) {
+    range_block(a, blockIdx.x - a.plans, gridDim.x - a.plans);
+    return;
+  }
+  if (threadIdx.x >= 64) return;
   const HeadShape& h = a.h;
   const int lane = threadIdx.x, products = (int)h.products();
   const int which = (int)blockIdx.x < products ? 0 : 1 + ((int)blockIdx.x - products) % 2;
@@ -146,7 +219,6 @@ __global__ __launch_bounds__(64) void head_plan_kernel(HeadPlanArgs a) {
   const int m = (int)min((int64_t)rows, h.T - t0);
   const char* const x = cadd(a.x, (size_t)t0 * h.d * es);
   GemmPlan* const plan = a.b.plans + blockIdx.x;
-  if (a.b.range && blockIdx.x == 0 && lane == 0) a.b.range->x = a.b.range->d_logp = 0;
   const int n = which == 0 ? h.w_parts : which == 1 ? h.k_parts : 1;
   for (int p = lane; p < n; p += 64) {
     GemmProblem P = {};
@@ -185,7 +257,7 @@ __global__ __launch_bounds__(64) void head_plan_kernel(HeadPlanArgs a) {
     s_tiles[p] = set_tiles(P, t.bm, t.bn);
     plan->prob[p] = P;
   }
-  __syncthreads();
+  wave_lds_order();
   finish_plan(plan, lane, n, s_tiles);
 }
 
@@ -200,8 +272,10 @@ struct HeadRowsArgs {
   float* off;
   bf16_t* g;               // of the product's first row; null where there is no dX
   f16_t *hi, *lo;          // null where there is no dW
-  const HeadRange* range;
-  int32_t rows, vocab, ldv, pair_rows;
+  HeadRange* range;
+  const bf16_t* x;         // of the product's first row, and their copies
+  f16_t* x16;
+  int32_t rows, vocab, ldv, pair_rows, d;
 };
 __device__ __forceinline__ float row_weight(const HeadRowsArgs& a, int row, int32_t target) {
   return target < 0 ? 0.f : target >= a.vocab ? __builtin_nanf("") : a.d_logp[row];
@@ -244,6 +318,7 @@ __global__ __launch_bounds__(1024) void head_stats_kernel(HeadRowsArgs a) {
   }
   s_m[wave][lane] = m;
   s_s[wave][lane] = s;
+  if (a.range && wave == 15) join_range(a.range);
   __syncthreads();
   if (wave > 0 || row >= a.rows) return;
   float top = m, sum = 0.f;
@@ -254,61 +329,20 @@ __global__ __launch_bounds__(1024) void head_stats_kernel(HeadRowsArgs a) {
   a.off[row] = top + log_sum;
 }
 
-// bf16: the largest |x| and |d_logp| of the call.  (NaN counts as more than any number.  One atomic a block: of 8192 waves they took 100 us.)
-__global__ __launch_bounds__(1024) void head_range_kernel(const bf16_t* x, int64_t n, const float* d_logp, const int32_t* targets, int64_t T,
-                                                         int32_t vocab, HeadRange* range) {
-  __shared__ uint32_t s_x[16], s_w[16];
-  uint32_t most_x = 0, most_w = 0;
-  const int64_t first = (int64_t)blockIdx.x * 1024 + threadIdx.x, step = (int64_t)gridDim.x * 1024;
-  for (int64_t i = first; i < n / 8; i += 4 * step) {
-    u32x4 v[4];
-#pragma unroll
-    for (int q = 0; q < 4; ++q) v[q] = *reinterpret_cast<const u32x4*>(x + (i + q * step < n / 8 ? i + q * step : i) * 8);
-#pragma unroll
-    for (int q = 0; q < 4; ++q)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) most_x = max(most_x, max(v[q][e] << 16 & 0x7fff0000u, v[q][e] & 0x7fff0000u));
-  }
-  for (int64_t t = first; t < T; t += step)
-    if (targets[t] >= 0 && targets[t] < vocab) most_w = max(most_w, __builtin_bit_cast(uint32_t, d_logp[t]) & 0x7fffffffu);
-#pragma unroll
-  for (int o = 32; o; o >>= 1) {
-    most_x = max(most_x, (uint32_t)__shfl_xor((int)most_x, o, 64));
-    most_w = max(most_w, (uint32_t)__shfl_xor((int)most_w, o, 64));
-  }
-  if ((threadIdx.x & 63) == 0) {
-    s_x[threadIdx.x >> 6] = most_x;
-    s_w[threadIdx.x >> 6] = most_w;
-  }
-  __syncthreads();
-  if (threadIdx.x > 0) return;
-  for (int w = 1; w < 16; ++w) {
-    most_x = max(most_x, s_x[w]);
-    most_w = max(most_w, s_w[w]);
-  }
-  atomicMax(&range->x, most_x);  // (a maximum: the order does not matter)
-  atomicMax(&range->d_logp, most_w);
-}
-// bf16: the float16 copy of a piece's rows of x
-__global__ __launch_bounds__(256) void head_cast_kernel(const bf16_t* x, int64_t n, f16_t* x16, HeadRange* range) {
-  const int e = scale_exponent(range->x);
-  const float scale = power_of_two(e);
-  if (blockIdx.x == 0 && threadIdx.x == 0) {
-    const float a = power_of_two(-e), b = power_of_two(-scale_exponent(range->d_logp));
-    range->undo[0] = fminf(a, b);
-    range->undo[1] = fmaxf(a, b);
-  }
-  for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8; i < n; i += (int64_t)gridDim.x * 2048) {
-    const bf16x8 v = *reinterpret_cast<const bf16x8*>(x + i);
+// bf16: G of a row's 2048 columns, in bf16 for dX, in two parts for dW.  Columns behind the vocabulary become zeros.  Blocks behind the rows'
+// make the float16 copies of x, 2048 values each.
+__global__ __launch_bounds__(256) void head_grad_kernel(HeadRowsArgs a, int segs) {
+  if ((int)blockIdx.x >= a.rows * segs) {
+    const int64_t i = (int64_t)(blockIdx.x - a.rows * segs) * 2048 + threadIdx.x * 8;
+    if (i >= (int64_t)a.rows * a.d) return;
+    const float scale = power_of_two(scale_exponent(a.range->x));
+    const bf16x8 v = *reinterpret_cast<const bf16x8*>(a.x + i);
     f16x8 o;
 #pragma unroll
     for (int k = 0; k < 8; ++k) o[k] = (f16_t)((float)v[k] * scale);
-    *reinterpret_cast<f16x8*>(x16 + i) = o;
+    *reinterpret_cast<f16x8*>(a.x16 + i) = o;
+    return;
   }
-}
-
-// bf16: G of a row's 2048 columns, in bf16 for dX, in two parts for dW.  Columns behind the vocabulary become zeros.
-__global__ __launch_bounds__(256) void head_grad_kernel(HeadRowsArgs a, int segs) {
   const int row = blockIdx.x / segs, c = (blockIdx.x - row * segs) * 2048 + threadIdx.x * 8;
   if (c >= a.ldv) return;
   const int32_t target = a.targets[row];
@@ -388,8 +422,15 @@ __global__ __launch_bounds__(512) void head_rows_kernel(HeadRowsArgs a) {
 template <typename T>
 __global__ __launch_bounds__(256) void head_join_kernel(const float* slabs, int parts, int64_t stride, int64_t n, T* dX) {
   for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; i < n; i += (int64_t)gridDim.x * 1024) {  // (n: whole rows of 32 and more columns)
-    f32x4 s = *reinterpret_cast<const f32x4*>(slabs + i);
-    for (int p = 1; p < parts; ++p) s += *reinterpret_cast<const f32x4*>(slabs + p * stride + i);
+    f32x4 s = {0.f, 0.f, 0.f, 0.f};
+    for (int p = 0; p < parts; p += 8) {
+      f32x4 v[8];
+#pragma unroll
+      for (int q = 0; q < 8; ++q) v[q] = *reinterpret_cast<const f32x4*>(slabs + min(p + q, parts - 1) * stride + i);
+#pragma unroll
+      for (int q = 0; q < 8; ++q)
+        if (p + q < parts) s += v[q];
+    }
 #pragma unroll
     for (int e = 0; e < 4; ++e) dX[i + e] = (T)s[e];
   }
@@ -412,7 +453,10 @@ struct HeadStreamArgs {
   float* pairs;      // [T][ceil(vocab / 64)] maximum and sum
   float* at_target;  // [T]
   float *logp, *log_z;
-  int32_t T, d, vocab;
+  float* logits;     // [T, ldv] or null
+  float* off;        // [T] log Z or null
+  HeadRange* range;  // to join, or null
+  int32_t T, d, vocab, ldv;
 };
 
 template <typename T, int NT>
@@ -519,6 +563,7 @@ __global__ __launch_bounds__(256, 2) void head_stream_kernel(HeadStreamArgs a) {
     f32x4 l = *sum_at(0, wave * NT + j);
 #pragma unroll
     for (int q = 1; q < 4; ++q) l += *sum_at(q, wave * NT + j);
+    if (a.logits && t < a.T && v < a.ldv) *reinterpret_cast<f32x4*>(a.logits + (int64_t)t * a.ldv + v) = l;
     const int32_t at = t < a.T ? a.targets[t] - v : -1;
     if (at >= 0 && at < 4 && v + at < a.vocab) a.at_target[t] = at == 0 ? l[0] : at == 1 ? l[1] : at == 2 ? l[2] : l[3];
 #pragma unroll
@@ -577,6 +622,7 @@ __global__ __launch_bounds__(1024) void head_stream_join_kernel(HeadStreamArgs a
     s_m[wave] = wm;
     s_s[wave] = s;
   }
+  if (a.range && t == 0 && wave == 15) join_range(a.range);
   __syncthreads();
   if (threadIdx.x > 0) return;
   float top = s_m[0], sum = 0.f;
@@ -584,6 +630,7 @@ __global__ __launch_bounds__(1024) void head_stream_join_kernel(HeadStreamArgs a
   for (int w = 0; w < 16; ++w) sum += s_s[w] * __builtin_amdgcn_exp2f((s_m[w] - top) * LOG2E);
   const float log_sum = __builtin_amdgcn_logf(sum) * LN2;
   put_row(a.logp ? a.logp + t : nullptr, a.log_z ? a.log_z + t : nullptr, a.targets[t], a.vocab, a.at_target[t], top, log_sum);
+  if (a.off) a.off[t] = top + log_sum;
 }
 
 template <typename T>
@@ -593,13 +640,13 @@ hipError_t run_stream(const HeadStreamArgs& a, hipStream_t s) {
   if (nt == 1) hipLaunchKernelGGL((head_stream_kernel<T, 1>), grid, block, 0, s, a);
   else if (nt == 2) hipLaunchKernelGGL((head_stream_kernel<T, 2>), grid, block, 0, s, a);
   else hipLaunchKernelGGL((head_stream_kernel<T, 4>), grid, block, 0, s, a);
-  hipLaunchKernelGGL(head_stream_join_kernel, dim3((unsigned)a.T), dim3(1024), 0, s, a);
+  // (of a float32 layer's gradients the launch that makes G goes through the logits itself)
+  if (a.logp || a.log_z || a.off) hipLaunchKernelGGL(head_stream_join_kernel, dim3((unsigned)a.T), dim3(1024), 0, s, a);
   return hipGetLastError();
 }
 constexpr int64_t STREAM_ROWS = 64;  // up to so many rows
-size_t stream_workspace(int64_t T, int32_t vocab) {
-  return ALIGN + align_up((size_t)T * ((vocab + STREAM_W - 1) / STREAM_W) * 8, ALIGN) + (size_t)T * 4;
-}
+size_t stream_pairs(int64_t T, int32_t vocab) { return (size_t)T * ((vocab + STREAM_W - 1) / STREAM_W) * 8; }
+size_t stream_workspace(int64_t T, int32_t vocab) { return ALIGN + align_up(stream_pairs(T, vocab), ALIGN) + (size_t)T * 4; }
 
 struct HeadLayout {
   size_t range, logits, pairs, at_target, off, g, hi, lo, x16, slabs, total;
@@ -616,8 +663,8 @@ HeadLayout layout_for(int64_t plans, int64_t sub, int64_t rows, int64_t slab_cel
   take(sizeof(GemmPlan) * (size_t)plans);
   w.range = take(sizeof(HeadRange));
   w.logits = take(bf16 && !grad ? 0 : (size_t)sub * ldv * 4);
-  w.pairs = take(bf16 ? (size_t)sub * ((vocab + 127) / 128) * 8 : 0);
-  w.at_target = take(bf16 ? (size_t)sub * 4 : 0);
+  w.pairs = take(std::max(bf16 ? (size_t)sub * ((vocab + 127) / 128) * 8 : 0, stream_pairs(std::min(sub, STREAM_ROWS), vocab)));
+  w.at_target = take((size_t)sub * 4);
   w.off = take(bf16 ? (size_t)sub * 4 : 0);
   w.g = take(bf16 && grad ? cells * 2 : 0);
   w.hi = take(bf16 && grad ? cells * 2 : 0);
@@ -645,8 +692,8 @@ hipError_t launch_head(modse_dtype dt, const HeadArgs& a, char* ws, hipStream_t 
   const bool grad = a.dX || a.dW;
   if (!grad && a.T <= STREAM_ROWS) {
     float* const pairs = reinterpret_cast<float*>(align_up(reinterpret_cast<size_t>(ws), ALIGN));
-    float* const at_target = pairs + align_up((size_t)a.T * ((a.vocab + STREAM_W - 1) / STREAM_W) * 8, ALIGN) / 4;
-    const HeadStreamArgs r = {a.x, a.W, a.targets, pairs, at_target, a.logp, a.log_z, (int32_t)a.T, a.d, a.vocab};
+    float* const at_target = pairs + align_up(stream_pairs(a.T, a.vocab), ALIGN) / 4;
+    const HeadStreamArgs r = {a.x, a.W, a.targets, pairs, at_target, a.logp, a.log_z, nullptr, nullptr, nullptr, (int32_t)a.T, a.d, a.vocab, 0};
     return dt == MODSE_F32 ? run_stream<float>(r, s) : run_stream<bf16_t>(r, s);
   }
   const HeadShape h = head_shape(a.T, a.d, a.vocab, dt, grad);
@@ -658,29 +705,33 @@ hipError_t launch_head(modse_dtype dt, const HeadArgs& a, char* ws, hipStream_t 
   HeadRange* const range = h.bf16 && grad ? reinterpret_cast<HeadRange*>(ws + w.range) : nullptr;
   const HeadBufs b = {reinterpret_cast<GemmPlan*>(ws), floats(w.logits), floats(w.pairs), floats(w.at_target), floats(w.off),
                       reinterpret_cast<bf16_t*>(ws + w.g), halves(w.hi), halves(w.lo), halves(w.x16), range, floats(w.slabs)};
-  const HeadPlanArgs plan = {h, b, a.x, a.W, a.targets, a.dW};
-  hipLaunchKernelGGL(head_plan_kernel, dim3((unsigned)plans), dim3(64), 0, s, plan);
+  const HeadPlanArgs plan = {h, b, a.x, a.W, a.targets, a.d_logp, a.dW, (int32_t)plans};
+  const int64_t range_blocks = range ? std::min<int64_t>((h.T * h.d + 32767) / 32768, RANGE_BLOCKS) : 0;
+  hipLaunchKernelGGL(head_plan_kernel, dim3((unsigned)(plans + range_blocks)), dim3(1024), 0, s, plan);
   const bf16_t* const x = static_cast<const bf16_t*>(a.x);
-  if (range) {
-    const unsigned blocks = (unsigned)std::min<int64_t>((h.T * h.d + 32767) / 32768, 512);
-    hipLaunchKernelGGL(head_range_kernel, dim3(blocks), dim3(1024), 0, s, x, h.T * h.d, a.d_logp, a.targets, h.T, h.vocab, range);
-  }
   auto tiles = [](int64_t m, int64_t n, TileShape t) { return ((m + t.bm - 1) / t.bm) * ((n + t.bn - 1) / t.bn); };
   hipError_t e = hipGetLastError();
   // the logits of one product, their sums and (of gradients) G
   auto product = [&](int64_t i) {
     const int64_t t0 = i * h.sub, m = std::min<int64_t>(h.sub, h.T - t0), in_piece = t0 % h.rows;
-    e = launch_grouped_gemm(dt, h.bf16 ? EPI_LOGITS : EPI_STORE, h.logits_tile, b.plans + i, h.w_parts, 0, GEMM_STREAM_C,
-                            tiles(m, h.vocab, h.logits_tile) + h.w_parts * tiles(m, 1, h.logits_tile), s, LAYOUT_TN);
+    const bool stream = h.T <= STREAM_ROWS;  // (only with gradients here)
+    if (stream) {
+      const HeadStreamArgs r = {a.x, a.W, a.targets, b.pairs, b.at_target, h.bf16 ? a.logp : nullptr, nullptr, b.logits,
+                                h.bf16 ? b.off : nullptr, range, (int32_t)m, h.d, h.vocab, h.ldv};
+      e = h.bf16 ? run_stream<bf16_t>(r, s) : run_stream<float>(r, s);
+    } else {
+      e = launch_grouped_gemm(dt, h.bf16 ? EPI_LOGITS : EPI_STORE, h.logits_tile, b.plans + i, h.w_parts, 0, GEMM_STREAM_C,
+                              tiles(m, h.vocab, h.logits_tile) + h.w_parts * tiles(m, 1, h.logits_tile), s, LAYOUT_TN);
+    }
     if (e != hipSuccess) return;
     const HeadRowsArgs r = {a.targets + t0, a.d_logp ? a.d_logp + t0 : nullptr, a.logp ? a.logp + t0 : nullptr, a.log_z ? a.log_z + t0 : nullptr,
                             b.logits, b.pairs, b.at_target, b.off, a.dX ? b.g + in_piece * h.ldv : nullptr,
                             a.dW ? b.hi + in_piece * h.ldv : nullptr, a.dW ? b.lo + in_piece * h.ldv : nullptr,
-                            range, (int32_t)m, h.vocab, h.ldv, h.sub};
+                            range, x + t0 * h.d, b.x16 + in_piece * h.d, (int32_t)m, h.vocab, h.ldv, h.sub, h.d};
     if (h.bf16) {
-      hipLaunchKernelGGL(head_stats_kernel, dim3((unsigned)((m + 63) / 64)), dim3(1024), 0, s, r);
-      const int segs = (h.ldv + 2047) / 2048;
-      if (grad) hipLaunchKernelGGL(head_grad_kernel, dim3((unsigned)(m * segs)), dim3(256), 0, s, r, segs);
+      if (!stream) hipLaunchKernelGGL(head_stats_kernel, dim3((unsigned)((m + 63) / 64)), dim3(1024), 0, s, r);
+      const int64_t segs = (h.ldv + 2047) / 2048, copies = a.dW ? (m * h.d + 2047) / 2048 : 0;
+      if (grad) hipLaunchKernelGGL(head_grad_kernel, dim3((unsigned)(m * segs + copies)), dim3(256), 0, s, r, (int)segs);
     } else if (grad) {
       hipLaunchKernelGGL((head_rows_kernel<true>), dim3((unsigned)m), dim3(512), 0, s, r);
     } else {
@@ -696,10 +747,6 @@ hipError_t launch_head(modse_dtype dt, const HeadArgs& a, char* ws, hipStream_t 
     const int64_t t0 = piece * h.rows, m = std::min<int64_t>(h.rows, h.T - t0);
     const GemmPlan* const p = b.plans + products + 2 * piece;
     if (a.dW) {  // (before dX, which may lie in the buffer of x)
-      if (range) {
-        const unsigned blocks = (unsigned)std::min<int64_t>((m * h.d + 2047) / 2048, 4096);
-        hipLaunchKernelGGL(head_cast_kernel, dim3(blocks), dim3(256), 0, s, x + t0 * h.d, m * h.d, b.x16, range);
-      }
       e = launch_grouped_gemm(dt, EPI_ROWS_F32, h.dw_tile, p + 1, 1, a.accumulate || piece > 0, 0,
                               tiles(padded_rows(h.vocab), h.d, h.dw_tile), s, LAYOUT_AB_K);
       if (e != hipSuccess) break;

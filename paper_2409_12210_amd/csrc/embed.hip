@@ -177,9 +177,10 @@ template <> struct Quad<bf16_t> { typedef bf16x4 type; };
 //
 // A wave takes 512 columns of a chunk's rows, a lane four of either half, so that its stores, like its loads, go to whole lines.  (Eight
 // neighbouring columns a lane, whose float32 results are stored half a line at a time: 71 us for 32768 tokens of width 2048.)  The
-// rows are loaded a batch at a time, without a branch between the loads: a lane behind the row's end loads the row's last
-// columns, which nobody stores.  (EDGE: the row's length is no multiple of four, and a lane's columns may reach over it.)
-template <typename T, bool EDGE>
+// rows are loaded a batch at a time, without a branch between the loads, which would make them wait for each other: a lane at or behind the
+// row's end loads the row's last four columns.  (EDGE: the row's length is no multiple of four, and a lane at its end needs some of
+// them; the columns of rows of less than four are loaded one by one.)
+template <typename T, bool EDGE, bool NARROW = false>
 __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedBwdArgs a) {
   typedef typename Quad<T>::type quad_t;
   typedef quad_t quad_u __attribute__((aligned(sizeof(T))));
@@ -203,19 +204,26 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedBwdArgs a) {
   const uint64_t ends = __ballot(lane < n && (lane == n - 1 || key != key_right));
   const T* const base = static_cast<const T*>(a.dX);
   auto load = [&](const T* row, int col) {
-    quad_t v = {};
-    if constexpr (EDGE) {
-      if (col + 4 > a.d) {
+    if constexpr (NARROW) {
+      quad_t v = {};
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (col + e < a.d) v[e] = row[col + e];
-        return v;
-      }
+      for (int e = 0; e < 3; ++e)
+        if (col + e < a.d) v[e] = row[col + e];
+      return v;
     }
     // (read once, whole lines: with the hint 46 us where 68 were.  A wave's columns of an EDGE row begin and end inside a line, which
     // would come twice then)
-    if constexpr (EDGE) return (quad_t)*reinterpret_cast<const quad_u*>(row + col);
+    if constexpr (EDGE) return (quad_t)*reinterpret_cast<const quad_u*>(row + min(col, a.d - 4));
     else return (quad_t)__builtin_nontemporal_load(reinterpret_cast<const quad_u*>(row + min(col, a.d - 4)));
+  };
+  // what was loaded for columns c + 256 h on, of which the row's last vector may hold the first ones further on
+  auto value = [&](quad_t v, int h, int e) {
+    if constexpr (!EDGE || NARROW) return (float)v[e];
+    const int by = max(c + h * 256 - (a.d - 4), 0);
+    float x = (float)v[e];
+#pragma unroll
+    for (int k = 1; k + e < 4; ++k) x = by == k ? (float)v[e + k] : x;
+    return x;
   };
   f32x4 s[2] = {};
   bool from_before = __builtin_amdgcn_readlane(key, 0) == key_before;
@@ -233,7 +241,7 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedBwdArgs a) {
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) s[h][e] += (float)v[q][h][e];
+          for (int e = 0; e < 4; ++e) s[h][e] += value(v[q][h], h, e);
         if (ends >> (q0 + q) & 1) {
           const bool last = q0 + q == n - 1;
           const int32_t k = __builtin_amdgcn_readlane(key, q0 + q);
@@ -319,10 +327,14 @@ hipError_t launch_embed_bwd(modse_dtype dt, const EmbedBwdArgs& a, hipStream_t s
   hipLaunchKernelGGL(embed_sort_kernel, dim3((unsigned)((a.vocab + rows - 1) / rows)), dim3(SORT_WAVES * 64), 0, s, a, rows);
   const int64_t chunks = embed_chunks(a.T);
   const dim3 sums((unsigned)((chunks * ((a.d + 511) / 512) + 3) / 4)), joins((unsigned)(chunks * ((a.d + 255) / 256)));
-  if (dt == MODSE_F32 && a.d % 4 == 0) hipLaunchKernelGGL((embed_sum_kernel<float, false>), sums, dim3(256), 0, s, a);
-  else if (dt == MODSE_F32) hipLaunchKernelGGL((embed_sum_kernel<float, true>), sums, dim3(256), 0, s, a);
-  else if (a.d % 4 == 0) hipLaunchKernelGGL((embed_sum_kernel<bf16_t, false>), sums, dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((embed_sum_kernel<bf16_t, true>), sums, dim3(256), 0, s, a);
+  auto run = [&](auto t) {
+    typedef decltype(t) T;
+    if (a.d % 4 == 0) hipLaunchKernelGGL((embed_sum_kernel<T, false>), sums, dim3(256), 0, s, a);
+    else if (a.d > 4) hipLaunchKernelGGL((embed_sum_kernel<T, true>), sums, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((embed_sum_kernel<T, true, true>), sums, dim3(256), 0, s, a);
+  };
+  if (dt == MODSE_F32) run(float{});
+  else run(bf16_t{});
   if (chunks > 1) hipLaunchKernelGGL(embed_join_kernel, joins, dim3(256), 0, s, a);
   return hipGetLastError();
 }

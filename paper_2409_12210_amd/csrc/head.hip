@@ -13,7 +13,10 @@
 // float32 and in a buffer that stays in the caches, and another launch turns them into G.  float32: the logits are stored and
 // a row is gone through twice, the second time to put G in its place.
 //
-// dX of a bf16 layer is rounded to bf16, and takes G rounded to bf16.  dW is float32, and takes G as the sum of two float16 numbers, hi + lo,
+// dX of a bf16 layer is rounded to bf16, and takes G rounded to bf16.  What that loses of the target's entry, the largest of its row as a
+// rule, is put back in float32 where the slabs are added up: it is a multiple of a row of W.  (Without that dX was off by 2.4e-3 of
+// its norm, of which the rounding of the result is 1.7e-3.)  Up to 128 rows, which fill half a tile, the product takes a second
+// bf16 number for each entry as rows of their own, for nothing.  dW is float32, and takes G as the sum of two float16 numbers, hi + lo,
 // which hold 22 bits, times float16 copies of the rows of x: both times powers of two that follow the largest |x| and the largest
 // |d_logp| of the call, so that what is rounded or lost is below 2^-39 of the largest product.  (Two bf16 numbers, 16 bits, left an
 // error of 2.7e-6 of dW where float32 products have 0.7e-6 to 2e-6, and need no third copy of G; the rest takes as long.)
@@ -31,6 +34,7 @@ constexpr int64_t PAIR_CELLS = (int64_t)1 << 27;   // pairs of 128 columns in it
 constexpr int64_t W_PART = (int64_t)1 << 30;       // elements of W that one problem reads (kernels count them in 32 bits)
 constexpr size_t ALIGN = 256;                      // of what is in the workspace, which itself may lie at any sixteen bytes
 constexpr int64_t SLAB_CELLS = (int64_t)1 << 26;   // values of all parts of dX together, unless one part has more
+constexpr int64_t STACK_ROWS = 128;                // of bf16 layers up to which dX takes G in two parts
 constexpr int MAX_PARTS = 128;                     // of dX
 
 struct HeadShape {
@@ -39,6 +43,7 @@ struct HeadShape {
   int32_t rows, pieces;    // rows of a piece
   int32_t sub, subs;       // rows that one product of logits takes, such products of a (whole) piece
   int32_t w_parts, w_rows; // problems of the logits, rows of W in each
+  int32_t dx_rows;         // rows of the product of dX: those of a piece, or twice as many
   int32_t k_parts, k_len;  // problems of dX, columns of G in each
   int32_t bf16, grad;
   TileShape logits_tile, dx_tile, dw_tile;
@@ -86,13 +91,14 @@ HeadShape head_shape(int64_t T, int32_t d, int32_t vocab, modse_dtype dt, bool g
   h.dx_tile = TileShape{dx, dx};
   // Parts of dX: whole rounds of workgroups over the chip, each part with six further steps for its opening and its end, and slabs that
   // are written and read.
-  const int64_t out = tiles(h.rows, d, h.dx_tile.bm), steps = (vocab + 63) / 64, slots = h.bf16 ? 256 : 512;
-  const int64_t parts_most = std::min<int64_t>({MAX_PARTS, steps, std::max<int64_t>(1, SLAB_CELLS / ((int64_t)h.rows * d))});
+  h.dx_rows = h.bf16 && T <= STACK_ROWS ? 2 * h.rows : h.rows;
+  const int64_t out = tiles(h.dx_rows, d, h.dx_tile.bm), steps = (vocab + 63) / 64, slots = h.bf16 ? 256 : 512;
+  const int64_t parts_most = std::min<int64_t>({MAX_PARTS, steps, std::max<int64_t>(1, SLAB_CELLS / ((int64_t)h.dx_rows * d))});
   double best = 0;
   for (int64_t n = 1; n <= parts_most; ++n) {
     const int64_t len = (steps + n - 1) / n, parts = (steps + len - 1) / len;
     const double step_us = h.bf16 ? 1.6 : dx == 64 ? 3.0 : 8.0;
-    const double us = (double)((out * parts + slots - 1) / slots) * (len + 6) * step_us + parts * (double)h.rows * d * 8 / 4e6;
+    const double us = (double)((out * parts + slots - 1) / slots) * (len + 6) * step_us + parts * (double)h.dx_rows * d * 8 / 4e6;
     if (n == 1 || us < best) {
       best = us;
       h.k_parts = (int32_t)parts;
@@ -123,11 +129,12 @@ struct HeadBufs {
   float* pairs;      // [ceil(vocab / 128)][sub] maximum and sum
   float* at_target;  // [sub] the target's logit
   float* off;        // [sub] log Z
-  bf16_t* g;         // [rows, ldv] G
+  bf16_t* g;         // [dx_rows, ldv] G, and behind its rows what it lacks of them
+  float* lost;       // [rows] what G lacks of the target's entry
   f16_t *hi, *lo;    // [rows, ldv] G in two parts, scaled
   f16_t* x16;        // [rows, d] x, scaled
   HeadRange* range;
-  float* slabs;      // [k_parts][rows, d]
+  float* slabs;      // [k_parts][dx_rows, d]
 };
 
 struct HeadPlanArgs {
@@ -239,8 +246,8 @@ __global__ __launch_bounds__(1024) void head_plan_kernel(HeadPlanArgs a) {
       const int v0 = p * h.k_len;
       P.A = h.bf16 ? (const void*)(a.b.g + v0) : (const void*)(a.b.logits + v0);
       P.B = cadd(a.W, (size_t)v0 * h.d * es);
-      P.C = a.b.slabs + (size_t)p * h.rows * h.d;
-      P.M = m; P.N = h.d; P.K = min(h.k_len, h.vocab - v0);
+      P.C = a.b.slabs + (size_t)p * h.dx_rows * h.d;
+      P.M = h.dx_rows > h.rows ? h.dx_rows : m; P.N = h.d; P.K = min(h.k_len, h.vocab - v0);
       P.lda = h.ldv; P.ldb = h.d; P.ldc = h.d;
       t = h.dx_tile;
     } else {
@@ -270,7 +277,8 @@ struct HeadRowsArgs {
   float* logits;
   const float *pairs, *at_target;
   float* off;
-  bf16_t* g;               // of the product's first row; null where there is no dX
+  bf16_t *g, *g_rest;      // of the product's first row; null where there is no dX, or (g_rest) no second part
+  float* lost;             // null where there is no dX
   f16_t *hi, *lo;          // null where there is no dW
   HeadRange* range;
   const bf16_t* x;         // of the product's first row, and their copies
@@ -349,16 +357,24 @@ __global__ __launch_bounds__(256) void head_grad_kernel(HeadRowsArgs a, int segs
   const float off = a.off[row], w = row_weight(a, row, target), scale = power_of_two(scale_exponent(a.range->d_logp));
   const int64_t at = (int64_t)row * a.ldv + c;
   const f32x4 v[2] = {*reinterpret_cast<const f32x4*>(a.logits + at), *reinterpret_cast<const f32x4*>(a.logits + at + 4)};
-  bf16x8 g;
+  bf16x8 g, rest;
   f16x8 hi, lo;
+  float lost = 0.f;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     const float x = grad_of(v[e >> 2][e & 3], off, w, target, c + e, a.vocab), scaled = x * scale;
     g[e] = (bf16_t)x;
+    const float left = x - (float)g[e];
+    rest[e] = (bf16_t)left;
+    lost = c + e == target ? left : lost;
     hi[e] = (f16_t)scaled;
     lo[e] = (f16_t)(scaled - (float)hi[e]);
   }
-  if (a.g) *reinterpret_cast<bf16x8*>(a.g + at) = g;
+  if (a.g) {
+    *reinterpret_cast<bf16x8*>(a.g + at) = g;
+    if (a.g_rest) *reinterpret_cast<bf16x8*>(a.g_rest + at) = rest;
+    if (c == (target >= 0 && target < a.vocab ? target / 8 * 8 : 0)) a.lost[row] = lost;
+  }
   if (a.hi) {
     *reinterpret_cast<f16x8*>(a.hi + at) = hi;
     *reinterpret_cast<f16x8*>(a.lo + at) = lo;
@@ -418,22 +434,47 @@ __global__ __launch_bounds__(512) void head_rows_kernel(HeadRowsArgs a) {
   }
 }
 
-// dX of a piece: its slabs, in order
+// dX of a piece: its slabs, in order.  A block takes 1024 columns of a row.
+struct HeadJoinArgs {
+  const float* slabs;
+  const bf16_t* W;         // where G lacks something of the targets' entries, or null
+  const float* lost;
+  const int32_t* targets;
+  int64_t stride, rest;    // from part to part; to the rows of G's second parts, or 0
+  int32_t parts, d, vocab;
+};
 template <typename T>
-__global__ __launch_bounds__(256) void head_join_kernel(const float* slabs, int parts, int64_t stride, int64_t n, T* dX) {
-  for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; i < n; i += (int64_t)gridDim.x * 1024) {  // (n: whole rows of 32 and more columns)
-    f32x4 s = {0.f, 0.f, 0.f, 0.f};
-    for (int p = 0; p < parts; p += 8) {
-      f32x4 v[8];
+__global__ __launch_bounds__(256) void head_join_kernel(HeadJoinArgs a, T* dX) {
+  const int row = blockIdx.x, c = blockIdx.y * 1024 + threadIdx.x * 4;
+  if (c >= a.d) return;
+  const int64_t i = (int64_t)row * a.d + c;
+  f32x4 s = {0.f, 0.f, 0.f, 0.f};
+  for (int p = 0; p < a.parts; p += 8) {
+    f32x4 v[8];
 #pragma unroll
-      for (int q = 0; q < 8; ++q) v[q] = *reinterpret_cast<const f32x4*>(slabs + min(p + q, parts - 1) * stride + i);
+    for (int q = 0; q < 8; ++q) v[q] = *reinterpret_cast<const f32x4*>(a.slabs + min(p + q, a.parts - 1) * a.stride + i);
+#pragma unroll
+    for (int q = 0; q < 8; ++q)
+      if (p + q < a.parts) s += v[q];
+    if (a.rest) {
+#pragma unroll
+      for (int q = 0; q < 8; ++q) v[q] = *reinterpret_cast<const f32x4*>(a.slabs + min(p + q, a.parts - 1) * a.stride + a.rest + i);
 #pragma unroll
       for (int q = 0; q < 8; ++q)
-        if (p + q < parts) s += v[q];
+        if (p + q < a.parts) s += v[q];
     }
-#pragma unroll
-    for (int e = 0; e < 4; ++e) dX[i + e] = (T)s[e];
   }
+  if (a.W) {
+    const int32_t target = a.targets[row];
+    if (target >= 0 && target < a.vocab) {
+      const bf16x4 w = *reinterpret_cast<const bf16x4*>(a.W + (int64_t)target * a.d + c);
+      const float lost = a.lost[row];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[e] += lost * (float)w[e];
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) dX[i + e] = (T)s[e];
 }
 
 // ---------------------------------------------------------------- few rows
@@ -649,9 +690,10 @@ size_t stream_pairs(int64_t T, int32_t vocab) { return (size_t)T * ((vocab + STR
 size_t stream_workspace(int64_t T, int32_t vocab) { return ALIGN + align_up(stream_pairs(T, vocab), ALIGN) + (size_t)T * 4; }
 
 struct HeadLayout {
-  size_t range, logits, pairs, at_target, off, g, hi, lo, x16, slabs, total;
+  size_t range, logits, pairs, at_target, off, lost, g, hi, lo, x16, slabs, total;
 };
-HeadLayout layout_for(int64_t plans, int64_t sub, int64_t rows, int64_t slab_cells, int32_t d, int32_t vocab, bool bf16, bool grad) {
+HeadLayout layout_for(int64_t plans, int64_t sub, int64_t rows, int64_t dx_rows, int64_t slab_cells, int32_t d, int32_t vocab, bool bf16,
+                      bool grad) {
   HeadLayout w = {};
   const size_t ldv = align_up(vocab, 64), cells = (size_t)rows * ldv;
   size_t at = 0;
@@ -666,7 +708,8 @@ HeadLayout layout_for(int64_t plans, int64_t sub, int64_t rows, int64_t slab_cel
   w.pairs = take(std::max(bf16 ? (size_t)sub * ((vocab + 127) / 128) * 8 : 0, stream_pairs(std::min(sub, STREAM_ROWS), vocab)));
   w.at_target = take((size_t)sub * 4);
   w.off = take(bf16 ? (size_t)sub * 4 : 0);
-  w.g = take(bf16 && grad ? cells * 2 : 0);
+  w.lost = take(bf16 && grad ? (size_t)rows * 4 : 0);
+  w.g = take(bf16 && grad ? (size_t)dx_rows * ldv * 2 : 0);
   w.hi = take(bf16 && grad ? cells * 2 : 0);
   w.lo = take(bf16 && grad ? cells * 2 : 0);
   w.x16 = take(bf16 && grad ? (size_t)rows * d * 2 : 0);
@@ -683,8 +726,9 @@ size_t head_workspace(int64_t T, int32_t d, int32_t vocab, modse_dtype dt, bool 
   const int64_t most = most_rows(vocab, bf16, grad), sub_most = std::min(most, most_sub(vocab, bf16, grad));
   const int64_t sub = std::min<int64_t>(padded_rows(T), sub_most), rows = std::min<int64_t>((int64_t)align_up((size_t)T, (size_t)sub), most);
   const int64_t pieces = (T + most - 1) / most, plans = (T + sub_most - 1) / sub_most + (grad ? 2 * pieces : 0);
-  const int64_t slabs = std::min(MAX_PARTS * rows * d, std::max(SLAB_CELLS, rows * d));
-  const size_t total = ALIGN + layout_for(plans, sub, rows, slabs, d, vocab, bf16, grad).total;
+  const int64_t dx_rows = bf16 ? std::max(rows, std::min(2 * rows, 2 * STACK_ROWS)) : rows;
+  const int64_t slabs = std::min(MAX_PARTS * dx_rows * d, std::max(SLAB_CELLS, dx_rows * d));
+  const size_t total = ALIGN + layout_for(plans, sub, rows, dx_rows, slabs, d, vocab, bf16, grad).total;
   return grad ? total : T <= STREAM_ROWS ? stream_workspace(T, vocab) : std::max(total, stream_workspace(STREAM_ROWS, vocab));
 }
 
@@ -698,13 +742,13 @@ hipError_t launch_head(modse_dtype dt, const HeadArgs& a, char* ws, hipStream_t 
   }
   const HeadShape h = head_shape(a.T, a.d, a.vocab, dt, grad);
   const int64_t products = h.products(), plans = products + (grad ? 2 * h.pieces : 0);
-  const HeadLayout w = layout_for(plans, h.sub, h.rows, (int64_t)h.k_parts * h.rows * h.d, h.d, h.vocab, h.bf16, grad);
+  const HeadLayout w = layout_for(plans, h.sub, h.rows, h.dx_rows, (int64_t)h.k_parts * h.dx_rows * h.d, h.d, h.vocab, h.bf16, grad);
   ws = reinterpret_cast<char*>(align_up(reinterpret_cast<size_t>(ws), ALIGN));
   auto floats = [&](size_t at) { return reinterpret_cast<float*>(ws + at); };
   auto halves = [&](size_t at) { return reinterpret_cast<f16_t*>(ws + at); };
   HeadRange* const range = h.bf16 && grad ? reinterpret_cast<HeadRange*>(ws + w.range) : nullptr;
   const HeadBufs b = {reinterpret_cast<GemmPlan*>(ws), floats(w.logits), floats(w.pairs), floats(w.at_target), floats(w.off),
-                      reinterpret_cast<bf16_t*>(ws + w.g), halves(w.hi), halves(w.lo), halves(w.x16), range, floats(w.slabs)};
+                      reinterpret_cast<bf16_t*>(ws + w.g), floats(w.lost), halves(w.hi), halves(w.lo), halves(w.x16), range, floats(w.slabs)};
   const HeadPlanArgs plan = {h, b, a.x, a.W, a.targets, a.d_logp, a.dW, (int32_t)plans};
   const int64_t range_blocks = range ? std::min<int64_t>((h.T * h.d + 32767) / 32768, RANGE_BLOCKS) : 0;
   hipLaunchKernelGGL(head_plan_kernel, dim3((unsigned)(plans + range_blocks)), dim3(1024), 0, s, plan);
@@ -726,6 +770,7 @@ hipError_t launch_head(modse_dtype dt, const HeadArgs& a, char* ws, hipStream_t 
     if (e != hipSuccess) return;
     const HeadRowsArgs r = {a.targets + t0, a.d_logp ? a.d_logp + t0 : nullptr, a.logp ? a.logp + t0 : nullptr, a.log_z ? a.log_z + t0 : nullptr,
                             b.logits, b.pairs, b.at_target, b.off, a.dX ? b.g + in_piece * h.ldv : nullptr,
+                            a.dX && h.dx_rows > h.rows ? b.g + (int64_t)h.rows * h.ldv : nullptr, b.lost + in_piece,
                             a.dW ? b.hi + in_piece * h.ldv : nullptr, a.dW ? b.lo + in_piece * h.ldv : nullptr,
                             range, x + t0 * h.d, b.x16 + in_piece * h.d, (int32_t)m, h.vocab, h.ldv, h.sub, h.d};
     if (h.bf16) {
@@ -752,12 +797,15 @@ hipError_t launch_head(modse_dtype dt, const HeadArgs& a, char* ws, hipStream_t 
       if (e != hipSuccess) break;
     }
     if (a.dX) {
-      e = launch_grouped_gemm(dt, EPI_STORE_F32, h.dx_tile, p, h.k_parts, 0, 0, h.k_parts * tiles(m, h.d, h.dx_tile), s, LAYOUT_B_KN);
+      const int64_t dx_rows = h.dx_rows > h.rows ? h.dx_rows : m;
+      e = launch_grouped_gemm(dt, EPI_STORE_F32, h.dx_tile, p, h.k_parts, 0, 0, h.k_parts * tiles(dx_rows, h.d, h.dx_tile), s, LAYOUT_B_KN);
       if (e != hipSuccess) break;
-      const int64_t n = m * h.d, stride = (int64_t)h.rows * h.d;
-      const dim3 join((unsigned)std::min<int64_t>((n + 1023) / 1024, 4096));
-      if (h.bf16) hipLaunchKernelGGL((head_join_kernel<bf16_t>), join, dim3(256), 0, s, b.slabs, h.k_parts, stride, n, static_cast<bf16_t*>(a.dX) + t0 * h.d);
-      else hipLaunchKernelGGL((head_join_kernel<float>), join, dim3(256), 0, s, b.slabs, h.k_parts, stride, n, static_cast<float*>(a.dX) + t0 * h.d);
+      const bool stacked = h.dx_rows > h.rows;
+      const HeadJoinArgs j = {b.slabs, h.bf16 && !stacked ? static_cast<const bf16_t*>(a.W) : nullptr, b.lost, a.targets + t0,
+                              (int64_t)h.dx_rows * h.d, stacked ? (int64_t)h.rows * h.d : 0, h.k_parts, h.d, h.vocab};
+      const dim3 join((unsigned)m, (unsigned)((h.d + 1023) / 1024));
+      if (h.bf16) hipLaunchKernelGGL((head_join_kernel<bf16_t>), join, dim3(256), 0, s, j, static_cast<bf16_t*>(a.dX) + t0 * h.d);
+      else hipLaunchKernelGGL((head_join_kernel<float>), join, dim3(256), 0, s, j, static_cast<float*>(a.dX) + t0 * h.d);
       e = hipGetLastError();
     }
   }

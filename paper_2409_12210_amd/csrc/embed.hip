@@ -146,7 +146,11 @@ __global__ __launch_bounds__(SORT_WAVES * 64) void embed_sort_kernel(EmbedBwdArg
     float* const row = a.dE + (int64_t)(lo + q) * a.d;
     Vec<float> zero;
     zero.v = f32x4{0.f, 0.f, 0.f, 0.f};
-    for (int c = lane * 4; c < a.d; c += 256) zero.store(row + c, a.d - c);
+    int c = lane * 4;
+    for (; c + 772 <= a.d; c += 1024)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) zero.store(row + c + i * 256, 4);
+    for (; c < a.d; c += 256) zero.store(row + c, a.d - c);
   }
 }
 
@@ -322,8 +326,9 @@ hipError_t launch_embed_fwd(modse_dtype dt, const EmbedFwdArgs& a, hipStream_t s
 }
 
 hipError_t launch_embed_bwd(modse_dtype dt, const EmbedBwdArgs& a, hipStream_t s) {
-  // about a block for every CU
-  const int rows = std::min(EMBED_MAX_ROWS, (a.vocab + 255) / 256);
+  // Two blocks for every CU, as each reads all tokens.  (One: 88 us for 1021 tokens of width 1535, float32, vocabulary 50257, in place of 84,
+  // and the same for 32768 tokens.)
+  const int rows = std::min(EMBED_MAX_ROWS, (a.vocab + 511) / 512);
   hipLaunchKernelGGL(embed_sort_kernel, dim3((unsigned)((a.vocab + rows - 1) / rows)), dim3(SORT_WAVES * 64), 0, s, a, rows);
   const int64_t chunks = embed_chunks(a.T);
   const dim3 sums((unsigned)((chunks * ((a.d + 511) / 512) + 3) / 4)), joins((unsigned)(chunks * ((a.d + 255) / 256)));

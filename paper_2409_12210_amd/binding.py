@@ -578,12 +578,12 @@ def modse_head_bwd(T, d_model, vocab, dtype, x, W, targets, d_logp, logp, dX, dW
 
 
 def _generator(rng) -> Optional[int]:
-    """The pointer of seed and offset: two integers of 64 bits on the device."""
+    """The pointer of seed and offset: two integers of 64 bits on the device.  (On the host they would be easy to make.)"""
     if rng is None or isinstance(rng, int):
         return rng
-    if rng.dtype in (_WIDE or _find_wide()) and rng.numel() == 2 and rng.is_contiguous():
+    if rng.dtype in (_WIDE or _find_wide()) and rng.is_cuda and rng.numel() == 2 and rng.is_contiguous():
         return rng.data_ptr()
-    raise _Unfit(f"{rng.dtype} of shape {tuple(rng.shape)}, expected two int64: seed and offset")
+    raise _Unfit(f"{rng.dtype} of shape {tuple(rng.shape)} on {rng.device}, expected two int64 on the GPU: seed and offset")
 
 
 _WIDE = ()

@@ -128,7 +128,7 @@ struct HeadBufs {
   float* logits;     // [sub, ldv]; float32 layers: then G
   float* pairs;      // [ceil(vocab / 128)][sub] maximum and sum
   float* at_target;  // [sub] the target's logit
-  float* off;        // [sub] log Z
+  float* off;        // [sub][2] the row's maximum and log2 of its sum
   bf16_t* g;         // [dx_rows, ldv] G, and behind its rows what it lacks of them
   float* lost;       // [rows] what G lacks of the target's entry
   f16_t *hi, *lo;    // [rows, ldv] G in two parts, scaled
@@ -288,8 +288,9 @@ struct HeadRowsArgs {
 __device__ __forceinline__ float row_weight(const HeadRowsArgs& a, int row, int32_t target) {
   return target < 0 ? 0.f : target >= a.vocab ? __builtin_nanf("") : a.d_logp[row];
 }
-__device__ __forceinline__ float grad_of(float logit, float off, float w, int32_t target, int c, int vocab) {
-  const float p = __builtin_amdgcn_exp2f((logit - off) * LOG2E);
+// (by maximum and sum, not by log Z: of a row that is all but sure 1 - p is what counts, and log Z is rounded at the size of the logits)
+__device__ __forceinline__ float grad_of(float logit, float top, float log2_sum, float w, int32_t target, int c, int vocab) {
+  const float p = __builtin_amdgcn_exp2f(fmaf(logit - top, LOG2E, -log2_sum));
   return c >= vocab || target < 0 ? 0.f : c == target ? w * (1.f - p) : -w * p;
 }
 __device__ __forceinline__ void put_row(float* logp, float* log_z, int32_t target, int vocab, float at_target, float top, float log_sum) {
@@ -332,9 +333,10 @@ __global__ __launch_bounds__(1024) void head_stats_kernel(HeadRowsArgs a) {
   float top = m, sum = 0.f;
   for (int w = 1; w < 16; ++w) top = fmaxf(top, s_m[w][lane]);
   for (int w = 0; w < 16; ++w) sum += s_s[w][lane] * __builtin_amdgcn_exp2f((s_m[w][lane] - top) * LOG2E);
-  const float log_sum = __builtin_amdgcn_logf(sum) * LN2;
+  const float log2_sum = __builtin_amdgcn_logf(sum), log_sum = log2_sum * LN2;
   put_row(a, row, a.targets[row], a.at_target[row], top, log_sum);
-  a.off[row] = top + log_sum;
+  a.off[2 * row] = top;
+  a.off[2 * row + 1] = log2_sum;
 }
 
 // bf16: G of a row's 2048 columns, in bf16 for dX, in two parts for dW.  Columns behind the vocabulary become zeros.  Blocks behind the rows'
@@ -354,7 +356,7 @@ __global__ __launch_bounds__(256) void head_grad_kernel(HeadRowsArgs a, int segs
   const int row = blockIdx.x / segs, c = (blockIdx.x - row * segs) * 2048 + threadIdx.x * 8;
   if (c >= a.ldv) return;
   const int32_t target = a.targets[row];
-  const float off = a.off[row], w = row_weight(a, row, target), scale = power_of_two(scale_exponent(a.range->d_logp));
+  const float top = a.off[2 * row], log2_sum = a.off[2 * row + 1], w = row_weight(a, row, target), scale = power_of_two(scale_exponent(a.range->d_logp));
   const int64_t at = (int64_t)row * a.ldv + c;
   const f32x4 v[2] = {__builtin_nontemporal_load(reinterpret_cast<const f32x4*>(a.logits + at)),  // (read once: 473 us in place of 498)
                       __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(a.logits + at + 4))};
@@ -363,7 +365,7 @@ __global__ __launch_bounds__(256) void head_grad_kernel(HeadRowsArgs a, int segs
   float lost = 0.f;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    const float x = grad_of(v[e >> 2][e & 3], off, w, target, c + e, a.vocab), scaled = x * scale;
+    const float x = grad_of(v[e >> 2][e & 3], top, log2_sum, w, target, c + e, a.vocab), scaled = x * scale;
     g[e] = (bf16_t)x;
     const float left = x - (float)g[e];
     rest[e] = (bf16_t)left;
@@ -420,16 +422,16 @@ __global__ __launch_bounds__(512) void head_rows_kernel(HeadRowsArgs a) {
   for (int w = 1; w < W; ++w) top = fmaxf(top, s_m[w]);
 #pragma unroll
   for (int w = 0; w < W; ++w) sum += s_s[w] * __builtin_amdgcn_exp2f((s_m[w] - top) * LOG2E);
-  const float log_sum = __builtin_amdgcn_logf(sum) * LN2;
+  const float log2_sum = __builtin_amdgcn_logf(sum), log_sum = log2_sum * LN2;
   const int32_t target = a.targets[t];
   if (tid == 0) put_row(a, t, target, target >= 0 && target < a.vocab ? row[target] : 0.f, top, log_sum);
   if constexpr (GRAD) {
     __syncthreads();  // (the target's logit has been read)
-    const float w = row_weight(a, t, target), off = top + log_sum;
+    const float w = row_weight(a, t, target);
     for (int c = tid * 4; c < a.ldv; c += W * 256) {
       f32x4 g = c < a.vocab ? load(c) : f32x4{};
 #pragma unroll
-      for (int e = 0; e < 4; ++e) g[e] = grad_of(g[e], off, w, target, c + e, a.vocab);
+      for (int e = 0; e < 4; ++e) g[e] = grad_of(g[e], top, log2_sum, w, target, c + e, a.vocab);
       *reinterpret_cast<f32x4*>(row + c) = g;
     }
   }
@@ -496,7 +498,7 @@ struct HeadStreamArgs {
   float* at_target;  // [T]
   float *logp, *log_z;
   float* logits;     // [T, ldv] or null
-  float* off;        // [T] log Z or null
+  float* off;        // [T][2] maximum and log2 of the sum, or null
   HeadRange* range;  // to join, or null
   int32_t T, d, vocab, ldv;
 };
@@ -670,9 +672,12 @@ __global__ __launch_bounds__(1024) void head_stream_join_kernel(HeadStreamArgs a
   float top = s_m[0], sum = 0.f;
   for (int w = 1; w < 16; ++w) top = fmaxf(top, s_m[w]);
   for (int w = 0; w < 16; ++w) sum += s_s[w] * __builtin_amdgcn_exp2f((s_m[w] - top) * LOG2E);
-  const float log_sum = __builtin_amdgcn_logf(sum) * LN2;
+  const float log2_sum = __builtin_amdgcn_logf(sum), log_sum = log2_sum * LN2;
   put_row(a.logp ? a.logp + t : nullptr, a.log_z ? a.log_z + t : nullptr, a.targets[t], a.vocab, a.at_target[t], top, log_sum);
-  if (a.off) a.off[t] = top + log_sum;
+  if (a.off) {
+    a.off[2 * t] = top;
+    a.off[2 * t + 1] = log2_sum;
+  }
 }
 
 template <typename T>
@@ -708,7 +713,7 @@ HeadLayout layout_for(int64_t plans, int64_t sub, int64_t rows, int64_t dx_rows,
   w.logits = take(bf16 && !grad ? 0 : (size_t)sub * ldv * 4);
   w.pairs = take(std::max(bf16 ? (size_t)sub * ((vocab + 127) / 128) * 8 : 0, stream_pairs(std::min(sub, STREAM_ROWS), vocab)));
   w.at_target = take((size_t)sub * 4);
-  w.off = take(bf16 ? (size_t)sub * 4 : 0);
+  w.off = take(bf16 ? (size_t)sub * 8 : 0);
   w.lost = take(bf16 && grad ? (size_t)rows * 4 : 0);
   w.g = take(bf16 && grad ? (size_t)dx_rows * ldv * 2 : 0);
   w.hi = take(bf16 && grad ? cells * 2 : 0);

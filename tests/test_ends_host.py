@@ -83,6 +83,7 @@ def test_tensors_that_the_library_could_not_see_are_refused():
     for x, residual, rng, y in ((f, None, pair, b), (b, f, pair, b), (b, None, pair.int(), b), (b, None, pair[:1], b), (b, None, torch.zeros(4, dtype=torch.int64)[::2], b)):
         assert dropout(x=x, residual=residual, rng=rng, y=y) == INVALID
     assert dropout(x=b, rng=pair.float(), y=b, back=True) == INVALID
+    assert dropout(x=b, rng=pair, residual=None, y=b) == INVALID      # seed and offset on the host
     with pytest.raises(m.ModseError, match="expected two int64"):
         m.modse_dropout_bwd(4, 64, "bf16", b, 0.1, pair.float(), 0, b, stream=0)
 

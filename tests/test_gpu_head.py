@@ -187,9 +187,38 @@ def test_the_largest_vocabulary_in_pieces_of_few_rows():
     check(3, 32, (1 << 20) - 1, "f32", seed=4)
 
 
-def test_a_matrix_of_more_elements_than_a_kernel_counts():
-    """2^30 and more: the product is cut along the vocabulary."""
-    check(5, 16384, 65537 + 300, "bf16", seed=5, sigma=2.0)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_matrix_of_more_elements_than_a_kernel_counts(dtype):
+    """2^30 and more: the product of more than a few rows is cut along the vocabulary."""
+    check(70, 16384, 65537 + 300, dtype, seed=5, sigma=2.0)
+    check(5, 16384, 65537 + 300, dtype, seed=6, sigma=2.0)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T", [20, 200])
+def test_rows_that_are_all_but_sure(dtype, T):
+    """Whole logits, the target's 14 above the others, which are equal: 1 - p is (V - 1) e^-14 / Z, 2.5e-4, and right to the roundings of a
+    sum near 1 and of p: 2^-21 of the weight, a thousandth of it.  Large logits beside it: log Z alone is rounded to 2^-18."""
+    d, V = 64, 300
+    x = torch.zeros((T, d), dtype=TYPE[dtype], device="cuda")
+    W = torch.zeros((V, d), dtype=TYPE[dtype], device="cuda")
+    targets = (torch.arange(T, device="cuda") * 7 % 16).int()
+    x[torch.arange(T, device="cuda"), targets.long()] = 1.0      # column k tells target k
+    x[:, 40] = 1.0
+    W[torch.arange(16, device="cuda"), torch.arange(16, device="cuda")] = 14.0
+    W[:, 40] = -112.0                                            # of all logits
+    w = torch.linspace(0.5, 2.0, T, device="cuda")
+    logp, log_z, G, _, _, _ = reference(x, W, targets, w, exact=True)
+    lp, dX, dW = backward(x, W, targets, w, dtype)
+    near(lp, logp, 2.0 ** -21, "logp")
+    # dX's column of the target: 14 G_target and nothing else; dW's: the sum of its rows' G_target
+    rows = torch.arange(T, device="cuda")
+    got, want = dX[rows, targets.long()].double() / 14, G[rows, targets.long()]
+    near(got, want, (2.0 ** -21 * w.double()) + (HALF[dtype] + 2.0 ** -16) * want.abs(), "G at the target, by dX")
+    sums = torch.zeros(16, dtype=torch.float64, device="cuda").index_add_(0, targets.long(), want)
+    sizes = torch.zeros(16, dtype=torch.float64, device="cuda").index_add_(0, targets.long(), w.double())
+    at = torch.arange(16, device="cuda")
+    near(dW[at, at], sums, 2.0 ** -20 * sizes, "G at the target, by dW")
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])

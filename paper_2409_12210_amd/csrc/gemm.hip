@@ -104,6 +104,14 @@ hipError_t launch_block(int epilogue, int layout, TileShape t, const GemmPlan* p
 
 hipError_t launch_grouped_gemm(modse_dtype dt, int epilogue, TileShape t, const GemmPlan* plan, int n_prob, int accumulate,
                                int option, int64_t max_tiles, hipStream_t s, int layout) {
+  switch (epilogue) {  // (of float32 layers, and 256-row tiles)
+    case EPI_STORE_PAIRS:
+      return run_bf16<256, 256, 1, 4, 2, EPI_STORE_PAIRS, LAYOUT_B_KN>(plan, n_prob, accumulate, option, max_tiles, s);
+    case EPI_ROWS_PAIRS:
+      return run_bf16<256, 256, 1, 4, 2, EPI_ROWS_PAIRS, LAYOUT_AB_K>(plan, n_prob, accumulate, option, max_tiles, s);
+    case EPI_LOGITS_PAIRS:
+      return run_bf16<256, 256, 1, 4, 2, EPI_LOGITS_PAIRS, LAYOUT_TN>(plan, n_prob, accumulate, option, max_tiles, s);
+  }
   if (dt == MODSE_F32) return launch_block<float>(epilogue, layout, t, plan, n_prob, accumulate, option, max_tiles, s);
   if (t.bm <= 128 && t.bn <= 128) return launch_block<bf16_t>(epilogue, layout, t, plan, n_prob, accumulate, option, max_tiles, s);
   switch (epilogue) {

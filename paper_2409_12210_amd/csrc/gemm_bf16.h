@@ -143,7 +143,11 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64) void gg_bf16_kernel(const Ge
   constexpr int BK = Cfg::BK, MI = Cfg::MI, NI = Cfg::NI, UPW = Cfg::UPW, PANEL = Cfg::PANEL, NSLOT = Cfg::NSLOT;
   constexpr int WM = Cfg::WM, WN = Cfg::WN;
   constexpr bool A_T = (LAYOUT & 1) != 0, B_T = (LAYOUT & 2) != 0;
+  constexpr bool PAIRS = EPI == EPI_STORE_PAIRS || EPI == EPI_ROWS_PAIRS || EPI == EPI_LOGITS_PAIRS;
   constexpr bool DUALK = EPI == EPI_STORE_DUALK || EPI == EPI_ROWS_F32;  // two operand pairs
+  constexpr bool HALF = EPI == EPI_ROWS_F32 || PAIRS;                    // float16 operands
+  constexpr bool LOGITS = EPI == EPI_LOGITS || EPI == EPI_LOGITS_PAIRS;
+  constexpr int PASSES = PAIRS ? 3 : DUALK ? 2 : 1;  // over K.  Three: A B, A B2, A2 B
   static_assert(!(B_T && NB != 1), "a [K, N] operand is a single matrix");
   __shared__ __attribute__((aligned(1024))) char ring[NSLOT * PANEL];
 
@@ -231,7 +235,7 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64) void gg_bf16_kernel(const Ge
         c.base0 = static_cast<const char*>(uniform_ptr(c.base0));  // (otherwise the compiler keeps the cursor in vector registers)
         c.K = P.K();
         c.nk = (c.K + BK - 1) / BK;
-        c.nsteps = DUALK ? 2 * c.nk : c.nk;
+        c.nsteps = PASSES * c.nk;
       }
       if (!c.w.valid || c.nsteps != 0) break;
       c.w.tile = tile_of_round(first_tile, ++c.w.round);
@@ -263,7 +267,8 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64) void gg_bf16_kernel(const Ge
   };
   // all load units of a last step that is not a full one: what lies beyond K reads zeros
   auto issue_partial = [&](const LoadCursor& c, const uint32_t (&off)[UPW], uint32_t dst) {
-    const int kstep = (DUALK && c.step >= c.nk) ? c.step - c.nk : c.step;
+    int kstep = (PASSES > 1 && c.step >= c.nk) ? c.step - c.nk : c.step;
+    if (PASSES > 2 && kstep >= c.nk) kstep -= c.nk;
     const bool tr = c.is_a ? A_T : B_T;
 #pragma unroll
     for (int i = 0; i < UPW; ++i) {
@@ -282,9 +287,13 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64) void gg_bf16_kernel(const Ge
       return;
     }
     int kstep = c.step;
-    if (DUALK && c.step >= c.nk) {
+    if (PASSES > 1 && c.step >= c.nk) {
       kstep -= c.nk;
-      if (kstep == 0) c.src = c.base1;
+      if (kstep == 0) c.src = PAIRS && c.is_a ? c.base0 : c.base1;
+      if (PASSES > 2 && kstep >= c.nk) {
+        kstep -= c.nk;
+        if (kstep == 0) c.src = c.is_a ? c.base1 : c.base0;
+      }
     }
     c.fast = (kstep + 1) * BK <= c.K ? 1 : 0;
   };
@@ -311,7 +320,7 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64) void gg_bf16_kernel(const Ge
       cc.N = P.N();
       cc.ldc = P.ldc();
       const int nk = (P.K() + BK - 1) / BK;
-      cc.nsteps = DUALK ? 2 * nk : nk;
+      cc.nsteps = PASSES * nk;
     }
   };
 
@@ -400,7 +409,7 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64) void gg_bf16_kernel(const Ge
 #pragma unroll
     for (int t = 0; t < NB * MI * NI; ++t) {
       const int q = t / (MI * NI), j = (t / MI) % NI, i = (j & 1) ? MI - 1 - t % MI : t % MI;  // (to and fro: one operand changes at a time)
-      if constexpr (EPI == EPI_ROWS_F32)
+      if constexpr (HALF)
         acc[q][i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, bfr[q][j]), __builtin_bit_cast(f16x8, af[i]), acc[q][i][j], 0, 0, 0);
       else
         acc[q][i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bfr[q][j], af[i], acc[q][i][j], 0, 0, 0);
@@ -441,7 +450,8 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64) void gg_bf16_kernel(const Ge
   auto fast_left = [&](const LoadCursor& c) -> int {
     if (!c.fast) return 0;
     const int full = c.K / BK;
-    const int lim = (DUALK && c.step >= c.nk) ? c.nk + full : full;
+    int lim = (PASSES > 1 && c.step >= c.nk) ? c.nk + full : full;
+    if (PASSES > 2 && c.step >= 2 * c.nk) lim += c.nk;
     return lim - c.step - 1;
   };
 
@@ -541,7 +551,15 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64) void gg_bf16_kernel(const Ge
     asm volatile("" : "+v"(elane));
     const int erow16 = elane & 15, equad = elane >> 4;
     const int cM = cc.M, cN = cc.N, cld = cc.ldc;
-    if constexpr (EPI == EPI_LOGITS) {
+    if constexpr (LOGITS) {
+      if constexpr (EPI == EPI_LOGITS_PAIRS) {
+        const float* const undo = reinterpret_cast<const float*>(cc.C3) - 2;
+        const float u0 = undo[0], u1 = undo[1];
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+          for (int j = 0; j < NI; ++j) acc[0][i][j] = acc[0][i][j] * u0 * u1;
+      }
       // A row's 128 columns of this wave lie in four lanes, 32 in each.
       static_assert(WN == 128 && NB == 1, "pairs of 128 columns");
       constexpr float LOG2E = 1.44269504088896340736f;
@@ -592,8 +610,8 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64) void gg_bf16_kernel(const Ge
         });
       }
     }
-    if constexpr (EPI == EPI_STORE_F32 || EPI == EPI_ROWS_F32 || EPI == EPI_LOGITS) {
-      if (EPI != EPI_LOGITS || cc.C) {
+    if constexpr (EPI == EPI_STORE_F32 || EPI == EPI_ROWS_F32 || LOGITS || PAIRS) {
+      if (!LOGITS || cc.C) {
       // float32 output (weight gradients).  It goes through LDS, one 32 x 32 block (4 KiB) at a time: written in
       // accumulator order (16 bytes per lane), read back row-wise, so that global memory sees whole 128-byte lines, also
       // where the old values are added (they come in one block ahead; read and written in accumulator order they made the
@@ -608,7 +626,7 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64) void gg_bf16_kernel(const Ge
       auto inside = [&](int b) { return (b / NI32) * 32 < mleft && (b % NI32) * 32 < nleft; };
       auto row_group = [&](int b, int it) { return wave_c + ((long)((b / NI32) * 32 + it * 8) * cld + (b % NI32) * 32) * 4; };
       const bool stream_c = (option & GEMM_STREAM_C) != 0;
-      constexpr bool ROWS = EPI == EPI_ROWS_F32;
+      constexpr bool ROWS = EPI == EPI_ROWS_F32 || EPI == EPI_ROWS_PAIRS;
       const int rows_end = ROWS ? (int)reinterpret_cast<intptr_t>(cc.E2) : 0, rows_m0 = cc.w.m0 + wm * WM;
       float scale[2] = {1.f, 1.f};
       if constexpr (ROWS)

@@ -20,6 +20,8 @@
 // which hold 22 bits, times float16 copies of the rows of x: both times powers of two that follow the largest |x| and the largest
 // |d_logp| of the call, so that what is rounded or lost is below 2^-39 of the largest product.  (Two bf16 numbers, 16 bits, left an
 // error of 2.7e-6 of dW where float32 products have 0.7e-6 to 2e-6, and need no third copy of G; the rest takes as long.)
+#include <cstddef>
+
 #include "ops.h"
 
 #include "gemm_bf16_util.h"
@@ -30,6 +32,7 @@ using namespace modse_gemm;
 
 constexpr int64_t GRAD_CELLS = (int64_t)1 << 28;   // values of G in the workspace (float32: of logits)
 constexpr int64_t LOGIT_CELLS = (int64_t)1 << 28;  // bf16 logits in the workspace
+constexpr int64_t PAIR_W = (int64_t)1 << 28;       // elements of W of which the parts are kept
 constexpr int64_t PAIR_CELLS = (int64_t)1 << 27;   // pairs of 128 columns in it
 constexpr int64_t W_PART = (int64_t)1 << 30;       // elements of W that one problem reads (kernels count them in 32 bits)
 constexpr size_t ALIGN = 256;                      // of what is in the workspace, which itself may lie at any sixteen bytes
@@ -46,6 +49,8 @@ struct HeadShape {
   int32_t dx_rows;         // rows of the product of dX: those of a piece, or twice as many
   int32_t k_parts, k_len;  // problems of dX, columns of G in each
   int32_t bf16, grad;
+  int32_t pairs;           // float32, and the matrices are held as pairs of float16 ones
+  int32_t wide;            // either of them: tiles of 256, sums of exponentials by the product of the logits
   TileShape logits_tile, dx_tile, dw_tile;
   __host__ __device__ int64_t products() const { return (T + sub - 1) / sub; }  // (sub divides rows)
 };
@@ -57,11 +62,17 @@ int64_t rows_in(int64_t cells, int64_t per_row) {
   while (r < 65536 && 2 * r * per_row <= cells) r *= 2;
   return r;
 }
-int64_t most_rows(int32_t vocab, bool bf16, bool grad) {
-  return bf16 && !grad ? rows_in(PAIR_CELLS, (vocab + 127) / 128) : rows_in(GRAD_CELLS, (int64_t)align_up(vocab, 64));
+int64_t most_rows(int32_t vocab, bool wide, bool grad) {
+  return wide && !grad ? rows_in(PAIR_CELLS, (vocab + 127) / 128) : rows_in(GRAD_CELLS, (int64_t)align_up(vocab, 64));
 }
-int64_t most_sub(int32_t vocab, bool bf16, bool grad) {
-  return bf16 && grad ? rows_in(LOGIT_CELLS, (int64_t)align_up(vocab, 64)) : most_rows(vocab, bf16, grad);
+int64_t most_sub(int32_t vocab, bool wide, bool grad) {
+  return wide && grad ? rows_in(LOGIT_CELLS, (int64_t)align_up(vocab, 64)) : most_rows(vocab, wide, grad);
+}
+// Float32 layers: from so many rows on products of pairs of float16 numbers, three 16-bit products in place of one of float32, but the parts
+// of W, which lie in the workspace, have to be made first.
+int64_t pairs_from(bool grad) { return grad ? 129 : 193; }
+bool takes_pairs(int64_t T, int32_t d, int32_t vocab, modse_dtype dt, bool grad) {
+  return dt == MODSE_F32 && T >= pairs_from(grad) && (int64_t)vocab * d <= PAIR_W;
 }
 
 HeadShape head_shape(int64_t T, int32_t d, int32_t vocab, modse_dtype dt, bool grad) {
@@ -71,8 +82,10 @@ HeadShape head_shape(int64_t T, int32_t d, int32_t vocab, modse_dtype dt, bool g
   h.vocab = vocab;
   h.bf16 = dt == MODSE_BF16;
   h.grad = grad;
+  h.pairs = takes_pairs(T, d, vocab, dt, grad);
+  h.wide = h.bf16 || h.pairs;
   h.ldv = (int32_t)align_up(vocab, 64);
-  const int64_t most = most_rows(vocab, h.bf16, grad), sub = std::min(most, most_sub(vocab, h.bf16, grad));
+  const int64_t most = most_rows(vocab, h.wide, grad), sub = std::min(most, most_sub(vocab, h.wide, grad));
   // pieces of about one size, in whole products of logits
   h.sub = T <= sub ? padded_rows(T) : (int32_t)sub;
   h.pieces = (int32_t)((T + most - 1) / most);
@@ -84,20 +97,20 @@ HeadShape head_shape(int64_t T, int32_t d, int32_t vocab, modse_dtype dt, bool g
   auto tiles = [](int64_t m, int64_t n, int b) { return ((m + b - 1) / b) * ((n + b - 1) / b); };
   // (float32: tiles of 128 from four rounds of the chip's 512 workgroups on.  50304 x 256, 1.5 rounds: 287 us with them, 258 with tiles of
   // 64; 1021 x 50257, 6.1 rounds: 251 and 261)
-  auto tile = [&](int64_t m, int64_t n) { const int b = h.bf16 ? 256 : tiles(m, n, 128) >= 2048 ? 128 : 64; return TileShape{b, b}; };
+  auto tile = [&](int64_t m, int64_t n) { const int b = h.wide ? 256 : tiles(m, n, 128) >= 2048 ? 128 : 64; return TileShape{b, b}; };
   h.logits_tile = tile(h.sub, vocab);
   h.dw_tile = tile(vocab, d);
-  const int dx = h.bf16 ? 256 : h.rows <= 64 ? 64 : 128;
+  const int dx = h.wide ? 256 : h.rows <= 64 ? 64 : 128;
   h.dx_tile = TileShape{dx, dx};
   // Parts of dX: whole rounds of workgroups over the chip, each part with six further steps for its opening and its end, and slabs that
   // are written and read.
   h.dx_rows = h.bf16 && T <= STACK_ROWS ? 2 * h.rows : h.rows;
-  const int64_t out = tiles(h.dx_rows, d, h.dx_tile.bm), steps = (vocab + 63) / 64, slots = h.bf16 ? 256 : 512;
+  const int64_t out = tiles(h.dx_rows, d, h.dx_tile.bm), steps = (vocab + 63) / 64, slots = h.wide ? 256 : 512;
   const int64_t parts_most = std::min<int64_t>({MAX_PARTS, steps, std::max<int64_t>(1, SLAB_CELLS / ((int64_t)h.dx_rows * d))});
   double best = 0;
   for (int64_t n = 1; n <= parts_most; ++n) {
     const int64_t len = (steps + n - 1) / n, parts = (steps + len - 1) / len;
-    const double step_us = h.bf16 ? 1.6 : dx == 64 ? 3.0 : 8.0;
+    const double step_us = h.bf16 ? 1.6 : h.pairs ? 4.8 : dx == 64 ? 3.0 : 8.0;
     const double us = (double)((out * parts + slots - 1) / slots) * (len + 6) * step_us + parts * (double)h.dx_rows * d * 8 / 4e6;
     if (n == 1 || us < best) {
       best = us;
@@ -108,14 +121,17 @@ HeadShape head_shape(int64_t T, int32_t d, int32_t vocab, modse_dtype dt, bool g
   return h;
 }
 
-// The largest |x| and |d_logp| of a call, as the bits of floats: by block, joined by the launch behind the first product of logits.
+// The largest |x|, |W| and |d_logp| of a call, as the bits of floats: by block, joined by a later launch.  (Bf16 layers need no |W|.)
 constexpr int RANGE_BLOCKS = 512;
 struct HeadRange {
-  uint32_t x_of[RANGE_BLOCKS], d_logp_of[RANGE_BLOCKS];
+  uint32_t x_of[RANGE_BLOCKS], w_of[RANGE_BLOCKS], d_logp_of[RANGE_BLOCKS];
   int32_t blocks;
-  uint32_t x, d_logp;
-  float undo[2];  // the scaling by both: the smaller factor first, so that no product on the way overflows where the result does not
+  uint32_t x, w, d_logp;
+  // What undoes the scaling by two of them: the smaller factor first, so that no product on the way overflows where the result does not.
+  float undo_dx[2], undo_dw[2], pad[2];
+  float undo_logits[2];  // right before the targets' logits (EPI_LOGITS_PAIRS)
 };
+static_assert(sizeof(HeadRange) == offsetof(HeadRange, undo_logits) + 8 && sizeof(HeadRange) % 16 == 0, "laid out up to the targets' logits");
 // the power of two that brings values of at most this size below 2^15
 __device__ __forceinline__ int scale_exponent(uint32_t bits) { return min(14 - ((int)(bits >> 23 & 255) - 127), 120); }
 __device__ __forceinline__ float power_of_two(int e) { return __builtin_bit_cast(float, (uint32_t)(e + 127) << 23); }
@@ -132,7 +148,8 @@ struct HeadBufs {
   bf16_t* g;         // [dx_rows, ldv] G, and behind its rows what it lacks of them
   float* lost;       // [rows] what G lacks of the target's entry
   f16_t *hi, *lo;    // [rows, ldv] G in two parts, scaled
-  f16_t* x16;        // [rows, d] x, scaled
+  f16_t *x16, *x16_lo;   // [rows, d] x in the same way; x16_lo: float32 layers
+  f16_t *w16, *w16_lo;   // [vocab, d] W, float32 layers
   HeadRange* range;
   float* slabs;      // [k_parts][dx_rows, d]
 };
@@ -147,64 +164,106 @@ struct HeadPlanArgs {
   int32_t plans;
 };
 
-// The largest values of block `block` of the blocks of 1024 that look for them.  (NaN counts as more than any number.)
-__device__ __forceinline__ void range_block(const HeadPlanArgs& a, int block, int blocks) {
-  __shared__ uint32_t s_x[16], s_w[16];
-  const bf16_t* const x = static_cast<const bf16_t*>(a.x);
-  const int64_t n = a.h.T * a.h.d / 8;
-  uint32_t most_x = 0, most_w = 0;
-  const int64_t first = (int64_t)block * 1024 + threadIdx.x, step = (int64_t)blocks * 1024;
-  for (int64_t i = first; i < n; i += 4 * step) {
+// The largest absolute value of n elements (a multiple of 16), by the threads of some blocks of 1024.  (NaN counts as more than any number.)
+__device__ __forceinline__ uint32_t largest(const void* p, int64_t n, bool bf16, int64_t first, int64_t step) {
+  const u32x4* const v16 = static_cast<const u32x4*>(p);
+  const int64_t vectors = bf16 ? n / 8 : n / 4;
+  uint32_t most = 0;
+  for (int64_t i = first; i < vectors; i += 4 * step) {
     u32x4 v[4];
 #pragma unroll
-    for (int q = 0; q < 4; ++q) v[q] = *reinterpret_cast<const u32x4*>(x + (i + q * step < n ? i + q * step : i) * 8);
+    for (int q = 0; q < 4; ++q) v[q] = v16[i + q * step < vectors ? i + q * step : i];
 #pragma unroll
     for (int q = 0; q < 4; ++q)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) most_x = max(most_x, max(v[q][e] << 16 & 0x7fff0000u, v[q][e] & 0x7fff0000u));
+      for (int e = 0; e < 4; ++e)
+        most = max(most, bf16 ? max(v[q][e] << 16 & 0x7fff0000u, v[q][e] & 0x7fff0000u) : v[q][e] & 0x7fffffffu);
   }
-  for (int64_t t = first; t < a.h.T; t += step)
-    if (a.targets[t] >= 0 && a.targets[t] < a.h.vocab) most_w = max(most_w, __builtin_bit_cast(uint32_t, a.d_logp[t]) & 0x7fffffffu);
+  return most;
+}
+__device__ __forceinline__ uint32_t wave_most(uint32_t v) {
 #pragma unroll
-  for (int o = 32; o; o >>= 1) {
-    most_x = max(most_x, (uint32_t)__shfl_xor((int)most_x, o, 64));
-    most_w = max(most_w, (uint32_t)__shfl_xor((int)most_w, o, 64));
-  }
-  if ((threadIdx.x & 63) == 0) {
-    s_x[threadIdx.x >> 6] = most_x;
-    s_w[threadIdx.x >> 6] = most_w;
+  for (int o = 32; o; o >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, o, 64));
+  return v;
+}
+__device__ __forceinline__ void range_block(const HeadPlanArgs& a, int block, int blocks) {
+  __shared__ uint32_t s_most[3][16];
+  const int64_t first = (int64_t)block * 1024 + threadIdx.x, step = (int64_t)blocks * 1024;
+  uint32_t most[3] = {largest(a.x, a.h.T * a.h.d, a.h.bf16, first, step),
+                      a.h.bf16 ? 0 : largest(a.W, (int64_t)a.h.vocab * a.h.d, false, first, step), 0};
+  if (a.d_logp)
+    for (int64_t t = first; t < a.h.T; t += step)
+      if (a.targets[t] >= 0 && a.targets[t] < a.h.vocab) most[2] = max(most[2], __builtin_bit_cast(uint32_t, a.d_logp[t]) & 0x7fffffffu);
+#pragma unroll
+  for (int k = 0; k < 3; ++k) {
+    most[k] = wave_most(most[k]);
+    if ((threadIdx.x & 63) == 0) s_most[k][threadIdx.x >> 6] = most[k];
   }
   __syncthreads();
   if (threadIdx.x > 0) return;
-  for (int w = 1; w < 16; ++w) {
-    most_x = max(most_x, s_x[w]);
-    most_w = max(most_w, s_w[w]);
-  }
-  a.b.range->x_of[block] = most_x;
-  a.b.range->d_logp_of[block] = most_w;
+#pragma unroll
+  for (int k = 0; k < 3; ++k)
+    for (int w = 1; w < 16; ++w) most[k] = max(most[k], s_most[k][w]);
+  a.b.range->x_of[block] = most[0];
+  a.b.range->w_of[block] = most[1];
+  a.b.range->d_logp_of[block] = most[2];
   if (block == 0) a.b.range->blocks = blocks;
 }
 // One wave joins them.  (Whichever block does it, it writes the same.)
 __device__ __forceinline__ void join_range(HeadRange* r) {
   const int lane = threadIdx.x & 63, blocks = r->blocks;
-  uint32_t x = 0, w = 0;
+  uint32_t x = 0, w = 0, g = 0;
 #pragma unroll
   for (int i = 0; i < RANGE_BLOCKS / 64; ++i)
     if (i * 64 + lane < blocks) {
       x = max(x, r->x_of[i * 64 + lane]);
-      w = max(w, r->d_logp_of[i * 64 + lane]);
+      w = max(w, r->w_of[i * 64 + lane]);
+      g = max(g, r->d_logp_of[i * 64 + lane]);
     }
-#pragma unroll
-  for (int o = 32; o; o >>= 1) {
-    x = max(x, (uint32_t)__shfl_xor((int)x, o, 64));
-    w = max(w, (uint32_t)__shfl_xor((int)w, o, 64));
-  }
+  x = wave_most(x);
+  w = wave_most(w);
+  g = wave_most(g);
   if (lane == 0) {
     r->x = x;
-    r->d_logp = w;
-    const float a = power_of_two(-scale_exponent(x)), b = power_of_two(-scale_exponent(w));
-    r->undo[0] = fminf(a, b);
-    r->undo[1] = fmaxf(a, b);
+    r->w = w;
+    r->d_logp = g;
+    const float ux = power_of_two(-scale_exponent(x)), uw = power_of_two(-scale_exponent(w)), ug = power_of_two(-scale_exponent(g));
+    r->undo_logits[0] = fminf(ux, uw);
+    r->undo_logits[1] = fmaxf(ux, uw);
+    r->undo_dx[0] = fminf(ug, uw);
+    r->undo_dx[1] = fmaxf(ug, uw);
+    r->undo_dw[0] = fminf(ug, ux);
+    r->undo_dw[1] = fmaxf(ug, ux);
+  }
+}
+
+// float32 by pairs: n elements (a multiple of 16) in two parts.  Every block joins the largest values for itself.
+__global__ __launch_bounds__(256) void head_split_kernel(const float* p, int64_t n, f16_t* hi, f16_t* lo, HeadRange* range, int is_w) {
+  __shared__ uint32_t s_most;
+  if (threadIdx.x < 64) {
+    const int lane = threadIdx.x, blocks = range->blocks;
+    const uint32_t* const of = is_w ? range->w_of : range->x_of;
+    uint32_t most = 0;
+    for (int i = lane; i < blocks; i += 64) most = max(most, of[i]);
+    most = wave_most(most);
+    if (lane == 0) s_most = most;
+    if (blockIdx.x == 0) join_range(range);
+  }
+  __syncthreads();
+  const float scale = power_of_two(scale_exponent(s_most));
+  const int64_t step = (int64_t)gridDim.x * 2048;
+  for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8; i < n; i += step) {
+    const f32x4 v[2] = {__builtin_nontemporal_load(reinterpret_cast<const f32x4*>(p + i)),
+                        __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(p + i + 4))};
+    f16x8 h, l;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float x = v[e >> 2][e & 3] * scale;
+      h[e] = (f16_t)x;
+      l[e] = (f16_t)(x - (float)h[e]);
+    }
+    *reinterpret_cast<f16x8*>(hi + i) = h;
+    *reinterpret_cast<f16x8*>(lo + i) = l;
   }
 }
 
@@ -234,7 +293,14 @@ __global__ __launch_bounds__(1024) void head_plan_kernel(HeadPlanArgs a) {
       const int v0 = p * h.w_rows;
       P.A = x;
       P.B = cadd(a.W, (size_t)v0 * h.d * es);
-      if (h.grad || !h.bf16) P.C = a.b.logits + v0;
+      if (h.pairs) {
+        const int64_t in_piece = t0 % h.rows * h.d;
+        P.A = a.b.x16 + in_piece;
+        P.A2 = a.b.x16_lo + in_piece;
+        P.B = a.b.w16 + (size_t)v0 * h.d;
+        P.B2 = a.b.w16_lo + (size_t)v0 * h.d;
+      }
+      if (h.grad || !h.wide) P.C = a.b.logits + v0;
       P.C2 = a.b.pairs;
       P.C3 = a.b.at_target;
       P.E1 = a.targets + t0;
@@ -246,15 +312,22 @@ __global__ __launch_bounds__(1024) void head_plan_kernel(HeadPlanArgs a) {
       const int v0 = p * h.k_len;
       P.A = h.bf16 ? (const void*)(a.b.g + v0) : (const void*)(a.b.logits + v0);
       P.B = cadd(a.W, (size_t)v0 * h.d * es);
+      if (h.pairs) {
+        P.A = a.b.hi + v0;
+        P.A2 = a.b.lo + v0;
+        P.B = a.b.w16 + (size_t)v0 * h.d;
+        P.B2 = a.b.w16_lo + (size_t)v0 * h.d;
+      }
       P.C = a.b.slabs + (size_t)p * h.dx_rows * h.d;
       P.M = h.dx_rows > h.rows ? h.dx_rows : m; P.N = h.d; P.K = min(h.k_len, h.vocab - v0);
       P.lda = h.ldv; P.ldb = h.d; P.ldc = h.d;
       t = h.dx_tile;
     } else {
-      P.A = h.bf16 ? (const void*)a.b.hi : (const void*)a.b.logits;
+      P.A = h.wide ? (const void*)a.b.hi : (const void*)a.b.logits;
       P.A2 = a.b.lo;
-      P.B = P.B2 = h.bf16 ? (const void*)a.b.x16 : x;
-      P.E1 = a.b.range ? a.b.range->undo : nullptr;
+      P.B = P.B2 = h.wide ? (const void*)a.b.x16 : x;
+      if (h.pairs) P.B2 = a.b.x16_lo;
+      P.E1 = a.b.range ? a.b.range->undo_dw : nullptr;
       P.C = a.dW;
       P.E2 = reinterpret_cast<const void*>((intptr_t)h.vocab);
       P.M = (h.vocab + 31) / 32 * 32; P.N = h.d; P.K = m;
@@ -301,7 +374,7 @@ __device__ __forceinline__ void put_row(const HeadRowsArgs& a, int row, int32_t 
   put_row(a.logp ? a.logp + row : nullptr, a.log_z ? a.log_z + row : nullptr, target, a.vocab, at_target, top, log_sum);
 }
 
-// bf16: joins the pairs of 64 rows.  Sixteen waves, each takes every sixteenth pair of a row.
+// Joins the pairs of 64 rows.  Sixteen waves, each takes every sixteenth pair of a row.
 __global__ __launch_bounds__(1024) void head_stats_kernel(HeadRowsArgs a) {
   __shared__ float s_m[16][64], s_s[16][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -443,6 +516,7 @@ struct HeadJoinArgs {
   const bf16_t* W;         // where G lacks something of the targets' entries, or null
   const float* lost;
   const int32_t* targets;
+  const float* undo;       // factors of the slabs, or null
   int64_t stride, rest;    // from part to part; to the rows of G's second parts, or 0
   int32_t parts, d, vocab;
 };
@@ -467,6 +541,7 @@ __global__ __launch_bounds__(256) void head_join_kernel(HeadJoinArgs a, T* dX) {
         if (p + q < a.parts) s += v[q];
     }
   }
+  if (a.undo) s = s * a.undo[0] * a.undo[1];
   if (a.W) {
     const int32_t target = a.targets[row];
     if (target >= 0 && target < a.vocab) {
@@ -696,11 +771,12 @@ size_t stream_pairs(int64_t T, int32_t vocab) { return (size_t)T * ((vocab + STR
 size_t stream_workspace(int64_t T, int32_t vocab) { return ALIGN + align_up(stream_pairs(T, vocab), ALIGN) + (size_t)T * 4; }
 
 struct HeadLayout {
-  size_t range, logits, pairs, at_target, off, lost, g, hi, lo, x16, slabs, total;
+  size_t range, logits, pairs, at_target, off, lost, g, hi, lo, x16, x16_lo, w16, w16_lo, slabs, total;
 };
 HeadLayout layout_for(int64_t plans, int64_t sub, int64_t rows, int64_t dx_rows, int64_t slab_cells, int32_t d, int32_t vocab, bool bf16,
-                      bool grad) {
+                      bool pairs, bool grad) {
   HeadLayout w = {};
+  const bool wide = bf16 || pairs;
   const size_t ldv = align_up(vocab, 64), cells = (size_t)rows * ldv;
   size_t at = 0;
   auto take = [&](size_t bytes) {
@@ -709,33 +785,47 @@ HeadLayout layout_for(int64_t plans, int64_t sub, int64_t rows, int64_t dx_rows,
     return here;
   };
   take(sizeof(GemmPlan) * (size_t)plans);
-  w.range = take(sizeof(HeadRange));
-  w.logits = take(bf16 && !grad ? 0 : (size_t)sub * ldv * 4);
-  w.pairs = take(std::max(bf16 ? (size_t)sub * ((vocab + 127) / 128) * 8 : 0, stream_pairs(std::min(sub, STREAM_ROWS), vocab)));
+  // (the range ends where the targets' logits begin)
+  at = align_up(at + sizeof(HeadRange), ALIGN);
+  w.range = at - sizeof(HeadRange);
   w.at_target = take((size_t)sub * 4);
-  w.off = take(bf16 ? (size_t)sub * 8 : 0);
+  w.logits = take(wide && !grad ? 0 : (size_t)sub * ldv * 4);
+  w.pairs = take(std::max(wide ? (size_t)sub * ((vocab + 127) / 128) * 8 : 0, stream_pairs(std::min(sub, STREAM_ROWS), vocab)));
+  w.off = take(wide ? (size_t)sub * 8 : 0);
   w.lost = take(bf16 && grad ? (size_t)rows * 4 : 0);
   w.g = take(bf16 && grad ? (size_t)dx_rows * ldv * 2 : 0);
-  w.hi = take(bf16 && grad ? cells * 2 : 0);
-  w.lo = take(bf16 && grad ? cells * 2 : 0);
-  w.x16 = take(bf16 && grad ? (size_t)rows * d * 2 : 0);
+  w.hi = take(wide && grad ? cells * 2 : 0);
+  w.lo = take(wide && grad ? cells * 2 : 0);
+  w.x16 = take(pairs || (bf16 && grad) ? (size_t)rows * d * 2 : 0);
+  w.x16_lo = take(pairs ? (size_t)rows * d * 2 : 0);
+  w.w16 = take(pairs ? (size_t)vocab * d * 2 : 0);
+  w.w16_lo = take(pairs ? (size_t)vocab * d * 2 : 0);
   w.slabs = take(grad ? (size_t)slab_cells * 4 : 0);
   w.total = at;
   return w;
+}
+// of all batches of at most T rows of one kind: the most plans, rows of a product and of a piece, slabs
+size_t most_workspace(int64_t T, int32_t d, int32_t vocab, bool bf16, bool pairs, bool grad) {
+  const bool wide = bf16 || pairs;
+  const int64_t most = most_rows(vocab, wide, grad), sub_most = std::min(most, most_sub(vocab, wide, grad));
+  const int64_t sub = std::min<int64_t>(padded_rows(T), sub_most), rows = std::min<int64_t>((int64_t)align_up((size_t)T, (size_t)sub), most);
+  const int64_t pieces = (T + most - 1) / most, plans = (T + sub_most - 1) / sub_most + (grad ? 2 * pieces : 0);
+  const int64_t dx_rows = bf16 ? std::max(rows, std::min(2 * rows, 2 * STACK_ROWS)) : rows;
+  const int64_t slabs = std::min(MAX_PARTS * dx_rows * d, std::max(SLAB_CELLS, dx_rows * d));
+  return ALIGN + layout_for(plans, sub, rows, dx_rows, slabs, d, vocab, bf16, pairs, grad).total;
 }
 }  // namespace
 
 size_t head_workspace(int64_t T, int32_t d, int32_t vocab, modse_dtype dt, bool grad) {
   if (T == 0) return 0;
-  // of all batches of at most T rows: the most plans, rows of a product and of a piece, slabs
-  const bool bf16 = dt == MODSE_BF16;
-  const int64_t most = most_rows(vocab, bf16, grad), sub_most = std::min(most, most_sub(vocab, bf16, grad));
-  const int64_t sub = std::min<int64_t>(padded_rows(T), sub_most), rows = std::min<int64_t>((int64_t)align_up((size_t)T, (size_t)sub), most);
-  const int64_t pieces = (T + most - 1) / most, plans = (T + sub_most - 1) / sub_most + (grad ? 2 * pieces : 0);
-  const int64_t dx_rows = bf16 ? std::max(rows, std::min(2 * rows, 2 * STACK_ROWS)) : rows;
-  const int64_t slabs = std::min(MAX_PARTS * dx_rows * d, std::max(SLAB_CELLS, dx_rows * d));
-  const size_t total = ALIGN + layout_for(plans, sub, rows, dx_rows, slabs, d, vocab, bf16, grad).total;
-  return grad ? total : T <= STREAM_ROWS ? stream_workspace(T, vocab) : std::max(total, stream_workspace(STREAM_ROWS, vocab));
+  size_t most = 0;
+  if (!grad) {
+    most = stream_workspace(std::min(T, STREAM_ROWS), vocab);
+    if (T <= STREAM_ROWS) return most;
+  }
+  const bool bf16 = dt == MODSE_BF16, pairs = takes_pairs(T, d, vocab, dt, grad);
+  if (pairs) most = std::max(most, most_workspace(T, d, vocab, false, true, grad));
+  return std::max(most, most_workspace(pairs ? std::min(T, pairs_from(grad) - 1) : T, d, vocab, bf16, false, grad));
 }
 
 hipError_t launch_head(modse_dtype dt, const HeadArgs& a, char* ws, hipStream_t s) {
@@ -748,16 +838,23 @@ hipError_t launch_head(modse_dtype dt, const HeadArgs& a, char* ws, hipStream_t 
   }
   const HeadShape h = head_shape(a.T, a.d, a.vocab, dt, grad);
   const int64_t products = h.products(), plans = products + (grad ? 2 * h.pieces : 0);
-  const HeadLayout w = layout_for(plans, h.sub, h.rows, h.dx_rows, (int64_t)h.k_parts * h.dx_rows * h.d, h.d, h.vocab, h.bf16, grad);
+  const HeadLayout w = layout_for(plans, h.sub, h.rows, h.dx_rows, (int64_t)h.k_parts * h.dx_rows * h.d, h.d, h.vocab, h.bf16, h.pairs, grad);
   ws = reinterpret_cast<char*>(align_up(reinterpret_cast<size_t>(ws), ALIGN));
   auto floats = [&](size_t at) { return reinterpret_cast<float*>(ws + at); };
   auto halves = [&](size_t at) { return reinterpret_cast<f16_t*>(ws + at); };
-  HeadRange* const range = h.bf16 && grad ? reinterpret_cast<HeadRange*>(ws + w.range) : nullptr;
+  HeadRange* const range = h.pairs || (h.bf16 && grad) ? reinterpret_cast<HeadRange*>(ws + w.range) : nullptr;
   const HeadBufs b = {reinterpret_cast<GemmPlan*>(ws), floats(w.logits), floats(w.pairs), floats(w.at_target), floats(w.off),
-                      reinterpret_cast<bf16_t*>(ws + w.g), floats(w.lost), halves(w.hi), halves(w.lo), halves(w.x16), range, floats(w.slabs)};
+                      reinterpret_cast<bf16_t*>(ws + w.g), floats(w.lost), halves(w.hi), halves(w.lo), halves(w.x16), halves(w.x16_lo),
+                      halves(w.w16), halves(w.w16_lo), range, floats(w.slabs)};
   const HeadPlanArgs plan = {h, b, a.x, a.W, a.targets, a.d_logp, a.dW, (int32_t)plans};
-  const int64_t range_blocks = range ? std::min<int64_t>((h.T * h.d + 32767) / 32768, RANGE_BLOCKS) : 0;
+  const int64_t looked_at = h.T * h.d + (h.pairs ? (int64_t)h.vocab * h.d : 0);
+  const int64_t range_blocks = range ? std::min<int64_t>((looked_at + 32767) / 32768, RANGE_BLOCKS) : 0;
   hipLaunchKernelGGL(head_plan_kernel, dim3((unsigned)(plans + range_blocks)), dim3(1024), 0, s, plan);
+  auto split = [&](const void* p, int64_t n, f16_t* hi, f16_t* lo, int is_w) {
+    const dim3 grid((unsigned)std::min<int64_t>((n + 2047) / 2048, 2048));
+    hipLaunchKernelGGL(head_split_kernel, grid, dim3(256), 0, s, static_cast<const float*>(p), n, hi, lo, range, is_w);
+  };
+  if (h.pairs) split(a.W, (int64_t)h.vocab * h.d, b.w16, b.w16_lo, 1);
   const bf16_t* const x = static_cast<const bf16_t*>(a.x);
   auto tiles = [](int64_t m, int64_t n, TileShape t) { return ((m + t.bm - 1) / t.bm) * ((n + t.bn - 1) / t.bn); };
   hipError_t e = hipGetLastError();
@@ -765,23 +862,25 @@ hipError_t launch_head(modse_dtype dt, const HeadArgs& a, char* ws, hipStream_t 
   auto product = [&](int64_t i) {
     const int64_t t0 = i * h.sub, m = std::min<int64_t>(h.sub, h.T - t0), in_piece = t0 % h.rows;
     const bool stream = h.T <= STREAM_ROWS;  // (only with gradients here)
+    if (h.pairs && in_piece == 0)
+      split(static_cast<const float*>(a.x) + t0 * h.d, std::min<int64_t>(h.rows, h.T - t0) * h.d, b.x16, b.x16_lo, 0);
     if (stream) {
       const HeadStreamArgs r = {a.x, a.W, a.targets, b.pairs, b.at_target, h.bf16 ? a.logp : nullptr, nullptr, b.logits,
                                 h.bf16 ? b.off : nullptr, range, (int32_t)m, h.d, h.vocab, h.ldv};
       e = h.bf16 ? run_stream<bf16_t>(r, s) : run_stream<float>(r, s);
     } else {
-      e = launch_grouped_gemm(dt, h.bf16 ? EPI_LOGITS : EPI_STORE, h.logits_tile, b.plans + i, h.w_parts, 0, GEMM_STREAM_C,
-                              tiles(m, h.vocab, h.logits_tile) + h.w_parts * tiles(m, 1, h.logits_tile), s, LAYOUT_TN);
+      e = launch_grouped_gemm(dt, h.pairs ? EPI_LOGITS_PAIRS : h.bf16 ? EPI_LOGITS : EPI_STORE, h.logits_tile, b.plans + i, h.w_parts, 0,
+                              GEMM_STREAM_C, tiles(m, h.vocab, h.logits_tile) + h.w_parts * tiles(m, 1, h.logits_tile), s, LAYOUT_TN);
     }
     if (e != hipSuccess) return;
     const HeadRowsArgs r = {a.targets + t0, a.d_logp ? a.d_logp + t0 : nullptr, a.logp ? a.logp + t0 : nullptr, a.log_z ? a.log_z + t0 : nullptr,
-                            b.logits, b.pairs, b.at_target, b.off, a.dX ? b.g + in_piece * h.ldv : nullptr,
+                            b.logits, b.pairs, b.at_target, b.off, a.dX && h.bf16 ? b.g + in_piece * h.ldv : nullptr,
                             a.dX && h.dx_rows > h.rows ? b.g + (int64_t)h.rows * h.ldv : nullptr, b.lost + in_piece,
-                            a.dW ? b.hi + in_piece * h.ldv : nullptr, a.dW ? b.lo + in_piece * h.ldv : nullptr,
+                            a.dW || h.pairs ? b.hi + in_piece * h.ldv : nullptr, a.dW || h.pairs ? b.lo + in_piece * h.ldv : nullptr,
                             range, x + t0 * h.d, b.x16 + in_piece * h.d, (int32_t)m, h.vocab, h.ldv, h.sub, h.d};
-    if (h.bf16) {
+    if (h.wide) {
       if (!stream) hipLaunchKernelGGL(head_stats_kernel, dim3((unsigned)((m + 63) / 64)), dim3(1024), 0, s, r);
-      const int64_t segs = (h.ldv + 2047) / 2048, copies = a.dW ? (m * h.d + 2047) / 2048 : 0;
+      const int64_t segs = (h.ldv + 2047) / 2048, copies = a.dW && h.bf16 ? (m * h.d + 2047) / 2048 : 0;
       if (grad) hipLaunchKernelGGL(head_grad_kernel, dim3((unsigned)(m * segs + copies)), dim3(256), 0, s, r, (int)segs);
     } else if (grad) {
       hipLaunchKernelGGL((head_rows_kernel<true>), dim3((unsigned)m), dim3(512), 0, s, r);
@@ -798,17 +897,18 @@ hipError_t launch_head(modse_dtype dt, const HeadArgs& a, char* ws, hipStream_t 
     const int64_t t0 = piece * h.rows, m = std::min<int64_t>(h.rows, h.T - t0);
     const GemmPlan* const p = b.plans + products + 2 * piece;
     if (a.dW) {  // (before dX, which may lie in the buffer of x)
-      e = launch_grouped_gemm(dt, EPI_ROWS_F32, h.dw_tile, p + 1, 1, a.accumulate || piece > 0, 0,
+      e = launch_grouped_gemm(dt, h.pairs ? EPI_ROWS_PAIRS : EPI_ROWS_F32, h.dw_tile, p + 1, 1, a.accumulate || piece > 0, 0,
                               tiles(padded_rows(h.vocab), h.d, h.dw_tile), s, LAYOUT_AB_K);
       if (e != hipSuccess) break;
     }
     if (a.dX) {
-      const int64_t dx_rows = h.dx_rows > h.rows ? h.dx_rows : m;
-      e = launch_grouped_gemm(dt, EPI_STORE_F32, h.dx_tile, p, h.k_parts, 0, 0, h.k_parts * tiles(dx_rows, h.d, h.dx_tile), s, LAYOUT_B_KN);
-      if (e != hipSuccess) break;
       const bool stacked = h.dx_rows > h.rows;
+      e = launch_grouped_gemm(dt, h.pairs ? EPI_STORE_PAIRS : EPI_STORE_F32, h.dx_tile, p, h.k_parts, 0, 0,
+                              h.k_parts * tiles(stacked ? h.dx_rows : m, h.d, h.dx_tile), s, LAYOUT_B_KN);
+      if (e != hipSuccess) break;
       const HeadJoinArgs j = {b.slabs, h.bf16 && !stacked ? static_cast<const bf16_t*>(a.W) : nullptr, b.lost, a.targets + t0,
-                              (int64_t)h.dx_rows * h.d, stacked ? (int64_t)h.rows * h.d : 0, h.k_parts, h.d, h.vocab};
+                              h.pairs ? range->undo_dx : nullptr, (int64_t)h.dx_rows * h.d, stacked ? (int64_t)h.rows * h.d : 0, h.k_parts,
+                              h.d, h.vocab};
       const dim3 join((unsigned)m, (unsigned)((h.d + 1023) / 1024));
       if (h.bf16) hipLaunchKernelGGL((head_join_kernel<bf16_t>), join, dim3(256), 0, s, j, static_cast<bf16_t*>(a.dX) + t0 * h.d);
       else hipLaunchKernelGGL((head_join_kernel<float>), join, dim3(256), 0, s, j, static_cast<float*>(a.dX) + t0 * h.d);

@@ -1,12 +1,14 @@
 """Log probabilities from hidden rows and the output matrix, and their gradients, against the formulas in float64.
 
 Tolerances.  A logit is a sum of d products in float32, whose instructions drop what lies 2^-23 below a partial sum: off by at most
-e = (d + 2) 2^-23 sum |x W| (0 where the inputs are whole numbers whose sums float32 holds).  Sums of exponentials: V terms of one sign,
+e = (d + 6) 2^-23 sum |x W| (0 where the inputs are whole numbers whose sums float32 holds); four of these stand for float32 matrices that are
+held as pairs of float16 ones: 2^-23 of each factor, and 2^-22 of the product of the second parts, which is left out.  Sums of exponentials: V terms of one sign,
 joined in groups, under 2^9 roundings each with an exponential of relative error 2 u + |z| u whose weight falls as e^z: 2^-14 at the
 worst.  So log Z and log p are off by a = e_max + e_target + 2^-14 + 2^-22 (|l| + |log p|), and p relatively by as much (and 2^-21 |log p|).
 G = w (1[target] - p) adds 2^-22 |w| at the target.  For dX of bf16 layers it is rounded to half a step of bf16, but for the target's
 entry, and all of them up to 128 rows, which are held to 2^-16.  For dW of bf16 layers it is held to
-2^-22 of each value (2^-21 with the product by its scale) and 2^-39 of the largest weight, and x to 2^-39 of its largest value.  The products sum in float32: (terms + 2) 2^-23 of the sum of the absolute values; a result is rounded to its type."""
+2^-22 of each value (2^-21 with the product by its scale) and 2^-39 of the largest weight, and x to 2^-39 of its largest value; so are, of
+many rows of float32 layers, G, x and W, and to 2^-22 of each value.  The products sum in float32: (terms + 2) 2^-23 of the sum of the absolute values; a result is rounded to its type."""
 import numpy as np
 import pytest
 import torch
@@ -73,7 +75,7 @@ def reference(x, W, targets, w, exact=False):
     x, W, w = x.double(), W.double(), w.double()
     d = x.shape[1]
     logits = x @ W.t().contiguous()
-    e = 0.0 if exact else ((d + 2) * 2.0 ** -23) * (x.abs() @ W.abs().t().contiguous())
+    e = 0.0 if exact else ((d + 6) * 2.0 ** -23) * (x.abs() @ W.abs().t().contiguous())
     at, has = targets.clamp_min(0).long()[:, None], targets >= 0
     log_z = logits.logsumexp(1)
     logp = logits.gather(1, at)[:, 0] - log_z
@@ -113,25 +115,34 @@ def check(T, d, V, dtype, seed=0, whole=False, sigma=2.5, times_x=1.0, times_w=1
     x64, W64 = x.double(), W.double()
     size = G.abs() + tol_G
     rounded = torch.zeros_like(size)
+    most_w = w[targets >= 0].double().abs().max() if (targets >= 0).any() else 0.0
+    in_parts = 2.0 ** -21 * size + 2.0 ** -39 * most_w
+    pairs = dtype == "f32" and T > 128
     if dtype == "bf16":
         rounded = size * (2.0 ** -16 if T <= 128 else HALF[dtype])
         at = targets.clamp_min(0).long()[:, None]
         rounded.scatter_(1, at, 2.0 ** -16 * size.gather(1, at))
+    elif pairs:
+        rounded = in_parts
     terms = size @ W64.abs()
     tol_dX = (tol_G + rounded) @ W64.abs() + (V + 2) * 2.0 ** -23 * terms
+    if pairs:
+        tol_dX += 2.0 ** -20 * terms + size.sum(1, keepdim=True) * 2.0 ** -39 * W64.abs().max()
     want = G @ W64
     near(dX, want, tol_dX + HALF[dtype] * (want.abs() + tol_dX), "dX", T, d, V, dtype)
-    held = dtype == "bf16"
-    most_w, most_x = w[targets >= 0].double().abs().max() if (targets >= 0).any() else 0.0, x64.abs().max()
-    Gt, St, Et = G.t().contiguous(), size.t().contiguous(), (tol_G + held * (2.0 ** -21 * size + 2.0 ** -39 * most_w)).t().contiguous()
+    held = dtype == "bf16" or pairs
+    Gt, St, Et = G.t().contiguous(), size.t().contiguous(), (tol_G + held * in_parts).t().contiguous()
     terms = St @ x64.abs()
-    tol_dW = Et @ x64.abs() + held * St.sum(1, keepdim=True) * 2.0 ** -39 * most_x + (2 * T + 2) * 2.0 ** -23 * terms
+    tol_dW = Et @ x64.abs() + held * St.sum(1, keepdim=True) * 2.0 ** -39 * x64.abs().max() + (2 * T + 2) * 2.0 ** -23 * terms
+    if pairs:
+        tol_dW += 2.0 ** -20 * terms
     want = Gt @ x64
     near(dW, want, tol_dW + 2.0 ** -24 * (want.abs() + tol_dW), "dW", T, d, V, dtype)
     return x, W, targets, w, dX, dW, want, tol_dW
 
 
-SHAPES = [(1, 32, 1), (1, 64, 7), (2, 32, 31), (3, 96, 32), (5, 64, 33), (16, 128, 100), (17, 32, 255), (33, 96, 257), (64, 2048, 700),
+# (rows: a stream over W up to 64, dX in two parts up to 128, float32 by pairs from 129 and, scored, 193 on)
+SHAPES = [(1, 32, 1), (128, 96, 513), (192, 64, 777), (193, 64, 778), (520, 96, 31), (1, 64, 7), (2, 32, 31), (3, 96, 32), (5, 64, 33), (16, 128, 100), (17, 32, 255), (33, 96, 257), (64, 2048, 700),
           (65, 512, 1023), (63, 64, 8191), (49, 256, 64), (32, 32, 65), (129, 64, 1500), (255, 64, 300), (257, 128, 1000), (300, 256, 5003), (1000, 64, 4097), (40, 96, 50257), (4, 4096, 9001)]
 
 
@@ -165,21 +176,24 @@ def test_sums_are_added_to_and_results_are_the_same_bits_again(T, d, V, dtype):
 def test_rows_and_gradients_of_any_size(times_x, times_w, dtype):
     """Powers of two leave the logits as they are."""
     check(70, 64, 300, dtype, seed=13, times_x=times_x, times_w=times_w)
+    check(200, 64, 300, dtype, seed=14, times_x=times_x, times_w=times_w)
 
 
-def test_weights_and_rows_of_sizes_far_apart():
-    T, d, V = 64, 64, 300
-    x, W, targets, w = inputs(T, d, V, "bf16", 14)
+@pytest.mark.parametrize("dtype,T", [("bf16", 64), ("bf16", 200), ("f32", 200)])
+def test_weights_and_rows_of_sizes_far_apart(dtype, T):
+    d, V = 64, 300
+    x, W, targets, w = inputs(T, d, V, dtype, 14)
     w = w * 2.0 ** torch.linspace(-30, 0, T, device="cuda")
     x[::3] *= 2.0 ** -12
     logp, log_z, G, tol, tol_z, tol_G = reference(x, W, targets, w)
-    lp, dX, dW = backward(x, W, targets, w, "bf16")
+    lp, dX, dW = backward(x, W, targets, w, dtype)
     x64, size = x.double(), G.abs() + tol_G
-    tol_dW = (tol_G + 2.0 ** -21 * size + 2.0 ** -39 * w.abs().max()).t().contiguous() @ x64.abs() + (
+    tol_dW = 2.0 ** -20 * (size.t().contiguous() @ x64.abs()) + (tol_G + 2.0 ** -21 * size + 2.0 ** -39 * w.abs().max()).t().contiguous() @ x64.abs() + (
         size.t().sum(1, keepdim=True) * 2.0 ** -39 * x64.abs().max()) + (2 * T + 3) * 2.0 ** -23 * (size.t().contiguous() @ x64.abs())
     near(dW, G.t().contiguous() @ x64, tol_dW, "dW")
     want = G @ W.double()
-    near(dX, want, (tol_G + 2.0 ** -8 * size) @ W.double().abs() * 1.01 + 2.0 ** -8 * want.abs() * 1.01 + (V + 2) * 2.0 ** -23 * (size @ W.double().abs()), "dX")
+    half = HALF[dtype] if dtype == "bf16" else 2.0 ** -20
+    near(dX, want, (tol_G + half * size + 2.0 ** -39 * w.abs().max()) @ W.double().abs() * 1.01 + half * want.abs() * 1.01 + (V + 2) * 2.0 ** -23 * (size @ W.double().abs()), "dX")
 
 
 def test_the_largest_vocabulary_in_pieces_of_few_rows():

@@ -20,6 +20,7 @@
 // which hold 22 bits, times float16 copies of the rows of x: both times powers of two that follow the largest |x| and the largest
 // |d_logp| of the call, so that what is rounded or lost is below 2^-39 of the largest product.  (Two bf16 numbers, 16 bits, left an
 // error of 2.7e-6 of dW where float32 products have 0.7e-6 to 2e-6, and need no third copy of G; the rest takes as long.)
+#include <cmath>
 #include <cstddef>
 
 #include "ops.h"
@@ -38,7 +39,8 @@ constexpr int64_t W_PART = (int64_t)1 << 30;       // elements of W that one pro
 constexpr size_t ALIGN = 256;                      // of what is in the workspace, which itself may lie at any sixteen bytes
 constexpr int64_t SLAB_CELLS = (int64_t)1 << 26;   // values of all parts of dX together, unless one part has more
 constexpr int64_t STACK_ROWS = 128;                // of bf16 layers up to which dX takes G in two parts
-constexpr int MAX_PARTS = 128;                     // of dX
+constexpr int MAX_PARTS = 128;                     // of dX, of dW (problems of a product: fewer than 192)
+static_assert(MAX_PARTS <= MODSE_MAX_PROBLEMS, "a problem for each");
 
 struct HeadShape {
   int64_t T;
@@ -48,6 +50,7 @@ struct HeadShape {
   int32_t w_parts, w_rows; // problems of the logits, rows of W in each
   int32_t dx_rows;         // rows of the product of dX: those of a piece, or twice as many
   int32_t k_parts, k_len;  // problems of dX, columns of G in each
+  int32_t w_split, w_len;  // problems of dW, rows in each
   int32_t bf16, grad;
   int32_t pairs;           // float32, and the matrices are held as pairs of float16 ones
   int32_t wide;            // either of them: tiles of 256, sums of exponentials by the product of the logits
@@ -68,11 +71,26 @@ int64_t most_rows(int32_t vocab, bool wide, bool grad) {
 int64_t most_sub(int32_t vocab, bool wide, bool grad) {
   return wide && grad ? rows_in(LOGIT_CELLS, (int64_t)align_up(vocab, 64)) : most_rows(vocab, wide, grad);
 }
-// Float32 layers: from so many rows on products of pairs of float16 numbers, three 16-bit products in place of one of float32, but the parts
-// of W, which lie in the workspace, have to be made first.
-int64_t pairs_from(bool grad) { return grad ? 129 : 193; }
+// Float32 layers: the rows from which on products of pairs of float16 numbers are faster, three 16-bit products in place of one of float32,
+// with the largest values and the parts of W (and some launches) before them.  At 105 and 1150 TFLOP/s, 5 TB/s and tiles that are 128 rows too
+// high on average.  Float32 / pairs, us: gradients with 32000 x 2048, 128 rows 505, 256 830 / 590, 1024 3060 / 1200; with 50257 x 256, 256
+// rows 227 / 202, 1024 733 / 466; scoring with 32000 x 2048, 256 rows 288 / 304, 512 550 / 323.
+int64_t pairs_from(int32_t d, int32_t vocab, bool grad) {
+  const double cells = (double)vocab * d, products = grad ? 6 : 2;
+  const double fixed = 3 * products * 128 * cells / 1.15e9 + 12 * cells / 5e6 + (grad ? 50 : 35);
+  return std::max<int64_t>(129, (int64_t)std::ceil(fixed / (products * cells * (1 / 1.05e8 - 3 / 1.15e9))));
+}
 bool takes_pairs(int64_t T, int32_t d, int32_t vocab, modse_dtype dt, bool grad) {
-  return dt == MODSE_F32 && T >= pairs_from(grad) && (int64_t)vocab * d <= PAIR_W;
+  return dt == MODSE_F32 && (int64_t)vocab * d <= PAIR_W && T >= pairs_from(d, vocab, grad);
+}
+// Up to so many rows the logits are made by a stream over W (below): blocks of 64 rows of each, while there are two for every CU at the most, or
+// one block of rows.
+constexpr int STREAM_W = 64;
+int64_t stream_rows(int32_t vocab) { return std::max<int64_t>(1, 512 / ((vocab + STREAM_W - 1) / STREAM_W)) * 64; }
+// Parts of dW's sum over the tokens, where it has too few tiles for the chip: slabs like those of dX, added up behind it.
+int64_t dw_most_parts(int32_t d, int32_t vocab, bool wide) {
+  const int64_t tiles = (int64_t)((vocab + 255) / 256) * ((d + 255) / 256);
+  return wide && tiles <= 128 ? std::min<int64_t>(MAX_PARTS, 256 / tiles) : 1;
 }
 
 HeadShape head_shape(int64_t T, int32_t d, int32_t vocab, modse_dtype dt, bool grad) {
@@ -100,6 +118,9 @@ HeadShape head_shape(int64_t T, int32_t d, int32_t vocab, modse_dtype dt, bool g
   auto tile = [&](int64_t m, int64_t n) { const int b = h.wide ? 256 : tiles(m, n, 128) >= 2048 ? 128 : 64; return TileShape{b, b}; };
   h.logits_tile = tile(h.sub, vocab);
   h.dw_tile = tile(vocab, d);
+  const int64_t w_steps = (h.rows + 63) / 64, w_split = std::min(dw_most_parts(d, vocab, h.wide), std::max<int64_t>(1, w_steps / 4));
+  h.w_len = (int32_t)((w_steps + w_split - 1) / w_split) * 64;
+  h.w_split = (h.rows + h.w_len - 1) / h.w_len;
   const int dx = h.wide ? 256 : h.rows <= 64 ? 64 : 128;
   h.dx_tile = TileShape{dx, dx};
   // Parts of dX: whole rounds of workgroups over the chip, each part with six further steps for its opening and its end, and slabs that
@@ -285,7 +306,7 @@ __global__ __launch_bounds__(1024) void head_plan_kernel(HeadPlanArgs a) {
   const int m = (int)min((int64_t)rows, h.T - t0);
   const char* const x = cadd(a.x, (size_t)t0 * h.d * es);
   GemmPlan* const plan = a.b.plans + blockIdx.x;
-  const int n = which == 0 ? h.w_parts : which == 1 ? h.k_parts : 1;
+  const int n = which == 0 ? h.w_parts : which == 1 ? h.k_parts : h.w_split;
   for (int p = lane; p < n; p += 64) {
     GemmProblem P = {};
     TileShape t;
@@ -323,14 +344,16 @@ __global__ __launch_bounds__(1024) void head_plan_kernel(HeadPlanArgs a) {
       P.lda = h.ldv; P.ldb = h.d; P.ldc = h.d;
       t = h.dx_tile;
     } else {
-      P.A = h.wide ? (const void*)a.b.hi : (const void*)a.b.logits;
-      P.A2 = a.b.lo;
-      P.B = P.B2 = h.wide ? (const void*)a.b.x16 : x;
-      if (h.pairs) P.B2 = a.b.x16_lo;
+      const int r0 = p * h.w_len;  // (behind the last piece's rows: a part of zeros)
+      const size_t g0 = (size_t)r0 * h.ldv, x0 = (size_t)r0 * h.d;
+      P.A = h.wide ? (const void*)(a.b.hi + g0) : (const void*)a.b.logits;
+      P.A2 = a.b.lo + g0;
+      P.B = P.B2 = h.wide ? (const void*)(a.b.x16 + x0) : x;
+      if (h.pairs) P.B2 = a.b.x16_lo + x0;
       P.E1 = a.b.range ? a.b.range->undo_dw : nullptr;
-      P.C = a.dW;
+      P.C = h.w_split > 1 ? a.b.slabs + (size_t)p * h.vocab * h.d : a.dW;
       P.E2 = reinterpret_cast<const void*>((intptr_t)h.vocab);
-      P.M = (h.vocab + 31) / 32 * 32; P.N = h.d; P.K = m;
+      P.M = (h.vocab + 31) / 32 * 32; P.N = h.d; P.K = max(min(h.w_len, m - r0), 0);
       P.lda = h.ldv; P.ldb = h.d; P.ldc = h.d;
       t = h.dw_tile;
     }
@@ -555,6 +578,22 @@ __global__ __launch_bounds__(256) void head_join_kernel(HeadJoinArgs a, T* dX) {
   for (int e = 0; e < 4; ++e) dX[i + e] = (T)s[e];
 }
 
+// dW: the parts of its sum, in order, added to what there is or stored.
+__global__ __launch_bounds__(256) void head_dw_join_kernel(const float* slabs, int parts, int64_t n, float* dW, int accumulate) {
+  const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;  // (n: whole rows of 32 and more columns)
+  if (i >= n) return;
+  f32x4 s = accumulate ? *reinterpret_cast<const f32x4*>(dW + i) : f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int p = 0; p < parts; p += 8) {
+    f32x4 v[8];
+#pragma unroll
+    for (int q = 0; q < 8; ++q) v[q] = *reinterpret_cast<const f32x4*>(slabs + min(p + q, parts - 1) * n + i);
+#pragma unroll
+    for (int q = 0; q < 8; ++q)
+      if (p + q < parts) s += v[q];
+  }
+  *reinterpret_cast<f32x4*>(dW + i) = s;
+}
+
 // ---------------------------------------------------------------- few rows
 // Bound by the stream of W.  A block takes 64 rows of W and up to 16 NT rows of x; its four waves share the sum over d out and go their
 // own ways until the end: each moves 128 bytes of all these rows at a time straight into LDS of its own, whole lines with the
@@ -564,8 +603,6 @@ __global__ __launch_bounds__(256) void head_join_kernel(HeadJoinArgs a, T* dX) {
 // bytes a load, one row x 131072, d = 4096, took 190 us without the hint and 269 with it, as each line then came twice; this way
 // 166, 6.5 TB/s.)  The waves' sums meet in LDS; what leaves the block is, for every row of x, the maximum and the sum of exponentials of
 // its 64 logits.  A second launch joins them.
-constexpr int STREAM_W = 64;
-
 struct HeadStreamArgs {
   const void *x, *W;
   const int32_t* targets;
@@ -766,7 +803,6 @@ hipError_t run_stream(const HeadStreamArgs& a, hipStream_t s) {
   if (a.logp || a.log_z || a.off) hipLaunchKernelGGL(head_stream_join_kernel, dim3((unsigned)a.T), dim3(1024), 0, s, a);
   return hipGetLastError();
 }
-constexpr int64_t STREAM_ROWS = 64;  // up to so many rows
 size_t stream_pairs(int64_t T, int32_t vocab) { return (size_t)T * ((vocab + STREAM_W - 1) / STREAM_W) * 8; }
 size_t stream_workspace(int64_t T, int32_t vocab) { return ALIGN + align_up(stream_pairs(T, vocab), ALIGN) + (size_t)T * 4; }
 
@@ -790,7 +826,7 @@ HeadLayout layout_for(int64_t plans, int64_t sub, int64_t rows, int64_t dx_rows,
   w.range = at - sizeof(HeadRange);
   w.at_target = take((size_t)sub * 4);
   w.logits = take(wide && !grad ? 0 : (size_t)sub * ldv * 4);
-  w.pairs = take(std::max(wide ? (size_t)sub * ((vocab + 127) / 128) * 8 : 0, stream_pairs(std::min(sub, STREAM_ROWS), vocab)));
+  w.pairs = take(std::max(wide ? (size_t)sub * ((vocab + 127) / 128) * 8 : 0, stream_pairs(std::min(sub, stream_rows(vocab)), vocab)));
   w.off = take(wide ? (size_t)sub * 8 : 0);
   w.lost = take(bf16 && grad ? (size_t)rows * 4 : 0);
   w.g = take(bf16 && grad ? (size_t)dx_rows * ldv * 2 : 0);
@@ -811,7 +847,8 @@ size_t most_workspace(int64_t T, int32_t d, int32_t vocab, bool bf16, bool pairs
   const int64_t sub = std::min<int64_t>(padded_rows(T), sub_most), rows = std::min<int64_t>((int64_t)align_up((size_t)T, (size_t)sub), most);
   const int64_t pieces = (T + most - 1) / most, plans = (T + sub_most - 1) / sub_most + (grad ? 2 * pieces : 0);
   const int64_t dx_rows = bf16 ? std::max(rows, std::min(2 * rows, 2 * STACK_ROWS)) : rows;
-  const int64_t slabs = std::min(MAX_PARTS * dx_rows * d, std::max(SLAB_CELLS, dx_rows * d));
+  const int64_t dw_parts = dw_most_parts(d, vocab, wide);
+  const int64_t slabs = std::max(std::min(MAX_PARTS * dx_rows * d, std::max(SLAB_CELLS, dx_rows * d)), dw_parts > 1 ? dw_parts * vocab * d : 0);
   return ALIGN + layout_for(plans, sub, rows, dx_rows, slabs, d, vocab, bf16, pairs, grad).total;
 }
 }  // namespace
@@ -820,17 +857,17 @@ size_t head_workspace(int64_t T, int32_t d, int32_t vocab, modse_dtype dt, bool 
   if (T == 0) return 0;
   size_t most = 0;
   if (!grad) {
-    most = stream_workspace(std::min(T, STREAM_ROWS), vocab);
-    if (T <= STREAM_ROWS) return most;
+    most = stream_workspace(std::min(T, stream_rows(vocab)), vocab);
+    if (T <= stream_rows(vocab)) return most;
   }
   const bool bf16 = dt == MODSE_BF16, pairs = takes_pairs(T, d, vocab, dt, grad);
   if (pairs) most = std::max(most, most_workspace(T, d, vocab, false, true, grad));
-  return std::max(most, most_workspace(pairs ? std::min(T, pairs_from(grad) - 1) : T, d, vocab, bf16, false, grad));
+  return std::max(most, most_workspace(pairs ? std::min(T, pairs_from(d, vocab, grad) - 1) : T, d, vocab, bf16, false, grad));
 }
 
 hipError_t launch_head(modse_dtype dt, const HeadArgs& a, char* ws, hipStream_t s) {
   const bool grad = a.dX || a.dW;
-  if (!grad && a.T <= STREAM_ROWS) {
+  if (!grad && a.T <= stream_rows(a.vocab)) {
     float* const pairs = reinterpret_cast<float*>(align_up(reinterpret_cast<size_t>(ws), ALIGN));
     float* const at_target = pairs + align_up(stream_pairs(a.T, a.vocab), ALIGN) / 4;
     const HeadStreamArgs r = {a.x, a.W, a.targets, pairs, at_target, a.logp, a.log_z, nullptr, nullptr, nullptr, (int32_t)a.T, a.d, a.vocab, 0};
@@ -838,7 +875,8 @@ hipError_t launch_head(modse_dtype dt, const HeadArgs& a, char* ws, hipStream_t 
   }
   const HeadShape h = head_shape(a.T, a.d, a.vocab, dt, grad);
   const int64_t products = h.products(), plans = products + (grad ? 2 * h.pieces : 0);
-  const HeadLayout w = layout_for(plans, h.sub, h.rows, h.dx_rows, (int64_t)h.k_parts * h.dx_rows * h.d, h.d, h.vocab, h.bf16, h.pairs, grad);
+  const int64_t slabs = std::max((int64_t)h.k_parts * h.dx_rows * h.d, h.w_split > 1 ? (int64_t)h.w_split * h.vocab * h.d : 0);
+  const HeadLayout w = layout_for(plans, h.sub, h.rows, h.dx_rows, slabs, h.d, h.vocab, h.bf16, h.pairs, grad);
   ws = reinterpret_cast<char*>(align_up(reinterpret_cast<size_t>(ws), ALIGN));
   auto floats = [&](size_t at) { return reinterpret_cast<float*>(ws + at); };
   auto halves = [&](size_t at) { return reinterpret_cast<f16_t*>(ws + at); };
@@ -861,12 +899,12 @@ hipError_t launch_head(modse_dtype dt, const HeadArgs& a, char* ws, hipStream_t 
   // the logits of one product, their sums and (of gradients) G
   auto product = [&](int64_t i) {
     const int64_t t0 = i * h.sub, m = std::min<int64_t>(h.sub, h.T - t0), in_piece = t0 % h.rows;
-    const bool stream = h.T <= STREAM_ROWS;  // (only with gradients here)
+    const bool stream = h.T <= stream_rows(h.vocab) && products == 1;  // (only with gradients here)
     if (h.pairs && in_piece == 0)
       split(static_cast<const float*>(a.x) + t0 * h.d, std::min<int64_t>(h.rows, h.T - t0) * h.d, b.x16, b.x16_lo, 0);
     if (stream) {
-      const HeadStreamArgs r = {a.x, a.W, a.targets, b.pairs, b.at_target, h.bf16 ? a.logp : nullptr, nullptr, b.logits,
-                                h.bf16 ? b.off : nullptr, range, (int32_t)m, h.d, h.vocab, h.ldv};
+      const HeadStreamArgs r = {a.x, a.W, a.targets, b.pairs, b.at_target, h.wide ? a.logp : nullptr, nullptr, b.logits,
+                                h.wide ? b.off : nullptr, range, (int32_t)m, h.d, h.vocab, h.ldv};
       e = h.bf16 ? run_stream<bf16_t>(r, s) : run_stream<float>(r, s);
     } else {
       e = launch_grouped_gemm(dt, h.pairs ? EPI_LOGITS_PAIRS : h.bf16 ? EPI_LOGITS : EPI_STORE, h.logits_tile, b.plans + i, h.w_parts, 0,
@@ -897,8 +935,14 @@ hipError_t launch_head(modse_dtype dt, const HeadArgs& a, char* ws, hipStream_t 
     const int64_t t0 = piece * h.rows, m = std::min<int64_t>(h.rows, h.T - t0);
     const GemmPlan* const p = b.plans + products + 2 * piece;
     if (a.dW) {  // (before dX, which may lie in the buffer of x)
-      e = launch_grouped_gemm(dt, h.pairs ? EPI_ROWS_PAIRS : EPI_ROWS_F32, h.dw_tile, p + 1, 1, a.accumulate || piece > 0, 0,
-                              tiles(padded_rows(h.vocab), h.d, h.dw_tile), s, LAYOUT_AB_K);
+      const int accumulate = a.accumulate || piece > 0;
+      e = launch_grouped_gemm(dt, h.pairs ? EPI_ROWS_PAIRS : EPI_ROWS_F32, h.dw_tile, p + 1, h.w_split, h.w_split > 1 ? 0 : accumulate, 0,
+                              h.w_split * tiles(padded_rows(h.vocab), h.d, h.dw_tile), s, LAYOUT_AB_K);
+      if (e == hipSuccess && h.w_split > 1) {
+        const int64_t n = (int64_t)h.vocab * h.d;
+        hipLaunchKernelGGL(head_dw_join_kernel, dim3((unsigned)((n + 1023) / 1024)), dim3(256), 0, s, b.slabs, h.w_split, n, a.dW, accumulate);
+        e = hipGetLastError();
+      }
       if (e != hipSuccess) break;
     }
     if (a.dX) {

@@ -141,9 +141,22 @@ def check(T, d, V, dtype, seed=0, whole=False, sigma=2.5, times_x=1.0, times_w=1
     return x, W, targets, w, dX, dW, want, tol_dW
 
 
-# (rows: a stream over W up to 64, dX in two parts up to 128, float32 by pairs from 129 and, scored, 193 on)
-SHAPES = [(1, 32, 1), (128, 96, 513), (192, 64, 777), (193, 64, 778), (520, 96, 31), (1, 64, 7), (2, 32, 31), (3, 96, 32), (5, 64, 33), (16, 128, 100), (17, 32, 255), (33, 96, 257), (64, 2048, 700),
-          (65, 512, 1023), (63, 64, 8191), (49, 256, 64), (32, 32, 65), (129, 64, 1500), (255, 64, 300), (257, 128, 1000), (300, 256, 5003), (1000, 64, 4097), (40, 96, 50257), (4, 4096, 9001)]
+# A stream over W where a few rows or a small vocabulary make few blocks, tiles of 256 x 256 (float32: less) beyond; dX in two parts up to 128
+# rows; dW's sum in parts where the vocabulary is small
+SHAPES = [(1, 32, 1), (1, 64, 7), (2, 32, 31), (3, 96, 32), (5, 64, 33), (16, 128, 100), (17, 32, 255), (33, 96, 257), (64, 2048, 700),
+          (65, 512, 1023), (63, 64, 8191), (49, 256, 64), (32, 32, 65), (129, 64, 1500), (255, 64, 300), (257, 128, 1000), (300, 256, 5003),
+          (1000, 64, 4097), (40, 96, 50257), (4, 4096, 9001), (128, 96, 513), (192, 64, 777), (520, 96, 31), (70, 64, 40000), (65, 512, 33000),
+          (128, 32, 16500), (129, 96, 20011), (200, 64, 12345), (257, 128, 9001), (520, 32, 5003), (700, 160, 3333), (2100, 64, 1001),
+          (3000, 256, 256), (4100, 32, 32)]
+# float32 by pairs of float16 numbers, from the rows on where that is faster
+PAIRS = [(5000, 64, 4097), (2600, 160, 3333), (10001, 64, 4097), (300, 256, 50257), (300, 2048, 32000), (520, 96, 131073), (9000, 512, 1000)]
+
+
+@pytest.mark.parametrize("T,d,V", PAIRS)
+def test_float32_by_pairs(T, d, V):
+    check(T, d, V, "f32", seed=T + V)
+    check(T, d, V, "f32", seed=T + V + 1, whole=d <= 512)
+    check(T, d, V, "bf16", seed=T + V)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -154,7 +167,7 @@ def test_log_probabilities_and_gradients(T, d, V, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("T,d,V", [(1, 32, 5), (70, 64, 333), (300, 256, 2000), (9001, 32, 100)])
+@pytest.mark.parametrize("T,d,V", [(1, 32, 5), (70, 64, 333), (300, 256, 2000), (9001, 32, 100), (700, 96, 5003), (5001, 64, 4097), (40, 64, 9000)])
 def test_sums_are_added_to_and_results_are_the_same_bits_again(T, d, V, dtype):
     """Also more rows than a piece has; also dX in the buffer of x, and either gradient alone."""
     x, W, targets, w, dX, dW, want, tol = check(T, d, V, dtype, seed=7)
@@ -177,11 +190,12 @@ def test_rows_and_gradients_of_any_size(times_x, times_w, dtype):
     """Powers of two leave the logits as they are."""
     check(70, 64, 300, dtype, seed=13, times_x=times_x, times_w=times_w)
     check(200, 64, 300, dtype, seed=14, times_x=times_x, times_w=times_w)
+    check(4800, 96, 2900, dtype, seed=15, times_x=times_x, times_w=times_w)
 
 
-@pytest.mark.parametrize("dtype,T", [("bf16", 64), ("bf16", 200), ("f32", 200)])
+@pytest.mark.parametrize("dtype,T", [("bf16", 64), ("bf16", 200), ("f32", 200), ("f32", 5000), ("bf16", 5000)])
 def test_weights_and_rows_of_sizes_far_apart(dtype, T):
-    d, V = 64, 300
+    d, V = 64, 300 if T < 1000 else 4097
     x, W, targets, w = inputs(T, d, V, dtype, 14)
     w = w * 2.0 ** torch.linspace(-30, 0, T, device="cuda")
     x[::3] *= 2.0 ** -12
@@ -283,7 +297,8 @@ def test_targets_that_are_none_and_targets_beyond(dtype):
     assert lp[7].isnan() and dX[7].isnan().all() and dX[others].isfinite().all() and dW.isnan().all()
 
 
-@pytest.mark.parametrize("dtype,T,d,V", [("bf16", 100, 128, 1000), ("f32", 33, 64, 500), ("bf16", 5, 256, 3000), ("bf16", 1, 64, 2000)])
+@pytest.mark.parametrize("dtype,T,d,V", [("bf16", 100, 128, 1000), ("f32", 33, 64, 500), ("bf16", 5, 256, 3000), ("bf16", 1, 64, 2000), ("bf16", 300, 64, 7001), ("f32", 300, 64, 7001),
+                                          ("f32", 4800, 96, 2900)])
 def test_capture_replay_and_another_stream(dtype, T, d, V):
     x, W, targets, w = inputs(T, d, V, dtype, 1)
     ws = workspace(T, d, V, dtype, m.WS_BWD)[0]

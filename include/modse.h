@@ -328,14 +328,21 @@ modse_status modse_embed_bwd(int64_t T, int32_t d_model, int32_t vocab, modse_dt
                              float scale, float* dE, int accumulate, void* ws, size_t ws_bytes, void* hip_stream);
 
 /* Log probabilities from the last hidden rows: logits l = x W^T, of which a
- * workspace of a fixed size holds a piece at a time.
+ * workspace holds a piece at a time: it stops growing with T (some GiB for gradients).
  *   x        [T, d_model] of `dtype` (d_model a multiple of 32 up to 16384; T up to 2^24)
  *   W        [vocab, d_model] of `dtype`, the output matrix (vocab 1..2^20)
- *   targets  [T] int32.  Negative: no target, logp 0 and no gradient.  One that is not
- *            below vocab: logp NaN, and so are its row of dX and all of dW
+ *   targets  [T] int32.  Negative: no target, logp 0 and no gradient, whatever stands in
+ *            that row of x and d_logp.  One that is not below vocab: logp NaN, and so
+ *            are its row of dX and all of dW
  *   logp     [T] float32 out: log softmax(l_t)[target_t]
  *   log_z    [T] float32 out: log sum_v e^l_tv.  modse_head_fwd: either may be NULL
- * x, W, dX, dW and the workspace lie at addresses that are multiples of 16. */
+ * x, W, dX, dW and the workspace lie at addresses that are multiples of 16.
+ * Float32 with more rows than a few hundred (as many as make that the faster way), and
+ * vocab d_model up to 2^28: x and W are held in 22 bits each, x down to 2^-39 of the
+ * largest value of its row (modse_head_bwd: of all rows with a target), W down to 2^-39
+ * of its largest; what is smaller may be lost.  The workspace then also holds the parts
+ * of W, 4 vocab d_model bytes.  An infinity or NaN in a row of x makes that row's logp
+ * NaN (and its row of dX, and dW), one in W every row's. */
 modse_status modse_head_workspace_size(int64_t T, int32_t d_model, int32_t vocab, modse_dtype dtype, int which, size_t* bytes);
 modse_status modse_head_fwd(int64_t T, int32_t d_model, int32_t vocab, modse_dtype dtype, const void* x, const void* W,
                             const int32_t* targets, float* logp, float* log_z, void* ws, size_t ws_bytes, void* hip_stream);
@@ -348,8 +355,9 @@ modse_status modse_head_fwd(int64_t T, int32_t d_model, int32_t vocab, modse_dty
  *   dW      [vocab, d_model] float32 out, or NULL: overwritten, or added to with
  *           accumulate = 1
  * In bf16 the gradient of the logits is rounded to bf16 for dX.  For dW it is held in
- * 22 bits, down to 2^-39 of the largest |d_logp| (of a row with a target), and x
- * exactly, down to 2^-39 of the largest |x|: what is smaller may be lost.
+ * 22 bits, down to 2^-39 of the largest |d_logp|, and x exactly, down to 2^-39 of the
+ * largest |x| (both of rows with a target): what is smaller may be lost.  So it is for
+ * dX and dW in float32 where x and W are held in 22 bits.
  * Workspace sizes: MODSE_WS_FWD and MODSE_WS_BWD for the two calls.  Sums run in an
  * order that the sizes alone fix, the two calls' in orders of their own.  T == 0
  * leaves dW as it is. */

@@ -95,7 +95,8 @@ enum GemmEpilogue {
   // there is a C.  E2: the problem's first column in the lower half, the pairs of a row block of 128 columns in the upper
   EPI_LOGITS = 6,
   // EPI_STORE_F32, EPI_ROWS_F32 and EPI_LOGITS of float32 matrices that are held as sums of two float16 ones each, (A + A2) (B + B2)^T less
-  // the product of the second parts.  Of EPI_LOGITS_PAIRS the two floats before C3 are factors of acc.
+  // the product of the second parts.  Of EPI_LOGITS_PAIRS the float before C3 and, for each
+  // row, one behind C3's [E2 >> 32] floats are factors of acc.
   EPI_STORE_PAIRS = 7,
   EPI_ROWS_PAIRS = 8,
   EPI_LOGITS_PAIRS = 9,

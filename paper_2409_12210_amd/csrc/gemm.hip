@@ -65,7 +65,7 @@ hipError_t run_block(const GemmPlan* plan, int n_prob, int accumulate, int optio
 template <typename T, int EPI, int LAYOUT>
 hipError_t run_block_tile(TileShape t, const GemmPlan* plan, int n_prob, int accumulate, int option, int64_t max_tiles, hipStream_t s) {
   if (t.bm == 128) return run_block<T, 128, EPI == EPI_SWIGLU ? 64 : 128, EPI, LAYOUT>(plan, n_prob, accumulate, option, max_tiles, s);
-  if constexpr (std::is_same_v<T, float> && EPI != EPI_STORE_F32)
+  if constexpr (std::is_same_v<T, float> && EPI != EPI_STORE_F32 && EPI != EPI_ROWS_F32)
     if (t.bm == 32) return run_block<T, 32, 32, EPI, LAYOUT>(plan, n_prob, accumulate, option, max_tiles, s);
   constexpr int BN = std::is_same_v<T, float> || EPI == EPI_SWIGLU ? 64 : 128;
   if constexpr (!std::is_same_v<T, float> && LAYOUT == LAYOUT_TN && EPI != EPI_SWIGLU)

@@ -553,12 +553,16 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64) void gg_bf16_kernel(const Ge
     const int cM = cc.M, cN = cc.N, cld = cc.ldc;
     if constexpr (LOGITS) {
       if constexpr (EPI == EPI_LOGITS_PAIRS) {
-        const float* const undo = reinterpret_cast<const float*>(cc.C3) - 2;
-        const float u0 = undo[0], u1 = undo[1];
+        const float* const undo = reinterpret_cast<const float*>(cc.C3);
+        const float of_b = undo[-1];
+        const float* const of_a = undo + (reinterpret_cast<uint64_t>(cc.E2) >> 32);
 #pragma unroll
-        for (int i = 0; i < MI; ++i)
+        for (int i = 0; i < MI; ++i) {
+          // (the smaller factor first, so that no product on the way overflows where the result does not)
+          const float u = of_a[min(cc.w.m0 + wm * WM + erow16 + i * 16, cM - 1)], u0 = fminf(u, of_b), u1 = fmaxf(u, of_b);
 #pragma unroll
           for (int j = 0; j < NI; ++j) acc[0][i][j] = acc[0][i][j] * u0 * u1;
+        }
       }
       // A row's 128 columns of this wave lie in four lanes, 32 in each.
       static_assert(WN == 128 && NB == 1, "pairs of 128 columns");

@@ -4,14 +4,22 @@
 //   l = x W^T,  log Z_t = log sum_v e^l_tv,  logp_t = l_t,target - log Z_t
 //   G_tv = w_t (1[v = target_t] - e^(l_tv - log Z_t)),  dX = G W,  dW = G^T x
 //
-// The batch is taken in pieces of rows whose G fits a workspace of a fixed size.  The products are those of the grouped GEMM kernels,
+// The batch is taken in pieces of rows whose G fits a workspace that stops growing with the batch.  The products are those of the grouped GEMM kernels,
 // whose problem tables one launch makes for the whole call.  dX is a product over the whole vocabulary with few columns, so its
 // sum is cut into parts that fill the chip; the parts are float32 slabs that a last launch adds up in order.
 //
 // bf16: the product of the logits leaves, for every row and 128 columns, their maximum and sum of exponentials, and the target's logit
 // (EPI_LOGITS); one launch joins them.  Without gradients no logit is stored.  With gradients the logits of a few rows are, in
-// float32 and in a buffer that stays in the caches, and another launch turns them into G.  float32: the logits are stored and
-// a row is gone through twice, the second time to put G in its place.
+// float32 and in a buffer that stays in the caches, and another launch turns them into G.
+//
+// float32 takes the same way from some hundred rows on: x, W and G are held as the sums of two float16 matrices, hi + lo, times powers of
+// two that bring the largest value below 2^15.  Three products of float16 matrices, hi hi' + hi lo' + lo hi', in one accumulator leave
+// out 2^-22 of a product; they take 3 of the 16-bit matrix rate where float32 instructions take 16 (1021 x 256 x 50257 with gradients:
+// 470 us in place of 731).  Fewer rows, or a W of more than 2^28 elements: products in float32; the logits are stored and a row is gone
+// through twice, the second time to put G in its place.
+//
+// Up to 64 rows (small vocabularies: more) a stream over W makes the logits, see "few rows".  dW of a small vocabulary has few tiles,
+// so its sum over the tokens is cut into parts as well (float32, 1000 x 512, 4096 rows: with the stream 160 us in place of 337 for the whole call).
 //
 // dX of a bf16 layer is rounded to bf16, and takes G rounded to bf16.  What that loses of the target's entry, the largest of its row as a
 // rule, is put back in float32 where the slabs are added up: it is a multiple of a row of W.  (Without that dX was off by 2.4e-3 of
@@ -142,17 +150,18 @@ HeadShape head_shape(int64_t T, int32_t d, int32_t vocab, modse_dtype dt, bool g
   return h;
 }
 
-// The largest |x|, |W| and |d_logp| of a call, as the bits of floats: by block, joined by a later launch.  (Bf16 layers need no |W|.)
+// The largest finite |x| and |d_logp| of the rows with a target and the largest |W| of a call, as the bits of floats: by block, joined by a
+// later launch.  (Bf16 layers need no |W|; scoring scales each row of x by itself.)
 constexpr int RANGE_BLOCKS = 512;
 struct HeadRange {
   uint32_t x_of[RANGE_BLOCKS], w_of[RANGE_BLOCKS], d_logp_of[RANGE_BLOCKS];
   int32_t blocks;
   uint32_t x, w, d_logp;
   // What undoes the scaling by two of them: the smaller factor first, so that no product on the way overflows where the result does not.
-  float undo_dx[2], undo_dw[2], pad[2];
-  float undo_logits[2];  // right before the targets' logits (EPI_LOGITS_PAIRS)
+  float undo_dx[2], undo_dw[2], pad[3];
+  float undo_w;  // right before the targets' logits (EPI_LOGITS_PAIRS)
 };
-static_assert(sizeof(HeadRange) == offsetof(HeadRange, undo_logits) + 8 && sizeof(HeadRange) % 16 == 0, "laid out up to the targets' logits");
+static_assert(sizeof(HeadRange) == offsetof(HeadRange, undo_w) + 4 && sizeof(HeadRange) % 16 == 0, "laid out up to the targets' logits");
 // the power of two that brings values of at most this size below 2^15
 __device__ __forceinline__ int scale_exponent(uint32_t bits) { return min(14 - ((int)(bits >> 23 & 255) - 127), 120); }
 __device__ __forceinline__ float power_of_two(int e) { return __builtin_bit_cast(float, (uint32_t)(e + 127) << 23); }
@@ -164,13 +173,14 @@ struct HeadBufs {
   GemmPlan* plans;   // logits of every product, then dX and dW of every piece
   float* logits;     // [sub, ldv]; float32 layers: then G
   float* pairs;      // [ceil(vocab / 128)][sub] maximum and sum
-  float* at_target;  // [sub] the target's logit
+  float* at_target;  // [sub] the target's logit, and behind them [sub] what undoes the scaling of a row of x (float32 by pairs)
   float* off;        // [sub][2] the row's maximum and log2 of its sum
   bf16_t* g;         // [dx_rows, ldv] G, and behind its rows what it lacks of them
   float* lost;       // [rows] what G lacks of the target's entry
   f16_t *hi, *lo;    // [rows, ldv] G in two parts, scaled
   f16_t *x16, *x16_lo;   // [rows, d] x in the same way; x16_lo: float32 layers
   f16_t *w16, *w16_lo;   // [vocab, d] W, float32 layers
+  float* x32;        // [rows, d] x, zeros in rows without a target: float32 layers that take no pairs
   HeadRange* range;
   float* slabs;      // [k_parts][dx_rows, d]
 };
@@ -185,23 +195,28 @@ struct HeadPlanArgs {
   int32_t plans;
 };
 
-// The largest absolute value of n elements (a multiple of 16), by the threads of some blocks of 1024.  (NaN counts as more than any number.)
-__device__ __forceinline__ uint32_t largest(const void* p, int64_t n, bool bf16, int64_t first, int64_t step) {
-  const u32x4* const v16 = static_cast<const u32x4*>(p);
-  const int64_t vectors = bf16 ? n / 8 : n / 4;
+// Infinities and NaN count as 0: they stay what they are in the parts, and the other values keep theirs.
+__device__ __forceinline__ uint32_t finite(uint32_t bits) { return (bits & 0x7fffffffu) < 0x7f800000u ? bits & 0x7fffffffu : 0; }
+__device__ __forceinline__ uint32_t largest(u32x4 v, bool bf16) {
+  uint32_t most = 0;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) most = max(most, bf16 ? max(finite(v[e] << 16), finite(v[e] & 0xffff0000u)) : finite(v[e]));
+  return most;
+}
+// of sixteen-byte vectors, every `step`th from `first` on
+__device__ __forceinline__ uint32_t largest(const u32x4* v16, int64_t vectors, bool bf16, int64_t first, int64_t step) {
   uint32_t most = 0;
   for (int64_t i = first; i < vectors; i += 4 * step) {
     u32x4 v[4];
 #pragma unroll
     for (int q = 0; q < 4; ++q) v[q] = v16[i + q * step < vectors ? i + q * step : i];
 #pragma unroll
-    for (int q = 0; q < 4; ++q)
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        most = max(most, bf16 ? max(v[q][e] << 16 & 0x7fff0000u, v[q][e] & 0x7fff0000u) : v[q][e] & 0x7fffffffu);
+    for (int q = 0; q < 4; ++q) most = max(most, largest(v[q], bf16));
   }
   return most;
 }
+// lanes that share a row of so many vectors: a power of two
+__device__ __forceinline__ int lanes_of(int vectors) { return vectors >= 64 ? 64 : 1 << (32 - __builtin_clz(max(vectors, 2) - 1)); }
 __device__ __forceinline__ uint32_t wave_most(uint32_t v) {
 #pragma unroll
   for (int o = 32; o; o >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, o, 64));
@@ -210,11 +225,17 @@ __device__ __forceinline__ uint32_t wave_most(uint32_t v) {
 __device__ __forceinline__ void range_block(const HeadPlanArgs& a, int block, int blocks) {
   __shared__ uint32_t s_most[3][16];
   const int64_t first = (int64_t)block * 1024 + threadIdx.x, step = (int64_t)blocks * 1024;
-  uint32_t most[3] = {largest(a.x, a.h.T * a.h.d, a.h.bf16, first, step),
-                      a.h.bf16 ? 0 : largest(a.W, (int64_t)a.h.vocab * a.h.d, false, first, step), 0};
-  if (a.d_logp)
-    for (int64_t t = first; t < a.h.T; t += step)
-      if (a.targets[t] >= 0 && a.targets[t] < a.h.vocab) most[2] = max(most[2], __builtin_bit_cast(uint32_t, a.d_logp[t]) & 0x7fffffffu);
+  const bool bf16 = a.h.bf16;
+  uint32_t most[3] = {0, bf16 ? 0 : largest(static_cast<const u32x4*>(a.W), (int64_t)a.h.vocab * a.h.d / 4, false, first, step), 0};
+  if (a.d_logp) {
+    const int vectors = bf16 ? a.h.d / 8 : a.h.d / 4, lanes = lanes_of(vectors), lane = threadIdx.x & (lanes - 1);
+    for (int64_t t = first / lanes; t < a.h.T; t += step / lanes) {
+      const int32_t target = a.targets[t];
+      if (target < 0 || target >= a.h.vocab) continue;
+      most[0] = max(most[0], largest(static_cast<const u32x4*>(a.x) + t * vectors, vectors, bf16, lane, lanes));
+      most[2] = max(most[2], finite(__builtin_bit_cast(uint32_t, a.d_logp[t])));
+    }
+  }
 #pragma unroll
   for (int k = 0; k < 3; ++k) {
     most[k] = wave_most(most[k]);
@@ -249,8 +270,7 @@ __device__ __forceinline__ void join_range(HeadRange* r) {
     r->w = w;
     r->d_logp = g;
     const float ux = power_of_two(-scale_exponent(x)), uw = power_of_two(-scale_exponent(w)), ug = power_of_two(-scale_exponent(g));
-    r->undo_logits[0] = fminf(ux, uw);
-    r->undo_logits[1] = fmaxf(ux, uw);
+    r->undo_w = uw;
     r->undo_dx[0] = fminf(ug, uw);
     r->undo_dx[1] = fmaxf(ug, uw);
     r->undo_dw[0] = fminf(ug, ux);
@@ -258,14 +278,25 @@ __device__ __forceinline__ void join_range(HeadRange* r) {
   }
 }
 
-// float32 by pairs: n elements (a multiple of 16) in two parts.  Every block joins the largest values for itself.
-__global__ __launch_bounds__(256) void head_split_kernel(const float* p, int64_t n, f16_t* hi, f16_t* lo, HeadRange* range, int is_w) {
+// float32 by pairs: eight elements in two parts
+__device__ __forceinline__ void put_parts(const f32x4 (&v)[2], float scale, f16_t* hi, f16_t* lo) {
+  f16x8 h, l;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const float x = v[e >> 2][e & 3] * scale;
+    h[e] = (f16_t)x;
+    l[e] = (f16_t)(x - (float)h[e]);
+  }
+  *reinterpret_cast<f16x8*>(hi) = h;
+  *reinterpret_cast<f16x8*>(lo) = l;
+}
+// W, n elements (a multiple of 16).  Every block joins the largest values for itself, the first one all of them.
+__global__ __launch_bounds__(256) void head_split_w_kernel(const float* W, int64_t n, f16_t* hi, f16_t* lo, HeadRange* range) {
   __shared__ uint32_t s_most;
   if (threadIdx.x < 64) {
     const int lane = threadIdx.x, blocks = range->blocks;
-    const uint32_t* const of = is_w ? range->w_of : range->x_of;
     uint32_t most = 0;
-    for (int i = lane; i < blocks; i += 64) most = max(most, of[i]);
+    for (int i = lane; i < blocks; i += 64) most = max(most, range->w_of[i]);
     most = wave_most(most);
     if (lane == 0) s_most = most;
     if (blockIdx.x == 0) join_range(range);
@@ -274,17 +305,36 @@ __global__ __launch_bounds__(256) void head_split_kernel(const float* p, int64_t
   const float scale = power_of_two(scale_exponent(s_most));
   const int64_t step = (int64_t)gridDim.x * 2048;
   for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8; i < n; i += step) {
-    const f32x4 v[2] = {__builtin_nontemporal_load(reinterpret_cast<const f32x4*>(p + i)),
-                        __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(p + i + 4))};
-    f16x8 h, l;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const float x = v[e >> 2][e & 3] * scale;
-      h[e] = (f16_t)x;
-      l[e] = (f16_t)(x - (float)h[e]);
+    const f32x4 v[2] = {__builtin_nontemporal_load(reinterpret_cast<const f32x4*>(W + i)),
+                        __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(W + i + 4))};
+    put_parts(v, scale, hi + i, lo + i);
+  }
+}
+// Rows of x, some lanes of a wave each.  Scoring: each by its own largest value, so that what stands in one row (one that pads the batch,
+// say) does not touch another.  Gradients, whose sum for dW runs over rows: by that of all rows with a target, and zeros for the others.
+__global__ __launch_bounds__(256) void head_split_x_kernel(const float* x, const int32_t* targets, int rows, int d, int vocab, int grad,
+                                                           const HeadRange* range, f16_t* hi, f16_t* lo, float* undo, int undo_rows) {
+  const int lanes = lanes_of(d / 8), lane = threadIdx.x & (lanes - 1);
+  const int64_t row = ((int64_t)blockIdx.x * 256 + threadIdx.x) / lanes;
+  if (row >= rows) return;
+  const int64_t at = row * d;
+  uint32_t most = 0;
+  if (grad) {
+    most = range->x;
+  } else {
+    most = largest(reinterpret_cast<const u32x4*>(x + at), d / 4, false, lane, lanes);
+    for (int o = lanes / 2; o; o >>= 1) most = max(most, (uint32_t)__shfl_xor((int)most, o, 64));
+  }
+  const int e = scale_exponent(most);
+  if (lane == 0 && row < undo_rows) undo[row] = power_of_two(-e);
+  const bool there = !grad || (targets[row] >= 0 && targets[row] < vocab);
+  for (int c = lane * 8; c < d; c += lanes * 8) {
+    f32x4 v[2] = {};
+    if (there) {
+      v[0] = *reinterpret_cast<const f32x4*>(x + at + c);
+      v[1] = *reinterpret_cast<const f32x4*>(x + at + c + 4);
     }
-    *reinterpret_cast<f16x8*>(hi + i) = h;
-    *reinterpret_cast<f16x8*>(lo + i) = l;
+    put_parts(v, power_of_two(e), hi + at + c, lo + at + c);
   }
 }
 
@@ -348,7 +398,7 @@ __global__ __launch_bounds__(1024) void head_plan_kernel(HeadPlanArgs a) {
       const size_t g0 = (size_t)r0 * h.ldv, x0 = (size_t)r0 * h.d;
       P.A = h.wide ? (const void*)(a.b.hi + g0) : (const void*)a.b.logits;
       P.A2 = a.b.lo + g0;
-      P.B = P.B2 = h.wide ? (const void*)(a.b.x16 + x0) : x;
+      P.B = P.B2 = h.wide ? (const void*)(a.b.x16 + x0) : a.b.x32;
       if (h.pairs) P.B2 = a.b.x16_lo + x0;
       P.E1 = a.b.range ? a.b.range->undo_dw : nullptr;
       P.C = h.w_split > 1 ? a.b.slabs + (size_t)p * h.vocab * h.d : a.dW;
@@ -377,8 +427,9 @@ struct HeadRowsArgs {
   float* lost;             // null where there is no dX
   f16_t *hi, *lo;          // null where there is no dW
   HeadRange* range;
-  const bf16_t* x;         // of the product's first row, and their copies
+  const void* x;           // of the product's first row, and their copies for dW, with zeros in rows without a target
   f16_t* x16;
+  float* x32;              // (float32 layers) null where there is no dW
   int32_t rows, vocab, ldv, pair_rows, d;
 };
 __device__ __forceinline__ float row_weight(const HeadRowsArgs& a, int row, int32_t target) {
@@ -442,10 +493,11 @@ __global__ __launch_bounds__(256) void head_grad_kernel(HeadRowsArgs a, int segs
     const int64_t i = (int64_t)(blockIdx.x - a.rows * segs) * 2048 + threadIdx.x * 8;
     if (i >= (int64_t)a.rows * a.d) return;
     const float scale = power_of_two(scale_exponent(a.range->x));
-    const bf16x8 v = *reinterpret_cast<const bf16x8*>(a.x + i);
+    const int32_t target = a.targets[(uint32_t)i / (uint32_t)a.d];
+    const bf16x8 v = *reinterpret_cast<const bf16x8*>(static_cast<const bf16_t*>(a.x) + i);
     f16x8 o;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) o[k] = (f16_t)((float)v[k] * scale);
+    for (int k = 0; k < 8; ++k) o[k] = target >= 0 && target < a.vocab ? (f16_t)((float)v[k] * scale) : (f16_t)0.f;
     *reinterpret_cast<f16x8*>(a.x16 + i) = o;
     return;
   }
@@ -524,6 +576,10 @@ __global__ __launch_bounds__(512) void head_rows_kernel(HeadRowsArgs a) {
   if constexpr (GRAD) {
     __syncthreads();  // (the target's logit has been read)
     const float w = row_weight(a, t, target);
+    if (a.x32)
+      for (int c = tid * 4; c < a.d; c += W * 256)
+        *reinterpret_cast<f32x4*>(a.x32 + (int64_t)t * a.d + c) =
+            target >= 0 && target < a.vocab ? *reinterpret_cast<const f32x4*>(static_cast<const float*>(a.x) + (int64_t)t * a.d + c) : f32x4{};
     for (int c = tid * 4; c < a.ldv; c += W * 256) {
       f32x4 g = c < a.vocab ? load(c) : f32x4{};
 #pragma unroll
@@ -807,7 +863,7 @@ size_t stream_pairs(int64_t T, int32_t vocab) { return (size_t)T * ((vocab + STR
 size_t stream_workspace(int64_t T, int32_t vocab) { return ALIGN + align_up(stream_pairs(T, vocab), ALIGN) + (size_t)T * 4; }
 
 struct HeadLayout {
-  size_t range, logits, pairs, at_target, off, lost, g, hi, lo, x16, x16_lo, w16, w16_lo, slabs, total;
+  size_t range, logits, pairs, at_target, off, lost, g, hi, lo, x16, x16_lo, w16, w16_lo, x32, slabs, total;
 };
 HeadLayout layout_for(int64_t plans, int64_t sub, int64_t rows, int64_t dx_rows, int64_t slab_cells, int32_t d, int32_t vocab, bool bf16,
                       bool pairs, bool grad) {
@@ -824,7 +880,7 @@ HeadLayout layout_for(int64_t plans, int64_t sub, int64_t rows, int64_t dx_rows,
   // (the range ends where the targets' logits begin)
   at = align_up(at + sizeof(HeadRange), ALIGN);
   w.range = at - sizeof(HeadRange);
-  w.at_target = take((size_t)sub * 4);
+  w.at_target = take((size_t)sub * (pairs ? 8 : 4));
   w.logits = take(wide && !grad ? 0 : (size_t)sub * ldv * 4);
   w.pairs = take(std::max(wide ? (size_t)sub * ((vocab + 127) / 128) * 8 : 0, stream_pairs(std::min(sub, stream_rows(vocab)), vocab)));
   w.off = take(wide ? (size_t)sub * 8 : 0);
@@ -836,6 +892,7 @@ HeadLayout layout_for(int64_t plans, int64_t sub, int64_t rows, int64_t dx_rows,
   w.x16_lo = take(pairs ? (size_t)rows * d * 2 : 0);
   w.w16 = take(pairs ? (size_t)vocab * d * 2 : 0);
   w.w16_lo = take(pairs ? (size_t)vocab * d * 2 : 0);
+  w.x32 = take(!wide && grad ? (size_t)rows * d * 4 : 0);
   w.slabs = take(grad ? (size_t)slab_cells * 4 : 0);
   w.total = at;
   return w;
@@ -883,25 +940,30 @@ hipError_t launch_head(modse_dtype dt, const HeadArgs& a, char* ws, hipStream_t 
   HeadRange* const range = h.pairs || (h.bf16 && grad) ? reinterpret_cast<HeadRange*>(ws + w.range) : nullptr;
   const HeadBufs b = {reinterpret_cast<GemmPlan*>(ws), floats(w.logits), floats(w.pairs), floats(w.at_target), floats(w.off),
                       reinterpret_cast<bf16_t*>(ws + w.g), floats(w.lost), halves(w.hi), halves(w.lo), halves(w.x16), halves(w.x16_lo),
-                      halves(w.w16), halves(w.w16_lo), range, floats(w.slabs)};
+                      halves(w.w16), halves(w.w16_lo), floats(w.x32), range, floats(w.slabs)};
   const HeadPlanArgs plan = {h, b, a.x, a.W, a.targets, a.d_logp, a.dW, (int32_t)plans};
   const int64_t looked_at = h.T * h.d + (h.pairs ? (int64_t)h.vocab * h.d : 0);
   const int64_t range_blocks = range ? std::min<int64_t>((looked_at + 32767) / 32768, RANGE_BLOCKS) : 0;
   hipLaunchKernelGGL(head_plan_kernel, dim3((unsigned)(plans + range_blocks)), dim3(1024), 0, s, plan);
-  auto split = [&](const void* p, int64_t n, f16_t* hi, f16_t* lo, int is_w) {
-    const dim3 grid((unsigned)std::min<int64_t>((n + 2047) / 2048, 2048));
-    hipLaunchKernelGGL(head_split_kernel, grid, dim3(256), 0, s, static_cast<const float*>(p), n, hi, lo, range, is_w);
-  };
-  if (h.pairs) split(a.W, (int64_t)h.vocab * h.d, b.w16, b.w16_lo, 1);
-  const bf16_t* const x = static_cast<const bf16_t*>(a.x);
+  if (h.pairs) {
+    const int64_t n = (int64_t)h.vocab * h.d;
+    hipLaunchKernelGGL(head_split_w_kernel, dim3((unsigned)std::min<int64_t>((n + 2047) / 2048, 2048)), dim3(256), 0, s,
+                       static_cast<const float*>(a.W), n, b.w16, b.w16_lo, range);
+  }
   auto tiles = [](int64_t m, int64_t n, TileShape t) { return ((m + t.bm - 1) / t.bm) * ((n + t.bn - 1) / t.bn); };
   hipError_t e = hipGetLastError();
   // the logits of one product, their sums and (of gradients) G
   auto product = [&](int64_t i) {
     const int64_t t0 = i * h.sub, m = std::min<int64_t>(h.sub, h.T - t0), in_piece = t0 % h.rows;
     const bool stream = h.T <= stream_rows(h.vocab) && products == 1;  // (only with gradients here)
-    if (h.pairs && in_piece == 0)
-      split(static_cast<const float*>(a.x) + t0 * h.d, std::min<int64_t>(h.rows, h.T - t0) * h.d, b.x16, b.x16_lo, 0);
+    if (h.pairs && in_piece == 0) {
+      int lanes = 64;
+      while (lanes > 2 && lanes / 2 >= h.d / 8) lanes /= 2;
+      const int64_t rows = std::min<int64_t>(h.rows, h.T - t0);
+      hipLaunchKernelGGL(head_split_x_kernel, dim3((unsigned)((rows * lanes + 255) / 256)), dim3(256), 0, s,
+                         static_cast<const float*>(a.x) + t0 * h.d, a.targets + t0, (int)rows, h.d, h.vocab, (int)grad, range, b.x16, b.x16_lo,
+                         b.at_target + h.sub, h.sub);
+    }
     if (stream) {
       const HeadStreamArgs r = {a.x, a.W, a.targets, b.pairs, b.at_target, h.wide ? a.logp : nullptr, nullptr, b.logits,
                                 h.wide ? b.off : nullptr, range, (int32_t)m, h.d, h.vocab, h.ldv};
@@ -915,7 +977,8 @@ hipError_t launch_head(modse_dtype dt, const HeadArgs& a, char* ws, hipStream_t 
                             b.logits, b.pairs, b.at_target, b.off, a.dX && h.bf16 ? b.g + in_piece * h.ldv : nullptr,
                             a.dX && h.dx_rows > h.rows ? b.g + (int64_t)h.rows * h.ldv : nullptr, b.lost + in_piece,
                             a.dW || h.pairs ? b.hi + in_piece * h.ldv : nullptr, a.dW || h.pairs ? b.lo + in_piece * h.ldv : nullptr,
-                            range, x + t0 * h.d, b.x16 + in_piece * h.d, (int32_t)m, h.vocab, h.ldv, h.sub, h.d};
+                            range, static_cast<const char*>(a.x) + (size_t)t0 * h.d * (h.bf16 ? 2 : 4), b.x16 + in_piece * h.d,
+                            a.dW && !h.wide ? b.x32 + in_piece * h.d : nullptr, (int32_t)m, h.vocab, h.ldv, h.sub, h.d};
     if (h.wide) {
       if (!stream) hipLaunchKernelGGL(head_stats_kernel, dim3((unsigned)((m + 63) / 64)), dim3(1024), 0, s, r);
       const int64_t segs = (h.ldv + 2047) / 2048, copies = a.dW && h.bf16 ? (m * h.d + 2047) / 2048 : 0;

@@ -297,6 +297,34 @@ def test_targets_that_are_none_and_targets_beyond(dtype):
     assert lp[7].isnan() and dX[7].isnan().all() and dX[others].isfinite().all() and dW.isnan().all()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,d,V", [(40, 64, 300), (200, 64, 12345), (700, 96, 5003), (5000, 64, 4097)])
+def test_what_stands_in_one_row_touches_no_other(T, d, V, dtype):
+    """Rows without a target may hold anything; infinities and NaN in a row with one are that row's, and dW's.  The same bits elsewhere."""
+    x, W, targets, w = inputs(T, d, V, dtype, T + V)
+    rows = [1, 5, T // 2, T - 1]
+    targets[rows] = torch.tensor([-1, -7, -1, -2], dtype=torch.int32, device="cuda")
+    others = torch.ones(T, dtype=torch.bool, device="cuda")
+    others[rows] = False
+    for no_target in (True, False):
+        x[rows] = 0.0
+        filled = x.clone()
+        for row, value in zip(rows, (NAN, float("inf"), 1e30, -float("inf"))):
+            filled[row] = value
+        if not no_target:
+            targets[rows] = 3
+            x[rows[2]] = filled[rows[2]] = 1.0      # (a large number is one like others)
+        (a, b), (c, e) = forward(x, W, targets, dtype), forward(filled, W, targets, dtype)
+        assert torch.equal(a[others], c[others]) and torch.equal(b[others], e[others]) and a.isfinite().all()
+        was, now = backward(x, W, targets, w, dtype), backward(filled, W, targets, w, dtype)
+        assert torch.equal(was[0][others], now[0][others]) and torch.equal(was[1][others], now[1][others])
+        if no_target:
+            assert (c[rows] == 0).all() and torch.equal(was[0], now[0]) and torch.equal(was[1], now[1]) and torch.equal(was[2], now[2])
+        else:
+            wrong = [rows[0], rows[1], rows[3]]
+            assert c[wrong].isnan().all() and now[0][wrong].isnan().all() and now[1][wrong].isnan().all() and now[2].isnan().all()
+
+
 @pytest.mark.parametrize("dtype,T,d,V", [("bf16", 100, 128, 1000), ("f32", 33, 64, 500), ("bf16", 5, 256, 3000), ("bf16", 1, 64, 2000), ("bf16", 300, 64, 7001), ("f32", 300, 64, 7001),
                                           ("f32", 4800, 96, 2900)])
 def test_capture_replay_and_another_stream(dtype, T, d, V):

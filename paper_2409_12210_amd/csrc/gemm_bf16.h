@@ -576,7 +576,7 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64) void gg_bf16_kernel(const Ge
         const int row0 = cc.w.m0 + wm * WM + erow16;
         int want[MI];  // the target's column from this lane's first one on
 #pragma unroll
-        for (int i = 0; i < MI; ++i) want[i] = targets[min(row0 + i * 16, cM - 1)];
+        for (int i = 0; i < MI; ++i) want[i] = max(targets[min(row0 + i * 16, cM - 1)], -1);
         static_for<MI>([&](auto block) {
           constexpr int i = decltype(block)::value;
           const int row = row0 + i * 16;

@@ -817,7 +817,7 @@ __global__ __launch_bounds__(256, 2) void head_stream_kernel(HeadStreamArgs a) {
 #pragma unroll
     for (int q = 1; q < 4; ++q) l += *sum_at(q, wave * NT + j);
     if (a.logits && t < a.T && v < a.ldv) *reinterpret_cast<f32x4*>(a.logits + (int64_t)t * a.ldv + v) = l;
-    const int32_t at = t < a.T ? a.targets[t] - v : -1;
+    const int32_t at = t < a.T ? max(a.targets[t], -1) - v : -1;
     if (at >= 0 && at < 4 && v + at < a.vocab) a.at_target[t] = at == 0 ? l[0] : at == 1 ? l[1] : at == 2 ? l[2] : l[3];
 #pragma unroll
     for (int e = 0; e < 4; ++e)

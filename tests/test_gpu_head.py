@@ -149,7 +149,8 @@ SHAPES = [(1, 32, 1), (1, 64, 7), (2, 32, 31), (3, 96, 32), (5, 64, 33), (16, 12
           (128, 32, 16500), (129, 96, 20011), (200, 64, 12345), (257, 128, 9001), (520, 32, 5003), (700, 160, 3333), (2100, 64, 1001),
           (3000, 256, 256), (4100, 32, 32)]
 # float32 by pairs of float16 numbers, from the rows on where that is faster
-PAIRS = [(5000, 64, 4097), (2600, 160, 3333), (10001, 64, 4097), (300, 256, 50257), (300, 2048, 32000), (520, 96, 131073), (9000, 512, 1000)]
+PAIRS = [(5000, 64, 4097), (2600, 160, 3333), (10001, 64, 4097), (300, 256, 50257), (300, 2048, 32000), (520, 96, 131073), (9000, 512, 1000),
+         (70000, 256, 256)]
 
 
 @pytest.mark.parametrize("T,d,V", PAIRS)
@@ -279,8 +280,8 @@ def test_far_apart_and_equal_logits(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-def test_targets_that_are_none_and_targets_beyond(dtype):
-    T, d, V = 40, 64, 300
+@pytest.mark.parametrize("T,d,V", [(40, 64, 300), (300, 64, 9001), (5000, 64, 4097)])
+def test_targets_that_are_none_and_targets_beyond(dtype, T, d, V):
     x, W, targets, w = inputs(T, d, V, dtype, 12)
     w[3] = NAN                                        # of a row without a target: not used
     targets[3] = np.iinfo(np.int32).min

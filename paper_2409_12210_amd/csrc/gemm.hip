@@ -65,7 +65,7 @@ hipError_t run_block(const GemmPlan* plan, int n_prob, int accumulate, int optio
 template <typename T, int EPI, int LAYOUT>
 hipError_t run_block_tile(TileShape t, const GemmPlan* plan, int n_prob, int accumulate, int option, int64_t max_tiles, hipStream_t s) {
   if (t.bm == 128) return run_block<T, 128, EPI == EPI_SWIGLU ? 64 : 128, EPI, LAYOUT>(plan, n_prob, accumulate, option, max_tiles, s);
-  if constexpr (std::is_same_v<T, float> && EPI != EPI_STORE_F32 && EPI != EPI_ROWS_F32)
+  if constexpr (std::is_same_v<T, float> && EPI != EPI_STORE_F32 && EPI != EPI_ROWS_F32 && EPI != EPI_LOGITS)
     if (t.bm == 32) return run_block<T, 32, 32, EPI, LAYOUT>(plan, n_prob, accumulate, option, max_tiles, s);
   constexpr int BN = std::is_same_v<T, float> || EPI == EPI_SWIGLU ? 64 : 128;
   if constexpr (!std::is_same_v<T, float> && LAYOUT == LAYOUT_TN && EPI != EPI_SWIGLU)
@@ -94,6 +94,9 @@ hipError_t launch_block(int epilogue, int layout, TileShape t, const GemmPlan* p
       }
       if (layout == LAYOUT_TN) return run_block_tile<T, EPI_STORE_F32, LAYOUT_TN>(t, plan, n_prob, accumulate, option, max_tiles, s);
       return run_block_tile<T, EPI_STORE_F32, LAYOUT_AB_K>(t, plan, n_prob, accumulate, option, max_tiles, s);  // (bf16: where dX has 256-row tiles)
+    case EPI_LOGITS:
+      if constexpr (std::is_same_v<T, float>) return run_block_tile<T, EPI_LOGITS, LAYOUT_TN>(t, plan, n_prob, accumulate, option, max_tiles, s);
+      else return run_block<T, 128, 128, EPI_LOGITS, LAYOUT_TN>(plan, n_prob, accumulate, option, max_tiles, s);
     case EPI_ROWS_F32:
       if constexpr (std::is_same_v<T, float>) return run_block_tile<T, EPI_ROWS_F32, LAYOUT_AB_K>(t, plan, n_prob, accumulate, option, max_tiles, s);
       else return hipErrorInvalidValue;

@@ -383,7 +383,7 @@ __device__ __forceinline__ void gg_block(const GemmPlan* __restrict__ plan, int 
   // A wave stages units of 32 rows x 128 bytes (64 for a 32-column bf16 tile) through LDS, so that global memory sees
   // whole lines: written in accumulator order, read back row-wise.  The staging area lies in the slots that the step
   // after the last one would use: nobody reads them any more and no load is on its way into them.
-  typedef std::conditional_t<F32 || EPI == EPI_STORE_F32, float, bf16_t> out_t;
+  typedef std::conditional_t<F32 || EPI == EPI_STORE_F32 || EPI == EPI_LOGITS, float, bf16_t> out_t;
   static_assert(F32 || EPI != EPI_ROWS_F32, "for float32");
   constexpr int OS = sizeof(out_t), UC = OS == 4 ? 32 : (WN < 64 ? WN : 64);  // columns of a unit
   constexpr int CPR = UC * OS / 16, ITS = 32 * CPR / 64, NJU = WN / UC, JPU = UC / 32;
@@ -435,6 +435,45 @@ __device__ __forceinline__ void gg_block(const GemmPlan* __restrict__ plan, int 
       if (o >= 0) put(C, o, v);
     }
   };
+  if constexpr (EPI == EPI_LOGITS) {  // maximum and sum of each row's columns of this wave, and the target's logit
+    static_assert(!A_T && !B_T && NB == 1, "rows of logits");
+    constexpr float LOG2E = 1.44269504088896340736f;
+    const int nw = n0 + wn * WN, nleft = N - nw;  // the wave's first column, columns from there on
+    const uint64_t place = reinterpret_cast<uint64_t>(P.E2());
+    const int first_col = (int)(uint32_t)place + nw;
+    float* const part = static_cast<float*>(P.C2()) + (size_t)(first_col / WN) * (place >> 32) * 2;
+    const int32_t* const targets = static_cast<const int32_t*>(P.E1());
+    if (nleft > 0) {
+#pragma unroll
+      for (int i = 0; i < MI; ++i) {
+        const int row = m0 + wm * WM + i * 32 + er;
+        const int at = max(targets[min(row, M - 1)], -1) - first_col - khalf * 4;
+        float m = -__builtin_inff(), there = 0.f, s = 0.f;
+        auto value = [&](int j, int x) { return j * 32 + (x >> 2) * 8 + (x & 3) + khalf * 4 < nleft ? acc[0][i][j][x] : -__builtin_inff(); };
+#pragma unroll
+        for (int j = 0; j < NI; ++j)
+#pragma unroll
+          for (int x = 0; x < 16; ++x) {
+            const float v = value(j, x);
+            m = fmaxf(m, v);
+            there = at == j * 32 + (x >> 2) * 8 + (x & 3) ? v : there;
+          }
+        m = fmaxf(m, __shfl_xor(m, 32, 64));
+#pragma unroll
+        for (int j = 0; j < NI; ++j)
+#pragma unroll
+          for (int x = 0; x < 16; ++x) s += __builtin_amdgcn_exp2f((value(j, x) - m) * LOG2E);
+        s += __shfl_xor(s, 32, 64);
+        if (row < M) {
+          typedef float f32x2 __attribute__((ext_vector_type(2)));
+          if (khalf == 0) *reinterpret_cast<f32x2*>(part + (size_t)row * 2) = f32x2{m, s};
+          if (at >= 0 && at < WN && (at & 4) == 0 && at + khalf * 4 < nleft)
+            static_cast<float*>(P.C3())[row] = there;
+        }
+      }
+    }
+    if (!P.C()) return;
+  }
 #pragma unroll
   for (int i = 0; i < MI; ++i) {
     if (m0 + wm * WM + i * 32 >= M) break;

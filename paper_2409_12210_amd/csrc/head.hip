@@ -8,15 +8,14 @@
 // whose problem tables one launch makes for the whole call.  dX is a product over the whole vocabulary with few columns, so its
 // sum is cut into parts that fill the chip; the parts are float32 slabs that a last launch adds up in order.
 //
-// bf16: the product of the logits leaves, for every row and 128 columns, their maximum and sum of exponentials, and the target's logit
-// (EPI_LOGITS); one launch joins them.  Without gradients no logit is stored.  With gradients the logits of a few rows are, in
-// float32 and in a buffer that stays in the caches, and another launch turns them into G.
+// The product of the logits leaves, for every row and 32 to 128 columns, their maximum and sum of exponentials, and the target's logit
+// (EPI_LOGITS); one launch joins them.  Without gradients no logit is stored.  With gradients the logits are, in float32, and another
+// launch turns them into G.
 //
-// float32 takes the same way from some hundred rows on: x, W and G are held as the sums of two float16 matrices, hi + lo, times powers of
+// float32 from some hundred rows on: x, W and G are held as the sums of two float16 matrices, hi + lo, times powers of
 // two that bring the largest value below 2^15.  Three products of float16 matrices, hi hi' + hi lo' + lo hi', in one accumulator leave
 // out 2^-22 of a product; they take 3 of the 16-bit matrix rate where float32 instructions take 16 (1021 x 256 x 50257 with gradients:
-// 470 us in place of 731).  Fewer rows, or a W of more than 2^28 elements: products in float32; the logits are stored and a row is gone
-// through twice, the second time to put G in its place.
+// 470 us in place of 731).  Fewer rows, or a W of more than 2^28 elements: products in float32, and G in the place of the logits.
 //
 // Up to 64 rows (small vocabularies: more) a stream over W makes the logits, see "few rows".  dW of a small vocabulary has few tiles,
 // so its sum over the tokens is cut into parts as well (float32, 1000 x 512, 4096 rows: with the stream 160 us in place of 337 for the whole call).
@@ -63,6 +62,7 @@ struct HeadShape {
   int32_t pairs;           // float32, and the matrices are held as pairs of float16 ones
   int32_t wide;            // either of them: tiles of 256, sums of exponentials by the product of the logits
   TileShape logits_tile, dx_tile, dw_tile;
+  __host__ __device__ int pair_cols() const { return logits_tile.bn / 2; }  // columns of a pair of maximum and sum
   __host__ __device__ int64_t products() const { return (T + sub - 1) / sub; }  // (sub divides rows)
 };
 
@@ -81,8 +81,8 @@ int64_t most_sub(int32_t vocab, bool wide, bool grad) {
 }
 // Float32 layers: the rows from which on products of pairs of float16 numbers are faster, three 16-bit products in place of one of float32,
 // with the largest values and the parts of W (and some launches) before them.  At 105 and 1150 TFLOP/s, 5 TB/s and tiles that are 128 rows too
-// high on average.  Float32 / pairs, us: gradients with 32000 x 2048, 128 rows 505, 256 830 / 590, 1024 3060 / 1200; with 50257 x 256, 256
-// rows 227 / 202, 1024 733 / 466; scoring with 32000 x 2048, 256 rows 288 / 304, 512 550 / 323.
+// high on average.  Float32 / pairs, us: gradients with 32000 x 2048, 256 rows 830 / 575, 1024 3060 / 1150; with 50257 x 256, 256 rows 227 / 195,
+// 1024 733 / 455; scoring with 32000 x 2048, 256 rows 262 / 294, 512 550 / 313; with 50257 x 256, 300 rows 81 / 97, 400 106 / 97.
 int64_t pairs_from(int32_t d, int32_t vocab, bool grad) {
   const double cells = (double)vocab * d, products = grad ? 6 : 2;
   const double fixed = 3 * products * 128 * cells / 1.15e9 + 12 * cells / 5e6 + (grad ? 50 : 35);
@@ -95,6 +95,17 @@ bool takes_pairs(int64_t T, int32_t d, int32_t vocab, modse_dtype dt, bool grad)
 // one block of rows.
 constexpr int STREAM_W = 64;
 int64_t stream_rows(int32_t vocab) { return std::max<int64_t>(1, 512 / ((vocab + STREAM_W - 1) / STREAM_W)) * 64; }
+// Bf16 layers: the logits take tiles of 128, two of which share a CU, where tiles of 256 are few or a tile is but a few steps of K.  Tiles of
+// 256 / 128, us: 128 rows with 32000 x 2048 54 / 36, 131072 x 128 41 / 22; 256 rows 55 / 51, 35 / 30; 512 rows with 32000 x 1024 44 / 53, 131072
+// x 512 86 / 88, 50257 x 256 38 / 33, 4096 rows 177 / 157; with gradients 512 rows x 50257 x 256 198 / 182, 2048 rows 541 / 562.
+constexpr int64_t BLOCK_ROWS = 256, BLOCK_ROWS_GRAD = 1024;
+bool takes_blocks(int64_t T, int32_t d, bool grad) { return T <= BLOCK_ROWS || (d <= 256 && (!grad || T <= BLOCK_ROWS_GRAD)); }
+// pairs of maximum and sum for so many rows of any batch
+size_t pair_cells(int64_t rows, int32_t d, int32_t vocab, bool wide, bool grad) {
+  auto of = [&](int64_t n, int cols) { return (size_t)n * ((vocab + cols - 1) / cols); };
+  const int64_t block_rows = d > 256 ? BLOCK_ROWS : grad ? BLOCK_ROWS_GRAD : rows;
+  return wide ? std::max(of(rows, 128), of(std::min(rows, block_rows), 64)) : of(rows, 32);
+}
 // Parts of dW's sum over the tokens, where it has too few tiles for the chip: slabs like those of dX, added up behind it.
 int64_t dw_most_parts(int32_t d, int32_t vocab, bool wide) {
   const int64_t tiles = (int64_t)((vocab + 255) / 256) * ((d + 255) / 256);
@@ -124,7 +135,7 @@ HeadShape head_shape(int64_t T, int32_t d, int32_t vocab, modse_dtype dt, bool g
   // (float32: tiles of 128 from four rounds of the chip's 512 workgroups on.  50304 x 256, 1.5 rounds: 287 us with them, 258 with tiles of
   // 64; 1021 x 50257, 6.1 rounds: 251 and 261)
   auto tile = [&](int64_t m, int64_t n) { const int b = h.wide ? 256 : tiles(m, n, 128) >= 2048 ? 128 : 64; return TileShape{b, b}; };
-  h.logits_tile = tile(h.sub, vocab);
+  h.logits_tile = h.bf16 && takes_blocks(T, d, grad) ? TileShape{128, 128} : tile(h.sub, vocab);
   h.dw_tile = tile(vocab, d);
   const int64_t w_steps = (h.rows + 63) / 64, w_split = std::min(dw_most_parts(d, vocab, h.wide), std::max<int64_t>(1, w_steps / 4));
   h.w_len = (int32_t)((w_steps + w_split - 1) / w_split) * 64;
@@ -172,7 +183,7 @@ typedef f16_t f16x8 __attribute__((ext_vector_type(8)));
 struct HeadBufs {
   GemmPlan* plans;   // logits of every product, then dX and dW of every piece
   float* logits;     // [sub, ldv]; float32 layers: then G
-  float* pairs;      // [ceil(vocab / 128)][sub] maximum and sum
+  float* pairs;      // [ceil(vocab / pair_cols)][sub] maximum and sum
   float* at_target;  // [sub] the target's logit, and behind them [sub] what undoes the scaling of a row of x (float32 by pairs)
   float* off;        // [sub][2] the row's maximum and log2 of its sum
   bf16_t* g;         // [dx_rows, ldv] G, and behind its rows what it lacks of them
@@ -371,7 +382,7 @@ __global__ __launch_bounds__(1024) void head_plan_kernel(HeadPlanArgs a) {
         P.B = a.b.w16 + (size_t)v0 * h.d;
         P.B2 = a.b.w16_lo + (size_t)v0 * h.d;
       }
-      if (h.grad || !h.wide) P.C = a.b.logits + v0;
+      if (h.grad) P.C = a.b.logits + v0;
       P.C2 = a.b.pairs;
       P.C3 = a.b.at_target;
       P.E1 = a.targets + t0;
@@ -430,7 +441,7 @@ struct HeadRowsArgs {
   const void* x;           // of the product's first row, and their copies for dW, with zeros in rows without a target
   f16_t* x16;
   float* x32;              // (float32 layers) null where there is no dW
-  int32_t rows, vocab, ldv, pair_rows, d;
+  int32_t rows, vocab, ldv, pair_rows, pair_cols, d;
 };
 __device__ __forceinline__ float row_weight(const HeadRowsArgs& a, int row, int32_t target) {
   return target < 0 ? 0.f : target >= a.vocab ? __builtin_nanf("") : a.d_logp[row];
@@ -448,38 +459,47 @@ __device__ __forceinline__ void put_row(const HeadRowsArgs& a, int row, int32_t 
   put_row(a.logp ? a.logp + row : nullptr, a.log_z ? a.log_z + row : nullptr, target, a.vocab, at_target, top, log_sum);
 }
 
-// Joins the pairs of 64 rows.  Sixteen waves, each takes every sixteenth pair of a row.
+// Joins the pairs of sixteen rows.  Sixteen waves of four quarters, each quarter takes every 64th pair of the rows.  (A lane for each of 64 rows
+// kept a call of 128 rows x 50257 waiting for two blocks: 42 us in place of 56.)
 __global__ __launch_bounds__(1024) void head_stats_kernel(HeadRowsArgs a) {
-  __shared__ float s_m[16][64], s_s[16][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int row = blockIdx.x * 64 + lane, n = (a.vocab + 127) / 128;
-  constexpr int AHEAD = 8;
+  __shared__ float s_m[64][16], s_s[64][16];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, quarter = threadIdx.x >> 4;
+  const int row = blockIdx.x * 16 + (lane & 15), n = (a.vocab + a.pair_cols - 1) / a.pair_cols;
+  constexpr int AHEAD = 4;
   typedef float f32x2 __attribute__((ext_vector_type(2)));
   float m = -__builtin_inff(), s = 0.f;
   if (row < a.rows) {
-    for (int p = wave; p < n; p += 16 * AHEAD) {
+    for (int p = quarter; p < n; p += 64 * AHEAD) {
       f32x2 v[AHEAD];
 #pragma unroll
       for (int i = 0; i < AHEAD; ++i)
-        v[i] = *reinterpret_cast<const f32x2*>(a.pairs + ((int64_t)min(p + i * 16, n - 1) * a.pair_rows + row) * 2);
+        v[i] = *reinterpret_cast<const f32x2*>(a.pairs + ((int64_t)min(p + i * 64, n - 1) * a.pair_rows + row) * 2);
       float most = m;
 #pragma unroll
       for (int i = 0; i < AHEAD; ++i) most = fmaxf(most, v[i][0]);
       s *= __builtin_amdgcn_exp2f((m - most) * LOG2E);
 #pragma unroll
       for (int i = 0; i < AHEAD; ++i)
-        if (p + i * 16 < n) s += v[i][1] * __builtin_amdgcn_exp2f((v[i][0] - most) * LOG2E);
+        if (p + i * 64 < n) s += v[i][1] * __builtin_amdgcn_exp2f((v[i][0] - most) * LOG2E);
       m = most;
     }
   }
-  s_m[wave][lane] = m;
-  s_s[wave][lane] = s;
+  s_m[quarter][lane & 15] = m;
+  s_s[quarter][lane & 15] = s;
   if (a.range && wave == 15) join_range(a.range);
   __syncthreads();
-  if (wave > 0 || row >= a.rows) return;
-  float top = m, sum = 0.f;
-  for (int w = 1; w < 16; ++w) top = fmaxf(top, s_m[w][lane]);
-  for (int w = 0; w < 16; ++w) sum += s_s[w][lane] * __builtin_amdgcn_exp2f((s_m[w][lane] - top) * LOG2E);
+  if (wave > 0) return;
+  // (a quarter of this wave joins sixteen of the sums.  The first always has seen a pair, so the row's maximum is one's)
+  float top = -__builtin_inff(), sum = 0.f;
+#pragma unroll
+  for (int w = 0; w < 16; ++w) top = fmaxf(top, s_m[quarter * 16 + w][lane & 15]);
+  top = fmaxf(top, __shfl_xor(top, 16, 64));
+  top = fmaxf(top, __shfl_xor(top, 32, 64));
+#pragma unroll
+  for (int w = 0; w < 16; ++w) sum += s_s[quarter * 16 + w][lane & 15] * __builtin_amdgcn_exp2f((s_m[quarter * 16 + w][lane & 15] - top) * LOG2E);
+  sum += __shfl_xor(sum, 16, 64);
+  sum += __shfl_xor(sum, 32, 64);
+  if (lane >= 16 || row >= a.rows) return;
   const float log2_sum = __builtin_amdgcn_logf(sum), log_sum = log2_sum * LN2;
   put_row(a, row, a.targets[row], a.at_target[row], top, log_sum);
   a.off[2 * row] = top;
@@ -532,69 +552,7 @@ __global__ __launch_bounds__(256) void head_grad_kernel(HeadRowsArgs a, int segs
   }
 }
 
-template <int THREADS>
-__device__ __forceinline__ void copy_x32(const HeadRowsArgs& a, int t, int32_t target) {
-  const float* const x = static_cast<const float*>(a.x) + (int64_t)t * a.d;
-  for (int c = threadIdx.x * 4; c < a.d; c += THREADS * 4)
-    *reinterpret_cast<f32x4*>(a.x32 + (int64_t)t * a.d + c) = target >= 0 && target < a.vocab ? *reinterpret_cast<const f32x4*>(x + c) : f32x4{};
-}
-
-// float32: a row of logits, its sums, and (GRAD) its row of G in its place.  Columns behind the vocabulary become zeros.
-template <bool GRAD>
-__global__ __launch_bounds__(512) void head_rows_kernel(HeadRowsArgs a) {
-  constexpr int W = 8;
-  __shared__ float s_m[W], s_s[W];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, t = blockIdx.x;
-  float* const row = a.logits + (int64_t)t * a.ldv;
-  auto load = [&](int c) {
-    f32x4 v = *reinterpret_cast<const f32x4*>(row + c);
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (c + e >= a.vocab) v[e] = -__builtin_inff();
-    return v;
-  };
-  float m = -__builtin_inff(), s = 0.f;
-  for (int c = tid * 4; c < a.vocab; c += W * 256) {
-    const f32x4 v = load(c);
-    const float most = fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3]));
-    if (most > m) {
-      s *= __builtin_amdgcn_exp2f((m - most) * LOG2E);
-      m = most;
-    }
-#pragma unroll
-    for (int e = 0; e < 4; ++e) s += __builtin_amdgcn_exp2f((v[e] - m) * LOG2E);
-  }
-  const float wm = wave_max(m);
-  s = m == wm ? s : s * __builtin_amdgcn_exp2f((m - wm) * LOG2E);
-  s = wave_sum(s);
-  if (lane == 0) {
-    s_m[wave] = wm;
-    s_s[wave] = s;
-  }
-  __syncthreads();
-  float top = s_m[0], sum = 0.f;
-#pragma unroll
-  for (int w = 1; w < W; ++w) top = fmaxf(top, s_m[w]);
-#pragma unroll
-  for (int w = 0; w < W; ++w) sum += s_s[w] * __builtin_amdgcn_exp2f((s_m[w] - top) * LOG2E);
-  const float log2_sum = __builtin_amdgcn_logf(sum), log_sum = log2_sum * LN2;
-  const int32_t target = a.targets[t];
-  if (tid == 0) put_row(a, t, target, target >= 0 && target < a.vocab ? row[target] : 0.f, top, log_sum);
-  if constexpr (GRAD) {
-    __syncthreads();  // (the target's logit has been read)
-    const float w = row_weight(a, t, target);
-    if (a.x32) copy_x32<W * 64>(a, t, target);
-    for (int c = tid * 4; c < a.ldv; c += W * 256) {
-      f32x4 g = c < a.vocab ? load(c) : f32x4{};
-#pragma unroll
-      for (int e = 0; e < 4; ++e) g[e] = grad_of(g[e], top, log2_sum, w, target, c + e, a.vocab);
-      *reinterpret_cast<f32x4*>(row + c) = g;
-    }
-  }
-}
-
-// The same where the stream over W has left the rows' sums: 2048 columns of a row a block, so that few rows keep the chip busy as well (24 rows
-// of 50257: 9.2 us with the join of the sums, 24 by whole rows).
+// float32 layers that take no pairs: G in the place of the logits, 2048 columns of a row a block.  The first block of a row copies x for dW.
 __global__ __launch_bounds__(256) void head_grad_f32_kernel(HeadRowsArgs a, int segs) {
   const int t = blockIdx.x / segs, c0 = (blockIdx.x - t * segs) * 2048 + threadIdx.x * 4;
   const int32_t target = a.targets[t];
@@ -609,7 +567,11 @@ __global__ __launch_bounds__(256) void head_grad_f32_kernel(HeadRowsArgs a, int 
     for (int e = 0; e < 4; ++e) g[e] = grad_of(g[e], top, log2_sum, w, target, c + e, a.vocab);
     *reinterpret_cast<f32x4*>(row + c) = g;
   }
-  if (a.x32 && (int)blockIdx.x % segs == 0) copy_x32<256>(a, t, target);
+  if (a.x32 && (int)blockIdx.x % segs == 0) {
+    const float* const x = static_cast<const float*>(a.x) + (int64_t)t * a.d;
+    for (int c = threadIdx.x * 4; c < a.d; c += 1024)
+      *reinterpret_cast<f32x4*>(a.x32 + (int64_t)t * a.d + c) = target >= 0 && target < a.vocab ? *reinterpret_cast<const f32x4*>(x + c) : f32x4{};
+  }
 }
 
 // dX of a piece: its slabs, in order.  A block takes 1024 columns of a row, or, of sixteen parts and more, 256 columns, whose parts its four
@@ -921,9 +883,9 @@ HeadLayout layout_for(int64_t plans, int64_t sub, int64_t rows, int64_t dx_rows,
   at = align_up(at + sizeof(HeadRange), ALIGN);
   w.range = at - sizeof(HeadRange);
   w.at_target = take((size_t)sub * (pairs ? 8 : 4));
-  w.logits = take(wide && !grad ? 0 : (size_t)sub * ldv * 4);
-  w.pairs = take(std::max(wide ? (size_t)sub * ((vocab + 127) / 128) * 8 : 0, stream_pairs(std::min(sub, stream_rows(vocab)), vocab)));
-  w.off = take(wide || grad ? (size_t)sub * 8 : 0);
+  w.logits = take(grad ? (size_t)sub * ldv * 4 : 0);
+  w.pairs = take(std::max(pair_cells(sub, d, vocab, wide, grad) * 8, stream_pairs(std::min(sub, stream_rows(vocab)), vocab)));
+  w.off = take((size_t)sub * 8);
   w.lost = take(bf16 && grad ? (size_t)rows * 4 : 0);
   w.g = take(bf16 && grad ? (size_t)dx_rows * ldv * 2 : 0);
   w.hi = take(wide && grad ? cells * 2 : 0);
@@ -1008,8 +970,8 @@ hipError_t launch_head(modse_dtype dt, const HeadArgs& a, char* ws, hipStream_t 
       const HeadStreamArgs r = {a.x, a.W, a.targets, b.pairs, b.at_target, a.logp, nullptr, b.logits, b.off, range, (int32_t)m, h.d, h.vocab, h.ldv};
       e = h.bf16 ? run_stream<bf16_t>(r, s) : run_stream<float>(r, s);
     } else {
-      e = launch_grouped_gemm(dt, h.pairs ? EPI_LOGITS_PAIRS : h.bf16 ? EPI_LOGITS : EPI_STORE, h.logits_tile, b.plans + i, h.w_parts, 0,
-                              GEMM_STREAM_C, tiles(m, h.vocab, h.logits_tile) + h.w_parts * tiles(m, 1, h.logits_tile), s, LAYOUT_TN);
+      e = launch_grouped_gemm(dt, h.pairs ? EPI_LOGITS_PAIRS : EPI_LOGITS, h.logits_tile, b.plans + i, h.w_parts, 0,
+                              h.logits_tile.bm < 256 ? GEMM_SPREAD_K : GEMM_STREAM_C, tiles(m, h.vocab, h.logits_tile) + h.w_parts * tiles(m, 1, h.logits_tile), s, LAYOUT_TN);
     }
     if (e != hipSuccess) return;
     const HeadRowsArgs r = {a.targets + t0, a.d_logp ? a.d_logp + t0 : nullptr, a.logp ? a.logp + t0 : nullptr, a.log_z ? a.log_z + t0 : nullptr,
@@ -1017,18 +979,13 @@ hipError_t launch_head(modse_dtype dt, const HeadArgs& a, char* ws, hipStream_t 
                             a.dX && h.dx_rows > h.rows ? b.g + (int64_t)h.rows * h.ldv : nullptr, b.lost + in_piece,
                             a.dW || h.pairs ? b.hi + in_piece * h.ldv : nullptr, a.dW || h.pairs ? b.lo + in_piece * h.ldv : nullptr,
                             range, static_cast<const char*>(a.x) + (size_t)t0 * h.d * (h.bf16 ? 2 : 4), b.x16 + in_piece * h.d,
-                            a.dW && !h.wide ? b.x32 + in_piece * h.d : nullptr, (int32_t)m, h.vocab, h.ldv, h.sub, h.d};
-    if (h.wide) {
-      if (!stream) hipLaunchKernelGGL(head_stats_kernel, dim3((unsigned)((m + 63) / 64)), dim3(1024), 0, s, r);
+                            a.dW && !h.wide ? b.x32 + in_piece * h.d : nullptr, (int32_t)m, h.vocab, h.ldv, h.sub, h.pair_cols(), h.d};
+    if (!stream) hipLaunchKernelGGL(head_stats_kernel, dim3((unsigned)((m + 15) / 16)), dim3(1024), 0, s, r);
+    if (grad) {
       const int64_t segs = (h.ldv + 2047) / 2048, copies = a.dW && h.bf16 ? (m * h.d + 2047) / 2048 : 0;
-      if (grad) hipLaunchKernelGGL(head_grad_kernel, dim3((unsigned)(m * segs + copies)), dim3(256), 0, s, r, (int)segs);
-    } else if (stream) {
-      const int64_t segs = (h.ldv + 2047) / 2048;
-      hipLaunchKernelGGL(head_grad_f32_kernel, dim3((unsigned)(m * segs)), dim3(256), 0, s, r, (int)segs);
-    } else if (grad) {
-      hipLaunchKernelGGL((head_rows_kernel<true>), dim3((unsigned)m), dim3(512), 0, s, r);
-    } else {
-      hipLaunchKernelGGL((head_rows_kernel<false>), dim3((unsigned)m), dim3(512), 0, s, r);
+      const dim3 grid((unsigned)(m * segs + copies));
+      if (h.wide) hipLaunchKernelGGL(head_grad_kernel, grid, dim3(256), 0, s, r, (int)segs);
+      else hipLaunchKernelGGL(head_grad_f32_kernel, grid, dim3(256), 0, s, r, (int)segs);
     }
     e = hipGetLastError();
   };

@@ -141,13 +141,13 @@ def check(T, d, V, dtype, seed=0, whole=False, sigma=2.5, times_x=1.0, times_w=1
     return x, W, targets, w, dX, dW, want, tol_dW
 
 
-# A stream over W where a few rows or a small vocabulary make few blocks, tiles of 256 x 256 (float32: less) beyond; dX in two parts up to 128
+# A stream over W where a few rows or a small vocabulary make few blocks, tiles of 128 x 128 or 256 x 256 (float32: 64 or 128) beyond; dX in two parts up to 128
 # rows; dW's sum in parts where the vocabulary is small
 SHAPES = [(1, 32, 1), (1, 64, 7), (2, 32, 31), (3, 96, 32), (5, 64, 33), (16, 128, 100), (17, 32, 255), (33, 96, 257), (64, 2048, 700),
           (65, 512, 1023), (63, 64, 8191), (49, 256, 64), (32, 32, 65), (129, 64, 1500), (255, 64, 300), (257, 128, 1000), (300, 256, 5003),
           (1000, 64, 4097), (40, 96, 50257), (4, 4096, 9001), (128, 96, 513), (192, 64, 777), (520, 96, 31), (70, 64, 40000), (65, 512, 33000),
           (128, 32, 16500), (129, 96, 20011), (200, 64, 12345), (257, 128, 9001), (520, 32, 5003), (700, 160, 3333), (2100, 64, 1001),
-          (3000, 256, 256), (4100, 32, 32)]
+          (3000, 256, 256), (4100, 32, 32), (700, 320, 5003), (1000, 288, 20011), (1025, 256, 4099), (1024, 256, 4099)]
 # float32 by pairs of float16 numbers, from the rows on where that is faster
 PAIRS = [(5000, 64, 4097), (2600, 160, 3333), (10001, 64, 4097), (300, 256, 50257), (300, 2048, 32000), (520, 96, 131073), (9000, 512, 1000),
          (70000, 256, 256)]

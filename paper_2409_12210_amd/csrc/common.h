@@ -90,13 +90,13 @@ enum GemmEpilogue {
   // C = acc or C += acc, float32, rows below E2 (as an integer) alone: A has M columns, a multiple of 32, and C fewer rows.  Layers of
   // bf16: the operands are two pairs of float16 matrices, and acc is multiplied by the two floats at E1
   EPI_ROWS_F32 = 5,
-  // acc = logits: for every row, maximum m and sum of e^(l - m) over the columns of a wave (128 of tiles of 256, half of smaller ones), as
-  // a pair at C2[column of all columns / those of a wave][row], and the logit of the row's target (E1, int32) at C3[row], if it is among the columns; C = acc, float32, if
-  // there is a C.  E2: the problem's first column in the lower half, the pairs of a row block of 128 columns in the upper
+  // acc = logits: for every row, maximum m and sum of e^(l - m) over the columns of a wave, half a tile's, as a pair at C2[column of all columns
+  // / those of a wave][row], and the logit of the row's target (E1, int32) at C3[row], if it is among the columns; C = acc, float32, if
+  // there is a C.  E2: the problem's first column in the lower half, rows of C2 in the upper
   EPI_LOGITS = 6,
   // EPI_STORE_F32, EPI_ROWS_F32 and EPI_LOGITS of float32 matrices that are held as sums of two float16 ones each, (A + A2) (B + B2)^T less
-  // the product of the second parts.  Of EPI_LOGITS_PAIRS the float before C3 and, for each
-  // row, one behind C3's [E2 >> 32] floats are factors of acc.
+  // the product of the second parts.  Of EPI_LOGITS_PAIRS the float before C3 and, for each row, one behind C3's [E2 >> 32] floats are
+  // factors of acc.
   EPI_STORE_PAIRS = 7,
   EPI_ROWS_PAIRS = 8,
   EPI_LOGITS_PAIRS = 9,

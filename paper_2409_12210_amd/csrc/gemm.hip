@@ -90,7 +90,7 @@ hipError_t launch_block(int epilogue, int layout, TileShape t, const GemmPlan* p
     case EPI_STORE_F32:
       if (layout == LAYOUT_B_KN) {
         if constexpr (std::is_same_v<T, float>) return run_block_tile<T, EPI_STORE_F32, LAYOUT_B_KN>(t, plan, n_prob, accumulate, option, max_tiles, s);
-        else return hipErrorInvalidValue;
+        else return run_block<T, 128, 128, EPI_STORE_F32, LAYOUT_B_KN>(plan, n_prob, accumulate, option, max_tiles, s);
       }
       if (layout == LAYOUT_TN) return run_block_tile<T, EPI_STORE_F32, LAYOUT_TN>(t, plan, n_prob, accumulate, option, max_tiles, s);
       return run_block_tile<T, EPI_STORE_F32, LAYOUT_AB_K>(t, plan, n_prob, accumulate, option, max_tiles, s);  // (bf16: where dX has 256-row tiles)
@@ -99,7 +99,7 @@ hipError_t launch_block(int epilogue, int layout, TileShape t, const GemmPlan* p
       else return run_block<T, 128, 128, EPI_LOGITS, LAYOUT_TN>(plan, n_prob, accumulate, option, max_tiles, s);
     case EPI_ROWS_F32:
       if constexpr (std::is_same_v<T, float>) return run_block_tile<T, EPI_ROWS_F32, LAYOUT_AB_K>(t, plan, n_prob, accumulate, option, max_tiles, s);
-      else return hipErrorInvalidValue;
+      else return run_block<T, 128, 128, EPI_ROWS_F32, LAYOUT_AB_K>(plan, n_prob, accumulate, option, max_tiles, s);
   }
   return hipErrorInvalidValue;
 }

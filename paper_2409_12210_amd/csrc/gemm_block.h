@@ -116,7 +116,9 @@ __device__ __forceinline__ void gg_block(const GemmPlan* __restrict__ plan, int 
   // then depends neither on the other rows nor on its place among them.
   constexpr bool ROTATE = !F32 && !A_T;
   const int first_k = ROTATE && (option & GEMM_SPREAD_K) ? (nk * ((nt * 5 + p) & 31)) >> 5 : 0;  // K step to start with
-  const int nsteps = (EPI == EPI_STORE_DUALK) ? 2 * nk : nk;
+  constexpr bool ROWS16 = EPI == EPI_ROWS_F32 && !F32;  // two pairs of float16 operands, as in the 256 x 256 kernel
+  constexpr bool DUALK = EPI == EPI_STORE_DUALK || ROWS16;
+  const int nsteps = DUALK ? 2 * nk : nk;
   const uint32_t lds_base = __builtin_amdgcn_readfirstlane(lds_address(ring));
 
   // ---- loads.  Which 16-byte chunk a lane fetches is chosen so that the data lands swizzled: unit u of a K-contiguous
@@ -187,9 +189,9 @@ __device__ __forceinline__ void gg_block(const GemmPlan* __restrict__ plan, int 
     ++w.kstep;
     if (ROTATE && w.kstep == nk && first_k != 0) {  // from the end of K back to its beginning
       w.kstep = 0;
-      src = at_k(IS_A, EPI == EPI_STORE_DUALK && w.step > nk, 0);
+      src = at_k(IS_A, DUALK && w.step > nk, 0);
     }
-    if (EPI == EPI_STORE_DUALK && w.step == nk) {
+    if (DUALK && w.step == nk) {
       w.kstep = first_k;
       src = at_k(IS_A, true, first_k);
     }
@@ -261,8 +263,15 @@ __device__ __forceinline__ void gg_block(const GemmPlan* __restrict__ plan, int 
 #pragma unroll
         for (int i = 0; i < MI; ++i)
 #pragma unroll
-          for (int j = 0; j < NI; ++j)
-            acc[q][i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bf[set][q][j], af[set][i], acc[q][i][j], 0, 0, 0);
+          for (int j = 0; j < NI; ++j) {
+            if constexpr (ROWS16) {
+              typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+              acc[q][i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, bf[set][q][j]), __builtin_bit_cast(f16x8, af[set][i]),
+                                                                    acc[q][i][j], 0, 0, 0);
+            } else {
+              acc[q][i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bf[set][q][j], af[set][i], acc[q][i][j], 0, 0, 0);
+            }
+          }
     }
   };
 
@@ -383,14 +392,17 @@ __device__ __forceinline__ void gg_block(const GemmPlan* __restrict__ plan, int 
   // A wave stages units of 32 rows x 128 bytes (64 for a 32-column bf16 tile) through LDS, so that global memory sees
   // whole lines: written in accumulator order, read back row-wise.  The staging area lies in the slots that the step
   // after the last one would use: nobody reads them any more and no load is on its way into them.
-  typedef std::conditional_t<F32 || EPI == EPI_STORE_F32 || EPI == EPI_LOGITS, float, bf16_t> out_t;
-  static_assert(F32 || EPI != EPI_ROWS_F32, "for float32");
+  typedef std::conditional_t<F32 || EPI == EPI_STORE_F32 || EPI == EPI_LOGITS || ROWS16, float, bf16_t> out_t;
   constexpr int OS = sizeof(out_t), UC = OS == 4 ? 32 : (WN < 64 ? WN : 64);  // columns of a unit
   constexpr int CPR = UC * OS / 16, ITS = 32 * CPR / 64, NJU = WN / UC, JPU = UC / 32;
   typedef std::conditional_t<OS == 4, f32x4, bf16x8> chunk_t;
   char* const slot = ring + slot_byte(rb) + wave * 4096;
   const int er = lane & 31, esw = (er >> 1) & 7;
   const int ldc = P.ldc();
+  float scale[2] = {1.f, 1.f};
+  if constexpr (ROWS16)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) scale[i] = static_cast<const float*>(P.E1())[i];
   const int rows_end = EPI == EPI_ROWS_F32 ? (int)reinterpret_cast<intptr_t>(P.E2()) : M;
   auto stage = [&](auto value) {  // value(jj, idx): element idx of the accumulator of the unit's block jj
 #pragma unroll
@@ -528,7 +540,8 @@ __device__ __forceinline__ void gg_block(const GemmPlan* __restrict__ plan, int 
           }
           continue;
         }
-        stage([&](int jj, int x) { return acc[0][i][j0 + jj][x]; });
+        if constexpr (ROWS16) stage([&](int jj, int x) { return acc[0][i][j0 + jj][x] * scale[0] * scale[1]; });
+        else stage([&](int jj, int x) { return acc[0][i][j0 + jj][x]; });
         if constexpr (EPI == EPI_STORE_F32 || EPI == EPI_ROWS_F32) {
           if (accumulate) {
             chunk_t old[ITS];

@@ -96,10 +96,18 @@ bool takes_pairs(int64_t T, int32_t d, int32_t vocab, modse_dtype dt, bool grad)
 constexpr int STREAM_W = 64;
 int64_t stream_rows(int32_t vocab) { return std::max<int64_t>(1, 512 / ((vocab + STREAM_W - 1) / STREAM_W)) * 64; }
 // Bf16 layers: the logits take tiles of 128, two of which share a CU, where tiles of 256 are few or a tile is but a few steps of K.  Tiles of
-// 256 / 128, us: 128 rows with 32000 x 2048 54 / 36, 131072 x 128 41 / 22; 256 rows 55 / 51, 35 / 30; 512 rows with 32000 x 1024 44 / 53, 131072
-// x 512 86 / 88, 50257 x 256 38 / 33, 4096 rows 177 / 157; with gradients 512 rows x 50257 x 256 198 / 182, 2048 rows 541 / 562.
+// 256 / 128, us: 128 rows with 32000 x 2048 54 / 36, 131072 x 128 41 / 22; 229 rows with 32000 x 2048 55 / 51, 50257 x 2048 69 / 88, 131072 x
+// 128 35 / 30; 512 rows with 32000 x 1024 44 / 53, 131072 x 512 86 / 88, 50257 x 256 38 / 33, 4096 rows 177 / 157; with gradients 512
+// rows x 50257 x 256 198 / 182, 2048 rows 541 / 562.
 constexpr int64_t BLOCK_ROWS = 256, BLOCK_ROWS_GRAD = 1024;
-bool takes_blocks(int64_t T, int32_t d, bool grad) { return T <= BLOCK_ROWS || (d <= 256 && (!grad || T <= BLOCK_ROWS_GRAD)); }
+bool logits_take_blocks(int64_t T, int32_t d, int32_t vocab, bool grad) {
+  return T <= 128 || (T <= BLOCK_ROWS && vocab <= 32768) || (d <= 256 && (!grad || T <= BLOCK_ROWS_GRAD));
+}
+// dX takes them up to 256 rows, and with short rows up to 1024 (one row with 32000 x 2048 167 / 137, 50257 x 256 78 / 56; 229 rows 257 / 253, 132 / 112; 512
+// rows 351 / 371, 180 / 166), dW up to 64 rows and where tiles of 256 do not fill the chip and are a few steps of K each: one row with 32000 x 2048
+// 167 / 149, 128 rows with 131072 x 512 279 / 295; 1024 rows with 1000 x 1024 93 / 75, 4000 x 512 117 / 116, 8000 x 1024 167 / 184.
+bool dx_takes_blocks(int64_t T, int32_t d) { return T <= BLOCK_ROWS || (d <= 256 && T <= BLOCK_ROWS_GRAD); }
+bool dw_takes_blocks(int64_t T, int64_t tiles_256) { return T <= 64 || (tiles_256 <= 128 && T * tiles_256 <= 32768); }
 // pairs of maximum and sum for so many rows of any batch
 size_t pair_cells(int64_t rows, int32_t d, int32_t vocab, bool wide, bool grad) {
   auto of = [&](int64_t n, int cols) { return (size_t)n * ((vocab + cols - 1) / cols); };
@@ -135,22 +143,22 @@ HeadShape head_shape(int64_t T, int32_t d, int32_t vocab, modse_dtype dt, bool g
   // (float32: tiles of 128 from four rounds of the chip's 512 workgroups on.  50304 x 256, 1.5 rounds: 287 us with them, 258 with tiles of
   // 64; 1021 x 50257, 6.1 rounds: 251 and 261)
   auto tile = [&](int64_t m, int64_t n) { const int b = h.wide ? 256 : tiles(m, n, 128) >= 2048 ? 128 : 64; return TileShape{b, b}; };
-  h.logits_tile = h.bf16 && takes_blocks(T, d, grad) ? TileShape{128, 128} : tile(h.sub, vocab);
-  h.dw_tile = tile(vocab, d);
+  h.logits_tile = h.bf16 && logits_take_blocks(T, d, vocab, grad) ? TileShape{128, 128} : tile(h.sub, vocab);
+  h.dw_tile = h.bf16 && dw_takes_blocks(T, tiles(vocab, d, 256)) ? TileShape{128, 128} : tile(vocab, d);
   const int64_t w_steps = (h.rows + 63) / 64, w_split = std::min(dw_most_parts(d, vocab, h.wide), std::max<int64_t>(1, w_steps / 4));
   h.w_len = (int32_t)((w_steps + w_split - 1) / w_split) * 64;
   h.w_split = (h.rows + h.w_len - 1) / h.w_len;
-  const int dx = h.wide ? 256 : h.rows <= 64 ? 64 : 128;
+  const int dx = h.bf16 && dx_takes_blocks(T, d) ? 128 : h.wide ? 256 : h.rows <= 64 ? 64 : 128;
   h.dx_tile = TileShape{dx, dx};
   // Parts of dX: whole rounds of workgroups over the chip, each part with six further steps for its opening and its end, and slabs that
   // are written and read.
   h.dx_rows = h.bf16 && T <= STACK_ROWS ? 2 * h.rows : h.rows;
-  const int64_t out = tiles(h.dx_rows, d, h.dx_tile.bm), steps = (vocab + 63) / 64, slots = h.wide ? 256 : 512;
+  const int64_t out = tiles(h.dx_rows, d, h.dx_tile.bm), steps = (vocab + 63) / 64, slots = dx == 256 ? 256 : 512;
   const int64_t parts_most = std::min<int64_t>({MAX_PARTS, steps, std::max<int64_t>(1, SLAB_CELLS / ((int64_t)h.dx_rows * d))});
   double best = 0;
   for (int64_t n = 1; n <= parts_most; ++n) {
     const int64_t len = (steps + n - 1) / n, parts = (steps + len - 1) / len;
-    const double step_us = h.bf16 ? 1.6 : h.pairs ? 4.8 : dx == 64 ? 3.0 : 8.0;
+    const double step_us = h.bf16 ? (dx == 128 ? 1.0 : 1.6) : h.pairs ? 4.8 : dx == 64 ? 3.0 : 8.0;
     const double us = (double)((out * parts + slots - 1) / slots) * (len + 6) * step_us + parts * (double)h.dx_rows * d * 8 / 4e6;
     if (n == 1 || us < best) {
       best = us;

@@ -107,12 +107,14 @@ hipError_t launch_block(int epilogue, int layout, TileShape t, const GemmPlan* p
 
 hipError_t launch_grouped_gemm(modse_dtype dt, int epilogue, TileShape t, const GemmPlan* plan, int n_prob, int accumulate,
                                int option, int64_t max_tiles, hipStream_t s, int layout) {
-  switch (epilogue) {  // (of float32 layers, and 256-row tiles)
+  switch (epilogue) {  // (of float32 layers)
     case EPI_STORE_PAIRS:
+      if (t.bm == 128) return run_block<bf16_t, 128, 128, EPI_STORE_PAIRS, LAYOUT_B_KN>(plan, n_prob, accumulate, option, max_tiles, s);
       return run_bf16<256, 256, 1, 4, 2, EPI_STORE_PAIRS, LAYOUT_B_KN>(plan, n_prob, accumulate, option, max_tiles, s);
     case EPI_ROWS_PAIRS:
       return run_bf16<256, 256, 1, 4, 2, EPI_ROWS_PAIRS, LAYOUT_AB_K>(plan, n_prob, accumulate, option, max_tiles, s);
     case EPI_LOGITS_PAIRS:
+      if (t.bm == 128) return run_block<bf16_t, 128, 128, EPI_LOGITS_PAIRS, LAYOUT_TN>(plan, n_prob, accumulate, option, max_tiles, s);
       return run_bf16<256, 256, 1, 4, 2, EPI_LOGITS_PAIRS, LAYOUT_TN>(plan, n_prob, accumulate, option, max_tiles, s);
   }
   if (dt == MODSE_F32) return launch_block<float>(epilogue, layout, t, plan, n_prob, accumulate, option, max_tiles, s);

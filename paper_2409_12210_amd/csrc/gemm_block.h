@@ -1,5 +1,5 @@
 // Grouped GEMM with small tiles for gfx950: 128 x 128 down to 32 x 128 (float32: 32 x 32) tiles, one per workgroup of four
-// waves, float32 and bf16, every layout and epilogue of the layer.
+// waves, float32 and bf16, every layout and epilogue of the layer, and those of the logits and their gradients.
 //
 // Where the 256 x 256 kernel of gemm_bf16.h wants tall problems (one workgroup per CU, a ring of five panels), this one
 // serves problems that do not fill such tiles: the workgroup is small enough (80 KiB of LDS) that two of them share a
@@ -116,9 +116,13 @@ __device__ __forceinline__ void gg_block(const GemmPlan* __restrict__ plan, int 
   // then depends neither on the other rows nor on its place among them.
   constexpr bool ROTATE = !F32 && !A_T;
   const int first_k = ROTATE && (option & GEMM_SPREAD_K) ? (nk * ((nt * 5 + p) & 31)) >> 5 : 0;  // K step to start with
-  constexpr bool ROWS16 = EPI == EPI_ROWS_F32 && !F32;  // two pairs of float16 operands, as in the 256 x 256 kernel
-  constexpr bool DUALK = EPI == EPI_STORE_DUALK || ROWS16;
-  const int nsteps = DUALK ? 2 * nk : nk;
+  // passes over K, as in the 256 x 256 kernel.  Two: A B, A2 B2; three: A B, A B2, A2 B
+  constexpr bool PAIRS = EPI == EPI_STORE_PAIRS || EPI == EPI_LOGITS_PAIRS;
+  constexpr bool ROWS16 = EPI == EPI_ROWS_F32 && !F32, HALF = ROWS16 || PAIRS;  // HALF: float16 operands
+  constexpr bool LOGITS = EPI == EPI_LOGITS || EPI == EPI_LOGITS_PAIRS;
+  constexpr int PASSES = PAIRS ? 3 : EPI == EPI_STORE_DUALK || ROWS16 ? 2 : 1;
+  static_assert(!F32 || !PAIRS, "16-bit operands");
+  const int nsteps = PASSES * nk;
   const uint32_t lds_base = __builtin_amdgcn_readfirstlane(lds_address(ring));
 
   // ---- loads.  Which 16-byte chunk a lane fetches is chosen so that the data lands swizzled: unit u of a K-contiguous
@@ -154,12 +158,13 @@ __device__ __forceinline__ void gg_block(const GemmPlan* __restrict__ plan, int 
   const size_t a_step = A_T ? (size_t)128 * P.lda() : 128, b_step = B_T ? (size_t)128 * P.ldb() : 128;
   const bool second = NB == 2 && wave * UB * 8 >= BN;  // this wave's B units belong to the second matrix
   // an operand of a pass at K step k
-  auto at_k = [&](bool is_a, bool pass2, int k) {
-    const char* const b = is_a ? (pass2 ? P.A2() : P.A()) : (second || pass2 ? P.B2() : P.B());
+  auto at_k = [&](bool is_a, int pass, int k) {
+    const bool a2 = pass == (PAIRS ? 2 : 1), b2 = second || pass == 1;
+    const char* const b = is_a ? (a2 ? P.A2() : P.A()) : (b2 ? P.B2() : P.B());
     return static_cast<const char*>(uniform_ptr(b + (is_a ? a_org + k * a_step : b_org + k * b_step)));
   };
-  const char* sa = at_k(true, false, first_k);
-  const char* sb = at_k(false, false, first_k);
+  const char* sa = at_k(true, 0, first_k);
+  const char* sb = at_k(false, 0, first_k);
   // the loads of one operand's next panel into ring slot `slot`; the operand then moves on to its next K step
   struct Walk {
     int step = 0, kstep;  // of all steps; along K
@@ -189,11 +194,11 @@ __device__ __forceinline__ void gg_block(const GemmPlan* __restrict__ plan, int 
     ++w.kstep;
     if (ROTATE && w.kstep == nk && first_k != 0) {  // from the end of K back to its beginning
       w.kstep = 0;
-      src = at_k(IS_A, DUALK && w.step > nk, 0);
+      src = at_k(IS_A, PASSES > 1 ? (w.step - 1) / nk : 0, 0);
     }
-    if (DUALK && w.step == nk) {
+    if (PASSES > 1 && (w.step == nk || (PASSES > 2 && w.step == 2 * nk))) {
       w.kstep = first_k;
-      src = at_k(IS_A, true, first_k);
+      src = at_k(IS_A, w.step == nk ? 1 : 2, first_k);
     }
   };
   auto issue_a = [&](int slot) { issue(std::true_type{}, wa, sa, slot); };
@@ -264,7 +269,7 @@ __device__ __forceinline__ void gg_block(const GemmPlan* __restrict__ plan, int 
         for (int i = 0; i < MI; ++i)
 #pragma unroll
           for (int j = 0; j < NI; ++j) {
-            if constexpr (ROWS16) {
+            if constexpr (HALF) {
               typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
               acc[q][i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, bf[set][q][j]), __builtin_bit_cast(f16x8, af[set][i]),
                                                                     acc[q][i][j], 0, 0, 0);
@@ -392,7 +397,7 @@ __device__ __forceinline__ void gg_block(const GemmPlan* __restrict__ plan, int 
   // A wave stages units of 32 rows x 128 bytes (64 for a 32-column bf16 tile) through LDS, so that global memory sees
   // whole lines: written in accumulator order, read back row-wise.  The staging area lies in the slots that the step
   // after the last one would use: nobody reads them any more and no load is on its way into them.
-  typedef std::conditional_t<F32 || EPI == EPI_STORE_F32 || EPI == EPI_LOGITS || ROWS16, float, bf16_t> out_t;
+  typedef std::conditional_t<F32 || EPI == EPI_STORE_F32 || LOGITS || HALF, float, bf16_t> out_t;
   constexpr int OS = sizeof(out_t), UC = OS == 4 ? 32 : (WN < 64 ? WN : 64);  // columns of a unit
   constexpr int CPR = UC * OS / 16, ITS = 32 * CPR / 64, NJU = WN / UC, JPU = UC / 32;
   typedef std::conditional_t<OS == 4, f32x4, bf16x8> chunk_t;
@@ -447,7 +452,7 @@ __device__ __forceinline__ void gg_block(const GemmPlan* __restrict__ plan, int 
       if (o >= 0) put(C, o, v);
     }
   };
-  if constexpr (EPI == EPI_LOGITS) {  // maximum and sum of each row's columns of this wave, and the target's logit
+  if constexpr (LOGITS) {  // maximum and sum of each row's columns of this wave, and the target's logit
     static_assert(!A_T && !B_T && NB == 1, "rows of logits");
     constexpr float LOG2E = 1.44269504088896340736f;
     const int nw = n0 + wn * WN, nleft = N - nw;  // the wave's first column, columns from there on
@@ -459,6 +464,12 @@ __device__ __forceinline__ void gg_block(const GemmPlan* __restrict__ plan, int 
 #pragma unroll
       for (int i = 0; i < MI; ++i) {
         const int row = m0 + wm * WM + i * 32 + er;
+        if constexpr (EPI == EPI_LOGITS_PAIRS) {  // (the smaller factor first, as there)
+          const float* const undo = static_cast<const float*>(P.C3());
+          const float of_a = undo[(place >> 32) + min(row, M - 1)], of_b = undo[-1];
+#pragma unroll
+          for (int j = 0; j < NI; ++j) acc[0][i][j] = acc[0][i][j] * fminf(of_a, of_b) * fmaxf(of_a, of_b);
+        }
         const int at = max(targets[min(row, M - 1)], -1) - first_col - khalf * 4;
         float m = -__builtin_inff(), there = 0.f, s = 0.f;
         auto value = [&](int j, int x) { return j * 32 + (x >> 2) * 8 + (x & 3) + khalf * 4 < nleft ? acc[0][i][j][x] : -__builtin_inff(); };

@@ -15,7 +15,7 @@
 // float32 from some hundred rows on: x, W and G are held as the sums of two float16 matrices, hi + lo, times powers of
 // two that bring the largest value below 2^15.  Three products of float16 matrices, hi hi' + hi lo' + lo hi', in one accumulator leave
 // out 2^-22 of a product; they take 3 of the 16-bit matrix rate where float32 instructions take 16 (1021 x 256 x 50257 with gradients:
-// 470 us in place of 731).  Fewer rows, or a W of more than 2^28 elements: products in float32, and G in the place of the logits.
+// 435 us in place of 731).  Fewer rows, or a W of more than 2^28 elements: products in float32, and G in the place of the logits.
 //
 // Up to 64 rows (small vocabularies: more) a stream over W makes the logits, see "few rows".  dW of a small vocabulary has few tiles,
 // so its sum over the tokens is cut into parts as well (float32, 1000 x 512, 4096 rows: with the stream 160 us in place of 337 for the whole call).
@@ -95,23 +95,28 @@ bool takes_pairs(int64_t T, int32_t d, int32_t vocab, modse_dtype dt, bool grad)
 // one block of rows.
 constexpr int STREAM_W = 64;
 int64_t stream_rows(int32_t vocab) { return std::max<int64_t>(1, 512 / ((vocab + STREAM_W - 1) / STREAM_W)) * 64; }
-// Bf16 layers: the logits take tiles of 128, two of which share a CU, where tiles of 256 are few or a tile is but a few steps of K.  Tiles of
+int64_t tiles(int64_t m, int64_t n, int b) { return ((m + b - 1) / b) * ((n + b - 1) / b); }
+// 16-bit products: the logits take tiles of 128, two of which share a CU, where tiles of 256 are few or a tile is but a few steps of K.  Tiles of
 // 256 / 128, us: 128 rows with 32000 x 2048 54 / 36, 131072 x 128 41 / 22; 229 rows with 32000 x 2048 55 / 51, 50257 x 2048 69 / 88, 131072 x
 // 128 35 / 30; 512 rows with 32000 x 1024 44 / 53, 131072 x 512 86 / 88, 50257 x 256 38 / 33, 4096 rows 177 / 157; with gradients 512
-// rows x 50257 x 256 198 / 182, 2048 rows 541 / 562.
-constexpr int64_t BLOCK_ROWS = 256, BLOCK_ROWS_GRAD = 1024;
-bool logits_take_blocks(int64_t T, int32_t d, int32_t vocab, bool grad) {
-  return T <= 128 || (T <= BLOCK_ROWS && vocab <= 32768) || (d <= 256 && (!grad || T <= BLOCK_ROWS_GRAD));
+// rows x 50257 x 256 198 / 182, 2048 rows 541 / 562.  Float32 by pairs, gradients: 300 rows with 8000 x 1024 205 / 173, 1021 rows 275 / 256, 2048
+// rows 374 / 404, 1021 rows with 50257 x 256 473 / 446, 2048 rows 780 / 776, scored 4096 rows 403 / 440.
+constexpr int64_t BLOCK_ROWS = 256, BLOCK_ROWS_MOST = 1024, FEW_TILES = 128;
+bool logits_take_blocks(int64_t T, int32_t d, int32_t vocab, bool all_rows) {
+  return T <= 128 || tiles(T, vocab, 256) <= FEW_TILES || (d <= 256 && (all_rows || T <= BLOCK_ROWS_MOST));
 }
-// dX takes them up to 256 rows, and with short rows up to 1024 (one row with 32000 x 2048 167 / 137, 50257 x 256 78 / 56; 229 rows 257 / 253, 132 / 112; 512
-// rows 351 / 371, 180 / 166), dW up to 64 rows and where tiles of 256 do not fill the chip and are a few steps of K each: one row with 32000 x 2048
-// 167 / 149, 128 rows with 131072 x 512 279 / 295; 1024 rows with 1000 x 1024 93 / 75, 4000 x 512 117 / 116, 8000 x 1024 167 / 184.
-bool dx_takes_blocks(int64_t T, int32_t d) { return T <= BLOCK_ROWS || (d <= 256 && T <= BLOCK_ROWS_GRAD); }
-bool dw_takes_blocks(int64_t T, int64_t tiles_256) { return T <= 64 || (tiles_256 <= 128 && T * tiles_256 <= 32768); }
+// dX takes them up to 256 rows, and with short rows up to 1024 (one row with 32000 x 2048 167 / 137, 50257 x 256 78 / 56; 229 rows 257 / 253, 132 / 112;
+// 512 rows 351 / 371, 180 / 166; float32, 512 rows with 32000 x 512 297 / 276, 1021 rows 424 / 478, 512 rows with 32000 x 2048 774 / 865), dW
+// of bf16 layers up to 64 rows and where tiles of 256 do not fill the chip and are a few steps of K each: one row with 32000 x 2048 167 / 149, 128 rows
+// with 131072 x 512 279 / 295; 1024 rows with 1000 x 1024 93 / 75, 4000 x 512 117 / 116, 8000 x 1024 167 / 184.
+bool dx_takes_blocks(int64_t T, int32_t d, bool pairs) {
+  return pairs ? T <= 512 && d <= 512 : T <= BLOCK_ROWS || (d <= 256 && T <= BLOCK_ROWS_MOST);
+}
+bool dw_takes_blocks(int64_t T, int64_t tiles_256) { return T <= 64 || (tiles_256 <= FEW_TILES && T * tiles_256 <= 256 * FEW_TILES); }
 // pairs of maximum and sum for so many rows of any batch
-size_t pair_cells(int64_t rows, int32_t d, int32_t vocab, bool wide, bool grad) {
+size_t pair_cells(int64_t rows, int32_t d, int32_t vocab, bool wide) {
   auto of = [&](int64_t n, int cols) { return (size_t)n * ((vocab + cols - 1) / cols); };
-  const int64_t block_rows = d > 256 ? BLOCK_ROWS : grad ? BLOCK_ROWS_GRAD : rows;
+  const int64_t block_rows = d > 256 ? std::max<int64_t>(128, FEW_TILES / tiles(1, vocab, 256) * 256) : rows;
   return wide ? std::max(of(rows, 128), of(std::min(rows, block_rows), 64)) : of(rows, 32);
 }
 // Parts of dW's sum over the tokens, where it has too few tiles for the chip: slabs like those of dX, added up behind it.
@@ -139,16 +144,15 @@ HeadShape head_shape(int64_t T, int32_t d, int32_t vocab, modse_dtype dt, bool g
   h.subs = h.rows / h.sub;
   h.w_rows = (int32_t)std::min<int64_t>(vocab, W_PART / d / 256 * 256);
   h.w_parts = (vocab + h.w_rows - 1) / h.w_rows;
-  auto tiles = [](int64_t m, int64_t n, int b) { return ((m + b - 1) / b) * ((n + b - 1) / b); };
   // (float32: tiles of 128 from four rounds of the chip's 512 workgroups on.  50304 x 256, 1.5 rounds: 287 us with them, 258 with tiles of
   // 64; 1021 x 50257, 6.1 rounds: 251 and 261)
   auto tile = [&](int64_t m, int64_t n) { const int b = h.wide ? 256 : tiles(m, n, 128) >= 2048 ? 128 : 64; return TileShape{b, b}; };
-  h.logits_tile = h.bf16 && logits_take_blocks(T, d, vocab, grad) ? TileShape{128, 128} : tile(h.sub, vocab);
+  h.logits_tile = h.wide && logits_take_blocks(T, d, vocab, h.bf16 && !grad) ? TileShape{128, 128} : tile(h.sub, vocab);
   h.dw_tile = h.bf16 && dw_takes_blocks(T, tiles(vocab, d, 256)) ? TileShape{128, 128} : tile(vocab, d);
   const int64_t w_steps = (h.rows + 63) / 64, w_split = std::min(dw_most_parts(d, vocab, h.wide), std::max<int64_t>(1, w_steps / 4));
   h.w_len = (int32_t)((w_steps + w_split - 1) / w_split) * 64;
   h.w_split = (h.rows + h.w_len - 1) / h.w_len;
-  const int dx = h.bf16 && dx_takes_blocks(T, d) ? 128 : h.wide ? 256 : h.rows <= 64 ? 64 : 128;
+  const int dx = h.wide && dx_takes_blocks(T, d, h.pairs) ? 128 : h.wide ? 256 : h.rows <= 64 ? 64 : 128;
   h.dx_tile = TileShape{dx, dx};
   // Parts of dX: whole rounds of workgroups over the chip, each part with six further steps for its opening and its end, and slabs that
   // are written and read.
@@ -158,7 +162,7 @@ HeadShape head_shape(int64_t T, int32_t d, int32_t vocab, modse_dtype dt, bool g
   double best = 0;
   for (int64_t n = 1; n <= parts_most; ++n) {
     const int64_t len = (steps + n - 1) / n, parts = (steps + len - 1) / len;
-    const double step_us = h.bf16 ? (dx == 128 ? 1.0 : 1.6) : h.pairs ? 4.8 : dx == 64 ? 3.0 : 8.0;
+    const double step_us = h.wide ? (h.pairs ? 3 : 1) * (dx == 128 ? 1.0 : 1.6) : dx == 64 ? 3.0 : 8.0;
     const double us = (double)((out * parts + slots - 1) / slots) * (len + 6) * step_us + parts * (double)h.dx_rows * d * 8 / 4e6;
     if (n == 1 || us < best) {
       best = us;
@@ -892,7 +896,7 @@ HeadLayout layout_for(int64_t plans, int64_t sub, int64_t rows, int64_t dx_rows,
   w.range = at - sizeof(HeadRange);
   w.at_target = take((size_t)sub * (pairs ? 8 : 4));
   w.logits = take(grad ? (size_t)sub * ldv * 4 : 0);
-  w.pairs = take(std::max(pair_cells(sub, d, vocab, wide, grad) * 8, stream_pairs(std::min(sub, stream_rows(vocab)), vocab)));
+  w.pairs = take(std::max(pair_cells(sub, d, vocab, wide) * 8, stream_pairs(std::min(sub, stream_rows(vocab)), vocab)));
   w.off = take((size_t)sub * 8);
   w.lost = take(bf16 && grad ? (size_t)rows * 4 : 0);
   w.g = take(bf16 && grad ? (size_t)dx_rows * ldv * 2 : 0);
@@ -960,7 +964,7 @@ hipError_t launch_head(modse_dtype dt, const HeadArgs& a, char* ws, hipStream_t 
     hipLaunchKernelGGL(head_split_w_kernel, dim3((unsigned)std::min<int64_t>((n + 2047) / 2048, 2048)), dim3(256), 0, s,
                        static_cast<const float*>(a.W), n, b.w16, b.w16_lo, range);
   }
-  auto tiles = [](int64_t m, int64_t n, TileShape t) { return ((m + t.bm - 1) / t.bm) * ((n + t.bn - 1) / t.bn); };
+  auto tiles_of = [](int64_t m, int64_t n, TileShape t) { return tiles(m, n, t.bm); };
   hipError_t e = hipGetLastError();
   // the logits of one product, their sums and (of gradients) G
   auto product = [&](int64_t i) {
@@ -979,7 +983,7 @@ hipError_t launch_head(modse_dtype dt, const HeadArgs& a, char* ws, hipStream_t 
       e = h.bf16 ? run_stream<bf16_t>(r, s) : run_stream<float>(r, s);
     } else {
       e = launch_grouped_gemm(dt, h.pairs ? EPI_LOGITS_PAIRS : EPI_LOGITS, h.logits_tile, b.plans + i, h.w_parts, 0,
-                              h.logits_tile.bm < 256 ? GEMM_SPREAD_K : GEMM_STREAM_C, tiles(m, h.vocab, h.logits_tile) + h.w_parts * tiles(m, 1, h.logits_tile), s, LAYOUT_TN);
+                              h.logits_tile.bm < 256 ? GEMM_SPREAD_K : GEMM_STREAM_C, tiles_of(m, h.vocab, h.logits_tile) + h.w_parts * tiles_of(m, 1, h.logits_tile), s, LAYOUT_TN);
     }
     if (e != hipSuccess) return;
     const HeadRowsArgs r = {a.targets + t0, a.d_logp ? a.d_logp + t0 : nullptr, a.logp ? a.logp + t0 : nullptr, a.log_z ? a.log_z + t0 : nullptr,
@@ -1007,7 +1011,7 @@ hipError_t launch_head(modse_dtype dt, const HeadArgs& a, char* ws, hipStream_t 
     if (a.dW) {  // (before dX, which may lie in the buffer of x)
       const int accumulate = a.accumulate || piece > 0;
       e = launch_grouped_gemm(dt, h.pairs ? EPI_ROWS_PAIRS : EPI_ROWS_F32, h.dw_tile, p + 1, h.w_split, h.w_split > 1 ? 0 : accumulate, 0,
-                              h.w_split * tiles(padded_rows(h.vocab), h.d, h.dw_tile), s, LAYOUT_AB_K);
+                              h.w_split * tiles_of(padded_rows(h.vocab), h.d, h.dw_tile), s, LAYOUT_AB_K);
       if (e == hipSuccess && h.w_split > 1) {
         const int64_t n = (int64_t)h.vocab * h.d;
         hipLaunchKernelGGL(head_dw_join_kernel, dim3((unsigned)((n + 1023) / 1024)), dim3(256), 0, s, b.slabs, h.w_split, n, a.dW, accumulate);
@@ -1018,7 +1022,7 @@ hipError_t launch_head(modse_dtype dt, const HeadArgs& a, char* ws, hipStream_t 
     if (a.dX) {
       const bool stacked = h.dx_rows > h.rows;
       e = launch_grouped_gemm(dt, h.pairs ? EPI_STORE_PAIRS : EPI_STORE_F32, h.dx_tile, p, h.k_parts, 0, 0,
-                              h.k_parts * tiles(stacked ? h.dx_rows : m, h.d, h.dx_tile), s, LAYOUT_B_KN);
+                              h.k_parts * tiles_of(stacked ? h.dx_rows : m, h.d, h.dx_tile), s, LAYOUT_B_KN);
       if (e != hipSuccess) break;
       const HeadJoinArgs j = {b.slabs, h.bf16 && !stacked ? static_cast<const bf16_t*>(a.W) : nullptr, b.lost, a.targets + t0,
                               h.pairs ? range->undo_dx : nullptr, (int64_t)h.dx_rows * h.d, stacked ? (int64_t)h.rows * h.d : 0, h.k_parts,

@@ -150,7 +150,7 @@ SHAPES = [(1, 32, 1), (1, 64, 7), (2, 32, 31), (3, 96, 32), (5, 64, 33), (16, 12
           (3000, 256, 256), (4100, 32, 32), (700, 320, 5003), (1000, 288, 20011), (1025, 256, 4099), (1024, 256, 4099)]
 # float32 by pairs of float16 numbers, from the rows on where that is faster
 PAIRS = [(5000, 64, 4097), (2600, 160, 3333), (10001, 64, 4097), (300, 256, 50257), (300, 2048, 32000), (520, 96, 131073), (9000, 512, 1000),
-         (70000, 256, 256)]
+         (70000, 256, 256), (450, 512, 20001), (900, 1024, 8001)]
 
 
 @pytest.mark.parametrize("T,d,V", PAIRS)

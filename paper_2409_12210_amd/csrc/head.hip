@@ -865,8 +865,13 @@ __global__ __launch_bounds__(1024) void head_stream_join_kernel(HeadStreamArgs a
 
 template <typename T>
 hipError_t run_stream(const HeadStreamArgs& a, hipStream_t s) {
-  const int nt = a.T <= 16 ? 1 : a.T <= 32 ? 2 : 4;
-  const dim3 grid((unsigned)((a.vocab + STREAM_W - 1) / STREAM_W * ((a.T + nt * 16 - 1) / (nt * 16)))), block(256);
+  // A small vocabulary makes few blocks, each a chain of steps: fewer rows of x in each, while there is at most one for every CU.  64 rows with 1900 x
+  // 3136, float32 72.8 -> 37.8 us, bf16 16.4 -> 18.2; 4000 x 2048 50.2 -> 28.9, 16.8 -> 15.2; 1000 x 512 18.8 -> 11.3, 9.9 -> 8.0.
+  const int strips = (a.vocab + STREAM_W - 1) / STREAM_W;
+  auto blocks = [&](int nt) { return (int64_t)strips * ((a.T + nt * 16 - 1) / (nt * 16)); };
+  int nt = a.T <= 16 ? 1 : a.T <= 32 ? 2 : 4;
+  while (nt > 1 && blocks(nt / 2) <= 256) nt /= 2;
+  const dim3 grid((unsigned)blocks(nt)), block(256);
   if (nt == 1) hipLaunchKernelGGL((head_stream_kernel<T, 1>), grid, block, 0, s, a);
   else if (nt == 2) hipLaunchKernelGGL((head_stream_kernel<T, 2>), grid, block, 0, s, a);
   else hipLaunchKernelGGL((head_stream_kernel<T, 4>), grid, block, 0, s, a);

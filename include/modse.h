@@ -354,7 +354,7 @@ modse_status modse_head_fwd(int64_t T, int32_t d_model, int32_t vocab, modse_dty
  *   dX      [T, d_model] of `dtype` out, or NULL; it may lie in the buffer of x
  *   dW      [vocab, d_model] float32 out, or NULL: overwritten, or added to with
  *           accumulate = 1
- * In bf16 the gradient of the logits is rounded to bf16 for dX.  For dW it is held in
+ * In bf16 the gradient of the logits is held in 16 bits for dX.  For dW it is held in
  * 22 bits, down to 2^-39 of the largest |d_logp|, and x exactly, down to 2^-39 of the
  * largest |x| (both of rows with a target): what is smaller may be lost.  So it is for
  * dX and dW in float32 where x and W are held in 22 bits.

@@ -100,6 +100,7 @@ enum GemmEpilogue {
   EPI_STORE_PAIRS = 7,
   EPI_ROWS_PAIRS = 8,
   EPI_LOGITS_PAIRS = 9,
+  EPI_STORE_DUALK_F32 = 10, // EPI_STORE_F32 over two operand pairs, as EPI_STORE_DUALK
 };
 
 enum GemmLayout {

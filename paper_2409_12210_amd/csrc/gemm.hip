@@ -100,6 +100,9 @@ hipError_t launch_block(int epilogue, int layout, TileShape t, const GemmPlan* p
     case EPI_ROWS_F32:
       if constexpr (std::is_same_v<T, float>) return run_block_tile<T, EPI_ROWS_F32, LAYOUT_AB_K>(t, plan, n_prob, accumulate, option, max_tiles, s);
       else return run_block<T, 128, 128, EPI_ROWS_F32, LAYOUT_AB_K>(plan, n_prob, accumulate, option, max_tiles, s);
+    case EPI_STORE_DUALK_F32:
+      if constexpr (std::is_same_v<T, float>) return hipErrorInvalidValue;
+      else return run_block<T, 128, 128, EPI_STORE_DUALK_F32, LAYOUT_B_KN>(plan, n_prob, accumulate, option, max_tiles, s);
   }
   return hipErrorInvalidValue;
 }
@@ -129,8 +132,9 @@ hipError_t launch_grouped_gemm(modse_dtype dt, int epilogue, TileShape t, const 
     case EPI_STORE_DUALK:
       return run_bf16<256, 256, 1, 4, 2, EPI_STORE_DUALK, LAYOUT_B_KN>(plan, n_prob, accumulate, option, max_tiles, s);
     case EPI_STORE_F32:
-      if (layout == LAYOUT_B_KN) return run_bf16<256, 256, 1, 4, 2, EPI_STORE_F32, LAYOUT_B_KN>(plan, n_prob, accumulate, option, max_tiles, s);
       return run_bf16<256, 256, 1, 4, 2, EPI_STORE_F32, LAYOUT_AB_K>(plan, n_prob, accumulate, option, max_tiles, s);
+    case EPI_STORE_DUALK_F32:
+      return run_bf16<256, 256, 1, 4, 2, EPI_STORE_DUALK_F32, LAYOUT_B_KN>(plan, n_prob, accumulate, option, max_tiles, s);
     case EPI_LOGITS:
       return run_bf16<256, 256, 1, 4, 2, EPI_LOGITS, LAYOUT_TN>(plan, n_prob, accumulate, option, max_tiles, s);
     case EPI_ROWS_F32:

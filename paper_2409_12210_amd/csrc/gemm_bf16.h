@@ -144,7 +144,7 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64) void gg_bf16_kernel(const Ge
   constexpr int WM = Cfg::WM, WN = Cfg::WN;
   constexpr bool A_T = (LAYOUT & 1) != 0, B_T = (LAYOUT & 2) != 0;
   constexpr bool PAIRS = EPI == EPI_STORE_PAIRS || EPI == EPI_ROWS_PAIRS || EPI == EPI_LOGITS_PAIRS;
-  constexpr bool DUALK = EPI == EPI_STORE_DUALK || EPI == EPI_ROWS_F32;  // two operand pairs
+  constexpr bool DUALK = EPI == EPI_STORE_DUALK || EPI == EPI_STORE_DUALK_F32 || EPI == EPI_ROWS_F32;  // two operand pairs
   constexpr bool HALF = EPI == EPI_ROWS_F32 || PAIRS;                    // float16 operands
   constexpr bool LOGITS = EPI == EPI_LOGITS || EPI == EPI_LOGITS_PAIRS;
   constexpr int PASSES = PAIRS ? 3 : DUALK ? 2 : 1;  // over K.  Three: A B, A B2, A2 B
@@ -614,7 +614,7 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64) void gg_bf16_kernel(const Ge
         });
       }
     }
-    if constexpr (EPI == EPI_STORE_F32 || EPI == EPI_ROWS_F32 || LOGITS || PAIRS) {
+    if constexpr (EPI == EPI_STORE_F32 || EPI == EPI_STORE_DUALK_F32 || EPI == EPI_ROWS_F32 || LOGITS || PAIRS) {
       if (!LOGITS || cc.C) {
       // float32 output (weight gradients).  It goes through LDS, one 32 x 32 block (4 KiB) at a time: written in
       // accumulator order (16 bytes per lane), read back row-wise, so that global memory sees whole 128-byte lines, also

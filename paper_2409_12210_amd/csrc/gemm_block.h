@@ -120,7 +120,7 @@ __device__ __forceinline__ void gg_block(const GemmPlan* __restrict__ plan, int 
   constexpr bool PAIRS = EPI == EPI_STORE_PAIRS || EPI == EPI_LOGITS_PAIRS;
   constexpr bool ROWS16 = EPI == EPI_ROWS_F32 && !F32, HALF = ROWS16 || PAIRS;  // HALF: float16 operands
   constexpr bool LOGITS = EPI == EPI_LOGITS || EPI == EPI_LOGITS_PAIRS;
-  constexpr int PASSES = PAIRS ? 3 : EPI == EPI_STORE_DUALK || ROWS16 ? 2 : 1;
+  constexpr int PASSES = PAIRS ? 3 : EPI == EPI_STORE_DUALK || EPI == EPI_STORE_DUALK_F32 || ROWS16 ? 2 : 1;
   static_assert(!F32 || !PAIRS, "16-bit operands");
   const int nsteps = PASSES * nk;
   const uint32_t lds_base = __builtin_amdgcn_readfirstlane(lds_address(ring));
@@ -397,7 +397,7 @@ __device__ __forceinline__ void gg_block(const GemmPlan* __restrict__ plan, int 
   // A wave stages units of 32 rows x 128 bytes (64 for a 32-column bf16 tile) through LDS, so that global memory sees
   // whole lines: written in accumulator order, read back row-wise.  The staging area lies in the slots that the step
   // after the last one would use: nobody reads them any more and no load is on its way into them.
-  typedef std::conditional_t<F32 || EPI == EPI_STORE_F32 || LOGITS || HALF, float, bf16_t> out_t;
+  typedef std::conditional_t<F32 || EPI == EPI_STORE_F32 || EPI == EPI_STORE_DUALK_F32 || LOGITS || HALF, float, bf16_t> out_t;
   constexpr int OS = sizeof(out_t), UC = OS == 4 ? 32 : (WN < 64 ? WN : 64);  // columns of a unit
   constexpr int CPR = UC * OS / 16, ITS = 32 * CPR / 64, NJU = WN / UC, JPU = UC / 32;
   typedef std::conditional_t<OS == 4, f32x4, bf16x8> chunk_t;
@@ -553,7 +553,7 @@ __device__ __forceinline__ void gg_block(const GemmPlan* __restrict__ plan, int 
         }
         if constexpr (ROWS16) stage([&](int jj, int x) { return acc[0][i][j0 + jj][x] * scale[0] * scale[1]; });
         else stage([&](int jj, int x) { return acc[0][i][j0 + jj][x]; });
-        if constexpr (EPI == EPI_STORE_F32 || EPI == EPI_ROWS_F32) {
+        if constexpr (EPI == EPI_STORE_F32 || EPI == EPI_STORE_DUALK_F32 || EPI == EPI_ROWS_F32) {
           if (accumulate) {
             chunk_t old[ITS];
 #pragma unroll

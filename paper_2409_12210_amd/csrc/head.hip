@@ -20,11 +20,10 @@
 // Up to 64 rows (small vocabularies: more) a stream over W makes the logits, see "few rows".  dW of a small vocabulary has few tiles,
 // so its sum over the tokens is cut into parts as well (float32, 1000 x 512, 4096 rows: with the stream 160 us in place of 337 for the whole call).
 //
-// dX of a bf16 layer is rounded to bf16, and takes G rounded to bf16.  What that loses of the target's entry, the largest of its row as a
-// rule, is put back in float32 where the slabs are added up: it is a multiple of a row of W.  (Without that dX was off by 2.4e-3 of
-// its norm, of which the rounding of the result is 1.7e-3.)  Up to 128 rows, which fill half a tile, the product takes a second
-// bf16 number for each entry as rows of their own, for nothing.  dW is float32, and takes G as the sum of two float16 numbers, hi + lo,
-// which hold 22 bits, times float16 copies of the rows of x: both times powers of two that follow the largest |x| and the largest
+// dX of a bf16 layer takes G as the sum of two bf16 numbers, which hold 16 bits, in two passes over W; what they lose lies below the rounding
+// of the result.  (One number, with what it loses of the target's entry put back in float32: 2 T V d operations less, but where another token
+// has most of the probability an error of 2.0e-3 of the norm, of which the rounding of the result is 1.65e-3.)  Up to 128 rows, which fill half a
+// tile, the second numbers are rows of their own.  dW is float32, and takes G as the sum of two float16 numbers, hi + lo, which hold 22 bits, times float16 copies of the rows of x: both times powers of two that follow the largest |x| and the largest
 // |d_logp| of the call, so that what is rounded or lost is below 2^-39 of the largest product.  (Two bf16 numbers, 16 bits, left an
 // error of 2.7e-6 of dW where float32 products have 0.7e-6 to 2e-6, and need no third copy of G; the rest takes as long.)
 #include <cmath>
@@ -45,7 +44,7 @@ constexpr int64_t PAIR_CELLS = (int64_t)1 << 27;   // pairs of 128 columns in it
 constexpr int64_t W_PART = (int64_t)1 << 30;       // elements of W that one problem reads (kernels count them in 32 bits)
 constexpr size_t ALIGN = 256;                      // of what is in the workspace, which itself may lie at any sixteen bytes
 constexpr int64_t SLAB_CELLS = (int64_t)1 << 26;   // values of all parts of dX together, unless one part has more
-constexpr int64_t STACK_ROWS = 128;                // of bf16 layers up to which dX takes G in two parts
+constexpr int64_t STACK_ROWS = 128;                // of bf16 layers up to which the second numbers of G are rows of their own in the product of dX
 constexpr int MAX_PARTS = 128;                     // of dX, of dW (problems of a product: fewer than 192)
 static_assert(MAX_PARTS <= MODSE_MAX_PROBLEMS, "a problem for each");
 
@@ -163,7 +162,8 @@ HeadShape head_shape(int64_t T, int32_t d, int32_t vocab, modse_dtype dt, bool g
   for (int64_t n = 1; n <= parts_most; ++n) {
     const int64_t len = (steps + n - 1) / n, parts = (steps + len - 1) / len;
     const double step_us = h.wide ? (h.pairs ? 3 : 1) * (dx == 128 ? 1.0 : 1.6) : dx == 64 ? 3.0 : 8.0;
-    const double us = (double)((out * parts + slots - 1) / slots) * (len + 6) * step_us + parts * (double)h.dx_rows * d * 8 / 4e6;
+    const int64_t passes = h.bf16 && h.dx_rows == h.rows ? 2 : 1;  // (over K, of one length)
+    const double us = (double)((out * parts + slots - 1) / slots) * (passes * len + 6) * step_us + parts * (double)h.dx_rows * d * 8 / 4e6;
     if (n == 1 || us < best) {
       best = us;
       h.k_parts = (int32_t)parts;
@@ -198,8 +198,7 @@ struct HeadBufs {
   float* pairs;      // [ceil(vocab / pair_cols)][sub] maximum and sum
   float* at_target;  // [sub] the target's logit, and behind them [sub] what undoes the scaling of a row of x (float32 by pairs)
   float* off;        // [sub][2] the row's maximum and log2 of its sum
-  bf16_t* g;         // [dx_rows, ldv] G, and behind its rows what it lacks of them
-  float* lost;       // [rows] what G lacks of the target's entry
+  bf16_t* g;         // [2 rows, ldv] G, and behind its rows what bf16 lacks of them
   f16_t *hi, *lo;    // [rows, ldv] G in two parts, scaled
   f16_t *x16, *x16_lo;   // [rows, d] x in the same way; x16_lo: float32 layers
   f16_t *w16, *w16_lo;   // [vocab, d] W, float32 layers
@@ -412,6 +411,10 @@ __global__ __launch_bounds__(1024) void head_plan_kernel(HeadPlanArgs a) {
         P.B = a.b.w16 + (size_t)v0 * h.d;
         P.B2 = a.b.w16_lo + (size_t)v0 * h.d;
       }
+      if (h.bf16 && h.dx_rows == h.rows) {
+        P.A2 = a.b.g + (size_t)h.rows * h.ldv + v0;
+        P.B2 = P.B;
+      }
       P.C = a.b.slabs + (size_t)p * h.dx_rows * h.d;
       P.M = h.dx_rows > h.rows ? h.dx_rows : m; P.N = h.d; P.K = min(h.k_len, h.vocab - v0);
       P.lda = h.ldv; P.ldb = h.d; P.ldc = h.d;
@@ -446,8 +449,7 @@ struct HeadRowsArgs {
   float* logits;
   const float *pairs, *at_target;
   float* off;
-  bf16_t *g, *g_rest;      // of the product's first row; null where there is no dX, or (g_rest) no second part
-  float* lost;             // null where there is no dX
+  bf16_t *g, *g_rest;      // of the product's first row; null where there is no dX
   f16_t *hi, *lo;          // null where there is no dW
   HeadRange* range;
   const void* x;           // of the product's first row, and their copies for dW, with zeros in rows without a target
@@ -518,7 +520,7 @@ __global__ __launch_bounds__(1024) void head_stats_kernel(HeadRowsArgs a) {
   a.off[2 * row + 1] = log2_sum;
 }
 
-// bf16: G of a row's 2048 columns, in bf16 for dX, in two parts for dW.  Columns behind the vocabulary become zeros.  Blocks behind the rows'
+// 16-bit products: G of a row's 2048 columns, in two bf16 numbers for dX of bf16 layers, in two float16 ones for what else there is.  Columns behind the vocabulary become zeros.  Blocks behind the rows'
 // make the float16 copies of x, 2048 values each.
 __global__ __launch_bounds__(256) void head_grad_kernel(HeadRowsArgs a, int segs) {
   if ((int)blockIdx.x >= a.rows * segs) {
@@ -542,21 +544,17 @@ __global__ __launch_bounds__(256) void head_grad_kernel(HeadRowsArgs a, int segs
                       __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(a.logits + at + 4))};
   bf16x8 g, rest;
   f16x8 hi, lo;
-  float lost = 0.f;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     const float x = grad_of(v[e >> 2][e & 3], top, log2_sum, w, target, c + e, a.vocab), scaled = x * scale;
     g[e] = (bf16_t)x;
-    const float left = x - (float)g[e];
-    rest[e] = (bf16_t)left;
-    lost = c + e == target ? left : lost;
+    rest[e] = (bf16_t)(x - (float)g[e]);
     hi[e] = (f16_t)scaled;
     lo[e] = (f16_t)(scaled - (float)hi[e]);
   }
   if (a.g) {
     *reinterpret_cast<bf16x8*>(a.g + at) = g;
-    if (a.g_rest) *reinterpret_cast<bf16x8*>(a.g_rest + at) = rest;
-    if (c == (target >= 0 && target < a.vocab ? target / 8 * 8 : 0)) a.lost[row] = lost;
+    *reinterpret_cast<bf16x8*>(a.g_rest + at) = rest;
   }
   if (a.hi) {
     *reinterpret_cast<f16x8*>(a.hi + at) = hi;
@@ -590,12 +588,9 @@ __global__ __launch_bounds__(256) void head_grad_f32_kernel(HeadRowsArgs a, int 
 // waves share out (24 x 256, 128 parts: 4.9 us in place of 8.7; twice the parts, 64 rows: 6.9 in place of 14.6).
 struct HeadJoinArgs {
   const float* slabs;
-  const bf16_t* W;         // where G lacks something of the targets' entries, or null
-  const float* lost;
-  const int32_t* targets;
   const float* undo;       // factors of the slabs, or null
-  int64_t stride, rest;    // from part to part; to the rows of G's second parts, or 0
-  int32_t parts, d, vocab;
+  int64_t stride, rest;    // from part to part; to the rows of G's second numbers, or 0
+  int32_t parts, d;
 };
 template <typename T, bool SHARED>
 __global__ __launch_bounds__(256) void head_join_kernel(HeadJoinArgs a, T* dX) {
@@ -629,15 +624,6 @@ __global__ __launch_bounds__(256) void head_join_kernel(HeadJoinArgs a, T* dX) {
     for (int w = 1; w < 4; ++w) s += s_part[w][lane];
   }
   if (a.undo) s = s * a.undo[0] * a.undo[1];
-  if (a.W) {
-    const int32_t target = a.targets[row];
-    if (target >= 0 && target < a.vocab) {
-      const bf16x4 w = *reinterpret_cast<const bf16x4*>(a.W + (int64_t)target * a.d + c);
-      const float lost = a.lost[row];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) s[e] += lost * (float)w[e];
-    }
-  }
 #pragma unroll
   for (int e = 0; e < 4; ++e) dX[i + e] = (T)s[e];
 }
@@ -882,9 +868,9 @@ size_t stream_pairs(int64_t T, int32_t vocab) { return (size_t)T * ((vocab + STR
 size_t stream_workspace(int64_t T, int32_t vocab) { return ALIGN + align_up(stream_pairs(T, vocab), ALIGN) + (size_t)T * 4; }
 
 struct HeadLayout {
-  size_t range, logits, pairs, at_target, off, lost, g, hi, lo, x16, x16_lo, w16, w16_lo, x32, slabs, total;
+  size_t range, logits, pairs, at_target, off, g, hi, lo, x16, x16_lo, w16, w16_lo, x32, slabs, total;
 };
-HeadLayout layout_for(int64_t plans, int64_t sub, int64_t rows, int64_t dx_rows, int64_t slab_cells, int32_t d, int32_t vocab, bool bf16,
+HeadLayout layout_for(int64_t plans, int64_t sub, int64_t rows, int64_t slab_cells, int32_t d, int32_t vocab, bool bf16,
                       bool pairs, bool grad) {
   HeadLayout w = {};
   const bool wide = bf16 || pairs;
@@ -903,8 +889,7 @@ HeadLayout layout_for(int64_t plans, int64_t sub, int64_t rows, int64_t dx_rows,
   w.logits = take(grad ? (size_t)sub * ldv * 4 : 0);
   w.pairs = take(std::max(pair_cells(sub, d, vocab, wide) * 8, stream_pairs(std::min(sub, stream_rows(vocab)), vocab)));
   w.off = take((size_t)sub * 8);
-  w.lost = take(bf16 && grad ? (size_t)rows * 4 : 0);
-  w.g = take(bf16 && grad ? (size_t)dx_rows * ldv * 2 : 0);
+  w.g = take(bf16 && grad ? 2 * cells * 2 : 0);
   w.hi = take(wide && grad ? cells * 2 : 0);
   w.lo = take(wide && grad ? cells * 2 : 0);
   w.x16 = take(pairs || (bf16 && grad) ? (size_t)rows * d * 2 : 0);
@@ -925,7 +910,7 @@ size_t most_workspace(int64_t T, int32_t d, int32_t vocab, bool bf16, bool pairs
   const int64_t dx_rows = bf16 ? std::max(rows, std::min(2 * rows, 2 * STACK_ROWS)) : rows;
   const int64_t dw_parts = dw_most_parts(d, vocab, wide);
   const int64_t slabs = std::max(std::min(MAX_PARTS * dx_rows * d, std::max(SLAB_CELLS, dx_rows * d)), dw_parts > 1 ? dw_parts * vocab * d : 0);
-  return ALIGN + layout_for(plans, sub, rows, dx_rows, slabs, d, vocab, bf16, pairs, grad).total;
+  return ALIGN + layout_for(plans, sub, rows, slabs, d, vocab, bf16, pairs, grad).total;
 }
 }  // namespace
 
@@ -952,13 +937,13 @@ hipError_t launch_head(modse_dtype dt, const HeadArgs& a, char* ws, hipStream_t 
   const HeadShape h = head_shape(a.T, a.d, a.vocab, dt, grad);
   const int64_t products = h.products(), plans = products + (grad ? 2 * h.pieces : 0);
   const int64_t slabs = std::max((int64_t)h.k_parts * h.dx_rows * h.d, h.w_split > 1 ? (int64_t)h.w_split * h.vocab * h.d : 0);
-  const HeadLayout w = layout_for(plans, h.sub, h.rows, h.dx_rows, slabs, h.d, h.vocab, h.bf16, h.pairs, grad);
+  const HeadLayout w = layout_for(plans, h.sub, h.rows, slabs, h.d, h.vocab, h.bf16, h.pairs, grad);
   ws = reinterpret_cast<char*>(align_up(reinterpret_cast<size_t>(ws), ALIGN));
   auto floats = [&](size_t at) { return reinterpret_cast<float*>(ws + at); };
   auto halves = [&](size_t at) { return reinterpret_cast<f16_t*>(ws + at); };
   HeadRange* const range = h.pairs || (h.bf16 && grad) ? reinterpret_cast<HeadRange*>(ws + w.range) : nullptr;
   const HeadBufs b = {reinterpret_cast<GemmPlan*>(ws), floats(w.logits), floats(w.pairs), floats(w.at_target), floats(w.off),
-                      reinterpret_cast<bf16_t*>(ws + w.g), floats(w.lost), halves(w.hi), halves(w.lo), halves(w.x16), halves(w.x16_lo),
+                      reinterpret_cast<bf16_t*>(ws + w.g), halves(w.hi), halves(w.lo), halves(w.x16), halves(w.x16_lo),
                       halves(w.w16), halves(w.w16_lo), floats(w.x32), range, floats(w.slabs)};
   const HeadPlanArgs plan = {h, b, a.x, a.W, a.targets, a.d_logp, a.dW, (int32_t)plans};
   const int64_t looked_at = h.T * h.d + (h.pairs ? (int64_t)h.vocab * h.d : 0);
@@ -993,7 +978,7 @@ hipError_t launch_head(modse_dtype dt, const HeadArgs& a, char* ws, hipStream_t 
     if (e != hipSuccess) return;
     const HeadRowsArgs r = {a.targets + t0, a.d_logp ? a.d_logp + t0 : nullptr, a.logp ? a.logp + t0 : nullptr, a.log_z ? a.log_z + t0 : nullptr,
                             b.logits, b.pairs, b.at_target, b.off, a.dX && h.bf16 ? b.g + in_piece * h.ldv : nullptr,
-                            a.dX && h.dx_rows > h.rows ? b.g + (int64_t)h.rows * h.ldv : nullptr, b.lost + in_piece,
+                            a.dX && h.bf16 ? b.g + (h.rows + in_piece) * h.ldv : nullptr,
                             a.dW || h.pairs ? b.hi + in_piece * h.ldv : nullptr, a.dW || h.pairs ? b.lo + in_piece * h.ldv : nullptr,
                             range, static_cast<const char*>(a.x) + (size_t)t0 * h.d * (h.bf16 ? 2 : 4), b.x16 + in_piece * h.d,
                             a.dW && !h.wide ? b.x32 + in_piece * h.d : nullptr, (int32_t)m, h.vocab, h.ldv, h.sub, h.pair_cols(), h.d};
@@ -1026,12 +1011,11 @@ hipError_t launch_head(modse_dtype dt, const HeadArgs& a, char* ws, hipStream_t 
     }
     if (a.dX) {
       const bool stacked = h.dx_rows > h.rows;
-      e = launch_grouped_gemm(dt, h.pairs ? EPI_STORE_PAIRS : EPI_STORE_F32, h.dx_tile, p, h.k_parts, 0, 0,
+      e = launch_grouped_gemm(dt, h.pairs ? EPI_STORE_PAIRS : h.bf16 && !stacked ? EPI_STORE_DUALK_F32 : EPI_STORE_F32, h.dx_tile, p, h.k_parts, 0, 0,
                               h.k_parts * tiles_of(stacked ? h.dx_rows : m, h.d, h.dx_tile), s, LAYOUT_B_KN);
       if (e != hipSuccess) break;
-      const HeadJoinArgs j = {b.slabs, h.bf16 && !stacked ? static_cast<const bf16_t*>(a.W) : nullptr, b.lost, a.targets + t0,
-                              h.pairs ? range->undo_dx : nullptr, (int64_t)h.dx_rows * h.d, stacked ? (int64_t)h.rows * h.d : 0, h.k_parts,
-                              h.d, h.vocab};
+      const HeadJoinArgs j = {b.slabs, h.pairs ? range->undo_dx : nullptr, (int64_t)h.dx_rows * h.d, stacked ? (int64_t)h.rows * h.d : 0,
+                              h.k_parts, h.d};
       e = h.bf16 ? run_join(j, m, static_cast<bf16_t*>(a.dX) + t0 * h.d, s) : run_join(j, m, static_cast<float*>(a.dX) + t0 * h.d, s);
     }
   }

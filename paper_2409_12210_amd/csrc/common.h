@@ -81,6 +81,9 @@ struct GemmPlan {
   int32_t tile_start[MODSE_MAX_PROBLEMS + 1];  // prefix sum of mtiles*ntiles in problem order
 };
 
+// Maxima begin with it, not with -infinity, which may be a value (of a logit): the difference of two infinities is NaN.
+constexpr float LOWEST = -3.402823466e38f;
+
 enum GemmEpilogue {
   EPI_STORE = 0,       // C = acc (element type of the layer)
   EPI_STORE_F32 = 1,   // C = acc or C += acc, float32 (weight gradients)

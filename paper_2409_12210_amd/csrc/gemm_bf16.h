@@ -581,7 +581,7 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64) void gg_bf16_kernel(const Ge
           constexpr int i = decltype(block)::value;
           const int row = row0 + i * 16;
           const int at = want[i] - first_col - equad * 4;
-          float m = -__builtin_inff(), there = 0.f;
+          float m = LOWEST, there = 0.f;
           auto value = [&](int j, int x) { return j * 16 + equad * 4 + x < nleft ? acc[0][i][j][x] : -__builtin_inff(); };
           auto sums = [&](auto inside_tag) {
             constexpr bool INSIDE = decltype(inside_tag)::value;

@@ -471,7 +471,7 @@ __device__ __forceinline__ void gg_block(const GemmPlan* __restrict__ plan, int 
           for (int j = 0; j < NI; ++j) acc[0][i][j] = acc[0][i][j] * fminf(of_a, of_b) * fmaxf(of_a, of_b);
         }
         const int at = max(targets[min(row, M - 1)], -1) - first_col - khalf * 4;
-        float m = -__builtin_inff(), there = 0.f, s = 0.f;
+        float m = LOWEST, there = 0.f, s = 0.f;
         auto value = [&](int j, int x) { return j * 32 + (x >> 2) * 8 + (x & 3) + khalf * 4 < nleft ? acc[0][i][j][x] : -__builtin_inff(); };
 #pragma unroll
         for (int j = 0; j < NI; ++j)

@@ -481,7 +481,7 @@ __global__ __launch_bounds__(1024) void head_stats_kernel(HeadRowsArgs a) {
   const int row = blockIdx.x * 16 + (lane & 15), n = (a.vocab + a.pair_cols - 1) / a.pair_cols;
   constexpr int AHEAD = 4;
   typedef float f32x2 __attribute__((ext_vector_type(2)));
-  float m = -__builtin_inff(), s = 0.f;
+  float m = LOWEST, s = 0.f;
   if (row < a.rows) {
     for (int p = quarter; p < n; p += 64 * AHEAD) {
       f32x2 v[AHEAD];
@@ -503,8 +503,8 @@ __global__ __launch_bounds__(1024) void head_stats_kernel(HeadRowsArgs a) {
   if (a.range && wave == 15) join_range(a.range);
   __syncthreads();
   if (wave > 0) return;
-  // (a quarter of this wave joins sixteen of the sums.  The first always has seen a pair, so the row's maximum is one's)
-  float top = -__builtin_inff(), sum = 0.f;
+  // (a quarter of this wave joins sixteen of the sums)
+  float top = LOWEST, sum = 0.f;
 #pragma unroll
   for (int w = 0; w < 16; ++w) top = fmaxf(top, s_m[quarter * 16 + w][lane & 15]);
   top = fmaxf(top, __shfl_xor(top, 16, 64));
@@ -785,14 +785,14 @@ __global__ __launch_bounds__(256, 2) void head_stream_kernel(HeadStreamArgs a) {
     float m = fmaxf(fmaxf(l[0], l[1]), fmaxf(l[2], l[3]));
     m = fmaxf(m, __shfl_xor(m, 16, 64));
     m = fmaxf(m, __shfl_xor(m, 32, 64));
-    const float lowest = fmaxf(m, -3.402823466e38f);  // (a fragment behind the vocabulary has no maximum)
+    m = fmaxf(m, LOWEST);
     float s = 0.f;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) s += __builtin_amdgcn_exp2f((l[e] - lowest) * LOG2E);
+    for (int e = 0; e < 4; ++e) s += __builtin_amdgcn_exp2f((l[e] - m) * LOG2E);
     s += __shfl_xor(s, 16, 64);
     s += __shfl_xor(s, 32, 64);
     if (quad == 0) {
-      s_m[wave][j * 16 + r] = lowest;
+      s_m[wave][j * 16 + r] = m;
       s_s[wave][j * 16 + r] = s;
     }
   }
@@ -815,7 +815,7 @@ __global__ __launch_bounds__(1024) void head_stream_join_kernel(HeadStreamArgs a
   typedef float f32x2 __attribute__((ext_vector_type(2)));
   const int t = blockIdx.x, n = (a.vocab + STREAM_W - 1) / STREAM_W, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const f32x2* const pairs = reinterpret_cast<const f32x2*>(a.pairs) + (int64_t)t * n;
-  float m = -3.402823466e38f, s = 0.f;
+  float m = LOWEST, s = 0.f;
   for (int p = threadIdx.x; p < n; p += 1024 * AHEAD) {
     f32x2 v[AHEAD];
 #pragma unroll

@@ -26,7 +26,6 @@ constexpr int LIST_FULL = 128;  // at which the list is cut back to the n larges
 constexpr int LOOK = 32;        // entries of a thread that are loaded, and looked through, together, in vectors of sixteen bytes
 constexpr int GROUP = LOOK * 256;  // entries that a block takes at a time
 constexpr float LOG2E = 1.44269504088896340736f;
-constexpr float LOWEST = -3.402823466e38f;
 constexpr float FAR = -1e30f;   // differences of logits below it are held at it: e^FAR is 0, and 0 * FAR is no NaN
 constexpr float NIL = -200.f;   // where they are multiplied by a gradient first: e^NIL is 0, and NIL times any loss scale is finite
 

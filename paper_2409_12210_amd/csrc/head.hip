@@ -38,7 +38,6 @@ namespace {
 using namespace modse_gemm;
 
 constexpr int64_t GRAD_CELLS = (int64_t)1 << 28;   // values of G in the workspace (float32: of logits)
-constexpr int64_t LOGIT_CELLS = (int64_t)1 << 28;  // bf16 logits in the workspace
 constexpr int64_t PAIR_W = (int64_t)1 << 28;       // elements of W of which the parts are kept
 constexpr int64_t PAIR_CELLS = (int64_t)1 << 27;   // pairs of 128 columns in it
 constexpr int64_t W_PART = (int64_t)1 << 30;       // elements of W that one problem reads (kernels count them in 32 bits)
@@ -51,8 +50,7 @@ static_assert(MAX_PARTS <= MODSE_MAX_PROBLEMS, "a problem for each");
 struct HeadShape {
   int64_t T;
   int32_t d, vocab, ldv;   // ldv: distance of rows of logits and G
-  int32_t rows, pieces;    // rows of a piece
-  int32_t sub, subs;       // rows that one product of logits takes, such products of a (whole) piece
+  int32_t rows, pieces;    // rows of a piece (the last one may have fewer)
   int32_t w_parts, w_rows; // problems of the logits, rows of W in each
   int32_t dx_rows;         // rows of the product of dX: those of a piece, or twice as many
   int32_t k_parts, k_len;  // problems of dX, columns of G in each
@@ -62,7 +60,6 @@ struct HeadShape {
   int32_t wide;            // either of them: tiles of 256, sums of exponentials by the product of the logits
   TileShape logits_tile, dx_tile, dw_tile;
   __host__ __device__ int pair_cols() const { return logits_tile.bn / 2; }  // columns of a pair of maximum and sum
-  __host__ __device__ int64_t products() const { return (T + sub - 1) / sub; }  // (sub divides rows)
 };
 
 int32_t padded_rows(int64_t n) { return (int32_t)align_up((size_t)n, 32); }
@@ -74,9 +71,6 @@ int64_t rows_in(int64_t cells, int64_t per_row) {
 }
 int64_t most_rows(int32_t vocab, bool wide, bool grad) {
   return wide && !grad ? rows_in(PAIR_CELLS, (vocab + 127) / 128) : rows_in(GRAD_CELLS, (int64_t)align_up(vocab, 64));
-}
-int64_t most_sub(int32_t vocab, bool wide, bool grad) {
-  return wide && grad ? rows_in(LOGIT_CELLS, (int64_t)align_up(vocab, 64)) : most_rows(vocab, wide, grad);
 }
 // Float32 layers: the rows from which on products of pairs of float16 numbers are faster, three 16-bit products in place of one of float32,
 // with the largest values and the parts of W (and some launches) before them.  At 105 and 1150 TFLOP/s, 5 TB/s and tiles that are 128 rows too
@@ -134,19 +128,19 @@ HeadShape head_shape(int64_t T, int32_t d, int32_t vocab, modse_dtype dt, bool g
   h.pairs = takes_pairs(T, d, vocab, dt, grad);
   h.wide = h.bf16 || h.pairs;
   h.ldv = (int32_t)align_up(vocab, 64);
-  const int64_t most = most_rows(vocab, h.wide, grad), sub = std::min(most, most_sub(vocab, h.wide, grad));
-  // pieces of about one size, in whole products of logits
-  h.sub = T <= sub ? padded_rows(T) : (int32_t)sub;
+  // Pieces of about one size, whole tiles of 256: a last one of a few rows would go over all of W and dW for them.  Gradients of 8193 rows with
+  // 32000 x 2048, as 8192 + 1 / 4352 + 3841: bf16 5850 / 4975 us, float32 9870 / 8320; 2049 rows with
+  // 131072 x 2048, 2048 + 1 / 1280 + 769: 6580 / 5660, 11170 / 9710.
+  const int64_t most = most_rows(vocab, h.wide, grad);
   h.pieces = (int32_t)((T + most - 1) / most);
-  h.rows = (int32_t)align_up((size_t)((T + h.pieces - 1) / h.pieces), (size_t)h.sub);
+  h.rows = h.pieces == 1 ? padded_rows(T) : (int32_t)align_up((size_t)((T + h.pieces - 1) / h.pieces), 256);
   h.pieces = (int32_t)((T + h.rows - 1) / h.rows);
-  h.subs = h.rows / h.sub;
   h.w_rows = (int32_t)std::min<int64_t>(vocab, W_PART / d / 256 * 256);
   h.w_parts = (vocab + h.w_rows - 1) / h.w_rows;
   // (float32: tiles of 128 from four rounds of the chip's 512 workgroups on.  50304 x 256, 1.5 rounds: 287 us with them, 258 with tiles of
   // 64; 1021 x 50257, 6.1 rounds: 251 and 261)
   auto tile = [&](int64_t m, int64_t n) { const int b = h.wide ? 256 : tiles(m, n, 128) >= 2048 ? 128 : 64; return TileShape{b, b}; };
-  h.logits_tile = h.wide && logits_take_blocks(T, d, vocab, h.bf16 && !grad) ? TileShape{128, 128} : tile(h.sub, vocab);
+  h.logits_tile = h.wide && logits_take_blocks(T, d, vocab, h.bf16 && !grad) ? TileShape{128, 128} : tile(h.rows, vocab);
   h.dw_tile = h.bf16 && dw_takes_blocks(T, tiles(vocab, d, 256)) ? TileShape{128, 128} : tile(vocab, d);
   const int64_t w_steps = (h.rows + 63) / 64, w_split = std::min(dw_most_parts(d, vocab, h.wide), std::max<int64_t>(1, w_steps / 4));
   h.w_len = (int32_t)((w_steps + w_split - 1) / w_split) * 64;
@@ -193,11 +187,11 @@ typedef _Float16 f16_t;
 typedef f16_t f16x8 __attribute__((ext_vector_type(8)));
 
 struct HeadBufs {
-  GemmPlan* plans;   // logits of every product, then dX and dW of every piece
-  float* logits;     // [sub, ldv]; float32 layers: then G
-  float* pairs;      // [ceil(vocab / pair_cols)][sub] maximum and sum
-  float* at_target;  // [sub] the target's logit, and behind them [sub] what undoes the scaling of a row of x (float32 by pairs)
-  float* off;        // [sub][2] the row's maximum and log2 of its sum
+  GemmPlan* plans;   // logits of every piece, then dX and dW of every piece
+  float* logits;     // [rows, ldv]; float32 layers: then G
+  float* pairs;      // [ceil(vocab / pair_cols)][rows] maximum and sum
+  float* at_target;  // [rows] the target's logit, and behind them [rows] what undoes the scaling of a row of x (float32 by pairs)
+  float* off;        // [rows][2] the row's maximum and log2 of its sum
   bf16_t* g;         // [2 rows, ldv] G, and behind its rows what bf16 lacks of them
   f16_t *hi, *lo;    // [rows, ldv] G in two parts, scaled
   f16_t *x16, *x16_lo;   // [rows, d] x in the same way; x16_lo: float32 layers
@@ -335,7 +329,7 @@ __global__ __launch_bounds__(256) void head_split_w_kernel(const float* W, int64
 // Rows of x, some lanes of a wave each.  Scoring: each by its own largest value, so that what stands in one row (one that pads the batch,
 // say) does not touch another.  Gradients, whose sum for dW runs over rows: by that of all rows with a target, and zeros for the others.
 __global__ __launch_bounds__(256) void head_split_x_kernel(const float* x, const int32_t* targets, int rows, int d, int vocab, int grad,
-                                                           const HeadRange* range, f16_t* hi, f16_t* lo, float* undo, int undo_rows) {
+                                                           const HeadRange* range, f16_t* hi, f16_t* lo, float* undo) {
   const int lanes = lanes_of(d / 8), lane = threadIdx.x & (lanes - 1);
   const int64_t row = ((int64_t)blockIdx.x * 256 + threadIdx.x) / lanes;
   if (row >= rows) return;
@@ -348,7 +342,7 @@ __global__ __launch_bounds__(256) void head_split_x_kernel(const float* x, const
     for (int o = lanes / 2; o; o >>= 1) most = max(most, (uint32_t)__shfl_xor((int)most, o, 64));
   }
   const int e = scale_exponent(most);
-  if (lane == 0 && row < undo_rows) undo[row] = power_of_two(-e);
+  if (lane == 0) undo[row] = power_of_two(-e);
   const bool there = !grad || (targets[row] >= 0 && targets[row] < vocab);
   for (int c = lane * 8; c < d; c += lanes * 8) {
     f32x4 v[2] = {};
@@ -360,8 +354,8 @@ __global__ __launch_bounds__(256) void head_split_x_kernel(const float* x, const
   }
 }
 
-// The problems of one product, by a block's first wave: of the logits, one block for each, then of dX and of dW, a block for each
-// piece.  Blocks behind these look for the largest values.
+// The problems of one product, by a block's first wave: of the logits, a block for each piece, then of dX and of dW, a block for each.
+// Blocks behind these look for the largest values.
 __global__ __launch_bounds__(1024) void head_plan_kernel(HeadPlanArgs a) {
   __shared__ int s_tiles[MODSE_MAX_PROBLEMS];
   if ((int)blockIdx.x >= a.plans) {
@@ -370,12 +364,11 @@ __global__ __launch_bounds__(1024) void head_plan_kernel(HeadPlanArgs a) {
   }
   if (threadIdx.x >= 64) return;
   const HeadShape& h = a.h;
-  const int lane = threadIdx.x, products = (int)h.products();
-  const int which = (int)blockIdx.x < products ? 0 : 1 + ((int)blockIdx.x - products) % 2;
-  const int rows = which == 0 ? h.sub : h.rows;
-  const int64_t t0 = (int64_t)(which == 0 ? (int)blockIdx.x : ((int)blockIdx.x - products) / 2) * rows;
+  const int lane = threadIdx.x, behind = (int)blockIdx.x - h.pieces;
+  const int which = behind < 0 ? 0 : 1 + behind % 2;
+  const int64_t t0 = (int64_t)(which == 0 ? (int)blockIdx.x : behind / 2) * h.rows;
   const size_t es = h.bf16 ? 2 : 4;
-  const int m = (int)min((int64_t)rows, h.T - t0);
+  const int m = (int)min((int64_t)h.rows, h.T - t0);
   const char* const x = cadd(a.x, (size_t)t0 * h.d * es);
   GemmPlan* const plan = a.b.plans + blockIdx.x;
   const int n = which == 0 ? h.w_parts : which == 1 ? h.k_parts : h.w_split;
@@ -387,9 +380,8 @@ __global__ __launch_bounds__(1024) void head_plan_kernel(HeadPlanArgs a) {
       P.A = x;
       P.B = cadd(a.W, (size_t)v0 * h.d * es);
       if (h.pairs) {
-        const int64_t in_piece = t0 % h.rows * h.d;
-        P.A = a.b.x16 + in_piece;
-        P.A2 = a.b.x16_lo + in_piece;
+        P.A = a.b.x16;
+        P.A2 = a.b.x16_lo;
         P.B = a.b.w16 + (size_t)v0 * h.d;
         P.B2 = a.b.w16_lo + (size_t)v0 * h.d;
       }
@@ -397,7 +389,7 @@ __global__ __launch_bounds__(1024) void head_plan_kernel(HeadPlanArgs a) {
       P.C2 = a.b.pairs;
       P.C3 = a.b.at_target;
       P.E1 = a.targets + t0;
-      P.E2 = reinterpret_cast<const void*>((uint64_t)h.sub << 32 | (uint32_t)v0);
+      P.E2 = reinterpret_cast<const void*>((uint64_t)h.rows << 32 | (uint32_t)v0);
       P.M = m; P.N = min(h.w_rows, h.vocab - v0); P.K = h.d;
       P.lda = h.d; P.ldb = h.d; P.ldc = h.ldv;
       t = h.logits_tile;
@@ -520,8 +512,8 @@ __global__ __launch_bounds__(1024) void head_stats_kernel(HeadRowsArgs a) {
   a.off[2 * row + 1] = log2_sum;
 }
 
-// 16-bit products: G of a row's 2048 columns, in two bf16 numbers for dX of bf16 layers, in two float16 ones for what else there is.  Columns behind the vocabulary become zeros.  Blocks behind the rows'
-// make the float16 copies of x, 2048 values each.
+// 16-bit products: G of a row's 2048 columns, in two bf16 numbers for dX of bf16 layers, in two float16 ones for what else there is.  Columns
+// behind the vocabulary become zeros.  Blocks behind the rows' make the float16 copies of x of bf16 layers, 2048 values each.
 __global__ __launch_bounds__(256) void head_grad_kernel(HeadRowsArgs a, int segs) {
   if ((int)blockIdx.x >= a.rows * segs) {
     const int64_t i = (int64_t)(blockIdx.x - a.rows * segs) * 2048 + threadIdx.x * 8;
@@ -870,7 +862,7 @@ size_t stream_workspace(int64_t T, int32_t vocab) { return ALIGN + align_up(stre
 struct HeadLayout {
   size_t range, logits, pairs, at_target, off, g, hi, lo, x16, x16_lo, w16, w16_lo, x32, slabs, total;
 };
-HeadLayout layout_for(int64_t plans, int64_t sub, int64_t rows, int64_t slab_cells, int32_t d, int32_t vocab, bool bf16,
+HeadLayout layout_for(int64_t plans, int64_t rows, int64_t slab_cells, int32_t d, int32_t vocab, bool bf16,
                       bool pairs, bool grad) {
   HeadLayout w = {};
   const bool wide = bf16 || pairs;
@@ -885,10 +877,10 @@ HeadLayout layout_for(int64_t plans, int64_t sub, int64_t rows, int64_t slab_cel
   // (the range ends where the targets' logits begin)
   at = align_up(at + sizeof(HeadRange), ALIGN);
   w.range = at - sizeof(HeadRange);
-  w.at_target = take((size_t)sub * (pairs ? 8 : 4));
-  w.logits = take(grad ? (size_t)sub * ldv * 4 : 0);
-  w.pairs = take(std::max(pair_cells(sub, d, vocab, wide) * 8, stream_pairs(std::min(sub, stream_rows(vocab)), vocab)));
-  w.off = take((size_t)sub * 8);
+  w.at_target = take((size_t)rows * (pairs ? 8 : 4));
+  w.logits = take(grad ? cells * 4 : 0);
+  w.pairs = take(std::max(pair_cells(rows, d, vocab, wide) * 8, stream_pairs(std::min(rows, stream_rows(vocab)), vocab)));
+  w.off = take((size_t)rows * 8);
   w.g = take(bf16 && grad ? 2 * cells * 2 : 0);
   w.hi = take(wide && grad ? cells * 2 : 0);
   w.lo = take(wide && grad ? cells * 2 : 0);
@@ -901,16 +893,15 @@ HeadLayout layout_for(int64_t plans, int64_t sub, int64_t rows, int64_t slab_cel
   w.total = at;
   return w;
 }
-// of all batches of at most T rows of one kind: the most plans, rows of a product and of a piece, slabs
+// of all batches of at most T rows of one kind: the most plans, rows of a piece, slabs
 size_t most_workspace(int64_t T, int32_t d, int32_t vocab, bool bf16, bool pairs, bool grad) {
   const bool wide = bf16 || pairs;
-  const int64_t most = most_rows(vocab, wide, grad), sub_most = std::min(most, most_sub(vocab, wide, grad));
-  const int64_t sub = std::min<int64_t>(padded_rows(T), sub_most), rows = std::min<int64_t>((int64_t)align_up((size_t)T, (size_t)sub), most);
-  const int64_t pieces = (T + most - 1) / most, plans = (T + sub_most - 1) / sub_most + (grad ? 2 * pieces : 0);
+  const int64_t most = most_rows(vocab, wide, grad), rows = std::min<int64_t>(padded_rows(T), most);
+  const int64_t plans = (T + most - 1) / most * (grad ? 3 : 1);
   const int64_t dx_rows = bf16 ? std::max(rows, std::min(2 * rows, 2 * STACK_ROWS)) : rows;
   const int64_t dw_parts = dw_most_parts(d, vocab, wide);
   const int64_t slabs = std::max(std::min(MAX_PARTS * dx_rows * d, std::max(SLAB_CELLS, dx_rows * d)), dw_parts > 1 ? dw_parts * vocab * d : 0);
-  return ALIGN + layout_for(plans, sub, rows, slabs, d, vocab, bf16, pairs, grad).total;
+  return ALIGN + layout_for(plans, rows, slabs, d, vocab, bf16, pairs, grad).total;
 }
 }  // namespace
 
@@ -935,9 +926,9 @@ hipError_t launch_head(modse_dtype dt, const HeadArgs& a, char* ws, hipStream_t 
     return dt == MODSE_F32 ? run_stream<float>(r, s) : run_stream<bf16_t>(r, s);
   }
   const HeadShape h = head_shape(a.T, a.d, a.vocab, dt, grad);
-  const int64_t products = h.products(), plans = products + (grad ? 2 * h.pieces : 0);
+  const int64_t plans = (int64_t)h.pieces * (grad ? 3 : 1);
   const int64_t slabs = std::max((int64_t)h.k_parts * h.dx_rows * h.d, h.w_split > 1 ? (int64_t)h.w_split * h.vocab * h.d : 0);
-  const HeadLayout w = layout_for(plans, h.sub, h.rows, slabs, h.d, h.vocab, h.bf16, h.pairs, grad);
+  const HeadLayout w = layout_for(plans, h.rows, slabs, h.d, h.vocab, h.bf16, h.pairs, grad);
   ws = reinterpret_cast<char*>(align_up(reinterpret_cast<size_t>(ws), ALIGN));
   auto floats = [&](size_t at) { return reinterpret_cast<float*>(ws + at); };
   auto halves = [&](size_t at) { return reinterpret_cast<f16_t*>(ws + at); };
@@ -956,32 +947,28 @@ hipError_t launch_head(modse_dtype dt, const HeadArgs& a, char* ws, hipStream_t 
   }
   auto tiles_of = [](int64_t m, int64_t n, TileShape t) { return tiles(m, n, t.bm); };
   hipError_t e = hipGetLastError();
-  // the logits of one product, their sums and (of gradients) G
-  auto product = [&](int64_t i) {
-    const int64_t t0 = i * h.sub, m = std::min<int64_t>(h.sub, h.T - t0), in_piece = t0 % h.rows;
-    const bool stream = h.T <= stream_rows(h.vocab) && products == 1;  // (only with gradients here)
-    if (h.pairs && in_piece == 0) {
+  // the logits of a piece, their sums and (of gradients) G
+  auto logits = [&](int64_t piece, int64_t t0, int64_t m) {
+    const bool stream = h.T <= stream_rows(h.vocab) && h.pieces == 1;  // (only with gradients here)
+    if (h.pairs) {
       int lanes = 64;
       while (lanes > 2 && lanes / 2 >= h.d / 8) lanes /= 2;
-      const int64_t rows = std::min<int64_t>(h.rows, h.T - t0);
-      hipLaunchKernelGGL(head_split_x_kernel, dim3((unsigned)((rows * lanes + 255) / 256)), dim3(256), 0, s,
-                         static_cast<const float*>(a.x) + t0 * h.d, a.targets + t0, (int)rows, h.d, h.vocab, (int)grad, range, b.x16, b.x16_lo,
-                         b.at_target + h.sub, h.sub);
+      hipLaunchKernelGGL(head_split_x_kernel, dim3((unsigned)((m * lanes + 255) / 256)), dim3(256), 0, s, static_cast<const float*>(a.x) + t0 * h.d,
+                         a.targets + t0, (int)m, h.d, h.vocab, (int)grad, range, b.x16, b.x16_lo, b.at_target + h.rows);
     }
     if (stream) {
       const HeadStreamArgs r = {a.x, a.W, a.targets, b.pairs, b.at_target, a.logp, nullptr, b.logits, b.off, range, (int32_t)m, h.d, h.vocab, h.ldv};
       e = h.bf16 ? run_stream<bf16_t>(r, s) : run_stream<float>(r, s);
     } else {
-      e = launch_grouped_gemm(dt, h.pairs ? EPI_LOGITS_PAIRS : EPI_LOGITS, h.logits_tile, b.plans + i, h.w_parts, 0,
+      e = launch_grouped_gemm(dt, h.pairs ? EPI_LOGITS_PAIRS : EPI_LOGITS, h.logits_tile, b.plans + piece, h.w_parts, 0,
                               h.logits_tile.bm < 256 ? GEMM_SPREAD_K : GEMM_STREAM_C, tiles_of(m, h.vocab, h.logits_tile) + h.w_parts * tiles_of(m, 1, h.logits_tile), s, LAYOUT_TN);
     }
     if (e != hipSuccess) return;
     const HeadRowsArgs r = {a.targets + t0, a.d_logp ? a.d_logp + t0 : nullptr, a.logp ? a.logp + t0 : nullptr, a.log_z ? a.log_z + t0 : nullptr,
-                            b.logits, b.pairs, b.at_target, b.off, a.dX && h.bf16 ? b.g + in_piece * h.ldv : nullptr,
-                            a.dX && h.bf16 ? b.g + (h.rows + in_piece) * h.ldv : nullptr,
-                            a.dW || h.pairs ? b.hi + in_piece * h.ldv : nullptr, a.dW || h.pairs ? b.lo + in_piece * h.ldv : nullptr,
-                            range, static_cast<const char*>(a.x) + (size_t)t0 * h.d * (h.bf16 ? 2 : 4), b.x16 + in_piece * h.d,
-                            a.dW && !h.wide ? b.x32 + in_piece * h.d : nullptr, (int32_t)m, h.vocab, h.ldv, h.sub, h.pair_cols(), h.d};
+                            b.logits, b.pairs, b.at_target, b.off, a.dX && h.bf16 ? b.g : nullptr, a.dX && h.bf16 ? b.g + (int64_t)h.rows * h.ldv : nullptr,
+                            a.dW || h.pairs ? b.hi : nullptr, a.dW || h.pairs ? b.lo : nullptr, range,
+                            static_cast<const char*>(a.x) + (size_t)t0 * h.d * (h.bf16 ? 2 : 4), b.x16, a.dW && !h.wide ? b.x32 : nullptr,
+                            (int32_t)m, h.vocab, h.ldv, h.rows, h.pair_cols(), h.d};
     if (!stream) hipLaunchKernelGGL(head_stats_kernel, dim3((unsigned)((m + 15) / 16)), dim3(1024), 0, s, r);
     if (grad) {
       const int64_t segs = (h.ldv + 2047) / 2048, copies = a.dW && h.bf16 ? (m * h.d + 2047) / 2048 : 0;
@@ -991,13 +978,11 @@ hipError_t launch_head(modse_dtype dt, const HeadArgs& a, char* ws, hipStream_t 
     }
     e = hipGetLastError();
   };
-  for (int64_t i = 0; i < products && e == hipSuccess; ++i) {
-    product(i);
-    const int64_t piece = i / h.subs;
-    if (e != hipSuccess || !grad || ((i + 1) % h.subs != 0 && i + 1 < products)) continue;
-    // a piece is whole
+  for (int64_t piece = 0; piece < h.pieces && e == hipSuccess; ++piece) {
     const int64_t t0 = piece * h.rows, m = std::min<int64_t>(h.rows, h.T - t0);
-    const GemmPlan* const p = b.plans + products + 2 * piece;
+    logits(piece, t0, m);
+    if (e != hipSuccess || !grad) continue;
+    const GemmPlan* const p = b.plans + h.pieces + 2 * piece;
     if (a.dW) {  // (before dX, which may lie in the buffer of x)
       const int accumulate = a.accumulate || piece > 0;
       e = launch_grouped_gemm(dt, h.pairs ? EPI_ROWS_PAIRS : EPI_ROWS_F32, h.dw_tile, p + 1, h.w_split, h.w_split > 1 ? 0 : accumulate, 0,

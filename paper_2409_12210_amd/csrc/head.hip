@@ -5,7 +5,7 @@
 //   G_tv = w_t (1[v = target_t] - e^(l_tv - log Z_t)),  dX = G W,  dW = G^T x
 //
 // The batch is taken in pieces of rows whose G fits a workspace that stops growing with the batch.  The products are those of the grouped GEMM kernels,
-// whose problem tables one launch makes for the whole call.  dX is a product over the whole vocabulary with few columns, so its
+// whose problem tables one launch makes for sixteen pieces.  dX is a product over the whole vocabulary with few columns, so its
 // sum is cut into parts that fill the chip; the parts are float32 slabs that a last launch adds up in order.
 //
 // The product of the logits leaves, for every row and 32 to 128 columns, their maximum and sum of exponentials, and the target's logit
@@ -44,6 +44,7 @@ constexpr int64_t W_PART = (int64_t)1 << 30;       // elements of W that one pro
 constexpr size_t ALIGN = 256;                      // of what is in the workspace, which itself may lie at any sixteen bytes
 constexpr int64_t SLAB_CELLS = (int64_t)1 << 26;   // values of all parts of dX together, unless one part has more
 constexpr int64_t STACK_ROWS = 128;                // of bf16 layers up to which the second numbers of G are rows of their own in the product of dX
+constexpr int PLAN_PIECES = 16;                    // of which the problem tables, 25 KB a product, are there at a time
 constexpr int MAX_PARTS = 128;                     // of dX, of dW (problems of a product: fewer than 192)
 static_assert(MAX_PARTS <= MODSE_MAX_PROBLEMS, "a problem for each");
 
@@ -187,7 +188,7 @@ typedef _Float16 f16_t;
 typedef f16_t f16x8 __attribute__((ext_vector_type(8)));
 
 struct HeadBufs {
-  GemmPlan* plans;   // logits of every piece, then dX and dW of every piece
+  GemmPlan* plans;   // logits of some pieces, then dX and dW of each of them
   float* logits;     // [rows, ldv]; float32 layers: then G
   float* pairs;      // [ceil(vocab / pair_cols)][rows] maximum and sum
   float* at_target;  // [rows] the target's logit, and behind them [rows] what undoes the scaling of a row of x (float32 by pairs)
@@ -208,7 +209,7 @@ struct HeadPlanArgs {
   const int32_t* targets;
   const float* d_logp;
   float* dW;
-  int32_t plans;
+  int32_t first, pieces, plans;  // pieces whose problems are made, the first of them
 };
 
 // Infinities and NaN count as 0: they stay what they are in the parts, and the other values keep theirs.
@@ -355,7 +356,7 @@ __global__ __launch_bounds__(256) void head_split_x_kernel(const float* x, const
 }
 
 // The problems of one product, by a block's first wave: of the logits, a block for each piece, then of dX and of dW, a block for each.
-// Blocks behind these look for the largest values.
+// Blocks behind these, of the call's first such launch, look for the largest values.
 __global__ __launch_bounds__(1024) void head_plan_kernel(HeadPlanArgs a) {
   __shared__ int s_tiles[MODSE_MAX_PROBLEMS];
   if ((int)blockIdx.x >= a.plans) {
@@ -364,9 +365,9 @@ __global__ __launch_bounds__(1024) void head_plan_kernel(HeadPlanArgs a) {
   }
   if (threadIdx.x >= 64) return;
   const HeadShape& h = a.h;
-  const int lane = threadIdx.x, behind = (int)blockIdx.x - h.pieces;
+  const int lane = threadIdx.x, behind = (int)blockIdx.x - a.pieces;
   const int which = behind < 0 ? 0 : 1 + behind % 2;
-  const int64_t t0 = (int64_t)(which == 0 ? (int)blockIdx.x : behind / 2) * h.rows;
+  const int64_t t0 = (int64_t)(a.first + (which == 0 ? (int)blockIdx.x : behind / 2)) * h.rows;
   const size_t es = h.bf16 ? 2 : 4;
   const int m = (int)min((int64_t)h.rows, h.T - t0);
   const char* const x = cadd(a.x, (size_t)t0 * h.d * es);
@@ -893,11 +894,11 @@ HeadLayout layout_for(int64_t plans, int64_t rows, int64_t slab_cells, int32_t d
   w.total = at;
   return w;
 }
-// of all batches of at most T rows of one kind: the most plans, rows of a piece, slabs
+// of all batches of at most T rows of one kind: the most tables, rows of a piece, slabs
 size_t most_workspace(int64_t T, int32_t d, int32_t vocab, bool bf16, bool pairs, bool grad) {
   const bool wide = bf16 || pairs;
   const int64_t most = most_rows(vocab, wide, grad), rows = std::min<int64_t>(padded_rows(T), most);
-  const int64_t plans = (T + most - 1) / most * (grad ? 3 : 1);
+  const int64_t plans = std::min<int64_t>((T + most - 1) / most, PLAN_PIECES) * (grad ? 3 : 1);
   const int64_t dx_rows = bf16 ? std::max(rows, std::min(2 * rows, 2 * STACK_ROWS)) : rows;
   const int64_t dw_parts = dw_most_parts(d, vocab, wide);
   const int64_t slabs = std::max(std::min(MAX_PARTS * dx_rows * d, std::max(SLAB_CELLS, dx_rows * d)), dw_parts > 1 ? dw_parts * vocab * d : 0);
@@ -926,7 +927,7 @@ hipError_t launch_head(modse_dtype dt, const HeadArgs& a, char* ws, hipStream_t 
     return dt == MODSE_F32 ? run_stream<float>(r, s) : run_stream<bf16_t>(r, s);
   }
   const HeadShape h = head_shape(a.T, a.d, a.vocab, dt, grad);
-  const int64_t plans = (int64_t)h.pieces * (grad ? 3 : 1);
+  const int64_t plans = (int64_t)std::min(h.pieces, PLAN_PIECES) * (grad ? 3 : 1);
   const int64_t slabs = std::max((int64_t)h.k_parts * h.dx_rows * h.d, h.w_split > 1 ? (int64_t)h.w_split * h.vocab * h.d : 0);
   const HeadLayout w = layout_for(plans, h.rows, slabs, h.d, h.vocab, h.bf16, h.pairs, grad);
   ws = reinterpret_cast<char*>(align_up(reinterpret_cast<size_t>(ws), ALIGN));
@@ -936,10 +937,15 @@ hipError_t launch_head(modse_dtype dt, const HeadArgs& a, char* ws, hipStream_t 
   const HeadBufs b = {reinterpret_cast<GemmPlan*>(ws), floats(w.logits), floats(w.pairs), floats(w.at_target), floats(w.off),
                       reinterpret_cast<bf16_t*>(ws + w.g), halves(w.hi), halves(w.lo), halves(w.x16), halves(w.x16_lo),
                       halves(w.w16), halves(w.w16_lo), floats(w.x32), range, floats(w.slabs)};
-  const HeadPlanArgs plan = {h, b, a.x, a.W, a.targets, a.d_logp, a.dW, (int32_t)plans};
   const int64_t looked_at = h.T * h.d + (h.pairs ? (int64_t)h.vocab * h.d : 0);
   const int64_t range_blocks = range ? std::min<int64_t>((looked_at + 32767) / 32768, RANGE_BLOCKS) : 0;
-  hipLaunchKernelGGL(head_plan_kernel, dim3((unsigned)(plans + range_blocks)), dim3(1024), 0, s, plan);
+  auto make_plans = [&](int first) {  // returns how many pieces they are of
+    const int n = std::min(h.pieces - first, PLAN_PIECES), tables = n * (grad ? 3 : 1);
+    const HeadPlanArgs plan = {h, b, a.x, a.W, a.targets, a.d_logp, a.dW, first, n, tables};
+    hipLaunchKernelGGL(head_plan_kernel, dim3((unsigned)(tables + (first == 0 ? range_blocks : 0))), dim3(1024), 0, s, plan);
+    return n;
+  };
+  int planned = make_plans(0);
   if (h.pairs) {
     const int64_t n = (int64_t)h.vocab * h.d;
     hipLaunchKernelGGL(head_split_w_kernel, dim3((unsigned)std::min<int64_t>((n + 2047) / 2048, 2048)), dim3(256), 0, s,
@@ -948,7 +954,7 @@ hipError_t launch_head(modse_dtype dt, const HeadArgs& a, char* ws, hipStream_t 
   auto tiles_of = [](int64_t m, int64_t n, TileShape t) { return tiles(m, n, t.bm); };
   hipError_t e = hipGetLastError();
   // the logits of a piece, their sums and (of gradients) G
-  auto logits = [&](int64_t piece, int64_t t0, int64_t m) {
+  auto logits = [&](const GemmPlan* plan, int64_t t0, int64_t m) {
     const bool stream = h.T <= stream_rows(h.vocab) && h.pieces == 1;  // (only with gradients here)
     if (h.pairs) {
       int lanes = 64;
@@ -960,7 +966,7 @@ hipError_t launch_head(modse_dtype dt, const HeadArgs& a, char* ws, hipStream_t 
       const HeadStreamArgs r = {a.x, a.W, a.targets, b.pairs, b.at_target, a.logp, nullptr, b.logits, b.off, range, (int32_t)m, h.d, h.vocab, h.ldv};
       e = h.bf16 ? run_stream<bf16_t>(r, s) : run_stream<float>(r, s);
     } else {
-      e = launch_grouped_gemm(dt, h.pairs ? EPI_LOGITS_PAIRS : EPI_LOGITS, h.logits_tile, b.plans + piece, h.w_parts, 0,
+      e = launch_grouped_gemm(dt, h.pairs ? EPI_LOGITS_PAIRS : EPI_LOGITS, h.logits_tile, plan, h.w_parts, 0,
                               h.logits_tile.bm < 256 ? GEMM_SPREAD_K : GEMM_STREAM_C, tiles_of(m, h.vocab, h.logits_tile) + h.w_parts * tiles_of(m, 1, h.logits_tile), s, LAYOUT_TN);
     }
     if (e != hipSuccess) return;
@@ -980,9 +986,11 @@ hipError_t launch_head(modse_dtype dt, const HeadArgs& a, char* ws, hipStream_t 
   };
   for (int64_t piece = 0; piece < h.pieces && e == hipSuccess; ++piece) {
     const int64_t t0 = piece * h.rows, m = std::min<int64_t>(h.rows, h.T - t0);
-    logits(piece, t0, m);
+    const int at = (int)(piece % PLAN_PIECES);
+    if (at == 0 && piece > 0) planned = make_plans((int)piece);
+    logits(b.plans + at, t0, m);
     if (e != hipSuccess || !grad) continue;
-    const GemmPlan* const p = b.plans + h.pieces + 2 * piece;
+    const GemmPlan* const p = b.plans + planned + 2 * at;
     if (a.dW) {  // (before dX, which may lie in the buffer of x)
       const int accumulate = a.accumulate || piece > 0;
       e = launch_grouped_gemm(dt, h.pairs ? EPI_ROWS_PAIRS : EPI_ROWS_F32, h.dw_tile, p + 1, h.w_split, h.w_split > 1 ? 0 : accumulate, 0,

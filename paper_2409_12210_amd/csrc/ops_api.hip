@@ -51,7 +51,6 @@ modse_status check_head(int64_t T, int32_t d, int32_t vocab, const modse_dtype& 
   const modse_status st = check_vocab(T, d, vocab, dtype);
   if (st != MODSE_OK) return st;
   if (d % 32) return MODSE_ERR_INVALID_ARG;
-  // (pieces of at least half the rows that they could have, three blocks for each)
   return T > (int64_t)1 << 24 ? MODSE_ERR_UNSUPPORTED : MODSE_OK;
 }
 struct EmbedLayout {

@@ -339,8 +339,7 @@ modse_status modse_embed_bwd(int64_t T, int32_t d_model, int32_t vocab, modse_dt
  * x, W, dX, dW and the workspace lie at addresses that are multiples of 16.
  * Float32 with more rows than a few hundred (as many as make that the faster way), and
  * vocab d_model up to 2^28: x and W are held in 22 bits each, x down to 2^-39 of the
- * largest value of its row (modse_head_bwd: of all rows with a target), W down to 2^-39
- * of its largest; what is smaller may be lost.  The workspace then also holds the parts
+ * largest value of its row, W down to 2^-39 of its largest; what is smaller may be lost.  The workspace then also holds the parts
  * of W, 4 vocab d_model bytes.  An infinity or NaN in a row of x makes that row's logp
  * NaN (and its row of dX, and dW), one in W every row's. */
 modse_status modse_head_workspace_size(int64_t T, int32_t d_model, int32_t vocab, modse_dtype dtype, int which, size_t* bytes);
@@ -354,10 +353,11 @@ modse_status modse_head_fwd(int64_t T, int32_t d_model, int32_t vocab, modse_dty
  *   dX      [T, d_model] of `dtype` out, or NULL; it may lie in the buffer of x
  *   dW      [vocab, d_model] float32 out, or NULL: overwritten, or added to with
  *           accumulate = 1
- * In bf16 the gradient of the logits is held in 16 bits for dX.  For dW it is held in
- * 22 bits, down to 2^-39 of the largest |d_logp|, and x exactly, down to 2^-39 of the
- * largest |x| (both of rows with a target): what is smaller may be lost.  So it is for
- * dX and dW in float32 where x and W are held in 22 bits.
+ * In bf16 the gradient of the logits is held in 16 bits for dX.  For dW, and in float32
+ * where x and W are held in 22 bits, it is held in 22 bits, down to 2^-39 of the row's
+ * largest, |d_logp_t| (1 - p_t) of its target's p_t; what is smaller may be lost.  In the
+ * sums of dW a row counts down to 2^-39 of the largest |d_logp_t| (1 - p_t) max|x_t| of
+ * all rows with a target.  No row of logp or dX depends on another row.
  * Workspace sizes: MODSE_WS_FWD and MODSE_WS_BWD for the two calls.  Sums run in an
  * order that the sizes alone fix, the two calls' in orders of their own.  T == 0
  * leaves dW as it is. */

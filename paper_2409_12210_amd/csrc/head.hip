@@ -12,8 +12,8 @@
 // (EPI_LOGITS); one launch joins them.  Without gradients no logit is stored.  With gradients the logits are, in float32, and another
 // launch turns them into G.
 //
-// float32 from some hundred rows on: x, W and G are held as the sums of two float16 matrices, hi + lo, times powers of
-// two that bring the largest value below 2^15.  Three products of float16 matrices, hi hi' + hi lo' + lo hi', in one accumulator leave
+// float32 from some hundred rows on: x, W and G are held as the sums of two float16 matrices, hi + lo, times powers of two (see HeadRange)
+// that bring the largest value below 2^15.  Three products of float16 matrices, hi hi' + hi lo' + lo hi', in one accumulator leave
 // out 2^-22 of a product; they take 3 of the 16-bit matrix rate where float32 instructions take 16 (1021 x 256 x 50257 with gradients:
 // 435 us in place of 731).  Fewer rows, or a W of more than 2^28 elements: products in float32, and G in the place of the logits.
 //
@@ -23,9 +23,9 @@
 // dX of a bf16 layer takes G as the sum of two bf16 numbers, which hold 16 bits, in two passes over W; what they lose lies below the rounding
 // of the result.  (One number, with what it loses of the target's entry put back in float32: 2 T V d operations less, but where another token
 // has most of the probability an error of 2.0e-3 of the norm, of which the rounding of the result is 1.65e-3.)  Up to 128 rows, which fill half a
-// tile, the second numbers are rows of their own.  dW is float32, and takes G as the sum of two float16 numbers, hi + lo, which hold 22 bits, times float16 copies of the rows of x: both times powers of two that follow the largest |x| and the largest
-// |d_logp| of the call, so that what is rounded or lost is below 2^-39 of the largest product.  (Two bf16 numbers, 16 bits, left an
-// error of 2.7e-6 of dW where float32 products have 0.7e-6 to 2e-6, and need no third copy of G; the rest takes as long.)
+// tile, the second numbers are rows of their own.  dW is float32, and takes G as the sum of two float16 numbers, hi + lo, which hold 22
+// bits, times float16 copies of the rows of x, so that what is rounded or lost lies below 2^-39 of the largest product of a row's two factors.
+// (Two bf16 numbers, 16 bits, left an error of 2.7e-6 of dW where float32 products have 0.7e-6 to 2e-6; the rest takes as long.)
 #include <cmath>
 #include <cstddef>
 
@@ -168,21 +168,38 @@ HeadShape head_shape(int64_t T, int32_t d, int32_t vocab, modse_dtype dt, bool g
   return h;
 }
 
-// The largest finite |x| and |d_logp| of the rows with a target and the largest |W| of a call, as the bits of floats: by block, joined by a
-// later launch.  (Bf16 layers need no |W|; scoring scales each row of x by itself.)
+// Float16 numbers hold 2^15 to 2^-25, so what is taken in two of them goes by powers of two, of which the results are freed again.
+// A row of x: by its largest value, for its logits (no row touches another).  W: by its largest value.  A row of G: by the most that an entry of it can be,
+// |w| (1 - p_target), for dX and dW.  dW sums over the rows, so there the rows of x make up for those of G: row t of G times 2^r_t, row t of x
+// times 2^(C - r_t), with one C from the largest |w_t| (1 - p_target) max|x_t| so far in the call.
 constexpr int RANGE_BLOCKS = 512;
+constexpr int NO_ROW = -(1 << 20);
+constexpr int MOST_LINES = 64;  // (2048 rows that all change one number took 15 us)
 struct HeadRange {
-  uint32_t x_of[RANGE_BLOCKS], w_of[RANGE_BLOCKS], d_logp_of[RANGE_BLOCKS];
+  uint32_t w_of[RANGE_BLOCKS];  // the largest finite |W|, as the bits of a float, by block
   int32_t blocks;
-  uint32_t x, w, d_logp;
-  // What undoes the scaling by two of them: the smaller factor first, so that no product on the way overflows where the result does not.
-  float undo_dx[2], undo_dw[2], pad[3];
+  int32_t w_exponent;  // W is taken times 2 to it
+  float undo_dw[2];    // 2^-C, in two factors
+  int32_t most[MOST_LINES][32];  // [i][0]: exponent of the largest |w_t| (1 - p_target) max|x_t| so far of every 64th row, or NO_ROW
+  float pad[7];
   float undo_w;  // right before the targets' logits (EPI_LOGITS_PAIRS)
 };
 static_assert(sizeof(HeadRange) == offsetof(HeadRange, undo_w) + 4 && sizeof(HeadRange) % 16 == 0, "laid out up to the targets' logits");
+// floor(log2) of a float of so many bits; -127 of what is smaller than all normal ones
+__device__ __forceinline__ int exponent_of(uint32_t bits) { return (int)(bits >> 23 & 255) - 127; }
 // the power of two that brings values of at most this size below 2^15
-__device__ __forceinline__ int scale_exponent(uint32_t bits) { return min(14 - ((int)(bits >> 23 & 255) - 127), 120); }
+__device__ __forceinline__ int scale_exponent(uint32_t bits) { return min(14 - exponent_of(bits), 120); }
 __device__ __forceinline__ float power_of_two(int e) { return __builtin_bit_cast(float, (uint32_t)(e + 127) << 23); }
+// Times 2^e, any e: of NaN and infinities what they are, 0 below the smallest number.
+__device__ __forceinline__ float times_2(float x, int e) { return __builtin_amdgcn_ldexpf(x, e); }
+// C.  An entry of G lies below 2^(e_t + 2), e_t as in row_exponent, and is taken times 2^(13 - e_t); one of x, below 2^(f_t + 1), times 2^(C - 13 + e_t):
+// with C = 27 - max(e_t + f_t) both lie below 2^15.  (Where C would be more than 250, dW lies below the smallest float.)
+__device__ __forceinline__ int common_exponent(const HeadRange* range) {  // (by a wave)
+  int most = range->most[threadIdx.x % MOST_LINES][0];
+#pragma unroll
+  for (int o = 32; o; o >>= 1) most = max(most, __shfl_xor(most, o, 64));
+  return most == NO_ROW ? 0 : min(27 - most, 250);
+}
 
 typedef _Float16 f16_t;
 typedef f16_t f16x8 __attribute__((ext_vector_type(8)));
@@ -195,7 +212,8 @@ struct HeadBufs {
   float* off;        // [rows][2] the row's maximum and log2 of its sum
   bf16_t* g;         // [2 rows, ldv] G, and behind its rows what bf16 lacks of them
   f16_t *hi, *lo;    // [rows, ldv] G in two parts, scaled
-  f16_t *x16, *x16_lo;   // [rows, d] x in the same way; x16_lo: float32 layers
+  f16_t *x16, *x16_lo;   // [rows, d] x in the same way, for dW; x16_lo: float32 layers, there for the logits before
+  int32_t* exponents;    // [rows] rows of G are taken times 2 to it
   f16_t *w16, *w16_lo;   // [vocab, d] W, float32 layers
   float* x32;        // [rows, d] x, zeros in rows without a target: float32 layers that take no pairs
   HeadRange* range;
@@ -239,75 +257,41 @@ __device__ __forceinline__ uint32_t wave_most(uint32_t v) {
   for (int o = 32; o; o >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, o, 64));
   return v;
 }
+// float32 by pairs: W's largest value
 __device__ __forceinline__ void range_block(const HeadPlanArgs& a, int block, int blocks) {
-  __shared__ uint32_t s_most[3][16];
+  __shared__ uint32_t s_most[16];
   const int64_t first = (int64_t)block * 1024 + threadIdx.x, step = (int64_t)blocks * 1024;
-  const bool bf16 = a.h.bf16;
-  uint32_t most[3] = {0, bf16 ? 0 : largest(static_cast<const u32x4*>(a.W), (int64_t)a.h.vocab * a.h.d / 4, false, first, step), 0};
-  if (a.d_logp) {
-    const int vectors = bf16 ? a.h.d / 8 : a.h.d / 4, lanes = lanes_of(vectors), lane = threadIdx.x & (lanes - 1);
-    for (int64_t t = first / lanes; t < a.h.T; t += step / lanes) {
-      const int32_t target = a.targets[t];
-      if (target < 0 || target >= a.h.vocab) continue;
-      most[0] = max(most[0], largest(static_cast<const u32x4*>(a.x) + t * vectors, vectors, bf16, lane, lanes));
-      most[2] = max(most[2], finite(__builtin_bit_cast(uint32_t, a.d_logp[t])));
-    }
-  }
-#pragma unroll
-  for (int k = 0; k < 3; ++k) {
-    most[k] = wave_most(most[k]);
-    if ((threadIdx.x & 63) == 0) s_most[k][threadIdx.x >> 6] = most[k];
-  }
+  uint32_t most = wave_most(largest(static_cast<const u32x4*>(a.W), (int64_t)a.h.vocab * a.h.d / 4, false, first, step));
+  if ((threadIdx.x & 63) == 0) s_most[threadIdx.x >> 6] = most;
   __syncthreads();
   if (threadIdx.x > 0) return;
-#pragma unroll
-  for (int k = 0; k < 3; ++k)
-    for (int w = 1; w < 16; ++w) most[k] = max(most[k], s_most[k][w]);
-  a.b.range->x_of[block] = most[0];
-  a.b.range->w_of[block] = most[1];
-  a.b.range->d_logp_of[block] = most[2];
+  for (int w = 1; w < 16; ++w) most = max(most, s_most[w]);
+  a.b.range->w_of[block] = most;
   if (block == 0) a.b.range->blocks = blocks;
 }
-// One wave joins them.  (Whichever block does it, it writes the same.)
-__device__ __forceinline__ void join_range(HeadRange* r) {
-  const int lane = threadIdx.x & 63, blocks = r->blocks;
-  uint32_t x = 0, w = 0, g = 0;
-#pragma unroll
-  for (int i = 0; i < RANGE_BLOCKS / 64; ++i)
-    if (i * 64 + lane < blocks) {
-      x = max(x, r->x_of[i * 64 + lane]);
-      w = max(w, r->w_of[i * 64 + lane]);
-      g = max(g, r->d_logp_of[i * 64 + lane]);
-    }
-  x = wave_most(x);
-  w = wave_most(w);
-  g = wave_most(g);
-  if (lane == 0) {
-    r->x = x;
-    r->w = w;
-    r->d_logp = g;
-    const float ux = power_of_two(-scale_exponent(x)), uw = power_of_two(-scale_exponent(w)), ug = power_of_two(-scale_exponent(g));
-    r->undo_w = uw;
-    r->undo_dx[0] = fminf(ug, uw);
-    r->undo_dx[1] = fmaxf(ug, uw);
-    r->undo_dw[0] = fminf(ug, ux);
-    r->undo_dw[1] = fmaxf(ug, ux);
-  }
+// What a row's G and x are taken times, once its statistics are there: by the first wave of those that call it.  `largest_x`: of the row's finite values.
+// (1 - p as it is computed, of a p that may be rounded to 1.)  Rows without a gradient have no part in C, and their copies of x are 0.
+__device__ __forceinline__ int row_exponent(HeadRange* range, int row, float w, float p, uint32_t largest_x) {
+  const uint32_t size = __builtin_bit_cast(uint32_t, w) & 0x7fffffffu;
+  if (size == 0 || size >= 0x7f800000u) return -NO_ROW;
+  const int e = exponent_of(size) + exponent_of(__builtin_bit_cast(uint32_t, fmaxf(1.f - p, 0x1p-23f)));
+  atomicMax(&range->most[row % MOST_LINES][0], e + exponent_of(largest_x));  // (the order does not matter)
+  return 13 - e;
 }
 
 // float32 by pairs: eight elements in two parts
-__device__ __forceinline__ void put_parts(const f32x4 (&v)[2], float scale, f16_t* hi, f16_t* lo) {
+__device__ __forceinline__ void put_parts(const f32x4 (&v)[2], int exponent, f16_t* hi, f16_t* lo) {
   f16x8 h, l;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    const float x = v[e >> 2][e & 3] * scale;
+    const float x = times_2(v[e >> 2][e & 3], exponent);
     h[e] = (f16_t)x;
     l[e] = (f16_t)(x - (float)h[e]);
   }
   *reinterpret_cast<f16x8*>(hi) = h;
   *reinterpret_cast<f16x8*>(lo) = l;
 }
-// W, n elements (a multiple of 16).  Every block joins the largest values for itself, the first one all of them.
+// W, n elements (a multiple of 16).  Every block joins the largest values for itself.
 __global__ __launch_bounds__(256) void head_split_w_kernel(const float* W, int64_t n, f16_t* hi, f16_t* lo, HeadRange* range) {
   __shared__ uint32_t s_most;
   if (threadIdx.x < 64) {
@@ -315,48 +299,41 @@ __global__ __launch_bounds__(256) void head_split_w_kernel(const float* W, int64
     uint32_t most = 0;
     for (int i = lane; i < blocks; i += 64) most = max(most, range->w_of[i]);
     most = wave_most(most);
-    if (lane == 0) s_most = most;
-    if (blockIdx.x == 0) join_range(range);
+    if (lane == 0) {
+      s_most = most;
+      if (blockIdx.x == 0) {
+        range->w_exponent = scale_exponent(most);
+        range->undo_w = power_of_two(-scale_exponent(most));
+      }
+    }
   }
   __syncthreads();
-  const float scale = power_of_two(scale_exponent(s_most));
+  const int exponent = scale_exponent(s_most);
   const int64_t step = (int64_t)gridDim.x * 2048;
   for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8; i < n; i += step) {
     const f32x4 v[2] = {__builtin_nontemporal_load(reinterpret_cast<const f32x4*>(W + i)),
                         __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(W + i + 4))};
-    put_parts(v, scale, hi + i, lo + i);
+    put_parts(v, exponent, hi + i, lo + i);
   }
 }
-// Rows of x, some lanes of a wave each.  Scoring: each by its own largest value, so that what stands in one row (one that pads the batch,
-// say) does not touch another.  Gradients, whose sum for dW runs over rows: by that of all rows with a target, and zeros for the others.
-__global__ __launch_bounds__(256) void head_split_x_kernel(const float* x, const int32_t* targets, int rows, int d, int vocab, int grad,
-                                                           const HeadRange* range, f16_t* hi, f16_t* lo, float* undo) {
+// Rows of x, some lanes of a wave each, by their own largest values.
+__global__ __launch_bounds__(256) void head_split_x_kernel(const float* x, int rows, int d, f16_t* hi, f16_t* lo, float* undo) {
   const int lanes = lanes_of(d / 8), lane = threadIdx.x & (lanes - 1);
   const int64_t row = ((int64_t)blockIdx.x * 256 + threadIdx.x) / lanes;
   if (row >= rows) return;
   const int64_t at = row * d;
-  uint32_t most = 0;
-  if (grad) {
-    most = range->x;
-  } else {
-    most = largest(reinterpret_cast<const u32x4*>(x + at), d / 4, false, lane, lanes);
-    for (int o = lanes / 2; o; o >>= 1) most = max(most, (uint32_t)__shfl_xor((int)most, o, 64));
-  }
+  uint32_t most = largest(reinterpret_cast<const u32x4*>(x + at), d / 4, false, lane, lanes);
+  for (int o = lanes / 2; o; o >>= 1) most = max(most, (uint32_t)__shfl_xor((int)most, o, 64));
   const int e = scale_exponent(most);
   if (lane == 0) undo[row] = power_of_two(-e);
-  const bool there = !grad || (targets[row] >= 0 && targets[row] < vocab);
   for (int c = lane * 8; c < d; c += lanes * 8) {
-    f32x4 v[2] = {};
-    if (there) {
-      v[0] = *reinterpret_cast<const f32x4*>(x + at + c);
-      v[1] = *reinterpret_cast<const f32x4*>(x + at + c + 4);
-    }
-    put_parts(v, power_of_two(e), hi + at + c, lo + at + c);
+    const f32x4 v[2] = {*reinterpret_cast<const f32x4*>(x + at + c), *reinterpret_cast<const f32x4*>(x + at + c + 4)};
+    put_parts(v, e, hi + at + c, lo + at + c);
   }
 }
 
 // The problems of one product, by a block's first wave: of the logits, a block for each piece, then of dX and of dW, a block for each.
-// Blocks behind these, of the call's first such launch, look for the largest values.
+// Blocks behind these, of the call's first such launch, look for W's largest value.
 __global__ __launch_bounds__(1024) void head_plan_kernel(HeadPlanArgs a) {
   __shared__ int s_tiles[MODSE_MAX_PROBLEMS];
   if ((int)blockIdx.x >= a.plans) {
@@ -365,6 +342,7 @@ __global__ __launch_bounds__(1024) void head_plan_kernel(HeadPlanArgs a) {
   }
   if (threadIdx.x >= 64) return;
   const HeadShape& h = a.h;
+  if (a.first == 0 && blockIdx.x == 0 && a.b.range) a.b.range->most[threadIdx.x][0] = NO_ROW;
   const int lane = threadIdx.x, behind = (int)blockIdx.x - a.pieces;
   const int which = behind < 0 ? 0 : 1 + behind % 2;
   const int64_t t0 = (int64_t)(a.first + (which == 0 ? (int)blockIdx.x : behind / 2)) * h.rows;
@@ -444,18 +422,26 @@ struct HeadRowsArgs {
   float* off;
   bf16_t *g, *g_rest;      // of the product's first row; null where there is no dX
   f16_t *hi, *lo;          // null where there is no dW
-  HeadRange* range;
+  HeadRange* range;        // (16-bit products of gradients) or null
+  int32_t* exponents;
   const void* x;           // of the product's first row, and their copies for dW, with zeros in rows without a target
-  f16_t* x16;
+  f16_t *x16, *x16_lo;     // x16_lo: null of bf16 layers
   float* x32;              // (float32 layers) null where there is no dW
   int32_t rows, vocab, ldv, pair_rows, pair_cols, d;
 };
-__device__ __forceinline__ float row_weight(const HeadRowsArgs& a, int row, int32_t target) {
-  return target < 0 ? 0.f : target >= a.vocab ? __builtin_nanf("") : a.d_logp[row];
+__device__ __forceinline__ float row_weight(int32_t target, int vocab, const float* d_logp) {
+  return target < 0 ? 0.f : target >= vocab ? __builtin_nanf("") : *d_logp;
+}
+__device__ __forceinline__ uint32_t row_largest(const void* x, int64_t row, int d, bool bf16) {  // (by a wave)
+  const int vectors = bf16 ? d / 8 : d / 4;
+  return wave_most(largest(static_cast<const u32x4*>(x) + row * vectors, vectors, bf16, threadIdx.x & 63, 64));
 }
 // (by maximum and sum, not by log Z: of a row that is all but sure 1 - p is what counts, and log Z is rounded at the size of the logits)
+__device__ __forceinline__ float probability(float logit, float top, float log2_sum) {
+  return __builtin_amdgcn_exp2f(fmaf(logit - top, LOG2E, -log2_sum));
+}
 __device__ __forceinline__ float grad_of(float logit, float top, float log2_sum, float w, int32_t target, int c, int vocab) {
-  const float p = __builtin_amdgcn_exp2f(fmaf(logit - top, LOG2E, -log2_sum));
+  const float p = probability(logit, top, log2_sum);
   return c >= vocab || target < 0 ? 0.f : c == target ? w * (1.f - p) : -w * p;
 }
 __device__ __forceinline__ void put_row(float* logp, float* log_z, int32_t target, int vocab, float at_target, float top, float log_sum) {
@@ -470,6 +456,7 @@ __device__ __forceinline__ void put_row(const HeadRowsArgs& a, int row, int32_t 
 // kept a call of 128 rows x 50257 waiting for two blocks: 42 us in place of 56.)
 __global__ __launch_bounds__(1024) void head_stats_kernel(HeadRowsArgs a) {
   __shared__ float s_m[64][16], s_s[64][16];
+  __shared__ uint32_t s_x[16];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, quarter = threadIdx.x >> 4;
   const int row = blockIdx.x * 16 + (lane & 15), n = (a.vocab + a.pair_cols - 1) / a.pair_cols;
   constexpr int AHEAD = 4;
@@ -493,7 +480,10 @@ __global__ __launch_bounds__(1024) void head_stats_kernel(HeadRowsArgs a) {
   }
   s_m[quarter][lane & 15] = m;
   s_s[quarter][lane & 15] = s;
-  if (a.range && wave == 15) join_range(a.range);
+  if (a.range && blockIdx.x * 16 + wave < a.rows) {  // (a row a wave)
+    const uint32_t most = row_largest(a.x, blockIdx.x * 16 + wave, a.d, a.x16_lo == nullptr);
+    if (lane == 0) s_x[wave] = most;
+  }
   __syncthreads();
   if (wave > 0) return;
   // (a quarter of this wave joins sixteen of the sums)
@@ -508,30 +498,49 @@ __global__ __launch_bounds__(1024) void head_stats_kernel(HeadRowsArgs a) {
   sum += __shfl_xor(sum, 32, 64);
   if (lane >= 16 || row >= a.rows) return;
   const float log2_sum = __builtin_amdgcn_logf(sum), log_sum = log2_sum * LN2;
-  put_row(a, row, a.targets[row], a.at_target[row], top, log_sum);
+  const int32_t target = a.targets[row];
+  put_row(a, row, target, a.at_target[row], top, log_sum);
   a.off[2 * row] = top;
   a.off[2 * row + 1] = log2_sum;
+  if (a.range)
+    a.exponents[row] = row_exponent(a.range, row, row_weight(target, a.vocab, a.d_logp + row), probability(a.at_target[row], top, log2_sum), s_x[lane]);
 }
 
 // 16-bit products: G of a row's 2048 columns, in two bf16 numbers for dX of bf16 layers, in two float16 ones for what else there is.  Columns
-// behind the vocabulary become zeros.  Blocks behind the rows' make the float16 copies of x of bf16 layers, 2048 values each.
+// behind the vocabulary become zeros.  Blocks behind the rows' make the float16 copies of x, 2048 values each.
 __global__ __launch_bounds__(256) void head_grad_kernel(HeadRowsArgs a, int segs) {
   if ((int)blockIdx.x >= a.rows * segs) {
     const int64_t i = (int64_t)(blockIdx.x - a.rows * segs) * 2048 + threadIdx.x * 8;
+    const int common = common_exponent(a.range);
     if (i >= (int64_t)a.rows * a.d) return;
-    const float scale = power_of_two(scale_exponent(a.range->x));
-    const int32_t target = a.targets[(uint32_t)i / (uint32_t)a.d];
-    const bf16x8 v = *reinterpret_cast<const bf16x8*>(static_cast<const bf16_t*>(a.x) + i);
-    f16x8 o;
+    const int row = (int)((uint64_t)i / (uint32_t)a.d), e = common - a.exponents[row];
+    const int32_t target = a.targets[row];
+    const bool there = target >= 0 && target < a.vocab;
+    if (i == 0) {
+      a.range->undo_dw[0] = power_of_two(-common / 2);
+      a.range->undo_dw[1] = power_of_two(-common - -common / 2);
+    }
+    if (a.x16_lo) {
+      f32x4 v[2] = {};
+      if (there) {
+        v[0] = *reinterpret_cast<const f32x4*>(static_cast<const float*>(a.x) + i);
+        v[1] = *reinterpret_cast<const f32x4*>(static_cast<const float*>(a.x) + i + 4);
+      }
+      put_parts(v, e, a.x16 + i, a.x16_lo + i);
+    } else {
+      const bf16x8 v = *reinterpret_cast<const bf16x8*>(static_cast<const bf16_t*>(a.x) + i);
+      f16x8 o;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) o[k] = target >= 0 && target < a.vocab ? (f16_t)((float)v[k] * scale) : (f16_t)0.f;
-    *reinterpret_cast<f16x8*>(a.x16 + i) = o;
+      for (int k = 0; k < 8; ++k) o[k] = there ? (f16_t)times_2((float)v[k], e) : (f16_t)0.f;
+      *reinterpret_cast<f16x8*>(a.x16 + i) = o;
+    }
     return;
   }
   const int row = blockIdx.x / segs, c = (blockIdx.x - row * segs) * 2048 + threadIdx.x * 8;
   if (c >= a.ldv) return;
   const int32_t target = a.targets[row];
-  const float top = a.off[2 * row], log2_sum = a.off[2 * row + 1], w = row_weight(a, row, target), scale = power_of_two(scale_exponent(a.range->d_logp));
+  const float top = a.off[2 * row], log2_sum = a.off[2 * row + 1], w = row_weight(target, a.vocab, a.d_logp + row);
+  const int exponent = a.exponents[row];
   const int64_t at = (int64_t)row * a.ldv + c;
   const f32x4 v[2] = {__builtin_nontemporal_load(reinterpret_cast<const f32x4*>(a.logits + at)),  // (read once: 473 us in place of 498)
                       __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(a.logits + at + 4))};
@@ -539,7 +548,7 @@ __global__ __launch_bounds__(256) void head_grad_kernel(HeadRowsArgs a, int segs
   f16x8 hi, lo;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    const float x = grad_of(v[e >> 2][e & 3], top, log2_sum, w, target, c + e, a.vocab), scaled = x * scale;
+    const float x = grad_of(v[e >> 2][e & 3], top, log2_sum, w, target, c + e, a.vocab), scaled = times_2(x, exponent);
     g[e] = (bf16_t)x;
     rest[e] = (bf16_t)(x - (float)g[e]);
     hi[e] = (f16_t)scaled;
@@ -559,7 +568,7 @@ __global__ __launch_bounds__(256) void head_grad_kernel(HeadRowsArgs a, int segs
 __global__ __launch_bounds__(256) void head_grad_f32_kernel(HeadRowsArgs a, int segs) {
   const int t = blockIdx.x / segs, c0 = (blockIdx.x - t * segs) * 2048 + threadIdx.x * 4;
   const int32_t target = a.targets[t];
-  const float top = a.off[2 * t], log2_sum = a.off[2 * t + 1], w = row_weight(a, t, target);
+  const float top = a.off[2 * t], log2_sum = a.off[2 * t + 1], w = row_weight(target, a.vocab, a.d_logp + t);
   float* const row = a.logits + (int64_t)t * a.ldv;
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
@@ -581,7 +590,8 @@ __global__ __launch_bounds__(256) void head_grad_f32_kernel(HeadRowsArgs a, int 
 // waves share out (24 x 256, 128 parts: 4.9 us in place of 8.7; twice the parts, 64 rows: 6.9 in place of 14.6).
 struct HeadJoinArgs {
   const float* slabs;
-  const float* undo;       // factors of the slabs, or null
+  const int32_t* exponents;  // of G's rows, and of W, by which the slabs are too large; or null
+  const HeadRange* range;
   int64_t stride, rest;    // from part to part; to the rows of G's second numbers, or 0
   int32_t parts, d;
 };
@@ -616,7 +626,11 @@ __global__ __launch_bounds__(256) void head_join_kernel(HeadJoinArgs a, T* dX) {
 #pragma unroll
     for (int w = 1; w < 4; ++w) s += s_part[w][lane];
   }
-  if (a.undo) s = s * a.undo[0] * a.undo[1];
+  if (a.exponents) {
+    const int by = -a.exponents[row] - a.range->w_exponent;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) s[e] = times_2(s[e], by);
+  }
 #pragma unroll
   for (int e = 0; e < 4; ++e) dX[i + e] = (T)s[e];
 }
@@ -661,7 +675,9 @@ struct HeadStreamArgs {
   float *logp, *log_z;
   float* logits;     // [T, ldv] or null
   float* off;        // [T][2] maximum and log2 of the sum, or null
-  HeadRange* range;  // to join, or null
+  HeadRange* range;  // (16-bit products of gradients) or null, and what it needs
+  int32_t* exponents;
+  const float* d_logp;
   int32_t T, d, vocab, ldv;
 };
 
@@ -802,8 +818,9 @@ __global__ __launch_bounds__(256, 2) void head_stream_kernel(HeadStreamArgs a) {
 }
 
 // A block joins the pairs of one row.
-__global__ __launch_bounds__(1024) void head_stream_join_kernel(HeadStreamArgs a) {
+__global__ __launch_bounds__(1024) void head_stream_join_kernel(HeadStreamArgs a, bool bf16) {
   __shared__ float s_m[16], s_s[16];
+  __shared__ uint32_t s_x;
   constexpr int AHEAD = 4;
   typedef float f32x2 __attribute__((ext_vector_type(2)));
   const int t = blockIdx.x, n = (a.vocab + STREAM_W - 1) / STREAM_W, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -828,18 +845,23 @@ __global__ __launch_bounds__(1024) void head_stream_join_kernel(HeadStreamArgs a
     s_m[wave] = wm;
     s_s[wave] = s;
   }
-  if (a.range && t == 0 && wave == 15) join_range(a.range);
+  if (a.range && wave == 15) {
+    const uint32_t most = row_largest(a.x, t, a.d, bf16);
+    if (lane == 0) s_x = most;
+  }
   __syncthreads();
   if (threadIdx.x > 0) return;
   float top = s_m[0], sum = 0.f;
   for (int w = 1; w < 16; ++w) top = fmaxf(top, s_m[w]);
   for (int w = 0; w < 16; ++w) sum += s_s[w] * __builtin_amdgcn_exp2f((s_m[w] - top) * LOG2E);
   const float log2_sum = __builtin_amdgcn_logf(sum), log_sum = log2_sum * LN2;
-  put_row(a.logp ? a.logp + t : nullptr, a.log_z ? a.log_z + t : nullptr, a.targets[t], a.vocab, a.at_target[t], top, log_sum);
+  const int32_t target = a.targets[t];
+  put_row(a.logp ? a.logp + t : nullptr, a.log_z ? a.log_z + t : nullptr, target, a.vocab, a.at_target[t], top, log_sum);
   if (a.off) {
     a.off[2 * t] = top;
     a.off[2 * t + 1] = log2_sum;
   }
+  if (a.range) a.exponents[t] = row_exponent(a.range, t, row_weight(target, a.vocab, a.d_logp + t), probability(a.at_target[t], top, log2_sum), s_x);
 }
 
 template <typename T>
@@ -854,14 +876,14 @@ hipError_t run_stream(const HeadStreamArgs& a, hipStream_t s) {
   if (nt == 1) hipLaunchKernelGGL((head_stream_kernel<T, 1>), grid, block, 0, s, a);
   else if (nt == 2) hipLaunchKernelGGL((head_stream_kernel<T, 2>), grid, block, 0, s, a);
   else hipLaunchKernelGGL((head_stream_kernel<T, 4>), grid, block, 0, s, a);
-  if (a.logp || a.log_z || a.off) hipLaunchKernelGGL(head_stream_join_kernel, dim3((unsigned)a.T), dim3(1024), 0, s, a);
+  if (a.logp || a.log_z || a.off) hipLaunchKernelGGL(head_stream_join_kernel, dim3((unsigned)a.T), dim3(1024), 0, s, a, sizeof(T) == 2);
   return hipGetLastError();
 }
 size_t stream_pairs(int64_t T, int32_t vocab) { return (size_t)T * ((vocab + STREAM_W - 1) / STREAM_W) * 8; }
 size_t stream_workspace(int64_t T, int32_t vocab) { return ALIGN + align_up(stream_pairs(T, vocab), ALIGN) + (size_t)T * 4; }
 
 struct HeadLayout {
-  size_t range, logits, pairs, at_target, off, g, hi, lo, x16, x16_lo, w16, w16_lo, x32, slabs, total;
+  size_t range, logits, pairs, at_target, off, exponents, g, hi, lo, x16, x16_lo, w16, w16_lo, x32, slabs, total;
 };
 HeadLayout layout_for(int64_t plans, int64_t rows, int64_t slab_cells, int32_t d, int32_t vocab, bool bf16,
                       bool pairs, bool grad) {
@@ -882,6 +904,7 @@ HeadLayout layout_for(int64_t plans, int64_t rows, int64_t slab_cells, int32_t d
   w.logits = take(grad ? cells * 4 : 0);
   w.pairs = take(std::max(pair_cells(rows, d, vocab, wide) * 8, stream_pairs(std::min(rows, stream_rows(vocab)), vocab)));
   w.off = take((size_t)rows * 8);
+  w.exponents = take(wide && grad ? (size_t)rows * 4 : 0);
   w.g = take(bf16 && grad ? 2 * cells * 2 : 0);
   w.hi = take(wide && grad ? cells * 2 : 0);
   w.lo = take(wide && grad ? cells * 2 : 0);
@@ -923,7 +946,7 @@ hipError_t launch_head(modse_dtype dt, const HeadArgs& a, char* ws, hipStream_t 
   if (!grad && a.T <= stream_rows(a.vocab)) {
     float* const pairs = reinterpret_cast<float*>(align_up(reinterpret_cast<size_t>(ws), ALIGN));
     float* const at_target = pairs + align_up(stream_pairs(a.T, a.vocab), ALIGN) / 4;
-    const HeadStreamArgs r = {a.x, a.W, a.targets, pairs, at_target, a.logp, a.log_z, nullptr, nullptr, nullptr, (int32_t)a.T, a.d, a.vocab, 0};
+    const HeadStreamArgs r = {a.x, a.W, a.targets, pairs, at_target, a.logp, a.log_z, nullptr, nullptr, nullptr, nullptr, nullptr, (int32_t)a.T, a.d, a.vocab, 0};
     return dt == MODSE_F32 ? run_stream<float>(r, s) : run_stream<bf16_t>(r, s);
   }
   const HeadShape h = head_shape(a.T, a.d, a.vocab, dt, grad);
@@ -935,10 +958,9 @@ hipError_t launch_head(modse_dtype dt, const HeadArgs& a, char* ws, hipStream_t 
   auto halves = [&](size_t at) { return reinterpret_cast<f16_t*>(ws + at); };
   HeadRange* const range = h.pairs || (h.bf16 && grad) ? reinterpret_cast<HeadRange*>(ws + w.range) : nullptr;
   const HeadBufs b = {reinterpret_cast<GemmPlan*>(ws), floats(w.logits), floats(w.pairs), floats(w.at_target), floats(w.off),
-                      reinterpret_cast<bf16_t*>(ws + w.g), halves(w.hi), halves(w.lo), halves(w.x16), halves(w.x16_lo),
+                      reinterpret_cast<bf16_t*>(ws + w.g), halves(w.hi), halves(w.lo), halves(w.x16), halves(w.x16_lo), reinterpret_cast<int32_t*>(ws + w.exponents),
                       halves(w.w16), halves(w.w16_lo), floats(w.x32), range, floats(w.slabs)};
-  const int64_t looked_at = h.T * h.d + (h.pairs ? (int64_t)h.vocab * h.d : 0);
-  const int64_t range_blocks = range ? std::min<int64_t>((looked_at + 32767) / 32768, RANGE_BLOCKS) : 0;
+  const int64_t range_blocks = h.pairs ? std::min<int64_t>(((int64_t)h.vocab * h.d + 32767) / 32768, RANGE_BLOCKS) : 0;
   auto make_plans = [&](int first) {  // returns how many pieces they are of
     const int n = std::min(h.pieces - first, PLAN_PIECES), tables = n * (grad ? 3 : 1);
     const HeadPlanArgs plan = {h, b, a.x, a.W, a.targets, a.d_logp, a.dW, first, n, tables};
@@ -960,10 +982,11 @@ hipError_t launch_head(modse_dtype dt, const HeadArgs& a, char* ws, hipStream_t 
       int lanes = 64;
       while (lanes > 2 && lanes / 2 >= h.d / 8) lanes /= 2;
       hipLaunchKernelGGL(head_split_x_kernel, dim3((unsigned)((m * lanes + 255) / 256)), dim3(256), 0, s, static_cast<const float*>(a.x) + t0 * h.d,
-                         a.targets + t0, (int)m, h.d, h.vocab, (int)grad, range, b.x16, b.x16_lo, b.at_target + h.rows);
+                         (int)m, h.d, b.x16, b.x16_lo, b.at_target + h.rows);
     }
     if (stream) {
-      const HeadStreamArgs r = {a.x, a.W, a.targets, b.pairs, b.at_target, a.logp, nullptr, b.logits, b.off, range, (int32_t)m, h.d, h.vocab, h.ldv};
+      const HeadStreamArgs r = {a.x, a.W, a.targets, b.pairs, b.at_target, a.logp, nullptr, b.logits, b.off, range, b.exponents, a.d_logp,
+                                (int32_t)m, h.d, h.vocab, h.ldv};
       e = h.bf16 ? run_stream<bf16_t>(r, s) : run_stream<float>(r, s);
     } else {
       e = launch_grouped_gemm(dt, h.pairs ? EPI_LOGITS_PAIRS : EPI_LOGITS, h.logits_tile, plan, h.w_parts, 0,
@@ -972,12 +995,13 @@ hipError_t launch_head(modse_dtype dt, const HeadArgs& a, char* ws, hipStream_t 
     if (e != hipSuccess) return;
     const HeadRowsArgs r = {a.targets + t0, a.d_logp ? a.d_logp + t0 : nullptr, a.logp ? a.logp + t0 : nullptr, a.log_z ? a.log_z + t0 : nullptr,
                             b.logits, b.pairs, b.at_target, b.off, a.dX && h.bf16 ? b.g : nullptr, a.dX && h.bf16 ? b.g + (int64_t)h.rows * h.ldv : nullptr,
-                            a.dW || h.pairs ? b.hi : nullptr, a.dW || h.pairs ? b.lo : nullptr, range,
-                            static_cast<const char*>(a.x) + (size_t)t0 * h.d * (h.bf16 ? 2 : 4), b.x16, a.dW && !h.wide ? b.x32 : nullptr,
+                            a.dW || h.pairs ? b.hi : nullptr, a.dW || h.pairs ? b.lo : nullptr, grad ? range : nullptr, b.exponents,
+                            static_cast<const char*>(a.x) + (size_t)t0 * h.d * (h.bf16 ? 2 : 4), b.x16, h.pairs ? b.x16_lo : nullptr,
+                            a.dW && !h.wide ? b.x32 : nullptr,
                             (int32_t)m, h.vocab, h.ldv, h.rows, h.pair_cols(), h.d};
     if (!stream) hipLaunchKernelGGL(head_stats_kernel, dim3((unsigned)((m + 15) / 16)), dim3(1024), 0, s, r);
     if (grad) {
-      const int64_t segs = (h.ldv + 2047) / 2048, copies = a.dW && h.bf16 ? (m * h.d + 2047) / 2048 : 0;
+      const int64_t segs = (h.ldv + 2047) / 2048, copies = a.dW && h.wide ? (m * h.d + 2047) / 2048 : 0;
       const dim3 grid((unsigned)(m * segs + copies));
       if (h.wide) hipLaunchKernelGGL(head_grad_kernel, grid, dim3(256), 0, s, r, (int)segs);
       else hipLaunchKernelGGL(head_grad_f32_kernel, grid, dim3(256), 0, s, r, (int)segs);
@@ -1007,7 +1031,7 @@ hipError_t launch_head(modse_dtype dt, const HeadArgs& a, char* ws, hipStream_t 
       e = launch_grouped_gemm(dt, h.pairs ? EPI_STORE_PAIRS : h.bf16 && !stacked ? EPI_STORE_DUALK_F32 : EPI_STORE_F32, h.dx_tile, p, h.k_parts, 0, 0,
                               h.k_parts * tiles_of(stacked ? h.dx_rows : m, h.d, h.dx_tile), s, LAYOUT_B_KN);
       if (e != hipSuccess) break;
-      const HeadJoinArgs j = {b.slabs, h.pairs ? range->undo_dx : nullptr, (int64_t)h.dx_rows * h.d, stacked ? (int64_t)h.rows * h.d : 0,
+      const HeadJoinArgs j = {b.slabs, h.pairs ? b.exponents : nullptr, range, (int64_t)h.dx_rows * h.d, stacked ? (int64_t)h.rows * h.d : 0,
                               h.k_parts, h.d};
       e = h.bf16 ? run_join(j, m, static_cast<bf16_t*>(a.dX) + t0 * h.d, s) : run_join(j, m, static_cast<float*>(a.dX) + t0 * h.d, s);
     }

@@ -339,9 +339,14 @@ modse_status modse_embed_bwd(int64_t T, int32_t d_model, int32_t vocab, modse_dt
  * x, W, dX, dW and the workspace lie at addresses that are multiples of 16.
  * Float32 with more rows than a few hundred (as many as make that the faster way), and
  * vocab d_model up to 2^28: x and W are held in 22 bits each, x down to 2^-39 of the
- * largest value of its row, W down to 2^-39 of its largest; what is smaller may be lost.  The workspace then also holds the parts
- * of W, 4 vocab d_model bytes.  An infinity or NaN in a row of x makes that row's logp
- * NaN (and its row of dX, and dW), one in W every row's. */
+ * largest value of its row, W down to 2^-39 of its largest; what is smaller may be lost.
+ * Where that would be more than some values near 0 (more than 1 of 256 values of W other
+ * than 0 below 2^-20 of the largest, more than 1 of 16384 below 2^-30, or not all finite)
+ * the products with W are in float32, which takes longer.  The workspace of such calls
+ * also holds the parts of W, 4 vocab d_model bytes.
+ * An infinity or NaN in a row of x makes that row's logp NaN (and its row of dX, and dW).
+ * With infinities in W logits go by the products: one of -infinity has probability 0 (its
+ * row of W then makes dX NaN), one of +infinity or NaN makes its row's logp NaN. */
 modse_status modse_head_workspace_size(int64_t T, int32_t d_model, int32_t vocab, modse_dtype dtype, int which, size_t* bytes);
 modse_status modse_head_fwd(int64_t T, int32_t d_model, int32_t vocab, modse_dtype dtype, const void* x, const void* W,
                             const int32_t* targets, float* logp, float* log_z, void* ws, size_t ws_bytes, void* hip_stream);

@@ -241,6 +241,8 @@ enum GemmOption {
 // layout < 0: the layout that goes with the epilogue (see gemm.hip).
 hipError_t launch_grouped_gemm(modse_dtype dt, int epilogue, TileShape t, const GemmPlan* plan, int n_prob, int accumulate,
                                int option, int64_t max_tiles, hipStream_t s, int layout = -1);
+// float32, tiles of 128: EPI_LOGITS, or EPI_STORE_F32 with LAYOUT_B_KN, of a plan that has no tiles as a rule
+hipError_t launch_rare_gemm(int epilogue, const GemmPlan* plan, int n_prob, int64_t max_tiles, hipStream_t s);
 
 // Layers of small tiles: dX and, in the same launch, the weight gradients (wg, null where wgrad_beside_dx says no) and the shares of the
 // router's (dwg, may be null).  Float32 ones come with the weight gradients or not at all (dwg_beside_dx).

@@ -143,6 +143,15 @@ hipError_t launch_grouped_gemm(modse_dtype dt, int epilogue, TileShape t, const 
   return hipErrorInvalidValue;
 }
 
+hipError_t launch_rare_gemm(int epilogue, const GemmPlan* plan, int n_prob, int64_t max_tiles, hipStream_t s) {
+  const int64_t blocks = block_grid(max_tiles);
+  const dim3 grid((unsigned)std::min<int64_t>(blocks, 2 * num_cus()));
+  if (epilogue == EPI_LOGITS) hipLaunchKernelGGL((gg_f32_rare_kernel<EPI_LOGITS, LAYOUT_TN>), grid, dim3(256), 0, s, plan, n_prob, (int)blocks);
+  else if (epilogue == EPI_STORE_F32) hipLaunchKernelGGL((gg_f32_rare_kernel<EPI_STORE_F32, LAYOUT_B_KN>), grid, dim3(256), 0, s, plan, n_prob, (int)blocks);
+  else return hipErrorInvalidValue;
+  return hipGetLastError();
+}
+
 // Wherever the tiles allow it: in none of 58 layers drawn over the sizes that have such tiles was one launch slower by more than
 // the runs differ (figures at the kernels, gemm_block.h).
 bool dwg_beside_dx(modse_dtype dt, TileShape dx_tile, TileShape wg_tile) {

@@ -582,6 +582,17 @@ __global__ __launch_bounds__(256, 2) void gg_f32_kernel(const GemmPlan* __restri
   MODSE_RING(BM, NB * BN, 4);
   gg_block<float, BM, BN, NB, 2, 2, 4, EPI, LAYOUT>(plan, n_prob, accumulate, option, blockIdx.x, ring);
 }
+// A launch whose list is empty as a rule, where the device decides between two ways of a product: few workgroups that each take some of the tiles, as
+// one for every tile would take up to 9 us to find that there are none (two for every CU, or one: 4.8).
+template <int EPI, int LAYOUT>
+__global__ __launch_bounds__(256, 2) void gg_f32_rare_kernel(const GemmPlan* __restrict__ plan, int n_prob, int blocks) {
+  MODSE_RING(128, 128, 4);
+  if (plan->tile_start[n_prob] == 0) return;
+  for (int block = blockIdx.x; block < blocks; block += gridDim.x) {
+    gg_block<float, 128, 128, 1, 2, 2, 4, EPI, LAYOUT>(plan, n_prob, 0, 0, block, ring);
+    __syncthreads();  // (the next tile's panels come where waves may still be reading)
+  }
+}
 // Launches of few tiles.  Bound by latency: of the workgroup's start, of the loads of a K step, of the dependent matrix
 // instructions of a wave.  So the tile is small (32 x 32), its four waves take one K slice of a step each and add up through
 // LDS, and 32 to 36 KiB of ring let four workgroups of a CU wait at a time.  d = 256, 512 tokens: up-projection 14 -> 11 us,

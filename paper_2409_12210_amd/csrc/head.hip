@@ -15,7 +15,8 @@
 // float32 from some hundred rows on: x, W and G are held as the sums of two float16 matrices, hi + lo, times powers of two (see HeadRange)
 // that bring the largest value below 2^15.  Three products of float16 matrices, hi hi' + hi lo' + lo hi', in one accumulator leave
 // out 2^-22 of a product; they take 3 of the 16-bit matrix rate where float32 instructions take 16 (1021 x 256 x 50257 with gradients:
-// 435 us in place of 731).  Fewer rows, or a W of more than 2^28 elements: products in float32, and G in the place of the logits.
+// 445 us in place of 731).  Fewer rows, or a W of more than 2^28 elements: products in float32, and G in the place of the logits.  Where the device finds
+// values in W that its parts would lose, the products with W are in float32, too: by a second list of tiles, of which one is empty.
 //
 // Up to 64 rows (small vocabularies: more) a stream over W makes the logits, see "few rows".  dW of a small vocabulary has few tiles,
 // so its sum over the tokens is cut into parts as well (float32, 1000 x 512, 4096 rows: with the stream 160 us in place of 337 for the whole call).
@@ -39,7 +40,7 @@ using namespace modse_gemm;
 
 constexpr int64_t GRAD_CELLS = (int64_t)1 << 28;   // values of G in the workspace (float32: of logits)
 constexpr int64_t PAIR_W = (int64_t)1 << 28;       // elements of W of which the parts are kept
-constexpr int64_t PAIR_CELLS = (int64_t)1 << 27;   // pairs of 128 columns in it
+constexpr int64_t PAIR_CELLS = (int64_t)1 << 27;   // pairs of 128 columns in it (float32: of 32)
 constexpr int64_t W_PART = (int64_t)1 << 30;       // elements of W that one problem reads (kernels count them in 32 bits)
 constexpr size_t ALIGN = 256;                      // of what is in the workspace, which itself may lie at any sixteen bytes
 constexpr int64_t SLAB_CELLS = (int64_t)1 << 26;   // values of all parts of dX together, unless one part has more
@@ -70,13 +71,15 @@ int64_t rows_in(int64_t cells, int64_t per_row) {
   while (r < 65536 && 2 * r * per_row <= cells) r *= 2;
   return r;
 }
-int64_t most_rows(int32_t vocab, bool wide, bool grad) {
-  return wide && !grad ? rows_in(PAIR_CELLS, (vocab + 127) / 128) : rows_in(GRAD_CELLS, (int64_t)align_up(vocab, 64));
+int64_t most_rows(int32_t vocab, bool bf16, bool pairs, bool grad) {
+  if (grad || !(bf16 || pairs)) return rows_in(GRAD_CELLS, (int64_t)align_up(vocab, 64));
+  return bf16 ? rows_in(PAIR_CELLS, (vocab + 127) / 128) : rows_in(PAIR_CELLS, (vocab + 31) / 32);
 }
 // Float32 layers: the rows from which on products of pairs of float16 numbers are faster, three 16-bit products in place of one of float32,
 // with the largest values and the parts of W (and some launches) before them.  At 105 and 1150 TFLOP/s, 5 TB/s and tiles that are 128 rows too
-// high on average.  Float32 / pairs, us: gradients with 32000 x 2048, 256 rows 830 / 575, 1024 3060 / 1150; with 50257 x 256, 256 rows 227 / 195,
-// 1024 733 / 455; scoring with 32000 x 2048, 256 rows 262 / 294, 512 550 / 313; with 50257 x 256, 300 rows 81 / 97, 400 106 / 97.
+// high on average.  Float32 / pairs, us: gradients with 32000 x 2048, 256 rows 828 / 567, 1024 3045 / 1189; with 50257 x 256, 256 rows 217 / 187,
+// 1024 721 / 448; with 4097 x 64, 5000 rows 222 / 200; scoring with 32000 x 2048, 256 rows 264 / 277, 512 514 / 320; with 50257 x 256, 300 rows 81 / 90,
+// 400 106 / 103.
 int64_t pairs_from(int32_t d, int32_t vocab, bool grad) {
   const double cells = (double)vocab * d, products = grad ? 6 : 2;
   const double fixed = 3 * products * 128 * cells / 1.15e9 + 12 * cells / 5e6 + (grad ? 50 : 35);
@@ -108,10 +111,10 @@ bool dx_takes_blocks(int64_t T, int32_t d, bool pairs) {
 }
 bool dw_takes_blocks(int64_t T, int64_t tiles_256) { return T <= 64 || (tiles_256 <= FEW_TILES && T * tiles_256 <= 256 * FEW_TILES); }
 // pairs of maximum and sum for so many rows of any batch
-size_t pair_cells(int64_t rows, int32_t d, int32_t vocab, bool wide) {
+size_t pair_cells(int64_t rows, int32_t d, int32_t vocab, bool bf16) {
   auto of = [&](int64_t n, int cols) { return (size_t)n * ((vocab + cols - 1) / cols); };
   const int64_t block_rows = d > 256 ? std::max<int64_t>(128, FEW_TILES / tiles(1, vocab, 256) * 256) : rows;
-  return wide ? std::max(of(rows, 128), of(std::min(rows, block_rows), 64)) : of(rows, 32);
+  return bf16 ? std::max(of(rows, 128), of(std::min(rows, block_rows), 64)) : of(rows, 32);
 }
 // Parts of dW's sum over the tokens, where it has too few tiles for the chip: slabs like those of dX, added up behind it.
 int64_t dw_most_parts(int32_t d, int32_t vocab, bool wide) {
@@ -119,20 +122,22 @@ int64_t dw_most_parts(int32_t d, int32_t vocab, bool wide) {
   return wide && tiles <= 128 ? std::min<int64_t>(MAX_PARTS, 256 / tiles) : 1;
 }
 
-HeadShape head_shape(int64_t T, int32_t d, int32_t vocab, modse_dtype dt, bool grad) {
+// (plain: the products in float32 of a call that takes pairs)
+HeadShape head_shape(int64_t T, int32_t d, int32_t vocab, modse_dtype dt, bool grad, bool plain = false) {
   HeadShape h = {};
   h.T = T;
   h.d = d;
   h.vocab = vocab;
   h.bf16 = dt == MODSE_BF16;
   h.grad = grad;
-  h.pairs = takes_pairs(T, d, vocab, dt, grad);
+  const bool pairs = takes_pairs(T, d, vocab, dt, grad);
+  h.pairs = pairs && !plain;
   h.wide = h.bf16 || h.pairs;
   h.ldv = (int32_t)align_up(vocab, 64);
   // Pieces of about one size, whole tiles of 256: a last one of a few rows would go over all of W and dW for them.  Gradients of 8193 rows with
   // 32000 x 2048, as 8192 + 1 / 4352 + 3841: bf16 5850 / 4975 us, float32 9870 / 8320; 2049 rows with
   // 131072 x 2048, 2048 + 1 / 1280 + 769: 6580 / 5660, 11170 / 9710.
-  const int64_t most = most_rows(vocab, h.wide, grad);
+  const int64_t most = most_rows(vocab, h.bf16, pairs, grad);
   h.pieces = (int32_t)((T + most - 1) / most);
   h.rows = h.pieces == 1 ? padded_rows(T) : (int32_t)align_up((size_t)((T + h.pieces - 1) / h.pieces), 256);
   h.pieces = (int32_t)((T + h.rows - 1) / h.rows);
@@ -141,7 +146,7 @@ HeadShape head_shape(int64_t T, int32_t d, int32_t vocab, modse_dtype dt, bool g
   // (float32: tiles of 128 from four rounds of the chip's 512 workgroups on.  50304 x 256, 1.5 rounds: 287 us with them, 258 with tiles of
   // 64; 1021 x 50257, 6.1 rounds: 251 and 261)
   auto tile = [&](int64_t m, int64_t n) { const int b = h.wide ? 256 : tiles(m, n, 128) >= 2048 ? 128 : 64; return TileShape{b, b}; };
-  h.logits_tile = h.wide && logits_take_blocks(T, d, vocab, h.bf16 && !grad) ? TileShape{128, 128} : tile(h.rows, vocab);
+  h.logits_tile = plain || (h.wide && logits_take_blocks(T, d, vocab, h.bf16 && !grad)) ? TileShape{128, 128} : tile(h.rows, vocab);
   h.dw_tile = h.bf16 && dw_takes_blocks(T, tiles(vocab, d, 256)) ? TileShape{128, 128} : tile(vocab, d);
   const int64_t w_steps = (h.rows + 63) / 64, w_split = std::min(dw_most_parts(d, vocab, h.wide), std::max<int64_t>(1, w_steps / 4));
   h.w_len = (int32_t)((w_steps + w_split - 1) / w_split) * 64;
@@ -174,14 +179,15 @@ HeadShape head_shape(int64_t T, int32_t d, int32_t vocab, modse_dtype dt, bool g
 // times 2^(C - r_t), with one C from the largest |w_t| (1 - p_target) max|x_t| so far in the call.
 constexpr int RANGE_BLOCKS = 512;
 constexpr int NO_ROW = -(1 << 20);
-constexpr int MOST_LINES = 64;  // (2048 rows that all change one number took 15 us)
+constexpr int MOST_LINES = 64;  // that many blocks or rows change together, each in a line of its own (2048 rows one number: 15 us)
 struct HeadRange {
-  uint32_t w_of[RANGE_BLOCKS];  // the largest finite |W|, as the bits of a float, by block
-  int32_t blocks;
+  uint32_t w_of[RANGE_BLOCKS];  // the largest |W|, as the bits of a float, by block (of a NaN more than those of an infinity)
+  int32_t counts[MOST_LINES][32];   // [i][0 .. 2], of every 64th block: values of W that are not 0, those below 2^-20 and 2^-30 of its largest
   int32_t w_exponent;  // W is taken times 2 to it
+  int32_t plain;       // the products with W are in float32
   float undo_dw[2];    // 2^-C, in two factors
   int32_t most[MOST_LINES][32];  // [i][0]: exponent of the largest |w_t| (1 - p_target) max|x_t| so far of every 64th row, or NO_ROW
-  float pad[7];
+  float pad[3];
   float undo_w;  // right before the targets' logits (EPI_LOGITS_PAIRS)
 };
 static_assert(sizeof(HeadRange) == offsetof(HeadRange, undo_w) + 4 && sizeof(HeadRange) % 16 == 0, "laid out up to the targets' logits");
@@ -227,8 +233,16 @@ struct HeadPlanArgs {
   const int32_t* targets;
   const float* d_logp;
   float* dW;
-  int32_t first, pieces, plans;  // pieces whose problems are made, the first of them
+  HeadShape plain;     // of a call that takes pairs: its products with W in float32
+  int32_t first, pieces, tables;  // pieces whose problems are made, the first of them; their products
+  int32_t x_first, x_rows;        // rows of x that are split
+  int32_t range_blocks;
 };
+enum HeadProduct { LOGITS, DX, DW, PLAIN_LOGITS, PLAIN_DX };
+// The products of a piece that a call has tables for, and the i-th of them.
+__host__ __device__ inline int head_products(const HeadShape& h) { return (h.grad ? 3 : 1) + (h.pairs ? h.grad ? 2 : 1 : 0); }
+__host__ __device__ inline int head_product(const HeadShape& h, int i) { return h.grad || i == 0 ? i : PLAIN_LOGITS; }
+__host__ __device__ inline int head_table(const HeadShape& h, int product) { return h.grad || product == LOGITS ? product : 1; }
 
 // Infinities and NaN count as 0: they stay what they are in the parts, and the other values keep theirs.
 __device__ __forceinline__ uint32_t finite(uint32_t bits) { return (bits & 0x7fffffffu) < 0x7f800000u ? bits & 0x7fffffffu : 0; }
@@ -257,17 +271,49 @@ __device__ __forceinline__ uint32_t wave_most(uint32_t v) {
   for (int o = 32; o; o >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, o, 64));
   return v;
 }
-// float32 by pairs: W's largest value
-__device__ __forceinline__ void range_block(const HeadPlanArgs& a, int block, int blocks) {
+// float32 by pairs: W's largest value; clears the counts.
+__global__ __launch_bounds__(1024) void head_range_kernel(const u32x4* W, int64_t vectors, HeadRange* range) {
   __shared__ uint32_t s_most[16];
-  const int64_t first = (int64_t)block * 1024 + threadIdx.x, step = (int64_t)blocks * 1024;
-  uint32_t most = wave_most(largest(static_cast<const u32x4*>(a.W), (int64_t)a.h.vocab * a.h.d / 4, false, first, step));
+  if (blockIdx.x == 0 && threadIdx.x < 3 * MOST_LINES) range->counts[threadIdx.x / 3][threadIdx.x % 3] = 0;
+  uint32_t most = 0;
+  for (int64_t i = (int64_t)blockIdx.x * 1024 + threadIdx.x; i < vectors; i += (int64_t)gridDim.x * 4096) {
+    u32x4 v[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int64_t at = i + q * (int64_t)gridDim.x * 1024;
+      v[q] = W[at < vectors ? at : i];
+    }
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) most = max(most, v[q][e] & 0x7fffffffu);
+  }
+  most = wave_most(most);
   if ((threadIdx.x & 63) == 0) s_most[threadIdx.x >> 6] = most;
   __syncthreads();
   if (threadIdx.x > 0) return;
   for (int w = 1; w < 16; ++w) most = max(most, s_most[w]);
-  a.b.range->w_of[block] = most;
-  if (block == 0) a.b.range->blocks = blocks;
+  range->w_of[blockIdx.x] = most;
+}
+// By a wave: the bits of the largest |W|, those of an infinity or more where not all values are finite.
+__device__ __forceinline__ uint32_t largest_w(const HeadRange* range, int blocks) {
+  uint32_t most = 0;
+  for (int i = threadIdx.x & 63; i < blocks; i += 64) most = max(most, range->w_of[i]);
+  return wave_most(most);
+}
+__device__ __forceinline__ int wave_total(int v) {
+#pragma unroll
+  for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o, 64);
+  return v;
+}
+// What lies 2^-40 below W's largest value is lost by pairs.  Where that is more than a rounding of values that count, as beside a few far larger rows (which
+// keep columns out by a constant in x, say), the products with W are in float32 instead: where more than 1 of 256 values other than 0 are below 2^-20 of the largest,
+// or more than 1 of 16384 below 2^-30 (normal values: below 1e-5 and 1e-8 of them), or not all are finite.  By a wave.
+__device__ __forceinline__ bool w_takes_float32(const HeadRange* range, uint32_t most) {
+  int n[3];
+#pragma unroll
+  for (int k = 0; k < 3; ++k) n[k] = wave_total(range->counts[threadIdx.x % MOST_LINES][k]);
+  return most >= 0x7f800000u || n[1] > n[0] / 256 || n[2] > n[0] / 16384;
 }
 // What a row's G and x are taken times, once its statistics are there: by the first wave of those that call it.  `largest_x`: of the row's finite values.
 // (1 - p as it is computed, of a p that may be rounded to 1.)  Rows without a gradient have no part in C, and their copies of x are 0.
@@ -291,74 +337,96 @@ __device__ __forceinline__ void put_parts(const f32x4 (&v)[2], int exponent, f16
   *reinterpret_cast<f16x8*>(hi) = h;
   *reinterpret_cast<f16x8*>(lo) = l;
 }
-// W, n elements (a multiple of 16).  Every block joins the largest values for itself.
-__global__ __launch_bounds__(256) void head_split_w_kernel(const float* W, int64_t n, f16_t* hi, f16_t* lo, HeadRange* range) {
+// W's parts, of n elements (a multiple of 8).  Every block joins the largest values for itself.
+__global__ __launch_bounds__(256) void head_split_w_kernel(const float* W, int64_t n, f16_t* hi, f16_t* lo, HeadRange* range, int blocks) {
   __shared__ uint32_t s_most;
+  __shared__ int s_n[3][4];
   if (threadIdx.x < 64) {
-    const int lane = threadIdx.x, blocks = range->blocks;
-    uint32_t most = 0;
-    for (int i = lane; i < blocks; i += 64) most = max(most, range->w_of[i]);
-    most = wave_most(most);
-    if (lane == 0) {
-      s_most = most;
-      if (blockIdx.x == 0) {
-        range->w_exponent = scale_exponent(most);
-        range->undo_w = power_of_two(-scale_exponent(most));
-      }
-    }
+    const uint32_t most = largest_w(range, blocks);
+    if (threadIdx.x == 0) s_most = most < 0x7f800000u ? most : 0;
   }
   __syncthreads();
   const int exponent = scale_exponent(s_most);
+  const float most = __builtin_bit_cast(float, s_most), small = most * 0x1p-20f, smaller = most * 0x1p-30f;
+  int count[3] = {};
   const int64_t step = (int64_t)gridDim.x * 2048;
   for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8; i < n; i += step) {
     const f32x4 v[2] = {__builtin_nontemporal_load(reinterpret_cast<const f32x4*>(W + i)),
                         __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(W + i + 4))};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float size = fabsf(v[e >> 2][e & 3]);
+      count[0] += size > 0.f;
+      count[1] += size > 0.f && size < small;
+      count[2] += size > 0.f && size < smaller;
+    }
     put_parts(v, exponent, hi + i, lo + i);
   }
+#pragma unroll
+  for (int k = 0; k < 3; ++k) {
+    count[k] = wave_total(count[k]);
+    if ((threadIdx.x & 63) == 0) s_n[k][threadIdx.x >> 6] = count[k];
+  }
+  __syncthreads();
+  if (threadIdx.x >= 3) return;
+  int sum = 0;
+  for (int w = 0; w < 4; ++w) sum += s_n[threadIdx.x][w];
+  if (sum) atomicAdd(&range->counts[blockIdx.x % MOST_LINES][threadIdx.x], sum);
 }
-// Rows of x, some lanes of a wave each, by their own largest values.
-__global__ __launch_bounds__(256) void head_split_x_kernel(const float* x, int rows, int d, f16_t* hi, f16_t* lo, float* undo) {
-  const int lanes = lanes_of(d / 8), lane = threadIdx.x & (lanes - 1);
-  const int64_t row = ((int64_t)blockIdx.x * 256 + threadIdx.x) / lanes;
-  if (row >= rows) return;
+// Rows of x of a piece, some lanes of a wave each, by their own largest values.
+__device__ __forceinline__ void split_x(const HeadPlanArgs& a, int block) {
+  const int d = a.h.d, lanes = lanes_of(d / 8), lane = threadIdx.x & (lanes - 1);
+  const int64_t row = ((int64_t)block * 256 + threadIdx.x) / lanes;
+  if (row >= a.x_rows) return;
   const int64_t at = row * d;
+  const float* const x = static_cast<const float*>(a.x) + (int64_t)a.x_first * d;
   uint32_t most = largest(reinterpret_cast<const u32x4*>(x + at), d / 4, false, lane, lanes);
   for (int o = lanes / 2; o; o >>= 1) most = max(most, (uint32_t)__shfl_xor((int)most, o, 64));
   const int e = scale_exponent(most);
-  if (lane == 0) undo[row] = power_of_two(-e);
+  if (lane == 0) a.b.at_target[a.h.rows + row] = power_of_two(-e);
   for (int c = lane * 8; c < d; c += lanes * 8) {
     const f32x4 v[2] = {*reinterpret_cast<const f32x4*>(x + at + c), *reinterpret_cast<const f32x4*>(x + at + c + 4)};
-    put_parts(v, e, hi + at + c, lo + at + c);
+    put_parts(v, e, a.b.x16 + at + c, a.b.x16_lo + at + c);
   }
 }
 
-// The problems of one product, by a block's first wave: of the logits, a block for each piece, then of dX and of dW, a block for each.
-// Blocks behind these, of the call's first such launch, look for W's largest value.
-__global__ __launch_bounds__(1024) void head_plan_kernel(HeadPlanArgs a) {
+// The problems of one product of one piece, by a block's first wave.  Of the products by pairs and those in float32 one has no tiles.  Blocks behind
+// these split rows of x.
+__global__ __launch_bounds__(256) void head_plan_kernel(HeadPlanArgs a) {
   __shared__ int s_tiles[MODSE_MAX_PROBLEMS];
-  if ((int)blockIdx.x >= a.plans) {
-    range_block(a, blockIdx.x - a.plans, gridDim.x - a.plans);
+  const HeadShape& h = a.h;
+  if ((int)blockIdx.x >= a.tables) {
+    split_x(a, blockIdx.x - a.tables);
     return;
   }
   if (threadIdx.x >= 64) return;
-  const HeadShape& h = a.h;
-  if (a.first == 0 && blockIdx.x == 0 && a.b.range) a.b.range->most[threadIdx.x][0] = NO_ROW;
-  const int lane = threadIdx.x, behind = (int)blockIdx.x - a.pieces;
-  const int which = behind < 0 ? 0 : 1 + behind % 2;
-  const int64_t t0 = (int64_t)(a.first + (which == 0 ? (int)blockIdx.x : behind / 2)) * h.rows;
+  const int lane = threadIdx.x;
+  const uint32_t most = h.pairs ? largest_w(a.b.range, a.range_blocks) : 0;
+  const bool takes_float32 = h.pairs && w_takes_float32(a.b.range, most);
+  if (a.first == 0 && blockIdx.x == 0 && a.b.range) {
+    a.b.range->most[lane][0] = NO_ROW;
+    if (lane == 0) {
+      a.b.range->w_exponent = scale_exponent(most);
+      a.b.range->plain = takes_float32;
+      a.b.range->undo_w = power_of_two(-scale_exponent(most));
+    }
+  }
+  const int which = head_product(h, (int)blockIdx.x / a.pieces);
+  const int64_t t0 = (int64_t)(a.first + (int)blockIdx.x % a.pieces) * h.rows;
   const size_t es = h.bf16 ? 2 : 4;
   const int m = (int)min((int64_t)h.rows, h.T - t0);
   const char* const x = cadd(a.x, (size_t)t0 * h.d * es);
   GemmPlan* const plan = a.b.plans + blockIdx.x;
-  const int n = which == 0 ? h.w_parts : which == 1 ? h.k_parts : h.w_split;
+  const bool plain = which == PLAIN_LOGITS || which == PLAIN_DX, active = which == DW || plain == takes_float32;
+  const int n = which == LOGITS || which == PLAIN_LOGITS ? h.w_parts : which == DX ? h.k_parts : which == PLAIN_DX ? a.plain.k_parts : h.w_split;
   for (int p = lane; p < n; p += 64) {
     GemmProblem P = {};
     TileShape t;
-    if (which == 0) {
+    if (which == LOGITS || which == PLAIN_LOGITS) {
       const int v0 = p * h.w_rows;
       P.A = x;
       P.B = cadd(a.W, (size_t)v0 * h.d * es);
-      if (h.pairs) {
+      if (h.pairs && !plain) {
         P.A = a.b.x16;
         P.A2 = a.b.x16_lo;
         P.B = a.b.w16 + (size_t)v0 * h.d;
@@ -371,12 +439,12 @@ __global__ __launch_bounds__(1024) void head_plan_kernel(HeadPlanArgs a) {
       P.E2 = reinterpret_cast<const void*>((uint64_t)h.rows << 32 | (uint32_t)v0);
       P.M = m; P.N = min(h.w_rows, h.vocab - v0); P.K = h.d;
       P.lda = h.d; P.ldb = h.d; P.ldc = h.ldv;
-      t = h.logits_tile;
-    } else if (which == 1) {
-      const int v0 = p * h.k_len;
+      t = plain ? a.plain.logits_tile : h.logits_tile;
+    } else if (which == DX || which == PLAIN_DX) {
+      const int k_len = plain ? a.plain.k_len : h.k_len, v0 = p * k_len;
       P.A = h.bf16 ? (const void*)(a.b.g + v0) : (const void*)(a.b.logits + v0);
       P.B = cadd(a.W, (size_t)v0 * h.d * es);
-      if (h.pairs) {
+      if (h.pairs && !plain) {
         P.A = a.b.hi + v0;
         P.A2 = a.b.lo + v0;
         P.B = a.b.w16 + (size_t)v0 * h.d;
@@ -387,9 +455,9 @@ __global__ __launch_bounds__(1024) void head_plan_kernel(HeadPlanArgs a) {
         P.B2 = P.B;
       }
       P.C = a.b.slabs + (size_t)p * h.dx_rows * h.d;
-      P.M = h.dx_rows > h.rows ? h.dx_rows : m; P.N = h.d; P.K = min(h.k_len, h.vocab - v0);
+      P.M = h.dx_rows > h.rows ? h.dx_rows : m; P.N = h.d; P.K = min(k_len, h.vocab - v0);
       P.lda = h.ldv; P.ldb = h.d; P.ldc = h.d;
-      t = h.dx_tile;
+      t = plain ? a.plain.dx_tile : h.dx_tile;
     } else {
       const int r0 = p * h.w_len;  // (behind the last piece's rows: a part of zeros)
       const size_t g0 = (size_t)r0 * h.ldv, x0 = (size_t)r0 * h.d;
@@ -404,7 +472,8 @@ __global__ __launch_bounds__(1024) void head_plan_kernel(HeadPlanArgs a) {
       P.lda = h.ldv; P.ldb = h.d; P.ldc = h.d;
       t = h.dw_tile;
     }
-    s_tiles[p] = set_tiles(P, t.bm, t.bn);
+    const int tiles = set_tiles(P, t.bm, t.bn);
+    s_tiles[p] = active ? tiles : 0;
     plan->prob[p] = P;
   }
   wave_lds_order();
@@ -422,12 +491,12 @@ struct HeadRowsArgs {
   float* off;
   bf16_t *g, *g_rest;      // of the product's first row; null where there is no dX
   f16_t *hi, *lo;          // null where there is no dW
-  HeadRange* range;        // (16-bit products of gradients) or null
+  HeadRange* range;        // (16-bit products) or null
   int32_t* exponents;
   const void* x;           // of the product's first row, and their copies for dW, with zeros in rows without a target
   f16_t *x16, *x16_lo;     // x16_lo: null of bf16 layers
   float* x32;              // (float32 layers) null where there is no dW
-  int32_t rows, vocab, ldv, pair_rows, pair_cols, d;
+  int32_t rows, vocab, ldv, pair_rows, pair_cols, plain_cols, d;  // plain_cols: those of the products in float32 of a call that takes pairs, or 0
 };
 __device__ __forceinline__ float row_weight(int32_t target, int vocab, const float* d_logp) {
   return target < 0 ? 0.f : target >= vocab ? __builtin_nanf("") : *d_logp;
@@ -458,7 +527,7 @@ __global__ __launch_bounds__(1024) void head_stats_kernel(HeadRowsArgs a) {
   __shared__ float s_m[64][16], s_s[64][16];
   __shared__ uint32_t s_x[16];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, quarter = threadIdx.x >> 4;
-  const int row = blockIdx.x * 16 + (lane & 15), n = (a.vocab + a.pair_cols - 1) / a.pair_cols;
+  const int row = blockIdx.x * 16 + (lane & 15), pair_cols = a.plain_cols && a.range->plain ? a.plain_cols : a.pair_cols, n = (a.vocab + pair_cols - 1) / pair_cols;
   constexpr int AHEAD = 4;
   typedef float f32x2 __attribute__((ext_vector_type(2)));
   float m = LOWEST, s = 0.f;
@@ -480,7 +549,8 @@ __global__ __launch_bounds__(1024) void head_stats_kernel(HeadRowsArgs a) {
   }
   s_m[quarter][lane & 15] = m;
   s_s[quarter][lane & 15] = s;
-  if (a.range && blockIdx.x * 16 + wave < a.rows) {  // (a row a wave)
+  const bool exponents = a.range && a.d_logp;
+  if (exponents && blockIdx.x * 16 + wave < a.rows) {  // (a row a wave)
     const uint32_t most = row_largest(a.x, blockIdx.x * 16 + wave, a.d, a.x16_lo == nullptr);
     if (lane == 0) s_x[wave] = most;
   }
@@ -502,7 +572,7 @@ __global__ __launch_bounds__(1024) void head_stats_kernel(HeadRowsArgs a) {
   put_row(a, row, target, a.at_target[row], top, log_sum);
   a.off[2 * row] = top;
   a.off[2 * row + 1] = log2_sum;
-  if (a.range)
+  if (exponents)
     a.exponents[row] = row_exponent(a.range, row, row_weight(target, a.vocab, a.d_logp + row), probability(a.at_target[row], top, log2_sum), s_x[lane]);
 }
 
@@ -546,9 +616,11 @@ __global__ __launch_bounds__(256) void head_grad_kernel(HeadRowsArgs a, int segs
                       __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(a.logits + at + 4))};
   bf16x8 g, rest;
   f16x8 hi, lo;
+  f32x4 plain[2];
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     const float x = grad_of(v[e >> 2][e & 3], top, log2_sum, w, target, c + e, a.vocab), scaled = times_2(x, exponent);
+    plain[e >> 2][e & 3] = x;
     g[e] = (bf16_t)x;
     rest[e] = (bf16_t)(x - (float)g[e]);
     hi[e] = (f16_t)scaled;
@@ -557,6 +629,10 @@ __global__ __launch_bounds__(256) void head_grad_kernel(HeadRowsArgs a, int segs
   if (a.g) {
     *reinterpret_cast<bf16x8*>(a.g + at) = g;
     *reinterpret_cast<bf16x8*>(a.g_rest + at) = rest;
+  }
+  if (a.plain_cols && a.range->plain) {  // (for dX, in the logits' place)
+    *reinterpret_cast<f32x4*>(a.logits + at) = plain[0];
+    *reinterpret_cast<f32x4*>(a.logits + at + 4) = plain[1];
   }
   if (a.hi) {
     *reinterpret_cast<f16x8*>(a.hi + at) = hi;
@@ -593,7 +669,7 @@ struct HeadJoinArgs {
   const int32_t* exponents;  // of G's rows, and of W, by which the slabs are too large; or null
   const HeadRange* range;
   int64_t stride, rest;    // from part to part; to the rows of G's second numbers, or 0
-  int32_t parts, d;
+  int32_t parts, plain_parts, d;  // plain_parts: where the product is in float32
 };
 template <typename T, bool SHARED>
 __global__ __launch_bounds__(256) void head_join_kernel(HeadJoinArgs a, T* dX) {
@@ -602,7 +678,9 @@ __global__ __launch_bounds__(256) void head_join_kernel(HeadJoinArgs a, T* dX) {
   const int row = blockIdx.x, c = SHARED ? blockIdx.y * 256 + lane * 4 : blockIdx.y * 1024 + threadIdx.x * 4;
   if (!SHARED && c >= a.d) return;
   const int64_t i = (int64_t)row * a.d + min(c, a.d - 4);
-  const int share = SHARED ? (a.parts + 3) / 4 : a.parts, first = SHARED ? wave * share : 0, end = min(first + share, a.parts);
+  const bool plain = a.exponents && a.range->plain;
+  const int parts = plain ? a.plain_parts : a.parts;
+  const int share = SHARED ? (parts + 3) / 4 : parts, first = SHARED ? wave * share : 0, end = min(first + share, parts);
   f32x4 s = {0.f, 0.f, 0.f, 0.f};
   for (int p = first; p < end; p += 8) {
     f32x4 v[8];
@@ -626,7 +704,7 @@ __global__ __launch_bounds__(256) void head_join_kernel(HeadJoinArgs a, T* dX) {
 #pragma unroll
     for (int w = 1; w < 4; ++w) s += s_part[w][lane];
   }
-  if (a.exponents) {
+  if (a.exponents && !plain) {
     const int by = -a.exponents[row] - a.range->w_exponent;
 #pragma unroll
     for (int e = 0; e < 4; ++e) s[e] = times_2(s[e], by);
@@ -902,7 +980,7 @@ HeadLayout layout_for(int64_t plans, int64_t rows, int64_t slab_cells, int32_t d
   w.range = at - sizeof(HeadRange);
   w.at_target = take((size_t)rows * (pairs ? 8 : 4));
   w.logits = take(grad ? cells * 4 : 0);
-  w.pairs = take(std::max(pair_cells(rows, d, vocab, wide) * 8, stream_pairs(std::min(rows, stream_rows(vocab)), vocab)));
+  w.pairs = take(std::max(pair_cells(rows, d, vocab, bf16) * 8, stream_pairs(std::min(rows, stream_rows(vocab)), vocab)));
   w.off = take((size_t)rows * 8);
   w.exponents = take(wide && grad ? (size_t)rows * 4 : 0);
   w.g = take(bf16 && grad ? 2 * cells * 2 : 0);
@@ -920,8 +998,11 @@ HeadLayout layout_for(int64_t plans, int64_t rows, int64_t slab_cells, int32_t d
 // of all batches of at most T rows of one kind: the most tables, rows of a piece, slabs
 size_t most_workspace(int64_t T, int32_t d, int32_t vocab, bool bf16, bool pairs, bool grad) {
   const bool wide = bf16 || pairs;
-  const int64_t most = most_rows(vocab, wide, grad), rows = std::min<int64_t>(padded_rows(T), most);
-  const int64_t plans = std::min<int64_t>((T + most - 1) / most, PLAN_PIECES) * (grad ? 3 : 1);
+  const int64_t most = most_rows(vocab, bf16, pairs, grad), rows = std::min<int64_t>(padded_rows(T), most);
+  HeadShape h = {};
+  h.pairs = pairs;
+  h.grad = grad;
+  const int64_t plans = std::min<int64_t>((T + most - 1) / most, PLAN_PIECES) * head_products(h);
   const int64_t dx_rows = bf16 ? std::max(rows, std::min(2 * rows, 2 * STACK_ROWS)) : rows;
   const int64_t dw_parts = dw_most_parts(d, vocab, wide);
   const int64_t slabs = std::max(std::min(MAX_PARTS * dx_rows * d, std::max(SLAB_CELLS, dx_rows * d)), dw_parts > 1 ? dw_parts * vocab * d : 0);
@@ -950,8 +1031,9 @@ hipError_t launch_head(modse_dtype dt, const HeadArgs& a, char* ws, hipStream_t 
     return dt == MODSE_F32 ? run_stream<float>(r, s) : run_stream<bf16_t>(r, s);
   }
   const HeadShape h = head_shape(a.T, a.d, a.vocab, dt, grad);
-  const int64_t plans = (int64_t)std::min(h.pieces, PLAN_PIECES) * (grad ? 3 : 1);
-  const int64_t slabs = std::max((int64_t)h.k_parts * h.dx_rows * h.d, h.w_split > 1 ? (int64_t)h.w_split * h.vocab * h.d : 0);
+  const HeadShape f = h.pairs ? head_shape(a.T, a.d, a.vocab, dt, grad, true) : HeadShape{};  // (pieces of the same rows)
+  const int64_t plans = (int64_t)std::min(h.pieces, PLAN_PIECES) * head_products(h);
+  const int64_t slabs = std::max((int64_t)std::max(h.k_parts, f.k_parts) * h.dx_rows * h.d, h.w_split > 1 ? (int64_t)h.w_split * h.vocab * h.d : 0);
   const HeadLayout w = layout_for(plans, h.rows, slabs, h.d, h.vocab, h.bf16, h.pairs, grad);
   ws = reinterpret_cast<char*>(align_up(reinterpret_cast<size_t>(ws), ALIGN));
   auto floats = [&](size_t at) { return reinterpret_cast<float*>(ws + at); };
@@ -960,45 +1042,46 @@ hipError_t launch_head(modse_dtype dt, const HeadArgs& a, char* ws, hipStream_t 
   const HeadBufs b = {reinterpret_cast<GemmPlan*>(ws), floats(w.logits), floats(w.pairs), floats(w.at_target), floats(w.off),
                       reinterpret_cast<bf16_t*>(ws + w.g), halves(w.hi), halves(w.lo), halves(w.x16), halves(w.x16_lo), reinterpret_cast<int32_t*>(ws + w.exponents),
                       halves(w.w16), halves(w.w16_lo), floats(w.x32), range, floats(w.slabs)};
-  const int64_t range_blocks = h.pairs ? std::min<int64_t>(((int64_t)h.vocab * h.d + 32767) / 32768, RANGE_BLOCKS) : 0;
-  auto make_plans = [&](int first) {  // returns how many pieces they are of
-    const int n = std::min(h.pieces - first, PLAN_PIECES), tables = n * (grad ? 3 : 1);
-    const HeadPlanArgs plan = {h, b, a.x, a.W, a.targets, a.d_logp, a.dW, first, n, tables};
-    hipLaunchKernelGGL(head_plan_kernel, dim3((unsigned)(tables + (first == 0 ? range_blocks : 0))), dim3(1024), 0, s, plan);
-    return n;
-  };
-  int planned = make_plans(0);
+  const int64_t w_cells = (int64_t)h.vocab * h.d;
+  const int range_blocks = h.pairs ? (int)std::min<int64_t>((w_cells + 32767) / 32768, RANGE_BLOCKS) : 0;
   if (h.pairs) {
-    const int64_t n = (int64_t)h.vocab * h.d;
-    hipLaunchKernelGGL(head_split_w_kernel, dim3((unsigned)std::min<int64_t>((n + 2047) / 2048, 2048)), dim3(256), 0, s,
-                       static_cast<const float*>(a.W), n, b.w16, b.w16_lo, range);
+    hipLaunchKernelGGL(head_range_kernel, dim3(range_blocks), dim3(1024), 0, s, static_cast<const u32x4*>(a.W), w_cells / 4, range);
+    hipLaunchKernelGGL(head_split_w_kernel, dim3((unsigned)std::min<int64_t>((w_cells + 2047) / 2048, 2048)), dim3(256), 0, s,
+                       static_cast<const float*>(a.W), w_cells, b.w16, b.w16_lo, range, range_blocks);
   }
+  const bool stream = h.T <= stream_rows(h.vocab) && h.pieces == 1;  // (only with gradients here)
+  int planned = 0;  // pieces that there are tables of
+  auto begin = [&](int64_t piece, int64_t t0, int64_t m) {
+    const int first = (int)piece, n = piece % PLAN_PIECES ? 0 : std::min(h.pieces - first, PLAN_PIECES), tables = n * head_products(h);
+    if (n) planned = n;
+    int lanes = 64;
+    while (lanes > 2 && lanes / 2 >= h.d / 8) lanes /= 2;
+    const int64_t x_blocks = h.pairs && !stream ? (m * lanes + 255) / 256 : 0;
+    const HeadPlanArgs plan = {h, b, a.x, a.W, a.targets, a.d_logp, a.dW, f, first, n, tables, (int32_t)t0, (int32_t)m, range_blocks};
+    if (tables + x_blocks) hipLaunchKernelGGL(head_plan_kernel, dim3((unsigned)(tables + x_blocks)), dim3(256), 0, s, plan);
+  };
   auto tiles_of = [](int64_t m, int64_t n, TileShape t) { return tiles(m, n, t.bm); };
   hipError_t e = hipGetLastError();
   // the logits of a piece, their sums and (of gradients) G
-  auto logits = [&](const GemmPlan* plan, int64_t t0, int64_t m) {
-    const bool stream = h.T <= stream_rows(h.vocab) && h.pieces == 1;  // (only with gradients here)
-    if (h.pairs) {
-      int lanes = 64;
-      while (lanes > 2 && lanes / 2 >= h.d / 8) lanes /= 2;
-      hipLaunchKernelGGL(head_split_x_kernel, dim3((unsigned)((m * lanes + 255) / 256)), dim3(256), 0, s, static_cast<const float*>(a.x) + t0 * h.d,
-                         (int)m, h.d, b.x16, b.x16_lo, b.at_target + h.rows);
-    }
+  auto table = [&](int product, int at) { return b.plans + head_table(h, product) * planned + at; };
+  auto logits = [&](int at, int64_t t0, int64_t m) {
     if (stream) {
       const HeadStreamArgs r = {a.x, a.W, a.targets, b.pairs, b.at_target, a.logp, nullptr, b.logits, b.off, range, b.exponents, a.d_logp,
                                 (int32_t)m, h.d, h.vocab, h.ldv};
       e = h.bf16 ? run_stream<bf16_t>(r, s) : run_stream<float>(r, s);
     } else {
-      e = launch_grouped_gemm(dt, h.pairs ? EPI_LOGITS_PAIRS : EPI_LOGITS, h.logits_tile, plan, h.w_parts, 0,
-                              h.logits_tile.bm < 256 ? GEMM_SPREAD_K : GEMM_STREAM_C, tiles_of(m, h.vocab, h.logits_tile) + h.w_parts * tiles_of(m, 1, h.logits_tile), s, LAYOUT_TN);
+      auto most_tiles = [&](const HeadShape& p) { return tiles_of(m, p.vocab, p.logits_tile) + p.w_parts * tiles_of(m, 1, p.logits_tile); };
+      e = launch_grouped_gemm(dt, h.pairs ? EPI_LOGITS_PAIRS : EPI_LOGITS, h.logits_tile, table(LOGITS, at), h.w_parts, 0,
+                              h.logits_tile.bm < 256 ? GEMM_SPREAD_K : GEMM_STREAM_C, most_tiles(h), s, LAYOUT_TN);
+      if (e == hipSuccess && h.pairs) e = launch_rare_gemm(EPI_LOGITS, table(PLAIN_LOGITS, at), f.w_parts, most_tiles(f), s);
     }
     if (e != hipSuccess) return;
     const HeadRowsArgs r = {a.targets + t0, a.d_logp ? a.d_logp + t0 : nullptr, a.logp ? a.logp + t0 : nullptr, a.log_z ? a.log_z + t0 : nullptr,
                             b.logits, b.pairs, b.at_target, b.off, a.dX && h.bf16 ? b.g : nullptr, a.dX && h.bf16 ? b.g + (int64_t)h.rows * h.ldv : nullptr,
-                            a.dW || h.pairs ? b.hi : nullptr, a.dW || h.pairs ? b.lo : nullptr, grad ? range : nullptr, b.exponents,
+                            a.dW || h.pairs ? b.hi : nullptr, a.dW || h.pairs ? b.lo : nullptr, range, b.exponents,
                             static_cast<const char*>(a.x) + (size_t)t0 * h.d * (h.bf16 ? 2 : 4), b.x16, h.pairs ? b.x16_lo : nullptr,
                             a.dW && !h.wide ? b.x32 : nullptr,
-                            (int32_t)m, h.vocab, h.ldv, h.rows, h.pair_cols(), h.d};
+                            (int32_t)m, h.vocab, h.ldv, h.rows, h.pair_cols(), h.pairs ? f.pair_cols() : 0, h.d};
     if (!stream) hipLaunchKernelGGL(head_stats_kernel, dim3((unsigned)((m + 15) / 16)), dim3(1024), 0, s, r);
     if (grad) {
       const int64_t segs = (h.ldv + 2047) / 2048, copies = a.dW && h.wide ? (m * h.d + 2047) / 2048 : 0;
@@ -1011,13 +1094,12 @@ hipError_t launch_head(modse_dtype dt, const HeadArgs& a, char* ws, hipStream_t 
   for (int64_t piece = 0; piece < h.pieces && e == hipSuccess; ++piece) {
     const int64_t t0 = piece * h.rows, m = std::min<int64_t>(h.rows, h.T - t0);
     const int at = (int)(piece % PLAN_PIECES);
-    if (at == 0 && piece > 0) planned = make_plans((int)piece);
-    logits(b.plans + at, t0, m);
+    begin(piece, t0, m);
+    logits(at, t0, m);
     if (e != hipSuccess || !grad) continue;
-    const GemmPlan* const p = b.plans + planned + 2 * at;
     if (a.dW) {  // (before dX, which may lie in the buffer of x)
       const int accumulate = a.accumulate || piece > 0;
-      e = launch_grouped_gemm(dt, h.pairs ? EPI_ROWS_PAIRS : EPI_ROWS_F32, h.dw_tile, p + 1, h.w_split, h.w_split > 1 ? 0 : accumulate, 0,
+      e = launch_grouped_gemm(dt, h.pairs ? EPI_ROWS_PAIRS : EPI_ROWS_F32, h.dw_tile, table(DW, at), h.w_split, h.w_split > 1 ? 0 : accumulate, 0,
                               h.w_split * tiles_of(padded_rows(h.vocab), h.d, h.dw_tile), s, LAYOUT_AB_K);
       if (e == hipSuccess && h.w_split > 1) {
         const int64_t n = (int64_t)h.vocab * h.d;
@@ -1028,11 +1110,13 @@ hipError_t launch_head(modse_dtype dt, const HeadArgs& a, char* ws, hipStream_t 
     }
     if (a.dX) {
       const bool stacked = h.dx_rows > h.rows;
-      e = launch_grouped_gemm(dt, h.pairs ? EPI_STORE_PAIRS : h.bf16 && !stacked ? EPI_STORE_DUALK_F32 : EPI_STORE_F32, h.dx_tile, p, h.k_parts, 0, 0,
-                              h.k_parts * tiles_of(stacked ? h.dx_rows : m, h.d, h.dx_tile), s, LAYOUT_B_KN);
+      e = launch_grouped_gemm(dt, h.pairs ? EPI_STORE_PAIRS : h.bf16 && !stacked ? EPI_STORE_DUALK_F32 : EPI_STORE_F32, h.dx_tile,
+                              table(DX, at), h.k_parts, 0, 0, h.k_parts * tiles_of(stacked ? h.dx_rows : m, h.d, h.dx_tile), s, LAYOUT_B_KN);
+      if (e == hipSuccess && h.pairs)
+        e = launch_rare_gemm(EPI_STORE_F32, table(PLAIN_DX, at), f.k_parts, f.k_parts * tiles_of(m, h.d, f.dx_tile), s);
       if (e != hipSuccess) break;
       const HeadJoinArgs j = {b.slabs, h.pairs ? b.exponents : nullptr, range, (int64_t)h.dx_rows * h.d, stacked ? (int64_t)h.rows * h.d : 0,
-                              h.k_parts, h.d};
+                              h.k_parts, f.k_parts, h.d};
       e = h.bf16 ? run_join(j, m, static_cast<bf16_t*>(a.dX) + t0 * h.d, s) : run_join(j, m, static_cast<float*>(a.dX) + t0 * h.d, s);
     }
   }

@@ -1,8 +1,9 @@
 """A language model of one MoDSE layer, trained and asked for its next tokens with this library's operators: the norm in front of
 the layer and in front of the logits (modse_norm_*), the layer (modse_layer_*), the loss, its gradient and the alternatives of the next
 token (modse_logprobs_*), and the orthogonalised update of the expert matrices (modse_orthogonalize).  PyTorch holds the memory, looks up
-embeddings and multiplies by the output matrix; with --ends the library does that, too (modse_embed_*, modse_head_*), without the logits
-of a batch, and with --dropout P, which goes with it, a share P of the layer's output is dropped in training (modse_dropout_*).
+embeddings and multiplies by the output matrix; with --ends the library looks up embeddings, too (modse_embed_*), and in training multiplies by
+the output matrix (modse_head_*), without the logits of a batch (the alternatives still come from logits); with --dropout P, which goes with it, a
+share P of the layer's output is dropped in training (modse_dropout_*).
 
     python examples/tiny_lm.py [--dtype bf16] [--steps 60] [--ends [--dropout 0.1]]
 
@@ -162,7 +163,7 @@ def main():
     p = argparse.ArgumentParser(description=__doc__.split("\n")[0])
     p.add_argument("--dtype", choices=("bf16", "f32"), default="bf16")
     p.add_argument("--steps", type=int, default=60)
-    p.add_argument("--ends", action="store_true", help="embedding, output matrix and loss by the library, too")
+    p.add_argument("--ends", action="store_true", help="lookup of embeddings, and in training output matrix and loss, by the library, too")
     p.add_argument("--dropout", type=float, default=0.0, help="share of the layer's output that is dropped in training (with --ends)")
     a = p.parse_args()
     model, gen = TinyLM(dtype=a.dtype, ends=a.ends, dropout=a.dropout), torch.Generator(device="cuda").manual_seed(1)

@@ -328,7 +328,7 @@ modse_status modse_embed_bwd(int64_t T, int32_t d_model, int32_t vocab, modse_dt
                              float scale, float* dE, int accumulate, void* ws, size_t ws_bytes, void* hip_stream);
 
 /* Log probabilities from the last hidden rows: logits l = x W^T, of which a
- * workspace holds a piece at a time: it stops growing with T (some GiB for gradients).
+ * workspace holds a piece at a time: it stops growing with T (at 3 to 10 GiB for gradients).
  *   x        [T, d_model] of `dtype` (d_model a multiple of 32 up to 16384; T up to 2^24)
  *   W        [vocab, d_model] of `dtype`, the output matrix (vocab 1..2^20)
  *   targets  [T] int32.  Negative: no target, logp 0 and no gradient, whatever stands in

@@ -92,7 +92,8 @@ def load_library():
     lib.modse_head_workspace_size.argtypes = [i64, i32, i32, C.c_int, C.c_int, szp]
     lib.modse_head_fwd.argtypes = [i64, i32, i32, C.c_int, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.modse_head_bwd.argtypes = [i64, i32, i32, C.c_int, vp, vp, vp, vp, vp, vp, vp, C.c_int, vp, sz, vp]
-    for name in ("modse_head_workspace_size", "modse_head_fwd", "modse_head_bwd", "modse_embed_fwd", "modse_embed_bwd_workspace_size", "modse_embed_bwd", "modse_dropout_fwd", "modse_dropout_bwd",
+    for name in ("modse_head_workspace_size", "modse_head_fwd", "modse_head_bwd", "modse_embed_fwd", "modse_embed_bwd_workspace_size",
+                 "modse_embed_bwd", "modse_dropout_fwd", "modse_dropout_bwd",
                  "modse_norm_fwd", "modse_norm_bwd_workspace_size", "modse_norm_bwd", "modse_logprobs_workspace_size",
                  "modse_logprobs_fwd", "modse_logprobs_bwd", "modse_orthogonalize_workspace_size", "modse_orthogonalize",
                  "modse_workspace_size", "modse_saved_size", "modse_route", "modse_layer_fwd", "modse_layer_bwd",

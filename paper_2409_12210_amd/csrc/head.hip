@@ -15,11 +15,11 @@
 // float32 from some hundred rows on: x, W and G are held as the sums of two float16 matrices, hi + lo, times powers of two (see HeadRange)
 // that bring the largest value below 2^15.  Three products of float16 matrices, hi hi' + hi lo' + lo hi', in one accumulator leave
 // out 2^-22 of a product; they take 3 of the 16-bit matrix rate where float32 instructions take 16 (1021 x 256 x 50257 with gradients:
-// 445 us in place of 731).  Fewer rows, or a W of more than 2^28 elements: products in float32, and G in the place of the logits.  Where the device finds
+// 450 us in place of 731).  Fewer rows, or a W of more than 2^28 elements: products in float32, and G in the place of the logits.  Where the device finds
 // values in W that its parts would lose, the products with W are in float32, too: by a second list of tiles, of which one is empty.
 //
 // Up to 64 rows (small vocabularies: more) a stream over W makes the logits, see "few rows".  dW of a small vocabulary has few tiles,
-// so its sum over the tokens is cut into parts as well (float32, 1000 x 512, 4096 rows: with the stream 160 us in place of 337 for the whole call).
+// so its sum over the tokens is cut into parts as well (float32, 1000 x 512, 4096 rows: with the stream 150 us in place of 337 for the whole call).
 //
 // dX of a bf16 layer takes G as the sum of two bf16 numbers, which hold 16 bits, in two passes over W; what they lose lies below the rounding
 // of the result.  (One number, with what it loses of the target's entry put back in float32: 2 T V d operations less, but where another token
@@ -59,7 +59,7 @@ struct HeadShape {
   int32_t w_split, w_len;  // problems of dW, rows in each
   int32_t bf16, grad;
   int32_t pairs;           // float32, and the matrices are held as pairs of float16 ones
-  int32_t wide;            // either of them: tiles of 256, sums of exponentials by the product of the logits
+  int32_t wide;            // either of them: 16-bit products, tiles of 256 or 128
   TileShape logits_tile, dx_tile, dw_tile;
   __host__ __device__ int pair_cols() const { return logits_tile.bn / 2; }  // columns of a pair of maximum and sum
 };
@@ -96,16 +96,16 @@ int64_t tiles(int64_t m, int64_t n, int b) { return ((m + b - 1) / b) * ((n + b 
 // 16-bit products: the logits take tiles of 128, two of which share a CU, where tiles of 256 are few or a tile is but a few steps of K.  Tiles of
 // 256 / 128, us: 128 rows with 32000 x 2048 54 / 36, 131072 x 128 41 / 22; 229 rows with 32000 x 2048 55 / 51, 50257 x 2048 69 / 88, 131072 x
 // 128 35 / 30; 512 rows with 32000 x 1024 44 / 53, 131072 x 512 86 / 88, 50257 x 256 38 / 33, 4096 rows 177 / 157; with gradients 512
-// rows x 50257 x 256 198 / 182, 2048 rows 541 / 562.  Float32 by pairs, gradients: 300 rows with 8000 x 1024 205 / 173, 1021 rows 275 / 256, 2048
-// rows 374 / 404, 1021 rows with 50257 x 256 473 / 446, 2048 rows 780 / 776, scored 4096 rows 403 / 440.
+// rows x 50257 x 256 221 / 210, 2048 rows 631 / 642.  Float32 by pairs, gradients: 300 rows with 8000 x 1024 202 / 171, 1021 rows 275 / 257, 2048
+// rows 372 / 399, 1021 rows with 50257 x 256 478 / 449, 2048 rows 768 / 768, scored 4096 rows 415 / 443.
 constexpr int64_t BLOCK_ROWS = 256, BLOCK_ROWS_MOST = 1024, FEW_TILES = 128;
 bool logits_take_blocks(int64_t T, int32_t d, int32_t vocab, bool all_rows) {
   return T <= 128 || tiles(T, vocab, 256) <= FEW_TILES || (d <= 256 && (all_rows || T <= BLOCK_ROWS_MOST));
 }
-// dX takes them up to 256 rows, and with short rows up to 1024 (one row with 32000 x 2048 167 / 137, 50257 x 256 78 / 56; 229 rows 257 / 253, 132 / 112;
-// 512 rows 351 / 371, 180 / 166; float32, 512 rows with 32000 x 512 297 / 276, 1021 rows 424 / 478, 512 rows with 32000 x 2048 774 / 865), dW
-// of bf16 layers up to 64 rows and where tiles of 256 do not fill the chip and are a few steps of K each: one row with 32000 x 2048 167 / 149, 128 rows
-// with 131072 x 512 279 / 295; 1024 rows with 1000 x 1024 93 / 75, 4000 x 512 117 / 116, 8000 x 1024 167 / 184.
+// dX takes them up to 256 rows, and with short rows up to 1024 (one row with 32000 x 2048 167 / 137, 50257 x 256 78 / 56; 229 rows 287 / 292, 140 / 122;
+// 512 rows 405 / 464, 217 / 204; float32, 512 rows with 32000 x 512 302 / 278, 1021 rows 427 / 482, 512 rows with 32000 x 2048 745 / 862), dW
+// of bf16 layers up to 64 rows and where tiles of 256 do not fill the chip and are a few steps of K each: one row with 32000 x 2048 135 / 122, 128 rows
+// with 131072 x 512 252 / 267; 1024 rows with 1000 x 1024 97 / 80, 4000 x 512 105 / 98, 8000 x 1024 168 / 178.
 bool dx_takes_blocks(int64_t T, int32_t d, bool pairs) {
   return pairs ? T <= 512 && d <= 512 : T <= BLOCK_ROWS || (d <= 256 && T <= BLOCK_ROWS_MOST);
 }
